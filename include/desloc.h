@@ -364,6 +364,97 @@ DESLOC_API int desloc_step_static(const desloc_config *cfg, float *const *x, flo
                                   float lr_t, float clip_bound_t, int cuda_device, void *stream,
                                   uint32_t *mask_out);
 
+/*
+ * Around the step: what a program that trains language models with M workers does between the tokens and the gradients that
+ * desloc_step() reads -- embeddings looked up in the workers' replicas and their gradient, log probabilities of given tokens (the
+ * perplexity by which the paper compares its runs is exp of their mean, negated) and their gradient, and norm-based clipping of
+ * gradients on its own.
+ *
+ * All take a stream, only enqueue work and can be captured; the same inputs give the same bits.  Outputs may not overlap inputs, or
+ * one another, except where it says so.  Working memory is the caller's: what one call uses must not be used by another that may
+ * run at the same time (calls on one stream, one after the other, may share it), and a captured call needs its working memory for as
+ * long as the graph is replayed.  Sums are held in fp32 or more and rounded once, to the nearest, at the end.
+ */
+
+/* Types of token numbers. */
+typedef enum { DESLOC_I32 = 0, DESLOC_I64 = 1 } desloc_index_t;
+
+/* Rows in device memory: row (i, j) begins i*stride[0] + j*stride[1] elements behind `data`, its own elements follow one another.  For
+   tokens a row is one element.  `data` lies on a boundary of its type (DESLOC_E_INVALID); any other alignment will do. */
+typedef struct {
+    void *data;
+    int32_t dtype;     /* desloc_dtype_t; desloc_index_t for tokens */
+    int64_t stride[2]; /* in elements; rows that are written do not overlap */
+} desloc_rows;
+
+/*
+ * Embedding of n tokens per worker: row (m, i) of `out` := scale * row token(m, i) of worker m's x of tensor `tensor`, which is
+ * taken as rows of `width` elements; zeros where the token is outside [0, numel[tensor] / width).
+ *   tokens : element (m, i) = token i of worker m, i < n.       out : row (m, i), fp32 or bf16.
+ * DESLOC_E_RANGE: tensor, width (up to 2^20; it must divide numel[tensor], into at most 2^30 rows), n < 0 or > 2^30, a scale that is not finite.
+ */
+DESLOC_API int desloc_embed(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows *tokens, int64_t n, float scale,
+                            const desloc_rows *out, void *stream);
+
+/*
+ * Its gradient, in the place of worker m's gradient of that tensor and in cfg.grad_dtype, as the step calls read it:
+ *   row v := scale * sum of the rows (m, i) of `dout` with token(m, i) = v;
+ * zeros where there are none -- or, where `accumulate` is not 0, added to what the row holds, and rows without a token are left as they are
+ * (the gradient of an output head with the same weights is there already).  Rows of tokens outside the vocabulary are not read.
+ *   dout  : row (m, i), fp32 or bf16.
+ *   grads : host array of M*num_tensors DEVICE pointers, as for desloc_step(); only those of `tensor` are read.
+ *   work, work_bytes : device memory, 256-byte aligned, of desloc_embed_grad_bytes() bytes at least (DESLOC_E_RANGE where it is less).
+ */
+DESLOC_API int desloc_embed_grad(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows *tokens, int64_t n,
+                                 const desloc_rows *dout, float scale, int32_t accumulate, void *const *grads, void *work,
+                                 int64_t work_bytes, void *stream);
+DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor, int64_t width, int64_t n);
+
+/*
+ * Norm-based clipping on its own: out^m := f_m g^m over all tensors, f_m = min(1, max_norm / ||g^m||_2), per worker -- what
+ * desloc_step_normclip() does on the way into its step, for gradients that go elsewhere (desloc_step_host(), desloc_step_masked(),
+ * desloc_step_static(), a captured window, a log), or that were accumulated in fp32 and are handed to the step as bf16.
+ *   grads, grads_dtype : host array of M*num_tensors DEVICE pointers, fp32 or bf16.
+ *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.
+ *   norms, factors     : device, [M] floats each, or NULL.
+ *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
+ * max_norm must be > 0 and finite.  A norm that is not finite says that the gradients are not (or that their squares left fp32's range,
+ * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  Norms and factors are those that desloc_step_normclip() uses.
+ */
+DESLOC_API int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, const void *const *grads, int32_t out_dtype,
+                                 void *const *out, float *norms, float *factors, void *work, int64_t work_bytes, void *stream);
+DESLOC_API int64_t desloc_clip_grads_bytes(const desloc_ctx *ctx);
+
+/*
+ * Log probabilities of given tokens: for each of outer * inner rows x of `vocab` logits (of M workers: outer = M, inner = the tokens
+ * of a worker), with lse = log sum_j exp x_j and p_j = exp(x_j - lse),
+ *   logp     : x_token - lse; 0 where the token is outside [0, vocab).  (Everything else does not depend on the token.)
+ *   lse      : as it says.
+ *   entropy  : -sum_j p_j log p_j, or NULL.
+ *   top_ids, top_logp : [rows][top], numbers and log probabilities of the `top` (<= DESLOC_MAX_TOP; 0: NULL) largest logits, the largest
+ *              first, the lowest number first among equals.  Logits of -inf and NaN are never among them; places left over hold -1 and -inf.
+ * Results are dense, row (i, j) at i * inner + j.  Logits of -inf have probability 0.  A row of nothing but -inf has lse -inf, logp -inf
+ * and entropy 0; one that holds NaN or +inf has NaN in all of them but the numbers.
+ * No context: any device and stream.  DESLOC_E_RANGE for sizes out of range (vocab up to 2^30, outer * inner up to 2^28).
+ */
+#define DESLOC_MAX_TOP 32
+DESLOC_API int desloc_token_logprobs(int64_t outer, int64_t inner, int64_t vocab, const desloc_rows *logits, const desloc_rows *tokens,
+                                     int32_t top, float *logp, float *lse, float *entropy, int64_t *top_ids, float *top_logp,
+                                     int cuda_device, void *stream);
+
+/*
+ * The gradient of sum_r dlogp_r logp_r + dentropy_r entropy_r with respect to the logits:
+ *   out_j := dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy),
+ * the first part 0 where the token is outside [0, vocab).  A row whose two weights are 0 (or that has no token and no dentropy) gets zeros,
+ * whatever its logits hold, and so does one of nothing but -inf.
+ *   lse, entropy : of desloc_token_logprobs(), dense fp32.      dlogp, dentropy : dense fp32, any may hold 0.
+ *   dentropy     : or NULL; entropy is needed with it only.
+ *   out          : rows of the logits' type; may be the logits themselves.
+ */
+DESLOC_API int desloc_token_logprobs_grad(int64_t outer, int64_t inner, int64_t vocab, const desloc_rows *logits,
+                                          const desloc_rows *tokens, const float *lse, const float *dlogp, const float *entropy,
+                                          const float *dentropy, const desloc_rows *out, int cuda_device, void *stream);
+
 /* Static description of a status code; never NULL. */
 DESLOC_API const char *desloc_strerror(int status);
 

@@ -24,6 +24,8 @@ DESLOC_E_TOO_LARGE = -6
 DESLOC_E_DEVICE_WAIT = -7
 DESLOC_STATIC_MAX_POINTERS, DESLOC_STATIC_MAX_CHUNKS = 2048, 32768
 DESLOC_MAX_M = 256
+DESLOC_I32, DESLOC_I64 = 0, 1
+DESLOC_MAX_TOP = 32
 
 OPT_BY_NAME = {"adam": DESLOC_ADAM, "adopt": DESLOC_ADOPT, "sgdm": DESLOC_SGDM}
 DTYPE_BY_NAME = {"f32": DESLOC_F32, "bf16": DESLOC_BF16}
@@ -47,6 +49,15 @@ class DeslocConfig(ctypes.Structure):
         ("Kv", ctypes.c_int32),
         ("flags", ctypes.c_uint32),
     ]
+
+
+class DeslocRows(ctypes.Structure):
+    """Mirror of ``desloc_rows``: rows (i, j) at data + i * stride[0] + j * stride[1] elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("dtype", ctypes.c_int32), ("stride", ctypes.c_int64 * 2)]
+
+
+def rows(data: int, dtype: int, stride0: int, stride1: int) -> DeslocRows:
+    return DeslocRows(data or None, dtype, (ctypes.c_int64 * 2)(stride0, stride1))
 
 
 class DeslocError(RuntimeError):
@@ -126,6 +137,22 @@ _lib.desloc_plan_chunks_at.argtypes = [ctypes.POINTER(ctypes.c_int64), ctypes.c_
                                        ctypes.POINTER(ctypes.c_int64), ctypes.c_int64]
 _lib.desloc_chunk_elems.restype = ctypes.c_int64
 _lib.desloc_chunk_elems.argtypes = [ctypes.POINTER(DeslocConfig)]
+_I32, _I64, _F = ctypes.c_int32, ctypes.c_int64, ctypes.c_float
+_ROWS = ctypes.POINTER(DeslocRows)
+_lib.desloc_embed.restype = ctypes.c_int
+_lib.desloc_embed.argtypes = [_P, _I32, _I64, _ROWS, _I64, _F, _ROWS, _P]
+_lib.desloc_embed_grad.restype = ctypes.c_int
+_lib.desloc_embed_grad.argtypes = [_P, _I32, _I64, _ROWS, _I64, _ROWS, _F, _I32, _PP, _P, _I64, _P]
+_lib.desloc_embed_grad_bytes.restype = _I64
+_lib.desloc_embed_grad_bytes.argtypes = [_P, _I32, _I64, _I64]
+_lib.desloc_clip_grads.restype = ctypes.c_int
+_lib.desloc_clip_grads.argtypes = [_P, _F, _I32, _PP, _I32, _PP, _P, _P, _P, _I64, _P]
+_lib.desloc_clip_grads_bytes.restype = _I64
+_lib.desloc_clip_grads_bytes.argtypes = [_P]
+_lib.desloc_token_logprobs.restype = ctypes.c_int
+_lib.desloc_token_logprobs.argtypes = [_I64, _I64, _I64, _ROWS, _ROWS, _I32, _P, _P, _P, _P, _P, ctypes.c_int, _P]
+_lib.desloc_token_logprobs_grad.restype = ctypes.c_int
+_lib.desloc_token_logprobs_grad.argtypes = [_I64, _I64, _I64, _ROWS, _ROWS, _P, _P, _P, _P, _ROWS, ctypes.c_int, _P]
 _lib.desloc_strerror.restype = ctypes.c_char_p
 _lib.desloc_strerror.argtypes = [ctypes.c_int]
 _lib.desloc_last_cuda_error.restype = ctypes.c_int
@@ -282,6 +309,67 @@ def desloc_rel_change(ctx: int, array: int, then: Sequence[int], M: int, stream:
     if rc != DESLOC_OK:
         raise DeslocError(rc, "desloc_rel_change", _lib.desloc_last_cuda_error(ctx))
     return list(out)
+
+
+def desloc_embed(ctx: int, tensor: int, width: int, tokens: DeslocRows, n: int, scale: float, out: DeslocRows, stream: int = 0) -> None:
+    """Embedding of n tokens per worker from the workers' x of `tensor`."""
+    rc = _lib.desloc_embed(ctx, int(tensor), int(width), tokens, int(n), float(scale), out, stream or None)
+    if rc != DESLOC_OK:
+        raise DeslocError(rc, "desloc_embed", _lib.desloc_last_cuda_error(ctx))
+
+
+def desloc_embed_grad_bytes(ctx: int, tensor: int, width: int, n: int) -> int:
+    """Bytes of working memory that desloc_embed_grad() needs."""
+    r = int(_lib.desloc_embed_grad_bytes(ctx, int(tensor), int(width), int(n)))
+    if r < 0:
+        raise DeslocError(r, "desloc_embed_grad_bytes")
+    return r
+
+
+def desloc_embed_grad(ctx: int, tensor: int, width: int, tokens: DeslocRows, n: int, dout: DeslocRows, scale: float, accumulate: bool,
+                      grads, work: int, work_bytes: int, stream: int = 0) -> None:
+    """The embedding's gradient in the place of every worker's gradient of `tensor`."""
+    g = grads if isinstance(grads, ctypes.Array) else _ptr_array(grads)
+    rc = _lib.desloc_embed_grad(ctx, int(tensor), int(width), tokens, int(n), dout, float(scale), int(bool(accumulate)), g, work or None,
+                                int(work_bytes), stream or None)
+    if rc != DESLOC_OK:
+        raise DeslocError(rc, "desloc_embed_grad", _lib.desloc_last_cuda_error(ctx))
+
+
+def desloc_clip_grads_bytes(ctx: int) -> int:
+    """Bytes of working memory that desloc_clip_grads() needs."""
+    r = int(_lib.desloc_clip_grads_bytes(ctx))
+    if r < 0:
+        raise DeslocError(r, "desloc_clip_grads_bytes")
+    return r
+
+
+def desloc_clip_grads(ctx: int, max_norm: float, grads_dtype: int, grads, out_dtype: int, out, norms: int, factors: int, work: int,
+                      work_bytes: int, stream: int = 0) -> None:
+    """Every worker's gradients scaled to a norm of at most max_norm; norms, factors: device addresses of [M] floats, or 0."""
+    as_arr = lambda a: a if isinstance(a, ctypes.Array) else _ptr_array(a)
+    rc = _lib.desloc_clip_grads(ctx, float(max_norm), int(grads_dtype), as_arr(grads), int(out_dtype), as_arr(out), norms or None,
+                                factors or None, work or None, int(work_bytes), stream or None)
+    if rc != DESLOC_OK:
+        raise DeslocError(rc, "desloc_clip_grads", _lib.desloc_last_cuda_error(ctx))
+
+
+def desloc_token_logprobs(outer: int, inner: int, vocab: int, logits: DeslocRows, tokens: DeslocRows, top: int, logp: int, lse: int,
+                          entropy: int, top_ids: int, top_logp: int, cuda_device: int, stream: int = 0) -> None:
+    """Log probabilities of given tokens; logp, lse, entropy, top_ids, top_logp are device addresses (0: not asked for)."""
+    rc = _lib.desloc_token_logprobs(int(outer), int(inner), int(vocab), logits, tokens, int(top), logp or None, lse or None,
+                                    entropy or None, top_ids or None, top_logp or None, int(cuda_device), stream or None)
+    if rc != DESLOC_OK:
+        raise DeslocError(rc, "desloc_token_logprobs")
+
+
+def desloc_token_logprobs_grad(outer: int, inner: int, vocab: int, logits: DeslocRows, tokens: DeslocRows, lse: int, dlogp: int,
+                               entropy: int, dentropy: int, out: DeslocRows, cuda_device: int, stream: int = 0) -> None:
+    """Gradient of the weighted sum of log probabilities (and entropies) with respect to the logits."""
+    rc = _lib.desloc_token_logprobs_grad(int(outer), int(inner), int(vocab), logits, tokens, lse or None, dlogp or None, entropy or None,
+                                         dentropy or None, out, int(cuda_device), stream or None)
+    if rc != DESLOC_OK:
+        raise DeslocError(rc, "desloc_token_logprobs_grad")
 
 
 def desloc_set_workers(ctx: int, M_new: int, first_new: int, x, u, v, stream: int = 0) -> None:

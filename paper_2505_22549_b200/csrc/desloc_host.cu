@@ -18,6 +18,7 @@
 #include "desloc_inst.cuh"
 #include "desloc_internal.cuh"
 #include "desloc_norms.cuh"
+#include "desloc_ops.cuh"
 #include "desloc_readout.cuh"
 
 namespace desloc {
@@ -579,6 +580,32 @@ int run_step(desloc_ctx *ctx, uint32_t mask, float lr_t, float clip_bound_t,
     return rc;
 }
 
+// Runs `call` with the context's device current, unless a wait of an earlier step ran out.
+template <typename F>
+int on_device(desloc_ctx *ctx, const F &call) {
+    if (wait_ran_out(ctx)) return DESLOC_E_DEVICE_WAIT;
+    int dev_before = -1;
+    cudaError_t e = cudaGetDevice(&dev_before);
+    if (e == cudaSuccess && dev_before != ctx->device) e = cudaSetDevice(ctx->device);
+    if (e == cudaSuccess) e = call();
+    if (dev_before >= 0 && dev_before != ctx->device) cudaSetDevice(dev_before);
+    return e == cudaSuccess ? DESLOC_OK : cuda_fail(ctx, e);
+}
+
+// A tensor as rows of `width` elements, n tokens per worker: numbers of rows, columns and tokens that the kernels' 32-bit counters hold.
+int check_table(const desloc_ctx *ctx, int32_t tensor, int64_t width, int64_t n) {
+    if (tensor < 0 || tensor >= ctx->cfg.num_tensors || width < 1 || width > (1 << 20) || n < 0 || n > (1 << 30)) return DESLOC_E_RANGE;
+    const int64_t numel = ctx->numel[tensor];
+    return numel % width == 0 && numel / width <= (1 << 30) ? DESLOC_OK : DESLOC_E_RANGE;
+}
+
+int check_embedding(const desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows &tokens, int64_t n, float scale,
+                    const desloc_rows &rows) {
+    if (!desloc::is_token_rows(tokens) || !desloc::is_value_rows(rows)) return DESLOC_E_INVALID;
+    if (!std::isfinite(scale)) return DESLOC_E_RANGE;
+    return check_table(ctx, tensor, width, n);
+}
+
 }  // namespace
 
 extern "C" {
@@ -846,6 +873,101 @@ int desloc_rel_change(desloc_ctx *ctx, int32_t array, const float *const *then, 
     if (dev_before != ctx->device) cudaSetDevice(dev_before);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     return valid ? DESLOC_OK : DESLOC_E_DEVICE_WAIT;
+}
+
+int desloc_embed(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows *tokens, int64_t n, float scale, const desloc_rows *out,
+                 void *stream) {
+    desloc::NvtxRange range("desloc_embed");
+    if (!ctx || !tokens || !out) return DESLOC_E_NULL;
+    const int rc = check_embedding(ctx, tensor, width, *tokens, n, scale, *out);
+    if (rc != DESLOC_OK) return rc;
+    if (n == 0) return DESLOC_OK;
+    if (!tokens->data || !out->data) return DESLOC_E_NULL;
+    desloc::EmbedArgs a{};
+    a.x = reinterpret_cast<const float *const *>(ctx->res.d_tables) + tensor;
+    a.x_stride = ctx->cfg.num_tensors;
+    a.tokens = desloc::token_rows(*tokens);
+    a.out = out->data;
+    a.os0 = out->stride[0], a.os1 = out->stride[1];
+    a.n = static_cast<int>(n), a.width = static_cast<int>(width);
+    a.vocab = static_cast<int>(ctx->numel[tensor] / width);
+    a.scale = scale;
+    return on_device(ctx, [&] {
+        const cudaError_t e = desloc::launch_embed(a, ctx->cfg.M, out->dtype == DESLOC_BF16, static_cast<cudaStream_t>(stream));
+        if (e == cudaSuccess) ctx->launches += 1;
+        return e;
+    });
+}
+
+int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor, int64_t width, int64_t n) {
+    if (!ctx) return DESLOC_E_NULL;
+    const int rc = check_table(ctx, tensor, width, n);
+    if (rc != DESLOC_OK) return rc;
+    desloc::EmbedGradArgs a{};
+    a.n = static_cast<int>(n), a.width = static_cast<int>(width), a.vocab = static_cast<int>(ctx->numel[tensor] / width);
+    return desloc::plan_embed_grad(a, ctx->cfg.M, nullptr);
+}
+
+int desloc_embed_grad(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows *tokens, int64_t n, const desloc_rows *dout, float scale,
+                      int32_t accumulate, void *const *grads, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_embed_grad");
+    if (!ctx || !tokens || !dout || !grads || !work) return DESLOC_E_NULL;
+    const int rc = check_embedding(ctx, tensor, width, *tokens, n, scale, *dout);
+    if (rc != DESLOC_OK) return rc;
+    if (n > 0 && (!tokens->data || !dout->data)) return DESLOC_E_NULL;
+    if (reinterpret_cast<uintptr_t>(work) % 256) return DESLOC_E_INVALID;
+    desloc::EmbedGradArgs a{};
+    const desloc_config &c = ctx->cfg;
+    const bool bf16 = c.grad_dtype == DESLOC_BF16;
+    for (int m = 0; m < c.M; ++m) {
+        a.g[m] = grads[static_cast<int64_t>(m) * c.num_tensors + tensor];
+        if (!a.g[m]) return DESLOC_E_NULL;
+        if (reinterpret_cast<uintptr_t>(a.g[m]) % (bf16 ? 2 : 4)) return DESLOC_E_INVALID;
+    }
+    a.tokens = desloc::token_rows(*tokens);
+    a.dout = dout->data;
+    a.ds0 = dout->stride[0], a.ds1 = dout->stride[1];
+    a.n = static_cast<int>(n), a.width = static_cast<int>(width);
+    a.vocab = static_cast<int>(ctx->numel[tensor] / width);
+    a.scale = scale;
+    a.accumulate = accumulate != 0;
+    if (desloc::plan_embed_grad(a, c.M, static_cast<char *>(work)) > work_bytes) return DESLOC_E_RANGE;
+    return on_device(ctx, [&] {
+        int launches = 0;
+        const cudaError_t e = desloc::launch_embed_grad(a, c.M, dout->dtype == DESLOC_BF16, bf16, static_cast<cudaStream_t>(stream), &launches);
+        ctx->launches += launches;
+        return e;
+    });
+}
+
+int64_t desloc_clip_grads_bytes(const desloc_ctx *ctx) {
+    return ctx ? desloc::clip_work(ctx->cfg.M, ctx->cfg.num_tensors, ctx->nrchunks, nullptr, nullptr) : DESLOC_E_NULL;
+}
+
+int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, const void *const *grads, int32_t out_dtype, void *const *out,
+                      float *norms, float *factors, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_clip_grads");
+    if (!ctx || !grads || !out || !work) return DESLOC_E_NULL;
+    if (!(max_norm > 0.f) || !std::isfinite(max_norm)) return DESLOC_E_RANGE;
+    const auto known = [](int32_t t) { return t == DESLOC_F32 || t == DESLOC_BF16; };
+    if (!known(grads_dtype) || !known(out_dtype) || reinterpret_cast<uintptr_t>(work) % 256) return DESLOC_E_INVALID;
+    const desloc_config &c = ctx->cfg;
+    const uintptr_t gsz = grads_dtype == DESLOC_BF16 ? 2 : 4, osz = out_dtype == DESLOC_BF16 ? 2 : 4;
+    for (int64_t i = 0; i < ctx->nptr; ++i) {
+        if (!grads[i] || !out[i]) return DESLOC_E_NULL;
+        if (reinterpret_cast<uintptr_t>(grads[i]) % gsz || reinterpret_cast<uintptr_t>(out[i]) % osz) return DESLOC_E_INVALID;
+        if (grads[i] == out[i] && gsz != osz) return DESLOC_E_INVALID;
+    }
+    desloc::ClipWork w;
+    if (desloc::clip_work(c.M, c.num_tensors, ctx->nrchunks, &w, static_cast<char *>(work)) > work_bytes) return DESLOC_E_RANGE;
+    return on_device(ctx, [&] {
+        int launches = 0;
+        const cudaError_t e = desloc::launch_clip(ctx->d_rchunks, ctx->nrchunks, ctx->total_elems, grads, grads_dtype == DESLOC_BF16, out, out_dtype == DESLOC_BF16,
+                                                  c.num_tensors, c.M, max_norm, norms ? norms : w.norms, factors ? factors : w.norms + c.M, w,
+                                                  ctx->d_err, ctx->wait_limit, static_cast<cudaStream_t>(stream), &launches);
+        ctx->launches += launches;
+        return e;
+    });
 }
 
 int desloc_set_workers(desloc_ctx *ctx, int32_t M_new, int32_t first_new, float *const *x,

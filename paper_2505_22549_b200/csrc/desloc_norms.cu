@@ -8,6 +8,8 @@
 // partials of a row in fp64 in a fixed pattern.  No atomics.
 #include "desloc_norms.cuh"
 
+#include "desloc_ops.cuh"
+
 #include <type_traits>
 
 namespace desloc {
@@ -254,37 +256,33 @@ constexpr int64_t SMALL_BYTES = 4 << 20;   // of all workers
 constexpr int SMALL_MANY_CHUNKS = 40;
 constexpr int small_workers(bool bf16) { return (bf16 ? 3 : 2) * 148 / SMALL_BLOCKS; }
 
-__device__ __forceinline__ uint32_t first_block_addr(const void *shared) {
+__device__ __forceinline__ uint32_t block_addr(const void *shared, unsigned rank) {
     uint32_t r;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(smem_u32(shared)));
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(shared)), "r"(rank));
     return r;
 }
 
+// Where a warp's share of a worker's gradients lies: half chunks or whole ones where there is not a warp for each piece of them.
+struct SmallShare {
+    Chunk ch;
+    int e0, count;
+    __device__ __forceinline__ SmallShare(const Chunk *chunks, int nchunks, int at) : ch{}, e0(0), count(0) {
+        const int share = nchunks <= SMALL_WARPS / 4 ? SMALL_PIECES : nchunks <= SMALL_WARPS / 2 ? 2 : 1;
+        const int c = at / share, part = REDUCE_CHUNK_ELEMS / share;
+        if (c >= nchunks) return;
+        ch = chunks[c];
+        e0 = (at - c * share) * part;
+        count = min(ch.count - e0, part);
+    }
+};
+
+// The warp's sum of squares over its share, which begins at p; in lane 0.
 template <int MODE>
-__global__ void __cluster_dims__(SMALL_BLOCKS, 1, 1) __launch_bounds__(SMALL_THREADS)
-small_norms_kernel(const Chunk *chunks, int nchunks, const void *const *g, int nt, float max_norm, float *norms, float *scales) {
+__device__ __forceinline__ double small_sum(const char *p, int count) {
     using GT = std::conditional_t<MODE == RED_BF16, bf16_t, float>;
     constexpr int ESZ = static_cast<int>(sizeof(GT)), PER = 16 / ESZ, ROUNDS = SMALL_PIECE / PER / 32;
-    __shared__ double warp_sums[SMALL_THREADS / 32];
-    __shared__ double block_sums[SMALL_BLOCKS];   // (the first block's)
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int m = static_cast<int>(blockIdx.x) / SMALL_BLOCKS, rank = static_cast<int>(blockIdx.x) % SMALL_BLOCKS;
-    begin_and_let_next_begin();
-    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (do the blocks exist?  asked below)
-    // Half chunks or whole ones where there is not a warp for each piece of them.
-    const int at = rank * (SMALL_THREADS / 32) + warp;
-    const int share = nchunks <= SMALL_WARPS / 4 ? SMALL_PIECES : nchunks <= SMALL_WARPS / 2 ? 2 : 1;
-    const int c = at / share, part = REDUCE_CHUNK_ELEMS / share;
+    const int lane = threadIdx.x & 31;
     double total = 0.0;
-    int count = 0;
-    const char *p = nullptr;
-    if (c < nchunks) {
-        const Chunk ch = chunks[c];
-        const int e0 = (at - c * share) * part;
-        count = min(ch.count - e0, part);
-        p = reinterpret_cast<const char *>(g[static_cast<long long>(m) * nt + ch.tensor]) + (ch.start + e0) * static_cast<long long>(ESZ);
-    }
-    wait_for_earlier_kernels();
 #pragma unroll 1
     for (int done = 0; done < count; done += SMALL_PIECE, p += SMALL_PIECE * ESZ) {
         // 16-byte loads from the first boundary on; what lies around them element by element
@@ -307,22 +305,138 @@ small_norms_kernel(const Chunk *chunks, int nchunks, const void *const *g, int n
     }
 #pragma unroll
     for (int off = 16; off > 0; off >>= 1) total += __shfl_down_sync(0xffffffffu, total, off);
-    if (lane == 0) warp_sums[warp] = total;
+    return total;
+}
+
+// Adds what the blocks of a cluster hold, warp by warp and block by block: in the first block's threads 0, or (ALL) in every one's.
+template <bool ALL>
+__device__ __forceinline__ double small_total(double warp_sum, int rank) {
+    __shared__ double warp_sums[SMALL_THREADS / 32];
+    __shared__ double block_sums[SMALL_BLOCKS];
+    if (threadIdx.x % 32 == 0) warp_sums[threadIdx.x / 32] = warp_sum;
     __syncthreads();
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-    if (threadIdx.x == 0) {
+    if (threadIdx.x < (ALL ? SMALL_BLOCKS : 1)) {
         double t = 0.0;
 #pragma unroll
         for (int w = 0; w < SMALL_THREADS / 32; ++w) t += warp_sums[w];
-        asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(first_block_addr(&block_sums[rank])), "d"(t) : "memory");
+        asm volatile("st.shared::cluster.f64 [%0], %1;" :: "r"(block_addr(&block_sums[rank], threadIdx.x)), "d"(t) : "memory");
     }
     asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-    if (rank == 0 && threadIdx.x == 0) {
-        double t = 0.0;
+    double t = 0.0;
+    if (ALL || (rank == 0 && threadIdx.x == 0))
 #pragma unroll
         for (int r = 0; r < SMALL_BLOCKS; ++r) t += block_sums[r];
-        finish_norm(t, max_norm, norms + m, scales + m);
+    return t;
+}
+
+template <int MODE>
+__global__ void __cluster_dims__(SMALL_BLOCKS, 1, 1) __launch_bounds__(SMALL_THREADS)
+small_norms_kernel(const Chunk *chunks, int nchunks, const void *const *g, int nt, float max_norm, float *norms, float *scales) {
+    constexpr int ESZ = MODE == RED_BF16 ? 2 : 4;
+    const int m = static_cast<int>(blockIdx.x) / SMALL_BLOCKS, rank = static_cast<int>(blockIdx.x) % SMALL_BLOCKS;
+    begin_and_let_next_begin();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (do the blocks exist?  asked below)
+    const SmallShare s(chunks, nchunks, rank * (SMALL_THREADS / 32) + static_cast<int>(threadIdx.x >> 5));
+    const char *p = nullptr;
+    if (s.count > 0)
+        p = reinterpret_cast<const char *>(g[static_cast<long long>(m) * nt + s.ch.tensor]) + (s.ch.start + s.e0) * static_cast<long long>(ESZ);
+    wait_for_earlier_kernels();
+    const double t = small_total<false>(small_sum<MODE>(p, s.count), rank);
+    if (rank == 0 && threadIdx.x == 0) finish_norm(t, max_norm, norms + m, scales + m);
+}
+
+// ---- clipping on its own -----------------------------------------------------------------------------
+// to[i] := factor * from[i], n values, by `lanes` threads; eight at a time where both sides lie on 16-byte boundaries at the same
+// places.  `to` may be `from`.
+template <typename ST, typename DT>
+__device__ __forceinline__ void scale_span(const ST *from, DT *to, int n, float factor, int lane, int lanes) {
+    const uintptr_t f = reinterpret_cast<uintptr_t>(from), t = reinterpret_cast<uintptr_t>(to);
+    // (the side with the smaller elements says where)
+    const int to_boundary = sizeof(ST) <= sizeof(DT) ? static_cast<int>((0 - f) & 15u) / static_cast<int>(sizeof(ST))
+                                                     : static_cast<int>((0 - t) & 15u) / static_cast<int>(sizeof(DT));
+    const bool can = ((f + to_boundary * sizeof(ST)) & 15u) == 0 && ((t + to_boundary * sizeof(DT)) & 15u) == 0;
+    const int head = can ? min(n, to_boundary) : 0, wide = can ? (n - head) / 8 : 0;
+    for (int i = lane; i < n - 8 * wide; i += lanes) {
+        const int e = i < head ? i : i + 8 * wide;
+        const float one[1] = {static_cast<float>(from[e]) * factor};
+        store_values(to + e, one);
     }
+    for (int i0 = lane; i0 < wide; i0 += 4 * lanes) {
+        float v[4][8];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (i0 + k * lanes < wide) load_values(from + head + 8 * (i0 + k * lanes), v[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (i0 + k * lanes >= wide) break;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[k][e] *= factor;
+            store_values(to + head + 8 * (i0 + k * lanes), v[k]);
+        }
+    }
+}
+
+// Addresses on their way to the device in the kernel's parameters: a captured launch keeps them, no buffer has to.
+constexpr int ADDRESSES = 1000;
+struct Addresses {
+    const void *p[ADDRESSES];
+};
+__global__ void __launch_bounds__(256) addresses_kernel(const __grid_constant__ Addresses a, int n, const void **to) {
+    begin_and_let_next_begin();
+    wait_for_earlier_kernels();
+    for (int i = threadIdx.x; i < n; i += 256) to[i] = a.p[i];
+}
+
+// out^m = factor_m g^m, a chunk per block.  The last chunks first: of what the norms' pass read, the end is still in L2.
+constexpr int SCALE_THREADS = 128;
+
+template <typename ST, typename DT>
+__global__ void __launch_bounds__(SCALE_THREADS)
+scale_kernel(const Chunk *chunks, unsigned nchunks, const void *const *g, const void *const *out, int nt, const float *factors) {
+    begin_and_let_next_begin();
+    const unsigned item = gridDim.x - 1 - blockIdx.x;
+    const int m = static_cast<int>(item / nchunks);
+    const Chunk ch = chunks[item - m * nchunks];
+    wait_for_earlier_kernels();
+    const long long idx = static_cast<long long>(m) * nt + ch.tensor;
+    const ST *from = static_cast<const ST *>(g[idx]) + ch.start;
+    DT *to = static_cast<DT *>(const_cast<void *>(out[idx])) + ch.start;
+    const float factor = factors[m];
+    if (factor == 1.f && static_cast<const void *>(from) == static_cast<const void *>(to)) return;
+    scale_span(from, to, ch.count, factor, threadIdx.x, SCALE_THREADS);
+}
+
+// Small problems: norms as small_norms_kernel has them (the same bits), and what was read is in L2 for the second pass.  Few addresses travel
+// in the parameters: one launch in all.
+constexpr int SMALL_CLIP_ADDRESSES = 64;
+struct SmallClip {
+    const void *const *g, *const *out;   // tables, or null:
+    const void *few_g[SMALL_CLIP_ADDRESSES], *few_out[SMALL_CLIP_ADDRESSES];
+};
+
+template <typename ST, typename DT>
+__global__ void __cluster_dims__(SMALL_BLOCKS, 1, 1) __launch_bounds__(SMALL_THREADS)
+small_clip_kernel(const Chunk *chunks, int nchunks, const __grid_constant__ SmallClip a, int nt, float max_norm, float *norms, float *factors) {
+    constexpr int MODE = sizeof(ST) == 2 ? RED_BF16 : RED_F32;
+    const int m = static_cast<int>(blockIdx.x) / SMALL_BLOCKS, rank = static_cast<int>(blockIdx.x) % SMALL_BLOCKS;
+    begin_and_let_next_begin();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (do the blocks exist?  asked below)
+    const SmallShare s(chunks, nchunks, rank * (SMALL_THREADS / 32) + static_cast<int>(threadIdx.x >> 5));
+    wait_for_earlier_kernels();
+    const ST *from = nullptr;
+    DT *to = nullptr;
+    if (s.count > 0) {
+        const long long idx = static_cast<long long>(m) * nt + s.ch.tensor;
+        from = static_cast<const ST *>(a.g ? a.g[idx] : a.few_g[idx]) + s.ch.start + s.e0;
+        to = static_cast<DT *>(const_cast<void *>(a.g ? a.out[idx] : a.few_out[idx])) + s.ch.start + s.e0;
+    }
+    const double t = small_total<true>(small_sum<MODE>(reinterpret_cast<const char *>(from), s.count), rank);
+    float norm, factor;
+    finish_norm(t, max_norm, &norm, &factor);
+    if (rank == 0 && threadIdx.x == 0) norms[m] = norm, factors[m] = factor;
+    if (s.count > 0 && !(factor == 1.f && static_cast<const void *>(from) == static_cast<const void *>(to)))
+        scale_span(from, to, s.count, factor, threadIdx.x & 31, 32);
 }
 
 // dst^j[i] = mean over the M_src source replicas of src^m[i] (fp64 sum in the order
@@ -374,17 +488,7 @@ diag_norms_kernel(const float *partial, long long nchunks, const int *parts_of, 
 // All launches of this file may begin while the kernel in front of them still runs.
 template <typename... P, typename... A>
 cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, A... args) {
-    cudaLaunchConfig_t lc{};
-    lc.gridDim = grid;
-    lc.blockDim = dim3(threads);
-    lc.dynamicSmemBytes = smem;
-    lc.stream = stream;
-    cudaLaunchAttribute at{};
-    at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at.val.programmaticStreamSerializationAllowed = 1;
-    lc.attrs = &at;
-    lc.numAttrs = 1;
-    return cudaLaunchKernelEx(&lc, kernel, static_cast<P>(args)...);
+    return launch_op(kernel, grid, dim3(threads), smem, true, stream, args...);
 }
 
 unsigned grid_for(long long nitems) {
@@ -396,20 +500,24 @@ unsigned grid_for(long long nitems) {
 template <int MODE>
 static cudaError_t launch_sumsq(const Chunk *chunks, long long nchunks, const void *const *now, const void *const *then,
                                 int nt, int M, float *partial, long long *items, long long *stride, int *err,
-                                int wait_limit, cudaStream_t stream) {
+                                int wait_limit, cudaStream_t stream, bool overlap = true) {
     *items = (nchunks + red_chunks(MODE) - 1) / red_chunks(MODE);
     *stride = reduce_row(*items);
-    return launch(sumsq_kernel<MODE>, grid_for(*items * M), RED_THREADS, RED_BYTES, stream, chunks, nchunks, now, then, nt,
-                  M, partial, *stride, err, wait_limit);
+    return launch_op(sumsq_kernel<MODE>, grid_for(*items * M), dim3(RED_THREADS), RED_BYTES, overlap, stream, chunks, nchunks, now, then, nt,
+                     M, partial, *stride, err, wait_limit);
+}
+
+// A piece, half a chunk or a chunk for each warp of a cluster.  Beyond 4 MB in all the two stages read no slower (16 workers x 129 K parameters,
+// fp32, in 33 and 65 tensors, in a graph: 19.1 and 18.9 us in two stages, 20.0 and 20.2 in one; 2 bytes each 16.8 and 15.3, 15.7 and 14.1).
+static bool small_norms(long long nchunks, int64_t elems, int M, bool bf16) {
+    return (M <= small_workers(bf16) || nchunks >= SMALL_MANY_CHUNKS) && elems <= SMALL_WARPS * SMALL_PIECE && nchunks <= SMALL_WARPS &&
+           elems * M * (bf16 ? 2 : 4) <= SMALL_BYTES;
 }
 
 cudaError_t launch_grad_norms(const Chunk *chunks, long long nchunks, int64_t elems, const void *const *g, int nt,
                               int M, bool bf16, float max_norm, float *partial, float *norms,
                               float *scales, int *err, int wait_limit, cudaStream_t stream, int *launches) {
-    // A piece, half a chunk or a chunk for each warp of a cluster.  Beyond 4 MB in all the two stages read no slower (16 workers x 129 K parameters,
-    // fp32, in 33 and 65 tensors, in a graph: 19.1 and 18.9 us in two stages, 20.0 and 20.2 in one; 2 bytes each 16.8 and 15.3, 15.7 and 14.1).
-    if ((M <= small_workers(bf16) || nchunks >= SMALL_MANY_CHUNKS) && elems <= SMALL_WARPS * SMALL_PIECE && nchunks <= SMALL_WARPS &&
-        elems * M * (bf16 ? 2 : 4) <= SMALL_BYTES) {
+    if (small_norms(nchunks, elems, M, bf16)) {
         *launches = 1;
         return launch(bf16 ? small_norms_kernel<RED_BF16> : small_norms_kernel<RED_F32>, M * SMALL_BLOCKS, SMALL_THREADS, 0, stream, chunks,
                       nchunks, g, nt, max_norm, norms, scales);
@@ -421,6 +529,59 @@ cudaError_t launch_grad_norms(const Chunk *chunks, long long nchunks, int64_t el
              : launch_sumsq<RED_F32>(chunks, nchunks, g, nullptr, nt, M, partial, &items, &stride, err, wait_limit, stream);
     if (e != cudaSuccess) return e;
     return launch(norm_finalize_kernel, M, FINAL_THREADS, 0, stream, partial, items, stride, max_norm, norms, scales);
+}
+
+int64_t clip_work(int M, int nt, int64_t nrchunks, ClipWork *w, char *work) {
+    int64_t at = 0;
+    const auto take = [&](int64_t bytes) {
+        char *p = work ? work + at : nullptr;
+        at += (bytes + 255) & ~int64_t{255};
+        return p;
+    };
+    char *const tables = take(int64_t{16} * M * nt), *const norms = take(int64_t{8} * M), *const partial = take(int64_t{4} * M * reduce_row(nrchunks));
+    if (w) *w = {reinterpret_cast<const void **>(tables), reinterpret_cast<float *>(norms), reinterpret_cast<float *>(partial)};
+    return at;
+}
+
+cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, const void *const *g, bool g_bf16, void *const *out, bool out_bf16,
+                        int nt, int M, float max_norm, float *norms, float *factors, const ClipWork &w, int *err, int wait_limit,
+                        cudaStream_t stream, int *launches) {
+    const int nptr = M * nt;
+    const bool small = small_norms(nchunks, elems, M, g_bf16);
+    using bf = __nv_bfloat16;
+    *launches = 0;
+    SmallClip few{};
+    if (small && nptr <= SMALL_CLIP_ADDRESSES) {
+        for (int i = 0; i < nptr; ++i) few.few_g[i] = g[i], few.few_out[i] = out[i];
+    } else {
+        for (int i0 = 0; i0 < 2 * nptr; i0 += ADDRESSES) {
+            Addresses a;
+            const int n = 2 * nptr - i0 < ADDRESSES ? 2 * nptr - i0 : ADDRESSES;
+            for (int i = 0; i < n; ++i) a.p[i] = i0 + i < nptr ? g[i0 + i] : out[i0 + i - nptr];
+            const cudaError_t e = launch(addresses_kernel, 1, 256, 0, stream, a, n, w.tables + i0);
+            if (e != cudaSuccess) return e;
+            *launches += 1;
+        }
+        few.g = w.tables, few.out = w.tables + nptr;
+    }
+    cudaError_t e;
+    if (small) {
+        const auto kernel = g_bf16 ? (out_bf16 ? small_clip_kernel<bf, bf> : small_clip_kernel<bf, float>)
+                                   : (out_bf16 ? small_clip_kernel<float, bf> : small_clip_kernel<float, float>);
+        e = launch(kernel, M * SMALL_BLOCKS, SMALL_THREADS, 0, stream, chunks, static_cast<int>(nchunks), few, nt, max_norm, norms, factors);
+        if (e == cudaSuccess) *launches += 1;
+        return e;
+    }
+    long long items, stride;
+    // (behind the addresses: it looks at them before it waits)
+    e = g_bf16 ? launch_sumsq<RED_BF16>(chunks, nchunks, few.g, nullptr, nt, M, w.partial, &items, &stride, err, wait_limit, stream, false)
+               : launch_sumsq<RED_F32>(chunks, nchunks, few.g, nullptr, nt, M, w.partial, &items, &stride, err, wait_limit, stream, false);
+    if (e == cudaSuccess) e = launch(norm_finalize_kernel, M, FINAL_THREADS, 0, stream, w.partial, items, stride, max_norm, norms, factors);
+    const auto kernel = g_bf16 ? (out_bf16 ? scale_kernel<bf, bf> : scale_kernel<bf, float>) : (out_bf16 ? scale_kernel<float, bf> : scale_kernel<float, float>);
+    if (e == cudaSuccess)
+        e = launch(kernel, grid_for(nchunks * M), SCALE_THREADS, 0, stream, chunks, static_cast<unsigned>(nchunks), few.g, few.out, nt, factors);
+    if (e == cudaSuccess) *launches += 3;
+    return e;
 }
 
 cudaError_t launch_rel_change(const Chunk *chunks, long long nchunks, const float *const *now,

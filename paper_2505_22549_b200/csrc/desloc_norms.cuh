@@ -16,6 +16,17 @@ cudaError_t launch_grad_norms(const Chunk *chunks, long long nchunks, int64_t el
                               int M, bool bf16, float max_norm, float *partial, float *norms,
                               float *scales, int *err, int wait_limit, cudaStream_t stream, int *launches);
 
+// Clipping on its own: out^m = f_m g^m, norms and factors as above.  Working memory: tables of 2 * M * nt addresses, [2][M] norms and factors
+// (for callers that do not ask for them), partial as above.
+struct ClipWork {
+    const void **tables;
+    float *norms, *partial;
+};
+int64_t clip_work(int M, int nt, int64_t nrchunks, ClipWork *w, char *work);
+cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, const void *const *g, bool g_bf16, void *const *out, bool out_bf16,
+                        int nt, int M, float max_norm, float *norms, float *factors, const ClipWork &w, int *err, int wait_limit,
+                        cudaStream_t stream, int *launches);
+
 // partial: scratch of at least 2 * M * reduce_row(nchunks) floats; out[m] = ||now - then|| / ||then||
 // (out may be host memory that the device can write to).  *released is written with a release at system
 // scope, behind all that is in front in the stream.  Two launches.

@@ -1,8 +1,9 @@
-"""``DesLoc``: owns nothing but a context handle; holds references to the caller's tensors."""
+"""``DesLoc``: owns nothing but a context handle; holds references to the caller's tensors.  ``token_logprobs`` and its gradient
+need no context."""
 from __future__ import annotations
 
 import ctypes
-from typing import Optional, Sequence
+from typing import NamedTuple, Optional, Sequence
 
 import torch
 
@@ -24,6 +25,46 @@ _native.bind(*(_entry(getattr(B.raw_lib(), "desloc_" + n))
 _GRAD_MISFIT = "gradient tensor of wrong dtype, size or layout"
 _SNAP_MISFIT = "snapshot tensor of wrong dtype, size or layout"
 _HOST_MISFIT = "host gradient tensor of wrong dtype, size, layout or device"
+
+
+_TYPES = {torch.float32: B.DESLOC_F32, torch.bfloat16: B.DESLOC_BF16}
+_TORCH_TYPES = {code: t for t, code in _TYPES.items()}
+_TOKEN_TYPES = {torch.int32: B.DESLOC_I32, torch.int64: B.DESLOC_I64}
+
+
+def _merged(sizes, strides):
+    """The one stride of these dimensions taken as one, or None where they have none."""
+    size, stride = 1, 0
+    for n, s in zip(reversed(sizes), reversed(strides)):
+        if n == 1:
+            continue
+        if size == 1:
+            stride = s
+        elif s != size * stride:
+            return None
+        size *= n
+    return stride
+
+
+def _split(lead, tensors):
+    """(outer, inner, [strides of each tensor]): the dimensions `lead`, first ones of every tensor, as two; None where the tensors
+    do not lie so."""
+    for k in range(len(lead) + 1):
+        strides = [(_merged(lead[:k], t.stride()[:k]), _merged(lead[k:], t.stride()[k:len(lead)])) for t in tensors]
+        if all(a is not None and b is not None for a, b in strides):
+            outer = inner = 1
+            for n in lead[:k]:
+                outer *= n
+            for n in lead[k:]:
+                inner *= n
+            return outer, inner, strides
+    return None
+
+
+def _on(device, what, *tensors):
+    for t in tensors:
+        if t.device != device:
+            raise ValueError(f"{what} must be on {device}")
 
 
 class BoundGrads:
@@ -158,6 +199,95 @@ class DesLoc:
             self._raise(r, "desloc_rel_change")
         return r
 
+    def _rows_of(self, tensor: int, width: Optional[int]) -> int:
+        """Columns of a state tensor taken as rows: its last dimension, unless the caller says."""
+        if not 0 <= tensor < len(self.numel):
+            raise ValueError("no such tensor")
+        shape = self._keep[0][0][tensor].shape
+        if width is None and len(shape) < 2:
+            raise ValueError("the tensor has one dimension: say how wide its rows are")
+        return int(shape[-1] if width is None else width)
+
+    def _tokens(self, tokens: torch.Tensor):
+        if tokens.dtype not in _TOKEN_TYPES or tokens.dim() < 1 or tokens.shape[0] != self.M:
+            raise ValueError("tokens are int32 or int64, [workers, ...]")
+        _on(self.device, "tokens", tokens)
+        flat = tokens.reshape(self.M, -1)
+        return B.rows(flat.data_ptr(), _TOKEN_TYPES[flat.dtype], *flat.stride()), flat
+
+    def embed(self, tensor: int, tokens: torch.Tensor, scale: float = 1.0, dtype="bf16", width: Optional[int] = None,
+              out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """scale * rows of every worker's x of `tensor` by token, on torch's current stream.  tokens: [M, ...] -> [M, ..., width] of `dtype`
+        ("f32", "bf16"; that of `out` where it is given).  Tokens outside the vocabulary give zeros."""
+        width = self._rows_of(tensor, width)
+        rows, flat = self._tokens(tokens)
+        shape = tuple(tokens.shape) + (width,)
+        if out is None:
+            out = torch.empty(shape, dtype=_TORCH_TYPES[B.DTYPE_BY_NAME.get(dtype, dtype)], device=self.device)
+        elif tuple(out.shape) != shape or out.dtype not in _TYPES:
+            raise ValueError("out does not fit the tokens")
+        _on(self.device, "out", out)
+        to = _split(shape[:-1], [out]) if out.stride(-1) == 1 or width == 1 else None
+        if to is None or (to[0] != self.M and self.M * flat.shape[1] != to[1]):
+            raise ValueError("out has rows that the kernels do not reach: at most one stride behind the workers'")
+        stride = to[2][0] if to[0] == self.M else (to[2][0][1] * flat.shape[1], to[2][0][1])
+        B.desloc_embed(self.ctx, tensor, width, rows, flat.shape[1], scale, B.rows(out.data_ptr(), _TYPES[out.dtype], *stride),
+                       torch.cuda.current_stream(self.device).cuda_stream)
+        return out
+
+    def embed_grad(self, tensor: int, tokens: torch.Tensor, dout: torch.Tensor, grads, scale: float = 1.0, accumulate: bool = False,
+                   width: Optional[int] = None) -> None:
+        """The gradient of embed() into the workers' gradients of `tensor` in `grads` (what step() reads: nested lists, of which only that
+        tensor is looked at, or bind_grads()' handle).  accumulate: added to what they hold."""
+        width = self._rows_of(tensor, width)
+        rows, flat = self._tokens(tokens)
+        if tuple(dout.shape) != tuple(tokens.shape) + (width,) or dout.dtype not in _TYPES:
+            raise ValueError("dout does not fit the tokens")
+        _on(self.device, "dout", dout)
+        d = dout.reshape(self.M, -1, width) if flat.shape[1] else dout.new_empty(self.M, 0, width)
+        if d.stride(-1) != 1 and width > 1:
+            d = d.contiguous()
+        nt = len(self.numel)
+        if isinstance(grads, BoundGrads):
+            array = grads.array
+        else:
+            array = (ctypes.c_void_p * (self.M * nt))()
+            if len(grads) != self.M:
+                raise ValueError("need one gradient list per worker")
+            for m, row in enumerate(grads):
+                g = row[tensor]
+                if g.dtype != _TORCH_TYPES[self.grad_dtype] or g.numel() != self.numel[tensor] or not g.is_contiguous() or g.device != self.device:
+                    raise ValueError(_GRAD_MISFIT)
+                array[m * nt + tensor] = g.data_ptr()
+        n = flat.shape[1]
+        work = torch.empty(B.desloc_embed_grad_bytes(self.ctx, tensor, width, n), dtype=torch.uint8, device=self.device)
+        B.desloc_embed_grad(self.ctx, tensor, width, rows, n, B.rows(d.data_ptr(), _TYPES[d.dtype], *d.stride()[:2]), scale, accumulate, array,
+                            work.data_ptr(), work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+
+    def _list_of(self, table, grads):
+        """(address, type code) of a set of gradient tensors of one type, on this context's device."""
+        if isinstance(grads, BoundGrads):
+            return grads.address, self.grad_dtype
+        kind = _TYPES.get(grads[0][0].dtype) if len(grads) and len(grads[0]) else None
+        if kind is None:
+            raise ValueError(_GRAD_MISFIT)
+        for row in grads:
+            _on(self.device, "gradients", *row)
+        return self._fill(table, grads, kind, 0, _GRAD_MISFIT), kind
+
+    def clip_grads(self, grads, max_norm: float, out=None):
+        """Norm-based clipping on its own: every worker's gradients (nested lists, fp32 or bf16) times min(1, max_norm / their norm over the
+        whole tensor list), into `out` (the same, either type) or in place.  Returns (norms, factors), [M] fp32 on the device; nothing waits."""
+        address, kind = self._list_of(self._table, grads)
+        to, to_kind = (address, kind) if out is None else self._list_of(self._table2, out)
+        result = torch.empty(2, self.M, dtype=torch.float32, device=self.device)
+        work = torch.empty(B.desloc_clip_grads_bytes(self.ctx), dtype=torch.uint8, device=self.device)
+        n = self.M * len(self.numel)
+        at = lambda a: (ctypes.c_void_p * n).from_address(a)
+        B.desloc_clip_grads(self.ctx, max_norm, kind, at(address), to_kind, at(to), result[0].data_ptr(), result[1].data_ptr(), work.data_ptr(),
+                            work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+        return result[0], result[1]
+
     def set_workers(self, x, u, v, first_new: int) -> None:
         """New worker set (lists like the constructor's); workers first_new.. start from the mean
         of the current workers.  Synchronises the current stream."""
@@ -202,3 +332,72 @@ class DesLoc:
             self.close()
         except Exception:
             pass
+
+
+class TokenLogprobs(NamedTuple):
+    """What token_logprobs() returns; what was not asked for is None."""
+    logp: torch.Tensor                    # [...]
+    lse: torch.Tensor                     # [...]
+    entropy: Optional[torch.Tensor]       # [...]
+    top_ids: Optional[torch.Tensor]       # [..., top], int64
+    top_logp: Optional[torch.Tensor]      # [..., top]
+
+
+def _logit_rows(logits, tokens, *more):
+    """The two-level rows of logits, tokens and what else has one row each; copies what does not lie so."""
+    if logits.device.type != "cuda":
+        raise ValueError("logits must be CUDA tensors (there is no CPU path)")
+    if logits.dtype not in _TYPES or logits.dim() < 1 or logits.shape[-1] < 1:
+        raise ValueError("logits are fp32 or bf16, [..., vocabulary]")
+    if tokens.dtype not in _TOKEN_TYPES or tokens.shape != logits.shape[:-1]:
+        raise ValueError("tokens are int32 or int64, of the shape of the logits without their last dimension")
+    _on(logits.device, "tokens", tokens)
+    if logits.stride(-1) != 1 and logits.shape[-1] > 1:
+        logits = logits.contiguous()
+    lead = tuple(logits.shape[:-1])
+    found = _split(lead, [logits, tokens, *more])
+    if found is None:
+        logits, tokens = logits.contiguous(), tokens.contiguous()
+        found = _split(lead, [logits, tokens, *more])
+    if found is None:
+        raise ValueError("out has rows that the kernels do not reach: more than two strides")
+    return logits, tokens, found
+
+
+def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, entropy: bool = False, top: int = 0) -> TokenLogprobs:
+    """Log probabilities of `tokens` [...] under `logits` [..., vocabulary] (fp32 or bf16), on torch's current stream: logp (0 for tokens outside the
+    vocabulary), lse, and on request the entropy and the `top` likeliest tokens.  exp(-logp.mean(...)) is the perplexity."""
+    logits, tokens, (outer, inner, strides) = _logit_rows(logits, tokens)
+    lead, dev = logits.shape[:-1], logits.device
+    new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)
+    r = TokenLogprobs(new(*lead), new(*lead), new(*lead) if entropy else None, new(*lead, top, dtype=torch.int64) if top else None,
+                      new(*lead, top) if top else None)
+    at = lambda t: t.data_ptr() if t is not None else 0
+    B.desloc_token_logprobs(outer, inner, logits.shape[-1], B.rows(logits.data_ptr(), _TYPES[logits.dtype], *strides[0]),
+                            B.rows(tokens.data_ptr(), _TOKEN_TYPES[tokens.dtype], *strides[1]), top, *map(at, r), dev.index,
+                            torch.cuda.current_stream(dev).cuda_stream)
+    return r
+
+
+def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor, entropy: Optional[torch.Tensor] = None,
+                        dentropy: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) with respect to the logits, in their type; lse and entropy are what
+    token_logprobs() gave.  out may be the logits themselves."""
+    if out is None:
+        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
+    if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (out.stride(-1) != 1 and out.shape[-1] > 1):
+        raise ValueError("out does not fit the logits")
+    if dentropy is not None and entropy is None:
+        raise ValueError("the entropy's gradient needs the entropy")
+    logits, tokens, (outer, inner, strides) = _logit_rows(logits, tokens, out)
+    dense = []
+    for t in (lse, dlogp, entropy, dentropy):
+        if t is not None and (t.dtype != torch.float32 or t.shape != tokens.shape or t.device != logits.device):
+            raise ValueError("lse, dlogp, entropy and dentropy are fp32, of the tokens' shape, where the logits are")
+        dense.append(t if t is None or t.is_contiguous() else t.contiguous())
+    at = lambda t: t.data_ptr() if t is not None else 0
+    B.desloc_token_logprobs_grad(outer, inner, logits.shape[-1], B.rows(logits.data_ptr(), _TYPES[logits.dtype], *strides[0]),
+                                 B.rows(tokens.data_ptr(), _TOKEN_TYPES[tokens.dtype], *strides[1]), *map(at, dense),
+                                 B.rows(out.data_ptr(), _TYPES[out.dtype], *strides[2]), logits.device.index,
+                                 torch.cuda.current_stream(logits.device).cuda_stream)
+    return out

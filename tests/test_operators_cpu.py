@@ -1,0 +1,114 @@
+"""Operators around the step: what is refused before any CUDA call, and the layouts that the Python names accept."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2505_22549_b200 as d
+from paper_2505_22549_b200 import binding as B
+from paper_2505_22549_b200 import module
+
+
+def _logprobs(outer=2, inner=3, vocab=8, logits=None, tokens=None, top=0, logp=16, lse=16, entropy=0, ids=0, tlp=0, device=0):
+    logits = B.rows(64, d.DESLOC_F32, 24, 8) if logits is None else logits
+    tokens = B.rows(64, d.DESLOC_I64, 3, 1) if tokens is None else tokens
+    return lambda: B.desloc_token_logprobs(outer, inner, vocab, logits, tokens, top, logp, lse, entropy, ids, tlp, device)
+
+
+def _grad(outer=2, inner=3, vocab=8, logits=None, tokens=None, out=None, lse=16, dlogp=16, entropy=0, dentropy=0, device=0):
+    logits = B.rows(64, d.DESLOC_F32, 24, 8) if logits is None else logits
+    tokens = B.rows(64, d.DESLOC_I64, 3, 1) if tokens is None else tokens
+    out = B.rows(64, d.DESLOC_F32, 24, 8) if out is None else out
+    return lambda: B.desloc_token_logprobs_grad(outer, inner, vocab, logits, tokens, lse, dlogp, entropy, dentropy, out, device)
+
+
+REFUSED = [
+    (_logprobs(outer=-1), d.DESLOC_E_RANGE),
+    (_logprobs(inner=-1), d.DESLOC_E_RANGE),
+    (_logprobs(vocab=0), d.DESLOC_E_RANGE),
+    (_logprobs(vocab=(1 << 30) + 1), d.DESLOC_E_RANGE),
+    (_logprobs(outer=1 << 20, inner=1 << 20), d.DESLOC_E_RANGE),
+    (_logprobs(top=-1), d.DESLOC_E_RANGE),
+    (_logprobs(top=d.DESLOC_MAX_TOP + 1, ids=16, tlp=16), d.DESLOC_E_RANGE),
+    (_logprobs(device=-1), d.DESLOC_E_RANGE),
+    (_logprobs(logits=B.rows(64, 2, 24, 8)), d.DESLOC_E_INVALID),
+    (_logprobs(logits=B.rows(66, d.DESLOC_F32, 24, 8)), d.DESLOC_E_INVALID),
+    (_logprobs(tokens=B.rows(64, 7, 3, 1)), d.DESLOC_E_INVALID),
+    (_logprobs(tokens=B.rows(68, d.DESLOC_I64, 3, 1)), d.DESLOC_E_INVALID),
+    (_logprobs(logits=B.rows(0, d.DESLOC_F32, 24, 8)), d.DESLOC_E_NULL),
+    (_logprobs(tokens=B.rows(0, d.DESLOC_I64, 3, 1)), d.DESLOC_E_NULL),
+    (_logprobs(logp=0), d.DESLOC_E_NULL),
+    (_logprobs(lse=0), d.DESLOC_E_NULL),
+    (_logprobs(top=1, ids=16), d.DESLOC_E_NULL),
+    (_logprobs(top=1, tlp=16), d.DESLOC_E_NULL),
+    (_grad(vocab=0), d.DESLOC_E_RANGE),
+    (_grad(device=-1), d.DESLOC_E_RANGE),
+    (_grad(out=B.rows(64, d.DESLOC_BF16, 24, 8)), d.DESLOC_E_INVALID),
+    (_grad(out=B.rows(65, d.DESLOC_F32, 24, 8)), d.DESLOC_E_INVALID),
+    (_grad(out=B.rows(0, d.DESLOC_F32, 24, 8)), d.DESLOC_E_NULL),
+    (_grad(lse=0), d.DESLOC_E_NULL),
+    (_grad(dlogp=0), d.DESLOC_E_NULL),
+    (_grad(dentropy=16), d.DESLOC_E_NULL),
+]
+
+
+@pytest.mark.parametrize("k", range(len(REFUSED)))
+def test_logprobs_refused_before_any_cuda_call(k):
+    call, status = REFUSED[k]
+    with pytest.raises(d.DeslocError) as e:
+        call()
+    assert e.value.status == status
+
+
+def test_no_rows_is_no_work():
+    _logprobs(outer=0, logits=B.rows(0, d.DESLOC_F32, 0, 0), tokens=B.rows(0, d.DESLOC_I64, 0, 0), logp=0, lse=0)()
+    _grad(inner=0, logits=B.rows(0, d.DESLOC_F32, 0, 0), tokens=B.rows(0, d.DESLOC_I64, 0, 0), lse=0, dlogp=0)()
+
+
+def test_calls_with_a_context_refuse_none():
+    L, none = d.raw_lib(), B.rows(64, 0, 1, 1)
+    assert L.desloc_embed(None, 0, 8, none, 1, 1.0, none, None) == d.DESLOC_E_NULL
+    assert L.desloc_embed_grad(None, 0, 8, none, 1, none, 1.0, 0, None, None, 0, None) == d.DESLOC_E_NULL
+    assert L.desloc_embed_grad_bytes(None, 0, 8, 1) == d.DESLOC_E_NULL
+    assert L.desloc_clip_grads(None, 1.0, 0, None, 0, None, None, None, None, 0, None) == d.DESLOC_E_NULL
+    assert L.desloc_clip_grads_bytes(None) == d.DESLOC_E_NULL
+    assert L.desloc_token_logprobs(1, 1, 1, None, None, 0, None, None, None, None, None, 0, None) == d.DESLOC_E_NULL
+    assert L.desloc_token_logprobs_grad(1, 1, 1, none, none, None, None, None, None, None, 0, None) == d.DESLOC_E_NULL
+
+
+def test_rows_struct_is_the_headers():
+    assert ctypes.sizeof(B.DeslocRows) == 32
+    assert (B.DeslocRows.data.offset, B.DeslocRows.dtype.offset, B.DeslocRows.stride.offset) == (0, 8, 16)
+
+
+def test_host_tensors_are_refused():
+    x, t = torch.zeros(2, 3, 8), torch.zeros(2, 3, dtype=torch.int64)
+    with pytest.raises(ValueError, match="CUDA"):
+        d.token_logprobs(x, t)
+    with pytest.raises(ValueError, match="CUDA"):
+        d.token_logprobs_grad(x, t, torch.zeros(2, 3), torch.zeros(2, 3))
+
+
+def _reach(t, split):
+    """Element offsets of a tensor's rows from its outer and inner strides."""
+    outer, inner, strides = split
+    a, b = strides[t]
+    return [i * a + j * b for i in range(outer) for j in range(inner)]
+
+
+@pytest.mark.parametrize("make", [
+    lambda x: x, lambda x: x[:, :-1], lambda x: x[1:], lambda x: x[:, 1:3], lambda x: x[::2], lambda x: x[:, ::2], lambda x: x[0],
+    lambda x: x[:1], lambda x: x[:, :1], lambda x: x[0, 0], lambda x: x.transpose(0, 1), lambda x: x[:0], lambda x: x.unsqueeze(1),
+    lambda x: x.unsqueeze(0), lambda x: x.expand(2, 4, 5, 6), lambda x: x.view(2, 2, 5, 6)])
+def test_two_strides_reach_every_row(make):
+    x = make(torch.arange(4 * 5 * 6).view(4, 5, 6))
+    lead = tuple(x.shape[:-1])
+    split = module._split(lead, [x, torch.zeros(x.shape)])
+    assert split is not None
+    want = (x[..., 0] - x.storage_offset() * (x.numel() > 0)).reshape(-1).tolist() if x.numel() else []
+    assert _reach(0, split) == want
+
+
+def test_three_strides_are_more_than_two():
+    x = torch.arange(4 * 5 * 4 * 6).view(4, 5, 4, 6)[:, ::2, ::2]
+    assert module._split(tuple(x.shape[:-1]), [x]) is None
