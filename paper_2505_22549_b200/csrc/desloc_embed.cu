@@ -1,6 +1,8 @@
 // Embedding lookup from the workers' replicas, and its gradient by sorted tokens.
 #include "desloc_ops.cuh"
 
+#include <type_traits>
+
 namespace desloc {
 
 namespace {
@@ -45,11 +47,25 @@ __global__ void __launch_bounds__(EMBED_THREADS) embed_kernel(const EmbedArgs a)
 
 // ---- sort --------------------------------------------------------------------------------------------
 // Stable counting sort of a worker's tokens, a block for each value of the tokens' last bits: it goes over all of them twice, counts
-// its own and those of the blocks in front of it, and writes its part of the order.  No block waits for another.
-constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_AHEAD = 4;
+// its own and those of the blocks in front of it, and writes its part of the order and its runs (a run: the places of one token).  No
+// block waits for another.  Bound: latency; up to SORT_CACHED tokens stay in registers between the two times.
+constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_AHEAD = 16;
+constexpr int SORT_CACHED = SORT_THREADS * SORT_AHEAD;
 constexpr int SORT_KEYS = 760;   // most numbers that a block tells apart: counters of 47.5 KB
 
-__global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const EmbedGradArgs a) {
+// A run of `piece` or more places is cut into floor(length / piece) pieces of nearly equal length, summed by a block each.  Piece j of
+// a run that begins at place s has number ceil(s / piece) + j: no two runs' numbers meet, because ceil(a + b) >= ceil(a) + floor(b), and
+// place number * piece lies in the run.
+struct Pieces {
+    int first, n;
+    __device__ __forceinline__ Pieces(const EmbedGradArgs &a, int start, int length)
+        : first((start + a.piece - 1) / a.piece), n(length / a.piece) {}
+};
+
+// WIDE: 64-bit token numbers.
+template <bool CACHED, bool WIDE>
+__global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_constant__ EmbedGradArgs a) {
+    using Number = std::conditional_t<WIDE, long long, int>;
     extern __shared__ int hist[];   // [warp][key]: counts, then places
     __shared__ int s_warp[SORT_WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -60,26 +76,31 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const EmbedGra
     __syncthreads();
     wait_for_earlier_kernels();
     // a warp's share: consecutive positions, so that places by (key, warp) are places by (key, position)
-    const long long share = (static_cast<long long>(a.n) + SORT_THREADS - 1) / SORT_THREADS * 32;
-    const long long lo = min(static_cast<long long>(a.n), warp * share), hi = min(static_cast<long long>(a.n), lo + share);
-    const long long t0 = m * a.tokens.s0;
+    const int share = (a.n + SORT_THREADS - 1) / SORT_THREADS * 32;
+    const int lo = static_cast<int>(min(static_cast<long long>(a.n), static_cast<long long>(warp) * share)), hi = min(a.n - lo, share) + lo;
+    const Number *const tokens = static_cast<const Number *>(a.tokens.data) + m * a.tokens.s0;
+    int t[SORT_AHEAD];
+    const auto load = [&](int i0) {
+        Number v[SORT_AHEAD];
+        const Number *p = tokens + (i0 + lane) * a.tokens.s1;
+        const long long step = 32 * a.tokens.s1;
+#pragma unroll
+        for (int k = 0; k < SORT_AHEAD; ++k) v[k] = i0 + 32 * k < hi - lane ? p[k * step] : -1;
+#pragma unroll
+        for (int k = 0; k < SORT_AHEAD; ++k)
+            t[k] = static_cast<std::make_unsigned_t<Number>>(v[k]) < static_cast<unsigned>(a.vocab) ? static_cast<int>(v[k]) : -1;
+    };
     int before = 0;
-    for (long long i0 = lo; i0 < hi; i0 += 32 * SORT_AHEAD) {
-        int t[SORT_AHEAD];
+    for (int i0 = lo; i0 < hi; i0 += 32 * SORT_AHEAD) {
+        load(i0);
 #pragma unroll
         for (int k = 0; k < SORT_AHEAD; ++k) {
-            const long long i = i0 + 32 * k + lane;
-            t[k] = i < hi ? token_at(a.tokens, t0 + i * a.tokens.s1, a.vocab) : -1;
-        }
-#pragma unroll
-        for (int k = 0; k < SORT_AHEAD; ++k) {
-            if (t[k] < 0) continue;
-            if ((t[k] & mask) == b) atomicAdd(&mine[t[k] >> a.bits], 1);
-            before += (t[k] & mask) < b;
+            const int last = t[k] < 0 ? mask + 1 : t[k] & mask;
+            if (last == b) atomicAdd(&mine[t[k] >> a.bits], 1);
+            before += last < b;
         }
     }
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) before += __shfl_down_sync(0xffffffffu, before, off);
+    before = __reduce_add_sync(0xffffffffu, before);
     if (lane == 0) s_warp[warp] = before;
     __syncthreads();
     int base = 0;
@@ -111,35 +132,36 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const EmbedGra
         const long long v = (static_cast<long long>(key) << a.bits) | b;
         if (key < a.keys && v < a.vocab) {
             a.range[static_cast<long long>(m) * a.vocab + v] = make_int2(at, total);
-#pragma unroll
-            for (int w = 0; w < SORT_WARPS; ++w) {
-                const int c = hist[w * a.keys + key];
-                hist[w * a.keys + key] = at;
-                at += c;
+            if (total >= a.piece) {
+                const long long ticket = static_cast<long long>(m) * a.pieces + Pieces(a, at, total).first;
+                for (int c = 0; c < a.columns; ++c) a.tickets[ticket * a.columns + c] = 0;
             }
+            if (total > 0)
+#pragma unroll
+                for (int w = 0; w < SORT_WARPS; ++w) {
+                    const int c = hist[w * a.keys + key];
+                    hist[w * a.keys + key] = at;
+                    at += c;
+                }
         }
         base += all;
     }
     if (b == mask && tid == 0) a.count[m] = base;
     __syncthreads();
     int *order = a.order + static_cast<long long>(m) * a.n;
-    for (long long i0 = lo; i0 < hi; i0 += 32 * SORT_AHEAD) {
-        int t[SORT_AHEAD];
-#pragma unroll
-        for (int k = 0; k < SORT_AHEAD; ++k) {
-            const long long i = i0 + 32 * k + lane;
-            t[k] = i < hi ? token_at(a.tokens, t0 + i * a.tokens.s1, a.vocab) : -1;
-        }
+    for (int i0 = lo; i0 < hi; i0 += 32 * SORT_AHEAD) {
+        if (!CACHED) load(i0);
 #pragma unroll
         for (int k = 0; k < SORT_AHEAD; ++k) {
             const bool is = t[k] >= 0 && (t[k] & mask) == b;
             const unsigned who = __ballot_sync(0xffffffffu, is);
+            if (who == 0) continue;
             if (is) {
                 const int key = t[k] >> a.bits;
                 const unsigned same = __match_any_sync(who, key);
                 const int rank = __popc(same & ((1u << lane) - 1));
                 const int at = mine[key];
-                order[at + rank] = static_cast<int>(i0 + 32 * k + lane);
+                order[at + rank] = i0 + 32 * k + lane;
                 __syncwarp(who);
                 if (rank == 0) mine[key] = at + __popc(same);
             }
@@ -149,131 +171,213 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const EmbedGra
 }
 
 // ---- sums --------------------------------------------------------------------------------------------
-// A run (the positions of one token) of `piece` or more tokens is cut into floor(length / piece) pieces of nearly equal length, summed by
-// a block each; the row's sum adds them in order.  Piece j of a run that begins at place s has number ceil(s / piece) + j: no two
-// runs' numbers meet, because ceil(a + b) >= ceil(a) + floor(b), and place number * piece lies in the run.
-struct Pieces {
-    int first, n;
-    __device__ __forceinline__ Pieces(const EmbedGradArgs &a, int2 run)
-        : first(static_cast<int>((static_cast<long long>(run.x) + a.piece - 1) / a.piece)), n(run.y / a.piece) {}
-};
+// One launch, blocks of two kinds: pieces of long runs, and rows of the gradient in order: the sums of short runs, and the zeros of rows without a
+// token, which are most of a large vocabulary.  Bound: HBM, rows of dout read and the gradient written.
+constexpr int SUM_THREADS = 256, SUM_WARPS = SUM_THREADS / 32;
+constexpr int MOST_ROWS = 64;      // rows of the gradient that a block takes, at most
+constexpr int PIECES_ASKED = 4;    // piece numbers that a block looks up: most stand for none
 
-template <int N>
-__device__ __forceinline__ void add_to(float (&acc)[N], const float (&f)[N]) {
+// acc += rows order[lo], order[lo + step], ... below hi, N columns from `base` on, in order.
+template <int N, typename ST>
+__device__ __forceinline__ void add_rows(float (&acc)[N], const ST *base, long long stride, const int *order, int lo, int hi, int step) {
+    constexpr int AHEAD = N * sizeof(ST) > 16 ? 2 : 4;
+    using Piece = std::conditional_t<N == 1, ST, uint4>;
+    constexpr int WORDS = N == 1 ? 1 : N * static_cast<int>(sizeof(ST)) / 16;   // (unpacked when they are added: a row in flight costs four registers)
+    for (int i0 = lo; i0 < hi; i0 += AHEAD * step) {
+        Piece w[AHEAD][WORDS];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] += f[e];
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * step < hi) {
+                const Piece *row = reinterpret_cast<const Piece *>(base + order[i0 + k * step] * stride);
+#pragma unroll
+                for (int q = 0; q < WORDS; ++q) w[k][q] = row[q];
+            }
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k)
+            if (i0 + k * step < hi) {
+                float f[N];
+                load_values(reinterpret_cast<const ST *>(w[k]), f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[e] += f[e];
+            }
+    }
 }
 
-constexpr int PIECE_WARPS = 8;
+template <int N, typename GT>
+__device__ __forceinline__ void write_sum(const EmbedGradArgs &a, GT *out, float (&acc)[N]) {
+    float old[N] = {};
+    if (a.accumulate) load_values(out, old);
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = a.accumulate ? fmaf(acc[e], a.scale, old[e]) : acc[e] * a.scale;
+    store_values(out, acc);
+}
 
-template <typename ST, int N>
-__global__ void __launch_bounds__(32 * PIECE_WARPS) run_pieces_kernel(const EmbedGradArgs a) {
-    __shared__ float sums[PIECE_WARPS][32 * N];
-    begin_and_let_next_begin();
-    wait_for_earlier_kernels();
-    const int p = blockIdx.x, m = blockIdx.z, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const long long place = static_cast<long long>(p) * a.piece;
-    if (place >= a.count[m]) return;
-    const int *order = a.order + static_cast<long long>(m) * a.n;
-    const int tok = token_at(a.tokens, m * a.tokens.s0 + order[place] * a.tokens.s1, a.vocab);
-    const int2 run = a.range[static_cast<long long>(m) * a.vocab + tok];
-    const Pieces pc(a, run);
-    const int j = p - pc.first;
-    if (j < 0 || j >= pc.n) return;
-    const int lo = run.x + static_cast<int>(static_cast<long long>(run.y) * j / pc.n);
-    const int hi = run.x + static_cast<int>(static_cast<long long>(run.y) * (j + 1) / pc.n);
-    const int col = static_cast<int>((blockIdx.y * 32 + lane) * N);
-    float acc[N] = {};
-    if (col < a.width) {
-        const ST *base = static_cast<const ST *>(a.dout) + m * a.ds0 + col;
-        for (int i0 = lo + warp; i0 < hi; i0 += 4 * PIECE_WARPS) {
-            float f[4][N];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i0 + k * PIECE_WARPS < hi) load_values(base + order[i0 + k * PIECE_WARPS] * a.ds1, f[k]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i0 + k * PIECE_WARPS < hi) add_to(acc, f[k]);
-        }
-    }
+// Sums of the warps' accs, in their order, N columns per lane: column lane * N + e of the block is sums[...][e * 32 + lane].  In warp 0.
+template <int N>
+__device__ __forceinline__ void join_warps(float (&acc)[N], float (*sums)[32 * N]) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int e = 0; e < N; ++e) sums[warp][e * 32 + lane] = acc[e];
     __syncthreads();
-    float *out = a.partial + (static_cast<long long>(m) * a.pieces + p) * a.row + static_cast<long long>(blockIdx.y) * 32 * N;
-    for (int c = threadIdx.x; c < 32 * N; c += 32 * PIECE_WARPS) {   // column c = lane * N + element
-        if (blockIdx.y * 32 * N + c >= static_cast<unsigned>(a.width)) break;
-        const int at = (c % N) * 32 + c / N;
-        float t = 0.f;
+    if (warp == 0)
 #pragma unroll
-        for (int w = 0; w < PIECE_WARPS; ++w) t += sums[w][at];
-        out[c] = t;
-    }
-}
-
-// The rows of the gradient.  A warp takes 32 * N columns of a row: the run's rows of dout in order, or the sums of its pieces, or
-// nothing but zeros to write.  Bound: HBM writes of the whole gradient.
-constexpr int ROWS_THREADS = 256, ROWS_PER_BLOCK = 16;
-
-template <typename ST, typename GT, int N>
-__global__ void __launch_bounds__(ROWS_THREADS) grad_rows_kernel(const EmbedGradArgs a) {
-    __shared__ int2 runs[ROWS_PER_BLOCK];
-    begin_and_let_next_begin();
-    const int m = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int v0 = static_cast<int>(blockIdx.x) * ROWS_PER_BLOCK, rows = min(ROWS_PER_BLOCK, a.vocab - v0);
-    wait_for_earlier_kernels();
-    if (static_cast<int>(threadIdx.x) < rows) runs[threadIdx.x] = a.range[static_cast<long long>(m) * a.vocab + v0 + threadIdx.x];
-    __syncthreads();
-    const int *order = a.order + static_cast<long long>(m) * a.n;
-    const int parts = (a.width + 32 * N - 1) / (32 * N);
-    for (long long u = warp; u < static_cast<long long>(rows) * parts; u += ROWS_THREADS / 32) {
-        const int r = static_cast<int>(u / parts), col = static_cast<int>((u - static_cast<long long>(r) * parts) * 32 + lane) * N;
-        const int2 run = runs[r];
-        if (col >= a.width || (run.y == 0 && a.accumulate)) continue;
-        float acc[N] = {};
-        if (run.y >= a.piece) {
-            const Pieces pc(a, run);
-            const float *sum = a.partial + (static_cast<long long>(m) * a.pieces + pc.first) * a.row + col;
-            for (int j0 = 0; j0 < pc.n; j0 += 4) {
-                float f[4][N];
+        for (int e = 0; e < N; ++e) {
+            acc[e] = 0.f;
 #pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (j0 + k < pc.n) load_values(sum + (j0 + k) * a.row, f[k]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (j0 + k < pc.n) add_to(acc, f[k]);
-            }
-        } else {
-            const ST *base = static_cast<const ST *>(a.dout) + m * a.ds0 + col;
-            for (int i0 = run.x; i0 < run.x + run.y; i0 += 4) {
-                float f[4][N];
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i0 + k < run.x + run.y) load_values(base + order[i0 + k] * a.ds1, f[k]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (i0 + k < run.x + run.y) add_to(acc, f[k]);
-            }
+            for (int w = 0; w < SUM_WARPS; ++w) acc[e] += sums[w][e * 32 + lane];
         }
-        GT *out = static_cast<GT *>(a.g[m]) + static_cast<long long>(v0 + r) * a.width + col;
-        float old[N] = {};
-        if (a.accumulate) load_values(out, old);
+}
+
+// A piece of a long run: place in the run's order, token, first place and length of the run.
+struct Piece {
+    int j, tok, start, length;
+};
+
+// Piece number p of worker m; j < 0 where it stands for none.
+__device__ __forceinline__ Piece find_piece(const EmbedGradArgs &a, int m, int p) {
+    const long long place = static_cast<long long>(p) * a.piece;
+    if (p >= a.pieces || place >= a.count[m]) return {-1, 0, 0, 0};
+    const int position = a.order[static_cast<long long>(m) * a.n + place];
+    const int tok = token_at(a.tokens, m * a.tokens.s0 + position * a.tokens.s1, a.vocab);
+    const int2 run = a.range[static_cast<long long>(m) * a.vocab + tok];
+    const Pieces pc(a, run.x, run.y);
+    const int j = p - pc.first;
+    return {j < pc.n ? j : -1, tok, run.x, run.y};
+}
+
+// 32 * N columns of a piece.  The last block of a run's to arrive adds the pieces in their order and writes the row.
+template <typename ST, typename GT, int N>
+__device__ __forceinline__ void sum_piece(const EmbedGradArgs &a, int m, const Piece &q, int c, float (*sums)[32 * N]) {
+    __shared__ int s_last;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Pieces pc(a, q.start, q.length);
+    const int lo = q.start + static_cast<int>(static_cast<long long>(q.length) * q.j / pc.n);
+    const int hi = q.start + static_cast<int>(static_cast<long long>(q.length) * (q.j + 1) / pc.n);
+    const int col = (c * 32 + lane) * N;
+    const bool in = col < a.width;
+    float acc[N] = {};
+    if (in) add_rows(acc, static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, a.order + static_cast<long long>(m) * a.n, lo + warp, hi, SUM_WARPS);
+    join_warps<N>(acc, sums);
+    GT *out = static_cast<GT *>(a.g[m]) + static_cast<long long>(q.tok) * a.width + col;
+    if (pc.n > 1) {
+        float *const part = a.partial + (static_cast<long long>(m) * a.pieces + pc.first) * a.row + col;
+        if (warp == 0) {
+            if (in) store_values(part + q.j * a.row, acc);
+            __threadfence();
+            __syncwarp();
+            if (lane == 0) s_last = atomicAdd(&a.tickets[(static_cast<long long>(m) * a.pieces + pc.first) * a.columns + c], 1) == pc.n - 1;
+        }
+        __syncthreads();
+        if (!s_last) return;
+        __threadfence();
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] = a.accumulate ? fmaf(acc[e], a.scale, old[e]) : acc[e] * a.scale;
-        store_values(out, acc);
+        for (int e = 0; e < N; ++e) acc[e] = 0.f;
+        if (in)
+            for (int k0 = warp; k0 < pc.n; k0 += 2 * SUM_WARPS) {
+                float f[2][N];
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (k0 + k * SUM_WARPS < pc.n)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) f[k][e] = __ldcg(part + (k0 + k * SUM_WARPS) * a.row + e);
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+                    if (k0 + k * SUM_WARPS < pc.n)
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[e] += f[k][e];
+            }
+        join_warps<N>(acc, sums);
+    }
+    if (warp == 0 && in) write_sum<N>(a, out, acc);
+}
+
+// Zeros over `bytes` bytes (a multiple of two) from p on, by a warp.
+__device__ __forceinline__ void zero_span(char *p, long long bytes) {
+    const int lane = threadIdx.x & 31;
+    const int head = static_cast<int>(min(bytes, static_cast<long long>((0 - reinterpret_cast<uintptr_t>(p)) & 15u)));
+    const long long wide = (bytes - head) / 16;
+    const int rest = static_cast<int>(bytes - head - 16 * wide);
+    if (2 * lane < head) *reinterpret_cast<unsigned short *>(p + 2 * lane) = 0;
+    uint4 *w = reinterpret_cast<uint4 *>(p + head);
+#pragma unroll 4
+    for (long long i = lane; i < wide; i += 32) w[i] = make_uint4(0, 0, 0, 0);
+    if (2 * lane < rest) *reinterpret_cast<unsigned short *>(p + head + 16 * wide + 2 * lane) = 0;
+}
+
+template <typename ST, typename GT, int N>
+__global__ void __launch_bounds__(SUM_THREADS, 5) grad_sums_kernel(const __grid_constant__ EmbedGradArgs a, unsigned piece_blocks, int block_rows) {
+    __shared__ float sums[SUM_WARPS][32 * N];
+    __shared__ Piece s_piece[PIECES_ASKED];
+    __shared__ int4 s_run[MOST_ROWS];   // row of the block, first place, length
+    __shared__ int s_runs;
+    __shared__ unsigned s_none[MOST_ROWS / 32];
+    begin_and_let_next_begin();
+    const int m = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (tid == 0) s_runs = 0;
+    wait_for_earlier_kernels();
+    if (blockIdx.x < piece_blocks) {
+        const int c = static_cast<int>(blockIdx.x % a.columns), p0 = static_cast<int>(blockIdx.x / a.columns) * PIECES_ASKED;
+        if (tid < PIECES_ASKED) s_piece[tid] = find_piece(a, m, p0 + tid);
+        __syncthreads();
+        for (int k = 0; k < PIECES_ASKED; ++k) {
+            const Piece q = s_piece[k];
+            if (q.j < 0) continue;
+            sum_piece<ST, GT, N>(a, m, q, c, sums);
+            __syncthreads();   // (what it shares is free again)
+        }
+        return;
+    }
+    const int v0 = static_cast<int>(blockIdx.x - piece_blocks) * block_rows, rows = min(block_rows, a.vocab - v0);
+    __syncthreads();
+    if (tid < MOST_ROWS) {
+        int2 run = make_int2(0, -1);
+        if (tid < rows) run = a.range[static_cast<long long>(m) * a.vocab + v0 + tid];
+        const unsigned none = __ballot_sync(0xffffffffu, run.y == 0);
+        if (lane == 0) s_none[warp] = none;
+        if (run.y > 0 && run.y < a.piece) s_run[atomicAdd(&s_runs, 1)] = make_int4(tid, run.x, run.y, 0);
+    }
+    __syncthreads();
+    GT *const out = static_cast<GT *>(a.g[m]) + static_cast<long long>(v0) * a.width;
+    if (!a.accumulate) {
+        // neighbouring rows of a warp's at once
+        const int each = (block_rows + SUM_WARPS - 1) / SUM_WARPS, r0 = warp * each;   // (each: 1, 2, 4 or 8)
+        unsigned todo = r0 < MOST_ROWS ? s_none[r0 / 32] >> (r0 % 32) & ((1u << each) - 1) : 0;
+        while (todo) {
+            const int r = __ffs(todo) - 1, n = __ffs(~(todo >> r)) - 1;
+            zero_span(reinterpret_cast<char *>(out + static_cast<long long>(r0 + r) * a.width), n * (static_cast<long long>(a.width) * sizeof(GT)));
+            todo &= ~(((1u << n) - 1) << r);
+        }
+    }
+    const unsigned across = static_cast<unsigned>((a.width + N - 1) / N), units = static_cast<unsigned>(s_runs) * across;
+    for (unsigned f = tid; f < units; f += SUM_THREADS) {
+        const unsigned i = f / across;
+        const int col = static_cast<int>(f - i * across) * N;
+        const int4 run = s_run[i];
+        float acc[N] = {};
+        add_rows(acc, static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, a.order + static_cast<long long>(m) * a.n, run.y, run.y + run.z, 1);
+        write_sum<N>(a, out + static_cast<long long>(run.x) * a.width + col, acc);
     }
 }
 
 template <typename ST, typename GT, int N>
-cudaError_t launch_sums(const EmbedGradArgs &a, int M, cudaStream_t stream, int *launches) {
-    const unsigned cols = static_cast<unsigned>((a.width + 32 * N - 1) / (32 * N));
-    if (a.pieces > 0) {
-        const cudaError_t e = launch_op(run_pieces_kernel<ST, N>, dim3(a.pieces, cols, M), dim3(32 * PIECE_WARPS), 0, true, stream, a);
-        if (e != cudaSuccess) return e;
-        *launches += 1;
-    }
-    const cudaError_t e = launch_op(grad_rows_kernel<ST, GT, N>, dim3((a.vocab + ROWS_PER_BLOCK - 1) / ROWS_PER_BLOCK, M), dim3(ROWS_THREADS), 0, true, stream, a);
-    if (e == cudaSuccess) *launches += 1;
-    return e;
+cudaError_t launch_sums(const EmbedGradArgs &a, int M, cudaStream_t stream) {
+    // rows per block: as many as leave several rounds of blocks
+    int rows = MOST_ROWS;
+    while (rows > 1 && static_cast<int64_t>(a.vocab) * M < static_cast<int64_t>(rows) * 148 * 16) rows /= 2;
+    const int64_t piece_blocks = (static_cast<int64_t>(a.pieces) + PIECES_ASKED - 1) / PIECES_ASKED * a.columns;
+    const int64_t blocks = piece_blocks + (static_cast<int64_t>(a.vocab) + rows - 1) / rows;
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;   // (beyond any memory)
+    return launch_op(grad_sums_kernel<ST, GT, N>, dim3(static_cast<unsigned>(blocks), M), dim3(SUM_THREADS), 0, true, stream, a,
+                     static_cast<unsigned>(piece_blocks), rows);
+}
+
+// Eight columns at a time where every row of both sides begins on a 16-byte boundary.
+bool eight_columns(const EmbedGradArgs &a, int M, bool dout_bf16, bool grad_bf16) {
+    const long long ssz = dout_bf16 ? 2 : 4, gsz = grad_bf16 ? 2 : 4;
+    uintptr_t off = reinterpret_cast<uintptr_t>(a.dout) | static_cast<uintptr_t>(a.ds0 * ssz) | static_cast<uintptr_t>(a.ds1 * ssz) |
+                    static_cast<uintptr_t>(a.width * gsz);
+    for (int m = 0; m < M; ++m) off |= reinterpret_cast<uintptr_t>(a.g[m]);
+    return (off & 15u) == 0 && a.width % 8 == 0;
 }
 
 }  // namespace
@@ -289,10 +393,11 @@ int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
     a.bits = 0;
     while (((a.vocab - 1) >> a.bits) + 1 > SORT_KEYS) ++a.bits;
     a.keys = ((a.vocab - 1) >> a.bits) + 1;
-    a.piece = 64;
-    while (4LL * a.piece * a.piece < a.n) a.piece *= 2;
+    a.piece = 32;
+    while (16LL * a.piece * a.piece < a.n) a.piece *= 2;
     a.pieces = a.n < a.piece ? 0 : (a.n - 1) / a.piece + 1;   // (a number is below n / piece: its place lies in a run)
     a.row = (static_cast<int64_t>(a.width) + 7) & ~int64_t{7};
+    a.columns = static_cast<int>((static_cast<int64_t>(a.width) + 31) / 32);   // (as many as there can be: of one column a lane)
     int64_t at = 0;
     const auto take = [&](int64_t bytes) {
         char *p = work ? work + at : nullptr;
@@ -302,27 +407,29 @@ int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
     a.range = reinterpret_cast<int2 *>(take(static_cast<int64_t>(M) * a.vocab * 8));
     a.order = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * a.n * 4));
     a.count = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * 4));
+    a.tickets = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * a.pieces * a.columns * 4));
     a.partial = reinterpret_cast<float *>(take(static_cast<int64_t>(M) * a.pieces * a.row * 4));
     return at;
 }
 
-cudaError_t launch_embed_grad(const EmbedGradArgs &a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches) {
+cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches) {
+    const bool wide = eight_columns(a, M, dout_bf16, grad_bf16);
+    a.columns = (a.width + (wide ? 255 : 31)) / (wide ? 256 : 32);
     const size_t smem = static_cast<size_t>(SORT_WARPS) * a.keys * sizeof(int);
-    const cudaError_t e = launch_op(token_sort_kernel, dim3(1u << a.bits, M), dim3(SORT_THREADS), smem, true, stream, a);
+    const auto sort = a.n <= SORT_CACHED ? (a.tokens.wide ? token_sort_kernel<true, true> : token_sort_kernel<true, false>)
+                                         : (a.tokens.wide ? token_sort_kernel<false, true> : token_sort_kernel<false, false>);
+    cudaError_t e = launch_op(sort, dim3(1u << a.bits, M), dim3(SORT_THREADS), smem, true, stream, a);
     if (e != cudaSuccess) return e;
     *launches = 1;
-    // eight columns at a time where every row of both sides begins on a 16-byte boundary
-    const long long ssz = dout_bf16 ? 2 : 4, gsz = grad_bf16 ? 2 : 4;
-    uintptr_t off = reinterpret_cast<uintptr_t>(a.dout) | static_cast<uintptr_t>(a.ds0 * ssz) | static_cast<uintptr_t>(a.ds1 * ssz) |
-                    static_cast<uintptr_t>(a.width * gsz);
-    for (int m = 0; m < M; ++m) off |= reinterpret_cast<uintptr_t>(a.g[m]);
-    const bool wide = (off & 15u) == 0 && a.width % 8 == 0;
     using bf = __nv_bfloat16;
     if (dout_bf16)
-        return grad_bf16 ? (wide ? launch_sums<bf, bf, 8> : launch_sums<bf, bf, 1>)(a, M, stream, launches)
-                         : (wide ? launch_sums<bf, float, 8> : launch_sums<bf, float, 1>)(a, M, stream, launches);
-    return grad_bf16 ? (wide ? launch_sums<float, bf, 8> : launch_sums<float, bf, 1>)(a, M, stream, launches)
-                     : (wide ? launch_sums<float, float, 8> : launch_sums<float, float, 1>)(a, M, stream, launches);
+        e = grad_bf16 ? (wide ? launch_sums<bf, bf, 8> : launch_sums<bf, bf, 1>)(a, M, stream)
+                      : (wide ? launch_sums<bf, float, 8> : launch_sums<bf, float, 1>)(a, M, stream);
+    else
+        e = grad_bf16 ? (wide ? launch_sums<float, bf, 8> : launch_sums<float, bf, 1>)(a, M, stream)
+                      : (wide ? launch_sums<float, float, 8> : launch_sums<float, float, 1>)(a, M, stream);
+    if (e == cudaSuccess) *launches = 2;
+    return e;
 }
 
 }  // namespace desloc

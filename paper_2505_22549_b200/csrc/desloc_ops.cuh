@@ -113,18 +113,20 @@ struct EmbedGradArgs {
     int accumulate;
     // How the sort is cut: tokens with the same last `bits` bits go to the same block, which tells `keys` numbers apart.
     int bits, keys;
-    int piece, pieces;       // tokens in a piece of a long run (a power of two), pieces of a worker
-    // Working memory.
+    int piece, pieces;       // places in a piece of a long run (a power of two), pieces of a worker at most
+    int columns;             // groups of columns that a piece's blocks take
+    // Working memory, all of it written before it is read.
     int2 *range;             // [M][vocab] first place and length of a token's run
     int *order;              // [M][n] positions sorted by token (the vocabulary in another order), ascending in a run
     int *count;              // [M] how many of them
+    int *tickets;            // [M][pieces][columns]: pieces of a long run that are done, at its first piece
     float *partial;          // [M][pieces][row]: sums of the pieces of long runs
     long long row;
     void *g[DESLOC_MAX_M];
 };
 // Fills in the plan and the pointers into `work`; the bytes that it takes.
 int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work);
-cudaError_t launch_embed_grad(const EmbedGradArgs &a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches);
+cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches);
 
 struct LogprobArgs {
     const void *x;
