@@ -47,11 +47,11 @@ __global__ void __launch_bounds__(EMBED_THREADS) embed_kernel(const EmbedArgs a)
 
 // ---- sort --------------------------------------------------------------------------------------------
 // Stable counting sort of a worker's tokens, a block for each value of the tokens' last bits: it goes over all of them twice, counts
-// its own and those of the blocks in front of it, and writes its part of the order and its runs (a run: the places of one token).  No
-// block waits for another.  Bound: latency; up to SORT_CACHED tokens stay in registers between the two times.
-constexpr int SORT_THREADS = 512, SORT_WARPS = SORT_THREADS / 32, SORT_AHEAD = 16;
+// its own and those of the blocks in front of it, and writes its places.  A run is the places of one token.  No block waits for another.
+// Bound: latency; up to SORT_CACHED tokens stay in registers between the two times.
+constexpr int SORT_THREADS = 256, SORT_WARPS = SORT_THREADS / 32, SORT_AHEAD = 16;
 constexpr int SORT_CACHED = SORT_THREADS * SORT_AHEAD;
-constexpr int SORT_KEYS = 760;   // most numbers that a block tells apart: counters of 47.5 KB
+constexpr int SORT_KEYS = 768;   // most numbers that a block tells apart: 30 KB of shared memory
 
 // A run of `piece` or more places is cut into floor(length / piece) pieces of nearly equal length, summed by a block each.  Piece j of
 // a run that begins at place s has number ceil(s / piece) + j: no two runs' numbers meet, because ceil(a + b) >= ceil(a) + floor(b), and
@@ -62,15 +62,68 @@ struct Pieces {
         : first((start + a.piece - 1) / a.piece), n(length / a.piece) {}
 };
 
-// WIDE: 64-bit token numbers.
-template <bool CACHED, bool WIDE>
-__global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_constant__ EmbedGradArgs a) {
+// Zeros over `bytes` bytes (a multiple of two) from p on, by a warp.
+__device__ __forceinline__ void zero_span(char *p, long long bytes) {
+    const int lane = threadIdx.x & 31;
+    const int head = static_cast<int>(min(bytes, static_cast<long long>((0 - reinterpret_cast<uintptr_t>(p)) & 15u)));
+    const long long wide = (bytes - head) / 16;
+    const int rest = static_cast<int>(bytes - head - 16 * wide);
+    if (2 * lane < head) *reinterpret_cast<unsigned short *>(p + 2 * lane) = 0;
+    uint4 *w = reinterpret_cast<uint4 *>(p + head);
+#pragma unroll 4
+    for (long long i = lane; i < wide; i += 32) w[i] = make_uint4(0, 0, 0, 0);
+    if (2 * lane < rest) *reinterpret_cast<unsigned short *>(p + head + 16 * wide + 2 * lane) = 0;
+}
+
+// Zeros in the rows [v0, v0 + rows) that have no bit in `seen`, rows / 8 of them (at most 16) by each of a block's eight warps,
+// neighbouring ones at once.
+template <typename GT>
+__device__ __forceinline__ void zero_rows(const EmbedGradArgs &a, int m, int v0, int each, unsigned seen) {
+    unsigned todo = ~seen & ((1u << min(each, max(a.vocab - v0, 0))) - 1);
+    GT *const out = static_cast<GT *>(a.g[m]);
+    while (todo) {
+        const int r = __ffs(todo) - 1, n = __ffs(~(todo >> r)) - 1;
+        zero_span(reinterpret_cast<char *>(out + static_cast<long long>(v0 + r) * a.width), n * (static_cast<long long>(a.width) * sizeof(GT)));
+        todo &= ~(((1u << n) - 1) << r);
+    }
+}
+
+// The rows [block * zero_rows, ...) of the gradient that no token of the worker's stands for: zeros.
+constexpr int MOST_ZERO_ROWS = 16 * SORT_WARPS, ZEROS_AHEAD = 16384;
+
+template <bool WIDE, typename GT>
+__device__ __forceinline__ void zero_block(const EmbedGradArgs &a, int m, unsigned block, int rows) {
     using Number = std::conditional_t<WIDE, long long, int>;
-    extern __shared__ int hist[];   // [warp][key]: counts, then places
+    __shared__ unsigned s_seen[MOST_ZERO_ROWS / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, v0 = static_cast<int>(block) * rows, each = rows / SORT_WARPS;
+    if (tid < MOST_ZERO_ROWS / 32) s_seen[tid] = 0;
+    __syncthreads();
+    wait_for_earlier_kernels();
+    const Number *const tokens = static_cast<const Number *>(a.tokens.data) + m * a.tokens.s0;
+#pragma unroll 8
+    for (int i = tid; i < a.n; i += SORT_THREADS) {
+        const auto r = static_cast<std::make_unsigned_t<Number>>(tokens[i * a.tokens.s1] - v0);
+        if (r < static_cast<unsigned>(rows)) atomicOr(&s_seen[r / 32], 1u << (r % 32));
+    }
+    __syncthreads();
+    zero_rows<GT>(a, m, v0 + warp * each, each, s_seen[warp * each / 32] >> (warp * each % 32));
+}
+
+// WIDE: 64-bit token numbers.  Behind the sort's own blocks, `zero_blocks` per worker that write the gradient's zeros meanwhile.
+template <bool CACHED, bool WIDE, typename GT>
+__global__ void __launch_bounds__(SORT_THREADS, 3) token_sort_kernel(const __grid_constant__ EmbedGradArgs a, int M, unsigned zero_blocks, int rows) {
+    using Number = std::conditional_t<WIDE, long long, int>;
+    extern __shared__ int hist[];   // [warp][key]: counts, then places; then [key] first place and length
     __shared__ int s_warp[SORT_WARPS];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.x, m = blockIdx.y, mask = (1 << a.bits) - 1;
-    int *mine = hist + warp * a.keys;
+    const unsigned sort_blocks = static_cast<unsigned>(M) << a.bits;
+    if (blockIdx.x >= sort_blocks) {
+        begin_and_let_next_begin();
+        const unsigned block = blockIdx.x - sort_blocks, m = block / zero_blocks;
+        return zero_block<WIDE, GT>(a, static_cast<int>(m), block - m * zero_blocks, rows);
+    }
+    const int mask = (1 << a.bits) - 1, b = static_cast<int>(blockIdx.x) & mask, m = static_cast<int>(blockIdx.x >> a.bits);
+    int *const mine = hist + warp * a.keys, *const run_start = hist + SORT_WARPS * a.keys, *const run_length = run_start + a.keys;
     begin_and_let_next_begin();
     for (int k = tid; k < SORT_WARPS * a.keys; k += SORT_THREADS) hist[k] = 0;
     __syncthreads();
@@ -81,9 +134,9 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_c
     const Number *const tokens = static_cast<const Number *>(a.tokens.data) + m * a.tokens.s0;
     int t[SORT_AHEAD];
     const auto load = [&](int i0) {
-        Number v[SORT_AHEAD];
         const Number *p = tokens + (i0 + lane) * a.tokens.s1;
         const long long step = 32 * a.tokens.s1;
+        Number v[SORT_AHEAD];
 #pragma unroll
         for (int k = 0; k < SORT_AHEAD; ++k) v[k] = i0 + 32 * k < hi - lane ? p[k * step] : -1;
 #pragma unroll
@@ -131,24 +184,27 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_c
         int at = base + front + upto - total;
         const long long v = (static_cast<long long>(key) << a.bits) | b;
         if (key < a.keys && v < a.vocab) {
-            a.range[static_cast<long long>(m) * a.vocab + v] = make_int2(at, total);
-            if (total >= a.piece) {
-                const long long ticket = static_cast<long long>(m) * a.pieces + Pieces(a, at, total).first;
-                for (int c = 0; c < a.columns; ++c) a.tickets[ticket * a.columns + c] = 0;
-            }
-            if (total > 0)
+            a.seen[static_cast<long long>(m) * a.vocab + v] = total > 0;
+            if (total > 0) {
+                run_start[key] = at;
+                run_length[key] = total;
+                if (total >= a.piece) {
+                    const long long ticket = static_cast<long long>(m) * a.pieces + Pieces(a, at, total).first;
+                    for (int c = 0; c < a.columns; ++c) a.tickets[ticket * a.columns + c] = 0;
+                }
 #pragma unroll
                 for (int w = 0; w < SORT_WARPS; ++w) {
                     const int c = hist[w * a.keys + key];
                     hist[w * a.keys + key] = at;
                     at += c;
                 }
+            }
         }
         base += all;
     }
     if (b == mask && tid == 0) a.count[m] = base;
     __syncthreads();
-    int *order = a.order + static_cast<long long>(m) * a.n;
+    int4 *const places = a.places + static_cast<long long>(m) * a.n;
     for (int i0 = lo; i0 < hi; i0 += 32 * SORT_AHEAD) {
         if (!CACHED) load(i0);
 #pragma unroll
@@ -161,7 +217,7 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_c
                 const unsigned same = __match_any_sync(who, key);
                 const int rank = __popc(same & ((1u << lane) - 1));
                 const int at = mine[key];
-                order[at + rank] = i0 + 32 * k + lane;
+                places[at + rank] = make_int4(i0 + 32 * k + lane, t[k], run_start[key], run_length[key]);
                 __syncwarp(who);
                 if (rank == 0) mine[key] = at + __popc(same);
             }
@@ -171,204 +227,196 @@ __global__ void __launch_bounds__(SORT_THREADS) token_sort_kernel(const __grid_c
 }
 
 // ---- sums --------------------------------------------------------------------------------------------
-// One launch, blocks of two kinds: pieces of long runs, and rows of the gradient in order: the sums of short runs, and the zeros of rows without a
-// token, which are most of a large vocabulary.  Bound: HBM, rows of dout read and the gradient written.
+// One launch; a warp takes 32 * N columns of a piece of a long run, or of the short runs that begin in TILE places.  Behind them (where the sort's launch
+// has not written them) zeros in the rows without a token, which are most of a large vocabulary.  No barriers: warps wait for their loads alone.
+// Bound: HBM, rows of dout read and the gradient written; then instructions, some 50 per row and 32 * N columns.
 constexpr int SUM_THREADS = 256, SUM_WARPS = SUM_THREADS / 32;
-constexpr int MOST_ROWS = 64;      // rows of the gradient that a block takes, at most
-constexpr int PIECES_ASKED = 4;    // piece numbers that a block looks up: most stand for none
+constexpr int TILE = 8;
 
-// acc += rows order[lo], order[lo + step], ... below hi, N columns from `base` on, in order.
+// Rows in flight, unpacked when they are added: a row costs four registers.
 template <int N, typename ST>
-__device__ __forceinline__ void add_rows(float (&acc)[N], const ST *base, long long stride, const int *order, int lo, int hi, int step) {
-    constexpr int AHEAD = N * sizeof(ST) > 16 ? 2 : 4;
-    using Piece = std::conditional_t<N == 1, ST, uint4>;
-    constexpr int WORDS = N == 1 ? 1 : N * static_cast<int>(sizeof(ST)) / 16;   // (unpacked when they are added: a row in flight costs four registers)
-    for (int i0 = lo; i0 < hi; i0 += AHEAD * step) {
-        Piece w[AHEAD][WORDS];
+struct RowWords {
+    using Word = std::conditional_t<N == 1, ST, uint4>;
+    static constexpr int WORDS = N == 1 ? 1 : N * static_cast<int>(sizeof(ST)) / 16;
+    Word w[WORDS];
+    __device__ __forceinline__ void load(const ST *p) {
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (i0 + k * step < hi) {
-                const Piece *row = reinterpret_cast<const Piece *>(base + order[i0 + k * step] * stride);
-#pragma unroll
-                for (int q = 0; q < WORDS; ++q) w[k][q] = row[q];
-            }
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (i0 + k * step < hi) {
-                float f[N];
-                load_values(reinterpret_cast<const ST *>(w[k]), f);
-#pragma unroll
-                for (int e = 0; e < N; ++e) acc[e] += f[e];
-            }
+        for (int q = 0; q < WORDS; ++q) w[q] = reinterpret_cast<const Word *>(p)[q];
     }
-}
-
-template <int N, typename GT>
-__device__ __forceinline__ void write_sum(const EmbedGradArgs &a, GT *out, float (&acc)[N]) {
-    float old[N] = {};
-    if (a.accumulate) load_values(out, old);
+    __device__ __forceinline__ void add_to(float (&acc)[N]) const {
+        float f[N];
+        load_values(reinterpret_cast<const ST *>(w), f);
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = a.accumulate ? fmaf(acc[e], a.scale, old[e]) : acc[e] * a.scale;
-    store_values(out, acc);
-}
-
-// Sums of the warps' accs, in their order, N columns per lane: column lane * N + e of the block is sums[...][e * 32 + lane].  In warp 0.
-template <int N>
-__device__ __forceinline__ void join_warps(float (&acc)[N], float (*sums)[32 * N]) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-#pragma unroll
-    for (int e = 0; e < N; ++e) sums[warp][e * 32 + lane] = acc[e];
-    __syncthreads();
-    if (warp == 0)
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            acc[e] = 0.f;
-#pragma unroll
-            for (int w = 0; w < SUM_WARPS; ++w) acc[e] += sums[w][e * 32 + lane];
-        }
-}
-
-// A piece of a long run: place in the run's order, token, first place and length of the run.
-struct Piece {
-    int j, tok, start, length;
+        for (int e = 0; e < N; ++e) acc[e] += f[e];
+    }
 };
 
-// Piece number p of worker m; j < 0 where it stands for none.
-__device__ __forceinline__ Piece find_piece(const EmbedGradArgs &a, int m, int p) {
-    const long long place = static_cast<long long>(p) * a.piece;
-    if (p >= a.pieces || place >= a.count[m]) return {-1, 0, 0, 0};
-    const int position = a.order[static_cast<long long>(m) * a.n + place];
-    const int tok = token_at(a.tokens, m * a.tokens.s0 + position * a.tokens.s1, a.vocab);
-    const int2 run = a.range[static_cast<long long>(m) * a.vocab + tok];
-    const Pieces pc(a, run.x, run.y);
-    const int j = p - pc.first;
-    return {j < pc.n ? j : -1, tok, run.x, run.y};
+template <int N, typename GT>
+__device__ __forceinline__ void write_sum(const EmbedGradArgs &a, GT *out, const float (&acc)[N]) {
+    float v[N] = {};
+    if (a.accumulate) load_values(out, v);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = a.accumulate ? fmaf(acc[e], a.scale, v[e]) : acc[e] * a.scale;
+    store_values(out, v);
 }
 
-// 32 * N columns of a piece.  The last block of a run's to arrive adds the pieces in their order and writes the row.
-template <typename ST, typename GT, int N>
-__device__ __forceinline__ void sum_piece(const EmbedGradArgs &a, int m, const Piece &q, int c, float (*sums)[32 * N]) {
-    __shared__ int s_last;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const Pieces pc(a, q.start, q.length);
-    const int lo = q.start + static_cast<int>(static_cast<long long>(q.length) * q.j / pc.n);
-    const int hi = q.start + static_cast<int>(static_cast<long long>(q.length) * (q.j + 1) / pc.n);
-    const int col = (c * 32 + lane) * N;
-    const bool in = col < a.width;
-    float acc[N] = {};
-    if (in) add_rows(acc, static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, a.order + static_cast<long long>(m) * a.n, lo + warp, hi, SUM_WARPS);
-    join_warps<N>(acc, sums);
-    GT *out = static_cast<GT *>(a.g[m]) + static_cast<long long>(q.tok) * a.width + col;
-    if (pc.n > 1) {
-        float *const part = a.partial + (static_cast<long long>(m) * a.pieces + pc.first) * a.row + col;
-        if (warp == 0) {
-            if (in) store_values(part + q.j * a.row, acc);
-            __threadfence();
-            __syncwarp();
-            if (lane == 0) s_last = atomicAdd(&a.tickets[(static_cast<long long>(m) * a.pieces + pc.first) * a.columns + c], 1) == pc.n - 1;
-        }
-        __syncthreads();
-        if (!s_last) return;
-        __threadfence();
-#pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] = 0.f;
-        if (in)
-            for (int k0 = warp; k0 < pc.n; k0 += 2 * SUM_WARPS) {
-                float f[2][N];
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    if (k0 + k * SUM_WARPS < pc.n)
-#pragma unroll
-                        for (int e = 0; e < N; ++e) f[k][e] = __ldcg(part + (k0 + k * SUM_WARPS) * a.row + e);
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    if (k0 + k * SUM_WARPS < pc.n)
-#pragma unroll
-                        for (int e = 0; e < N; ++e) acc[e] += f[k][e];
-            }
-        join_warps<N>(acc, sums);
-    }
-    if (warp == 0 && in) write_sum<N>(a, out, acc);
-}
-
-// Zeros over `bytes` bytes (a multiple of two) from p on, by a warp.
-__device__ __forceinline__ void zero_span(char *p, long long bytes) {
+// Adds the rows of dout at places [lo, hi), in order, N columns from `base` on per lane (`in`: there are any), and calls finish(acc, place) with the
+// sum behind every place whose bit is set in ends(first place of 32) and starts anew.  The lanes hold the positions of 32 places.
+template <int N, typename ST, typename Ends, typename Finish>
+__device__ __forceinline__ void add_places(const int4 *places, int n, int lo, int hi, const ST *base, long long stride, bool in, const Ends &ends,
+                                           const Finish &finish) {
+    constexpr int AHEAD = N * sizeof(ST) > 16 ? 4 : 8;
     const int lane = threadIdx.x & 31;
-    const int head = static_cast<int>(min(bytes, static_cast<long long>((0 - reinterpret_cast<uintptr_t>(p)) & 15u)));
-    const long long wide = (bytes - head) / 16;
-    const int rest = static_cast<int>(bytes - head - 16 * wide);
-    if (2 * lane < head) *reinterpret_cast<unsigned short *>(p + 2 * lane) = 0;
-    uint4 *w = reinterpret_cast<uint4 *>(p + head);
-#pragma unroll 4
-    for (long long i = lane; i < wide; i += 32) w[i] = make_uint4(0, 0, 0, 0);
-    if (2 * lane < rest) *reinterpret_cast<unsigned short *>(p + head + 16 * wide + 2 * lane) = 0;
+    float acc[N] = {};
+    for (int s0 = lo; s0 < hi; s0 += 32) {
+        const int4 q = places[min(s0 + lane, n - 1)];
+        const unsigned last = ends(q, s0 + lane);
+        const int upto = min(32, hi - s0);
+        for (int i0 = 0; i0 < upto; i0 += AHEAD) {
+            RowWords<N, ST> row[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i0 + k < upto) {
+                    const int position = __shfl_sync(0xffffffffu, q.x, i0 + k);
+                    if (in) row[k].load(base + position * stride);
+                }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k)
+                if (i0 + k < upto) {
+                    if (in) row[k].add_to(acc);
+                    if (last >> (i0 + k) & 1u) {
+                        finish(acc, __shfl_sync(0xffffffffu, q.y, i0 + k));
+#pragma unroll
+                        for (int e = 0; e < N; ++e) acc[e] = 0.f;
+                    }
+                }
+        }
+    }
 }
 
+// The short runs that begin in places [s0, s0 + TILE): their places follow one another from the first beginning on; a long run that begins
+// here is the last one.
 template <typename ST, typename GT, int N>
-__global__ void __launch_bounds__(SUM_THREADS, 5) grad_sums_kernel(const __grid_constant__ EmbedGradArgs a, unsigned piece_blocks, int block_rows) {
-    __shared__ float sums[SUM_WARPS][32 * N];
-    __shared__ Piece s_piece[PIECES_ASKED];
-    __shared__ int4 s_run[MOST_ROWS];   // row of the block, first place, length
-    __shared__ int s_runs;
-    __shared__ unsigned s_none[MOST_ROWS / 32];
+__device__ __forceinline__ void sum_runs(const EmbedGradArgs &a, int m, int s0, int col) {
+    const int lane = threadIdx.x & 31, count = a.count[m];
+    const int4 *const places = a.places + static_cast<long long>(m) * a.n;
+    const int4 q = places[min(s0 + lane % TILE, a.n - 1)];   // position, token, first place and length of the run (beyond `count`: anything)
+    const unsigned begins = __ballot_sync(0xffffffffu, lane < TILE && s0 + lane < count && q.z == s0 + lane);
+    if (begins == 0) return;
+    const int last = 31 - __clz(begins), length = __shfl_sync(0xffffffffu, q.w, last);
+    const bool in = col < a.width;
+    GT *const out = static_cast<GT *>(a.g[m]) + col;
+    add_places<N>(
+        places, a.n, s0 + __ffs(begins) - 1, s0 + last + (length < a.piece ? length : 0), static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, in,
+        [](const int4 &q, int place) { return __ballot_sync(0xffffffffu, place + 1 == q.z + q.w); },
+        [&](const float(&acc)[N], int tok) {
+            if (in) write_sum<N>(a, out + static_cast<long long>(tok) * a.width, acc);
+        });
+}
+
+// Piece number p of long runs, if it stands for one.  The last warp of a run's to arrive adds the pieces in their order and writes the row.
+template <typename ST, typename GT, int N>
+__device__ __forceinline__ void sum_piece(const EmbedGradArgs &a, int m, int p, int c, int col) {
+    const int lane = threadIdx.x & 31;
+    const long long place = static_cast<long long>(p) * a.piece;
+    const int4 *const places = a.places + static_cast<long long>(m) * a.n;
+    const int4 q = places[min(place, static_cast<long long>(a.n) - 1)];
+    if (place >= a.count[m]) return;
+    const Pieces pc(a, q.z, q.w);
+    const int j = p - pc.first;
+    if (j < 0 || j >= pc.n) return;
+    const int lo = q.z + static_cast<int>(static_cast<long long>(q.w) * j / pc.n), hi = q.z + static_cast<int>(static_cast<long long>(q.w) * (j + 1) / pc.n);
+    const bool in = col < a.width;
+    GT *const out = static_cast<GT *>(a.g[m]) + static_cast<long long>(q.y) * a.width + col;
+    float *const part = a.partial + (static_cast<long long>(m) * a.pieces + pc.first) * a.row + col;
+    add_places<N>(
+        places, a.n, lo, hi, static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, in,
+        [&](const int4 &, int place) { return __ballot_sync(0xffffffffu, place + 1 == hi); },
+        [&](const float(&acc)[N], int) {
+            if (pc.n == 1) {
+                if (in) write_sum<N>(a, out, acc);
+            } else if (in) {
+                store_values(part + j * a.row, acc);
+            }
+        });
+    if (pc.n == 1) return;
+    __threadfence();
+    __syncwarp();
+    int arrived = 0;
+    if (lane == 0) arrived = atomicAdd(&a.tickets[(static_cast<long long>(m) * a.pieces + pc.first) * a.columns + c], 1);
+    if (__shfl_sync(0xffffffffu, arrived, 0) != pc.n - 1) return;
+    __threadfence();
+    if (!in) return;
+    float acc[N] = {};
+    for (int k0 = 0; k0 < pc.n; k0 += 4) {
+        float f[4][N];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k0 + k < pc.n)
+#pragma unroll
+                for (int e = 0; e < N; e += N == 1 ? 1 : 4) {
+                    if constexpr (N == 1) {
+                        f[k][e] = __ldcg(part + (k0 + k) * a.row + e);
+                    } else {
+                        const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + (k0 + k) * a.row + e));
+                        f[k][e] = v.x, f[k][e + 1] = v.y, f[k][e + 2] = v.z, f[k][e + 3] = v.w;
+                    }
+                }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (k0 + k < pc.n)
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[e] += f[k][e];
+    }
+    write_sum<N>(a, out, acc);
+}
+
+struct SumBlocks {
+    unsigned pieces, runs, rows;   // blocks of each kind, per worker
+    int block_rows;                // rows that a block of the third kind takes
+};
+
+template <typename ST, typename GT, int N>
+__global__ void __launch_bounds__(SUM_THREADS, 4) grad_sums_kernel(const __grid_constant__ EmbedGradArgs a, const SumBlocks blocks, int M) {
     begin_and_let_next_begin();
-    const int m = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (tid == 0) s_runs = 0;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    unsigned block = blockIdx.x;
     wait_for_earlier_kernels();
-    if (blockIdx.x < piece_blocks) {
-        const int c = static_cast<int>(blockIdx.x % a.columns), p0 = static_cast<int>(blockIdx.x / a.columns) * PIECES_ASKED;
-        if (tid < PIECES_ASKED) s_piece[tid] = find_piece(a, m, p0 + tid);
-        __syncthreads();
-        for (int k = 0; k < PIECES_ASKED; ++k) {
-            const Piece q = s_piece[k];
-            if (q.j < 0) continue;
-            sum_piece<ST, GT, N>(a, m, q, c, sums);
-            __syncthreads();   // (what it shares is free again)
-        }
-        return;
+    // the pieces of all workers first: they take longest
+    if (block < (blocks.pieces + blocks.runs) * M) {
+        const bool piece = block < blocks.pieces * M;
+        if (!piece) block -= blocks.pieces * M;
+        const unsigned per = piece ? blocks.pieces : blocks.runs, m = block / per, unit = (block - m * per) * SUM_WARPS + warp, i = unit / a.columns;
+        const int c = static_cast<int>(unit - i * a.columns), col = (c * 32 + lane) * N;
+        if (piece) return sum_piece<ST, GT, N>(a, static_cast<int>(m), static_cast<int>(i), c, col);
+        return sum_runs<ST, GT, N>(a, static_cast<int>(m), static_cast<int>(i) * TILE, col);
     }
-    const int v0 = static_cast<int>(blockIdx.x - piece_blocks) * block_rows, rows = min(block_rows, a.vocab - v0);
-    __syncthreads();
-    if (tid < MOST_ROWS) {
-        int2 run = make_int2(0, -1);
-        if (tid < rows) run = a.range[static_cast<long long>(m) * a.vocab + v0 + tid];
-        const unsigned none = __ballot_sync(0xffffffffu, run.y == 0);
-        if (lane == 0) s_none[warp] = none;
-        if (run.y > 0 && run.y < a.piece) s_run[atomicAdd(&s_runs, 1)] = make_int4(tid, run.x, run.y, 0);
-    }
-    __syncthreads();
-    GT *const out = static_cast<GT *>(a.g[m]) + static_cast<long long>(v0) * a.width;
-    if (!a.accumulate) {
-        // neighbouring rows of a warp's at once
-        const int each = (block_rows + SUM_WARPS - 1) / SUM_WARPS, r0 = warp * each;   // (each: 1, 2, 4 or 8)
-        unsigned todo = r0 < MOST_ROWS ? s_none[r0 / 32] >> (r0 % 32) & ((1u << each) - 1) : 0;
-        while (todo) {
-            const int r = __ffs(todo) - 1, n = __ffs(~(todo >> r)) - 1;
-            zero_span(reinterpret_cast<char *>(out + static_cast<long long>(r0 + r) * a.width), n * (static_cast<long long>(a.width) * sizeof(GT)));
-            todo &= ~(((1u << n) - 1) << r);
-        }
-    }
-    const unsigned across = static_cast<unsigned>((a.width + N - 1) / N), units = static_cast<unsigned>(s_runs) * across;
-    for (unsigned f = tid; f < units; f += SUM_THREADS) {
-        const unsigned i = f / across;
-        const int col = static_cast<int>(f - i * across) * N;
-        const int4 run = s_run[i];
-        float acc[N] = {};
-        add_rows(acc, static_cast<const ST *>(a.dout) + m * a.ds0 + col, a.ds1, a.order + static_cast<long long>(m) * a.n, run.y, run.y + run.z, 1);
-        write_sum<N>(a, out + static_cast<long long>(run.x) * a.width + col, acc);
-    }
+    block -= (blocks.pieces + blocks.runs) * M;
+    const unsigned m = block / blocks.rows;
+    const int each = blocks.block_rows / SUM_WARPS, v0 = static_cast<int>(block - m * blocks.rows) * blocks.block_rows + warp * each;
+    const unsigned seen = __ballot_sync(0xffffffffu, lane < each && v0 + lane < a.vocab && a.seen[static_cast<long long>(m) * a.vocab + v0 + lane]);
+    zero_rows<GT>(a, static_cast<int>(m), v0, each, seen);
 }
 
 template <typename ST, typename GT, int N>
-cudaError_t launch_sums(const EmbedGradArgs &a, int M, cudaStream_t stream) {
-    // rows per block: as many as leave several rounds of blocks
-    int rows = MOST_ROWS;
-    while (rows > 1 && static_cast<int64_t>(a.vocab) * M < static_cast<int64_t>(rows) * 148 * 16) rows /= 2;
-    const int64_t piece_blocks = (static_cast<int64_t>(a.pieces) + PIECES_ASKED - 1) / PIECES_ASKED * a.columns;
-    const int64_t blocks = piece_blocks + (static_cast<int64_t>(a.vocab) + rows - 1) / rows;
-    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;   // (beyond any memory)
-    return launch_op(grad_sums_kernel<ST, GT, N>, dim3(static_cast<unsigned>(blocks), M), dim3(SUM_THREADS), 0, true, stream, a,
-                     static_cast<unsigned>(piece_blocks), rows);
+cudaError_t launch_sums(const EmbedGradArgs &a, int M, int64_t zero_blocks, int rows, cudaStream_t stream) {
+    const auto blocks_of = [&](int64_t units) { return (units * a.columns + SUM_WARPS - 1) / SUM_WARPS; };
+    const int64_t pieces = blocks_of(a.pieces), runs = blocks_of((static_cast<int64_t>(a.n) + TILE - 1) / TILE);
+    const int64_t all = (pieces + runs + zero_blocks) * M;
+    if (all == 0) return cudaSuccess;
+    if (all > 0x7fffffff) return cudaErrorInvalidConfiguration;   // (beyond any memory)
+    const SumBlocks blocks{static_cast<unsigned>(pieces), static_cast<unsigned>(runs), static_cast<unsigned>(zero_blocks), rows};
+    return launch_op(grad_sums_kernel<ST, GT, N>, dim3(static_cast<unsigned>(all)), dim3(SUM_THREADS), 0, true, stream, a, blocks, M);
+}
+
+template <typename GT>
+cudaError_t launch_sort(const EmbedGradArgs &a, int M, int64_t zero_blocks, int rows, cudaStream_t stream) {
+    const size_t smem = static_cast<size_t>(SORT_WARPS + 2) * a.keys * sizeof(int);
+    const int64_t all = ((int64_t{1} << a.bits) + zero_blocks) * M;
+    if (all > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    const auto kernel = a.n <= SORT_CACHED ? (a.tokens.wide ? token_sort_kernel<true, true, GT> : token_sort_kernel<true, false, GT>)
+                                           : (a.tokens.wide ? token_sort_kernel<false, true, GT> : token_sort_kernel<false, false, GT>);
+    return launch_op(kernel, dim3(static_cast<unsigned>(all)), dim3(SORT_THREADS), smem, true, stream, a, M, static_cast<unsigned>(zero_blocks), rows);
 }
 
 // Eight columns at a time where every row of both sides begins on a 16-byte boundary.
@@ -390,9 +438,11 @@ cudaError_t launch_embed(const EmbedArgs &a, int M, bool bf16, cudaStream_t stre
 }
 
 int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
+    // As few blocks as their counters allow (each goes over all tokens), but enough of them.
     a.bits = 0;
-    while (((a.vocab - 1) >> a.bits) + 1 > SORT_KEYS) ++a.bits;
-    a.keys = ((a.vocab - 1) >> a.bits) + 1;
+    const auto keys = [&] { return ((a.vocab - 1) >> a.bits) + 1; };
+    while (keys() > SORT_KEYS || (keys() > 64 && (static_cast<int64_t>(M) << a.bits) < 128)) ++a.bits;
+    a.keys = keys();
     a.piece = 32;
     while (16LL * a.piece * a.piece < a.n) a.piece *= 2;
     a.pieces = a.n < a.piece ? 0 : (a.n - 1) / a.piece + 1;   // (a number is below n / piece: its place lies in a run)
@@ -404,8 +454,8 @@ int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
         at += (bytes + 255) & ~int64_t{255};
         return p;
     };
-    a.range = reinterpret_cast<int2 *>(take(static_cast<int64_t>(M) * a.vocab * 8));
-    a.order = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * a.n * 4));
+    a.seen = reinterpret_cast<unsigned char *>(take(static_cast<int64_t>(M) * a.vocab));
+    a.places = reinterpret_cast<int4 *>(take(static_cast<int64_t>(M) * a.n * 16));
     a.count = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * 4));
     a.tickets = reinterpret_cast<int *>(take(static_cast<int64_t>(M) * a.pieces * a.columns * 4));
     a.partial = reinterpret_cast<float *>(take(static_cast<int64_t>(M) * a.pieces * a.row * 4));
@@ -415,19 +465,22 @@ int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
 cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches) {
     const bool wide = eight_columns(a, M, dout_bf16, grad_bf16);
     a.columns = (a.width + (wide ? 255 : 31)) / (wide ? 256 : 32);
-    const size_t smem = static_cast<size_t>(SORT_WARPS) * a.keys * sizeof(int);
-    const auto sort = a.n <= SORT_CACHED ? (a.tokens.wide ? token_sort_kernel<true, true> : token_sort_kernel<true, false>)
-                                         : (a.tokens.wide ? token_sort_kernel<false, true> : token_sort_kernel<false, false>);
-    cudaError_t e = launch_op(sort, dim3(1u << a.bits, M), dim3(SORT_THREADS), smem, true, stream, a);
+    // Zeros: written while the tokens are sorted, by blocks that look all of them up themselves; beyond ZEROS_AHEAD tokens, where that takes
+    // too long, behind the sort, which knows.  Rows per block: 128, fewer where that leaves too few blocks.
+    int rows = MOST_ZERO_ROWS;
+    while (rows > SORT_WARPS && static_cast<int64_t>(a.vocab) * M < static_cast<int64_t>(rows) * 148 * 4) rows /= 2;
+    const int64_t zero_blocks = a.accumulate ? 0 : (static_cast<int64_t>(a.vocab) + rows - 1) / rows;
+    const int64_t ahead = a.n <= ZEROS_AHEAD ? zero_blocks : 0, behind = zero_blocks - ahead;
+    cudaError_t e = grad_bf16 ? launch_sort<__nv_bfloat16>(a, M, ahead, rows, stream) : launch_sort<float>(a, M, ahead, rows, stream);
     if (e != cudaSuccess) return e;
     *launches = 1;
     using bf = __nv_bfloat16;
     if (dout_bf16)
-        e = grad_bf16 ? (wide ? launch_sums<bf, bf, 8> : launch_sums<bf, bf, 1>)(a, M, stream)
-                      : (wide ? launch_sums<bf, float, 8> : launch_sums<bf, float, 1>)(a, M, stream);
+        e = grad_bf16 ? (wide ? launch_sums<bf, bf, 8> : launch_sums<bf, bf, 1>)(a, M, behind, rows, stream)
+                      : (wide ? launch_sums<bf, float, 8> : launch_sums<bf, float, 1>)(a, M, behind, rows, stream);
     else
-        e = grad_bf16 ? (wide ? launch_sums<float, bf, 8> : launch_sums<float, bf, 1>)(a, M, stream)
-                      : (wide ? launch_sums<float, float, 8> : launch_sums<float, float, 1>)(a, M, stream);
+        e = grad_bf16 ? (wide ? launch_sums<float, bf, 8> : launch_sums<float, bf, 1>)(a, M, behind, rows, stream)
+                      : (wide ? launch_sums<float, float, 8> : launch_sums<float, float, 1>)(a, M, behind, rows, stream);
     if (e == cudaSuccess) *launches = 2;
     return e;
 }

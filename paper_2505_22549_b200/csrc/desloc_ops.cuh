@@ -116,8 +116,9 @@ struct EmbedGradArgs {
     int piece, pieces;       // places in a piece of a long run (a power of two), pieces of a worker at most
     int columns;             // groups of columns that a piece's blocks take
     // Working memory, all of it written before it is read.
-    int2 *range;             // [M][vocab] first place and length of a token's run
-    int *order;              // [M][n] positions sorted by token (the vocabulary in another order), ascending in a run
+    unsigned char *seen;     // [M][vocab] whether the token occurs
+    int4 *places;            // [M][n] position, token, first place and length of the token's run: sorted by token (the vocabulary in another
+                             // order), then by position
     int *count;              // [M] how many of them
     int *tickets;            // [M][pieces][columns]: pieces of a long run that are done, at its first piece
     float *partial;          // [M][pieces][row]: sums of the pieces of long runs
