@@ -19,48 +19,152 @@ __device__ __forceinline__ float exp2_fast(float t) {
     return r;
 }
 
-// Running softmax of a part of a row: largest value m, S = sum of 2^t and A = sum of t 2^t with t = (x - m) log2 e.
-// Parts without values (or of nothing but -inf) have m = -FLT_MAX and S = 0; NaN and +inf end in a NaN S.
+// Running softmax of a part of a row: largest value m, S = sum of 2^t and A = sum of t 2^t, with t = x log2 e - base(m), one rounding: the
+// rounding of base(m) = m log2 e is the same in every term, and log_sum_of() takes it out again.  Rows whose largest value is beyond HUGE_LOGIT, where that
+// rounding is no small exponent, have t = (x - m) log2 e.  Parts without values (or of nothing but -inf) have m = -FLT_MAX and S = 0; NaN and +inf end in a NaN S.
 struct Running {
     float m, S, A;
 };
+constexpr float HUGE_LOGIT = 1e6f, LOWEST_LOGIT = -1e37f;
+__device__ __forceinline__ float base_of(float m) { return __fmul_rn(m, LOG2E); }
+__device__ __forceinline__ bool is_huge(float m) { return fabsf(m) > HUGE_LOGIT; }
+__device__ __forceinline__ float behind_base(float m) { return fmaf(m, LOG2E, -base_of(m)); }   // what the rounding took
 
 template <bool ENT>
 __device__ __forceinline__ void raise_to(Running &r, float m) {
-    const float d = fmaxf((r.m - m) * LOG2E, FAR_BELOW), f = exp2_fast(d);
+    float d = base_of(r.m) - base_of(m);
+    if (is_huge(r.m) || is_huge(m)) d = is_huge(r.m) && is_huge(m) ? (r.m - m) * LOG2E : is_huge(m) ? d - behind_base(m) : d + behind_base(r.m);
+    d = fmaxf(d, FAR_BELOW);   // (NaN, of infinities, too)
+    const float f = exp2_fast(d);
     if constexpr (ENT) r.A = f * fmaf(r.S, d, r.A);
     r.S *= f;
     r.m = m;
 }
 
-template <bool ENT>
-__device__ __forceinline__ Running join(Running a, Running b) {
-    const float m = fmaxf(a.m, b.m);
-    raise_to<ENT>(a, m);
-    raise_to<ENT>(b, m);
-    return {m, a.S + b.S, ENT ? a.A + b.A : 0.f};
+// The lanes' sums as one, in all of them: of groups of LANES.
+template <bool ENT, int LANES>
+__device__ __forceinline__ Running join_lanes(Running r) {
+    float m = r.m;
+#pragma unroll
+    for (int off = LANES / 2; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, off));
+    raise_to<ENT>(r, m);
+#pragma unroll
+    for (int off = LANES / 2; off > 0; off >>= 1) {
+        r.S += __shfl_xor_sync(0xffffffffu, r.S, off);
+        if constexpr (ENT) r.A += __shfl_xor_sync(0xffffffffu, r.A, off);
+    }
+    return r;
 }
 
-template <bool ENT, int N>
-__device__ __forceinline__ void take(Running &r, const float (&f)[N]) {
-    float top = f[0];
+// One value.
+template <bool ENT>
+__device__ __forceinline__ void take(Running &r, float x) {
+    if (x > r.m) raise_to<ENT>(r, x);
+    const float t = is_huge(r.m) ? (x - r.m) * LOG2E : fmaf(x, LOG2E, -base_of(r.m)), e = exp2_fast(t);
+    r.S += e;
+    if constexpr (ENT) r.A = fmaf(e, fmaxf(t, FAR_BELOW), r.A);
+}
+
+// log sum exp(x - m).
+__device__ __forceinline__ float log_sum_of(const Running &r) {
+    const float l = logf(r.S);
+    return is_huge(r.m) ? l : l - LN2 * behind_base(r.m);
+}
+
+// Sixteen bytes of a row as values; the largest of several; what stands in the place of missing ones.
+template <typename T>
+struct Words;
+template <>
+struct Words<float> {
+    static constexpr uint32_t NONE = 0xff800000u;   // -inf
+    static __device__ __forceinline__ float2 pair(const uint4 &w, int k) {
+        return k == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w));
+    }
+    template <int N>
+    static __device__ __forceinline__ float largest(const uint4 (&w)[N]) {
+        float m = -INFINITY;
 #pragma unroll
-    for (int k = 1; k < N; ++k) top = fmaxf(top, f[k]);
+        for (int k = 0; k < N; ++k)
+            m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), fmaxf(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
+        return m;
+    }
+    // -inf becomes a finite value whose exponential is 0 all the same; NaN stays
+    static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+        float r;
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(LOWEST_LOGIT));
+        return __float_as_uint(r);
+    }
+};
+template <>
+struct Words<__nv_bfloat16> {
+    static constexpr uint32_t NONE = 0xff80ff80u;
+    static __device__ __forceinline__ float2 pair(const uint4 &w, int k) {
+        const uint32_t v = k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w;
+        return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t b) {
+        uint32_t r;
+        asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+        return r;
+    }
+    template <int N>
+    static __device__ __forceinline__ float largest(const uint4 (&w)[N]) {
+        uint32_t m = NONE;
+#pragma unroll
+        for (int k = 0; k < N; ++k) m = larger(m, larger(larger(w[k].x, w[k].y), larger(w[k].z, w[k].w)));
+        return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+        uint32_t r;
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0xfcf0fcf0u));   // LOWEST_LOGIT
+        return r;
+    }
+};
+
+// A piece, value by value: of rows with values beyond HUGE_LOGIT only.
+template <typename T, bool ENT>
+__device__ __noinline__ Running take_slowly(Running r, uint4 w) {
+#pragma unroll
+    for (int e = 0; e < 8 / static_cast<int>(sizeof(T)); ++e) {
+        const float2 x = Words<T>::pair(w, e);
+        take<ENT>(r, x.x);
+        take<ENT>(r, x.y);
+    }
+    return r;
+}
+
+// N pieces, two values per instruction.
+template <typename T, bool ENT, int N>
+__device__ __forceinline__ void take_pieces(Running &r, uint4 (&w)[N]) {
+    const float top = Words<T>::largest(w);
     if (top > r.m) raise_to<ENT>(r, top);
+    if (is_huge(r.m)) {
+#pragma unroll
+        for (int k = 0; k < N; ++k) r = take_slowly<T, ENT>(r, w[k]);
+        return;
+    }
+    const float b = base_of(r.m);
+    const float2 scale = make_float2(LOG2E, LOG2E), from = make_float2(-b, -b);
+    float2 S = make_float2(r.S, 0.f), A = make_float2(ENT ? r.A : 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        const float t = (f[k] - r.m) * LOG2E, e = exp2_fast(t);
-        r.S += e;
-        if constexpr (ENT) r.A = fmaf(e, fmaxf(t, FAR_BELOW), r.A);
+        if constexpr (ENT) w[k] = make_uint4(Words<T>::finite(w[k].x), Words<T>::finite(w[k].y), Words<T>::finite(w[k].z), Words<T>::finite(w[k].w));
+#pragma unroll
+        for (int e = 0; e < 8 / static_cast<int>(sizeof(T)); ++e) {
+            const float2 t = __ffma2_rn(Words<T>::pair(w[k], e), scale, from), p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+            S = __fadd2_rn(S, p);
+            if constexpr (ENT) A = __ffma2_rn(p, t, A);
+        }
     }
+    r.S = S.x + S.y;
+    if constexpr (ENT) r.A = A.x + A.y;
 }
 
-// Lanes' values, the largest first.  MERGE: the lanes already hold one sequence that falls and then rises, or the other way round.
-template <bool MERGE>
+// Lanes' values, the largest first.
 __device__ __forceinline__ float sort_lanes(float v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int k = MERGE ? 32 : 2; k <= 32; k <<= 1) {
+    for (int k = 2; k <= 32; k <<= 1) {
 #pragma unroll
         for (int j = k >> 1; j > 0; j >>= 1) {
             const float o = __shfl_xor_sync(0xffffffffu, v, j);
@@ -93,23 +197,24 @@ struct Part {
     __device__ __forceinline__ int tail_at(int i) const { return head + pieces * PER + i; }
 };
 
-// visit(place in the part, value) of all that thread `tid` of `threads` takes, as logprobs_row() took them before.
-template <typename T, typename F>
-__device__ __forceinline__ void visit_own(const Part<T> &part, int tid, int threads, const F &visit) {
-    if (tid < part.head) visit(tid, static_cast<float>(part.p[tid]));
-    if (tid < part.tail) visit(part.tail_at(tid), static_cast<float>(part.p[part.tail_at(tid)]));
-#pragma unroll 4
-    for (int i = tid; i < part.pieces; i += threads) {
+// visit(place in the part, value) of all that thread `tid` of THREADS takes in logprobs_row(), lane `lane` of `lanes` that share them.
+template <int THREADS, typename T, typename F>
+__device__ __forceinline__ void visit_own(const Part<T> &part, int tid, int lane, int lanes, const F &visit) {
+    if (lane == 0 && tid < part.head) visit(tid, static_cast<float>(part.p[tid]));
+    if (lane == 0 && tid < part.tail) visit(part.tail_at(tid), static_cast<float>(part.p[part.tail_at(tid)]));
+    for (long long i = tid + lane * THREADS; i < part.pieces; i += lanes * THREADS) {
+        const int at = part.piece_at(static_cast<int>(i));
         float f[Part<T>::PER];
-        load_values(part.p + part.piece_at(i), f);
+        load_values(part.p + at, f);
 #pragma unroll
-        for (int k = 0; k < Part<T>::PER; ++k) visit(part.piece_at(i) + k, f[k]);
+        for (int k = 0; k < Part<T>::PER; ++k) visit(at + k, f[k]);
     }
 }
 
 template <int THREADS>
 struct TopShared {
-    float sorted[THREADS / 32][32];
+    float own[THREADS / 32][32];
+    float line;
     float value[CANDIDATES];
     int place[CANDIDATES];
     int n;
@@ -118,20 +223,16 @@ struct TopShared {
     unsigned long long best[THREADS / 32];
 };
 
-// The candidates' order: larger values first, lower places among equals.  Writes the first `top` of them, -1 where there are fewer.
-template <int THREADS>
-__device__ __forceinline__ void rank_candidates(TopShared<THREADS> &s, int n, int top) {
-    const int tid = threadIdx.x;
-    for (int i = tid; i < MOST_TOP; i += THREADS) s.out_value[i] = -INFINITY, s.out_place[i] = -1;
-    __syncthreads();
-    for (int i = tid; i < n; i += THREADS) {
+// The candidates' order: larger values first, lower places among equals (those that stand for nothing in a cluster's lists, -inf, have one place).  put(rank, value, place) for the first `top` of them.
+template <int THREADS, typename Put>
+__device__ __forceinline__ void rank_candidates(const TopShared<THREADS> &s, int n, int top, const Put &put) {
+    for (int i = threadIdx.x; i < n; i += THREADS) {
         const float v = s.value[i];
         const int at = s.place[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += s.value[j] > v || (s.value[j] == v && s.place[j] < at);
-        if (rank < top && v > -INFINITY) s.out_value[rank] = v, s.out_place[rank] = at;
+        for (int j = 0; j < n; ++j) rank += s.value[j] > v || (s.value[j] == v && (s.place[j] < at || (s.place[j] == at && j < i)));
+        if (rank < top) put(rank, v, at);
     }
-    __syncthreads();
 }
 
 // The `top` largest values of a part, whatever they are: goes over the part in order and puts what beats the last of the list into it, one at
@@ -193,39 +294,39 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
     }
 }
 
-// The `top` largest values of a part into s.out_*.  `own`: the largest that this thread has seen (-FLT_MAX: none).  The line is the top-th largest of the
-// threads' largest values: at least `top` values lie at or above it (all values, where fewer threads have any), only threads whose largest does have
-// such, and these look at what they took once more (some hundred bytes each, from L2).
+// Candidates for the `top` largest values of a part into s.value and s.place; how many, which may be more than there is room for.  s.own holds the largest
+// that each thread has seen (-FLT_MAX: none), behind a barrier.  The line is the top-th largest of 32 groups' of threads largest values: at least
+// `top` values lie at or above it (all values, where fewer groups have any), only threads whose largest does have such, and their warps look at what these
+// took once more (some hundred bytes each, from L2).
 template <typename T, int THREADS>
-__device__ __forceinline__ void top_of_part(const Part<T> &part, TopShared<THREADS> &s, float own, int top) {
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    s.sorted[warp][lane] = sort_lanes<false>(own);
-    if (tid == 0) s.n = 0;
-    __syncthreads();
+__device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared<THREADS> &s, float own, int top) {
+    const int tid = threadIdx.x;
+    if (tid < 32) {
+        float m = s.own[0][tid];
 #pragma unroll
-    for (int half = THREADS / 64; half > 0; half >>= 1) {
-        if (warp < half) s.sorted[warp][lane] = sort_lanes<true>(fmaxf(s.sorted[warp][lane], s.sorted[warp + half][31 - lane]));
-        __syncthreads();
+        for (int w = 1; w < THREADS / 32; ++w) m = fmaxf(m, s.own[w][tid]);
+        m = sort_lanes(m);
+        if (tid == top - 1) s.line = m;
+        if (tid == 0) s.n = 0;
     }
-    const float line = s.sorted[0][top - 1];
-    if (own >= line)
-        visit_own(part, tid, THREADS, [&](int at, float x) {
+    __syncthreads();
+    const float line = s.line;
+    for (unsigned who = __ballot_sync(0xffffffffu, own >= line); who; who &= who - 1)
+        visit_own<THREADS>(part, (tid & ~31) + __ffs(who) - 1, tid & 31, 32, [&](int at, float x) {
             if (x >= line) {
                 const int i = atomicAdd(&s.n, 1);
                 if (i < CANDIDATES) s.value[i] = x, s.place[i] = at;
             }
         });
     __syncthreads();
-    const int n = s.n;
-    if (n <= CANDIDATES) rank_candidates(s, n, top);
-    else top_in_order<T, THREADS>(part, s, top);
+    return s.n;
 }
 
 // A block per row, or a cluster of CL blocks that take a part of it each and hand what they found to the first one through its shared
-// memory.  Bound: HBM reads of the logits, once; 16-byte loads, four in flight per thread.
+// memory.  Bound: HBM reads of the logits, once; 16-byte loads, four to eight in flight per thread.
 template <typename T, bool ENT, bool TOP, int THREADS, int CL>
 __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
-    constexpr int PER = Part<T>::PER, WARPS = THREADS / 32;
+    constexpr int WARPS = THREADS / 32, AHEAD = 4;
     __shared__ Running s_warp[WARPS];
     __shared__ Running s_part[CL];
     __shared__ TopShared<TOP ? THREADS : 32> top;
@@ -247,40 +348,47 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
         if (tok >= 0) x_tok = static_cast<float>(x[tok]);
     }
     Running r{-FLT_MAX, 0.f, 0.f};
-    if (tid < part.head) {
-        const float f[1] = {static_cast<float>(part.p[tid])};
-        take<ENT>(r, f);
-    }
-    if (tid < part.tail) {
-        const float f[1] = {static_cast<float>(part.p[part.tail_at(tid)])};
-        take<ENT>(r, f);
-    }
-    for (int b = tid; b < part.pieces; b += 4 * THREADS) {
-        float f[4][PER];
+    const uint4 *const pieces = reinterpret_cast<const uint4 *>(part.p + part.head);
+    const auto load = [&](uint4(&w)[AHEAD], int b) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            if (b + k * THREADS < part.pieces) load_values(part.p + part.piece_at(b + k * THREADS), f[k]);
-            else
-#pragma unroll
-                for (int e = 0; e < PER; ++e) f[k][e] = -INFINITY;
+        for (int k = 0; k < AHEAD; ++k) {
+            constexpr uint32_t none = Words<T>::NONE;
+            w[k] = b + k * THREADS < part.pieces ? pieces[b + k * THREADS] : make_uint4(none, none, none, none);
         }
+    };
+    uint4 next[AHEAD];
+    load(next, tid);
+    if (tid < part.head) take<ENT>(r, static_cast<float>(part.p[tid]));
+    if (tid < part.tail) take<ENT>(r, static_cast<float>(part.p[part.tail_at(tid)]));
+    for (int b = tid; b < part.pieces; b += AHEAD * THREADS) {
+        uint4 w[AHEAD];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) take<ENT>(r, f[k]);
+        for (int k = 0; k < AHEAD; ++k) w[k] = next[k];
+        load(next, b + AHEAD * THREADS);
+        take_pieces<T, ENT>(r, w);
     }
     const float own = r.m;
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const Running o{__shfl_xor_sync(0xffffffffu, r.m, off), __shfl_xor_sync(0xffffffffu, r.S, off), ENT ? __shfl_xor_sync(0xffffffffu, r.A, off) : 0.f};
-        r = lane & off ? join<ENT>(o, r) : join<ENT>(r, o);   // the same order in both lanes
-    }
+    if constexpr (TOP) top.own[warp][lane] = own;
+    r = join_lanes<ENT, 32>(r);
     if (lane == 0) s_warp[warp] = r;
-    if constexpr (TOP) top_of_part<T, THREADS>(part, top, own, a.top);   // (its barriers are ours)
-    else __syncthreads();
-    r = s_warp[0];
-#pragma unroll
-    for (int w = 1; w < WARPS; ++w) r = join<ENT>(r, s_warp[w]);
+    __syncthreads();
+    int found = 0;
+    if constexpr (TOP) {
+        found = candidates_of_part(part, top, own, a.top);
+        if (found > CANDIDATES) top_in_order<T, THREADS>(part, top, a.top);
+    }
+    const bool listed = found > CANDIDATES;   // the list is in out_*, not among the candidates
+    if (CL == 1 && warp * 32 >= (listed ? 1 : max(found, 1))) return;
+    r = join_lanes<ENT, WARPS>(s_warp[lane % WARPS]);
     if constexpr (CL > 1) {
         // the parts' sums and [CL][top] candidates go to the first block
+        if constexpr (TOP) {
+            if (!listed) {
+                if (tid >= found && tid < a.top) top.out_value[tid] = -INFINITY, top.out_place[tid] = 0;
+                rank_candidates(top, found, a.top, [&](int k, float v, int at) { top.out_value[k] = v, top.out_place[k] = at; });
+                __syncthreads();
+            }
+        }
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
         const auto put = [](void *p, uint32_t v) {
             uint32_t to;
@@ -294,7 +402,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
         }
         if constexpr (TOP) {
             float v = 0.f;
-            int at = -1;
+            int at = 0;
             if (tid < a.top) v = top.out_value[tid], at = top.out_place[tid];
             // (every block is done with its own candidates)
             asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -305,24 +413,27 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (rank != 0) return;
-        r = s_part[0];
-#pragma unroll
-        for (int k = 1; k < CL; ++k) r = join<ENT>(r, s_part[k]);
-        if constexpr (TOP) rank_candidates(top, CL * a.top, a.top);   // (places that hold nothing are -inf, behind all others)
+        r = join_lanes<ENT, CL>(s_part[lane % CL]);
+        found = CL * a.top;   // (of which those that stand for nothing are -inf, behind all others)
     }
-    const float log_sum = logf(r.S);
+    const float log_sum = log_sum_of(r);
     const bool empty = r.S == 0.f;
     if (tid == 0) {
         a.lse[row] = empty ? -INFINITY : r.m + log_sum;
         a.logp[row] = tok < 0 ? 0.f : empty ? -INFINITY : (x_tok - r.m) - log_sum;
-        if constexpr (ENT) a.entropy[row] = empty ? 0.f : log_sum - LN2 * (r.A / r.S);
+        if constexpr (ENT) a.entropy[row] = empty ? 0.f : logf(r.S) - LN2 * (r.A / r.S);
     }
     if constexpr (TOP) {
-        if (tid < a.top) {
-            const float v = top.out_value[tid];
+        const auto put = [&](int k, float v, int at) {
             const bool any = v > -INFINITY;
-            a.top_ids[static_cast<long long>(row) * a.top + tid] = any ? top.out_place[tid] : -1;
-            a.top_logp[static_cast<long long>(row) * a.top + tid] = any ? (v - r.m) - log_sum : -INFINITY;
+            a.top_ids[static_cast<long long>(row) * a.top + k] = any ? at : -1;
+            a.top_logp[static_cast<long long>(row) * a.top + k] = any ? (v - r.m) - log_sum : -INFINITY;
+        };
+        if (CL == 1 && listed) {
+            if (tid < a.top) put(tid, top.out_value[tid], top.out_place[tid]);
+        } else {
+            if (tid >= found && tid < a.top) put(tid, -INFINITY, 0);
+            rank_candidates(top, found, a.top, put);
         }
     }
 }
@@ -343,8 +454,8 @@ template <typename T, bool ENT, bool TOP>
 cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
     // Few long rows: a cluster each.
     if (a.vocab >= 16384 && a.rows <= 148 / CLUSTER * 2)
-        return launch_op(logprobs_cluster_kernel<T, ENT, TOP, 512>, dim3(a.rows * CLUSTER), dim3(512), 0, true, stream, a);
-    if (a.vocab >= 8192) return launch_op(logprobs_kernel<T, ENT, TOP, 512>, dim3(a.rows), dim3(512), 0, true, stream, a);
+        return launch_op(logprobs_cluster_kernel<T, ENT, TOP, 256>, dim3(a.rows * CLUSTER), dim3(256), 0, true, stream, a);
+    if (a.vocab >= 8192) return launch_op(logprobs_kernel<T, ENT, TOP, 256>, dim3(a.rows), dim3(256), 0, true, stream, a);
     return launch_op(logprobs_kernel<T, ENT, TOP, 128>, dim3(a.rows), dim3(128), 0, true, stream, a);
 }
 
@@ -360,21 +471,11 @@ template <typename T>
 __device__ __noinline__ Running sum_of_row(const Part<T> part) {
     __shared__ Running s_warp[GRAD_THREADS / 32];
     Running r{-FLT_MAX, 0.f, 0.f};
-    visit_own(part, threadIdx.x, GRAD_THREADS, [&](int, float x) {
-        const float f[1] = {x};
-        take<false>(r, f);
-    });
-#pragma unroll
-    for (int off = 16; off > 0; off >>= 1) {
-        const Running o{__shfl_xor_sync(0xffffffffu, r.m, off), __shfl_xor_sync(0xffffffffu, r.S, off), 0.f};
-        r = threadIdx.x & off ? join<false>(o, r) : join<false>(r, o);
-    }
+    visit_own<GRAD_THREADS>(part, threadIdx.x, 0, 1, [&](int, float x) { take<false>(r, x); });
+    r = join_lanes<false, 32>(r);
     if (threadIdx.x % 32 == 0) s_warp[threadIdx.x / 32] = r;
     __syncthreads();
-    r = s_warp[0];
-#pragma unroll
-    for (int w = 1; w < GRAD_THREADS / 32; ++w) r = join<false>(r, s_warp[w]);
-    return r;
+    return join_lanes<false, GRAD_THREADS / 32>(s_warp[threadIdx.x % (GRAD_THREADS / 32)]);
 }
 
 template <typename T, bool ENT>
@@ -397,7 +498,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
     if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f) && !zero) {
         if (b != 0) return;
         const Running r = sum_of_row(part);
-        from = r.m, log_sum = logf(r.S);
+        from = r.m, log_sum = log_sum_of(r);
         end = blocks;
         __syncthreads();               // out may be the logits: all of the block have read them
     }

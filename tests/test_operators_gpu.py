@@ -257,7 +257,8 @@ def check_logprobs(x, t, top=0):
     biggest = x.double().nan_to_num(0.0, posinf=0.0, neginf=0.0).abs().amax(-1)
     log_sum = math.log(x.shape[-1]) + 1
     check(r.lse, lse, rel + U * (base + biggest + 2 * log_sum))
-    check(r.logp, logp, rel + 2 * U * (logp.abs().nan_to_num(0.0, neginf=0.0) + 2 * biggest + log_sum))
+    # (differences of logits, not the logits, are rounded on the way to logp)
+    check(r.logp, logp, rel + 4 * U * (logp.abs().nan_to_num(0.0, neginf=0.0) + log_sum))
     check(r.entropy, H, tol_H + 4 * U * log_sum)
     plain = d.token_logprobs(x, t)
     assert plain.entropy is None and plain.top_ids is None and plain.top_logp is None
@@ -265,8 +266,8 @@ def check_logprobs(x, t, top=0):
     if top:
         ids = top_ref(x, top)
         assert torch.equal(r.top_ids, ids)
-        want = torch.where(ids >= 0, x.double().gather(-1, ids.clamp(min=0)) - lse[..., None], -math.inf)
-        check(r.top_logp, want, rel[..., None] + 2 * U * (want.abs().nan_to_num(0.0, neginf=0.0) + 2 * biggest[..., None] + log_sum))
+        want = torch.where(ids >= 0, log_softmax_ref(x)[0].gather(-1, ids.clamp(min=0)), -math.inf)
+        check(r.top_logp, want, rel[..., None] + 4 * U * (want.abs().nan_to_num(0.0, neginf=0.0) + log_sum))
         again = d.token_logprobs(x, t, entropy=True, top=top)
         for a, b in zip(r, again):
             assert torch.equal(a.nan_to_num(7.0), b.nan_to_num(7.0))
@@ -332,6 +333,17 @@ def test_logprobs_when_most_values_of_a_thread_are_among_the_largest():
         x[:, :, torch.arange(k * 4, V, 512 * 4, device="cuda")[:, None] + torch.arange(4, device="cuda")] += 40.0
     check_logprobs(x, torch.zeros(2, 20, dtype=torch.int64, device="cuda"), 32)
     check_logprobs(x[:1, :2].contiguous(), torch.zeros(1, 2, dtype=torch.int64, device="cuda"), 32)
+
+
+@pytest.mark.parametrize("offset", [-3e6, -1e6, 3e2, 2e4, 1e6, 3e6, 2e9, 1e30])
+def test_logprobs_of_rows_far_from_zero(offset):
+    """Offsets that fp32 logits can have, differences from them as large as the type's steps there: in front of, across and behind 1e6."""
+    for V, rows in ((1031, 5), (20000, 3), (9000, 30)):
+        x = torch.randn(2, rows, V, generator=gen_of(V), device="cuda") * 3 + offset
+        if abs(offset) == 1e6:
+            x[:, 1] += 10.0
+        check_logprobs(x, torch.randint(0, V, (2, rows), generator=gen_of(1), device="cuda"), 5)
+        check_grad(x, torch.randint(0, V, (2, rows), generator=gen_of(1), device="cuda"), in_place=rows == 3)
 
 
 def test_logprobs_layouts():
