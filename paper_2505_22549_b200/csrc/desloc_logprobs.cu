@@ -478,6 +478,21 @@ __device__ __noinline__ Running sum_of_row(const Part<T> part) {
     return join_lanes<false, GRAD_THREADS / 32>(s_warp[threadIdx.x % (GRAD_THREADS / 32)]);
 }
 
+// All of a row with a large lse, value by value.
+template <typename T, bool ENT>
+__device__ __noinline__ void grad_slowly(const Part<T> part, T *out, int tok, float wa, float wb, float H) {
+    const Running r = sum_of_row(part);
+    const float log_sum = log_sum_of(r);
+    __syncthreads();   // out may be the logits: all of the block have read them
+    const int n = part.head + part.pieces * Part<T>::PER + part.tail;
+    for (int j = threadIdx.x; j < n; j += GRAD_THREADS) {
+        const float lp = (static_cast<float>(part.p[j]) - r.m) - log_sum, p = exp2_fast(lp * LOG2E);
+        const float w = ENT ? fmaf(wb, fmaxf(lp, FAR_BELOW) + H, wa) : wa;
+        const float g[1] = {j == tok ? fmaf(-p, w, wa) : -p * w};
+        store_values(out + j, g);
+    }
+}
+
 template <typename T, bool ENT>
 __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const LogprobGradArgs a, unsigned blocks) {
     constexpr int PER = Part<T>::PER;
@@ -488,54 +503,70 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
     // a block's share: whole pieces of 16 bytes of the logits; the first block has what is in front of them, the last one what is behind
     const Part<T> part(x, a.vocab);
     const bool alike = ((reinterpret_cast<uintptr_t>(x) ^ reinterpret_cast<uintptr_t>(out)) & 15u) == 0;
+    const uint4 *const pieces = reinterpret_cast<const uint4 *>(x + part.head);
+    const int first = static_cast<int>(b * (GRAD_THREADS * GRAD_AHEAD) + threadIdx.x), edge = static_cast<int>(threadIdx.x);
+    const int edge_at = b == 0 && edge < part.head ? edge : b == blocks - 1 && edge >= 32 && edge - 32 < part.tail ? part.tail_at(edge - 32) : -1;
     wait_for_earlier_kernels();
     const int tok = token_at(a.tokens, i * a.tokens.s0 + j * a.tokens.s1, a.vocab);
     const float wa = tok < 0 ? 0.f : a.dlogp[row], wb = ENT ? a.dentropy[row] : 0.f;
     const float lse = a.lse[row], H = ENT && wb != 0.f ? a.entropy[row] : 0.f;
-    const bool zero = (wa == 0.f && wb == 0.f) || lse == -INFINITY;
-    float from = lse, log_sum = 0.f;   // log p = (x - from) - log_sum
-    unsigned end = b + 1;              // shares that this block takes: its own, or all of them
-    if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f) && !zero) {
-        if (b != 0) return;
-        const Running r = sum_of_row(part);
-        from = r.m, log_sum = log_sum_of(r);
-        end = blocks;
-        __syncthreads();               // out may be the logits: all of the block have read them
-    }
-    const auto value = [&](float v, int at) {
-        const float lp = (v - from) - log_sum, p = exp2_fast(lp * LOG2E);
-        const float w = ENT ? fmaf(wb, fmaxf(lp, FAR_BELOW) + H, wa) : wa;
-        const float g = at == tok ? fmaf(-p, w, wa) : -p * w;
-        return zero ? 0.f : g;
-    };
-    for (unsigned share = b; share < end; ++share) {
-        const int first = static_cast<int>(share * (GRAD_THREADS * GRAD_AHEAD) + threadIdx.x);
-        float f[GRAD_AHEAD][PER];
-#pragma unroll
-        for (int k = 0; k < GRAD_AHEAD; ++k)
-            if (first + k * GRAD_THREADS < part.pieces && !zero) load_values(x + part.piece_at(first + k * GRAD_THREADS), f[k]);
+    if ((wa == 0.f && wb == 0.f) || lse == -INFINITY) {
+        const float none[PER] = {};
 #pragma unroll
         for (int k = 0; k < GRAD_AHEAD; ++k) {
-            if (first + k * GRAD_THREADS >= part.pieces) break;
             const int at = part.piece_at(first + k * GRAD_THREADS);
+            if (first + k * GRAD_THREADS >= part.pieces) break;
+            if (alike) store_values(out + at, none);
+            else
 #pragma unroll
-            for (int e = 0; e < PER; ++e) f[k][e] = value(f[k][e], at + e);
-            if (alike) {
-                store_values(out + at, f[k]);
-            } else {
+                for (int e = 0; e < PER; ++e) out[at + e] = T(0.f);
+        }
+        if (edge_at >= 0) out[edge_at] = T(0.f);
+        return;
+    }
+    if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f)) {
+        if (b == 0) grad_slowly<T, ENT>(part, out, tok, wa, wb, H);
+        return;
+    }
+    // p = 2^t / 2^off with t = x log2 e - base, base = lse log2 e rounded and off what the rounding took; -w = c0 + c1 t
+    const float base = base_of(lse), off = behind_base(lse), q = exp2_fast(-off);
+    const float c1 = ENT ? -q * wb * LN2 : 0.f, c0 = -q * (ENT ? fmaf(wb, H - off * LN2, wa) : wa);
+    const float2 scale = make_float2(LOG2E, LOG2E), from = make_float2(-base, -base), C0 = make_float2(c0, c0), C1 = make_float2(c1, c1);
+    uint4 w[GRAD_AHEAD];
 #pragma unroll
-                for (int e = 0; e < PER; ++e) {
-                    const float one[1] = {f[k][e]};
-                    store_values(out + at + e, one);
-                }
+    for (int k = 0; k < GRAD_AHEAD; ++k)
+        if (first + k * GRAD_THREADS < part.pieces) w[k] = pieces[first + k * GRAD_THREADS];
+#pragma unroll
+    for (int k = 0; k < GRAD_AHEAD; ++k) {
+        if (first + k * GRAD_THREADS >= part.pieces) break;
+        const int at = part.piece_at(first + k * GRAD_THREADS);
+        if constexpr (ENT) w[k] = make_uint4(Words<T>::finite(w[k].x), Words<T>::finite(w[k].y), Words<T>::finite(w[k].z), Words<T>::finite(w[k].w));
+        float g[PER];
+#pragma unroll
+        for (int e = 0; e < PER / 2; ++e) {
+            const float2 t = __ffma2_rn(Words<T>::pair(w[k], e), scale, from), p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
+            const float2 v = __fmul2_rn(p, ENT ? __ffma2_rn(t, C1, C0) : C0);
+            g[2 * e] = v.x, g[2 * e + 1] = v.y;
+        }
+        if (static_cast<unsigned>(tok - at) < PER)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) g[e] += tok == at + e ? wa : 0.f;
+        if (alike) {
+            store_values(out + at, g);
+        } else {
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                const float one[1] = {g[e]};
+                store_values(out + at + e, one);
             }
         }
     }
-    const int edge = static_cast<int>(threadIdx.x);
-    const int at = b == 0 && edge < part.head ? edge : end == blocks && edge >= 32 && edge - 32 < part.tail ? part.tail_at(edge - 32) : -1;
-    if (at >= 0) {
-        const float one[1] = {value(zero ? 0.f : static_cast<float>(x[at]), at)};
-        store_values(out + at, one);
+    if (edge_at >= 0) {
+        float t = fmaf(static_cast<float>(x[edge_at]), LOG2E, -base);
+        const float p = exp2_fast(t);
+        if constexpr (ENT) t = fmaxf(t, FAR_BELOW);
+        const float g[1] = {p * (ENT ? fmaf(t, c1, c0) : c0) + (edge_at == tok ? wa : 0.f)};
+        store_values(out + edge_at, g);
     }
 }
 
