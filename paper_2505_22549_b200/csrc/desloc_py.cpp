@@ -9,6 +9,8 @@
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -30,6 +32,13 @@ struct Entry {
     decltype(&desloc_rel_change) rel_change = nullptr;
     decltype(&desloc_get_diag_norms) diag_norms = nullptr;
     decltype(&desloc_step_host) step_host = nullptr;
+    decltype(&desloc_embed) embed = nullptr;
+    decltype(&desloc_embed_grad) embed_grad = nullptr;
+    decltype(&desloc_embed_grad_bytes) embed_grad_bytes = nullptr;
+    decltype(&desloc_clip_grads) clip_grads = nullptr;
+    decltype(&desloc_clip_grads_bytes) clip_grads_bytes = nullptr;
+    decltype(&desloc_token_logprobs) token_logprobs = nullptr;
+    decltype(&desloc_token_logprobs_grad) token_logprobs_grad = nullptr;
 } g_entry;
 
 struct Table {
@@ -86,7 +95,7 @@ bool as_pointer(PyObject *o, void **out) {
 }
 
 // fill(nested, kind, where, message) -> address of the pointer array [workers * tensors], row m = worker m.
-// kind: 0 = fp32, 1 = bf16.  where: 0 = any device, 1 = host only.  A tensor that does not fit raises
+// kind: 0 = fp32, 1 = bf16.  where: 0 = any device, 1 = host only, 2 + d = CUDA device d only.  A tensor that does not fit raises
 // ValueError(message).  Returns None at the first element that is no torch.Tensor: the caller marshals the lists then.
 PyObject *table_fill(PyObject *o, PyObject *const *args, Py_ssize_t nargs) {
     Table *self = reinterpret_cast<Table *>(o);
@@ -118,7 +127,7 @@ PyObject *table_fill(PyObject *o, PyObject *const *args, Py_ssize_t nargs) {
                 }
                 const at::Tensor &t = THPVariable_Unpack(item);
                 if (t.scalar_type() != want || t.numel() != (*self->numel)[k] || !t.is_contiguous() ||
-                    (where == 1 && t.is_cuda())) {
+                    (where == 1 && t.is_cuda()) || (where >= 2 && !(t.is_cuda() && t.get_device() == where - 2))) {
                     state = UNFIT;
                     break;
                 }
@@ -356,10 +365,268 @@ PyObject *call_diag_norms(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     return both;
 }
 
-// bind(addresses of desloc_step, _step_masked, _step_normclip, _step_diag, _rel_change, _get_diag_norms, _step_host)
+// ---- operators around the step --------------------------------------------------------------------
+// These take what most programs hand over: tensors on the right device, of a known type, in the usual layouts.  For everything else they return
+// None, and module.py, which copies, splits or refuses, goes its own way.  A status below 0 comes back as a number.
+int value_type(at::ScalarType t) { return t == at::kFloat ? DESLOC_F32 : t == at::kBFloat16 ? DESLOC_BF16 : -1; }
+int token_type(at::ScalarType t) { return t == at::kInt ? DESLOC_I32 : t == at::kLong ? DESLOC_I64 : -1; }
+
+const at::Tensor *tensor_on(PyObject *o, int64_t device) {
+    if (!THPVariable_Check(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.get_device() == device ? &t : nullptr;
+}
+at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType type, int64_t device) {
+    return at::empty(shape, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, static_cast<c10::DeviceIndex>(device))));
+}
+void *stream_of(int64_t device) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream(); }
+
+// Calls `body`, which returns a new reference (or null with an error set).
+template <typename F>
+PyObject *guarded(const F &body) {
+    try {
+        return body();
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+        return nullptr;
+    }
+}
+
+// Tokens [workers, ...], dense.
+bool worker_tokens(const at::Tensor *t, int64_t workers, desloc_rows *rows, int64_t *n) {
+    if (!t || t->dim() < 1 || t->size(0) != workers || token_type(t->scalar_type()) < 0 || !t->is_contiguous()) return false;
+    *n = workers ? t->numel() / workers : 0;
+    *rows = {t->data_ptr(), token_type(t->scalar_type()), {*n, 1}};
+    return true;
+}
+
+// (context, tensor, width, workers, tokens, scale, type, device) -> tensor [*tokens, width]
+PyObject *call_embed(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr;
+    int64_t tensor = 0, width = 0, workers = 0, type = 0, device = 0, n = 0;
+    float scale = 0.f;
+    if (nargs != 8) {
+        PyErr_SetString(PyExc_TypeError, "embed(ctx, tensor, width, workers, tokens, scale, type, device)");
+        return nullptr;
+    }
+    if (!as_pointer(args[0], &ctx) || !as_int64(args[1], &tensor) || !as_int64(args[2], &width) || !as_int64(args[3], &workers) ||
+        !as_float(args[5], &scale) || !as_int64(args[6], &type) || !as_int64(args[7], &device))
+        return nullptr;
+    return guarded([&]() -> PyObject * {
+        const at::Tensor *t = tensor_on(args[4], device);
+        desloc_rows tokens;
+        if (!worker_tokens(t, workers, &tokens, &n) || (type != DESLOC_F32 && type != DESLOC_BF16) || width < 1) Py_RETURN_NONE;
+        c10::SmallVector<int64_t, 4> shape(t->sizes().begin(), t->sizes().end());
+        shape.push_back(width);
+        const at::Tensor out = new_tensor(shape, type == DESLOC_BF16 ? at::kBFloat16 : at::kFloat, device);
+        const desloc_rows rows{out.data_ptr(), static_cast<int32_t>(type), {n * width, width}};
+        void *stream = stream_of(device);
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.embed(static_cast<desloc_ctx *>(ctx), static_cast<int32_t>(tensor), width, &tokens, n, scale, &rows, stream);
+        Py_END_ALLOW_THREADS
+        return rc == DESLOC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+    });
+}
+
+// (context, tensor, width, workers, tokens, dout, pointers or nested lists, tensors, elements, type, scale, accumulate, device) -> 0
+PyObject *call_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr;
+    int64_t tensor = 0, width = 0, workers = 0, tensors = 0, numel = 0, type = 0, accumulate = 0, device = 0, n = 0;
+    float scale = 0.f;
+    if (nargs != 13) {
+        PyErr_SetString(PyExc_TypeError, "embed_grad(ctx, tensor, width, workers, tokens, dout, grads, tensors, elements, type, scale, accumulate, device)");
+        return nullptr;
+    }
+    if (!as_pointer(args[0], &ctx) || !as_int64(args[1], &tensor) || !as_int64(args[2], &width) || !as_int64(args[3], &workers) ||
+        !as_int64(args[7], &tensors) || !as_int64(args[8], &numel) || !as_int64(args[9], &type) || !as_float(args[10], &scale) ||
+        !as_int64(args[11], &accumulate) || !as_int64(args[12], &device))
+        return nullptr;
+    return guarded([&]() -> PyObject * {
+        desloc_rows tokens;
+        const at::Tensor *t = tensor_on(args[4], device), *d = tensor_on(args[5], device);
+        if (!worker_tokens(t, workers, &tokens, &n) || !d || value_type(d->scalar_type()) < 0 || !d->is_contiguous() || d->dim() != t->dim() + 1 ||
+            d->size(-1) != width || d->sizes().slice(0, t->dim()) != t->sizes())
+            Py_RETURN_NONE;
+        const desloc_rows rows{d->data_ptr(), value_type(d->scalar_type()), {n * width, width}};
+        std::vector<void *> own;
+        void *const *grads = nullptr;
+        if (PyLong_Check(args[6])) {
+            grads = static_cast<void *const *>(PyLong_AsVoidPtr(args[6]));
+        } else {
+            if (!PyList_Check(args[6]) || PyList_GET_SIZE(args[6]) != workers) Py_RETURN_NONE;
+            own.resize(static_cast<size_t>(workers * tensors), nullptr);
+            for (int64_t m = 0; m < workers; ++m) {
+                PyObject *row = PyList_GET_ITEM(args[6], m);
+                if (!PyList_Check(row) || PyList_GET_SIZE(row) <= tensor) Py_RETURN_NONE;
+                const at::Tensor *g = tensor_on(PyList_GET_ITEM(row, tensor), device);
+                if (!g || value_type(g->scalar_type()) != type || g->numel() != numel || !g->is_contiguous()) Py_RETURN_NONE;
+                own[static_cast<size_t>(m * tensors + tensor)] = g->data_ptr();
+            }
+            grads = own.data();
+        }
+        const int64_t bytes = g_entry.embed_grad_bytes(static_cast<desloc_ctx *>(ctx), static_cast<int32_t>(tensor), width, n);
+        if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
+        const at::Tensor work = new_tensor({bytes}, at::kByte, device);
+        void *stream = stream_of(device), *at_work = work.data_ptr();
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.embed_grad(static_cast<desloc_ctx *>(ctx), static_cast<int32_t>(tensor), width, &tokens, n, &rows, scale,
+                                static_cast<int32_t>(accumulate), grads, at_work, bytes, stream);
+        Py_END_ALLOW_THREADS
+        return PyLong_FromLong(rc);
+    });
+}
+
+// (context, max_norm, type, pointers, type of out, pointers of out, workers, device) -> tensor [2, workers] of norms and factors
+PyObject *call_clip_grads(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr, *from = nullptr, *to = nullptr;
+    int64_t type = 0, out_type = 0, workers = 0, device = 0;
+    float max_norm = 0.f;
+    if (nargs != 8) {
+        PyErr_SetString(PyExc_TypeError, "clip_grads(ctx, max_norm, type, grads, out_type, out, workers, device)");
+        return nullptr;
+    }
+    if (!as_pointer(args[0], &ctx) || !as_float(args[1], &max_norm) || !as_int64(args[2], &type) || !as_pointer(args[3], &from) ||
+        !as_int64(args[4], &out_type) || !as_pointer(args[5], &to) || !as_int64(args[6], &workers) || !as_int64(args[7], &device))
+        return nullptr;
+    return guarded([&]() -> PyObject * {
+        const int64_t bytes = g_entry.clip_grads_bytes(static_cast<desloc_ctx *>(ctx));
+        if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
+        const at::Tensor result = new_tensor({2, workers}, at::kFloat, device), work = new_tensor({bytes}, at::kByte, device);
+        void *stream = stream_of(device), *at_work = work.data_ptr();
+        float *norms = static_cast<float *>(result.data_ptr());
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.clip_grads(static_cast<desloc_ctx *>(ctx), max_norm, static_cast<int32_t>(type), static_cast<const void *const *>(from),
+                                static_cast<int32_t>(out_type), static_cast<void *const *>(to), norms, norms + workers, at_work, bytes, stream);
+        Py_END_ALLOW_THREADS
+        return rc == DESLOC_OK ? THPVariable_Wrap(result) : PyLong_FromLong(rc);
+    });
+}
+
+// Rows of up to two dimensions in front of `last` dimensions.
+struct Lead {
+    int64_t n[2] = {1, 1};
+    bool of(const at::Tensor &t, int64_t last) {
+        const int64_t lead = t.dim() - last;
+        if (lead < 0 || lead > 2) return false;
+        for (int64_t k = 0; k < lead; ++k) n[2 - lead + k] = t.size(k);
+        return true;
+    }
+};
+desloc_rows rows_of(const at::Tensor &t, int64_t last, int type) {
+    desloc_rows r{t.data_ptr(), type, {0, 0}};
+    const int64_t lead = t.dim() - last;
+    for (int64_t k = 0; k < lead; ++k) r.stride[2 - lead + k] = t.stride(k);
+    return r;
+}
+bool logit_rows(const at::Tensor *x, const at::Tensor *t, Lead *lead) {
+    return x && t && x->dim() >= 1 && value_type(x->scalar_type()) >= 0 && token_type(t->scalar_type()) >= 0 && lead->of(*x, 1) &&
+           x->sizes().slice(0, x->dim() - 1) == t->sizes() && x->size(-1) >= 1 && (x->stride(-1) == 1 || x->size(-1) == 1);
+}
+// A tensor's device where it has one that these calls take.
+int64_t cuda_device_of(PyObject *o) {
+    if (!THPVariable_Check(o)) return -1;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() ? t.get_device() : -1;
+}
+
+// (logits, tokens, entropy, top) -> (logp, lse, entropy, top_ids, top_logp)
+PyObject *call_logprobs(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    int64_t top = 0;
+    if (nargs != 4) {
+        PyErr_SetString(PyExc_TypeError, "token_logprobs(logits, tokens, entropy, top)");
+        return nullptr;
+    }
+    const int with_entropy = PyObject_IsTrue(args[2]);
+    if (with_entropy < 0 || !as_int64(args[3], &top)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        const int64_t device = cuda_device_of(args[0]);
+        const at::Tensor *x = device < 0 ? nullptr : tensor_on(args[0], device), *t = device < 0 ? nullptr : tensor_on(args[1], device);
+        Lead lead;
+        if (!logit_rows(x, t, &lead) || top < 0 || top > DESLOC_MAX_TOP) Py_RETURN_NONE;
+        at::Tensor r[5];
+        r[0] = new_tensor(t->sizes(), at::kFloat, device);
+        r[1] = new_tensor(t->sizes(), at::kFloat, device);
+        if (with_entropy) r[2] = new_tensor(t->sizes(), at::kFloat, device);
+        if (top > 0) {
+            c10::SmallVector<int64_t, 4> shape(t->sizes().begin(), t->sizes().end());
+            shape.push_back(top);
+            r[3] = new_tensor(shape, at::kLong, device);
+            r[4] = new_tensor(shape, at::kFloat, device);
+        }
+        void *p[5];
+        for (int k = 0; k < 5; ++k) p[k] = r[k].defined() ? r[k].data_ptr() : nullptr;
+        const desloc_rows logits = rows_of(*x, 1, value_type(x->scalar_type())), tokens = rows_of(*t, 0, token_type(t->scalar_type()));
+        void *stream = stream_of(device);
+        const int64_t vocab = x->size(-1);
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.token_logprobs(lead.n[0], lead.n[1], vocab, &logits, &tokens, static_cast<int32_t>(top), static_cast<float *>(p[0]),
+                                    static_cast<float *>(p[1]), static_cast<float *>(p[2]), static_cast<int64_t *>(p[3]), static_cast<float *>(p[4]),
+                                    static_cast<int>(device), stream);
+        Py_END_ALLOW_THREADS
+        if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        PyObject *tuple = PyTuple_New(5);
+        for (int k = 0; tuple && k < 5; ++k) {
+            PyObject *o = r[k].defined() ? THPVariable_Wrap(r[k]) : Py_NewRef(Py_None);
+            if (!o) {
+                Py_CLEAR(tuple);
+                break;
+            }
+            PyTuple_SET_ITEM(tuple, k, o);
+        }
+        return tuple;
+    });
+}
+
+// (logits, tokens, lse, dlogp, entropy, dentropy, out or None) -> out
+PyObject *call_logprobs_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    if (nargs != 7) {
+        PyErr_SetString(PyExc_TypeError, "token_logprobs_grad(logits, tokens, lse, dlogp, entropy, dentropy, out)");
+        return nullptr;
+    }
+    return guarded([&]() -> PyObject * {
+        const int64_t device = cuda_device_of(args[0]);
+        const at::Tensor *x = device < 0 ? nullptr : tensor_on(args[0], device), *t = device < 0 ? nullptr : tensor_on(args[1], device);
+        Lead lead;
+        if (!logit_rows(x, t, &lead)) Py_RETURN_NONE;
+        const float *dense[4] = {};
+        for (int k = 0; k < 4; ++k) {
+            if (k >= 2 && args[2 + k] == Py_None) continue;
+            const at::Tensor *d = tensor_on(args[2 + k], device);
+            if (!d || d->scalar_type() != at::kFloat || d->sizes() != t->sizes() || !d->is_contiguous()) Py_RETURN_NONE;
+            dense[k] = static_cast<const float *>(d->data_ptr());
+        }
+        if (dense[3] && !dense[2] && t->numel() > 0) Py_RETURN_NONE;
+        at::Tensor out;
+        if (args[6] == Py_None) {
+            out = at::empty_like(*x, at::MemoryFormat::Contiguous);
+        } else {
+            const at::Tensor *o = tensor_on(args[6], device);
+            if (!o || o->scalar_type() != x->scalar_type() || o->sizes() != x->sizes() || (o->stride(-1) != 1 && o->size(-1) > 1)) Py_RETURN_NONE;
+            out = *o;
+        }
+        const desloc_rows logits = rows_of(*x, 1, value_type(x->scalar_type())), tokens = rows_of(*t, 0, token_type(t->scalar_type())),
+                          to = rows_of(out, 1, value_type(out.scalar_type()));
+        void *stream = stream_of(device);
+        const int64_t vocab = x->size(-1);
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.token_logprobs_grad(lead.n[0], lead.n[1], vocab, &logits, &tokens, dense[0], dense[1], dense[2], dense[3], &to,
+                                         static_cast<int>(device), stream);
+        Py_END_ALLOW_THREADS
+        return rc == DESLOC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
+    });
+}
+
+// bind(addresses of desloc_step, _step_masked, _step_normclip, _step_diag, _rel_change, _get_diag_norms, _step_host, and of the operators around the
+// step: _embed, _embed_grad, _embed_grad_bytes, _clip_grads, _clip_grads_bytes, _token_logprobs, _token_logprobs_grad)
 PyObject *bind_entries(PyObject *, PyObject *args) {
-    unsigned long long a[7];
-    if (!PyArg_ParseTuple(args, "KKKKKKK", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6])) return nullptr;
+    unsigned long long a[14];
+    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKK", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &a[12], &a[13]))
+        return nullptr;
     g_entry.step = reinterpret_cast<decltype(g_entry.step)>(a[0]);
     g_entry.step_masked = reinterpret_cast<decltype(g_entry.step_masked)>(a[1]);
     g_entry.step_normclip = reinterpret_cast<decltype(g_entry.step_normclip)>(a[2]);
@@ -367,6 +634,13 @@ PyObject *bind_entries(PyObject *, PyObject *args) {
     g_entry.rel_change = reinterpret_cast<decltype(g_entry.rel_change)>(a[4]);
     g_entry.diag_norms = reinterpret_cast<decltype(g_entry.diag_norms)>(a[5]);
     g_entry.step_host = reinterpret_cast<decltype(g_entry.step_host)>(a[6]);
+    g_entry.embed = reinterpret_cast<decltype(g_entry.embed)>(a[7]);
+    g_entry.embed_grad = reinterpret_cast<decltype(g_entry.embed_grad)>(a[8]);
+    g_entry.embed_grad_bytes = reinterpret_cast<decltype(g_entry.embed_grad_bytes)>(a[9]);
+    g_entry.clip_grads = reinterpret_cast<decltype(g_entry.clip_grads)>(a[10]);
+    g_entry.clip_grads_bytes = reinterpret_cast<decltype(g_entry.clip_grads_bytes)>(a[11]);
+    g_entry.token_logprobs = reinterpret_cast<decltype(g_entry.token_logprobs)>(a[12]);
+    g_entry.token_logprobs_grad = reinterpret_cast<decltype(g_entry.token_logprobs_grad)>(a[13]);
     Py_RETURN_NONE;
 }
 
@@ -381,6 +655,11 @@ PyMethodDef methods[] = {{"bind", bind_entries, METH_VARARGS, nullptr},
                          {"step_host", fast(call_step_host), METH_FASTCALL, nullptr},
                          {"diag_norms", fast(call_diag_norms), METH_FASTCALL, nullptr},
                          {"rel_change", fast(call_rel_change), METH_FASTCALL, nullptr},
+                         {"embed", fast(call_embed), METH_FASTCALL, nullptr},
+                         {"embed_grad", fast(call_embed_grad), METH_FASTCALL, nullptr},
+                         {"clip_grads", fast(call_clip_grads), METH_FASTCALL, nullptr},
+                         {"token_logprobs", fast(call_logprobs), METH_FASTCALL, nullptr},
+                         {"token_logprobs_grad", fast(call_logprobs_grad), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -20,7 +20,8 @@ if _native.torch_version != str(torch.__version__):
 
 _entry = lambda f: ctypes.cast(f, ctypes.c_void_p).value
 _native.bind(*(_entry(getattr(B.raw_lib(), "desloc_" + n))
-               for n in ("step", "step_masked", "step_normclip", "step_diag", "rel_change", "get_diag_norms", "step_host")))
+               for n in ("step", "step_masked", "step_normclip", "step_diag", "rel_change", "get_diag_norms", "step_host", "embed", "embed_grad",
+                         "embed_grad_bytes", "clip_grads", "clip_grads_bytes", "token_logprobs", "token_logprobs_grad")))
 
 _GRAD_MISFIT = "gradient tensor of wrong dtype, size or layout"
 _SNAP_MISFIT = "snapshot tensor of wrong dtype, size or layout"
@@ -145,7 +146,7 @@ class DesLoc:
             ptrs = []
             for row in nested:
                 for t, n in zip(row, self.numel):
-                    if t.dtype != want or t.numel() != n or not t.is_contiguous() or (where == 1 and t.is_cuda):
+                    if t.dtype != want or t.numel() != n or not t.is_contiguous() or (where == 1 and t.is_cuda) or (where >= 2 and t.get_device() != where - 2):
                         raise ValueError(misfit)
                     ptrs.append(t.data_ptr())
             if len(ptrs) != self.M * len(self.numel):
@@ -220,6 +221,10 @@ class DesLoc:
         """scale * rows of every worker's x of `tensor` by token, on torch's current stream.  tokens: [M, ...] -> [M, ..., width] of `dtype`
         ("f32", "bf16"; that of `out` where it is given).  Tokens outside the vocabulary give zeros."""
         width = self._rows_of(tensor, width)
+        if out is None:     # the usual layouts, natively
+            r = _native.embed(self.ctx, tensor, width, self.M, tokens, scale, B.DTYPE_BY_NAME.get(dtype, dtype), self._index)
+            if r is not None:
+                return r if type(r) is not int else self._raise(r, "desloc_embed")
         rows, flat = self._tokens(tokens)
         shape = tuple(tokens.shape) + (width,)
         if out is None:
@@ -240,6 +245,10 @@ class DesLoc:
         """The gradient of embed() into the workers' gradients of `tensor` in `grads` (what step() reads: nested lists, of which only that
         tensor is looked at, or bind_grads()' handle).  accumulate: added to what they hold."""
         width = self._rows_of(tensor, width)
+        r = _native.embed_grad(self.ctx, tensor, width, self.M, tokens, dout, grads.address if isinstance(grads, BoundGrads) else grads, len(self.numel),
+                               self.numel[tensor], self.grad_dtype, scale, accumulate, self._index)
+        if r is not None:
+            return None if r == 0 else self._raise(r, "desloc_embed_grad")
         rows, flat = self._tokens(tokens)
         if tuple(dout.shape) != tuple(tokens.shape) + (width,) or dout.dtype not in _TYPES:
             raise ValueError("dout does not fit the tokens")
@@ -271,22 +280,17 @@ class DesLoc:
         kind = _TYPES.get(grads[0][0].dtype) if len(grads) and len(grads[0]) else None
         if kind is None:
             raise ValueError(_GRAD_MISFIT)
-        for row in grads:
-            _on(self.device, "gradients", *row)
-        return self._fill(table, grads, kind, 0, _GRAD_MISFIT), kind
+        return self._fill(table, grads, kind, 2 + self._index, _GRAD_MISFIT), kind
 
     def clip_grads(self, grads, max_norm: float, out=None):
         """Norm-based clipping on its own: every worker's gradients (nested lists, fp32 or bf16) times min(1, max_norm / their norm over the
         whole tensor list), into `out` (the same, either type) or in place.  Returns (norms, factors), [M] fp32 on the device; nothing waits."""
         address, kind = self._list_of(self._table, grads)
         to, to_kind = (address, kind) if out is None else self._list_of(self._table2, out)
-        result = torch.empty(2, self.M, dtype=torch.float32, device=self.device)
-        work = torch.empty(B.desloc_clip_grads_bytes(self.ctx), dtype=torch.uint8, device=self.device)
-        n = self.M * len(self.numel)
-        at = lambda a: (ctypes.c_void_p * n).from_address(a)
-        B.desloc_clip_grads(self.ctx, max_norm, kind, at(address), to_kind, at(to), result[0].data_ptr(), result[1].data_ptr(), work.data_ptr(),
-                            work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
-        return result[0], result[1]
+        r = _native.clip_grads(self.ctx, max_norm, kind, address, to_kind, to, self.M, self._index)
+        if type(r) is int:
+            self._raise(r, "desloc_clip_grads")
+        return r[0], r[1]
 
     def set_workers(self, x, u, v, first_new: int) -> None:
         """New worker set (lists like the constructor's); workers first_new.. start from the mean
@@ -364,9 +368,16 @@ def _logit_rows(logits, tokens, *more):
     return logits, tokens, found
 
 
+def _refuse(status: int, where: str):
+    raise B.DeslocError(status, where)
+
+
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, entropy: bool = False, top: int = 0) -> TokenLogprobs:
     """Log probabilities of `tokens` [...] under `logits` [..., vocabulary] (fp32 or bf16), on torch's current stream: logp (0 for tokens outside the
     vocabulary), lse, and on request the entropy and the `top` likeliest tokens.  exp(-logp.mean(...)) is the perplexity."""
+    r = _native.token_logprobs(logits, tokens, entropy, top)     # the usual layouts, natively
+    if r is not None:
+        return TokenLogprobs(*r) if type(r) is not int else _refuse(r, "desloc_token_logprobs")
     logits, tokens, (outer, inner, strides) = _logit_rows(logits, tokens)
     lead, dev = logits.shape[:-1], logits.device
     new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)
@@ -383,6 +394,9 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.T
                         dentropy: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) with respect to the logits, in their type; lse and entropy are what
     token_logprobs() gave.  out may be the logits themselves."""
+    r = _native.token_logprobs_grad(logits, tokens, lse, dlogp, entropy, dentropy, out)
+    if r is not None:
+        return r if type(r) is not int else _refuse(r, "desloc_token_logprobs_grad")
     if out is None:
         out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     if out.shape != logits.shape or out.dtype != logits.dtype or out.device != logits.device or (out.stride(-1) != 1 and out.shape[-1] > 1):
