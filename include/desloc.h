@@ -419,7 +419,7 @@ DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor
  *   norms, factors     : device, [M] floats each, or NULL.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
  * max_norm must be > 0 and finite.  A norm that is not finite says that the gradients are not (or that their squares left fp32's range,
- * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  Norms and factors are those that desloc_step_normclip() uses.
+ * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  desloc_step_normclip() forms the same norms, up to the order of additions.
  */
 DESLOC_API int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, const void *const *grads, int32_t out_dtype,
                                  void *const *out, float *norms, float *factors, void *work, int64_t work_bytes, void *stream);

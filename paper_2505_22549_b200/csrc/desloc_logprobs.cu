@@ -174,10 +174,16 @@ __device__ __forceinline__ float sort_lanes(float v) {
     return v;
 }
 
-// Numbers that rise as the values do (-0 and 0 are one value).
-__device__ __forceinline__ uint32_t ordered(float x) {
+// A value and its place as one number: larger for larger values (-0 and 0 are one), then for lower places; 0 for nothing.
+using Key = unsigned long long;
+__device__ __forceinline__ Key key_of(float x, int place) {
     const uint32_t b = __float_as_uint(x + 0.f);
-    return b & 0x80000000u ? ~b : b | 0x80000000u;
+    return static_cast<Key>(b & 0x80000000u ? ~b : b | 0x80000000u) << 32 | (0xffffffffu - static_cast<uint32_t>(place));
+}
+__device__ __forceinline__ int place_of(Key key) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(key)); }
+__device__ __forceinline__ float value_of(Key key) {
+    const uint32_t b = static_cast<uint32_t>(key >> 32);
+    return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
 constexpr int MOST_TOP = DESLOC_MAX_TOP, CANDIDATES = 1024;
@@ -202,6 +208,7 @@ template <int THREADS, typename T, typename F>
 __device__ __forceinline__ void visit_own(const Part<T> &part, int tid, int lane, int lanes, const F &visit) {
     if (lane == 0 && tid < part.head) visit(tid, static_cast<float>(part.p[tid]));
     if (lane == 0 && tid < part.tail) visit(part.tail_at(tid), static_cast<float>(part.p[part.tail_at(tid)]));
+#pragma unroll 4
     for (long long i = tid + lane * THREADS; i < part.pieces; i += lanes * THREADS) {
         const int at = part.piece_at(static_cast<int>(i));
         float f[Part<T>::PER];
@@ -215,33 +222,35 @@ template <int THREADS>
 struct TopShared {
     float own[THREADS / 32][32];
     float line;
-    float value[CANDIDATES];
-    int place[CANDIDATES];
     int n;
-    float out_value[MOST_TOP];
-    int out_place[MOST_TOP];
-    unsigned long long best[THREADS / 32];
+    Key key[CANDIDATES];
+    Key out[MOST_TOP];   // the largest ones, in order, where they have been ranked
+    Key best[THREADS / 32];
 };
 
-// The candidates' order: larger values first, lower places among equals (those that stand for nothing in a cluster's lists, -inf, have one place).  put(rank, value, place) for the first `top` of them.
+// put(rank, key) for the `top` largest of n keys, in order, and put(rank, 0) where there are fewer.  (Keys but 0 differ.)
 template <int THREADS, typename Put>
-__device__ __forceinline__ void rank_candidates(const TopShared<THREADS> &s, int n, int top, const Put &put) {
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const float v = s.value[i];
-        const int at = s.place[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += s.value[j] > v || (s.value[j] == v && (s.place[j] < at || (s.place[j] == at && j < i)));
-        if (rank < top) put(rank, v, at);
+__device__ __forceinline__ void rank_keys(const Key *keys, int n, int top, const Put &put) {
+    for (int i = threadIdx.x; i < max(n, top); i += THREADS) {
+        const Key own = i < n ? keys[i] : 0;
+        int rank = 0, real = 0;
+#pragma unroll 8
+        for (int j = 0; j < n; ++j) {
+            const Key k = keys[j];
+            rank += k > own;
+            real += k != 0;
+        }
+        if (own != 0 && rank < top) put(rank, own);
+        if (i >= real && i < top) put(i, Key{0});
     }
 }
 
-// The `top` largest values of a part, whatever they are: goes over the part in order and puts what beats the last of the list into it, one at
-// a time.  Only for parts with more than CANDIDATES values at or above the line that top_of_part() draws.
+// The `top` largest values of a part, whatever they are, into s.out: goes over the part in order and puts what beats the last of the list into it,
+// one at a time.  Only for parts with more than CANDIDATES values at or above the line that candidates_of_part() draws.
 template <typename T, int THREADS>
 __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS> &s, int top) {
     const int tid = threadIdx.x;
-    for (int i = tid; i < MOST_TOP; i += THREADS) s.out_value[i] = -INFINITY, s.out_place[i] = -1;
-    if (tid == 0) s.n = 0;
+    for (int i = tid; i < MOST_TOP; i += THREADS) s.out[i] = 0;
     __syncthreads();
     const int rounds = 2 + (part.pieces + THREADS - 1) / THREADS;   // the head, the pieces, the tail
     for (int r = 0; r < rounds; ++r) {
@@ -256,19 +265,19 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
         }
         unsigned left = (1u << have) - 1;
         for (;;) {
-            const float line = s.n < top ? -INFINITY : s.out_value[top - 1];
-            unsigned long long best = 0;   // value, then low places first
+            const Key line = s.out[top - 1];
+            Key own = 0;
             int which = 0;
 #pragma unroll
             for (int k = 0; k < Part<T>::PER; ++k)
-                if ((left >> k & 1u) && f[k] > line) {
-                    const unsigned long long key = static_cast<unsigned long long>(ordered(f[k])) << 32 | (0xffffffffu - static_cast<unsigned>(at + k));
-                    if (key > best) best = key, which = k;
+                if ((left >> k & 1u) && f[k] > -INFINITY) {
+                    const Key key = key_of(f[k], at + k);
+                    if (key > line && key > own) own = key, which = k;
                 }
-            const unsigned long long own = best;
+            Key best = own;
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) {
-                const unsigned long long o = __shfl_xor_sync(0xffffffffu, best, off);
+                const Key o = __shfl_xor_sync(0xffffffffu, best, off);
                 best = o > best ? o : best;
             }
             if ((tid & 31) == 0) s.best[tid >> 5] = best;
@@ -276,25 +285,20 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
             best = 0;
 #pragma unroll
             for (int w = 0; w < THREADS / 32; ++w) best = s.best[w] > best ? s.best[w] : best;
-            const int n = s.n;
-            __syncthreads();
-            if (best == 0) break;
-            if (own == best) {   // one thread: places differ
-                float v = f[0];
-#pragma unroll
-                for (int k = 1; k < Part<T>::PER; ++k) v = which == k ? f[k] : v;
+            if (best == 0) break;   // (in all threads)
+            if (own == best) {      // one thread: places differ
                 left &= ~(1u << which);
-                int i = min(n, top - 1);
-                for (; i > 0 && s.out_value[i - 1] < v; --i) s.out_value[i] = s.out_value[i - 1], s.out_place[i] = s.out_place[i - 1];
-                s.out_value[i] = v, s.out_place[i] = at + which;
-                s.n = min(n + 1, top);
+                int i = top - 1;
+                for (; i > 0 && s.out[i - 1] < own; --i) s.out[i] = s.out[i - 1];
+                s.out[i] = own;
             }
             __syncthreads();
         }
+        __syncthreads();   // s.best has been read
     }
 }
 
-// Candidates for the `top` largest values of a part into s.value and s.place; how many, which may be more than there is room for.  s.own holds the largest
+// Candidates for the `top` largest values of a part into s.key; how many, which may be more than there is room for.  s.own holds the largest
 // that each thread has seen (-FLT_MAX: none), behind a barrier.  The line is the top-th largest of 32 groups' of threads largest values: at least
 // `top` values lie at or above it (all values, where fewer groups have any), only threads whose largest does have such, and their warps look at what these
 // took once more (some hundred bytes each, from L2).
@@ -311,13 +315,19 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
     }
     __syncthreads();
     const float line = s.line;
-    for (unsigned who = __ballot_sync(0xffffffffu, own >= line); who; who &= who - 1)
-        visit_own<THREADS>(part, (tid & ~31) + __ffs(who) - 1, tid & 31, 32, [&](int at, float x) {
-            if (x >= line) {
-                const int i = atomicAdd(&s.n, 1);
-                if (i < CANDIDATES) s.value[i] = x, s.place[i] = at;
-            }
-        });
+    const auto collect = [&](int at, float x) {
+        if (x >= line) {
+            const int i = atomicAdd(&s.n, 1);
+            if (i < CANDIDATES) s.key[i] = key_of(x, at);
+        }
+    };
+    // (a few pieces each: every thread its own, all at once)
+    if (part.pieces <= 4 * THREADS) {
+        if (own >= line) visit_own<THREADS>(part, tid, 0, 1, collect);
+    } else {
+        for (unsigned who = __ballot_sync(0xffffffffu, own >= line); who; who &= who - 1)
+            visit_own<THREADS>(part, (tid & ~31) + __ffs(who) - 1, tid & 31, 32, collect);
+    }
     __syncthreads();
     return s.n;
 }
@@ -330,6 +340,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     __shared__ Running s_warp[WARPS];
     __shared__ Running s_part[CL];
     __shared__ TopShared<TOP ? THREADS : 32> top;
+    __shared__ Key s_lists[TOP && CL > 1 ? CL * MOST_TOP : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const unsigned row = blockIdx.x / CL;
     const int rank = static_cast<int>(blockIdx.x % CL);
@@ -377,44 +388,34 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
         found = candidates_of_part(part, top, own, a.top);
         if (found > CANDIDATES) top_in_order<T, THREADS>(part, top, a.top);
     }
-    const bool listed = found > CANDIDATES;   // the list is in out_*, not among the candidates
+    const bool listed = found > CANDIDATES;   // they are in top.out, in order, not among the candidates
     if (CL == 1 && warp * 32 >= (listed ? 1 : max(found, 1))) return;
     r = join_lanes<ENT, WARPS>(s_warp[lane % WARPS]);
+    const Key *keys = listed ? top.out : top.key;
+    int n = listed ? a.top : found;
     if constexpr (CL > 1) {
-        // the parts' sums and [CL][top] candidates go to the first block
-        if constexpr (TOP) {
-            if (!listed) {
-                if (tid >= found && tid < a.top) top.out_value[tid] = -INFINITY, top.out_place[tid] = 0;
-                rank_candidates(top, found, a.top, [&](int k, float v, int at) { top.out_value[k] = v, top.out_place[k] = at; });
-                __syncthreads();
-            }
-        }
+        // the parts' sums and lists go to the first block
         asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
-        const auto put = [](void *p, uint32_t v) {
+        const auto there = [](void *p) {
             uint32_t to;
             asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(to) : "r"(smem_u32(p)));
-            asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(to), "r"(v) : "memory");
+            return to;
         };
+        const auto put = [&](void *p, uint32_t v) { asm volatile("st.shared::cluster.u32 [%0], %1;" :: "r"(there(p)), "r"(v) : "memory"); };
         if (tid == 0) {
             put(&s_part[rank].m, __float_as_uint(r.m));
             put(&s_part[rank].S, __float_as_uint(r.S));
             put(&s_part[rank].A, __float_as_uint(r.A));
         }
-        if constexpr (TOP) {
-            float v = 0.f;
-            int at = 0;
-            if (tid < a.top) v = top.out_value[tid], at = top.out_place[tid];
-            // (every block is done with its own candidates)
-            asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-            if (tid < a.top) {
-                put(&top.value[rank * a.top + tid], __float_as_uint(v));
-                put(&top.place[rank * a.top + tid], static_cast<uint32_t>(j0 + at));
-            }
-        }
+        if constexpr (TOP)
+            rank_keys<THREADS>(keys, n, a.top, [&](int k, Key key) {
+                const Key moved = key ? key - static_cast<Key>(j0) : 0;   // (the place in the row)
+                asm volatile("st.shared::cluster.u64 [%0], %1;" :: "r"(there(&s_lists[rank * a.top + k])), "l"(moved) : "memory");
+            });
         asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
         if (rank != 0) return;
         r = join_lanes<ENT, CL>(s_part[lane % CL]);
-        found = CL * a.top;   // (of which those that stand for nothing are -inf, behind all others)
+        keys = s_lists, n = CL * a.top;
     }
     const float log_sum = log_sum_of(r);
     const bool empty = r.S == 0.f;
@@ -423,19 +424,11 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
         a.logp[row] = tok < 0 ? 0.f : empty ? -INFINITY : (x_tok - r.m) - log_sum;
         if constexpr (ENT) a.entropy[row] = empty ? 0.f : logf(r.S) - LN2 * (r.A / r.S);
     }
-    if constexpr (TOP) {
-        const auto put = [&](int k, float v, int at) {
-            const bool any = v > -INFINITY;
-            a.top_ids[static_cast<long long>(row) * a.top + k] = any ? at : -1;
-            a.top_logp[static_cast<long long>(row) * a.top + k] = any ? (v - r.m) - log_sum : -INFINITY;
-        };
-        if (CL == 1 && listed) {
-            if (tid < a.top) put(tid, top.out_value[tid], top.out_place[tid]);
-        } else {
-            if (tid >= found && tid < a.top) put(tid, -INFINITY, 0);
-            rank_candidates(top, found, a.top, put);
-        }
-    }
+    if constexpr (TOP)
+        rank_keys<THREADS>(keys, n, a.top, [&](int k, Key key) {
+            a.top_ids[static_cast<long long>(row) * a.top + k] = key ? place_of(key) : -1;
+            a.top_logp[static_cast<long long>(row) * a.top + k] = key ? (value_of(key) - r.m) - log_sum : -INFINITY;
+        });
 }
 
 template <typename T, bool ENT, bool TOP, int THREADS>

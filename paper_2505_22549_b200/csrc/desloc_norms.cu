@@ -407,9 +407,10 @@ scale_kernel(const Chunk *chunks, unsigned nchunks, const void *const *g, const 
     scale_span(from, to, ch.count, factor, threadIdx.x, SCALE_THREADS);
 }
 
-// Small problems: norms as small_norms_kernel has them (the same bits), and what was read is in L2 for the second pass.  Few addresses travel
-// in the parameters: one launch in all.
-constexpr int SMALL_CLIP_ADDRESSES = 64;
+// Small problems: norms as small_norms_kernel has them (the same bits where a warp has one share, as there), and what was read is in L2 for the
+// second pass.  Few addresses travel in the parameters: one launch in all.
+constexpr int SMALL_CLIP_ADDRESSES = 128, SMALL_CLIP_SHARES = 4;
+constexpr int64_t SMALL_CLIP_BYTES = 16 << 20;   // of all workers
 struct SmallClip {
     const void *const *g, *const *out;   // tables, or null:
     const void *few_g[SMALL_CLIP_ADDRESSES], *few_out[SMALL_CLIP_ADDRESSES];
@@ -422,21 +423,25 @@ small_clip_kernel(const Chunk *chunks, int nchunks, const __grid_constant__ Smal
     const int m = static_cast<int>(blockIdx.x) / SMALL_BLOCKS, rank = static_cast<int>(blockIdx.x) % SMALL_BLOCKS;
     begin_and_let_next_begin();
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (do the blocks exist?  asked below)
-    const SmallShare s(chunks, nchunks, rank * (SMALL_THREADS / 32) + static_cast<int>(threadIdx.x >> 5));
+    const int at = rank * (SMALL_THREADS / 32) + static_cast<int>(threadIdx.x >> 5);
     wait_for_earlier_kernels();
-    const ST *from = nullptr;
-    DT *to = nullptr;
-    if (s.count > 0) {
-        const long long idx = static_cast<long long>(m) * nt + s.ch.tensor;
-        from = static_cast<const ST *>(a.g ? a.g[idx] : a.few_g[idx]) + s.ch.start + s.e0;
-        to = static_cast<DT *>(const_cast<void *>(a.g ? a.out[idx] : a.few_out[idx])) + s.ch.start + s.e0;
-    }
-    const double t = small_total<true>(small_sum<MODE>(reinterpret_cast<const char *>(from), s.count), rank);
+    double sum = 0.0;
+    const auto shares = [&](const auto &take) {   // of this warp: share `at` of every SMALL_WARPS chunks
+        for (int c0 = 0; c0 < nchunks; c0 += SMALL_WARPS) {
+            const SmallShare s(chunks + c0, nchunks - c0, at);
+            if (s.count <= 0) continue;
+            const long long idx = static_cast<long long>(m) * nt + s.ch.tensor, e = s.ch.start + s.e0;
+            take(static_cast<const ST *>(a.g ? a.g[idx] : a.few_g[idx]) + e, static_cast<DT *>(const_cast<void *>(a.g ? a.out[idx] : a.few_out[idx])) + e, s.count);
+        }
+    };
+    shares([&](const ST *from, DT *, int count) { sum += small_sum<MODE>(reinterpret_cast<const char *>(from), count); });
+    const double t = small_total<true>(sum, rank);
     float norm, factor;
     finish_norm(t, max_norm, &norm, &factor);
     if (rank == 0 && threadIdx.x == 0) norms[m] = norm, factors[m] = factor;
-    if (s.count > 0 && !(factor == 1.f && static_cast<const void *>(from) == static_cast<const void *>(to)))
-        scale_span(from, to, s.count, factor, threadIdx.x & 31, 32);
+    shares([&](const ST *from, DT *to, int count) {
+        if (!(factor == 1.f && static_cast<const void *>(from) == static_cast<const void *>(to))) scale_span(from, to, count, factor, threadIdx.x & 31, 32);
+    });
 }
 
 // dst^j[i] = mean over the M_src source replicas of src^m[i] (fp64 sum in the order
@@ -547,7 +552,9 @@ cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, c
                         int nt, int M, float max_norm, float *norms, float *factors, const ClipWork &w, int *err, int wait_limit,
                         cudaStream_t stream, int *launches) {
     const int nptr = M * nt;
-    const bool small = small_norms(nchunks, elems, M, g_bf16);
+    // A cluster per worker, up to SMALL_CLIP_SHARES chunks for each of its warps, where all clusters run at once.
+    const bool small = small_norms(nchunks, elems, M, g_bf16) ||
+                       (M <= 148 / SMALL_BLOCKS && nchunks <= SMALL_CLIP_SHARES * SMALL_WARPS && elems * M * (g_bf16 ? 2 : 4) <= SMALL_CLIP_BYTES);
     using bf = __nv_bfloat16;
     *launches = 0;
     SmallClip few{};

@@ -478,7 +478,7 @@ PyObject *call_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     });
 }
 
-// (context, max_norm, type, pointers, type of out, pointers of out, workers, device) -> tensor [2, workers] of norms and factors
+// (context, max_norm, type, pointers, type of out, pointers of out, workers, device) -> (norms, factors)
 PyObject *call_clip_grads(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     void *ctx = nullptr, *from = nullptr, *to = nullptr;
     int64_t type = 0, out_type = 0, workers = 0, device = 0;
@@ -493,15 +493,20 @@ PyObject *call_clip_grads(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     return guarded([&]() -> PyObject * {
         const int64_t bytes = g_entry.clip_grads_bytes(static_cast<desloc_ctx *>(ctx));
         if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
-        const at::Tensor result = new_tensor({2, workers}, at::kFloat, device), work = new_tensor({bytes}, at::kByte, device);
+        const at::Tensor norms = new_tensor({workers}, at::kFloat, device), factors = new_tensor({workers}, at::kFloat, device),
+                         work = new_tensor({bytes}, at::kByte, device);
         void *stream = stream_of(device), *at_work = work.data_ptr();
-        float *norms = static_cast<float *>(result.data_ptr());
+        float *at_norms = static_cast<float *>(norms.data_ptr()), *at_factors = static_cast<float *>(factors.data_ptr());
         int rc = 0;
         Py_BEGIN_ALLOW_THREADS
         rc = g_entry.clip_grads(static_cast<desloc_ctx *>(ctx), max_norm, static_cast<int32_t>(type), static_cast<const void *const *>(from),
-                                static_cast<int32_t>(out_type), static_cast<void *const *>(to), norms, norms + workers, at_work, bytes, stream);
+                                static_cast<int32_t>(out_type), static_cast<void *const *>(to), at_norms, at_factors, at_work, bytes, stream);
         Py_END_ALLOW_THREADS
-        return rc == DESLOC_OK ? THPVariable_Wrap(result) : PyLong_FromLong(rc);
+        if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        PyObject *n = THPVariable_Wrap(norms), *f = n ? THPVariable_Wrap(factors) : nullptr, *both = f ? PyTuple_Pack(2, n, f) : nullptr;
+        Py_XDECREF(n);
+        Py_XDECREF(f);
+        return both;
     });
 }
 

@@ -288,9 +288,7 @@ class DesLoc:
         address, kind = self._list_of(self._table, grads)
         to, to_kind = (address, kind) if out is None else self._list_of(self._table2, out)
         r = _native.clip_grads(self.ctx, max_norm, kind, address, to_kind, to, self.M, self._index)
-        if type(r) is int:
-            self._raise(r, "desloc_clip_grads")
-        return r[0], r[1]
+        return r if type(r) is not int else self._raise(r, "desloc_clip_grads")
 
     def set_workers(self, x, u, v, first_new: int) -> None:
         """New worker set (lists like the constructor's); workers first_new.. start from the mean

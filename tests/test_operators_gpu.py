@@ -477,12 +477,14 @@ def lists(M, numel, dtype, seed, packed, size=None):
     return out
 
 
-NUMEL = {"one": [1], "small": [4096], "ragged": [1, 7, 4097, 72, 5000, 33, 8], "many": [(i * 37) % 300 + 1 for i in range(700)], "large": [300000, 3, 1 << 20, 77777]}
+NUMEL = {"one": [1], "small": [4096], "ragged": [1, 7, 4097, 72, 5000, 33, 8], "many": [(i * 37) % 300 + 1 for i in range(700)], "large": [300000, 3, 1 << 20, 77777],
+         "mid": [200000, 5, 4096, 33] + [70] * 40, "chunks": [4000, 90] * 200}
 
 
 @pytest.mark.parametrize("src,dst", [(F32, F32), (F32, BF), (BF, BF), (BF, F32)])
 @pytest.mark.parametrize("packed", [False, True])
-@pytest.mark.parametrize("M,which", [(1, "one"), (2, "small"), (4, "ragged"), (3, "many"), (4, "large"), (40, "ragged"), (256, "small")])
+@pytest.mark.parametrize("M,which", [(1, "one"), (2, "small"), (4, "ragged"), (3, "many"), (4, "large"), (40, "ragged"), (256, "small"), (3, "mid"), (18, "mid"),
+                                     (19, "mid"), (2, "chunks")])
 def test_clip_grads(M, which, packed, src, dst):
     numel = NUMEL[which]
     opt, _ = context(M, [(n,) for n in numel], grad_dtype="bf16")
@@ -538,7 +540,9 @@ def test_clip_grads_scales_as_a_norm_clipped_step_does():
             norms, factors = opt.clip_grads(grads, 0.15, out=lists(M, numel, F32, 2, False))
             opt.step_normclip(0, 1e-3, grads, 0.15)
             n, f = opt.grad_norms()
-            assert norms.tolist() == n and factors.tolist() == f
+            # (the same kernels' sums up to 131072 parameters, else another order of additions: 75 roundings on either side)
+            for a, b in zip(norms.tolist() + factors.tolist(), n + f):
+                assert a == b if sum(numel) <= 131072 and M <= 37 else abs(a - b) <= 150 * U * b
 
 
 # ---- together ----------------------------------------------------------------------------------------
