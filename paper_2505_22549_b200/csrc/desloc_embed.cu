@@ -75,16 +75,16 @@ __device__ __forceinline__ void zero_span(char *p, long long bytes) {
     if (2 * lane < rest) *reinterpret_cast<unsigned short *>(p + head + 16 * wide + 2 * lane) = 0;
 }
 
-// Zeros in the rows [v0, v0 + rows) that have no bit in `seen`, rows / 8 of them (at most 16) by each of a block's eight warps,
+// Zeros in the rows [v0, v0 + rows) that have no bit in `seen`, `each` of them (at most 32) per warp,
 // neighbouring ones at once.
 template <typename GT>
 __device__ __forceinline__ void zero_rows(const EmbedGradArgs &a, int m, int v0, int each, unsigned seen) {
-    unsigned todo = ~seen & ((1u << min(each, max(a.vocab - v0, 0))) - 1);
+    unsigned long long todo = ~static_cast<unsigned long long>(seen) & ((1ull << min(each, max(a.vocab - v0, 0))) - 1);
     GT *const out = static_cast<GT *>(a.g[m]);
     while (todo) {
-        const int r = __ffs(todo) - 1, n = __ffs(~(todo >> r)) - 1;
+        const int r = __ffsll(static_cast<long long>(todo)) - 1, n = __ffsll(static_cast<long long>(~(todo >> r))) - 1;
         zero_span(reinterpret_cast<char *>(out + static_cast<long long>(v0 + r) * a.width), n * (static_cast<long long>(a.width) * sizeof(GT)));
-        todo &= ~(((1u << n) - 1) << r);
+        todo &= ~(((1ull << n) - 1) << r);
     }
 }
 
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(SORT_THREADS, 3) token_sort_kernel(const __gri
 // One launch; a warp takes 32 * N columns of a piece of a long run, or of the short runs that begin in TILE places.  Behind them (where the sort's launch
 // has not written them) zeros in the rows without a token, which are most of a large vocabulary.  No barriers: warps wait for their loads alone.
 // Bound: HBM, rows of dout read and the gradient written; then instructions, some 50 per row and 32 * N columns.
-constexpr int SUM_THREADS = 256, SUM_WARPS = SUM_THREADS / 32;
+constexpr int SUM_THREADS = 128, SUM_WARPS = SUM_THREADS / 32;
 constexpr int TILE = 8;
 
 // Rows in flight, unpacked when they are added: a row costs four registers.
@@ -377,7 +377,7 @@ struct SumBlocks {
 };
 
 template <typename ST, typename GT, int N>
-__global__ void __launch_bounds__(SUM_THREADS, 4) grad_sums_kernel(const __grid_constant__ EmbedGradArgs a, const SumBlocks blocks, int M) {
+__global__ void __launch_bounds__(SUM_THREADS, 7) grad_sums_kernel(const __grid_constant__ EmbedGradArgs a, const SumBlocks blocks, int M) {
     begin_and_let_next_begin();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     unsigned block = blockIdx.x;
@@ -469,6 +469,7 @@ cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_
     // too long, behind the sort, which knows.  Rows per block: 128, fewer where that leaves too few blocks.
     int rows = MOST_ZERO_ROWS;
     while (rows > SORT_WARPS && static_cast<int64_t>(a.vocab) * M < static_cast<int64_t>(rows) * 148 * 4) rows /= 2;
+    if (a.n > ZEROS_AHEAD && rows > 32 * SUM_WARPS) rows = 32 * SUM_WARPS;
     const int64_t zero_blocks = a.accumulate ? 0 : (static_cast<int64_t>(a.vocab) + rows - 1) / rows;
     const int64_t ahead = a.n <= ZEROS_AHEAD ? zero_blocks : 0, behind = zero_blocks - ahead;
     cudaError_t e = grad_bf16 ? launch_sort<__nv_bfloat16>(a, M, ahead, rows, stream) : launch_sort<float>(a, M, ahead, rows, stream);
