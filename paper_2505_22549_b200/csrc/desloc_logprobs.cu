@@ -360,24 +360,30 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     }
     Running r{-FLT_MAX, 0.f, 0.f};
     const uint4 *const pieces = reinterpret_cast<const uint4 *>(part.p + part.head);
-    const auto load = [&](uint4(&w)[AHEAD], int b) {
+    // whole rounds of AHEAD pieces per thread, then what is left; the next round's loads are on their way meanwhile
+    const int rounds = part.pieces / (AHEAD * THREADS);
+    uint4 next[AHEAD];
+    const auto load = [&](int round) {
+        const uint4 *const p = pieces + static_cast<long long>(round) * (AHEAD * THREADS) + tid;
+        const int left = part.pieces - round * (AHEAD * THREADS) - tid;
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) {
             constexpr uint32_t none = Words<T>::NONE;
-            w[k] = b + k * THREADS < part.pieces ? pieces[b + k * THREADS] : make_uint4(none, none, none, none);
+            if (round < rounds) next[k] = p[k * THREADS];
+            else next[k] = k * THREADS < left ? p[k * THREADS] : make_uint4(none, none, none, none);
         }
     };
-    uint4 next[AHEAD];
-    load(next, tid);
+    load(0);
     if (tid < part.head) take<ENT>(r, static_cast<float>(part.p[tid]));
     if (tid < part.tail) take<ENT>(r, static_cast<float>(part.p[part.tail_at(tid)]));
-    for (int b = tid; b < part.pieces; b += AHEAD * THREADS) {
+    for (int round = 0; round < rounds; ++round) {
         uint4 w[AHEAD];
 #pragma unroll
         for (int k = 0; k < AHEAD; ++k) w[k] = next[k];
-        load(next, b + AHEAD * THREADS);
+        load(round + 1);
         take_pieces<T, ENT>(r, w);
     }
+    if (rounds * (AHEAD * THREADS) + tid < part.pieces) take_pieces<T, ENT>(r, next);
     const float own = r.m;
     if constexpr (TOP) top.own[warp][lane] = own;
     r = join_lanes<ENT, 32>(r);
@@ -432,7 +438,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
 }
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS) logprobs_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(THREADS, 1280 / THREADS) logprobs_kernel(const LogprobArgs a) {
     logprobs_row<T, ENT, TOP, THREADS, 1>(a);
 }
 
