@@ -370,8 +370,8 @@ DESLOC_API int desloc_step_static(const desloc_config *cfg, float *const *x, flo
  * perplexity by which the paper compares its runs is exp of their mean, negated) and their gradient, and norm-based clipping of
  * gradients on its own.
  *
- * All take a stream, only enqueue work and can be captured; the same inputs give the same bits.  Outputs may not overlap inputs, or
- * one another, except where it says so.  Working memory is the caller's: what one call uses must not be used by another that may
+ * All take a stream, only enqueue work and can be captured (a captured call of a context belongs to its present workers, like a captured
+ * step); the same inputs give the same bits.  Outputs may not overlap inputs, or one another, except where it says so.  Working memory is the caller's: what one call uses must not be used by another that may
  * run at the same time (calls on one stream, one after the other, may share it), and a captured call needs its working memory for as
  * long as the graph is replayed.  Sums are held in fp32 or more and rounded once, to the nearest, at the end.
  */
@@ -419,7 +419,8 @@ DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor
  *   norms, factors     : device, [M] floats each, or NULL.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
  * max_norm must be > 0 and finite.  A norm that is not finite says that the gradients are not (or that their squares left fp32's range,
- * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  desloc_step_normclip() forms the same norms, up to the order of additions.
+ * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  desloc_step_normclip() forms the same norms, up to the order of
+ * additions.  Where a bounded wait on the device runs out, what is written is undefined, and later calls return DESLOC_E_DEVICE_WAIT.
  */
 DESLOC_API int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, const void *const *grads, int32_t out_dtype,
                                  void *const *out, float *norms, float *factors, void *work, int64_t work_bytes, void *stream);

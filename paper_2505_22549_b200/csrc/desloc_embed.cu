@@ -102,7 +102,8 @@ __device__ __forceinline__ void zero_block(const EmbedGradArgs &a, int m, unsign
     const Number *const tokens = static_cast<const Number *>(a.tokens.data) + m * a.tokens.s0;
 #pragma unroll 8
     for (int i = tid; i < a.n; i += SORT_THREADS) {
-        const auto r = static_cast<std::make_unsigned_t<Number>>(tokens[i * a.tokens.s1] - v0);
+        using Unsigned = std::make_unsigned_t<Number>;
+        const Unsigned r = static_cast<Unsigned>(tokens[i * a.tokens.s1]) - static_cast<Unsigned>(v0);
         if (r < static_cast<unsigned>(rows)) atomicOr(&s_seen[r / 32], 1u << (r % 32));
     }
     __syncthreads();

@@ -213,22 +213,25 @@ class DesLoc:
         if tokens.dtype not in _TOKEN_TYPES or tokens.dim() < 1 or tokens.shape[0] != self.M:
             raise ValueError("tokens are int32 or int64, [workers, ...]")
         _on(self.device, "tokens", tokens)
-        flat = tokens.reshape(self.M, -1)
+        flat = tokens.reshape(self.M, tokens.numel() // self.M)
         return B.rows(flat.data_ptr(), _TOKEN_TYPES[flat.dtype], *flat.stride()), flat
 
     def embed(self, tensor: int, tokens: torch.Tensor, scale: float = 1.0, dtype="bf16", width: Optional[int] = None,
               out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """scale * rows of every worker's x of `tensor` by token, on torch's current stream.  tokens: [M, ...] -> [M, ..., width] of `dtype`
-        ("f32", "bf16"; that of `out` where it is given).  Tokens outside the vocabulary give zeros."""
+        ("f32", "bf16" or torch's; that of `out` where it is given).  Tokens outside the vocabulary give zeros."""
         width = self._rows_of(tensor, width)
+        kind = _TYPES.get(dtype, B.DTYPE_BY_NAME.get(dtype))
+        if kind is None:
+            raise ValueError("embeddings are fp32 or bf16")
         if out is None:     # the usual layouts, natively
-            r = _native.embed(self.ctx, tensor, width, self.M, tokens, scale, B.DTYPE_BY_NAME.get(dtype, dtype), self._index)
+            r = _native.embed(self.ctx, tensor, width, self.M, tokens, scale, kind, self._index)
             if r is not None:
                 return r if type(r) is not int else self._raise(r, "desloc_embed")
         rows, flat = self._tokens(tokens)
         shape = tuple(tokens.shape) + (width,)
         if out is None:
-            out = torch.empty(shape, dtype=_TORCH_TYPES[B.DTYPE_BY_NAME.get(dtype, dtype)], device=self.device)
+            out = torch.empty(shape, dtype=_TORCH_TYPES[kind], device=self.device)
         elif tuple(out.shape) != shape or out.dtype not in _TYPES:
             raise ValueError("out does not fit the tokens")
         _on(self.device, "out", out)
@@ -253,7 +256,7 @@ class DesLoc:
         if tuple(dout.shape) != tuple(tokens.shape) + (width,) or dout.dtype not in _TYPES:
             raise ValueError("dout does not fit the tokens")
         _on(self.device, "dout", dout)
-        d = dout.reshape(self.M, -1, width) if flat.shape[1] else dout.new_empty(self.M, 0, width)
+        d = dout.reshape(self.M, flat.shape[1], width)
         if d.stride(-1) != 1 and width > 1:
             d = d.contiguous()
         nt = len(self.numel)

@@ -600,6 +600,43 @@ def test_a_tied_language_model_of_several_workers(grad_dtype):
     assert opt.counters()[0] == 4
 
 
+# ---- offsets that do not fit 32 bits -----------------------------------------------------------------
+def test_tables_of_more_than_two_to_the_31_elements():
+    V, D, n = (1 << 20) + 77, 2056, 50
+    x = torch.empty(1, V * D, device="cuda")
+    assert x.numel() > 1 << 31
+    opt = d.DesLoc([[x[0].view(V, D)]], [[torch.empty_like(x[0])]], None, opt="sgdm", grad_dtype="bf16", K=(1, 1, 1))
+    tokens = torch.cat([torch.arange(V - 20, V), torch.tensor([V - 1] * 40), torch.tensor([0, 5, V // 2])]).cuda()[None]
+    rows = torch.randn(tokens.shape[1], D, generator=gen_of(1), device="cuda")
+    x.view(V, D)[tokens[0]] = rows
+    assert torch.equal(opt.embed(0, tokens, dtype="f32")[0], x.view(V, D)[tokens[0]])
+    grads = [[torch.full((V, D), 5.0, dtype=BF, device="cuda")]]
+    dout = torch.randn(1, tokens.shape[1], D, generator=gen_of(2), device="cuda").to(BF)
+    opt.embed_grad(0, tokens, dout, grads)
+    seen = tokens.unique()
+    want = torch.stack([dout[0][tokens[0] == v].double().sum(0) for v in seen])
+    size = torch.stack([dout[0][tokens[0] == v].double().abs().sum(0) for v in seen])
+    check(grads[0][0][seen], want, size * 62 * U + want.abs() * HALF[BF] * 1.01)
+    empty = torch.ones(V, dtype=torch.bool, device="cuda")
+    empty[seen] = False
+    assert not bool(grads[0][0][-5000:][empty[-5000:]].any()) and not bool(grads[0][0][:5000][empty[:5000]].any())
+    assert int((grads[0][0] != 0).any(1).sum()) == len(seen)
+
+
+def test_rows_more_than_two_to_the_31_elements_apart():
+    V, far = 9000, (1 << 31) + 4096
+    buf = torch.empty(2 * far + V, dtype=BF, device="cuda")
+    x = buf.as_strided((3, V), (far, 1))
+    x.copy_(torch.randn(3, V, generator=gen_of(1), device="cuda") * 3)
+    t = torch.tensor([1, 2, V - 1], device="cuda")
+    check_logprobs(x, t, 5)
+    near = x.clone()
+    _, lse, _ = logprob_ref(near, t)
+    w = torch.ones(3, device="cuda")
+    want = d.token_logprobs_grad(near, t, lse.float(), w)
+    assert torch.equal(d.token_logprobs_grad(x, t, lse.float(), w, out=x), want)
+
+
 # ---- streams, graphs, refusals -----------------------------------------------------------------------
 def _all_calls(opt, s):
     out = opt.embed(0, s["tokens"], out=s["emb"])
@@ -648,6 +685,53 @@ def test_captured_calls_see_what_the_buffers_hold(V, n):
         for got in kept:
             for a, b in zip(got, fresh):
                 assert torch.equal(a, b)
+
+
+def test_captured_clipping_of_many_tensors():
+    """Thousands of addresses travel with the captured launches."""
+    numel = NUMEL["many"]
+    opt, _ = context(3, [(n,) for n in numel])
+    grads, out = lists(3, numel, F32, 1, True, [0.1, 1.0, 10.0]), lists(3, numel, BF, 2, True)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=side):
+        norms, factors = opt.clip_grads(grads, 2.0, out=out)
+    other = lists(3, numel, F32, 3, True)
+    opt.clip_grads(other, 2.0, out=lists(3, numel, BF, 4, True))        # other lists in between
+    for k in range(2):
+        for row in grads:
+            for t in row:
+                t.mul_(1.5)
+        for row in out:
+            for t in row:
+                t.zero_()
+        graph.replay()
+        got = [[t.clone() for t in row] for row in out]
+        n, f = norms.clone(), factors.clone()
+        n2, f2 = opt.clip_grads(grads, 2.0, out=out)
+        assert torch.equal(n, n2) and torch.equal(f, f2)
+        assert all(torch.equal(a, b) for x, y in zip(got, out) for a, b in zip(x, y))
+
+
+def test_a_wait_that_runs_out_is_reported_by_the_next_call():
+    numel = NUMEL["large"]
+    opt, _ = context(4, [(n,) for n in numel], grad_dtype="f32")
+    grads, out = lists(4, numel, F32, 1, False), lists(4, numel, F32, 2, False)
+    d.desloc_testing_set_wait_limit(opt.ctx, 0)
+    opt.clip_grads(grads, 1.0, out=out)
+    torch.cuda.synchronize()
+    tokens = torch.zeros(4, 3, dtype=torch.int64, device="cuda")
+    for call in (lambda: opt.clip_grads(grads, 1.0, out=out), lambda: opt.embed(0, tokens, width=1),
+                 lambda: opt.embed_grad(0, tokens, torch.zeros(4, 3, 1, device="cuda"), grads, width=1), lambda: opt.step(0, 1e-3, grads)):
+        with pytest.raises(d.DeslocError) as e:
+            call()
+        assert e.value.status == d.DESLOC_E_DEVICE_WAIT
+    d.desloc_testing_set_wait_limit(opt.ctx, -1)
+    norms, _ = opt.clip_grads(grads, 1.0, out=out)
+    for m in range(4):
+        want = float(torch.cat([t.double() for t in grads[m]]).norm())
+        assert abs(float(norms[m]) - want) <= 75 * U * want
 
 
 def test_calls_run_on_the_current_stream():
@@ -706,6 +790,12 @@ def test_refusals():
         refused(ValueError, lambda: opt.embed(0, bad))
         refused(ValueError, lambda: opt.embed_grad(0, bad, dout, g))
     refused(ValueError, lambda: opt.embed(5, tokens))
+    refused(ValueError, lambda: opt.embed(0, tokens, dtype="f16"))
+    refused(ValueError, lambda: opt.embed(0, tokens, dtype=torch.float16))
+    assert opt.embed(0, tokens, dtype=torch.float32).dtype == F32
+    none = torch.zeros(M, 0, dtype=torch.int64, device="cuda")
+    assert opt.embed(0, none, out=torch.zeros(M, 0, D, device="cuda")).shape == (M, 0, D)
+    opt.embed_grad(0, none, torch.zeros(M, 0, D, device="cuda"), tuple(g))
     refused(ValueError, lambda: opt.embed(-1, tokens))
     refused(ValueError, lambda: opt.embed(1, tokens))                            # one dimension and no width
     refused(d.DeslocError, lambda: opt.embed(1, tokens, width=5), d.DESLOC_E_RANGE)
