@@ -378,14 +378,17 @@ __device__ __forceinline__ void scale_span(const ST *from, DT *to, int n, float 
 }
 
 // Addresses on their way to the device in the kernel's parameters: a captured launch keeps them, no buffer has to.
-constexpr int ADDRESSES = 1000;
+// Blocks of a warp: parameters are read one address after the other by threads that ask for different ones.
+template <int N>
 struct Addresses {
-    const void *p[ADDRESSES];
+    const void *p[N];
 };
-__global__ void __launch_bounds__(256) addresses_kernel(const __grid_constant__ Addresses a, int n, const void **to) {
+template <int N>
+__global__ void __launch_bounds__(32) addresses_kernel(const __grid_constant__ Addresses<N> a, int n, const void **to) {
     begin_and_let_next_begin();
     wait_for_earlier_kernels();
-    for (int i = threadIdx.x; i < n; i += 256) to[i] = a.p[i];
+    const int i = static_cast<int>(blockIdx.x) * 32 + static_cast<int>(threadIdx.x);
+    if (i < n) to[i] = a.p[i];
 }
 
 // out^m = factor_m g^m, a chunk per block.  The last chunks first: of what the norms' pass read, the end is still in L2.
@@ -548,6 +551,14 @@ int64_t clip_work(int M, int nt, int64_t nrchunks, ClipWork *w, char *work) {
     return at;
 }
 
+// Addresses [i0, i0 + n) of the two lists behind one another, into their table.
+template <int N>
+static cudaError_t launch_addresses(const void *const *g, void *const *out, int nptr, int i0, int n, const void **tables, cudaStream_t stream) {
+    Addresses<N> a;
+    for (int i = 0; i < n; ++i) a.p[i] = i0 + i < nptr ? g[i0 + i] : out[i0 + i - nptr];
+    return launch(addresses_kernel<N>, (n + 31) / 32, 32, 0, stream, a, n, tables + i0);
+}
+
 cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, const void *const *g, bool g_bf16, void *const *out, bool out_bf16,
                         int nt, int M, float max_norm, float *norms, float *factors, const ClipWork &w, int *err, int wait_limit,
                         cudaStream_t stream, int *launches) {
@@ -561,13 +572,13 @@ cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, c
     if (small && nptr <= SMALL_CLIP_ADDRESSES) {
         for (int i = 0; i < nptr; ++i) few.few_g[i] = g[i], few.few_out[i] = out[i];
     } else {
-        for (int i0 = 0; i0 < 2 * nptr; i0 += ADDRESSES) {
-            Addresses a;
-            const int n = 2 * nptr - i0 < ADDRESSES ? 2 * nptr - i0 : ADDRESSES;
-            for (int i = 0; i < n; ++i) a.p[i] = i0 + i < nptr ? g[i0 + i] : out[i0 + i - nptr];
-            const cudaError_t e = launch(addresses_kernel, 1, 256, 0, stream, a, n, w.tables + i0);
+        for (int i0 = 0; i0 < 2 * nptr;) {
+            const int left = 2 * nptr - i0;
+            const cudaError_t e = left <= 500 ? launch_addresses<500>(g, out, nptr, i0, left, w.tables, stream)
+                                              : launch_addresses<2500>(g, out, nptr, i0, left < 2500 ? left : 2500, w.tables, stream);
             if (e != cudaSuccess) return e;
             *launches += 1;
+            i0 += 2500;
         }
         few.g = w.tables, few.out = w.tables + nptr;
     }
