@@ -2,7 +2,9 @@
 
 ``desloc_create / desloc_step / desloc_destroy`` and friends mirror include/desloc.h one to
 one (see binding.py).  ``DesLoc`` is a small convenience wrapper that keeps torch tensors
-alive and marshals their addresses; torch is used for device memory and streams only.
+alive and marshals their addresses; torch is used for device memory and streams only.  Around
+the step: ``DesLoc.embed``, ``embed_grad`` and ``clip_grads``, and ``token_logprobs`` and
+``token_logprobs_grad``, which need no context.
 
 The shared library is loaded on first use of any of those names, so that
 ``paper_2505_22549_b200.build`` can be imported to (re)build it.  There is no fallback: if

@@ -333,7 +333,11 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
 }
 
 // A block per row, or a cluster of CL blocks that take a part of it each and hand what they found to the first one through its shared
-// memory.  Bound: HBM reads of the logits, once; 16-byte loads, four to eight in flight per thread.
+// memory.  Bound: HBM reads of the logits, once (16-byte loads, four to eight in flight per thread), then the exponentials, 16 per clock and SM.
+// 4096 rows of 49152 bf16 logits with entropy and five alternatives: 78 us, 5.2 TB/s (0.79 of copy).  Before: value by value, blocks of 512 threads, the
+// alternatives looked for by single threads 172; blocks of 256 127 (of 128 134); two values per instruction and warps that look for alternatives 82;
+// whole rounds of loads without conditions and five blocks per SM 78 (four 82).  Without alternatives 8 us less.
+// Four rows of 49152 with 20 alternatives, clusters: 10.9 us (before keys that are ranked in one pass, and one barrier more, 23.7).
 template <typename T, bool ENT, bool TOP, int THREADS, int CL>
 __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     constexpr int WARPS = THREADS / 32, AHEAD = 4;
@@ -451,7 +455,7 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(THREADS) logpr
 
 template <typename T, bool ENT, bool TOP>
 cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
-    // Few long rows: a cluster each.
+    // Few long rows: a cluster each.  Shorter ones: as many threads as have a few pieces each.
     if (a.vocab >= 16384 && a.rows <= 148 / CLUSTER * 2)
         return launch_op(logprobs_cluster_kernel<T, ENT, TOP, 256>, dim3(a.rows * CLUSTER), dim3(256), 0, true, stream, a);
     if (a.vocab >= 8192) return launch_op(logprobs_kernel<T, ENT, TOP, 256>, dim3(a.rows), dim3(256), 0, true, stream, a);
@@ -460,6 +464,7 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
 
 // ---- gradient ----------------------------------------------------------------------------------------
 // out_j = a (1[j = token] - p_j) - b p_j (log p_j + H): elementwise over a row.  Bound: HBM, the logits read and as many bytes written.
+// 4096 rows of 49152 bf16 logits: 121 us, 6.6 TB/s (1.01 of copy); value by value 169; shares of 2 and 8 pieces a thread instead of 4 143 and 122.
 //
 // p_j = exp(x_j - lse) is off by |lse| 2^-24 from the rounding of lse.  Where that is more than an output of the type can bear (1.5e-5 for fp32, a quarter
 // of a step for bf16: logits of 1e4, or a row of the type's lowest value), the row's first block takes all of it, and goes over it for the largest
