@@ -93,7 +93,7 @@ __device__ __forceinline__ void zero_rows(const EmbedGradArgs &a, int m, int v0,
 }
 
 // The rows [block * zero_rows, ...) of the gradient that no token of the worker's stands for: zeros.
-constexpr int MOST_ZERO_ROWS = 16 * SORT_WARPS, ZEROS_AHEAD = 16384;   // (a block goes over all tokens: 2 us for 8192)
+constexpr int ZERO_ROWS = 32, MOST_ZERO_ROWS = 16 * SORT_WARPS, ZERO_BYTES = 300 * 1024, ZEROS_AHEAD = 16384;   // (a block goes over all tokens: 2 us for 8192)
 
 template <bool WIDE, typename GT>
 __device__ __forceinline__ void zero_block(const EmbedGradArgs &a, int m, unsigned block, int rows) {
@@ -245,8 +245,8 @@ constexpr int TILE = 8;
 // Rows in flight, unpacked when they are added: a row costs four registers.
 template <int N, typename ST>
 struct RowWords {
-    using Word = std::conditional_t<N == 1, ST, uint4>;
-    static constexpr int WORDS = N == 1 ? 1 : N * static_cast<int>(sizeof(ST)) / 16;
+    using Word = std::conditional_t<N == 1, ST, std::conditional_t<N == 2, std::conditional_t<sizeof(ST) == 2, uint32_t, uint2>, uint4>>;
+    static constexpr int WORDS = N <= 2 ? 1 : N * static_cast<int>(sizeof(ST)) / 16;
     Word w[WORDS];
     __device__ __forceinline__ void load(const ST *p) {
 #pragma unroll
@@ -363,8 +363,8 @@ __device__ __forceinline__ void sum_piece(const EmbedGradArgs &a, int m, int p, 
         for (int k = 0; k < 4; ++k)
             if (k0 + k < pc.n)
 #pragma unroll
-                for (int e = 0; e < N; e += N == 1 ? 1 : 4) {
-                    if constexpr (N == 1) {
+                for (int e = 0; e < N; e += N <= 2 ? 1 : 4) {
+                    if constexpr (N <= 2) {
                         f[k][e] = __ldcg(part + (k0 + k) * a.row + e);
                     } else {
                         const float4 v = __ldcg(reinterpret_cast<const float4 *>(part + (k0 + k) * a.row + e));
@@ -428,13 +428,19 @@ cudaError_t launch_sort(const EmbedGradArgs &a, int M, int64_t zero_blocks, int 
     return launch_op(kernel, dim3(static_cast<unsigned>(all)), dim3(SORT_THREADS), smem, true, stream, a, M, static_cast<unsigned>(zero_blocks), rows);
 }
 
-// Eight columns at a time where every row of both sides begins on a 16-byte boundary.
-bool eight_columns(const EmbedGradArgs &a, int M, bool dout_bf16, bool grad_bf16) {
+// Columns at a time: eight where every row of both sides begins on a 16-byte boundary, two where it begins on one of two elements, else one.
+int columns_at_a_time(const EmbedGradArgs &a, int M, bool dout_bf16, bool grad_bf16) {
     const long long ssz = dout_bf16 ? 2 : 4, gsz = grad_bf16 ? 2 : 4;
-    uintptr_t off = reinterpret_cast<uintptr_t>(a.dout) | static_cast<uintptr_t>(a.ds0 * ssz) | static_cast<uintptr_t>(a.ds1 * ssz) |
-                    static_cast<uintptr_t>(a.width * gsz);
-    for (int m = 0; m < M; ++m) off |= reinterpret_cast<uintptr_t>(a.g[m]);
-    return (off & 15u) == 0 && a.width % 8 == 0;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(a.dout) | static_cast<uintptr_t>(a.ds0 * ssz) | static_cast<uintptr_t>(a.ds1 * ssz);
+    uintptr_t to = static_cast<uintptr_t>(a.width * gsz);
+    for (int m = 0; m < M; ++m) to |= reinterpret_cast<uintptr_t>(a.g[m]);
+    if (((from | to) & 15u) == 0 && a.width % 8 == 0) return 8;
+    return (from & (2 * ssz - 1)) == 0 && (to & (2 * gsz - 1)) == 0 && a.width % 2 == 0 ? 2 : 1;
+}
+
+template <typename ST, typename GT>
+cudaError_t launch_sums(const EmbedGradArgs &a, int M, int columns, int64_t zero_blocks, int rows, cudaStream_t stream) {
+    return (columns == 8 ? launch_sums<ST, GT, 8> : columns == 2 ? launch_sums<ST, GT, 2> : launch_sums<ST, GT, 1>)(a, M, zero_blocks, rows, stream);
 }
 
 }  // namespace
@@ -472,11 +478,13 @@ int64_t plan_embed_grad(EmbedGradArgs &a, int M, char *work) {
 }
 
 cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_bf16, cudaStream_t stream, int *launches) {
-    const bool wide = eight_columns(a, M, dout_bf16, grad_bf16);
-    a.columns = (a.width + (wide ? 255 : 31)) / (wide ? 256 : 32);
+    const int columns = columns_at_a_time(a, M, dout_bf16, grad_bf16);
+    a.columns = (a.width + 32 * columns - 1) / (32 * columns);
     // Zeros: written while the tokens are sorted, by blocks that look all of them up themselves; beyond ZEROS_AHEAD tokens, where that takes
-    // too long, behind the sort, which knows.  Rows per block: 128, fewer where that leaves too few blocks.
+    // too long, behind the sort, which knows.  Rows per block: as many as have 300 KB of zeros to
+    // write (the more, the fewer blocks go over the tokens, and the later DRAM has something to do), fewer where that leaves too few blocks.
     int rows = MOST_ZERO_ROWS;
+    while (rows > ZERO_ROWS && static_cast<int64_t>(rows) * a.width * (grad_bf16 ? 2 : 4) > ZERO_BYTES) rows /= 2;
     while (rows > SORT_WARPS && static_cast<int64_t>(a.vocab) * M < static_cast<int64_t>(rows) * 148 * 4) rows /= 2;
     if (a.n > ZEROS_AHEAD && rows > 32 * SUM_WARPS) rows = 32 * SUM_WARPS;
     const int64_t zero_blocks = a.accumulate ? 0 : (static_cast<int64_t>(a.vocab) + rows - 1) / rows;
@@ -485,12 +493,8 @@ cudaError_t launch_embed_grad(EmbedGradArgs a, int M, bool dout_bf16, bool grad_
     if (e != cudaSuccess) return e;
     *launches = 1;
     using bf = __nv_bfloat16;
-    if (dout_bf16)
-        e = grad_bf16 ? (wide ? launch_sums<bf, bf, 8> : launch_sums<bf, bf, 1>)(a, M, behind, rows, stream)
-                      : (wide ? launch_sums<bf, float, 8> : launch_sums<bf, float, 1>)(a, M, behind, rows, stream);
-    else
-        e = grad_bf16 ? (wide ? launch_sums<float, bf, 8> : launch_sums<float, bf, 1>)(a, M, behind, rows, stream)
-                      : (wide ? launch_sums<float, float, 8> : launch_sums<float, float, 1>)(a, M, behind, rows, stream);
+    if (dout_bf16) e = (grad_bf16 ? launch_sums<bf, bf> : launch_sums<bf, float>)(a, M, columns, behind, rows, stream);
+    else e = (grad_bf16 ? launch_sums<float, bf> : launch_sums<float, float>)(a, M, columns, behind, rows, stream);
     if (e == cudaSuccess) *launches = 2;
     return e;
 }

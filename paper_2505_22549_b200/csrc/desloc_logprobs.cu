@@ -160,11 +160,12 @@ __device__ __forceinline__ void take_pieces(Running &r, uint4 (&w)[N]) {
     if constexpr (ENT) r.A = A.x + A.y;
 }
 
-// Lanes' values, the largest first.
+// Lanes' values, the largest first.  MERGE: they fall and then rise, or the other way round, already.
+template <bool MERGE>
 __device__ __forceinline__ float sort_lanes(float v) {
     const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int k = 2; k <= 32; k <<= 1) {
+    for (int k = MERGE ? 32 : 2; k <= 32; k <<= 1) {
 #pragma unroll
         for (int j = k >> 1; j > 0; j >>= 1) {
             const float o = __shfl_xor_sync(0xffffffffu, v, j);
@@ -186,7 +187,8 @@ __device__ __forceinline__ float value_of(Key key) {
     return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
-constexpr int MOST_TOP = DESLOC_MAX_TOP, CANDIDATES = 1024;
+constexpr int MOST_TOP = DESLOC_MAX_TOP;
+__host__ __device__ constexpr int candidates(int threads) { return threads > 32 ? 1024 : 256; }   // that a block has room for
 
 // The part of a row that a block takes, in pieces of 16 bytes: `head` values in front of the first boundary, `pieces`, `tail` values behind.
 template <typename T>
@@ -223,7 +225,7 @@ struct TopShared {
     float own[THREADS / 32][32];
     float line;
     int n;
-    Key key[CANDIDATES];
+    Key key[candidates(THREADS)];
     Key out[MOST_TOP];   // the largest ones, in order, where they have been ranked
     Key best[THREADS / 32];
 };
@@ -246,7 +248,7 @@ __device__ __forceinline__ void rank_keys(const Key *keys, int n, int top, const
 }
 
 // The `top` largest values of a part, whatever they are, into s.out: goes over the part in order and puts what beats the last of the list into it,
-// one at a time.  Only for parts with more than CANDIDATES values at or above the line that candidates_of_part() draws.
+// one at a time.  Only for parts with more than candidates(THREADS) values at or above the line that candidates_of_part() draws.
 template <typename T, int THREADS>
 __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS> &s, int top) {
     const int tid = threadIdx.x;
@@ -299,26 +301,43 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
 }
 
 // Candidates for the `top` largest values of a part into s.key; how many, which may be more than there is room for.  s.own holds the largest
-// that each thread has seen (-FLT_MAX: none), behind a barrier.  The line is the top-th largest of 32 groups' of threads largest values: at least
-// `top` values lie at or above it (all values, where fewer groups have any), only threads whose largest does have such, and their warps look at what these
+// that each thread has seen (-FLT_MAX: none), behind a barrier.  The line is the top-th largest of the threads' largest values, or of 32 groups' of threads where that
+// is near enough (32 groups and 32 alternatives: the line is the least of all, and half of the row above it; 16384 rows of 1000 logits 42 us and 168): at
+// least `top` values lie at or above it (all values, where fewer have any), only threads whose largest does have such, and their warps look at what these
 // took once more (some hundred bytes each, from L2).
+constexpr int TOP_OF_GROUPS = 8;
+
 template <typename T, int THREADS>
 __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared<THREADS> &s, float own, int top) {
-    const int tid = threadIdx.x;
-    if (tid < 32) {
-        float m = s.own[0][tid];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (THREADS == 32 || top <= TOP_OF_GROUPS) {
+        if (warp == 0) {
+            float m = s.own[0][lane];
 #pragma unroll
-        for (int w = 1; w < THREADS / 32; ++w) m = fmaxf(m, s.own[w][tid]);
-        m = sort_lanes(m);
-        if (tid == top - 1) s.line = m;
-        if (tid == 0) s.n = 0;
+            for (int w = 1; w < THREADS / 32; ++w) m = fmaxf(m, s.own[w][lane]);
+            m = sort_lanes<false>(m);
+            if (lane == top - 1) s.line = m;
+        }
+    } else {
+        s.own[warp][lane] = sort_lanes<false>(own);
+        __syncthreads();
+#pragma unroll
+        for (int half = THREADS / 64; half > 0; half >>= 1) {
+            if (warp < half) {
+                const float m = sort_lanes<true>(fmaxf(s.own[warp][lane], s.own[warp + half][31 - lane]));
+                s.own[warp][lane] = m;
+                if (half == 1 && lane == top - 1) s.line = m;
+            }
+            if (half > 1) __syncthreads();
+        }
     }
+    if (tid == 0) s.n = 0;
     __syncthreads();
     const float line = s.line;
     const auto collect = [&](int at, float x) {
         if (x >= line) {
             const int i = atomicAdd(&s.n, 1);
-            if (i < CANDIDATES) s.key[i] = key_of(x, at);
+            if (i < candidates(THREADS)) s.key[i] = key_of(x, at);
         }
     };
     // (a few pieces each: every thread its own, all at once)
@@ -396,9 +415,9 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     int found = 0;
     if constexpr (TOP) {
         found = candidates_of_part(part, top, own, a.top);
-        if (found > CANDIDATES) top_in_order<T, THREADS>(part, top, a.top);
+        if (found > candidates(THREADS)) top_in_order<T, THREADS>(part, top, a.top);
     }
-    const bool listed = found > CANDIDATES;   // they are in top.out, in order, not among the candidates
+    const bool listed = found > candidates(THREADS);   // they are in top.out, in order, not among the candidates
     if (CL == 1 && warp * 32 >= (listed ? 1 : max(found, 1))) return;
     r = join_lanes<ENT, WARPS>(s_warp[lane % WARPS]);
     const Key *keys = listed ? top.out : top.key;
@@ -442,7 +461,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
 }
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1280 / THREADS) logprobs_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(THREADS, THREADS > 32 ? 1280 / THREADS : 28) logprobs_kernel(const LogprobArgs a) {
     logprobs_row<T, ENT, TOP, THREADS, 1>(a);
 }
 
@@ -458,8 +477,13 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
     // Few long rows: a cluster each.  Shorter ones: as many threads as have a few pieces each.
     if (a.vocab >= 16384 && a.rows <= 148 / CLUSTER * 2)
         return launch_op(logprobs_cluster_kernel<T, ENT, TOP, 256>, dim3(a.rows * CLUSTER), dim3(256), 0, true, stream, a);
-    if (a.vocab >= 8192) return launch_op(logprobs_kernel<T, ENT, TOP, 256>, dim3(a.rows), dim3(256), 0, true, stream, a);
-    return launch_op(logprobs_kernel<T, ENT, TOP, 128>, dim3(a.rows), dim3(128), 0, true, stream, a);
+    // 16384 rows of 1000 bf16 logits: a warp each 18.8 us, 128 threads 27.2, 256 45.3; 7500 of 20000 with five alternatives 85, 67, 83; 1024 of 33000 33, 23, 20.
+    // (More alternatives than groups tell apart: 128 threads at least.)
+    constexpr int FEW = 1024, MANY = 4096;
+    const int pieces = TOP && a.top > TOP_OF_GROUPS && a.vocab / Part<T>::PER < FEW ? FEW : a.vocab / Part<T>::PER;
+    if (pieces >= MANY) return launch_op(logprobs_kernel<T, ENT, TOP, 256>, dim3(a.rows), dim3(256), 0, true, stream, a);
+    if (pieces >= FEW) return launch_op(logprobs_kernel<T, ENT, TOP, 128>, dim3(a.rows), dim3(128), 0, true, stream, a);
+    return launch_op(logprobs_kernel<T, ENT, TOP, 32>, dim3(a.rows), dim3(32), 0, true, stream, a);
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------

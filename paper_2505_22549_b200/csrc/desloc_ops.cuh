@@ -29,11 +29,17 @@ __device__ __forceinline__ int token_at(const TokenRows &t, long long at, int vo
     return v >= 0 && v < vocab ? static_cast<int>(v) : -1;
 }
 
-// N consecutive values as fp32, aligned to min(N * sizeof(T), 16) bytes; N = 1, 4 or 8.
+// N consecutive values as fp32, aligned to min(N * sizeof(T), 16) bytes; N = 1, 2, 4 or 8.
 template <int N, typename T>
 __device__ __forceinline__ void load_values(const T *p, float (&f)[N]) {
     if constexpr (N == 1) {
         f[0] = static_cast<float>(*p);
+    } else if constexpr (N == 2 && sizeof(T) == 4) {
+        const float2 v = *reinterpret_cast<const float2 *>(p);
+        f[0] = v.x, f[1] = v.y;
+    } else if constexpr (N == 2) {
+        const uint32_t w = *reinterpret_cast<const uint32_t *>(p);
+        f[0] = __uint_as_float(w << 16), f[1] = __uint_as_float(w & 0xffff0000u);
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
         for (int k = 0; k < N; k += 4) {
@@ -65,12 +71,15 @@ __device__ __forceinline__ void store_values(T *p, const float (&f)[N]) {
     if constexpr (sizeof(T) == 4) {
         if constexpr (N == 1) {
             *p = f[0];
+        } else if constexpr (N == 2) {
+            *reinterpret_cast<float2 *>(p) = make_float2(f[0], f[1]);
         } else {
 #pragma unroll
             for (int k = 0; k < N; k += 4) *reinterpret_cast<float4 *>(p + k) = make_float4(f[k], f[k + 1], f[k + 2], f[k + 3]);
         }
     } else {
         if constexpr (N == 1) *p = __float2bfloat16_rn(f[0]);
+        else if constexpr (N == 2) *reinterpret_cast<uint32_t *>(p) = pack_bf16(f[0], f[1]);
         else if constexpr (N == 4) *reinterpret_cast<uint2 *>(p) = make_uint2(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]));
         else *reinterpret_cast<uint4 *>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
     }
