@@ -14,37 +14,40 @@ namespace {
 // dependent loads.
 constexpr int EMBED_THREADS = 128;
 
+// N columns at a time, four times as many in flight.
+template <int N, typename OT>
+__device__ __forceinline__ void embed_row(const float *row, OT *out, int width, float scale, bool none) {
+    const int lanes = blockDim.x, n = width / N;
+    for (int c = threadIdx.x; c < n; c += 4 * lanes) {
+        float f[4][N];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (!none && c + k * lanes < n) load_values(row + N * (c + k * lanes), f[k]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (c + k * lanes >= n) break;
+#pragma unroll
+            for (int e = 0; e < N; ++e) f[k][e] = none ? 0.f : f[k][e] * scale;
+            store_values(out + N * (c + k * lanes), f[k]);
+        }
+    }
+}
+
 template <typename OT>
 __global__ void __launch_bounds__(EMBED_THREADS) embed_kernel(const EmbedArgs a) {
     begin_and_let_next_begin();
-    const int m = blockIdx.y, lanes = blockDim.x;
-    const int i = static_cast<int>(blockIdx.x * blockDim.y + threadIdx.y);
+    const int m = blockIdx.y, i = static_cast<int>(blockIdx.x * blockDim.y + threadIdx.y);
     wait_for_earlier_kernels();
     if (i >= a.n) return;
     const int tok = token_at(a.tokens, m * a.tokens.s0 + i * a.tokens.s1, a.vocab);
     OT *out = static_cast<OT *>(a.out) + m * a.os0 + i * a.os1;
     const float *row = a.x[static_cast<long long>(m) * a.x_stride] + static_cast<long long>(max(tok, 0)) * a.width;
-    const bool none = tok < 0;
-    if (a.width % 4 == 0 && (reinterpret_cast<uintptr_t>(row) & 15u) == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(OT) - 1)) == 0) {
-        for (int c = threadIdx.x; c < a.width / 4; c += 4 * lanes) {
-            float f[4][4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (!none && c + k * lanes < a.width / 4) load_values(row + 4 * (c + k * lanes), f[k]);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                if (c + k * lanes >= a.width / 4) break;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) f[k][e] = none ? 0.f : f[k][e] * a.scale;
-                store_values(out + 4 * (c + k * lanes), f[k]);
-            }
-        }
-    } else {
-        for (int c = threadIdx.x; c < a.width; c += lanes) {
-            const float f[1] = {none ? 0.f : row[c] * a.scale};
-            store_values(out + c, f);
-        }
-    }
+    const auto on = [&](unsigned n) {
+        return a.width % n == 0 && reinterpret_cast<uintptr_t>(row) % (4 * n) == 0 && reinterpret_cast<uintptr_t>(out) % (n * sizeof(OT)) == 0;
+    };
+    if (on(4)) embed_row<4>(row, out, a.width, a.scale, tok < 0);
+    else if (on(2)) embed_row<2>(row, out, a.width, a.scale, tok < 0);
+    else embed_row<1>(row, out, a.width, a.scale, tok < 0);
 }
 
 // ---- sort --------------------------------------------------------------------------------------------
@@ -235,7 +238,7 @@ __global__ void __launch_bounds__(SORT_THREADS, 3) token_sort_kernel(const __gri
 // One launch; a warp takes 32 * N columns of a piece of a long run, or of the short runs that begin in TILE places.  Behind them (where the sort's launch
 // has not written them) zeros in the rows without a token, which are most of a large vocabulary.  No barriers: warps wait for their loads alone.
 // Bound: HBM, rows of dout read and the gradient written; then the latency of three loads in a row (place, position, row of dout) at 28 warps per SM.
-// 4 workers x 8192 tokens, 49152 rows, bf16: width 576 65.5 us in both launches (41 at the copy rate), width 2048 165 (143).  Before, at width 576: a
+// 4 workers x 8192 tokens, 49152 rows, bf16: width 576 65.5 us in both launches (41 at the copy rate), width 2048 161 (143).  Before, at width 576: a
 // block per 16 rows of the gradient 226 us (most blocks wait for one row's loads), the same with zeros and sums by threads 93, tiles of places with pieces
 // of long runs by whole blocks 82, pieces by warps 70, blocks of four warps instead of eight 65.5.  Zeros in the sums' warps, behind a sort alone: 65, but
 // width 2048 171 and small problems 12 instead of 9.

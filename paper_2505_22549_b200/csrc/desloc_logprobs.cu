@@ -187,7 +187,7 @@ __device__ __forceinline__ float value_of(Key key) {
     return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
-constexpr int MOST_TOP = DESLOC_MAX_TOP;
+constexpr int MOST_TOP = DESLOC_MAX_TOP, WARP_ROWS = 4;
 __host__ __device__ constexpr int candidates(int threads) { return threads > 32 ? 1024 : 256; }   // that a block has room for
 
 // The part of a row that a block takes, in pieces of 16 bytes: `head` values in front of the first boundary, `pieces`, `tail` values behind.
@@ -218,6 +218,13 @@ __device__ __forceinline__ void visit_own(const Part<T> &part, int tid, int lane
 #pragma unroll
         for (int k = 0; k < Part<T>::PER; ++k) visit(at + k, f[k]);
     }
+}
+
+// A barrier of the threads that share a row.
+template <int THREADS>
+__device__ __forceinline__ void row_barrier() {
+    if constexpr (THREADS == 32) __syncwarp();
+    else __syncthreads();
 }
 
 template <int THREADS>
@@ -253,7 +260,7 @@ template <typename T, int THREADS>
 __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS> &s, int top) {
     const int tid = threadIdx.x;
     for (int i = tid; i < MOST_TOP; i += THREADS) s.out[i] = 0;
-    __syncthreads();
+    row_barrier<THREADS>();
     const int rounds = 2 + (part.pieces + THREADS - 1) / THREADS;   // the head, the pieces, the tail
     for (int r = 0; r < rounds; ++r) {
         float f[Part<T>::PER];
@@ -283,7 +290,7 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
                 best = o > best ? o : best;
             }
             if ((tid & 31) == 0) s.best[tid >> 5] = best;
-            __syncthreads();
+            row_barrier<THREADS>();
             best = 0;
 #pragma unroll
             for (int w = 0; w < THREADS / 32; ++w) best = s.best[w] > best ? s.best[w] : best;
@@ -294,9 +301,9 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
                 for (; i > 0 && s.out[i - 1] < own; --i) s.out[i] = s.out[i - 1];
                 s.out[i] = own;
             }
-            __syncthreads();
+            row_barrier<THREADS>();
         }
-        __syncthreads();   // s.best has been read
+        row_barrier<THREADS>();   // s.best has been read
     }
 }
 
@@ -305,7 +312,7 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
 // is near enough (32 groups and 32 alternatives: the line is the least of all, and half of the row above it; 16384 rows of 1000 logits 42 us and 168): at
 // least `top` values lie at or above it (all values, where fewer have any), only threads whose largest does have such, and their warps look at what these
 // took once more (some hundred bytes each, from L2).
-constexpr int TOP_OF_GROUPS = 8;
+constexpr int TOP_OF_GROUPS = 16;
 
 template <typename T, int THREADS>
 __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared<THREADS> &s, float own, int top) {
@@ -320,7 +327,7 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
         }
     } else {
         s.own[warp][lane] = sort_lanes<false>(own);
-        __syncthreads();
+        row_barrier<THREADS>();
 #pragma unroll
         for (int half = THREADS / 64; half > 0; half >>= 1) {
             if (warp < half) {
@@ -328,11 +335,11 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
                 s.own[warp][lane] = m;
                 if (half == 1 && lane == top - 1) s.line = m;
             }
-            if (half > 1) __syncthreads();
+            if (half > 1) row_barrier<THREADS>();
         }
     }
     if (tid == 0) s.n = 0;
-    __syncthreads();
+    row_barrier<THREADS>();
     const float line = s.line;
     const auto collect = [&](int at, float x) {
         if (x >= line) {
@@ -347,7 +354,7 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
         for (unsigned who = __ballot_sync(0xffffffffu, own >= line); who; who &= who - 1)
             visit_own<THREADS>(part, (tid & ~31) + __ffs(who) - 1, tid & 31, 32, collect);
     }
-    __syncthreads();
+    row_barrier<THREADS>();
     return s.n;
 }
 
@@ -360,14 +367,21 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
 template <typename T, bool ENT, bool TOP, int THREADS, int CL>
 __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     constexpr int WARPS = THREADS / 32, AHEAD = 4;
-    __shared__ Running s_warp[WARPS];
+    constexpr int ROWS = THREADS == 32 ? WARP_ROWS : 1;   // of a block: rows of a warp each share one
+    __shared__ Running s_warps[ROWS][WARPS];
     __shared__ Running s_part[CL];
-    __shared__ TopShared<TOP ? THREADS : 32> top;
+    __shared__ TopShared<THREADS> tops[TOP ? ROWS : 1];
     __shared__ Key s_lists[TOP && CL > 1 ? CL * MOST_TOP : 1];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const unsigned row = blockIdx.x / CL;
+    const unsigned slot = ROWS > 1 ? threadIdx.y : 0, row = blockIdx.x / CL * ROWS + slot;
     const int rank = static_cast<int>(blockIdx.x % CL);
+    Running(&s_warp)[WARPS] = s_warps[slot];
+    auto &top = tops[TOP ? slot : 0];
     begin_and_let_next_begin();
+    if (ROWS > 1 && row >= a.rows) {
+        wait_for_earlier_kernels();
+        return;
+    }
     if constexpr (CL > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // (do the blocks exist?  asked below)
     const unsigned i = row / a.inner, j = row - i * a.inner;
     const T *x = static_cast<const T *>(a.x) + i * a.xs0 + j * a.xs1;
@@ -411,7 +425,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     if constexpr (TOP) top.own[warp][lane] = own;
     r = join_lanes<ENT, 32>(r);
     if (lane == 0) s_warp[warp] = r;
-    __syncthreads();
+    row_barrier<THREADS>();
     int found = 0;
     if constexpr (TOP) {
         found = candidates_of_part(part, top, own, a.top);
@@ -461,7 +475,7 @@ __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
 }
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS > 32 ? 1280 / THREADS : 28) logprobs_kernel(const LogprobArgs a) {
+__global__ void __launch_bounds__(THREADS > 32 ? THREADS : 32 * WARP_ROWS, THREADS > 32 ? 1280 / THREADS : 10) logprobs_kernel(const LogprobArgs a) {
     logprobs_row<T, ENT, TOP, THREADS, 1>(a);
 }
 
@@ -477,13 +491,13 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
     // Few long rows: a cluster each.  Shorter ones: as many threads as have a few pieces each.
     if (a.vocab >= 16384 && a.rows <= 148 / CLUSTER * 2)
         return launch_op(logprobs_cluster_kernel<T, ENT, TOP, 256>, dim3(a.rows * CLUSTER), dim3(256), 0, true, stream, a);
-    // 16384 rows of 1000 bf16 logits: a warp each 18.8 us, 128 threads 27.2, 256 45.3; 7500 of 20000 with five alternatives 85, 67, 83; 1024 of 33000 33, 23, 20.
-    // (More alternatives than groups tell apart: 128 threads at least.)
+    // 16384 rows of 1000 bf16 logits: a warp each, four to a block, 10.5 us (one to a block 18.8), 128 threads 27.2, 256 45.3; 7500 of 20000 with five
+    // alternatives 85, 67, 83; 1024 of 33000 33, 23, 20.  (More alternatives than 32 groups tell apart: 128 threads at least.)
     constexpr int FEW = 1024, MANY = 4096;
     const int pieces = TOP && a.top > TOP_OF_GROUPS && a.vocab / Part<T>::PER < FEW ? FEW : a.vocab / Part<T>::PER;
     if (pieces >= MANY) return launch_op(logprobs_kernel<T, ENT, TOP, 256>, dim3(a.rows), dim3(256), 0, true, stream, a);
     if (pieces >= FEW) return launch_op(logprobs_kernel<T, ENT, TOP, 128>, dim3(a.rows), dim3(128), 0, true, stream, a);
-    return launch_op(logprobs_kernel<T, ENT, TOP, 32>, dim3(a.rows), dim3(32), 0, true, stream, a);
+    return launch_op(logprobs_kernel<T, ENT, TOP, 32>, dim3((a.rows + WARP_ROWS - 1) / WARP_ROWS), dim3(32, WARP_ROWS), 0, true, stream, a);
 }
 
 // ---- gradient ----------------------------------------------------------------------------------------

@@ -415,7 +415,7 @@ scale_kernel(const Chunk *chunks, unsigned nchunks, const void *const *g, const 
 // second pass.  Few addresses travel in the parameters: one launch in all.  From Python: 4096 parameters x 2 7.3 us (4.4 on the GPU), 0.2 M x 4 in 21
 // packed tensors, bf16, 8.8 us (by four launches 17.0).
 constexpr int SMALL_CLIP_ADDRESSES = 128, SMALL_CLIP_SHARES = 4;
-constexpr int64_t SMALL_CLIP_BYTES = 16 << 20;   // of all workers
+constexpr int64_t SMALL_CLIP_BYTES = 3 << 19;   // of a worker: eight SMs read 6.6 MB in 45 us, four launches take 17 for any small list
 struct SmallClip {
     const void *const *g, *const *out;   // tables, or null:
     const void *few_g[SMALL_CLIP_ADDRESSES], *few_out[SMALL_CLIP_ADDRESSES];
@@ -567,7 +567,7 @@ cudaError_t launch_clip(const Chunk *chunks, long long nchunks, int64_t elems, c
     const int nptr = M * nt;
     // A cluster per worker, up to SMALL_CLIP_SHARES chunks for each of its warps, where all clusters run at once.
     const bool small = small_norms(nchunks, elems, M, g_bf16) ||
-                       (M <= 148 / SMALL_BLOCKS && nchunks <= SMALL_CLIP_SHARES * SMALL_WARPS && elems * M * (g_bf16 ? 2 : 4) <= SMALL_CLIP_BYTES);
+                       (M <= 148 / SMALL_BLOCKS && nchunks <= SMALL_CLIP_SHARES * SMALL_WARPS && elems * (g_bf16 ? 2 : 4) <= SMALL_CLIP_BYTES);
     using bf = __nv_bfloat16;
     *launches = 0;
     SmallClip few{};
