@@ -418,8 +418,8 @@ DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor
  *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.
  *   norms, factors     : device, [M] floats each, or NULL.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
- * max_norm must be > 0 and finite.  A norm that is not finite says that the gradients are not (or that their squares left fp32's range,
- * beyond 1e19): f_m is 0 for an infinite norm and 1 for NaN.  desloc_step_normclip() forms the same norms, up to the order of
+ * max_norm must be > 0 and finite.  Squares are fp32 (values below 1e-22 count as 0).  A norm that is not finite says that the gradients are not, or that sums of
+ * some thousand squares left fp32's range (values beyond 1e17): f_m is 0 for an infinite norm and 1 for NaN.  desloc_step_normclip() forms the same norms, up to the order of
  * additions.  Where a bounded wait on the device runs out, what is written is undefined, and later calls return DESLOC_E_DEVICE_WAIT.
  */
 DESLOC_API int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, const void *const *grads, int32_t out_dtype,
