@@ -384,7 +384,7 @@ typedef enum { DESLOC_I32 = 0, DESLOC_I64 = 1 } desloc_index_t;
 typedef struct {
     void *data;
     int32_t dtype;     /* desloc_dtype_t; desloc_index_t for tokens */
-    int64_t stride[2]; /* in elements; rows that are written do not overlap */
+    int64_t stride[2]; /* in elements; rows that are written may not overlap (DESLOC_E_INVALID) */
 } desloc_rows;
 
 /*
@@ -402,7 +402,8 @@ DESLOC_API int desloc_embed(desloc_ctx *ctx, int32_t tensor, int64_t width, cons
  * zeros where there are none -- or, where `accumulate` is not 0, added to what the row holds, and rows without a token are left as they are
  * (the gradient of an output head with the same weights is there already).  Rows of tokens outside the vocabulary are not read.
  *   dout  : row (m, i), fp32 or bf16.
- *   grads : host array of M*num_tensors DEVICE pointers, as for desloc_step(); only those of `tensor` are read.
+ *   grads : host array of M*num_tensors DEVICE pointers, as for desloc_step(); only those of `tensor` are read.  DESLOC_E_INVALID where those of
+ *           two workers overlap.
  *   work, work_bytes : device memory, 256-byte aligned, of desloc_embed_grad_bytes() bytes at least (DESLOC_E_RANGE where it is less).
  */
 DESLOC_API int desloc_embed_grad(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows *tokens, int64_t n,
@@ -415,7 +416,8 @@ DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor
  * desloc_step_normclip() does on the way into its step, for gradients that go elsewhere (desloc_step_host(), desloc_step_masked(),
  * desloc_step_static(), a captured window, a log), or that were accumulated in fp32 and are handed to the step as bf16.
  *   grads, grads_dtype : host array of M*num_tensors DEVICE pointers, fp32 or bf16.
- *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.
+ *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.  DESLOC_E_INVALID where a worker and the next
+ *                        have the same address for a tensor.
  *   norms, factors     : device, [M] floats each, or NULL.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
  * max_norm must be > 0 and finite.  Squares are fp32 (values below 1e-22 count as 0).  A norm that is not finite says that the gradients are not, or that sums of

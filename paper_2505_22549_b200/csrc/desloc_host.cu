@@ -599,6 +599,16 @@ int check_table(const desloc_ctx *ctx, int32_t tensor, int64_t width, int64_t n)
     return numel % width == 0 && numel / width <= (1 << 30) ? DESLOC_OK : DESLOC_E_RANGE;
 }
 
+// Whether some of `count` (<= DESLOC_MAX_M) pieces of memory that are written share bytes.
+bool share_memory(void *const *at, int count, int64_t bytes) {
+    uintptr_t sorted[DESLOC_MAX_M];
+    for (int i = 0; i < count; ++i) sorted[i] = reinterpret_cast<uintptr_t>(at[i]);
+    std::sort(sorted, sorted + count);
+    for (int i = 1; i < count; ++i)
+        if (sorted[i] - sorted[i - 1] < static_cast<uintptr_t>(bytes)) return true;
+    return false;
+}
+
 int check_embedding(const desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows &tokens, int64_t n, float scale,
                     const desloc_rows &rows) {
     if (!desloc::is_token_rows(tokens) || !desloc::is_value_rows(rows)) return DESLOC_E_INVALID;
@@ -883,6 +893,7 @@ int desloc_embed(desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_ro
     if (rc != DESLOC_OK) return rc;
     if (n == 0) return DESLOC_OK;
     if (!tokens->data || !out->data) return DESLOC_E_NULL;
+    if (desloc::rows_overlap(*out, ctx->cfg.M, n, width)) return DESLOC_E_INVALID;
     desloc::EmbedArgs a{};
     a.x = reinterpret_cast<const float *const *>(ctx->res.d_tables) + tensor;
     a.x_stride = ctx->cfg.num_tensors;
@@ -924,6 +935,7 @@ int desloc_embed_grad(desloc_ctx *ctx, int32_t tensor, int64_t width, const desl
         if (!a.g[m]) return DESLOC_E_NULL;
         if (reinterpret_cast<uintptr_t>(a.g[m]) % (bf16 ? 2 : 4)) return DESLOC_E_INVALID;
     }
+    if (share_memory(a.g, c.M, ctx->numel[tensor] * (bf16 ? 2 : 4))) return DESLOC_E_INVALID;
     a.tokens = desloc::token_rows(*tokens);
     a.dout = dout->data;
     a.ds0 = dout->stride[0], a.ds1 = dout->stride[1];
@@ -957,6 +969,7 @@ int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, cons
         if (!grads[i] || !out[i]) return DESLOC_E_NULL;
         if (reinterpret_cast<uintptr_t>(grads[i]) % gsz || reinterpret_cast<uintptr_t>(out[i]) % osz) return DESLOC_E_INVALID;
         if (grads[i] == out[i] && gsz != osz) return DESLOC_E_INVALID;
+        if (i >= c.num_tensors && out[i] == out[i - c.num_tensors]) return DESLOC_E_INVALID;   // one list for several workers: scaled more than once
     }
     desloc::ClipWork w;
     if (desloc::clip_work(c.M, c.num_tensors, ctx->nrchunks, &w, static_cast<char *>(work)) > work_bytes) return DESLOC_E_RANGE;

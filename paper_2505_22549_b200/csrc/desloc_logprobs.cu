@@ -695,6 +695,7 @@ int desloc_token_logprobs_grad(int64_t outer, int64_t inner, int64_t vocab, cons
     if (!desloc::is_value_rows(*out) || out->dtype != logits->dtype) return DESLOC_E_INVALID;
     if (outer * inner == 0) return DESLOC_OK;
     if (!logits->data || !tokens->data || !out->data || !lse || !dlogp || (dentropy && !entropy)) return DESLOC_E_NULL;
+    if (desloc::rows_overlap(*out, outer, inner, vocab)) return DESLOC_E_INVALID;
     desloc::LogprobGradArgs a{};
     a.x = logits->data;
     a.xs0 = logits->stride[0], a.xs1 = logits->stride[1];

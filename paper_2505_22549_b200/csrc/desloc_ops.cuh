@@ -1,5 +1,7 @@
 // Operators around the step: launchers, and what their kernels share.
 #pragma once
+#include <cmath>
+
 #include <cuda_bf16.h>
 
 #include "../../include/desloc.h"
@@ -20,6 +22,15 @@ inline bool is_value_rows(const desloc_rows &r) {
 }
 inline bool is_token_rows(const desloc_rows &r) {
     return (r.dtype == DESLOC_I32 || r.dtype == DESLOC_I64) && reinterpret_cast<uintptr_t>(r.data) % (r.dtype == DESLOC_I64 ? 8 : 4) == 0;
+}
+// Whether rows of `width` elements that are written share some: of the two strides the smaller one (over what it reaches) has to pass a row, the larger
+// one all of those.  (In double: strides and counts are the caller's, and a product may leave 64 bits.)
+inline bool rows_overlap(const desloc_rows &r, int64_t outer, int64_t inner, int64_t width) {
+    double s[2] = {std::fabs(static_cast<double>(r.stride[0])), std::fabs(static_cast<double>(r.stride[1]))};
+    double n[2] = {static_cast<double>(outer), static_cast<double>(inner)};
+    const int first = n[1] <= 1 || (n[0] > 1 && s[0] < s[1]) ? 0 : 1;
+    const double reach = n[first] <= 1 ? width : s[first] * (n[first] - 1) + width;
+    return (n[first] > 1 && s[first] < width) || (n[1 - first] > 1 && s[1 - first] < reach);
 }
 inline TokenRows token_rows(const desloc_rows &r) { return {r.data, r.stride[0], r.stride[1], r.dtype == DESLOC_I64}; }
 

@@ -74,6 +74,14 @@ class BoundGrads:
     def __init__(self, array, keep):
         self.array, self._keep = array, keep
         self.address = ctypes.addressof(array)
+        self._device = None
+
+    def device(self) -> int:
+        """The device of all tensors, looked up once; -1 where there is none."""
+        if self._device is None:
+            found = {t.get_device() for row in self._keep for t in row}
+            self._device = found.pop() if len(found) == 1 else -1
+        return self._device
 
 
 class DesLoc:
@@ -248,7 +256,7 @@ class DesLoc:
         """The gradient of embed() into the workers' gradients of `tensor` in `grads` (what step() reads: nested lists, of which only that
         tensor is looked at, or bind_grads()' handle).  accumulate: added to what they hold."""
         width = self._rows_of(tensor, width)
-        r = _native.embed_grad(self.ctx, tensor, width, self.M, tokens, dout, grads.address if isinstance(grads, BoundGrads) else grads, len(self.numel),
+        r = _native.embed_grad(self.ctx, tensor, width, self.M, tokens, dout, self._bound(grads) if isinstance(grads, BoundGrads) else grads, len(self.numel),
                                self.numel[tensor], self.grad_dtype, scale, accumulate, self._index)
         if r is not None:
             return None if r == 0 else self._raise(r, "desloc_embed_grad")
@@ -276,10 +284,16 @@ class DesLoc:
         B.desloc_embed_grad(self.ctx, tensor, width, rows, n, B.rows(d.data_ptr(), _TYPES[d.dtype], *d.stride()[:2]), scale, accumulate, array,
                             work.data_ptr(), work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
 
+    def _bound(self, grads) -> int:
+        """Address of a handle's array, if it was made for as many workers as there are now, of tensors on this device."""
+        if len(grads.array) != self.M * len(self.numel) or grads.device() != self._index:
+            raise ValueError(_GRAD_MISFIT)
+        return grads.address
+
     def _list_of(self, table, grads):
         """(address, type code) of a set of gradient tensors of one type, on this context's device."""
         if isinstance(grads, BoundGrads):
-            return grads.address, self.grad_dtype
+            return self._bound(grads), self.grad_dtype
         kind = _TYPES.get(grads[0][0].dtype) if len(grads) and len(grads[0]) else None
         if kind is None:
             raise ValueError(_GRAD_MISFIT)

@@ -112,3 +112,21 @@ def test_two_strides_reach_every_row(make):
 def test_three_strides_are_more_than_two():
     x = torch.arange(4 * 5 * 4 * 6).view(4, 5, 4, 6)[:, ::2, ::2]
     assert module._split(tuple(x.shape[:-1]), [x]) is None
+
+
+@pytest.mark.parametrize("outer, inner, strides, overlap", [
+    (2, 3, (24, 8), False), (2, 3, (8, 16), False), (3, 2, (8, 24), False), (2, 3, (-24, -8), False), (1, 3, (0, 8), False), (2, 1, (8, 0), False),
+    (1, 1, (0, 0), False), (2, 3, (0, 8), True), (2, 3, (24, 0), True), (2, 3, (24, 7), True), (2, 3, (23, 8), True), (2, 3, (8, 15), True),
+    (2, 3, (8, 8), True), (1, 3, (100, 4), True), (2, 1, (7, 100), True), (2, 3, (-24, -7), True)])
+def test_written_rows_that_overlap_are_refused(outer, inner, strides, overlap):
+    reached = sorted(i * strides[0] + j * strides[1] for i in range(outer) for j in range(inner))
+    assert overlap == any(b - a < 8 for a, b in zip(reached, reached[1:]))
+    if overlap:     # (what is not refused would run)
+        with pytest.raises(d.DeslocError) as e:
+            _grad(outer=outer, inner=inner, out=B.rows(1 << 20, d.DESLOC_F32, *strides))()
+        assert e.value.status == d.DESLOC_E_INVALID
+
+
+def test_the_device_of_bound_gradients():
+    rows = [[torch.zeros(3), torch.zeros(2)] for _ in range(2)]
+    assert module.BoundGrads((ctypes.c_void_p * 4)(), rows).device() == -1

@@ -864,3 +864,49 @@ def test_refusals():
     refused(d.DeslocError, lambda: clip(ot=0), d.DESLOC_E_INVALID)               # in place, another type
     refused(d.DeslocError, lambda: clip(g=[0] * 4), d.DESLOC_E_NULL)
     refused(d.DeslocError, lambda: clip(o=[ptrs[0] + 1] + ptrs[1:]), d.DESLOC_E_INVALID)
+
+
+@pytest.mark.parametrize("M", [2, 5])
+def test_outputs_that_overlap_are_refused(M):
+    V, D, dev = 50, 8, "cuda"
+    opt, _ = context(M, [(V, D), (13,)])
+    tokens, dout = torch.zeros(M, 4, dtype=torch.int64, device=dev), torch.ones(M, 4, D, device=dev)
+    g = [[torch.zeros(V, D, dtype=BF, device=dev), torch.zeros(13, dtype=BF, device=dev)] for _ in range(M)]
+
+    def invalid(call):
+        with pytest.raises(d.DeslocError) as e:
+            call()
+        assert e.value.status == d.DESLOC_E_INVALID
+
+    one = torch.zeros(D, device=dev)
+    invalid(lambda: opt.embed(0, tokens, out=one.expand(M, 4, D)))
+    invalid(lambda: opt.embed(0, tokens, out=torch.zeros(4, D, device=dev).expand(M, 4, D)))
+    invalid(lambda: opt.embed(0, tokens, out=torch.zeros(M * 4 * D, device=dev).as_strided((M, 4, D), (4 * D, D - 1, 1))))
+    both = torch.zeros(4, M, D, device=dev)
+    opt.embed(0, tokens, out=both.transpose(0, 1))                               # rows of the workers in turn do not
+    assert torch.equal(both.transpose(0, 1), opt.embed(0, tokens, dtype="f32"))
+    whole = torch.zeros(2 * V * D, dtype=BF, device=dev)
+    invalid(lambda: opt.embed_grad(0, tokens, dout, g[:M - 1] + g[:1]))
+    invalid(lambda: opt.embed_grad(0, tokens, dout, [[whole[V * D:], g[0][1]]] + g[:M - 2] + [[whole[V * D - 1:-1], g[0][1]]]))
+    opt.embed_grad(0, tokens, dout, [[whole[V * D:], g[0][1]]] + g[:M - 2] + [[whole[:V * D], g[0][1]]])   # one behind the other do not
+    assert whole[::V * D].tolist() == [4, 4]
+    invalid(lambda: opt.clip_grads(g[:1] * M, 1.0))
+    invalid(lambda: opt.clip_grads(g, 1.0, out=[[a[0].clone(), g[0][1]] for a in g]))
+    opt.clip_grads(g[:1] * M, 1.0, out=g[1:] + [[t.clone() for t in g[0]]])      # read by all of them is fine
+    x, t = torch.zeros(8, device=dev).expand(2, 3, 8), torch.zeros(2, 3, dtype=torch.int64, device=dev)
+    r, w = d.token_logprobs(x, t), torch.ones(2, 3, device=dev)
+    invalid(lambda: d.token_logprobs_grad(x, t, r.lse, w, out=x))                # rows that all are one
+    assert d.token_logprobs_grad(x, t, r.lse, w).shape == x.shape
+
+
+def test_bound_gradients_of_other_workers_or_from_the_host_are_refused():
+    V, D, dev = 50, 8, "cuda"
+    opt, state = context(1, [(V, D)])
+    two, _ = context(2, [(V, D)])
+    tokens, dout = torch.zeros(2, 4, dtype=torch.int64, device=dev), torch.ones(2, 4, D, device=dev)
+    few = opt.bind_grads([[torch.zeros(V, D, dtype=BF, device=dev)]])
+    host = two.bind_grads([[torch.zeros(V, D, dtype=BF)] for _ in range(2)])
+    for bound in (few, host):
+        for call in (lambda: two.embed_grad(0, tokens, dout, bound), lambda: two.clip_grads(bound, 1.0)):
+            with pytest.raises(ValueError, match="gradient tensor"):
+                call()
