@@ -450,6 +450,7 @@ DESLOC_API int desloc_token_logprobs(int64_t outer, int64_t inner, int64_t vocab
  *   out_j := dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy),
  * the first part 0 where the token is outside [0, vocab).  A row whose two weights are 0 (or that has no token and no dentropy) gets zeros,
  * whatever its logits hold, and so does one of nothing but -inf.
+ * Probabilities below 2^-126 are 0, and 0 times any finite weight is 0: masked logits have no gradient.
  *   lse, entropy : of desloc_token_logprobs(), dense fp32.      dlogp, dentropy : dense fp32, any may hold 0.
  *   dentropy     : or NULL; entropy is needed with it only.
  *   out          : rows of the logits' type; may be the logits themselves.

@@ -25,7 +25,7 @@ __device__ __forceinline__ float exp2_fast(float t) {
 struct Running {
     float m, S, A;
 };
-constexpr float HUGE_LOGIT = 1e6f, LOWEST_LOGIT = -1e37f;
+constexpr float HUGE_LOGIT = 1e6f;
 __device__ __forceinline__ float base_of(float m) { return __fmul_rn(m, LOG2E); }
 __device__ __forceinline__ bool is_huge(float m) { return fabsf(m) > HUGE_LOGIT; }
 __device__ __forceinline__ float behind_base(float m) { return fmaf(m, LOG2E, -base_of(m)); }   // what the rounding took
@@ -88,10 +88,12 @@ struct Words<float> {
             m = fmaxf(m, fmaxf(fmaxf(__uint_as_float(w[k].x), __uint_as_float(w[k].y)), fmaxf(__uint_as_float(w[k].z), __uint_as_float(w[k].w))));
         return m;
     }
-    // -inf becomes a finite value whose exponential is 0 all the same; NaN stays
-    static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+    static constexpr uint32_t LOWEST = 0xfcf0bdc2u;   // -1e37: finite, and its exponential 0
+    static __device__ __forceinline__ uint32_t both(float x) { return __float_as_uint(x); }
+    // The larger of each; NaN stays.
+    static __device__ __forceinline__ uint32_t at_least(uint32_t low, uint32_t w) {
         float r;
-        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(LOWEST_LOGIT));
+        asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(__uint_as_float(w)), "f"(__uint_as_float(low)));
         return __float_as_uint(r);
     }
 };
@@ -114,12 +116,19 @@ struct Words<__nv_bfloat16> {
         for (int k = 0; k < N; ++k) m = larger(m, larger(larger(w[k].x, w[k].y), larger(w[k].z, w[k].w)));
         return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
     }
-    static __device__ __forceinline__ uint32_t finite(uint32_t w) {
+    static constexpr uint32_t LOWEST = 0xfcf0fcf0u;
+    static __device__ __forceinline__ uint32_t both(float x) { return pack_bf16(x, x); }
+    static __device__ __forceinline__ uint32_t at_least(uint32_t low, uint32_t w) {
         uint32_t r;
-        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0xfcf0fcf0u));   // LOWEST_LOGIT
+        asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(low));
         return r;
     }
 };
+
+template <typename T>
+__device__ __forceinline__ void raise_words(uint32_t low, uint4 &w) {
+    w = make_uint4(Words<T>::at_least(low, w.x), Words<T>::at_least(low, w.y), Words<T>::at_least(low, w.z), Words<T>::at_least(low, w.w));
+}
 
 // A piece, value by value: of rows with values beyond HUGE_LOGIT only.
 template <typename T, bool ENT>
@@ -148,7 +157,7 @@ __device__ __forceinline__ void take_pieces(Running &r, uint4 (&w)[N]) {
     float2 S = make_float2(r.S, 0.f), A = make_float2(ENT ? r.A : 0.f, 0.f);
 #pragma unroll
     for (int k = 0; k < N; ++k) {
-        if constexpr (ENT) w[k] = make_uint4(Words<T>::finite(w[k].x), Words<T>::finite(w[k].y), Words<T>::finite(w[k].z), Words<T>::finite(w[k].w));
+        if constexpr (ENT) raise_words<T>(Words<T>::LOWEST, w[k]);
 #pragma unroll
         for (int e = 0; e < 8 / static_cast<int>(sizeof(T)); ++e) {
             const float2 t = __ffma2_rn(Words<T>::pair(w[k], e), scale, from), p = make_float2(exp2_fast(t.x), exp2_fast(t.y));
@@ -509,6 +518,10 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
 // logit and the sum behind it instead: slow, and rare.
 constexpr int GRAD_THREADS = 256, GRAD_AHEAD = 4;
 
+// With entropy, log p is a factor beside the caller's weight.  Logits more than NO_LOGIT below lse, whose p is 0 (2^-126 is e^-87; bf16's steps at the largest
+// lse take 64 of the 200), stand NO_LOGIT below it, so that 0 * weight * log p is 0 for weights up to MOST_WEIGHT; rows with larger ones go value by value.
+constexpr float NO_LOGIT = 200.f, MOST_WEIGHT = 1e30f;
+
 template <typename T>
 __device__ __noinline__ Running sum_of_row(const Part<T> part) {
     __shared__ Running s_warp[GRAD_THREADS / 32];
@@ -520,7 +533,7 @@ __device__ __noinline__ Running sum_of_row(const Part<T> part) {
     return join_lanes<false, GRAD_THREADS / 32>(s_warp[threadIdx.x % (GRAD_THREADS / 32)]);
 }
 
-// All of a row with a large lse, value by value.
+// All of a row with a large lse or weights that a product with log p may not bear, value by value.
 template <typename T, bool ENT>
 __device__ __noinline__ void grad_slowly(const Part<T> part, T *out, int tok, float wa, float wb, float H) {
     const Running r = sum_of_row(part);
@@ -528,9 +541,8 @@ __device__ __noinline__ void grad_slowly(const Part<T> part, T *out, int tok, fl
     __syncthreads();   // out may be the logits: all of the block have read them
     const int n = part.head + part.pieces * Part<T>::PER + part.tail;
     for (int j = threadIdx.x; j < n; j += GRAD_THREADS) {
-        const float lp = (static_cast<float>(part.p[j]) - r.m) - log_sum, p = exp2_fast(lp * LOG2E);
-        const float w = ENT ? fmaf(wb, fmaxf(lp, FAR_BELOW) + H, wa) : wa;
-        const float g[1] = {j == tok ? fmaf(-p, w, wa) : -p * w};
+        const float lp = (static_cast<float>(part.p[j]) - r.m) - log_sum, p = exp2_fast(lp * LOG2E), one = j == tok ? fmaf(-p, wa, wa) : -p * wa;
+        const float g[1] = {ENT ? fmaf(-p * (fmaxf(lp, FAR_BELOW) + H), wb, one) : one};   // (0 comes before the weight)
         store_values(out + j, g);
     }
 }
@@ -566,7 +578,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
         if (edge_at >= 0) out[edge_at] = T(0.f);
         return;
     }
-    if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f)) {
+    if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f) || fabsf(wa) > MOST_WEIGHT || (ENT && fabsf(wb) > MOST_WEIGHT)) {
         if (b == 0) grad_slowly<T, ENT>(part, out, tok, wa, wb, H);
         return;
     }
@@ -574,6 +586,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
     const float base = base_of(lse), off = behind_base(lse), q = exp2_fast(-off);
     const float c1 = ENT ? -q * wb * LN2 : 0.f, c0 = -q * (ENT ? fmaf(wb, H - off * LN2, wa) : wa);
     const float2 scale = make_float2(LOG2E, LOG2E), from = make_float2(-base, -base), C0 = make_float2(c0, c0), C1 = make_float2(c1, c1);
+    const uint32_t low = Words<T>::both(lse - NO_LOGIT);
     uint4 w[GRAD_AHEAD];
 #pragma unroll
     for (int k = 0; k < GRAD_AHEAD; ++k)
@@ -582,7 +595,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
     for (int k = 0; k < GRAD_AHEAD; ++k) {
         if (first + k * GRAD_THREADS >= part.pieces) break;
         const int at = part.piece_at(first + k * GRAD_THREADS);
-        if constexpr (ENT) w[k] = make_uint4(Words<T>::finite(w[k].x), Words<T>::finite(w[k].y), Words<T>::finite(w[k].z), Words<T>::finite(w[k].w));
+        if constexpr (ENT) raise_words<T>(low, w[k]);
         float g[PER];
 #pragma unroll
         for (int e = 0; e < PER / 2; ++e) {
@@ -606,7 +619,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
     if (edge_at >= 0) {
         float t = fmaf(static_cast<float>(x[edge_at]), LOG2E, -base);
         const float p = exp2_fast(t);
-        if constexpr (ENT) t = fmaxf(t, FAR_BELOW);
+        if constexpr (ENT) t = fmaxf(t, -NO_LOGIT * LOG2E);
         const float g[1] = {p * (ENT ? fmaf(t, c1, c0) : c0) + (edge_at == tok ? wa : 0.f)};
         store_values(out + edge_at, g);
     }

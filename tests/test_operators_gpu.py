@@ -422,6 +422,32 @@ def test_logprobs_grad_of_masked_rows(kind, dtype):
     check_grad(x, torch.randint(0, 1031, (2, 5), generator=gen_of(4), device="cuda", dtype=torch.int32))
 
 
+@pytest.mark.parametrize("weight", [40.0, 1e5, 1e10, -1e29, 1e31, 1e36])
+@pytest.mark.parametrize("dtype", [F32, BF])
+@pytest.mark.parametrize("lowest", [False, True])
+def test_logprobs_grad_of_masked_logits_is_zero_whatever_the_weights(lowest, dtype, weight):
+    """A probability of 0 takes any weight to 0: in pieces of 16 bytes, in front of them and behind, near zero and where rows are summed anew."""
+    V = 1031
+    low = torch.finfo(dtype).min if lowest else -math.inf
+    for offset, first in ((0.0, 0), (0.0, 3), (-100.0, 5), (3e4, 1)):
+        x = (torch.randn(2, 5, V, generator=gen_of(6), device="cuda") * 3 + offset).to(dtype)
+        x[..., ::3] = low
+        x[:, 1, 10:] = low
+        x = torch.cat([x.new_zeros(2, 5, first), x], -1)[..., first:]
+        t = torch.randint(0, V, (2, 5), generator=gen_of(7), device="cuda")
+        _, lse, H = logprob_ref(x, t)
+        lse, H = lse.float(), H.float()
+        a, b = torch.randn(2, 5, generator=gen_of(8), device="cuda"), torch.randn(2, 5, generator=gen_of(9), device="cuda") * 0.1
+        b = b + math.copysign(1.0, weight)          # nowhere near 0
+        for a1, b1 in ((a, b * abs(weight)), (a * abs(weight), b), (a * abs(weight), b * abs(weight))):
+            want, tol = grad_ref(x, t, lse, a1, H, b1)
+            got = d.token_logprobs_grad(x, t, lse, a1, H, b1)
+            masked = (x <= low) & (torch.arange(V, device="cuda") != t[..., None])
+            assert bool((got[masked] == 0).all())
+            # (a probability below 2^-126 is 0)
+            check(got, want, tol + 2.0 ** -126 * (a1.abs() + 100 * b1.abs()).double()[..., None])
+
+
 def test_logprobs_grad_layouts():
     g = gen_of(8)
     for dtype, V in ((BF, 1000), (F32, 1001), (BF, 9001)):
