@@ -450,6 +450,8 @@ DESLOC_API int desloc_token_logprobs(int64_t outer, int64_t inner, int64_t vocab
  *   out_j := dlogp (1[j = token] - p_j) - dentropy p_j (log p_j + entropy),
  * the first part 0 where the token is outside [0, vocab).  A row whose two weights are 0 (or that has no token and no dentropy) gets zeros,
  * whatever its logits hold, and so does one of nothing but -inf.
+ * p_j and log p_j come from lse as it is given: off by |lse| 2^-24 (relative, and absolute), so that the token's entry is off by |dlogp| p |lse| 2^-24 however
+ * little 1 - p is.  Where |lse| is more than 256, they come from the row itself.
  * Probabilities below 2^-126 are 0, and 0 times any finite weight is 0: masked logits have no gradient.
  *   lse, entropy : of desloc_token_logprobs(), dense fp32.      dlogp, dentropy : dense fp32, any may hold 0.
  *   dentropy     : or NULL; entropy is needed with it only.

@@ -513,14 +513,14 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
 // out_j = a (1[j = token] - p_j) - b p_j (log p_j + H): elementwise over a row.  Bound: HBM, the logits read and as many bytes written.
 // 4096 rows of 49152 bf16 logits: 121 us, 6.6 TB/s (1.01 of copy); value by value 169; shares of 2 and 8 pieces a thread instead of 4 143 and 122.
 //
-// p_j = exp(x_j - lse) is off by |lse| 2^-24 from the rounding of lse.  Where that is more than an output of the type can bear (1.5e-5 for fp32, a quarter
-// of a step for bf16: logits of 1e4, or a row of the type's lowest value), the row's first block takes all of it, and goes over it for the largest
-// logit and the sum behind it instead: slow, and rare.
+// p_j = exp(x_j - lse) is off by |lse| 2^-24 of itself from the rounding of lse, and what the token's own entry and the entropy's part leave of a difference
+// is off by as much of p, however little is left.  Where that passes 1.5e-5 (FAR_LSE; a few steps of 1 - p already in bf16, where the next logit is 8 below),
+// the row's first block takes all of the row, and goes over it for the largest logit and the sum behind it instead: slow, and rare.
 constexpr int GRAD_THREADS = 256, GRAD_AHEAD = 4;
 
 // With entropy, log p is a factor beside the caller's weight.  Logits more than NO_LOGIT below lse, whose p is 0 (2^-126 is e^-87; bf16's steps at the largest
-// lse take 64 of the 200), stand NO_LOGIT below it, so that 0 * weight * log p is 0 for weights up to MOST_WEIGHT; rows with larger ones go value by value.
-constexpr float NO_LOGIT = 200.f, MOST_WEIGHT = 1e30f;
+// lse take one of the 200), stand NO_LOGIT below it, so that 0 * weight * log p is 0 for weights up to MOST_WEIGHT; rows with larger ones go value by value.
+constexpr float NO_LOGIT = 200.f, MOST_WEIGHT = 1e30f, FAR_LSE = 256.f;
 
 template <typename T>
 __device__ __noinline__ Running sum_of_row(const Part<T> part) {
@@ -541,7 +541,7 @@ __device__ __noinline__ void grad_slowly(const Part<T> part, T *out, int tok, fl
     __syncthreads();   // out may be the logits: all of the block have read them
     const int n = part.head + part.pieces * Part<T>::PER + part.tail;
     for (int j = threadIdx.x; j < n; j += GRAD_THREADS) {
-        const float lp = (static_cast<float>(part.p[j]) - r.m) - log_sum, p = exp2_fast(lp * LOG2E), one = j == tok ? fmaf(-p, wa, wa) : -p * wa;
+        const float lp = (static_cast<float>(part.p[j]) - r.m) - log_sum, p = exp2_fast(lp * LOG2E), one = j == tok ? -expm1f(lp) * wa : -p * wa;
         const float g[1] = {ENT ? fmaf(-p * (fmaxf(lp, FAR_BELOW) + H), wb, one) : one};   // (0 comes before the weight)
         store_values(out + j, g);
     }
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(GRAD_THREADS) logprobs_grad_kernel(const Logpr
         if (edge_at >= 0) out[edge_at] = T(0.f);
         return;
     }
-    if (fabsf(lse) > (sizeof(T) == 2 ? 16384.f : 256.f) || fabsf(wa) > MOST_WEIGHT || (ENT && fabsf(wb) > MOST_WEIGHT)) {
+    if (fabsf(lse) > FAR_LSE || fabsf(wa) > MOST_WEIGHT || (ENT && fabsf(wb) > MOST_WEIGHT)) {
         if (b == 0) grad_slowly<T, ENT>(part, out, tok, wa, wb, H);
         return;
     }

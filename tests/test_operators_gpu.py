@@ -448,6 +448,24 @@ def test_logprobs_grad_of_masked_logits_is_zero_whatever_the_weights(lowest, dty
             check(got, want, tol + 2.0 ** -126 * (a1.abs() + 100 * b1.abs()).double()[..., None])
 
 
+@pytest.mark.parametrize("offset", [0.0, 304.0, 600.0, -1016.0, 1504.0, -1504.0, 1968.0])
+def test_logprobs_grad_of_confident_bf16_rows_far_from_zero(offset):
+    """1 - p at the token of rows whose next logits are a few steps below: what is left of it does not drown in the rounding of a large lse."""
+    V = 1031
+    x = torch.full((4, 3, V), offset - 200.0, device="cuda").to(BF)
+    t = torch.randint(0, V, (4, 3), generator=gen_of(3), device="cuda")
+    for k in range(1, 4):
+        x.scatter_(-1, ((t + 7 * k) % V)[..., None], offset - 8.0)
+    x.scatter_(-1, t[..., None], offset)
+    r = d.token_logprobs(x, t, entropy=True)
+    a = torch.full((4, 3), -0.75, device="cuda")
+    lp = log_softmax_ref(x)[0].gather(-1, t[..., None])[..., 0]
+    want = a.double() * -torch.expm1(lp)
+    got = d.token_logprobs_grad(x, t, r.lse, a).gather(-1, t[..., None])[..., 0]
+    # near zero: lse, x - lse and 2^t, 2^-22 each at most; far: a sum of a few terms, its logarithm, a product
+    check(got, want, want.abs() * HALF[BF] * 1.01 + a.abs().double() * (2.0 ** -22 + 16 * U))
+
+
 def test_logprobs_grad_layouts():
     g = gen_of(8)
     for dtype, V in ((BF, 1000), (F32, 1001), (BF, 9001)):
