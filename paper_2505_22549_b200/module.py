@@ -69,10 +69,10 @@ def _on(device, what, *tensors):
 
 
 class BoundGrads:
-    """Gradient tensors already checked and marshalled (see DesLoc.bind_grads)."""
+    """Gradient tensors already checked and marshalled (see DesLoc.bind_grads): `fits` says for what (workers, sizes, type)."""
 
-    def __init__(self, array, keep):
-        self.array, self._keep = array, keep
+    def __init__(self, array, keep, fits=None):
+        self.array, self._keep, self.fits = array, keep, fits
         self.address = ctypes.addressof(array)
         self._device = None
 
@@ -123,24 +123,36 @@ class DesLoc:
         # one buffer of pointers per kind of argument, written anew at every call
         self._table = _native.Table(self.numel, self.M)
         self._table2 = _native.Table(self.numel, self.M)
+        self._fits = (self.M, tuple(self.numel), self.grad_dtype)
 
     def bind_grads(self, grads: Sequence[Sequence[torch.Tensor]]):
         """Check a set of gradient tensors once and return a handle every step method accepts in
         place of the nested lists: a loop that reuses its gradient buffers then pays no
-        per-step marshalling.  The handle keeps the tensors alive."""
+        per-step marshalling.  The handle keeps the tensors alive, and is refused where other workers, sizes or another
+        type are wanted than it was checked for."""
         if isinstance(grads, BoundGrads):
+            self._handle(grads)
             return grads
         n = self.M * len(self.numel)
+        grads = [tuple(row) for row in grads]
         # (a table of its own: another thread may be inside a step, which reads the buffer of self._table with
         # the interpreter's lock released)
         table = _native.Table(self.numel, self.M)
         address = self._fill(table, grads, self.grad_dtype, 0, _GRAD_MISFIT)
-        return BoundGrads((ctypes.c_void_p * n).from_buffer_copy((ctypes.c_void_p * n).from_address(address)), grads)
+        return BoundGrads((ctypes.c_void_p * n).from_buffer_copy((ctypes.c_void_p * n).from_address(address)), grads, self._fits)
+
+    def _handle(self, grads) -> int:
+        """Address of a handle's array, if it was made for the workers, sizes and type that these are."""
+        if grads.fits is not self._fits:
+            if grads.fits != self._fits:
+                raise ValueError(_GRAD_MISFIT)
+            grads.fits = self._fits     # (the next look is a short one)
+        return grads.address
 
     def _grad_address(self, grads) -> int:
         """Address of the array of gradient pointers, good until the next call of this method."""
         if isinstance(grads, BoundGrads):
-            return grads.address
+            return self._handle(grads)
         return self._fill(self._table, grads, self.grad_dtype, 0, _GRAD_MISFIT)
 
     def _fill(self, table, nested, kind: int, where: int, misfit: str) -> int:
@@ -285,10 +297,11 @@ class DesLoc:
                             work.data_ptr(), work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
 
     def _bound(self, grads) -> int:
-        """Address of a handle's array, if it was made for as many workers as there are now, of tensors on this device."""
-        if len(grads.array) != self.M * len(self.numel) or grads.device() != self._index:
+        """The same, if its tensors are on this device."""
+        address = self._handle(grads)
+        if grads.device() != self._index:
             raise ValueError(_GRAD_MISFIT)
-        return grads.address
+        return address
 
     def _list_of(self, table, grads):
         """(address, type code) of a set of gradient tensors of one type, on this context's device."""

@@ -130,3 +130,53 @@ def test_written_rows_that_overlap_are_refused(outer, inner, strides, overlap):
 def test_the_device_of_bound_gradients():
     rows = [[torch.zeros(3), torch.zeros(2)] for _ in range(2)]
     assert module.BoundGrads((ctypes.c_void_p * 4)(), rows).device() == -1
+
+
+def _engine(M, numel, grad_dtype, index=0):
+    eng = d.DesLoc.__new__(d.DesLoc)                       # no context: marshalling only
+    eng.ctx, eng.M, eng.numel, eng.grad_dtype, eng._index = None, M, numel, grad_dtype, index
+    eng._tables()
+    return eng
+
+
+@pytest.mark.parametrize("M, numel, kind", [(2, [4, 6], d.DESLOC_BF16), (2, [4, 5], d.DESLOC_F32), (2, [6, 4], d.DESLOC_F32), (1, [4, 6, 4, 6], d.DESLOC_F32),
+                                            (4, [10], d.DESLOC_F32), (1, [4, 6], d.DESLOC_F32), (3, [4, 6], d.DESLOC_F32)])
+def test_gradients_bound_for_other_tensors_are_refused(M, numel, kind):
+    """A handle stands for what it was checked as: workers, sizes and type."""
+    eng, other = _engine(2, [4, 6], d.DESLOC_F32), _engine(M, numel, kind)
+    dtype = torch.bfloat16 if kind == d.DESLOC_BF16 else torch.float32
+    bound = other.bind_grads([[torch.zeros(n, dtype=dtype) for n in numel] for _ in range(M)])
+    bound._device = eng._index                             # (as if it lay on the device)
+    assert other._bound(bound) == other._grad_address(bound) == bound.address
+    for call in (eng._bound, eng._grad_address, lambda b: eng._list_of(eng._table, b), eng.bind_grads):
+        with pytest.raises(ValueError, match="gradient tensor"):
+            call(bound)
+
+
+def test_gradients_bound_for_equal_tensors_are_taken():
+    eng, other = _engine(2, [4, 6], d.DESLOC_F32), _engine(2, [4, 6], d.DESLOC_F32)
+    bound = other.bind_grads([[torch.zeros(4), torch.zeros(6)] for _ in range(2)])
+    bound._device = eng._index
+    assert eng._bound(bound) == eng._grad_address(bound) == bound.address and eng.bind_grads(bound) is bound
+    eng.M = 3                                              # other workers from here on
+    eng._tables()
+    with pytest.raises(ValueError, match="gradient tensor"):
+        eng._grad_address(bound)
+
+
+def test_a_handle_keeps_the_tensors_that_it_was_made_from():
+    """Whatever becomes of the lists: a generator is used up, a list may hold another tensor later."""
+    import gc
+    import weakref
+    eng = _engine(2, [4, 6], d.DESLOC_F32)
+    lists = [[torch.zeros(4), torch.zeros(6)] for _ in range(2)]
+    seen = [weakref.ref(t) for row in lists for t in row]
+    for given in (lists, (row for row in [list(row) for row in lists])):
+        bound = eng.bind_grads(given)
+    assert [t.data_ptr() for row in bound._keep for t in row] == list(bound.array) == [r().data_ptr() for r in seen]
+    lists[0][1] = torch.zeros(6)
+    del lists[1], given
+    gc.collect()
+    assert all(r() is not None for r in seen)
+    eng.bind_grads([[torch.zeros(4), torch.zeros(6)] for _ in range(2)])
+    assert [t.data_ptr() for row in bound._keep for t in row] == list(bound.array)
