@@ -416,8 +416,8 @@ DESLOC_API int64_t desloc_embed_grad_bytes(const desloc_ctx *ctx, int32_t tensor
  * desloc_step_normclip() does on the way into its step, for gradients that go elsewhere (desloc_step_host(), desloc_step_masked(),
  * desloc_step_static(), a captured window, a log), or that were accumulated in fp32 and are handed to the step as bf16.
  *   grads, grads_dtype : host array of M*num_tensors DEVICE pointers, fp32 or bf16.
- *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.  DESLOC_E_INVALID where a worker and the next
- *                        have the same address for a tensor.
+ *   out, out_dtype     : the same of what is written; out[i] may be grads[i] where the types are equal.  DESLOC_E_INVALID where a tensor of `out` shares
+ *                        bytes with another of `out` or with any other of `grads` (tensors of `grads` may be the same ones, where `out` lies elsewhere).
  *   norms, factors     : device, [M] floats each, or NULL.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_clip_grads_bytes() bytes at least.
  * max_norm must be > 0 and finite.  Squares are fp32 (values below 1e-22 count as 0).  A norm that is not finite says that the gradients are not, or that sums of

@@ -52,6 +52,13 @@ DESLOC_API int32_t desloc_testing_kernel_of(const desloc_config *cfg, uint32_t m
 /* Groups of pieces that desloc_step_host() has had brought by a kernel, not by copies, in this context so far. */
 DESLOC_API int64_t desloc_testing_gathers(const desloc_ctx *ctx);
 
+/*
+ * Whether desloc_clip_grads() refuses these lists: 1 where a tensor of `out` shares bytes with another one of `out`, or with one of `grads` but for
+ * itself at its own place and in the same type; else 0.  Host-only, addresses alone.  Negative desloc_status on bad input.
+ */
+DESLOC_API int32_t desloc_testing_clip_shares(const int64_t *numel, int32_t num_tensors, int32_t M, int32_t grads_dtype, const void *const *grads,
+                                              int32_t out_dtype, void *const *out);
+
 #ifdef __cplusplus
 }
 #endif

@@ -120,6 +120,8 @@ _lib.desloc_testing_set_max_blocks.restype = ctypes.c_int
 _lib.desloc_testing_set_max_blocks.argtypes = [_P, ctypes.c_int64]
 _lib.desloc_testing_set_staging.restype = ctypes.c_int
 _lib.desloc_testing_set_staging.argtypes = [_P, ctypes.c_int32]
+_lib.desloc_testing_clip_shares.restype = ctypes.c_int32
+_lib.desloc_testing_clip_shares.argtypes = [ctypes.POINTER(ctypes.c_int64), ctypes.c_int32, ctypes.c_int32, ctypes.c_int32, _PP, ctypes.c_int32, _PP]
 _lib.desloc_testing_kernel_of.restype = ctypes.c_int32
 _lib.desloc_testing_kernel_of.argtypes = [ctypes.POINTER(DeslocConfig), ctypes.c_uint32, ctypes.c_int64, ctypes.c_int32, ctypes.c_int32,
                                            ctypes.POINTER(ctypes.c_int64)]
@@ -419,6 +421,15 @@ def desloc_testing_set_staging(ctx: int, mode: int) -> None:
     rc = _lib.desloc_testing_set_staging(ctx, int(mode))
     if rc != DESLOC_OK:
         raise DeslocError(rc, "desloc_testing_set_staging")
+
+
+def desloc_testing_clip_shares(numel: Sequence[int], M: int, grads_dtype: int, grads, out_dtype: int, out) -> bool:
+    """Whether desloc_clip_grads() refuses these lists of addresses because of what they share."""
+    r = int(_lib.desloc_testing_clip_shares((ctypes.c_int64 * len(numel))(*numel), len(numel), int(M), int(grads_dtype), _ptr_array(grads), int(out_dtype),
+                                            _ptr_array(out)))
+    if r < 0:
+        raise DeslocError(r, "desloc_testing_clip_shares")
+    return bool(r)
 
 
 def desloc_testing_kernel_of(cfg: DeslocConfig, mask: int, nchunks: int = 0, layout: int = 0, diag: bool = False):

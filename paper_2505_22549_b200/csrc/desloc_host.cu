@@ -609,6 +609,42 @@ bool share_memory(void *const *at, int count, int64_t bytes) {
     return false;
 }
 
+// Whether a list of tensors that is written shares bytes with itself or with a list that is read, but for a tensor that is read and written at its own
+// place.  Sorted by address first, unless they lie so already.  Host vectors: throws std::bad_alloc.
+bool share_memory(const int64_t *numel, int num_tensors, int M, const void *const *from, uintptr_t from_size, void *const *to, uintptr_t to_size) {
+    struct Span {
+        uintptr_t lo, hi;
+        int64_t index;
+    };
+    const int64_t n = static_cast<int64_t>(M) * num_tensors;
+    const auto span = [&](const void *p, int64_t i, uintptr_t size) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        return Span{at, at + static_cast<uintptr_t>(numel[i % num_tensors]) * size, i};
+    };
+    const auto before = [](const Span &a, const Span &b) { return a.lo < b.lo; };
+    std::vector<Span> spans(static_cast<size_t>(n));
+    uintptr_t from_lo = UINTPTR_MAX, from_hi = 0;
+    bool in_place = from_size == to_size;
+    for (int64_t i = 0; i < n; ++i) {
+        spans[i] = span(to[i], i, to_size);
+        const Span r = span(from[i], i, from_size);
+        from_lo = std::min(from_lo, r.lo), from_hi = std::max(from_hi, r.hi);
+        in_place = in_place && from[i] == to[i];
+    }
+    if (!std::is_sorted(spans.begin(), spans.end(), before)) std::sort(spans.begin(), spans.end(), before);
+    for (int64_t i = 1; i < n; ++i)
+        if (spans[i].lo < spans[i - 1].hi) return true;
+    if (in_place || n == 0 || from_hi <= spans.front().lo || spans.back().hi <= from_lo) return false;
+    for (int64_t i = 0; i < n; ++i) {
+        const Span r = span(from[i], i, from_size);
+        // (their ends rise as their beginnings do)
+        auto w = std::upper_bound(spans.begin(), spans.end(), r.lo, [](uintptr_t lo, const Span &s) { return lo < s.hi; });
+        for (; w != spans.end() && w->lo < r.hi; ++w)
+            if (w->index != i || w->lo != r.lo || from_size != to_size) return true;
+    }
+    return false;
+}
+
 int check_embedding(const desloc_ctx *ctx, int32_t tensor, int64_t width, const desloc_rows &tokens, int64_t n, float scale,
                     const desloc_rows &rows) {
     if (!desloc::is_token_rows(tokens) || !desloc::is_value_rows(rows)) return DESLOC_E_INVALID;
@@ -968,8 +1004,11 @@ int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, cons
     for (int64_t i = 0; i < ctx->nptr; ++i) {
         if (!grads[i] || !out[i]) return DESLOC_E_NULL;
         if (reinterpret_cast<uintptr_t>(grads[i]) % gsz || reinterpret_cast<uintptr_t>(out[i]) % osz) return DESLOC_E_INVALID;
-        if (grads[i] == out[i] && gsz != osz) return DESLOC_E_INVALID;
-        if (i >= c.num_tensors && out[i] == out[i - c.num_tensors]) return DESLOC_E_INVALID;   // one list for several workers: scaled more than once
+    }
+    try {
+        if (share_memory(ctx->numel.data(), c.num_tensors, c.M, grads, gsz, out, osz)) return DESLOC_E_INVALID;
+    } catch (const std::bad_alloc &) {
+        return DESLOC_E_NOMEM;
     }
     desloc::ClipWork w;
     if (desloc::clip_work(c.M, c.num_tensors, ctx->nrchunks, &w, static_cast<char *>(work)) > work_bytes) return DESLOC_E_RANGE;
@@ -1087,6 +1126,17 @@ int desloc_testing_set_wait_limit(desloc_ctx *ctx, int32_t polls) {
     ctx->wait_limit = polls < 0 ? desloc::DEFAULT_WAIT_LIMIT : polls;
     if (polls < 0) *static_cast<volatile int *>(ctx->h_err) = 0;
     return DESLOC_OK;
+}
+
+int32_t desloc_testing_clip_shares(const int64_t *numel, int32_t num_tensors, int32_t M, int32_t grads_dtype, const void *const *grads, int32_t out_dtype,
+                                   void *const *out) {
+    if (!numel || !grads || !out) return DESLOC_E_NULL;
+    if (num_tensors < 1 || M < 1 || M > DESLOC_MAX_M) return DESLOC_E_RANGE;
+    try {
+        return share_memory(numel, num_tensors, M, grads, grads_dtype == DESLOC_BF16 ? 2 : 4, out, out_dtype == DESLOC_BF16 ? 2 : 4) ? 1 : 0;
+    } catch (const std::bad_alloc &) {
+        return DESLOC_E_NOMEM;
+    }
 }
 
 int32_t desloc_testing_kernel_of(const desloc_config *cfg, uint32_t mask, int64_t nchunks, int32_t layout, int32_t diag, int64_t *blocks) {

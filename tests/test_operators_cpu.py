@@ -180,3 +180,62 @@ def test_a_handle_keeps_the_tensors_that_it_was_made_from():
     assert all(r() is not None for r in seen)
     eng.bind_grads([[torch.zeros(4), torch.zeros(6)] for _ in range(2)])
     assert [t.data_ptr() for row in bound._keep for t in row] == list(bound.array)
+
+
+def _shares(numel, grads_size, grads, out_size, out):
+    """Byte for byte."""
+    nt, spans = len(numel), []
+    for i, (a, b) in enumerate(zip(grads, out)):
+        spans.append((set(range(a, a + grads_size * numel[i % nt])), set(range(b, b + out_size * numel[i % nt]))))
+    for i, (_, w) in enumerate(spans):
+        for j, (r, v) in enumerate(spans):
+            if i != j and w & (r | v):
+                return True
+        if w & spans[i][0] and (grads[i] != out[i] or grads_size != out_size):
+            return True
+    return False
+
+
+@pytest.mark.parametrize("M, numel, grads, out, types, shares", [
+    (3, [4], [100, 200, 300], [100, 200, 300], (0, 0), False),              # in place
+    (3, [4], [100, 200, 100], [100, 200, 100], (0, 0), True),               # the first and the third worker the same
+    (3, [4], [100, 100, 100], [200, 300, 400], (0, 0), False),              # read by all of them
+    (3, [4], [100, 200, 300], [400, 500, 400], (0, 0), True),
+    (2, [4, 4], [100, 100, 200, 216], [100, 100, 200, 216], (0, 0), True),  # a tensor listed twice
+    (2, [4, 4], [100, 116, 200, 216], [116, 100, 200, 216], (0, 0), True),  # two tensors for one another
+    (2, [4, 4], [100, 116, 200, 216], [300, 316, 400, 412], (0, 0), True),  # four bytes of each
+    (2, [4, 4], [100, 116, 200, 216], [300, 316, 400, 416], (0, 0), False),
+    (2, [4], [100, 200], [100, 200], (0, 1), True),                         # in place, another type
+    (2, [4], [100, 200], [116, 216], (0, 1), False),
+    (2, [4], [100, 200], [112, 216], (0, 1), True),
+    (2, [4], [100, 200], [200, 100], (0, 0), True),                         # the workers' for one another
+    (2, [4], [100, 200], [300, 200], (0, 0), False),                        # one of them in place
+    (2, [8], [100, 200], [104, 300], (0, 0), True),                         # its own, shifted
+    (2, [8], [100, 200], [92, 300], (0, 0), True),
+])
+def test_lists_that_share_memory(M, numel, grads, out, types, shares):
+    size = [2 if t == d.DESLOC_BF16 else 4 for t in types]
+    assert _shares(numel, size[0], grads, size[1], out) == shares
+    assert B.desloc_testing_clip_shares(numel, M, types[0], grads, types[1], out) == shares
+
+
+def test_lists_that_share_memory_or_nearly_do():
+    import random
+    rng, seen = random.Random(5), [0, 0]
+    for _ in range(4000):
+        M, numel, types = rng.randint(1, 4), [rng.randint(1, 6) for _ in range(rng.randint(1, 4))], (rng.randint(0, 1), rng.randint(0, 1))
+        size = [2 if t == d.DESLOC_BF16 else 4 for t in types]
+        n, room = M * len(numel), rng.choice([200, 1000, 4000])
+        lists = []
+        for k in range(2):
+            at, flat = 4096 + 4 * rng.randint(0, room // 4), []
+            for i in range(n):
+                flat.append(at if rng.random() < 0.7 else 4096 + 4 * rng.randint(0, room // 4))
+                at = flat[-1] + size[k] * numel[i % len(numel)] + 2 * rng.randint(0, 3)
+            lists.append(flat)
+        if rng.random() < 0.4:
+            lists[1] = [a if rng.random() < 0.9 else b for a, b in zip(*lists)]
+        want = _shares(numel, size[0], lists[0], size[1], lists[1])
+        seen[want] += 1
+        assert B.desloc_testing_clip_shares(numel, M, types[0], lists[0], types[1], lists[1]) == want
+    assert min(seen) > 300

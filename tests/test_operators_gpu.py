@@ -954,3 +954,30 @@ def test_bound_gradients_of_other_workers_or_from_the_host_are_refused():
         for call in (lambda: two.embed_grad(0, tokens, dout, bound), lambda: two.clip_grads(bound, 1.0)):
             with pytest.raises(ValueError, match="gradient tensor"):
                 call()
+
+
+def test_clipping_refuses_lists_that_share_memory():
+    M, numel = 3, [40, 13]
+    opt, _ = context(M, [(n,) for n in numel])
+    new = lambda dtype=BF: [[torch.ones(n, dtype=dtype, device="cuda") for n in numel] for _ in range(M)]
+
+    def invalid(call):
+        with pytest.raises(d.DeslocError) as e:
+            call()
+        assert e.value.status == d.DESLOC_E_INVALID
+
+    g, to = new(), new()
+    for lists in ([g[0], g[1], g[0]], [g[0], g[1], [g[0][0], g[2][1]]], [[g[0][0], g[0][0][:13]], g[1], g[2]]):
+        invalid(lambda: opt.clip_grads(lists, 1.0))
+        invalid(lambda: opt.clip_grads(new(F32), 1.0, out=lists))
+    invalid(lambda: opt.clip_grads(g, 1.0, out=[g[1], g[0], g[2]]))
+    buf = torch.ones(41, dtype=BF, device="cuda")
+    invalid(lambda: opt.clip_grads([[buf[:40], g[0][1]], g[1], g[2]], 1.0, out=[[buf[1:], to[0][1]], to[1], to[2]]))
+    assert all(bool((t == 1).all()) for row in g + to for t in row)      # nothing ran
+    opt.clip_grads([g[0], g[1], g[0]], 1.0, out=to)                       # read by two of them
+    assert torch.equal(to[0][0], to[2][0])
+    mixed = [to[0], g[1], to[2]]                                          # one worker in place
+    opt.clip_grads(g, 1.0, out=mixed)
+    for m in range(M):
+        for k in range(2):
+            check(mixed[m][k], torch.full((numel[k],), 1 / math.sqrt(53), dtype=torch.float64, device="cuda"), HALF[BF] * 1.01 / math.sqrt(53))
