@@ -610,38 +610,51 @@ bool share_memory(void *const *at, int count, int64_t bytes) {
 }
 
 // Whether a list of tensors that is written shares bytes with itself or with a list that is read, but for a tensor that is read and written at its own
-// place.  Sorted by address first, unless they lie so already.  Host vectors: throws std::bad_alloc.
+// place.  One look where addresses rise, as those of packed tensors do, and the lists lie apart; else by sorted addresses.  Host vectors: throws std::bad_alloc.
 bool share_memory(const int64_t *numel, int num_tensors, int M, const void *const *from, uintptr_t from_size, void *const *to, uintptr_t to_size) {
     struct Span {
         uintptr_t lo, hi;
         int64_t index;
     };
-    const int64_t n = static_cast<int64_t>(M) * num_tensors;
-    const auto span = [&](const void *p, int64_t i, uintptr_t size) {
-        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
-        return Span{at, at + static_cast<uintptr_t>(numel[i % num_tensors]) * size, i};
-    };
-    const auto before = [](const Span &a, const Span &b) { return a.lo < b.lo; };
-    std::vector<Span> spans(static_cast<size_t>(n));
-    uintptr_t from_lo = UINTPTR_MAX, from_hi = 0;
-    bool in_place = from_size == to_size;
-    for (int64_t i = 0; i < n; ++i) {
-        spans[i] = span(to[i], i, to_size);
-        const Span r = span(from[i], i, from_size);
-        from_lo = std::min(from_lo, r.lo), from_hi = std::max(from_hi, r.hi);
-        in_place = in_place && from[i] == to[i];
+    uintptr_t from_lo = UINTPTR_MAX, from_hi = 0, to_lo = UINTPTR_MAX, to_hi = 0;
+    bool in_place = from_size == to_size, rising = true;
+    int64_t i = 0;
+    for (int m = 0; m < M; ++m)
+        for (int k = 0; k < num_tensors; ++k, ++i) {
+            const uintptr_t r = reinterpret_cast<uintptr_t>(from[i]), w = reinterpret_cast<uintptr_t>(to[i]), n = static_cast<uintptr_t>(numel[k]);
+            rising = rising && w >= to_hi;
+            from_lo = std::min(from_lo, r), from_hi = std::max(from_hi, r + n * from_size);
+            to_lo = std::min(to_lo, w), to_hi = std::max(to_hi, w + n * to_size);
+            in_place = in_place && r == w;
+        }
+    const bool apart = in_place || from_hi <= to_lo || to_hi <= from_lo;
+    if (rising && apart) return false;
+    std::vector<Span> spans;
+    spans.reserve(static_cast<size_t>(i));
+    for (int m = 0; m < M; ++m)
+        for (int k = 0; k < num_tensors; ++k) {
+            const uintptr_t w = reinterpret_cast<uintptr_t>(to[spans.size()]);
+            spans.push_back({w, w + static_cast<uintptr_t>(numel[k]) * to_size, static_cast<int64_t>(spans.size())});
+        }
+    if (!rising) {
+        std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.lo < b.lo; });
+        for (size_t at = 1; at < spans.size(); ++at)
+            if (spans[at].lo < spans[at - 1].hi) return true;
     }
-    if (!std::is_sorted(spans.begin(), spans.end(), before)) std::sort(spans.begin(), spans.end(), before);
-    for (int64_t i = 1; i < n; ++i)
-        if (spans[i].lo < spans[i - 1].hi) return true;
-    if (in_place || n == 0 || from_hi <= spans.front().lo || spans.back().hi <= from_lo) return false;
-    for (int64_t i = 0; i < n; ++i) {
-        const Span r = span(from[i], i, from_size);
-        // (their ends rise as their beginnings do)
-        auto w = std::upper_bound(spans.begin(), spans.end(), r.lo, [](uintptr_t lo, const Span &s) { return lo < s.hi; });
-        for (; w != spans.end() && w->lo < r.hi; ++w)
-            if (w->index != i || w->lo != r.lo || from_size != to_size) return true;
-    }
+    if (apart) return false;
+    // The first span that ends behind `lo`, if `at` is it.  (Their ends rise as their beginnings do.)
+    const auto is_first = [&](size_t at, uintptr_t lo) { return (at == 0 || spans[at - 1].hi <= lo) && (at == spans.size() || spans[at].hi > lo); };
+    size_t first = 0;
+    i = 0;
+    for (int m = 0; m < M; ++m)
+        for (int k = 0; k < num_tensors; ++k, ++i) {
+            const uintptr_t lo = reinterpret_cast<uintptr_t>(from[i]), hi = lo + static_cast<uintptr_t>(numel[k]) * from_size;
+            if (!is_first(first, lo)) first = std::min(first + 1, spans.size());     // (lists that lie alike: the next one)
+            if (!is_first(first, lo))
+                first = std::upper_bound(spans.begin(), spans.end(), lo, [](uintptr_t p, const Span &s) { return p < s.hi; }) - spans.begin();
+            for (size_t w = first; w < spans.size() && spans[w].lo < hi; ++w)
+                if (spans[w].index != i || spans[w].lo != lo || from_size != to_size) return true;
+        }
     return false;
 }
 
