@@ -393,6 +393,24 @@ PyObject *guarded(const F &body) {
     }
 }
 
+// Written behind torch's back: a tensor that autograd has saved is refused in backward() from here on, as after any operation in place.  (Tensors of
+// inference mode count no versions.)
+void wrote(const at::Tensor &t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// The same for a tensor or for those in nested lists and tuples.
+void wrote_all(PyObject *o) {
+    if (THPVariable_Check(o)) return wrote(THPVariable_Unpack(o));
+    if (!PyList_Check(o) && !PyTuple_Check(o)) return;
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(o); ++i) wrote_all(PySequence_Fast_GET_ITEM(o, i));
+}
+PyObject *call_wrote(PyObject *, PyObject *o) {
+    return guarded([&]() -> PyObject * {
+        wrote_all(o);
+        Py_RETURN_NONE;
+    });
+}
+
 // Tokens [workers, ...], dense.
 bool worker_tokens(const at::Tensor *t, int64_t workers, desloc_rows *rows, int64_t *n) {
     if (!t || t->dim() < 1 || t->size(0) != workers || token_type(t->scalar_type()) < 0 || !t->is_contiguous()) return false;
@@ -451,6 +469,7 @@ PyObject *call_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
             Py_RETURN_NONE;
         const desloc_rows rows{d->data_ptr(), value_type(d->scalar_type()), {n * width, width}};
         std::vector<void *> own;
+        std::vector<at::Tensor> written;
         void *const *grads = nullptr;
         if (PyLong_Check(args[6])) {
             grads = static_cast<void *const *>(PyLong_AsVoidPtr(args[6]));
@@ -463,6 +482,7 @@ PyObject *call_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                 const at::Tensor *g = tensor_on(PyList_GET_ITEM(row, tensor), device);
                 if (!g || value_type(g->scalar_type()) != type || g->numel() != numel || !g->is_contiguous()) Py_RETURN_NONE;
                 own[static_cast<size_t>(m * tensors + tensor)] = g->data_ptr();
+                written.push_back(*g);
             }
             grads = own.data();
         }
@@ -475,17 +495,19 @@ PyObject *call_embed_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
         rc = g_entry.embed_grad(static_cast<desloc_ctx *>(ctx), static_cast<int32_t>(tensor), width, &tokens, n, &rows, scale,
                                 static_cast<int32_t>(accumulate), grads, at_work, bytes, stream);
         Py_END_ALLOW_THREADS
+        if (rc == DESLOC_OK)
+            for (const at::Tensor &g : written) wrote(g);
         return PyLong_FromLong(rc);
     });
 }
 
-// (context, max_norm, type, pointers, type of out, pointers of out, workers, device) -> (norms, factors)
+// (context, max_norm, type, pointers, type of out, pointers of out, workers, device, tensors of out) -> (norms, factors)
 PyObject *call_clip_grads(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
     void *ctx = nullptr, *from = nullptr, *to = nullptr;
     int64_t type = 0, out_type = 0, workers = 0, device = 0;
     float max_norm = 0.f;
-    if (nargs != 8) {
-        PyErr_SetString(PyExc_TypeError, "clip_grads(ctx, max_norm, type, grads, out_type, out, workers, device)");
+    if (nargs != 9) {
+        PyErr_SetString(PyExc_TypeError, "clip_grads(ctx, max_norm, type, grads, out_type, out, workers, device, written)");
         return nullptr;
     }
     if (!as_pointer(args[0], &ctx) || !as_float(args[1], &max_norm) || !as_int64(args[2], &type) || !as_pointer(args[3], &from) ||
@@ -504,6 +526,7 @@ PyObject *call_clip_grads(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
                                 static_cast<int32_t>(out_type), static_cast<void *const *>(to), at_norms, at_factors, at_work, bytes, stream);
         Py_END_ALLOW_THREADS
         if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        wrote_all(args[8]);
         PyObject *n = THPVariable_Wrap(norms), *f = n ? THPVariable_Wrap(factors) : nullptr, *both = f ? PyTuple_Pack(2, n, f) : nullptr;
         Py_XDECREF(n);
         Py_XDECREF(f);
@@ -623,6 +646,7 @@ PyObject *call_logprobs_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs
         rc = g_entry.token_logprobs_grad(lead.n[0], lead.n[1], vocab, &logits, &tokens, dense[0], dense[1], dense[2], dense[3], &to,
                                          static_cast<int>(device), stream);
         Py_END_ALLOW_THREADS
+        if (rc == DESLOC_OK && args[6] != Py_None) wrote(out);
         return rc == DESLOC_OK ? THPVariable_Wrap(out) : PyLong_FromLong(rc);
     });
 }
@@ -661,6 +685,7 @@ PyMethodDef methods[] = {{"bind", bind_entries, METH_VARARGS, nullptr},
                          {"step_host", fast(call_step_host), METH_FASTCALL, nullptr},
                          {"diag_norms", fast(call_diag_norms), METH_FASTCALL, nullptr},
                          {"rel_change", fast(call_rel_change), METH_FASTCALL, nullptr},
+                         {"wrote", call_wrote, METH_O, nullptr},
                          {"embed", fast(call_embed), METH_FASTCALL, nullptr},
                          {"embed_grad", fast(call_embed_grad), METH_FASTCALL, nullptr},
                          {"clip_grads", fast(call_clip_grads), METH_FASTCALL, nullptr},

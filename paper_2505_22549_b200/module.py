@@ -261,6 +261,7 @@ class DesLoc:
         stride = to[2][0] if to[0] == self.M else (to[2][0][1] * flat.shape[1], to[2][0][1])
         B.desloc_embed(self.ctx, tensor, width, rows, flat.shape[1], scale, B.rows(out.data_ptr(), _TYPES[out.dtype], *stride),
                        torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote(out)
         return out
 
     def embed_grad(self, tensor: int, tokens: torch.Tensor, dout: torch.Tensor, grads, scale: float = 1.0, accumulate: bool = False,
@@ -271,7 +272,11 @@ class DesLoc:
         r = _native.embed_grad(self.ctx, tensor, width, self.M, tokens, dout, self._bound(grads) if isinstance(grads, BoundGrads) else grads, len(self.numel),
                                self.numel[tensor], self.grad_dtype, scale, accumulate, self._index)
         if r is not None:
-            return None if r == 0 else self._raise(r, "desloc_embed_grad")
+            if r != 0:
+                self._raise(r, "desloc_embed_grad")
+            if isinstance(grads, BoundGrads):   # (lists: done natively)
+                _native.wrote([row[tensor] for row in grads._keep])
+            return None
         rows, flat = self._tokens(tokens)
         if tuple(dout.shape) != tuple(tokens.shape) + (width,) or dout.dtype not in _TYPES:
             raise ValueError("dout does not fit the tokens")
@@ -295,6 +300,7 @@ class DesLoc:
         work = torch.empty(B.desloc_embed_grad_bytes(self.ctx, tensor, width, n), dtype=torch.uint8, device=self.device)
         B.desloc_embed_grad(self.ctx, tensor, width, rows, n, B.rows(d.data_ptr(), _TYPES[d.dtype], *d.stride()[:2]), scale, accumulate, array,
                             work.data_ptr(), work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote([row[tensor] for row in (grads._keep if isinstance(grads, BoundGrads) else grads)])
 
     def _bound(self, grads) -> int:
         """The same, if its tensors are on this device."""
@@ -317,7 +323,9 @@ class DesLoc:
         whole tensor list), into `out` (the same, either type) or in place.  Returns (norms, factors), [M] fp32 on the device; nothing waits."""
         address, kind = self._list_of(self._table, grads)
         to, to_kind = (address, kind) if out is None else self._list_of(self._table2, out)
-        r = _native.clip_grads(self.ctx, max_norm, kind, address, to_kind, to, self.M, self._index)
+        written = grads if out is None else out
+        r = _native.clip_grads(self.ctx, max_norm, kind, address, to_kind, to, self.M, self._index,
+                               written._keep if isinstance(written, BoundGrads) else written)
         return r if type(r) is not int else self._raise(r, "desloc_clip_grads")
 
     def set_workers(self, x, u, v, first_new: int) -> None:
@@ -402,7 +410,8 @@ def _refuse(status: int, where: str):
 
 def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, entropy: bool = False, top: int = 0) -> TokenLogprobs:
     """Log probabilities of `tokens` [...] under `logits` [..., vocabulary] (fp32 or bf16), on torch's current stream: logp (0 for tokens outside the
-    vocabulary), lse, and on request the entropy and the `top` likeliest tokens.  exp(-logp.mean(...)) is the perplexity."""
+    vocabulary), lse, and on request the entropy and the `top` likeliest tokens.  exp(-logp.mean(...)) is the perplexity.  torch records nothing: the
+    results require no gradient even where the logits do; token_logprobs_grad() is what goes back."""
     r = _native.token_logprobs(logits, tokens, entropy, top)     # the usual layouts, natively
     if r is not None:
         return TokenLogprobs(*r) if type(r) is not int else _refuse(r, "desloc_token_logprobs")
@@ -421,7 +430,7 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, entropy: bool = F
 def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.Tensor, dlogp: torch.Tensor, entropy: Optional[torch.Tensor] = None,
                         dentropy: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gradient of sum(dlogp * logp) + sum(dentropy * entropy) with respect to the logits, in their type; lse and entropy are what
-    token_logprobs() gave.  out may be the logits themselves."""
+    token_logprobs() gave.  out may be the logits themselves; it counts as changed in place for torch."""
     r = _native.token_logprobs_grad(logits, tokens, lse, dlogp, entropy, dentropy, out)
     if r is not None:
         return r if type(r) is not int else _refuse(r, "desloc_token_logprobs_grad")
@@ -442,4 +451,5 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, lse: torch.T
                                  B.rows(tokens.data_ptr(), _TOKEN_TYPES[tokens.dtype], *strides[1]), *map(at, dense),
                                  B.rows(out.data_ptr(), _TYPES[out.dtype], *strides[2]), logits.device.index,
                                  torch.cuda.current_stream(logits.device).cuda_stream)
+    _native.wrote(out)
     return out

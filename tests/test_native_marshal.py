@@ -94,3 +94,14 @@ def test_a_module_built_for_another_torch_is_refused():
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True,
                        cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
     assert r.returncode != 0 and "was built for torch" in r.stderr and "paper_2505_22549_b200.build" in r.stderr
+
+
+def test_written_tensors_count_as_changed(native):
+    a, b, c = torch.zeros(4), torch.zeros(3), torch.zeros(2)
+    native.wrote([[a, b[1:]], (c, None, 5), "text"])
+    native.wrote(a)
+    native.wrote(None)
+    assert (a._version, b._version, c._version) == (2, 1, 1)
+    with torch.inference_mode():
+        made_there = torch.zeros(2)
+    native.wrote([made_there])               # (has no versions)

@@ -981,3 +981,54 @@ def test_clipping_refuses_lists_that_share_memory():
     for m in range(M):
         for k in range(2):
             check(mixed[m][k], torch.full((numel[k],), 1 / math.sqrt(53), dtype=torch.float64, device="cuda"), HALF[BF] * 1.01 / math.sqrt(53))
+
+
+def test_what_is_written_counts_as_changed():
+    """torch's version counters rise for what a call writes, and for nothing else: a saved tensor that was overwritten is refused in backward()."""
+    M, V, D, n = 2, 50, 8, 6
+    opt, _ = context(M, [(V, D), (13,)], grad_dtype="f32")
+    tokens, dout = tokens_of(M, n, V, 1), torch.ones(M, n, D, device="cuda")
+    new = lambda: [[torch.zeros(V, D, device="cuda"), torch.zeros(13, device="cuda")] for _ in range(M)]
+    versions = lambda lists: [[t._version for t in row] for row in lists]
+    out = torch.zeros(M, n, D, device="cuda")
+    before = out._version, tokens._version
+    opt.embed(0, tokens, out=out)
+    assert out._version > before[0] and tokens._version == before[1]
+    for bind in (False, True):
+        grads, to = new(), new()
+        given, given_to = (opt.bind_grads(grads), opt.bind_grads(to)) if bind else (grads, to)
+        v = versions(grads)
+        opt.embed_grad(0, tokens, dout, given)
+        opt.embed_grad(0, tokens[:, ::2], dout[:, ::2], given, accumulate=True)
+        assert all(row[0]._version > w[0] and row[1]._version == w[1] for row, w in zip(grads, v))
+        v, w = versions(grads), versions(to)
+        opt.clip_grads(given, 1.0, out=given_to)
+        assert versions(grads) == v and all(a > b for x, y in zip(versions(to), w) for a, b in zip(x, y))
+        opt.clip_grads(given, 1.0)
+        assert all(a > b for x, y in zip(versions(grads), v) for a, b in zip(x, y))
+    z = torch.randn(M, n, V, generator=gen_of(2), device="cuda", requires_grad=True)
+    for view in (lambda x: x, lambda x: x[:, ::2], lambda x: x[:, None, None]):
+        logits = torch.tanh(z)
+        own, t = view(logits.detach()), view(tokens)
+        r = d.token_logprobs(own, t)
+        assert logits._version == 0
+        d.token_logprobs_grad(own, t, r.lse, torch.ones_like(r.lse), out=own)
+        assert logits._version == 1
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            logits.sum().backward()
+
+
+def test_outputs_made_in_inference_mode_are_taken():
+    M, V, D, n = 2, 50, 8, 6
+    opt, _ = context(M, [(V, D)], grad_dtype="f32")
+    tokens = tokens_of(M, n, V, 1)
+    with torch.inference_mode():
+        out, grads, x = torch.zeros(M, n, D, device="cuda"), [[torch.zeros(V, D, device="cuda")] for _ in range(M)], torch.zeros(M, n, V, device="cuda")
+    for mode in (False, True):
+        with torch.inference_mode(mode):
+            opt.embed(0, tokens, out=out)
+            opt.embed_grad(0, tokens, out, grads)
+            opt.clip_grads(grads, 1.0)
+            r = d.token_logprobs(x, tokens)
+            d.token_logprobs_grad(x, tokens, r.lse, torch.ones_like(r.lse), out=x)
+    torch.cuda.synchronize()
