@@ -415,6 +415,8 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, entropy: bool = F
     r = _native.token_logprobs(logits, tokens, entropy, top)     # the usual layouts, natively
     if r is not None:
         return TokenLogprobs(*r) if type(r) is not int else _refuse(r, "desloc_token_logprobs")
+    if not 0 <= top <= B.DESLOC_MAX_TOP:
+        _refuse(B.DESLOC_E_RANGE, "desloc_token_logprobs")
     logits, tokens, (outer, inner, strides) = _logit_rows(logits, tokens)
     lead, dev = logits.shape[:-1], logits.device
     new = lambda *shape, dtype=torch.float32: torch.empty(shape, dtype=dtype, device=dev)

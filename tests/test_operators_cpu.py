@@ -239,3 +239,12 @@ def test_lists_that_share_memory_or_nearly_do():
         seen[want] += 1
         assert B.desloc_testing_clip_shares(numel, M, types[0], lists[0], types[1], lists[1]) == want
     assert min(seen) > 300
+
+
+@pytest.mark.parametrize("top", [-1, -(1 << 40), d.DESLOC_MAX_TOP + 1, 1 << 40])
+def test_a_number_of_alternatives_out_of_range_is_the_librarys_refusal(top):
+    """Before anything is allocated for it."""
+    for shape in ((2, 3), (2, 2, 2, 2)):
+        with pytest.raises(d.DeslocError) as e:
+            d.token_logprobs(torch.zeros(*shape, 8), torch.zeros(shape, dtype=torch.int64), top=top)
+        assert e.value.status == d.DESLOC_E_RANGE
