@@ -797,6 +797,55 @@ def test_calls_run_on_the_current_stream():
         assert torch.equal(a, b)
 
 
+def test_calls_read_and_write_behind_what_is_on_their_stream():
+    """Inputs are overwritten and outputs spoiled on a side stream, behind work that takes longer than the host: each call has to see that."""
+    M, V, D, n = 2, 500, 32, 40
+    opt, _ = context(M, [(V, D)])
+    s, coming = _state(M, V, D, n), _state(M, V, D, n)
+    _refill(coming, 11)
+    want = [t.clone() for t in _all_calls(opt, coming)]
+    old = _all_calls(opt, s)
+    lse, H = old[2].clone(), old[3].clone()          # (the forward's, of the inputs that come)
+    lse.copy_(want[2]), H.copy_(want[3])
+    dl = d.token_logprobs_grad(coming["logits"], coming["tokens"], lse, coming["w"], H, coming["w"])
+    grads = [[torch.empty_like(g[0])] for g in coming["grads"]]
+    for g, c in zip(grads, coming["grads"]):
+        g[0].copy_(c[0])
+    big = torch.ones(1 << 26, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+
+    def late():
+        for _ in range(100):
+            big.mul_(1.0001)
+        for k in ("tokens", "logits", "w", "dout"):
+            s[k].copy_(coming[k])
+        s["emb"].fill_(3.0)
+        for k in ("grads", "clipped"):
+            for row in s[k]:
+                row[0].fill_(3.0)
+
+    for again in range(2):                           # (the first time memory is allocated)
+        _refill(s, 5)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            late()
+            emb = opt.embed(0, s["tokens"], out=s["emb"]).clone()
+            fresh = opt.embed(0, s["tokens"])
+            r = d.token_logprobs(s["logits"], s["tokens"], entropy=True, top=4)
+            grad = d.token_logprobs_grad(s["logits"], s["tokens"], lse, s["w"], H, s["w"])
+            opt.embed_grad(0, s["tokens"], s["dout"], s["grads"])
+            own = [row[0].clone() for row in s["grads"]]
+            for row, g in zip(s["grads"], grads):
+                row[0].copy_(g[0])
+            norms, factors = opt.clip_grads(s["grads"], 0.5, out=s["clipped"])
+            clipped = [row[0].clone() for row in s["clipped"]]
+            assert again == 0 or not side.query()        # (the work in front was still running when all of this was called)
+        side.synchronize()
+        for a, b in zip([emb, fresh, *r, grad, norms, factors, *own, *clipped], [want[0], want[0], *want[1:6], dl, *want[7:9], *want[9:9 + M], *want[9 + M:]]):
+            assert torch.equal(a, b)
+
+
 def test_two_streams_at_once():
     """Calls without common working memory do not disturb one another."""
     M, V, D, n = 2, 3000, 256, 2000
