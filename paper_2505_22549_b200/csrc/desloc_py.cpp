@@ -400,9 +400,10 @@ void wrote(const at::Tensor &t) {
 }
 // The same for a tensor or for those in nested lists and tuples.
 void wrote_all(PyObject *o) {
-    if (THPVariable_Check(o)) return wrote(THPVariable_Unpack(o));
-    if (!PyList_Check(o) && !PyTuple_Check(o)) return;
-    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(o); ++i) wrote_all(PySequence_Fast_GET_ITEM(o, i));
+    if (PyList_Check(o) || PyTuple_Check(o))   // (first: torch's check of what is no tensor is slow)
+        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(o); ++i) wrote_all(PySequence_Fast_GET_ITEM(o, i));
+    else if (THPVariable_Check(o))
+        wrote(THPVariable_Unpack(o));
 }
 PyObject *call_wrote(PyObject *, PyObject *o) {
     return guarded([&]() -> PyObject * {
