@@ -398,12 +398,15 @@ PyObject *guarded(const F &body) {
 void wrote(const at::Tensor &t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
-// The same for a tensor or for those in nested lists and tuples.
-void wrote_all(PyObject *o) {
-    if (PyList_Check(o) || PyTuple_Check(o))   // (first: torch's check of what is no tensor is slow)
-        for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(o); ++i) wrote_all(PySequence_Fast_GET_ITEM(o, i));
-    else if (THPVariable_Check(o))
-        wrote(THPVariable_Unpack(o));
+// The same for a tensor or for those in sequences of sequences, whatever kind of sequence fill() takes.
+void wrote_all(PyObject *o, int depth = 2) {
+    const bool list = PyList_Check(o) || PyTuple_Check(o);   // (first: torch's check of what is no tensor is slow)
+    if (!list && THPVariable_Check(o)) return wrote(THPVariable_Unpack(o));
+    if (depth == 0 || (!list && !PySequence_Check(o))) return;
+    PyObject *items = PySequence_Fast(o, "");
+    if (!items) return PyErr_Clear();
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(items); ++i) wrote_all(PySequence_Fast_GET_ITEM(items, i), depth - 1);
+    Py_DECREF(items);
 }
 PyObject *call_wrote(PyObject *, PyObject *o) {
     return guarded([&]() -> PyObject * {

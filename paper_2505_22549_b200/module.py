@@ -152,7 +152,7 @@ class DesLoc:
     def _grad_address(self, grads) -> int:
         """Address of the array of gradient pointers, good until the next call of this method."""
         if isinstance(grads, BoundGrads):
-            return self._handle(grads)
+            return grads.address if grads.fits is self._fits else self._handle(grads)
         return self._fill(self._table, grads, self.grad_dtype, 0, _GRAD_MISFIT)
 
     def _fill(self, table, nested, kind: int, where: int, misfit: str) -> int:

@@ -105,3 +105,8 @@ def test_written_tensors_count_as_changed(native):
     with torch.inference_mode():
         made_there = torch.zeros(2)
     native.wrote([made_there])               # (has no versions)
+    rows = [torch.nn.ParameterList([torch.zeros(2), torch.zeros(3)]) for _ in range(2)]      # (the table takes them, too)
+    assert native.Table([2, 3], 2).fill(rows, 0, 0, "misfit")
+    before = [t._version for row in rows for t in row]
+    native.wrote(rows)
+    assert [t._version for row in rows for t in row] == [v + 1 for v in before]
