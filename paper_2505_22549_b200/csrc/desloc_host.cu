@@ -1016,7 +1016,7 @@ int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, cons
     const uintptr_t gsz = grads_dtype == DESLOC_BF16 ? 2 : 4, osz = out_dtype == DESLOC_BF16 ? 2 : 4;
     for (int64_t i = 0; i < ctx->nptr; ++i) {
         if (!grads[i] || !out[i]) return DESLOC_E_NULL;
-        if (reinterpret_cast<uintptr_t>(grads[i]) % gsz || reinterpret_cast<uintptr_t>(out[i]) % osz) return DESLOC_E_INVALID;
+        if ((reinterpret_cast<uintptr_t>(grads[i]) & (gsz - 1)) || (reinterpret_cast<uintptr_t>(out[i]) & (osz - 1))) return DESLOC_E_INVALID;
     }
     try {
         if (share_memory(ctx->numel.data(), c.num_tensors, c.M, grads, gsz, out, osz)) return DESLOC_E_INVALID;

@@ -15,6 +15,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <cstring>
 #include <exception>
 #include <new>
 #include <vector>
@@ -398,15 +399,34 @@ PyObject *guarded(const F &body) {
 void wrote(const at::Tensor &t) {
     if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
 }
-// The same for a tensor or for those in sequences of sequences, whatever kind of sequence fill() takes.
-void wrote_all(PyObject *o, int depth = 2) {
+// Views of one tensor hold one counter: of some in a row the first one is enough.
+bool same_counter(const at::Tensor &a, const at::Tensor &b) {
+    const c10::VariableVersion &u = a.unsafeGetTensorImpl()->version_counter(), &v = b.unsafeGetTensorImpl()->version_counter();
+    const void *at[2];
+    static_assert(sizeof u == sizeof at[0]);   // (a reference to the counter)
+    std::memcpy(&at[0], &u, sizeof u);
+    std::memcpy(&at[1], &v, sizeof v);
+    return at[0] && at[0] == at[1];
+}
+// The same for a tensor or for those in sequences of sequences, whatever kind of sequence fill() takes.  `last`: the one before, which `o` keeps alive.
+void wrote_all(PyObject *o, const at::Tensor *&last, int depth) {
     const bool list = PyList_Check(o) || PyTuple_Check(o);   // (first: torch's check of what is no tensor is slow)
-    if (!list && THPVariable_Check(o)) return wrote(THPVariable_Unpack(o));
+    if (!list && THPVariable_Check(o)) {
+        const at::Tensor &t = THPVariable_Unpack(o);
+        if (!last || !same_counter(*last, t)) wrote(t);
+        last = &t;
+        return;
+    }
     if (depth == 0 || (!list && !PySequence_Check(o))) return;
     PyObject *items = PySequence_Fast(o, "");
     if (!items) return PyErr_Clear();
-    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(items); ++i) wrote_all(PySequence_Fast_GET_ITEM(items, i), depth - 1);
+    for (Py_ssize_t i = 0; i < PySequence_Fast_GET_SIZE(items); ++i) wrote_all(PySequence_Fast_GET_ITEM(items, i), last, depth - 1);
+    if (!list) last = nullptr;   // (its items may go with it)
     Py_DECREF(items);
+}
+void wrote_all(PyObject *o) {
+    const at::Tensor *last = nullptr;
+    wrote_all(o, last, 2);
 }
 PyObject *call_wrote(PyObject *, PyObject *o) {
     return guarded([&]() -> PyObject * {

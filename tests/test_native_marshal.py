@@ -110,3 +110,6 @@ def test_written_tensors_count_as_changed(native):
     before = [t._version for row in rows for t in row]
     native.wrote(rows)
     assert [t._version for row in rows for t in row] == [v + 1 for v in before]
+    buf, other = torch.zeros(12), torch.zeros(2)                # views of one tensor have one counter: risen is enough
+    native.wrote([[buf[:4], buf[4:6], other], [buf[6:]], [buf.data]])
+    assert buf._version > 0 and other._version == 1
