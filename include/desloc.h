@@ -384,7 +384,8 @@ typedef enum { DESLOC_I32 = 0, DESLOC_I64 = 1 } desloc_index_t;
 typedef struct {
     void *data;
     int32_t dtype;     /* desloc_dtype_t; desloc_index_t for tokens */
-    int64_t stride[2]; /* in elements; rows that are written may not overlap (DESLOC_E_INVALID) */
+    int64_t stride[2]; /* in elements; rows that are written may not overlap: one stride passes a row, the other all that the first
+                          reaches (DESLOC_E_INVALID) */
 } desloc_rows;
 
 /*

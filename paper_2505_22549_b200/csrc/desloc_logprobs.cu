@@ -318,7 +318,7 @@ __device__ __noinline__ void top_in_order(const Part<T> part, TopShared<THREADS>
 
 // Candidates for the `top` largest values of a part into s.key; how many, which may be more than there is room for.  s.own holds the largest
 // that each thread has seen (-FLT_MAX: none), behind a barrier.  The line is the top-th largest of the threads' largest values, or of 32 groups' of threads where that
-// is near enough (32 groups and 32 alternatives: the line is the least of all, and half of the row above it; 16384 rows of 1000 logits 42 us and 168): at
+// is near enough (32 groups and 32 alternatives: the line is the least of all, and half of the row above it; 16384 rows of 1000 bf16 logits 66 us and 168): at
 // least `top` values lie at or above it (all values, where fewer have any), only threads whose largest does have such, and their warps look at what these
 // took once more (some hundred bytes each, from L2).
 constexpr int TOP_OF_GROUPS = 16;
@@ -369,10 +369,10 @@ __device__ __forceinline__ int candidates_of_part(const Part<T> &part, TopShared
 
 // A block per row, or a cluster of CL blocks that take a part of it each and hand what they found to the first one through its shared
 // memory.  Bound: HBM reads of the logits, once (16-byte loads, four to eight in flight per thread), then the exponentials, 16 per clock and SM.
-// 4096 rows of 49152 bf16 logits with entropy and five alternatives: 78 us, 5.2 TB/s (0.79 of copy).  Before: value by value, blocks of 512 threads, the
-// alternatives looked for by single threads 172; blocks of 256 127 (of 128 134); two values per instruction and warps that look for alternatives 82;
-// whole rounds of loads without conditions and five blocks per SM 78 (four 82).  Without alternatives 8 us less.
-// Four rows of 49152 with 20 alternatives, clusters: 10.9 us (before keys that are ranked in one pass, and one barrier more, 23.7).
+// 4096 rows of 49152 bf16 logits with entropy and five alternatives: 83 us, 4.9 TB/s (0.74 of copy), 76 at its best.  Before, each at its best: value by
+// value, blocks of 512 threads, the alternatives looked for by single threads 172; blocks of 256 127 (of 128 134); two values per instruction and warps that
+// look for alternatives 82; whole rounds of loads without conditions and five blocks per SM 78 (four 82).  Without alternatives 6 us less.
+// Four rows of 49152 with 20 alternatives, clusters: 10.5 to 11.5 us (before keys that are ranked in one pass, and one barrier more, 23.7).
 template <typename T, bool ENT, bool TOP, int THREADS, int CL>
 __device__ __forceinline__ void logprobs_row(const LogprobArgs &a) {
     constexpr int WARPS = THREADS / 32, AHEAD = 4;
@@ -511,11 +511,12 @@ cudaError_t launch_rows(const LogprobArgs &a, cudaStream_t stream) {
 
 // ---- gradient ----------------------------------------------------------------------------------------
 // out_j = a (1[j = token] - p_j) - b p_j (log p_j + H): elementwise over a row.  Bound: HBM, the logits read and as many bytes written.
-// 4096 rows of 49152 bf16 logits: 121 us, 6.6 TB/s (1.01 of copy); value by value 169; shares of 2 and 8 pieces a thread instead of 4 143 and 122.
+// 4096 rows of 49152 bf16 logits: 122 us, 6.6 TB/s (1.01 of copy); value by value 169; shares of 2 and 8 pieces a thread instead of 4 143 and 122.
 //
 // p_j = exp(x_j - lse) is off by |lse| 2^-24 of itself from the rounding of lse, and what the token's own entry and the entropy's part leave of a difference
 // is off by as much of p, however little is left.  Where that passes 1.5e-5 (FAR_LSE; a few steps of 1 - p already in bf16, where the next logit is 8 below),
-// the row's first block takes all of the row, and goes over it for the largest logit and the sum behind it instead: slow, and rare.
+// the row's first block takes all of the row, and goes over it for the largest logit and the sum behind it instead: slow (4096 rows of 49152 bf16 logits at
+// 300: 502 us instead of 119, fp32 669 instead of 233), and rare.
 constexpr int GRAD_THREADS = 256, GRAD_AHEAD = 4;
 
 // With entropy, log p is a factor beside the caller's weight.  Logits more than NO_LOGIT below lse, whose p is 0 (2^-126 is e^-87; bf16's steps at the largest

@@ -392,7 +392,8 @@ __global__ void __launch_bounds__(32) addresses_kernel(const __grid_constant__ A
 }
 
 // out^m = factor_m g^m, a chunk per block.  The last chunks first: of what the norms' pass read, the end is still in L2.  135 M parameters x 4 workers,
-// fp32 to bf16: 450 us, 7.1 TB/s; with the norms (302 us) and the addresses 853 us, 6.3 TB/s of what both passes move.
+// fp32 to bf16: 450 us, 7.1 TB/s, by itself (what it wrote last is in L2 at its end); 516, 6.3 TB/s, in passes in a row, with the norms (306 us) and the
+// addresses 861 us.
 constexpr int SCALE_THREADS = 128;
 
 template <typename ST, typename DT>
@@ -412,8 +413,8 @@ scale_kernel(const Chunk *chunks, unsigned nchunks, const void *const *g, const 
 }
 
 // Small problems: norms as small_norms_kernel has them (the same bits where a warp has one share, as there), and what was read is in L2 for the
-// second pass.  Few addresses travel in the parameters: one launch in all.  From Python: 4096 parameters x 2 7.3 us (4.4 on the GPU), 0.2 M x 4 in 21
-// packed tensors, bf16, 8.8 us (by four launches 17.0).
+// second pass.  Few addresses travel in the parameters: one launch in all.  From Python: 4096 parameters x 2 7.0 us (4.4 on the GPU), 0.2 M x 4 in 21
+// packed tensors, bf16, 8.8 us (5.4 on the GPU; by four launches 17.0).
 constexpr int SMALL_CLIP_ADDRESSES = 128, SMALL_CLIP_SHARES = 4;
 constexpr int64_t SMALL_CLIP_BYTES = 3 << 19;   // of a worker: eight SMs read 6.6 MB in 45 us, four launches take 17 for any small list
 struct SmallClip {
