@@ -462,6 +462,84 @@ DESLOC_API int desloc_token_logprobs_grad(int64_t outer, int64_t inner, int64_t 
                                           const desloc_rows *tokens, const float *lse, const float *dlogp, const float *entropy,
                                           const float *dentropy, const desloc_rows *out, int cuda_device, void *stream);
 
+/*
+ * The gated feed-forward block of every worker with its own weights, in bf16 with sums in fp32:
+ *   g = h gate^T,  u = h up^T,  z = g / (1 + exp(-g)) * u,  y = z down^T        (gate, up [hidden, width]; down [width, hidden])
+ * for `tokens` rows h of each worker.  g, u and z are rounded to bf16 where they are kept or enter a product; z comes from g and u as the sums have them.
+ */
+typedef struct {
+    int32_t gate, up, down;      /* numbers of the three tensors, all different */
+    int64_t width, hidden;       /* width * hidden = numel of each (DESLOC_E_RANGE); both up to 2^20 */
+    int64_t tokens;              /* per worker, 0 .. 2^24 */
+    const void *const *weights;  /* host array of M*num_tensors DEVICE pointers to bf16 copies of x, as they enter the products; only the three are read */
+    desloc_rows h;               /* row (m, i), bf16 */
+} desloc_ffn;
+
+/*
+ * y as above.
+ *   kept_gate, kept_up : device, bf16, dense [M][tokens][hidden]: g and u for the way back; both or neither (NULL).
+ *   y                  : row (m, i), bf16.
+ *   work, work_bytes   : device memory, 256-byte aligned, of desloc_gated_ffn_bytes() bytes at least; that answer goes by the sizes and by how h and the weights
+ *                        lie (rows that begin on 16-byte boundaries are read in place, others are copied first).
+ */
+DESLOC_API int desloc_gated_ffn(desloc_ctx *ctx, const desloc_ffn *ffn, void *kept_gate, void *kept_up, const desloc_rows *y, void *work, int64_t work_bytes,
+                                void *stream);
+DESLOC_API int64_t desloc_gated_ffn_bytes(const desloc_ctx *ctx, const desloc_ffn *ffn);
+
+/*
+ * Its way back from dy: with s the sigmoid of g and dz = dy down,
+ *   du = dz g s,  dg = dz u s (1 + g (1 - s)),  dh = dg gate + du up;
+ * gradients of the weights dg^T h, du^T h and dy^T z in the place of the workers' gradients of the three tensors, in cfg.grad_dtype -- or, where `accumulate`
+ * is not 0, added to what those hold.  z, dg and du enter their products in bf16.
+ *   kept_gate, kept_up : what desloc_gated_ffn() kept.      dy, dh : rows (m, i), bf16.
+ *   grads              : host array of M*num_tensors DEVICE pointers, as for desloc_step(); only those of the three are read.  DESLOC_E_INVALID where two overlap.
+ */
+DESLOC_API int desloc_gated_ffn_grad(desloc_ctx *ctx, const desloc_ffn *ffn, const void *kept_gate, const void *kept_up, const desloc_rows *dy,
+                                     const desloc_rows *dh, int32_t accumulate, void *const *grads, void *work, int64_t work_bytes, void *stream);
+DESLOC_API int64_t desloc_gated_ffn_grad_bytes(const desloc_ctx *ctx, const desloc_ffn *ffn, const desloc_rows *dy);
+
+/*
+ * Orthogonalised updates: of matrices U [rows, columns], X_0 = U / (|U|_F + eps) and, for each of `steps` triples (a, b, c),
+ *   X := a X + (b G + c G^2) X,  G = X X^T,
+ * by which singular values of 1e-3 and more come near 1 (with the default triples, within 0.7 .. 1.2) and the singular vectors stay.  Products take fp16 operands with sums
+ * in fp32, X itself is carried in 22 bits from step to step; the result is off by some 2e-3 of its norm.  A matrix of zeros stays one; one that holds
+ * values that are not finite has results that are not, and no other matrix does.
+ */
+typedef enum {
+    DESLOC_SCALE_NONE = 0,
+    DESLOC_SCALE_ASPECT = 1, /* times sqrt(max(1, rows / columns)) */
+    DESLOC_SCALE_RMS = 2     /* times 0.2 sqrt(max(rows, columns)): entries as large as those of an Adam step */
+} desloc_scale_t;
+#define DESLOC_MAX_NEWTON_SCHULZ 32
+
+typedef struct {
+    const int32_t *tensors;     /* host, [count] numbers of tensors, no two alike */
+    const int64_t *columns;     /* host, [count]: each divides numel into rows; rows and columns up to 2^20 */
+    int32_t count;              /* of them, for every worker; 0: nothing is done */
+    int32_t steps;              /* 1 .. DESLOC_MAX_NEWTON_SCHULZ */
+    const float *coefficients;  /* host, [steps][3], finite, at most 64 in magnitude; NULL: (3.4445, -4.7750, 2.0315) at every step */
+    float eps;                  /* >= 0; 0 makes NaN of a matrix of zeros */
+    int32_t scale;              /* desloc_scale_t */
+    int32_t updates_dtype;
+    const void *const *updates; /* host array of M*num_tensors DEVICE pointers, only those of `tensors` are read; NULL: the context's u (fp32) */
+    const void *const *grads;   /* NULL, or the same of gradients in cfg.grad_dtype: U is then the look-ahead beta1 update + (1 - beta1) grad */
+} desloc_orthogonal;
+
+/*
+ * Results into `out` (the same indexing; fp32 or bf16).  out[i] may be updates[i], or grads[i], where the types are equal; DESLOC_E_INVALID where a matrix of `out` shares
+ * bytes with another of `out` or any other that is read.
+ *   work, work_bytes : device memory, 256-byte aligned, of desloc_orthogonal_bytes() bytes at least (whatever the addresses are).
+ */
+DESLOC_API int desloc_orthogonalize(desloc_ctx *ctx, const desloc_orthogonal *how, int32_t out_dtype, void *const *out, void *work, int64_t work_bytes, void *stream);
+
+/*
+ * The step of every worker's x along them: x := x (1 - lr weight_decay) - lr * result, weight_decay from the configuration.  With u from desloc_step() of
+ * an SGDM context at rate 0 (momentum and the averages of u and x, each on its period) in front, this is Algorithm 1 with orthogonalised momentum as OPT.
+ * lr must be finite.
+ */
+DESLOC_API int desloc_orthogonal_step(desloc_ctx *ctx, const desloc_orthogonal *how, float lr, void *work, int64_t work_bytes, void *stream);
+DESLOC_API int64_t desloc_orthogonal_bytes(const desloc_ctx *ctx, const desloc_orthogonal *how);
+
 /* Static description of a status code; never NULL. */
 DESLOC_API const char *desloc_strerror(int status);
 

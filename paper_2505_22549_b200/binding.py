@@ -26,6 +26,8 @@ DESLOC_STATIC_MAX_POINTERS, DESLOC_STATIC_MAX_CHUNKS = 2048, 32768
 DESLOC_MAX_M = 256
 DESLOC_I32, DESLOC_I64 = 0, 1
 DESLOC_MAX_TOP = 32
+DESLOC_SCALE_NONE, DESLOC_SCALE_ASPECT, DESLOC_SCALE_RMS = 0, 1, 2
+DESLOC_MAX_NEWTON_SCHULZ = 32
 
 OPT_BY_NAME = {"adam": DESLOC_ADAM, "adopt": DESLOC_ADOPT, "sgdm": DESLOC_SGDM}
 DTYPE_BY_NAME = {"f32": DESLOC_F32, "bf16": DESLOC_BF16}
@@ -58,6 +60,19 @@ class DeslocRows(ctypes.Structure):
 
 def rows(data: int, dtype: int, stride0: int, stride1: int) -> DeslocRows:
     return DeslocRows(data or None, dtype, (ctypes.c_int64 * 2)(stride0, stride1))
+
+
+class DeslocFfn(ctypes.Structure):
+    """Mirror of ``desloc_ffn``."""
+    _fields_ = [("gate", ctypes.c_int32), ("up", ctypes.c_int32), ("down", ctypes.c_int32), ("width", ctypes.c_int64), ("hidden", ctypes.c_int64),
+                ("tokens", ctypes.c_int64), ("weights", ctypes.POINTER(ctypes.c_void_p)), ("h", DeslocRows)]
+
+
+class DeslocOrthogonal(ctypes.Structure):
+    """Mirror of ``desloc_orthogonal``."""
+    _fields_ = [("tensors", ctypes.POINTER(ctypes.c_int32)), ("columns", ctypes.POINTER(ctypes.c_int64)), ("count", ctypes.c_int32),
+                ("steps", ctypes.c_int32), ("coefficients", ctypes.POINTER(ctypes.c_float)), ("eps", ctypes.c_float), ("scale", ctypes.c_int32),
+                ("updates_dtype", ctypes.c_int32), ("updates", ctypes.POINTER(ctypes.c_void_p)), ("grads", ctypes.POINTER(ctypes.c_void_p))]
 
 
 class DeslocError(RuntimeError):
@@ -155,6 +170,21 @@ _lib.desloc_token_logprobs.restype = ctypes.c_int
 _lib.desloc_token_logprobs.argtypes = [_I64, _I64, _I64, _ROWS, _ROWS, _I32, _P, _P, _P, _P, _P, ctypes.c_int, _P]
 _lib.desloc_token_logprobs_grad.restype = ctypes.c_int
 _lib.desloc_token_logprobs_grad.argtypes = [_I64, _I64, _I64, _ROWS, _ROWS, _P, _P, _P, _P, _ROWS, ctypes.c_int, _P]
+_FFN, _ORTH = ctypes.POINTER(DeslocFfn), ctypes.POINTER(DeslocOrthogonal)
+_lib.desloc_gated_ffn.restype = ctypes.c_int
+_lib.desloc_gated_ffn.argtypes = [_P, _FFN, _P, _P, _ROWS, _P, _I64, _P]
+_lib.desloc_gated_ffn_bytes.restype = _I64
+_lib.desloc_gated_ffn_bytes.argtypes = [_P, _FFN]
+_lib.desloc_gated_ffn_grad.restype = ctypes.c_int
+_lib.desloc_gated_ffn_grad.argtypes = [_P, _FFN, _P, _P, _ROWS, _ROWS, _I32, _PP, _P, _I64, _P]
+_lib.desloc_gated_ffn_grad_bytes.restype = _I64
+_lib.desloc_gated_ffn_grad_bytes.argtypes = [_P, _FFN, _ROWS]
+_lib.desloc_orthogonalize.restype = ctypes.c_int
+_lib.desloc_orthogonalize.argtypes = [_P, _ORTH, _I32, _PP, _P, _I64, _P]
+_lib.desloc_orthogonal_step.restype = ctypes.c_int
+_lib.desloc_orthogonal_step.argtypes = [_P, _ORTH, _F, _P, _I64, _P]
+_lib.desloc_orthogonal_bytes.restype = _I64
+_lib.desloc_orthogonal_bytes.argtypes = [_P, _ORTH]
 _lib.desloc_strerror.restype = ctypes.c_char_p
 _lib.desloc_strerror.argtypes = [ctypes.c_int]
 _lib.desloc_last_cuda_error.restype = ctypes.c_int
@@ -372,6 +402,71 @@ def desloc_token_logprobs_grad(outer: int, inner: int, vocab: int, logits: Deslo
                                          dentropy or None, out, int(cuda_device), stream or None)
     if rc != DESLOC_OK:
         raise DeslocError(rc, "desloc_token_logprobs_grad")
+
+
+def _address(array):
+    """A host array of device pointers given as a ctypes array, a sequence of integers or the address of one (0 or None: none)."""
+    if array is None or isinstance(array, int):
+        return ctypes.cast(array or None, _PP)
+    return ctypes.cast(array if isinstance(array, ctypes.Array) else _ptr_array(array), _PP)
+
+
+def ffn(gate: int, up: int, down: int, width: int, hidden: int, tokens: int, weights, h: DeslocRows) -> DeslocFfn:
+    return DeslocFfn(int(gate), int(up), int(down), int(width), int(hidden), int(tokens), _address(weights), h)
+
+
+def orthogonal(tensors: Sequence[int], columns: Sequence[int], steps: int = 5, coefficients=None, eps: float = 1e-7, scale: int = DESLOC_SCALE_NONE,
+               updates_dtype: int = DESLOC_F32, updates=None, grads=None) -> DeslocOrthogonal:
+    """coefficients: 3 * steps numbers, or None; updates, grads: host arrays of addresses, or None."""
+    n = len(tensors)
+    if len(columns) != n or (coefficients is not None and len(coefficients) != 3 * steps):
+        raise ValueError("one number of columns per tensor, three coefficients per step")
+    return DeslocOrthogonal((ctypes.c_int32 * max(1, n))(*tensors), (ctypes.c_int64 * max(1, n))(*columns), n, int(steps),
+                            (ctypes.c_float * len(coefficients))(*coefficients) if coefficients is not None else None, float(eps), int(scale),
+                            int(updates_dtype), _address(updates), _address(grads))
+
+
+def _checked(ctx: int, rc: int, where: str) -> int:
+    if rc < 0:
+        raise DeslocError(rc, where, _lib.desloc_last_cuda_error(ctx) if ctx else 0)
+    return int(rc)
+
+
+def desloc_gated_ffn_bytes(ctx: int, ffn: DeslocFfn) -> int:
+    """Bytes of working memory that desloc_gated_ffn() needs."""
+    return _checked(ctx, _lib.desloc_gated_ffn_bytes(ctx, ffn), "desloc_gated_ffn_bytes")
+
+
+def desloc_gated_ffn(ctx: int, ffn: DeslocFfn, kept_gate: int, kept_up: int, y: DeslocRows, work: int, work_bytes: int, stream: int = 0) -> None:
+    """The gated feed-forward block of every worker; kept_gate, kept_up: device addresses, or 0."""
+    _checked(ctx, _lib.desloc_gated_ffn(ctx, ffn, kept_gate or None, kept_up or None, y, work or None, int(work_bytes), stream or None), "desloc_gated_ffn")
+
+
+def desloc_gated_ffn_grad_bytes(ctx: int, ffn: DeslocFfn, dy: DeslocRows) -> int:
+    """Bytes of working memory that desloc_gated_ffn_grad() needs."""
+    return _checked(ctx, _lib.desloc_gated_ffn_grad_bytes(ctx, ffn, dy), "desloc_gated_ffn_grad_bytes")
+
+
+def desloc_gated_ffn_grad(ctx: int, ffn: DeslocFfn, kept_gate: int, kept_up: int, dy: DeslocRows, dh: DeslocRows, accumulate: bool, grads, work: int,
+                          work_bytes: int, stream: int = 0) -> None:
+    """Its way back: dh and the gradients of the three weights."""
+    _checked(ctx, _lib.desloc_gated_ffn_grad(ctx, ffn, kept_gate or None, kept_up or None, dy, dh, int(bool(accumulate)), _address(grads), work or None,
+                                             int(work_bytes), stream or None), "desloc_gated_ffn_grad")
+
+
+def desloc_orthogonal_bytes(ctx: int, how: DeslocOrthogonal) -> int:
+    """Bytes of working memory that desloc_orthogonalize() and desloc_orthogonal_step() need."""
+    return _checked(ctx, _lib.desloc_orthogonal_bytes(ctx, how), "desloc_orthogonal_bytes")
+
+
+def desloc_orthogonalize(ctx: int, how: DeslocOrthogonal, out_dtype: int, out, work: int, work_bytes: int, stream: int = 0) -> None:
+    """Orthogonalised updates into `out`."""
+    _checked(ctx, _lib.desloc_orthogonalize(ctx, how, int(out_dtype), _address(out), work or None, int(work_bytes), stream or None), "desloc_orthogonalize")
+
+
+def desloc_orthogonal_step(ctx: int, how: DeslocOrthogonal, lr: float, work: int, work_bytes: int, stream: int = 0) -> None:
+    """The step of x along orthogonalised updates."""
+    _checked(ctx, _lib.desloc_orthogonal_step(ctx, how, float(lr), work or None, int(work_bytes), stream or None), "desloc_orthogonal_step")
 
 
 def desloc_set_workers(ctx: int, M_new: int, first_new: int, x, u, v, stream: int = 0) -> None:

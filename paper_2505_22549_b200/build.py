@@ -11,6 +11,7 @@ import concurrent.futures as cf
 import glob
 import hashlib
 import os
+import re
 import subprocess
 import sys
 
@@ -40,12 +41,24 @@ def _sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.cu")))
 
 
+def _included(src: str) -> list:
+    """The headers of this tree that a translation unit includes, directly or not."""
+    found, todo = set(), [src]
+    while todo:
+        at = todo.pop()
+        for name in re.findall(r'^\s*#\s*include\s*"([^"]+)"', open(at).read(), re.M):
+            for folder in (os.path.dirname(at), INCLUDE):
+                path = os.path.normpath(os.path.join(folder, name))
+                if os.path.exists(path) and path not in found:
+                    found.add(path)
+                    todo.append(path)
+    return sorted(found)
+
+
 def _fingerprint(src: str) -> str:
-    """Hash of one translation unit with every header it may include and the flags."""
+    """Hash of one translation unit with the headers it includes and the flags."""
     h = hashlib.sha256()
-    files = [src] + sorted(glob.glob(os.path.join(CSRC, "*.cuh"))) + \
-        sorted(glob.glob(os.path.join(INCLUDE, "*.h")))
-    for f in files:
+    for f in [src] + _included(src):
         h.update(os.path.basename(f).encode())
         h.update(open(f, "rb").read())
     h.update(" ".join(NVCC_FLAGS).encode())

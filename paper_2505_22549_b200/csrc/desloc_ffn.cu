@@ -1,0 +1,430 @@
+// The gated feed-forward block of every worker, with its own weights, and its backward pass.
+#include "desloc_blocks.cuh"
+#include "desloc_gemm.cuh"
+
+namespace desloc {
+
+namespace {
+
+__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+
+__device__ __forceinline__ bool piece_of(const GemmGroup &g, int row0, int col0, bool wide, Piece &p) {
+    p.rows = min(32, g.m - row0), p.cols = min(32, g.n - col0), p.wide = wide;
+    return p.rows > 0 && p.cols > 0;
+}
+template <typename T>
+__device__ __forceinline__ T *at(T *p, long long elements) { return p + elements; }
+
+struct NoArgs {};
+
+// ---- forward -----------------------------------------------------------------------------------------
+// z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.
+struct UpEpilogue {
+    __device__ static void piece(const GemmArgs<UpEpilogue> &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        Piece p;
+        if (!piece_of(g, row0, col0, g.wide & 1, p)) return;
+        float gv[32], uv[32];
+        tmem_load32(d, gv);
+        tmem_load32(d + a.tile_n / 2, uv);
+        tmem_wait();
+        uint32_t w[16];
+        const long long kept = row0 * g.in_ld + col0;
+        if (g.out[1]) {
+            const Piece q{p.rows, p.cols, (g.wide & 2) != 0};
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
+            store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + kept, g.in_ld, q, w);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(uv[2 * e], uv[2 * e + 1]);
+            store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + kept, g.in_ld, q, w);
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) gv[e] = gv[e] * sigmoid(gv[e]) * uv[e];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
+        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p, w);
+    }
+};
+
+// A product as it is, in bf16 or fp32, or added to what is there.
+template <bool BF16, bool ADD>
+struct StoreEpilogue {
+    __device__ static void piece(const GemmArgs<StoreEpilogue> &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        Piece p;
+        if (!piece_of(g, row0, col0, g.wide & 1, p)) return;
+        float v[32];
+        tmem_load32(d, v);
+        tmem_wait();
+        const long long to = row0 * g.out_ld + col0;
+        if constexpr (BF16) {
+            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(g.out[0]) + to;
+            uint32_t w[16];
+            if constexpr (ADD) {
+                load_piece16(st, lane, out, g.out_ld, p, w);
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float2 was = unpack_bf16(w[e]);
+                    v[2 * e] += was.x, v[2 * e + 1] += was.y;
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            store_piece16(st, lane, out, g.out_ld, p, w);
+        } else {
+            float *out = static_cast<float *>(g.out[0]) + to;
+            if constexpr (ADD) {
+                float was[32];
+                load_piece32(st, lane, out, g.out_ld, p, was);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] += was[e];
+            }
+            store_piece32(st, lane, out, g.out_ld, p, v);
+        }
+    }
+};
+
+// ---- backward ----------------------------------------------------------------------------------------
+// From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.
+struct DzEpilogue {
+    __device__ static void piece(const GemmArgs<DzEpilogue> &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        Piece p;
+        if (!piece_of(g, row0, col0, (g.wide & 2) != 0, p)) return;
+        uint32_t gw[16], uw[16], zw[16];
+        const long long from = row0 * g.in_ld + col0, to = row0 * g.out_ld + col0;
+        load_piece16(st, lane, static_cast<const __nv_bfloat16 *>(g.in[0]) + from, g.in_ld, p, gw);
+        load_piece16(st, lane, static_cast<const __nv_bfloat16 *>(g.in[1]) + from, g.in_ld, p, uw);
+        float v[32];
+        tmem_load32(d, v);
+        tmem_wait();
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const float2 gg = unpack_bf16(gw[e]), uu = unpack_bf16(uw[e]);
+            const float sx = sigmoid(gg.x), sy = sigmoid(gg.y), ax = gg.x * sx, ay = gg.y * sy;
+            zw[e] = pack_bf16(ax * uu.x, ay * uu.y);
+            gw[e] = pack_bf16(v[2 * e] * uu.x * (sx + ax * (1.f - sx)), v[2 * e + 1] * uu.y * (sy + ay * (1.f - sy)));
+            uw[e] = pack_bf16(v[2 * e] * ax, v[2 * e + 1] * ay);
+        }
+        p.wide = g.wide & 1;
+        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p, zw);
+        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + to, g.out_ld, p, gw);
+        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + to, g.out_ld, p, uw);
+    }
+};
+
+// ---- rows that the copy engine does not take ---------------------------------------------------------
+// Copies matrices into rows of a multiple of eight values.  Bound: HBM, two bytes each way; a warp per row, lanes along it.
+constexpr int PACK_MOST = 64;
+struct PackArgs {
+    const unsigned short *from[PACK_MOST];
+    unsigned short *to;
+    long long from_ld, to_ld, to_batch;
+    int rows, cols;
+};
+__global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackArgs a) {
+    begin_and_let_next_begin();
+    wait_for_earlier_kernels();
+    const unsigned short *from = a.from[blockIdx.y];
+    unsigned short *to = a.to + blockIdx.y * a.to_batch;
+    const int lane = threadIdx.x & 31;
+    for (long long r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < a.rows; r += gridDim.x * 8ll)
+        for (int c = lane; c < a.cols; c += 32) to[r * a.to_ld + c] = from[r * a.from_ld + c];
+}
+
+int64_t padded(int64_t n) { return (n + 7) & ~int64_t{7}; }
+
+// An operand of every worker's: where it lies, or where it is copied to.
+struct Operand {
+    bool batched;               // one map for all workers, at `data`
+    const void *data;
+    const void *const *each;    // or an address per worker
+    int64_t rows, cols, ld, batch_ld;
+    bool packed;
+    int64_t bytes;              // of the copy
+
+    static Operand rows_of(const void *data, int M, int64_t rows, int64_t cols, long long s0, long long s1) {
+        Operand o{true, data, nullptr, rows, cols, rows == 1 ? padded(cols) : s1, M == 1 ? padded(cols) * rows : s0, false, 0};
+        o.packed = !boxes_fit(data, o.ld) || !boxes_fit(data, o.batch_ld) || o.ld < cols || o.batch_ld < 1 || o.ld >= (1ll << 38) || o.batch_ld >= (1ll << 38);
+        if (o.packed) o.bytes = M * rows * padded(cols) * 2;
+        return o;
+    }
+    static Operand weights(const void *const *each, int M, int64_t rows, int64_t cols) {
+        Operand o{false, nullptr, each, rows, cols, cols, 0, false, 0};
+        for (int m = 0; m < M; ++m) o.packed = o.packed || !boxes_fit(each[m], cols);
+        if (o.packed) o.bytes = M * rows * padded(cols) * 2;
+        return o;
+    }
+    // Fetches the operand of the workers [m0, m0 + n) in boxes of `box_rows`: from map `first` on, one map for all or one each.
+    template <typename E>
+    cudaError_t maps(GemmArgs<E> &a, int first, int every, int M, int m0, int n, int box_rows) const {
+        if (batched) return encode_boxes(&a.maps[first], data, true, cols, rows, M, ld, batch_ld, box_rows);
+        for (int i = 0; i < n; ++i) {
+            const cudaError_t e = encode_boxes(&a.maps[first + i * every], each[m0 + i], true, cols, rows, 1, ld, padded(cols) * rows, box_rows);
+            if (e != cudaSuccess) return e;
+        }
+        return cudaSuccess;
+    }
+};
+
+struct Bump {
+    char *work;
+    int64_t used = 0;
+    void *take(int64_t bytes) {
+        char *p = work ? work + used : nullptr;
+        used += (bytes + 255) & ~int64_t{255};
+        return p;
+    }
+};
+
+// Copies an operand where it has to be, and says where it is from then on.
+cudaError_t pack(Operand &o, int M, long long s0, long long s1, Bump &bump, cudaStream_t stream, int *launches) {
+    if (!o.packed) return cudaSuccess;
+    PackArgs a{};
+    a.to = static_cast<unsigned short *>(bump.take(o.bytes));
+    a.rows = static_cast<int>(o.rows), a.cols = static_cast<int>(o.cols);
+    a.from_ld = o.batched ? s1 : o.ld;
+    a.to_ld = padded(o.cols), a.to_batch = o.rows * a.to_ld;
+    const unsigned short *const base = static_cast<const unsigned short *>(o.data);
+    unsigned short *const start = a.to;
+    for (int m0 = 0; m0 < M; m0 += PACK_MOST) {
+        const int n = std::min(PACK_MOST, M - m0);
+        for (int i = 0; i < n; ++i) a.from[i] = o.batched ? base + (m0 + i) * s0 : static_cast<const unsigned short *>(o.each[m0 + i]);
+        a.to = start + m0 * a.to_batch;
+        const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((o.rows + 7) / 8, std::max(1, 8 * NUM_SMS / n)));
+        const cudaError_t e = launch_op(pack_kernel, dim3(blocks, n), dim3(256), 0, true, stream, a);
+        if (e != cudaSuccess) return e;
+        ++*launches;
+    }
+    o.batched = true, o.data = start, o.ld = a.to_ld, o.batch_ld = a.to_batch;
+    return cudaSuccess;
+}
+
+// Columns of a tile: of 256, 128 and 64 (dual: of both halves) the ones that take the fewest rounds of blocks, weighed by what a round costs: the
+// products of so many columns, and the rows of A that every tile brings again (worth some 64 columns).
+template <typename F>
+int pick_tile_n(bool dual, const F &tiles) {
+    int best = 0;
+    int64_t least = 0;
+    for (int n = 256; n >= (dual ? 128 : 64); n /= 2) {
+        const int64_t rounds = (tiles(dual ? n / 2 : n) + NUM_SMS - 1) / NUM_SMS, cost = rounds * (n + 64);
+        if (!best || cost < least) best = n, least = cost;
+    }
+    return best;
+}
+
+constexpr int WORKERS = 16;   // of a launch: three groups and two maps each at most
+
+struct Run {
+    cudaStream_t stream;
+    int *err, wait_limit, *launches;
+};
+
+bool wide16(const void *p, long long ld) { return boxes_fit(p, ld); }
+bool wide32(const void *p, long long ld) { return ((reinterpret_cast<uintptr_t>(p) | static_cast<uintptr_t>(ld * 4)) & 15u) == 0; }
+
+cudaError_t product_store(const Operand &x, const Operand &w, int M, int tokens, int n, int k, void *out, long long s0, long long s1, const Run &r) {
+    using E = StoreEpilogue<true, false>;
+    static thread_local GemmArgs<E> a;
+    for (int m0 = 0; m0 < M; m0 += WORKERS) {
+        const int some = std::min(WORKERS, M - m0), tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(tokens, n, t, false); });
+        begin_gemm(a, true, tile, false, false, 1);
+        cudaError_t e = x.maps(a, 0, 0, M, m0, some, GEMM_BM);
+        if (e == cudaSuccess) e = w.maps(a, 1, 1, M, m0, some, tile);
+        if (e != cudaSuccess) return e;
+        for (int i = 0; i < some; ++i) {
+            GemmGroup &g = add_group(a, tokens, n, k, 1);
+            g.a_map = 0, g.a_batch = m0 + i;
+            g.b_map = static_cast<short>(w.batched ? 1 : 1 + i), g.b_batch = w.batched ? m0 + i : 0;
+            g.out[0] = static_cast<__nv_bfloat16 *>(out) + (m0 + i) * s0;
+            g.out_ld = s1;
+            g.wide = wide16(g.out[0], s1);
+        }
+        e = launch_gemm(a, r.err, r.wait_limit, r.stream, r.launches);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+struct Operands {
+    Operand h, dy, gate, up, down;
+    Operands(const FfnArgs &a, bool backward)
+        : h(Operand::rows_of(a.h, a.M, a.tokens, a.width, a.hs0, a.hs1)),
+          dy(backward ? Operand::rows_of(a.dy, a.M, a.tokens, a.width, a.dys0, a.dys1) : Operand{}),
+          gate(Operand::weights(a.gate, a.M, a.hidden, a.width)), up(Operand::weights(a.up, a.M, a.hidden, a.width)),
+          down(Operand::weights(a.down, a.M, a.width, a.hidden)) {}
+    cudaError_t pack_all(const FfnArgs &a, bool backward, Bump &bump, const Run &r) {
+        cudaError_t e = pack(h, a.M, a.hs0, a.hs1, bump, r.stream, r.launches);
+        if (e == cudaSuccess && backward) e = pack(dy, a.M, a.dys0, a.dys1, bump, r.stream, r.launches);
+        for (Operand *o : {&gate, &up, &down})
+            if (e == cudaSuccess) e = pack(*o, a.M, 0, 0, bump, r.stream, r.launches);
+        return e;
+    }
+};
+
+// A k- or m/n-major operand of `rows` token rows in working memory.
+Operand inner_operand(const void *data, const FfnArgs &a, int64_t cols) {
+    return Operand::rows_of(data, a.M, a.tokens, cols, a.tokens * padded(cols), padded(cols));
+}
+
+template <bool BF16, bool ADD>
+cudaError_t weight_grads(const FfnArgs &a, const Operands &o, const Operand &z, const Operand &dg, const Operand &du, const Run &r) {
+    using E = StoreEpilogue<BF16, ADD>;
+    static thread_local GemmArgs<E> g;
+    for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
+        const int some = std::min(WORKERS, a.M - m0);
+        const int tile = pick_tile_n(false, [&](int t) {
+            return static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, t, false) + tiles_of(a.width, a.hidden, t, false));
+        });
+        begin_gemm(g, true, tile, false, false, 1);
+        int map = 0;
+        for (const Operand *x : {&dg, &du, &o.dy, &o.h, &z}) {
+            const cudaError_t e = x->maps(g, map++, 0, a.M, m0, some, 64);
+            if (e != cudaSuccess) return e;
+        }
+        for (int which = 0; which < 3; ++which)
+            for (int i = 0; i < some; ++i) {
+                GemmGroup &group = which < 2 ? add_group(g, a.hidden, a.width, a.tokens, 1) : add_group(g, a.width, a.hidden, a.tokens, 1);
+                group.a_map = static_cast<short>(which), group.b_map = which < 2 ? 3 : 4;
+                group.a_mn = group.b_mn = 1;
+                group.a_batch = group.b_batch = m0 + i;
+                group.out[0] = which == 0 ? a.dgate[m0 + i] : which == 1 ? a.dup[m0 + i] : a.ddown[m0 + i];
+                group.out_ld = which < 2 ? a.width : a.hidden;
+                group.wide = BF16 ? wide16(group.out[0], group.out_ld) : wide32(group.out[0], group.out_ld);
+            }
+        const cudaError_t e = launch_gemm(g, r.err, r.wait_limit, r.stream, r.launches);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+int64_t ffn_work(const FfnArgs &a, bool backward) {
+    Bump bump{nullptr};
+    const Operands o(a, backward);
+    for (const Operand *x : {&o.h, &o.dy, &o.gate, &o.up, &o.down}) bump.take(x->bytes);
+    for (int i = 0; i < (backward ? 3 : 1); ++i) bump.take(static_cast<int64_t>(a.M) * a.tokens * padded(a.hidden) * 2);
+    return bump.used;
+}
+
+cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
+    const Run r{stream, err, wait_limit, launches};
+    Bump bump{work};
+    Operands o(a, false);
+    const long long ld = padded(a.hidden), per = a.tokens * ld;
+    __nv_bfloat16 *const z = static_cast<__nv_bfloat16 *>(bump.take(a.M * per * 2));
+    cudaError_t e = o.pack_all(a, false, bump, r);
+    if (e != cudaSuccess) return e;
+    static thread_local GemmArgs<UpEpilogue> g;
+    for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
+        const int some = std::min(WORKERS, a.M - m0);
+        const int tile = pick_tile_n(true, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, t, false); });
+        begin_gemm(g, true, tile, true, false, 1);
+        e = o.h.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
+        // (gate and up of a worker next to one another: the second half of a tile's columns is the next map's)
+        if (e == cudaSuccess) e = o.gate.maps(g, 1, 2, a.M, m0, some, tile / 2);
+        if (e == cudaSuccess) e = o.up.maps(g, 2, 2, a.M, m0, some, tile / 2);
+        if (e != cudaSuccess) return e;
+        // where the one is a single map and the other one each, both take one each
+        const bool batched = o.gate.batched && o.up.batched;
+        if (!batched) {
+            for (int half = 0; half < 2; ++half) {
+                const Operand &w = half ? o.up : o.gate;
+                if (!w.batched) continue;
+                for (int i = 0; i < some && e == cudaSuccess; ++i)
+                    e = encode_boxes(&g.maps[1 + half + 2 * i], static_cast<const __nv_bfloat16 *>(w.data) + (m0 + i) * w.batch_ld, true, w.cols, w.rows, 1, w.ld,
+                                     w.batch_ld, tile / 2);
+            }
+            if (e != cudaSuccess) return e;
+        }
+        for (int i = 0; i < some; ++i) {
+            const int m = m0 + i;
+            GemmGroup &group = add_group(g, a.tokens, a.hidden, a.width, 1);
+            group.a_batch = m;
+            group.b_map = static_cast<short>(batched ? 1 : 1 + 2 * i), group.b_batch = batched ? m : 0;
+            group.out[0] = z + m * per, group.out_ld = ld;
+            group.wide = 1;
+            if (a.kept_gate) {
+                const long long from = static_cast<long long>(m) * a.tokens * a.hidden;
+                group.out[1] = static_cast<__nv_bfloat16 *>(a.kept_gate) + from;
+                group.out[2] = static_cast<__nv_bfloat16 *>(a.kept_up) + from;
+                group.in_ld = a.hidden;
+                if (wide16(group.out[1], a.hidden) && wide16(group.out[2], a.hidden)) group.wide |= 2;
+            }
+        }
+        e = launch_gemm(g, err, wait_limit, stream, launches);
+        if (e != cudaSuccess) return e;
+    }
+    return product_store(inner_operand(z, a, a.hidden), o.down, a.M, a.tokens, a.width, a.hidden, a.y, a.ys0, a.ys1, r);
+}
+
+cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
+    const Run r{stream, err, wait_limit, launches};
+    Bump bump{work};
+    Operands o(a, true);
+    const long long ld = padded(a.hidden), per = a.tokens * ld;
+    __nv_bfloat16 *inner[3];
+    for (auto &p : inner) p = static_cast<__nv_bfloat16 *>(bump.take(a.M * per * 2));
+    cudaError_t e = o.pack_all(a, true, bump, r);
+    if (e != cudaSuccess) return e;
+    {
+        static thread_local GemmArgs<DzEpilogue> g;
+        for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
+            const int some = std::min(WORKERS, a.M - m0);
+            const int tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, t, false); });
+            begin_gemm(g, true, tile, false, false, 1);
+            e = o.dy.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
+            if (e == cudaSuccess) e = o.down.maps(g, 1, 1, a.M, m0, some, 64);
+            if (e != cudaSuccess) return e;
+            for (int i = 0; i < some; ++i) {
+                const int m = m0 + i;
+                GemmGroup &group = add_group(g, a.tokens, a.hidden, a.width, 1);
+                group.a_batch = m;
+                group.b_map = static_cast<short>(o.down.batched ? 1 : 1 + i), group.b_batch = o.down.batched ? m : 0;
+                group.b_mn = 1;
+                const long long from = static_cast<long long>(m) * a.tokens * a.hidden;
+                group.in[0] = static_cast<const __nv_bfloat16 *>(a.was_gate) + from;
+                group.in[1] = static_cast<const __nv_bfloat16 *>(a.was_up) + from;
+                group.in_ld = a.hidden;
+                for (int k = 0; k < 3; ++k) group.out[k] = inner[k] + m * per;
+                group.out_ld = ld;
+                group.wide = 1 | (wide16(group.in[0], a.hidden) && wide16(group.in[1], a.hidden) ? 2 : 0);
+            }
+            e = launch_gemm(g, err, wait_limit, stream, launches);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    const Operand z = inner_operand(inner[0], a, a.hidden), dg = inner_operand(inner[1], a, a.hidden), du = inner_operand(inner[2], a, a.hidden);
+    {
+        // dh = dg gate + du up, one accumulator
+        using E = StoreEpilogue<true, false>;
+        static thread_local GemmArgs<E> g;
+        for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
+            const int some = std::min(WORKERS, a.M - m0);
+            const int tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, t, false); });
+            begin_gemm(g, true, tile, false, false, 2);
+            e = dg.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
+            if (e == cudaSuccess) e = du.maps(g, 1, 0, a.M, m0, some, GEMM_BM);
+            for (int i = 0; i < some && e == cudaSuccess; ++i)
+                for (int seg = 0; seg < 2 && e == cudaSuccess; ++seg) {
+                    const Operand &w = seg ? o.up : o.gate;
+                    const void *from = w.batched ? static_cast<const __nv_bfloat16 *>(w.data) + (m0 + i) * w.batch_ld : w.each[m0 + i];
+                    e = encode_boxes(&g.maps[2 + 2 * i + seg], from, true, w.cols, w.rows, 1, w.ld, padded(w.cols) * w.rows, 64);
+                }
+            if (e != cudaSuccess) return e;
+            for (int i = 0; i < some; ++i) {
+                GemmGroup &group = add_group(g, a.tokens, a.width, a.hidden, 1);
+                group.a_batch = m0 + i;
+                group.b_map = static_cast<short>(2 + 2 * i), group.b_mn = 1;
+                group.out[0] = static_cast<__nv_bfloat16 *>(a.dh) + (m0 + i) * a.dhs0;
+                group.out_ld = a.dhs1;
+                group.wide = wide16(group.out[0], a.dhs1);
+            }
+            e = launch_gemm(g, err, wait_limit, stream, launches);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    if (a.grad_bf16) return a.accumulate ? weight_grads<true, true>(a, o, z, dg, du, r) : weight_grads<true, false>(a, o, z, dg, du, r);
+    return a.accumulate ? weight_grads<false, true>(a, o, z, dg, du, r) : weight_grads<false, false>(a, o, z, dg, du, r);
+}
+
+}  // namespace desloc

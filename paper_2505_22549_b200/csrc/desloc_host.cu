@@ -18,6 +18,7 @@
 #include "desloc_inst.cuh"
 #include "desloc_internal.cuh"
 #include "desloc_norms.cuh"
+#include "desloc_blocks.cuh"
 #include "desloc_ops.cuh"
 #include "desloc_readout.cuh"
 
@@ -599,9 +600,9 @@ int check_table(const desloc_ctx *ctx, int32_t tensor, int64_t width, int64_t n)
     return numel % width == 0 && numel / width <= (1 << 30) ? DESLOC_OK : DESLOC_E_RANGE;
 }
 
-// Whether some of `count` (<= DESLOC_MAX_M) pieces of memory that are written share bytes.
+// Whether some of `count` (<= 3 * DESLOC_MAX_M) pieces of memory that are written share bytes.
 bool share_memory(void *const *at, int count, int64_t bytes) {
-    uintptr_t sorted[DESLOC_MAX_M];
+    uintptr_t sorted[3 * DESLOC_MAX_M];
     for (int i = 0; i < count; ++i) sorted[i] = reinterpret_cast<uintptr_t>(at[i]);
     std::sort(sorted, sorted + count);
     for (int i = 1; i < count; ++i)
@@ -663,6 +664,103 @@ int check_embedding(const desloc_ctx *ctx, int32_t tensor, int64_t width, const 
     if (!desloc::is_token_rows(tokens) || !desloc::is_value_rows(rows)) return DESLOC_E_INVALID;
     if (!std::isfinite(scale)) return DESLOC_E_RANGE;
     return check_table(ctx, tensor, width, n);
+}
+
+// The block's numbers and weights, checked; `a` gets them.
+int check_ffn(const desloc_ctx *ctx, const desloc_ffn &f, desloc::FfnArgs &a) {
+    const desloc_config &c = ctx->cfg;
+    const int32_t three[3] = {f.gate, f.up, f.down};
+    for (int32_t k : three)
+        if (k < 0 || k >= c.num_tensors) return DESLOC_E_RANGE;
+    if (f.gate == f.up || f.gate == f.down || f.up == f.down) return DESLOC_E_INVALID;
+    if (f.width < 1 || f.width > (1 << 20) || f.hidden < 1 || f.hidden > (1 << 20) || f.tokens < 0 || f.tokens > (1 << 24)) return DESLOC_E_RANGE;
+    for (int32_t k : three)
+        if (ctx->numel[k] != f.width * f.hidden) return DESLOC_E_RANGE;
+    if (f.h.dtype != DESLOC_BF16 || !desloc::is_value_rows(f.h)) return DESLOC_E_INVALID;
+    if (!f.weights || (f.tokens > 0 && !f.h.data)) return DESLOC_E_NULL;
+    a.M = c.M, a.tokens = static_cast<int>(f.tokens), a.width = static_cast<int>(f.width), a.hidden = static_cast<int>(f.hidden);
+    a.h = f.h.data, a.hs0 = f.h.stride[0], a.hs1 = f.h.stride[1];
+    const void **to[3] = {a.gate, a.up, a.down};
+    for (int i = 0; i < 3; ++i)
+        for (int m = 0; m < c.M; ++m) {
+            const void *p = f.weights[static_cast<int64_t>(m) * c.num_tensors + three[i]];
+            if (!p) return DESLOC_E_NULL;
+            if (reinterpret_cast<uintptr_t>(p) % 2) return DESLOC_E_INVALID;
+            to[i][m] = p;
+        }
+    return DESLOC_OK;
+}
+
+// bf16 rows of the block's width that are read or written.
+int check_rows(const desloc_ctx *ctx, const desloc_ffn &f, const desloc_rows &r, bool written) {
+    if (r.dtype != DESLOC_BF16 || !desloc::is_value_rows(r)) return DESLOC_E_INVALID;
+    if (f.tokens > 0 && !r.data) return DESLOC_E_NULL;
+    return written && desloc::rows_overlap(r, ctx->cfg.M, f.tokens, f.width) ? DESLOC_E_INVALID : DESLOC_OK;
+}
+
+constexpr float kNewtonSchulz[3] = {3.4445f, -4.7750f, 2.0315f};
+
+// Checks a list of matrices and lays it out; `coefficients` holds the default ones where it has to.  Host vectors: throws std::bad_alloc.
+int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool addresses, std::vector<desloc::OrthMatrix> &list, std::vector<float> &coefficients,
+                     desloc::OrthArgs &a) {
+    const desloc_config &c = ctx->cfg;
+    if (how.count < 0 || how.count > c.num_tensors || how.steps < 1 || how.steps > DESLOC_MAX_NEWTON_SCHULZ) return DESLOC_E_RANGE;
+    if (how.count > 0 && (!how.tensors || !how.columns)) return DESLOC_E_NULL;
+    if (!std::isfinite(how.eps) || how.eps < 0.f) return DESLOC_E_RANGE;
+    const auto known = [](int32_t t) { return t == DESLOC_F32 || t == DESLOC_BF16; };
+    if (how.scale < DESLOC_SCALE_NONE || how.scale > DESLOC_SCALE_RMS || (how.updates && !known(how.updates_dtype))) return DESLOC_E_INVALID;
+    coefficients.clear();
+    for (int i = 0; i < 3 * how.steps; ++i) {
+        const float v = how.coefficients ? how.coefficients[i] : kNewtonSchulz[i % 3];
+        if (!std::isfinite(v) || std::fabs(v) > 64.f) return DESLOC_E_RANGE;
+        coefficients.push_back(v);
+    }
+    std::vector<char> seen(static_cast<size_t>(c.num_tensors), 0);
+    list.clear();
+    list.reserve(static_cast<size_t>(how.count) * c.M);
+    a.update_bf16 = how.updates && how.updates_dtype == DESLOC_BF16;
+    a.grad_bf16 = c.grad_dtype == DESLOC_BF16;
+    const uintptr_t usz = a.update_bf16 ? 2 : 4, gsz = a.grad_bf16 ? 2 : 4;
+    for (int i = 0; i < how.count; ++i) {
+        const int32_t k = how.tensors[i];
+        if (k < 0 || k >= c.num_tensors) return DESLOC_E_RANGE;
+        if (seen[k]) return DESLOC_E_INVALID;
+        seen[k] = 1;
+        const int64_t cols = how.columns[i];
+        if (cols < 1 || cols > (1 << 20) || ctx->numel[k] % cols || ctx->numel[k] / cols > (1 << 20)) return DESLOC_E_RANGE;
+        for (int m = 0; m < c.M; ++m) {
+            const int64_t at = static_cast<int64_t>(m) * c.num_tensors + k;
+            desloc::OrthMatrix x{static_cast<int>(ctx->numel[k] / cols), static_cast<int>(cols), static_cast<int>(at), nullptr, nullptr, nullptr};
+            if (addresses && how.updates) {
+                if (!(x.update = how.updates[at])) return DESLOC_E_NULL;
+                if (reinterpret_cast<uintptr_t>(x.update) % usz) return DESLOC_E_INVALID;
+            }
+            if (addresses && how.grads) {
+                if (!(x.grad = how.grads[at])) return DESLOC_E_NULL;
+                if (reinterpret_cast<uintptr_t>(x.grad) % gsz) return DESLOC_E_INVALID;
+            }
+            list.push_back(x);
+        }
+    }
+    a.list = list.data(), a.count = static_cast<int>(list.size()), a.steps = how.steps;
+    a.coefficients = coefficients.data();
+    a.eps = how.eps, a.beta = c.beta1, a.scale = how.scale;
+    a.u_table = reinterpret_cast<float *const *>(ctx->res.d_tables + ctx->nptr);
+    a.x_table = reinterpret_cast<float *const *>(ctx->res.d_tables);
+    return DESLOC_OK;
+}
+
+int run_orthogonal(desloc_ctx *ctx, const desloc::OrthArgs &a, void *work, int64_t work_bytes, void *stream) {
+    if (a.count == 0) return DESLOC_OK;
+    if (!work) return DESLOC_E_NULL;
+    if (reinterpret_cast<uintptr_t>(work) % 256) return DESLOC_E_INVALID;
+    if (desloc::orth_work(a) > work_bytes) return DESLOC_E_RANGE;
+    return on_device(ctx, [&] {
+        int launches = 0;
+        const cudaError_t e = desloc::launch_orth(a, static_cast<char *>(work), ctx->d_err, ctx->wait_limit, static_cast<cudaStream_t>(stream), &launches);
+        ctx->launches += launches;
+        return e;
+    });
 }
 
 }  // namespace
@@ -1033,6 +1131,152 @@ int desloc_clip_grads(desloc_ctx *ctx, float max_norm, int32_t grads_dtype, cons
         ctx->launches += launches;
         return e;
     });
+}
+
+int64_t desloc_gated_ffn_bytes(const desloc_ctx *ctx, const desloc_ffn *ffn) {
+    if (!ctx || !ffn) return DESLOC_E_NULL;
+    desloc::FfnArgs a{};
+    const int rc = check_ffn(ctx, *ffn, a);
+    return rc == DESLOC_OK ? desloc::ffn_work(a, false) : rc;
+}
+
+int desloc_gated_ffn(desloc_ctx *ctx, const desloc_ffn *ffn, void *kept_gate, void *kept_up, const desloc_rows *y, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_gated_ffn");
+    if (!ctx || !ffn || !y || !kept_gate != !kept_up) return DESLOC_E_NULL;
+    desloc::FfnArgs a{};
+    int rc = check_ffn(ctx, *ffn, a);
+    if (rc == DESLOC_OK) rc = check_rows(ctx, *ffn, *y, true);
+    if (rc != DESLOC_OK) return rc;
+    if (a.tokens == 0) return DESLOC_OK;
+    if (!work) return DESLOC_E_NULL;
+    if (reinterpret_cast<uintptr_t>(work) % 256 || reinterpret_cast<uintptr_t>(kept_gate) % 2 || reinterpret_cast<uintptr_t>(kept_up) % 2) return DESLOC_E_INVALID;
+    if (desloc::ffn_work(a, false) > work_bytes) return DESLOC_E_RANGE;
+    a.y = y->data, a.ys0 = y->stride[0], a.ys1 = y->stride[1];
+    a.kept_gate = kept_gate, a.kept_up = kept_up;
+    return on_device(ctx, [&] {
+        int launches = 0;
+        const cudaError_t e = desloc::launch_ffn(a, static_cast<char *>(work), ctx->d_err, ctx->wait_limit, static_cast<cudaStream_t>(stream), &launches);
+        ctx->launches += launches;
+        return e;
+    });
+}
+
+int64_t desloc_gated_ffn_grad_bytes(const desloc_ctx *ctx, const desloc_ffn *ffn, const desloc_rows *dy) {
+    if (!ctx || !ffn || !dy) return DESLOC_E_NULL;
+    desloc::FfnArgs a{};
+    int rc = check_ffn(ctx, *ffn, a);
+    if (rc == DESLOC_OK) rc = check_rows(ctx, *ffn, *dy, false);
+    if (rc != DESLOC_OK) return rc;
+    a.dy = dy->data, a.dys0 = dy->stride[0], a.dys1 = dy->stride[1];
+    return desloc::ffn_work(a, true);
+}
+
+int desloc_gated_ffn_grad(desloc_ctx *ctx, const desloc_ffn *ffn, const void *kept_gate, const void *kept_up, const desloc_rows *dy, const desloc_rows *dh,
+                          int32_t accumulate, void *const *grads, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_gated_ffn_grad");
+    if (!ctx || !ffn || !dy || !dh || !grads) return DESLOC_E_NULL;
+    desloc::FfnArgs a{};
+    int rc = check_ffn(ctx, *ffn, a);
+    if (rc == DESLOC_OK) rc = check_rows(ctx, *ffn, *dy, false);
+    if (rc == DESLOC_OK) rc = check_rows(ctx, *ffn, *dh, true);
+    if (rc != DESLOC_OK) return rc;
+    const desloc_config &c = ctx->cfg;
+    const bool bf16 = c.grad_dtype == DESLOC_BF16;
+    const int32_t three[3] = {ffn->gate, ffn->up, ffn->down};
+    void **to[3] = {a.dgate, a.dup, a.ddown};
+    void *all[3 * DESLOC_MAX_M];
+    for (int i = 0; i < 3; ++i)
+        for (int m = 0; m < c.M; ++m) {
+            void *p = grads[static_cast<int64_t>(m) * c.num_tensors + three[i]];
+            if (!p) return DESLOC_E_NULL;
+            if (reinterpret_cast<uintptr_t>(p) % (bf16 ? 2 : 4)) return DESLOC_E_INVALID;
+            to[i][m] = all[i * c.M + m] = p;
+        }
+    const int64_t bytes = ffn->width * ffn->hidden * (bf16 ? 2 : 4);
+    if (share_memory(all, 3 * c.M, bytes)) return DESLOC_E_INVALID;
+    a.accumulate = accumulate != 0, a.grad_bf16 = bf16;
+    if (a.tokens == 0) {
+        if (a.accumulate) return DESLOC_OK;
+        return on_device(ctx, [&] {
+            cudaError_t e = cudaSuccess;
+            for (int i = 0; i < 3 * c.M && e == cudaSuccess; ++i) e = cudaMemsetAsync(all[i], 0, static_cast<size_t>(bytes), static_cast<cudaStream_t>(stream));
+            return e;
+        });
+    }
+    if (!kept_gate || !kept_up || !work) return DESLOC_E_NULL;
+    if (reinterpret_cast<uintptr_t>(work) % 256 || reinterpret_cast<uintptr_t>(kept_gate) % 2 || reinterpret_cast<uintptr_t>(kept_up) % 2) return DESLOC_E_INVALID;
+    a.was_gate = kept_gate, a.was_up = kept_up;
+    a.dy = dy->data, a.dys0 = dy->stride[0], a.dys1 = dy->stride[1];
+    a.dh = dh->data, a.dhs0 = dh->stride[0], a.dhs1 = dh->stride[1];
+    if (desloc::ffn_work(a, true) > work_bytes) return DESLOC_E_RANGE;
+    return on_device(ctx, [&] {
+        int launches = 0;
+        const cudaError_t e = desloc::launch_ffn_grad(a, static_cast<char *>(work), ctx->d_err, ctx->wait_limit, static_cast<cudaStream_t>(stream), &launches);
+        ctx->launches += launches;
+        return e;
+    });
+}
+
+int64_t desloc_orthogonal_bytes(const desloc_ctx *ctx, const desloc_orthogonal *how) {
+    if (!ctx || !how) return DESLOC_E_NULL;
+    try {
+        std::vector<desloc::OrthMatrix> list;
+        std::vector<float> coefficients;
+        desloc::OrthArgs a{};
+        const int rc = check_orthogonal(ctx, *how, false, list, coefficients, a);
+        return rc == DESLOC_OK ? desloc::orth_work(a) : rc;
+    } catch (const std::bad_alloc &) {
+        return DESLOC_E_NOMEM;
+    }
+}
+
+int desloc_orthogonalize(desloc_ctx *ctx, const desloc_orthogonal *how, int32_t out_dtype, void *const *out, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_orthogonalize");
+    if (!ctx || !how || !out) return DESLOC_E_NULL;
+    if (out_dtype != DESLOC_F32 && out_dtype != DESLOC_BF16) return DESLOC_E_INVALID;
+    try {
+        std::vector<desloc::OrthMatrix> list;
+        std::vector<float> coefficients;
+        desloc::OrthArgs a{};
+        const int rc = check_orthogonal(ctx, *how, true, list, coefficients, a);
+        if (rc != DESLOC_OK) return rc;
+        a.out_bf16 = out_dtype == DESLOC_BF16;
+        const uintptr_t osz = a.out_bf16 ? 2 : 4;
+        std::vector<int64_t> numel;
+        std::vector<const void *> from, ahead;
+        std::vector<void *> to;
+        for (desloc::OrthMatrix &x : list) {
+            if (!(x.out = out[x.index])) return DESLOC_E_NULL;
+            if (reinterpret_cast<uintptr_t>(x.out) % osz) return DESLOC_E_INVALID;
+            numel.push_back(static_cast<int64_t>(x.rows) * x.cols);
+            from.push_back(x.update), ahead.push_back(x.grad), to.push_back(x.out);
+        }
+        const int n = static_cast<int>(list.size());
+        if (n > 0 && (share_memory(numel.data(), n, 1, how->updates ? from.data() : const_cast<const void *const *>(to.data()), how->updates ? (a.update_bf16 ? 2 : 4) : osz,
+                                   to.data(), osz) ||
+                      (how->grads && share_memory(numel.data(), n, 1, ahead.data(), a.grad_bf16 ? 2 : 4, to.data(), osz))))
+            return DESLOC_E_INVALID;
+        return run_orthogonal(ctx, a, work, work_bytes, stream);
+    } catch (const std::bad_alloc &) {
+        return DESLOC_E_NOMEM;
+    }
+}
+
+int desloc_orthogonal_step(desloc_ctx *ctx, const desloc_orthogonal *how, float lr, void *work, int64_t work_bytes, void *stream) {
+    desloc::NvtxRange range("desloc_orthogonal_step");
+    if (!ctx || !how) return DESLOC_E_NULL;
+    if (!std::isfinite(lr)) return DESLOC_E_RANGE;
+    try {
+        std::vector<desloc::OrthMatrix> list;
+        std::vector<float> coefficients;
+        desloc::OrthArgs a{};
+        const int rc = check_orthogonal(ctx, *how, true, list, coefficients, a);
+        if (rc != DESLOC_OK) return rc;
+        a.lr = lr, a.decay = static_cast<float>(1.0 - static_cast<double>(lr) * ctx->cfg.weight_decay);
+        return run_orthogonal(ctx, a, work, work_bytes, stream);
+    } catch (const std::bad_alloc &) {
+        return DESLOC_E_NOMEM;
+    }
 }
 
 int desloc_set_workers(desloc_ctx *ctx, int32_t M_new, int32_t first_new, float *const *x,

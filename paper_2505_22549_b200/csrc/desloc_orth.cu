@@ -1,0 +1,474 @@
+// Orthogonalised updates: Newton-Schulz products of every worker's matrices, from the momentum to the step.
+#include "desloc_blocks.cuh"
+#include "desloc_gemm.cuh"
+
+#include <algorithm>
+
+namespace desloc {
+
+namespace {
+
+// X := U / (|U| + eps), then `steps` times X := a X + (b G + c G^2) X with G = X X^T (of tall matrices: X := a X + X (b G + c G^2), G = X^T X, the same
+// by the shorter side).  Each step is three products: G and G^2 are symmetric, of them the lower triangle is computed and written to both places.
+//
+// Operands are fp16: with bf16's eight bits the result was off by 1 % of its norm (normal 576 x 1536 matrices) and by 10 % and more where few directions dominate,
+// since a step takes small singular values times a = 3.4 and the rounding errors next to them too.  X is carried as two fp16 numbers (hi + lo / 2^11, 22 bits): hi is
+// the operand, a X takes both, so that what is rounded away in one step is there in the next.  Off by 0.15 % for normal matrices, 0.03 % for few directions.
+// Everything is held times ORTH_UNIT: singular values stay below two, entries far below one.
+constexpr float ORTH_UNIT = 256.f, ORTH_LO = 2048.f;
+constexpr int ORTH_ROUND = 128, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
+constexpr int ORTH_THREADS = 256, ORTH_WARPS = ORTH_THREADS / 32;
+
+struct Sources {
+    const void *update[ORTH_ROUND];   // null: table[index]
+    const void *grad[ORTH_ROUND];     // null: none
+    int index[ORTH_ROUND];
+    int shape[ORTH_ROUND];
+    int number[ORTH_ROUND];           // of those of its shape
+    struct {
+        int rows, cols, ld, block_rows;
+        __half *hi, *lo;              // of the shape's first matrix
+    } shapes[ORTH_SHAPES];
+    float *const *table;
+    double *partial;                  // [matrices][most]
+    int most;
+    float beta, eps;
+};
+
+// The elements that a block of a matrix takes, as fp32: f(row, column, values) for N columns at a time, N = 4 where all rows begin on boundaries of 4 elements.
+template <typename UT, typename GT, typename F>
+__device__ __forceinline__ void visit_rows(const Sources &s, int which, const F &f) {
+    const auto &sh = s.shapes[s.shape[which]];
+    const int row0 = blockIdx.x * sh.block_rows, row1 = min(row0 + sh.block_rows, sh.rows);
+    const UT *u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]);
+    const GT *g = static_cast<const GT *>(s.grad[which]);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cols = sh.cols;
+    const float beta = s.beta, rest = 1.f - s.beta;
+    const auto go = [&](auto width) {
+        constexpr int N = decltype(width)::value;
+        for (int r = row0 + warp; r < row1; r += ORTH_WARPS) {
+            const long long at = static_cast<long long>(r) * cols;
+#pragma unroll 4
+            for (int c = lane * N; c < cols; c += 32 * N) {
+                float v[N];
+                load_values(u + at + c, v);
+                if (g) {
+                    float w[N];
+                    load_values(g + at + c, w);
+#pragma unroll
+                    for (int e = 0; e < N; ++e) v[e] = beta * v[e] + rest * w[e];
+                }
+                f(r, c, v);
+            }
+        }
+    };
+    const uintptr_t low = (reinterpret_cast<uintptr_t>(u) & (4 * sizeof(UT) - 1)) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(GT) - 1));
+    if (cols % 4 == 0 && low == 0) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
+}
+
+__device__ __forceinline__ double block_sum(double v) {
+    __shared__ double sums[ORTH_WARPS];
+#pragma unroll
+    for (int d = 16; d; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0;
+#pragma unroll
+    for (int w = 0; w < ORTH_WARPS; ++w) v += sums[w];
+    return v;
+}
+
+// Squares of a block's rows, summed in fp64 (fp32's range ends at values of 1e19).  Bound: HBM, each element read once.
+template <typename UT, typename GT>
+__global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_constant__ Sources s) {
+    begin_and_let_next_begin();
+    wait_for_earlier_kernels();
+    const auto &sh = s.shapes[s.shape[blockIdx.y]];
+    if (static_cast<int>(blockIdx.x) * sh.block_rows >= sh.rows) return;
+    double sum = 0;
+    visit_rows<UT, GT>(s, blockIdx.y, [&](int, int, const auto &v) {
+        double part = 0;
+        for (float x : v) part += static_cast<double>(x) * x;
+        sum += part;
+    });
+    sum = block_sum(sum);
+    if (threadIdx.x == 0) s.partial[static_cast<long long>(blockIdx.y) * s.most + blockIdx.x] = sum;
+}
+
+// X in two halves.  Bound: L2 or HBM, each element read again and four bytes written.
+template <typename UT, typename GT>
+__global__ void __launch_bounds__(ORTH_THREADS) orth_scale_kernel(const __grid_constant__ Sources s) {
+    begin_and_let_next_begin();
+    wait_for_earlier_kernels();
+    const int which = blockIdx.y;
+    const auto &sh = s.shapes[s.shape[which]];
+    if (static_cast<int>(blockIdx.x) * sh.block_rows >= sh.rows) return;
+    const int parts = (sh.rows + sh.block_rows - 1) / sh.block_rows;
+    double sum = 0;
+    for (int i = threadIdx.x; i < parts; i += ORTH_THREADS) sum += s.partial[static_cast<long long>(which) * s.most + i];
+    const float factor = static_cast<float>(static_cast<double>(ORTH_UNIT) / (sqrt(block_sum(sum)) + static_cast<double>(s.eps)));
+    const long long first = static_cast<long long>(s.number[which]) * sh.rows * sh.ld;
+    __half *const hi = sh.hi + first, *const lo = sh.lo + first;
+    visit_rows<UT, GT>(s, which, [&](int r, int c, const auto &v) {
+        constexpr int N = sizeof(v) / sizeof(float);
+        const long long at = static_cast<long long>(r) * sh.ld + c;
+        __half h[N], l[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float x = v[e] * factor;
+            h[e] = __float2half_rn(x);
+            l[e] = __float2half_rn((x - __half2float(h[e])) * ORTH_LO);
+        }
+        if constexpr (N == 4) {
+            *reinterpret_cast<uint2 *>(hi + at) = *reinterpret_cast<const uint2 *>(h);
+            *reinterpret_cast<uint2 *>(lo + at) = *reinterpret_cast<const uint2 *>(l);
+        } else {
+            hi[at] = h[0], lo[at] = l[0];
+        }
+    });
+}
+
+// ---- the products' epilogues -------------------------------------------------------------------------
+// A symmetric result: alpha times the sums, plus beta times in[0]; of the pieces below the diagonal the other one's place, too.
+struct SymArgs {
+    float c, b;
+};
+struct SymEpilogue {
+    float b;
+    __device__ static void piece(const GemmArgs<SymEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
+        if (p.rows <= 0 || p.cols <= 0 || col0 > row0) return;
+        __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
+        const long long at = row0 * g.out_ld + col0;
+        float v[32];
+        uint32_t w[16];
+        if (g.in[0]) load_piece16(st, lane, static_cast<const __half *>(g.in[0]) + batch * g.out_batch + at, g.out_ld, p, w);
+        tmem_load32(d, v);
+        tmem_wait();
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] *= g.alpha;
+        if (g.in[0]) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const float2 x = unpack_f16(w[e]);
+                v[2 * e] += a.epi.b * x.x, v[2 * e + 1] += a.epi.b * x.y;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 16; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+        store_piece16(st, lane, out + at, g.out_ld, p, w);
+        if (col0 < row0 && lane < p.rows) {   // (columns of the one are rows of the other: p.cols is 32 here)
+            __half *const t = out + col0 * g.out_ld + row0 + lane;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) t[e * g.out_ld] = __float2half_rn(v[e]);
+        }
+    }
+};
+
+// hi + lo / 2^11, times a, plus alpha times the sums.
+__device__ __forceinline__ void carried(char *st, int lane, const GemmGroup &g, long long at, const Piece &p, float a, uint32_t d, float (&v)[32]) {
+    uint32_t hi[16], lo[16];
+    load_piece16(st, lane, static_cast<const __half *>(g.in[0]) + at, g.in_ld, p, hi);
+    load_piece16(st, lane, static_cast<const __half *>(g.in[1]) + at, g.in_ld, p, lo);
+    tmem_load32(d, v);
+    tmem_wait();
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const float2 h = unpack_f16(hi[e]), l = unpack_f16(lo[e]);
+        v[2 * e] = v[2 * e] * g.alpha + a * (h.x + l.x * (1.f / ORTH_LO));
+        v[2 * e + 1] = v[2 * e + 1] * g.alpha + a * (h.y + l.y * (1.f / ORTH_LO));
+    }
+}
+
+// X of the next step, in two halves.
+struct NextEpilogue {
+    float a;
+    __device__ static void piece(const GemmArgs<NextEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
+        if (p.rows <= 0 || p.cols <= 0) return;
+        const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
+        float v[32];
+        carried(st, lane, g, at, p, a.epi.a, d, v);
+        uint32_t hi[16], lo[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+            const float2 h = unpack_f16(hi[e]);
+            lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
+        }
+        store_piece16(st, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p, hi);
+        store_piece16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p, lo);
+    }
+};
+
+// What the last step gives: to a tensor of the caller's, or into the step of x.
+enum { ORTH_TO_F32 = 0, ORTH_TO_BF16 = 1, ORTH_TO_X = 2 };
+template <int TO>
+struct LastEpilogue {
+    float a, scale[ORTH_SHAPES];      // of the shape: with 1 / ORTH_UNIT; of the step with the learning rate
+    float decay;
+    void *out[ORTH_ROUND];
+    float *const *table;
+    int index[ORTH_ROUND];
+    __device__ static void piece(const GemmArgs<LastEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
+        if (p.rows <= 0 || p.cols <= 0) return;
+        float v[32];
+        carried(st, lane, g, batch * g.in_batch + row0 * g.in_ld + col0, p, a.epi.a, d, v);
+        const float scale = a.epi.scale[&g - a.groups];
+        const int which = g.first + batch;
+        const long long at = row0 * g.out_ld + col0;
+        p.wide = false;
+        if constexpr (TO == ORTH_TO_BF16) {
+            __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(a.epi.out[which]);
+            p.wide = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * 2)) & 15) == 0;
+            uint32_t w[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e] * scale, v[2 * e + 1] * scale);
+            store_piece16(st, lane, out + at, g.out_ld, p, w);
+        } else {
+            float *const out = TO == ORTH_TO_X ? a.epi.table[a.epi.index[which]] : static_cast<float *>(a.epi.out[which]);
+            p.wide = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * 4)) & 15) == 0;
+            if constexpr (TO == ORTH_TO_X) {
+                float x[32];
+                load_piece32(st, lane, out + at, g.out_ld, p, x);
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] = a.epi.decay * x[e] - scale * v[e];
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] *= scale;
+            }
+            store_piece32(st, lane, out + at, g.out_ld, p, v);
+        }
+    }
+};
+
+// ---- rounds ------------------------------------------------------------------------------------------
+int64_t padded(int64_t n) { return (n + 7) & ~int64_t{7}; }
+
+struct Shape {
+    int rows, cols, count, first;     // matrices [first, first + count) of the round
+    int n, m;                         // the shorter and the longer side
+    bool tall;
+    int64_t ld, square_ld;
+    __half *hi[2], *lo, *gram, *poly;
+};
+struct Round {
+    int first, count;                 // of the sorted list
+    int nshapes;
+    Shape shapes[ORTH_SHAPES];
+    int64_t bytes;
+};
+int64_t matrix_bytes(int rows, int cols) {
+    const int64_t n = std::min(rows, cols);
+    return 6 * rows * padded(cols) + 4 * n * padded(n);
+}
+int block_rows(int cols) { return std::max(ORTH_WARPS, (16384 / std::max(cols, 1)) / ORTH_WARPS * ORTH_WARPS); }
+
+// The matrices from `first` on that are taken at once: as many as L2 holds, or as many as give every SM some tiles.
+constexpr int64_t ORTH_ROUND_BYTES = 80ll << 20;
+constexpr int ORTH_ROUND_TILES = 4 * NUM_SMS;
+Round next_round(const OrthArgs &a, int first) {
+    Round r{};
+    r.first = first;
+    int64_t tiles = 0;
+    while (first + r.count < a.count && r.count < ORTH_ROUND) {
+        const OrthMatrix &x = a.list[first + r.count];
+        const int64_t bytes = matrix_bytes(x.rows, x.cols);
+        const int n = std::min(x.rows, x.cols);
+        if (r.count > 0 && r.bytes + bytes > ORTH_ROUND_BYTES && tiles >= ORTH_ROUND_TILES) break;
+        if (r.nshapes == 0 || r.shapes[r.nshapes - 1].rows != x.rows || r.shapes[r.nshapes - 1].cols != x.cols) {
+            if (r.nshapes == ORTH_SHAPES) break;
+            Shape &s = r.shapes[r.nshapes++];
+            s.rows = x.rows, s.cols = x.cols, s.count = 0, s.first = r.count;
+            s.n = n, s.m = std::max(x.rows, x.cols), s.tall = x.rows > x.cols;
+            s.ld = padded(x.cols), s.square_ld = padded(n);
+        }
+        ++r.shapes[r.nshapes - 1].count;
+        ++r.count;
+        r.bytes += bytes;
+        tiles += tiles_of(n, n, 256, true);
+    }
+    return r;
+}
+// Places everything of a round in working memory; its end.
+int64_t place(Round &r, char *work, double **partial, int *most) {
+    int64_t used = 0;
+    const auto take = [&](int64_t bytes) {
+        char *p = work ? work + used : nullptr;
+        used += (bytes + 255) & ~int64_t{255};
+        return p;
+    };
+    int blocks = 1;
+    for (int i = 0; i < r.nshapes; ++i) {
+        Shape &s = r.shapes[i];
+        const int64_t x = s.count * s.rows * s.ld * 2, g = s.count * s.n * s.square_ld * 2;
+        for (__half **p : {&s.hi[0], &s.hi[1], &s.lo}) *p = reinterpret_cast<__half *>(take(x));
+        s.gram = reinterpret_cast<__half *>(take(g)), s.poly = reinterpret_cast<__half *>(take(g));
+        blocks = std::max(blocks, (s.rows + block_rows(s.cols) - 1) / block_rows(s.cols));
+    }
+    double *const p = reinterpret_cast<double *>(take(static_cast<int64_t>(r.count) * blocks * 8));
+    if (partial) *partial = p, *most = blocks;
+    return used;
+}
+
+void sort_list(const OrthArgs &a) {
+    std::sort(a.list, a.list + a.count, [](const OrthMatrix &x, const OrthMatrix &y) {
+        return x.rows != y.rows ? x.rows < y.rows : x.cols != y.cols ? x.cols < y.cols : x.index < y.index;
+    });
+}
+
+template <typename F>
+int pick_tile_n(const Round &r, const F &tiles) {
+    int best = 0;
+    int64_t least = 0;
+    for (int n = 256; n >= 64; n /= 2) {
+        int64_t all = 0;
+        for (int i = 0; i < r.nshapes; ++i) all += static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], n);
+        const int64_t cost = (all + NUM_SMS - 1) / NUM_SMS * (n + 64);
+        if (!best || cost < least) best = n, least = cost;
+    }
+    return best;
+}
+
+struct Run {
+    cudaStream_t stream;
+    int *err, wait_limit, *launches;
+};
+
+// A symmetric product of `from` (x: X of this step, else G) for all shapes.
+cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b, const Run &run) {
+    static thread_local GemmArgs<SymEpilogue> a;
+    const int tile = pick_tile_n(r, [](const Shape &s, int t) { return tiles_of(s.n, s.n, t, true); });
+    begin_gemm(a, false, tile, false, true, 1);
+    a.epi.b = b;
+    for (int i = 0; i < r.nshapes; ++i) {
+        const Shape &s = r.shapes[i];
+        const bool mn = gram && s.tall;
+        GemmGroup &g = add_group(a, s.n, s.n, gram ? s.m : s.n, s.count);
+        for (int side_b = 0; side_b < 2; ++side_b) {
+            const int box = mn ? 64 : side_b ? tile : GEMM_BM;
+            const cudaError_t e = gram ? encode_boxes(&a.maps[2 * i + side_b], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, box)
+                                       : encode_boxes(&a.maps[2 * i + side_b], s.gram, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, box);
+            if (e != cudaSuccess) return e;
+        }
+        g.a_map = static_cast<short>(2 * i), g.b_map = static_cast<short>(2 * i + 1);
+        g.a_mn = g.b_mn = mn;
+        g.alpha = alpha;
+        g.out[0] = gram ? s.gram : s.poly;
+        g.in[0] = gram ? nullptr : s.gram;
+        g.out_ld = s.square_ld, g.out_batch = s.n * s.square_ld;
+    }
+    return launch_gemm(a, run.err, run.wait_limit, run.stream, run.launches);
+}
+
+// X := a X + (polynomial of G) X, to the other side or, at last, to `epi`'s places.
+template <typename E>
+cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const long long *out_ld, const Run &run) {
+    const int tile = pick_tile_n(r, [](const Shape &s, int t) { return tiles_of(s.rows, s.cols, t, false); });
+    begin_gemm(a, false, tile, false, false, 1);
+    a.epi = epi;
+    for (int i = 0; i < r.nshapes; ++i) {
+        const Shape &s = r.shapes[i];
+        GemmGroup &g = add_group(a, s.rows, s.cols, s.n, s.count);
+        const int of_x = 2 * i + (s.tall ? 0 : 1), of_poly = 2 * i + (s.tall ? 1 : 0);
+        cudaError_t e = encode_boxes(&a.maps[of_x], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, s.tall ? GEMM_BM : 64);
+        if (e == cudaSuccess)
+            e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? tile : GEMM_BM);
+        if (e != cudaSuccess) return e;
+        g.a_map = static_cast<short>(2 * i), g.b_map = static_cast<short>(2 * i + 1);
+        g.b_mn = !s.tall;
+        g.alpha = 1.f / ORTH_UNIT;
+        g.in[0] = s.hi[side], g.in[1] = s.lo;
+        g.in_ld = s.ld, g.in_batch = s.rows * s.ld;
+        g.out[0] = s.hi[side ^ 1], g.out[1] = s.lo;
+        g.out_ld = out_ld ? out_ld[i] : s.ld;
+        g.first = s.first;
+    }
+    return launch_gemm(a, run.err, run.wait_limit, run.stream, run.launches);
+}
+
+template <int TO>
+cudaError_t last(const OrthArgs &a, const Round &r, int side, const Run &run) {
+    using E = LastEpilogue<TO>;
+    static thread_local GemmArgs<E> args;
+    static thread_local E epi;
+    epi.a = a.coefficients[3 * (a.steps - 1)];
+    epi.decay = a.decay;
+    epi.table = a.x_table;
+    long long ld[ORTH_SHAPES];
+    for (int i = 0; i < r.nshapes; ++i) {
+        const Shape &s = r.shapes[i];
+        const double longer = std::max(s.rows, s.cols);
+        const double scale = a.scale == DESLOC_SCALE_ASPECT ? std::sqrt(std::max(1.0, static_cast<double>(s.rows) / s.cols))
+                             : a.scale == DESLOC_SCALE_RMS  ? 0.2 * std::sqrt(longer)
+                                                            : 1.0;
+        epi.scale[i] = static_cast<float>(scale * (TO == ORTH_TO_X ? a.lr : 1.0) / ORTH_UNIT);
+        ld[i] = s.cols;
+    }
+    for (int i = 0; i < r.count; ++i) epi.out[i] = a.list[r.first + i].out, epi.index[i] = a.list[r.first + i].index;
+    return update(r, side, epi, args, ld, run);
+}
+
+template <typename UT, typename GT>
+cudaError_t prepare(const Sources &s, int count, const Run &run) {
+    const dim3 grid(s.most, count);
+    cudaError_t e = launch_op(orth_norm_kernel<UT, GT>, grid, dim3(ORTH_THREADS), 0, true, run.stream, s);
+    if (e == cudaSuccess) ++*run.launches, e = launch_op(orth_scale_kernel<UT, GT>, grid, dim3(ORTH_THREADS), 0, true, run.stream, s);
+    if (e == cudaSuccess) ++*run.launches;
+    return e;
+}
+
+}  // namespace
+
+int64_t orth_work(const OrthArgs &a) {
+    sort_list(a);
+    int64_t most = 0;
+    for (int at = 0; at < a.count;) {
+        Round r = next_round(a, at);
+        most = std::max(most, place(r, nullptr, nullptr, nullptr));
+        at += r.count;
+    }
+    return most;
+}
+
+cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
+    const Run run{stream, err, wait_limit, launches};
+    sort_list(a);
+    static thread_local Sources s;
+    static thread_local GemmArgs<NextEpilogue> next;
+    for (int at = 0; at < a.count;) {
+        Round r = next_round(a, at);
+        place(r, work, &s.partial, &s.most);
+        s.table = a.u_table, s.beta = a.beta, s.eps = a.eps;
+        for (int i = 0; i < r.nshapes; ++i) {
+            const Shape &sh = r.shapes[i];
+            s.shapes[i] = {sh.rows, sh.cols, static_cast<int>(sh.ld), block_rows(sh.cols), sh.hi[0], sh.lo};
+            for (int k = 0; k < sh.count; ++k) {
+                const OrthMatrix &x = a.list[at + sh.first + k];
+                s.update[sh.first + k] = x.update, s.grad[sh.first + k] = x.grad, s.index[sh.first + k] = x.index;
+                s.shape[sh.first + k] = i, s.number[sh.first + k] = k;
+            }
+        }
+        using bf = __nv_bfloat16;
+        cudaError_t e = a.update_bf16 ? (a.grad_bf16 ? prepare<bf, bf> : prepare<bf, float>)(s, r.count, run)
+                                      : (a.grad_bf16 ? prepare<float, bf> : prepare<float, float>)(s, r.count, run);
+        int side = 0;
+        for (int k = 0; k < a.steps && e == cudaSuccess; ++k, side ^= 1) {
+            const float *c = a.coefficients + 3 * k;
+            e = symmetric(r, true, side, 1.f / ORTH_UNIT, 0.f, run);
+            if (e == cudaSuccess) e = symmetric(r, false, side, c[2] / ORTH_UNIT, c[1], run);
+            if (e != cudaSuccess) break;
+            if (k + 1 < a.steps) e = update(r, side, NextEpilogue{c[0]}, next, nullptr, run);
+            else if (a.list[at].out == nullptr) e = last<ORTH_TO_X>(a, r, side, run);
+            else e = a.out_bf16 ? last<ORTH_TO_BF16>(a, r, side, run) : last<ORTH_TO_F32>(a, r, side, run);
+        }
+        if (e != cudaSuccess) return e;
+        at += r.count;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace desloc

@@ -328,6 +328,159 @@ class DesLoc:
                                written._keep if isinstance(written, BoundGrads) else written)
         return r if type(r) is not int else self._raise(r, "desloc_clip_grads")
 
+    # ---- products of the workers' matrices
+    def _addresses(self, nested, tensors, kind: int, misfit: str) -> ctypes.Array:
+        """Array of addresses as desloc_step() takes them, of the tensors `tensors` alone, checked."""
+        nt = len(self.numel)
+        if isinstance(nested, BoundGrads):
+            if kind != self.grad_dtype:
+                raise ValueError(misfit)
+            self._bound(nested)
+            return nested.array
+        if len(nested) != self.M:
+            raise ValueError("need one list of tensors per worker")
+        array, want = (ctypes.c_void_p * (self.M * nt))(), _TORCH_TYPES[kind]
+        for m, row in enumerate(nested):
+            if len(row) != nt:
+                raise ValueError("every worker needs the same tensor list")
+            for k in tensors:
+                t = row[k]
+                if t.dtype != want or t.numel() != self.numel[k] or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError(misfit)
+                array[m * nt + k] = t.data_ptr()
+        return array
+
+    def _kind(self, nested, tensors, misfit: str) -> int:
+        """Type code of a set of tensors of one type."""
+        if isinstance(nested, BoundGrads):
+            return self.grad_dtype
+        kind = _TYPES.get(nested[0][tensors[0]].dtype) if len(nested) else None
+        if kind is None:
+            raise ValueError(misfit)
+        return kind
+
+    def _numbers(self, tensors):
+        tensors = [int(k) for k in tensors]
+        if any(not 0 <= k < len(self.numel) for k in tensors) or len(set(tensors)) != len(tensors):
+            raise ValueError("tensors are numbers of this context's tensors, no two alike")
+        return tensors
+
+    def _activations(self, what: str, t: torch.Tensor, shape=None) -> tuple:
+        """(rows, tensor) of bf16 activations [M, ..., width]; copies what does not lie in rows."""
+        if t.dtype != torch.bfloat16 or t.dim() < 2 or t.shape[0] != self.M or (shape is not None and tuple(t.shape) != shape):
+            raise ValueError(f"{what} is bf16, [workers, ..., width]" + (f", {tuple(shape)} here" if shape is not None else ""))
+        _on(self.device, what, t)
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            t = t.contiguous()
+        inner = _merged(t.shape[1:-1], t.stride()[1:-1])
+        if inner is None:
+            t = t.contiguous()
+            inner = _merged(t.shape[1:-1], t.stride()[1:-1])
+        return B.rows(t.data_ptr(), B.DESLOC_BF16, t.stride(0), inner), t
+
+    def _result(self, what: str, out: Optional[torch.Tensor], shape) -> tuple:
+        """The same of activations that are written: a new tensor, or the caller's."""
+        if out is None:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=self.device)
+        elif tuple(out.shape) != shape or out.dtype != torch.bfloat16 or out.device != self.device:
+            raise ValueError(f"{what} does not fit")
+        inner = _merged(out.shape[1:-1], out.stride()[1:-1])
+        if inner is None or (out.stride(-1) != 1 and out.shape[-1] > 1):
+            raise ValueError(f"{what} has rows that the kernels do not reach: more than two strides")
+        return B.rows(out.data_ptr(), B.DESLOC_BF16, out.stride(0), inner), out
+
+    def _ffn(self, tensors, h: torch.Tensor, weights):
+        gate, up, down = tensors = self._numbers(tensors)
+        rows, h = self._activations("h", h)
+        width = int(h.shape[-1])
+        tokens = h.numel() // (self.M * width) if width else 0
+        if width < 1 or self.numel[gate] % width or any(self.numel[k] != self.numel[gate] for k in tensors):
+            raise ValueError("gate and up are [hidden, width], down is [width, hidden]")
+        hidden = self.numel[gate] // width
+        array = self._addresses(weights, tensors, B.DESLOC_BF16, "weights are bf16 copies of x: wrong dtype, size or layout")
+        return B.ffn(gate, up, down, width, hidden, tokens, array, rows), h, hidden
+
+    def gated_ffn(self, tensors, h: torch.Tensor, weights, keep: bool = False, out: Optional[torch.Tensor] = None):
+        """The gated feed-forward block down(silu(gate h) * (up h)) of every worker with its own weights, on torch's current stream.  tensors: numbers of gate,
+        up ([hidden, width]) and down ([width, hidden]); h: bf16 [M, ..., width]; weights: nested lists like x of bf16 copies, of which only those three are looked at.
+        Returns y like h, or with keep (y, (gate h, up h)) for gated_ffn_grad()."""
+        f, h, hidden = self._ffn(tensors, h, weights)
+        to, out = self._result("out", out, tuple(h.shape))
+        kept = tuple(torch.empty(tuple(h.shape[:-1]) + (hidden,), dtype=torch.bfloat16, device=self.device) for _ in range(2)) if keep else None
+        work = torch.empty(B.desloc_gated_ffn_bytes(self.ctx, f), dtype=torch.uint8, device=self.device)
+        B.desloc_gated_ffn(self.ctx, f, kept[0].data_ptr() if keep else 0, kept[1].data_ptr() if keep else 0, to, work.data_ptr(), work.numel(),
+                           torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote(out)
+        return (out, kept) if keep else out
+
+    def gated_ffn_grad(self, tensors, h: torch.Tensor, kept, dy: torch.Tensor, weights, grads, accumulate: bool = False,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """The way back of gated_ffn(): returns dh (into `out` where it is given) and writes the three weights' gradients into the workers' gradients in `grads` (what
+        step() reads, or bind_grads()' handle); accumulate: added to what they hold.  kept: what gated_ffn(keep=True) returned beside y."""
+        f, h, hidden = self._ffn(tensors, h, weights)
+        tensors = (f.gate, f.up, f.down)
+        shape = tuple(h.shape[:-1]) + (hidden,)
+        for t in kept:
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                raise ValueError("kept is the pair that gated_ffn(keep=True) returned for this h")
+        rows, dy = self._activations("dy", dy, tuple(h.shape))
+        to, out = self._result("out", out, tuple(h.shape))
+        array = self._addresses(grads, tensors, self.grad_dtype, _GRAD_MISFIT)
+        work = torch.empty(B.desloc_gated_ffn_grad_bytes(self.ctx, f, rows), dtype=torch.uint8, device=self.device)
+        B.desloc_gated_ffn_grad(self.ctx, f, kept[0].data_ptr(), kept[1].data_ptr(), rows, to, accumulate, array, work.data_ptr(), work.numel(),
+                                torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote(out)
+        _native.wrote([row[k] for row in (grads._keep if isinstance(grads, BoundGrads) else grads) for k in tensors])
+        return out
+
+    def _orthogonal(self, tensors, updates, grads, columns, steps, coefficients, eps, scale):
+        tensors = self._numbers(tensors)
+        if columns is None:
+            columns = [self._rows_of(k, None) for k in tensors]
+        codes = {"none": B.DESLOC_SCALE_NONE, "aspect": B.DESLOC_SCALE_ASPECT, "rms": B.DESLOC_SCALE_RMS}
+        if scale not in codes:
+            raise ValueError('scale is "none", "aspect" or "rms"')
+        if coefficients is not None:
+            coefficients = [float(v) for triple in coefficients for v in triple]
+            steps = len(coefficients) // 3
+        kind, misfit = B.DESLOC_F32, "update tensor of wrong dtype, size or layout"
+        if updates is not None and tensors:
+            kind = self._kind(updates, tensors, misfit)
+            updates = self._addresses(updates, tensors, kind, misfit)
+        if grads is not None and tensors:
+            grads = self._addresses(grads, tensors, self.grad_dtype, _GRAD_MISFIT)
+        return tensors, B.orthogonal(tensors, columns, steps, coefficients, eps, codes[scale], kind, updates if tensors else None, grads if tensors else None)
+
+    def orthogonalize(self, tensors, updates, grads=None, out=None, columns=None, steps: int = 5, coefficients=None, eps: float = 1e-7,
+                      scale: str = "none") -> None:
+        """Every worker's matrices `tensors` (numbers) of `updates` (nested lists like x, fp32 or bf16; None: the momentum u) brought to singular values near 1 by `steps`
+        Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad.  columns: of each matrix,
+        where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones.  scale: "none", "aspect"
+        (sqrt(max(1, rows / columns))) or "rms" (0.2 sqrt(max(rows, columns)))."""
+        tensors, how = self._orthogonal(tensors, updates, grads, columns, steps, coefficients, eps, scale)
+        if not tensors:
+            return
+        written = updates if out is None else out
+        if written is None:
+            written = self._keep[1]
+        misfit = "out tensor of wrong dtype, size or layout"
+        kind = self._kind(written, tensors, misfit)
+        work = torch.empty(B.desloc_orthogonal_bytes(self.ctx, how), dtype=torch.uint8, device=self.device)
+        B.desloc_orthogonalize(self.ctx, how, kind, self._addresses(written, tensors, kind, misfit), work.data_ptr(), work.numel(),
+                               torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote([row[k] for row in (written._keep if isinstance(written, BoundGrads) else written) for k in tensors])
+
+    def orthogonal_step(self, tensors, lr: float, updates=None, grads=None, columns=None, steps: int = 5, coefficients=None, eps: float = 1e-7,
+                        scale: str = "aspect") -> None:
+        """x of the matrices `tensors` := x (1 - lr weight_decay) - lr * orthogonalize(updates; the momentum u where None).  Behind step(t, 0.0, grads) of an SGDM
+        context, which brings the momentum and the averages of this step, it is the step of the orthogonalised momentum; grads: its look-ahead."""
+        tensors, how = self._orthogonal(tensors, updates, grads, columns, steps, coefficients, eps, scale)
+        if not tensors:
+            return
+        work = torch.empty(B.desloc_orthogonal_bytes(self.ctx, how), dtype=torch.uint8, device=self.device)
+        B.desloc_orthogonal_step(self.ctx, how, lr, work.data_ptr(), work.numel(), torch.cuda.current_stream(self.device).cuda_stream)
+        _native.wrote([row[k] for row in self._keep[0] for k in tensors])
+
     def set_workers(self, x, u, v, first_new: int) -> None:
         """New worker set (lists like the constructor's); workers first_new.. start from the mean
         of the current workers.  Synchronises the current stream."""
