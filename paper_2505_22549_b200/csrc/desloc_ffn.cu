@@ -2,65 +2,83 @@
 #include "desloc_blocks.cuh"
 #include "desloc_gemm.cuh"
 
+#include <type_traits>
+
 namespace desloc {
 
 namespace {
 
 __device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
 
-__device__ __forceinline__ bool piece_of(const GemmGroup &g, int row0, int col0, bool wide, Piece &p) {
-    p.rows = min(32, g.m - row0), p.cols = min(32, g.n - col0), p.wide = wide;
-    return p.rows > 0 && p.cols > 0;
-}
-template <typename T>
-__device__ __forceinline__ T *at(T *p, long long elements) { return p + elements; }
-
-struct NoArgs {};
-
 // ---- forward -----------------------------------------------------------------------------------------
 // z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.
 struct UpEpilogue {
-    __device__ static void piece(const GemmArgs<UpEpilogue> &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        Piece p;
-        if (!piece_of(g, row0, col0, g.wide & 1, p)) return;
+    struct Ahead {};
+    using Args = GemmArgs<UpEpilogue>;
+    __device__ static void fetch(const Args &, const GemmGroup &, int, int, int, int, Ahead &) {}
+    __device__ static void settle(char *, int, const Ahead &) {}
+    __device__ static void finish(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1), q = piece_at(g, row0, col0, (g.wide & 2) != 0);
+        if (p.none()) return;
         float gv[32], uv[32];
         tmem_load32(d, gv);
         tmem_load32(d + a.tile_n / 2, uv);
         tmem_wait();
         uint32_t w[16];
-        const long long kept = row0 * g.in_ld + col0;
         if (g.out[1]) {
-            const Piece q{p.rows, p.cols, (g.wide & 2) != 0};
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
-            store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + kept, g.in_ld, q, w);
+            put16(st + 2048, lane, w);
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(uv[2 * e], uv[2 * e + 1]);
-            store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + kept, g.in_ld, q, w);
+            put16(st + 4096, lane, w);
         }
 #pragma unroll
         for (int e = 0; e < 32; ++e) gv[e] = gv[e] * sigmoid(gv[e]) * uv[e];
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
-        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p, w);
+        put16(st, lane, w);
+        __syncwarp();
+        send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p);
+        if (g.out[1]) {
+            const long long kept = row0 * g.in_ld + col0;
+            send16(st + 2048, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + kept, g.in_ld, q);
+            send16(st + 4096, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + kept, g.in_ld, q);
+        }
     }
 };
 
 // A product as it is, in bf16 or fp32, or added to what is there.
 template <bool BF16, bool ADD>
 struct StoreEpilogue {
-    __device__ static void piece(const GemmArgs<StoreEpilogue> &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        Piece p;
-        if (!piece_of(g, row0, col0, g.wide & 1, p)) return;
+    struct Was {
+        uint4 v[BF16 ? 4 : 8];
+    };
+    struct Nothing {};
+    using Ahead = std::conditional_t<ADD, Was, Nothing>;
+    using Args = GemmArgs<StoreEpilogue>;
+    __device__ static void fetch(const Args &, const GemmGroup &g, int, int row0, int col0, int lane, Ahead &x) {
+        if constexpr (ADD) {
+            const Piece p = piece_at(g, row0, col0, g.wide & 1);
+            if constexpr (BF16) fetch16(static_cast<const __nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p, lane, x.v);
+            else fetch32(static_cast<const float *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p, lane, x.v);
+        }
+    }
+    __device__ static void settle(char *st, int lane, const Ahead &x) {
+        if constexpr (ADD && BF16) settle16(st, lane, x.v);
+        else if constexpr (ADD) settle32(st, lane, x.v);
+    }
+    __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1);
+        if (p.none()) return;
         float v[32];
         tmem_load32(d, v);
         tmem_wait();
         const long long to = row0 * g.out_ld + col0;
         if constexpr (BF16) {
-            __nv_bfloat16 *out = static_cast<__nv_bfloat16 *>(g.out[0]) + to;
             uint32_t w[16];
             if constexpr (ADD) {
-                load_piece16(st, lane, out, g.out_ld, p, w);
+                row16(st, lane, w);
 #pragma unroll
                 for (int e = 0; e < 16; ++e) {
                     const float2 was = unpack_bf16(w[e]);
@@ -69,16 +87,19 @@ struct StoreEpilogue {
             }
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            store_piece16(st, lane, out, g.out_ld, p, w);
+            put16(st, lane, w);
+            __syncwarp();
+            send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
         } else {
-            float *out = static_cast<float *>(g.out[0]) + to;
             if constexpr (ADD) {
                 float was[32];
-                load_piece32(st, lane, out, g.out_ld, p, was);
+                row32(st, lane, was);
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] += was[e];
             }
-            store_piece32(st, lane, out, g.out_ld, p, v);
+            put32(st, lane, v);
+            __syncwarp();
+            send32(st, lane, static_cast<float *>(g.out[0]) + to, g.out_ld, p);
         }
     }
 };
@@ -86,13 +107,26 @@ struct StoreEpilogue {
 // ---- backward ----------------------------------------------------------------------------------------
 // From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.
 struct DzEpilogue {
-    __device__ static void piece(const GemmArgs<DzEpilogue> &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        Piece p;
-        if (!piece_of(g, row0, col0, (g.wide & 2) != 0, p)) return;
+    struct Ahead {
+        uint4 g[4], u[4];
+    };
+    using Args = GemmArgs<DzEpilogue>;
+    __device__ static void fetch(const Args &, const GemmGroup &g, int, int row0, int col0, int lane, Ahead &x) {
+        const Piece p = piece_at(g, row0, col0, (g.wide & 2) != 0);
+        const long long from = row0 * g.in_ld + col0;
+        fetch16(static_cast<const __nv_bfloat16 *>(g.in[0]) + from, g.in_ld, p, lane, x.g);
+        fetch16(static_cast<const __nv_bfloat16 *>(g.in[1]) + from, g.in_ld, p, lane, x.u);
+    }
+    __device__ static void settle(char *st, int lane, const Ahead &x) {
+        settle16(st, lane, x.g);
+        settle16(st + 2048, lane, x.u);
+    }
+    __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1);
+        if (p.none()) return;
         uint32_t gw[16], uw[16], zw[16];
-        const long long from = row0 * g.in_ld + col0, to = row0 * g.out_ld + col0;
-        load_piece16(st, lane, static_cast<const __nv_bfloat16 *>(g.in[0]) + from, g.in_ld, p, gw);
-        load_piece16(st, lane, static_cast<const __nv_bfloat16 *>(g.in[1]) + from, g.in_ld, p, uw);
+        row16(st, lane, gw);
+        row16(st + 2048, lane, uw);
         float v[32];
         tmem_load32(d, v);
         tmem_wait();
@@ -104,10 +138,14 @@ struct DzEpilogue {
             gw[e] = pack_bf16(v[2 * e] * uu.x * (sx + ax * (1.f - sx)), v[2 * e + 1] * uu.y * (sy + ay * (1.f - sy)));
             uw[e] = pack_bf16(v[2 * e] * ax, v[2 * e + 1] * ay);
         }
-        p.wide = g.wide & 1;
-        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p, zw);
-        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + to, g.out_ld, p, gw);
-        store_piece16(st, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + to, g.out_ld, p, uw);
+        put16(st, lane, gw);   // (each lane where it has read)
+        put16(st + 2048, lane, uw);
+        put16(st + 4096, lane, zw);
+        __syncwarp();
+        const long long to = row0 * g.out_ld + col0;
+        send16(st + 4096, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
+        send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + to, g.out_ld, p);
+        send16(st + 2048, lane, static_cast<__nv_bfloat16 *>(g.out[2]) + to, g.out_ld, p);
     }
 };
 
@@ -198,19 +236,6 @@ cudaError_t pack(Operand &o, int M, long long s0, long long s1, Bump &bump, cuda
     return cudaSuccess;
 }
 
-// Columns of a tile: of 256, 128 and 64 (dual: of both halves) the ones that take the fewest rounds of blocks, weighed by what a round costs: the
-// products of so many columns, and the rows of A that every tile brings again (worth some 64 columns).
-template <typename F>
-int pick_tile_n(bool dual, const F &tiles) {
-    int best = 0;
-    int64_t least = 0;
-    for (int n = 256; n >= (dual ? 128 : 64); n /= 2) {
-        const int64_t rounds = (tiles(dual ? n / 2 : n) + NUM_SMS - 1) / NUM_SMS, cost = rounds * (n + 64);
-        if (!best || cost < least) best = n, least = cost;
-    }
-    return best;
-}
-
 constexpr int WORKERS = 16;   // of a launch: three groups and two maps each at most
 
 struct Run {
@@ -225,10 +250,11 @@ cudaError_t product_store(const Operand &x, const Operand &w, int M, int tokens,
     using E = StoreEpilogue<true, false>;
     static thread_local GemmArgs<E> a;
     for (int m0 = 0; m0 < M; m0 += WORKERS) {
-        const int some = std::min(WORKERS, M - m0), tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(tokens, n, t, false); });
-        begin_gemm(a, true, tile, false, false, 1);
+        const int some = std::min(WORKERS, M - m0);
+        const GemmCut cut = pick_cut(false, k, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(tokens, n, c, false, false); });
+        begin_gemm(a, true, cut, false, false, 1);
         cudaError_t e = x.maps(a, 0, 0, M, m0, some, GEMM_BM);
-        if (e == cudaSuccess) e = w.maps(a, 1, 1, M, m0, some, tile);
+        if (e == cudaSuccess) e = w.maps(a, 1, 1, M, m0, some, cut.box_n(false));
         if (e != cudaSuccess) return e;
         for (int i = 0; i < some; ++i) {
             GemmGroup &g = add_group(a, tokens, n, k, 1);
@@ -271,10 +297,10 @@ cudaError_t weight_grads(const FfnArgs &a, const Operands &o, const Operand &z, 
     static thread_local GemmArgs<E> g;
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
-        const int tile = pick_tile_n(false, [&](int t) {
-            return static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, t, false) + tiles_of(a.width, a.hidden, t, false));
+        const GemmCut cut = pick_cut(false, a.tokens, [&](const GemmCut &c) {
+            return static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, c, false, false) + tiles_of(a.width, a.hidden, c, false, false));
         });
-        begin_gemm(g, true, tile, false, false, 1);
+        begin_gemm(g, true, cut, false, false, 1);
         int map = 0;
         for (const Operand *x : {&dg, &du, &o.dy, &o.h, &z}) {
             const cudaError_t e = x->maps(g, map++, 0, a.M, m0, some, 64);
@@ -317,12 +343,13 @@ cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, c
     static thread_local GemmArgs<UpEpilogue> g;
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
-        const int tile = pick_tile_n(true, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, t, false); });
-        begin_gemm(g, true, tile, true, false, 1);
+        const GemmCut cut = pick_cut(true, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, true, false); });
+        const int box = cut.box_n(true);
+        begin_gemm(g, true, cut, true, false, 1);
         e = o.h.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
         // (gate and up of a worker next to one another: the second half of a tile's columns is the next map's)
-        if (e == cudaSuccess) e = o.gate.maps(g, 1, 2, a.M, m0, some, tile / 2);
-        if (e == cudaSuccess) e = o.up.maps(g, 2, 2, a.M, m0, some, tile / 2);
+        if (e == cudaSuccess) e = o.gate.maps(g, 1, 2, a.M, m0, some, box);
+        if (e == cudaSuccess) e = o.up.maps(g, 2, 2, a.M, m0, some, box);
         if (e != cudaSuccess) return e;
         // where the one is a single map and the other one each, both take one each
         const bool batched = o.gate.batched && o.up.batched;
@@ -332,7 +359,7 @@ cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, c
                 if (!w.batched) continue;
                 for (int i = 0; i < some && e == cudaSuccess; ++i)
                     e = encode_boxes(&g.maps[1 + half + 2 * i], static_cast<const __nv_bfloat16 *>(w.data) + (m0 + i) * w.batch_ld, true, w.cols, w.rows, 1, w.ld,
-                                     w.batch_ld, tile / 2);
+                                     w.batch_ld, box);
             }
             if (e != cudaSuccess) return e;
         }
@@ -370,8 +397,8 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<DzEpilogue> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const int tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, t, false); });
-            begin_gemm(g, true, tile, false, false, 1);
+            const GemmCut cut = pick_cut(false, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, false, false); });
+            begin_gemm(g, true, cut, false, false, 1);
             e = o.dy.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
             if (e == cudaSuccess) e = o.down.maps(g, 1, 1, a.M, m0, some, 64);
             if (e != cudaSuccess) return e;
@@ -400,8 +427,8 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<E> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const int tile = pick_tile_n(false, [&](int t) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, t, false); });
-            begin_gemm(g, true, tile, false, false, 2);
+            const GemmCut cut = pick_cut(false, 2 * a.hidden, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, c, false, false); });
+            begin_gemm(g, true, cut, false, false, 2);
             e = dg.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
             if (e == cudaSuccess) e = du.maps(g, 1, 0, a.M, m0, some, GEMM_BM);
             for (int i = 0; i < some && e == cudaSuccess; ++i)

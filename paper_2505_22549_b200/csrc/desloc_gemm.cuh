@@ -6,8 +6,14 @@
 // ever transposed in memory.  What lies outside a matrix is zeros, filled in by the copy engine.
 //
 // One block per SM, persistent: a warp requests boxes (TMA) into a ring of stages, a thread issues the products, eight warps empty one of two
-// accumulators while the other is being filled.
+// accumulators while the other is being filled, and fetch what they need from memory a piece ahead.
+//
+// Blocks work alone (128 rows of C a tile) or in pairs (256 rows; each brings its own 128 rows of A and half of B, and the tensor cores of both read both
+// halves).  What bounds the products of a block alone is its shared memory: for 64 k of a 128 x 256 tile 48 KB are written and read again, 768 cycles of 128 bytes, for
+// 512 cycles of products; of a pair each block moves 32 KB in those 512.
 #pragma once
+#include <atomic>
+
 #include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
@@ -18,7 +24,8 @@
 namespace desloc {
 
 constexpr int GEMM_BM = 128, GEMM_BK = 64, GEMM_MAX_STAGES = 8, GEMM_EPI_WARPS = 8, GEMM_THREADS = 128 + 32 * GEMM_EPI_WARPS;
-constexpr int GEMM_A_BYTES = GEMM_BM * GEMM_BK * 2, GEMM_STAGING = 4096;   // staging: of every warp that empties accumulators
+constexpr int GEMM_A_BYTES = GEMM_BM * GEMM_BK * 2;
+constexpr int GEMM_IN = 4096, GEMM_STAGING = 2 * GEMM_IN;   // of every warp that empties accumulators: pieces that come, pieces that go
 constexpr int GEMM_SMEM = 227 * 1024 - 2048, GEMM_MAX_GROUPS = 48, GEMM_MAX_MAPS = 64, GEMM_DRAIN_LIMIT = 1 << 22;
 
 // A number of matrices of the same sizes, or a worker's.
@@ -44,6 +51,7 @@ struct GemmArgs {
     GemmGroup groups[GEMM_MAX_GROUPS];
     int ngroups, tiles;
     int tile_n, stages, segments;   // columns of a tile; stages of the ring; pairs of operands that one accumulator sums
+    int pairs;               // blocks work in pairs
     int dual;                // the tile's columns are two halves, of two B operands
     int symmetric;           // only tiles that reach the lower triangle
     uint32_t idesc;          // without the operands' layouts
@@ -53,9 +61,22 @@ struct GemmArgs {
 };
 
 // ---- the machine's instructions ----------------------------------------------------------------------
-__device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int x, int y, int z, uint64_t *bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 :: "r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(bar)) : "memory");
+// (of a pair: the bytes are counted on the first block's barrier)
+template <int CG>
+__device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int x, int y, int z, uint32_t bar) {
+    if constexpr (CG == 1)
+        asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     :: "r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                     :: "r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+// The address of the first block's copy of a barrier.
+template <int CG>
+__device__ __forceinline__ uint32_t first_blocks(const uint64_t *bar) {
+    uint32_t at = smem_u32(bar);
+    if constexpr (CG == 2) asm volatile("mapa.shared::cluster.u32 %0, %0, 0;" : "+r"(at));
+    return at;
 }
 // Descriptor of an operand's tile in shared memory: 128-byte swizzle; k-major: groups of eight rows 1024 bytes apart; m/n-major: blocks of 64
 // columns 8192 bytes apart, groups of eight k 1024 bytes.
@@ -63,12 +84,23 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, int mn) {
     return static_cast<uint64_t>((addr >> 4) & 0x3fff) | (static_cast<uint64_t>(mn ? 8192 >> 4 : 1) << 16) | (static_cast<uint64_t>(1024 >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
 }
+template <int CG>
 __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
-                 :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
+    else
+        asm volatile("{\n .reg .pred p;\n setp.ne.u32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                     :: "r"(d), "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(add)) : "memory");
 }
+// The products so far, done: told to this barrier, of both blocks of a pair.
+template <int CG>
 __device__ __forceinline__ void mma_commit(uint64_t *bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
+    if constexpr (CG == 1)
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" :: "r"(smem_u32(bar)) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     :: "r"(smem_u32(bar)), "h"(static_cast<uint16_t>(3)) : "memory");
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -78,8 +110,15 @@ __device__ __forceinline__ void bar_init(uint64_t *bar, int count) {
 __device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint64_t *bar) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(bar)) : "memory");
+// One lane of a warp.  (By this instruction the compiler knows that what follows runs in one lane alone and holds addresses and descriptors in uniform registers; behind
+// `lane == 0` it did not, and every product took 150 cycles to issue.)
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}" : "=r"(one));
+    return one != 0;
+}
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // 32 columns of this warp's 32 rows: a row per lane.
 __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
@@ -100,48 +139,90 @@ __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.syn
 struct Piece {
     int rows, cols;   // how much of it lies inside
     bool wide;        // rows begin on 16-byte boundaries
+    __device__ __forceinline__ bool none() const { return rows <= 0 || cols <= 0; }
 };
+__device__ __forceinline__ Piece piece_at(const GemmGroup &g, int row0, int col0, bool wide) { return {min(32, g.m - row0), min(32, g.n - col0), wide}; }
 
+// f(number, row, column, place in the staging area) for the lane's 16 bytes each
 template <typename F>
 __device__ __forceinline__ void visit16(const Piece &p, int lane, const F &f) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = 8 * i + (lane >> 2), c = lane & 3;
-        if (row < p.rows && 8 * c < p.cols) f(row, 8 * c, row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
+        if (row < p.rows && 8 * c < p.cols) f(i, row, 8 * c, row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
+    }
+}
+template <typename F>
+__device__ __forceinline__ void visit32(const Piece &p, int lane, const F &f) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = 4 * i + (lane >> 3), c = lane & 7;
+        if (row < p.rows && 4 * c < p.cols) f(i, row, 4 * c, row * 128 + ((c ^ (row & 7)) << 4));
     }
 }
 __device__ __forceinline__ int place16(int lane, int c) { return lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4); }
+__device__ __forceinline__ int place32(int lane, int c) { return lane * 128 + ((c ^ (lane & 7)) << 4); }
 
-// memory -> w: 16 words of two values, the lane's row
-__device__ __forceinline__ void load_piece16(char *st, int lane, const void *from, long long ld, const Piece &p, uint32_t (&w)[16]) {
+// memory -> registers, as it lies there
+__device__ __forceinline__ void fetch16(const void *from, long long ld, const Piece &p, int lane, uint4 (&v)[4]) {
     const unsigned short *src = static_cast<const unsigned short *>(from);
-    __syncwarp();
-    visit16(p, lane, [&](int row, int col, int at) {
-        uint4 v;
+    visit16(p, lane, [&](int i, int row, int col, int) {
         if (p.wide && col + 8 <= p.cols) {
-            v = *reinterpret_cast<const uint4 *>(src + row * ld + col);
+            v[i] = *reinterpret_cast<const uint4 *>(src + row * ld + col);
         } else {
             uint32_t h[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[e] = col + e < p.cols ? src[row * ld + col + e] : 0;
-            v = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+            v[i] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
         }
-        *reinterpret_cast<uint4 *>(st + at) = v;
     });
-    __syncwarp();
+}
+__device__ __forceinline__ void fetch32(const float *src, long long ld, const Piece &p, int lane, uint4 (&v)[8]) {
+    visit32(p, lane, [&](int i, int row, int col, int) {
+        if (p.wide && col + 4 <= p.cols) {
+            v[i] = *reinterpret_cast<const uint4 *>(src + row * ld + col);
+        } else {
+            uint32_t h[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) h[e] = col + e < p.cols ? __float_as_uint(src[row * ld + col + e]) : 0;
+            v[i] = make_uint4(h[0], h[1], h[2], h[3]);
+        }
+    });
+}
+// registers -> staging area, whence each lane reads its row (behind a __syncwarp())
+__device__ __forceinline__ void settle16(char *st, int lane, const uint4 (&v)[4]) {
+    visit16({32, 32, true}, lane, [&](int i, int, int, int at) { *reinterpret_cast<uint4 *>(st + at) = v[i]; });
+}
+__device__ __forceinline__ void settle32(char *st, int lane, const uint4 (&v)[8]) {
+    visit32({32, 32, true}, lane, [&](int i, int, int, int at) { *reinterpret_cast<uint4 *>(st + at) = v[i]; });
+}
+__device__ __forceinline__ void row16(const char *st, int lane, uint32_t (&w)[16]) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
         const uint4 v = *reinterpret_cast<const uint4 *>(st + place16(lane, c));
         w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
     }
 }
-__device__ __forceinline__ void store_piece16(char *st, int lane, void *to, long long ld, const Piece &p, const uint32_t (&w)[16]) {
-    unsigned short *dst = static_cast<unsigned short *>(to);
-    __syncwarp();
+__device__ __forceinline__ void row32(const char *st, int lane, float (&v)[32]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+        const float4 x = *reinterpret_cast<const float4 *>(st + place32(lane, c));
+        v[4 * c] = x.x, v[4 * c + 1] = x.y, v[4 * c + 2] = x.z, v[4 * c + 3] = x.w;
+    }
+}
+// rows in lanes -> staging area
+__device__ __forceinline__ void put16(char *st, int lane, const uint32_t (&w)[16]) {
 #pragma unroll
     for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + place16(lane, c)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
-    __syncwarp();
-    visit16(p, lane, [&](int row, int col, int at) {
+}
+__device__ __forceinline__ void put32(char *st, int lane, const float (&v)[32]) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) *reinterpret_cast<float4 *>(st + place32(lane, c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+}
+// staging area -> memory (behind a __syncwarp())
+__device__ __forceinline__ void send16(const char *st, int lane, void *to, long long ld, const Piece &p) {
+    unsigned short *dst = static_cast<unsigned short *>(to);
+    visit16(p, lane, [&](int, int row, int col, int at) {
         const uint4 v = *reinterpret_cast<const uint4 *>(st + at);
         if (p.wide && col + 8 <= p.cols) {
             *reinterpret_cast<uint4 *>(dst + row * ld + col) = v;
@@ -153,44 +234,8 @@ __device__ __forceinline__ void store_piece16(char *st, int lane, void *to, long
         }
     });
 }
-
-template <typename F>
-__device__ __forceinline__ void visit32(const Piece &p, int lane, const F &f) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = 4 * i + (lane >> 3), c = lane & 7;
-        if (row < p.rows && 4 * c < p.cols) f(row, 4 * c, row * 128 + ((c ^ (row & 7)) << 4));
-    }
-}
-__device__ __forceinline__ int place32(int lane, int c) { return lane * 128 + ((c ^ (lane & 7)) << 4); }
-
-__device__ __forceinline__ void load_piece32(char *st, int lane, const float *src, long long ld, const Piece &p, float (&v)[32]) {
-    __syncwarp();
-    visit32(p, lane, [&](int row, int col, int at) {
-        float4 x;
-        if (p.wide && col + 4 <= p.cols) {
-            x = *reinterpret_cast<const float4 *>(src + row * ld + col);
-        } else {
-            float h[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = col + e < p.cols ? src[row * ld + col + e] : 0.f;
-            x = make_float4(h[0], h[1], h[2], h[3]);
-        }
-        *reinterpret_cast<float4 *>(st + at) = x;
-    });
-    __syncwarp();
-#pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const float4 x = *reinterpret_cast<const float4 *>(st + place32(lane, c));
-        v[4 * c] = x.x, v[4 * c + 1] = x.y, v[4 * c + 2] = x.z, v[4 * c + 3] = x.w;
-    }
-}
-__device__ __forceinline__ void store_piece32(char *st, int lane, float *dst, long long ld, const Piece &p, const float (&v)[32]) {
-    __syncwarp();
-#pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<float4 *>(st + place32(lane, c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-    __syncwarp();
-    visit32(p, lane, [&](int row, int col, int at) {
+__device__ __forceinline__ void send32(const char *st, int lane, float *dst, long long ld, const Piece &p) {
+    visit32(p, lane, [&](int, int row, int col, int at) {
         const float4 x = *reinterpret_cast<const float4 *>(st + at);
         if (p.wide && col + 4 <= p.cols) {
             *reinterpret_cast<float4 *>(dst + row * ld + col) = x;
@@ -211,11 +256,11 @@ __device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2
 __device__ __forceinline__ float2 unpack_bf16(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 
 // ---- the kernel --------------------------------------------------------------------------------------
-// Where a tile lies; advances with the tile's number.
+// Where a tile lies; goes on with the tile's number.
 struct TileWalk {
     int group = 0;
     int batch, i, j;   // matrix of the group, tile along m and n
-    template <typename A>
+    template <int CG, typename A>
     __device__ __forceinline__ const GemmGroup &find(const A &a, int tile) {
         while (group + 1 < a.ngroups && a.groups[group + 1].tile0 <= tile) ++group;
         const GemmGroup &g = a.groups[group];
@@ -224,7 +269,7 @@ struct TileWalk {
         t -= batch * g.per;
         if (a.symmetric) {   // row i of tiles reaches as far as the diagonal
             for (i = 0;; ++i) {
-                const int here = min((i * GEMM_BM + GEMM_BM - 1) / a.tile_n + 1, g.nt);
+                const int here = min((i * CG * GEMM_BM + CG * GEMM_BM - 1) / a.tile_n + 1, g.nt);
                 if (t < here) break;
                 t -= here;
             }
@@ -237,82 +282,105 @@ struct TileWalk {
     }
 };
 
-// E: the epilogue.  E::piece(args, group, batch, i, j, accumulator, column, staging, quadrant, lane) takes 32 columns (dual: of both halves) of a quadrant of 32 rows.
-template <typename E>
+// E, the epilogue, takes 32 x 32 pieces: of what it reads, E::Ahead is fetched one piece ahead by E::fetch(args, group, batch, row, column, lane, ahead), put into the staging area
+// by E::settle(staging, lane, ahead), and E::finish(args, group, batch, row, column, accumulator, staging, lane) does the rest.
+template <typename E, int CG>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs<E> a) {
     extern __shared__ __align__(1024) char gemm_smem[];
     __shared__ __align__(8) uint64_t full[GEMM_MAX_STAGES], empty[GEMM_MAX_STAGES], ready[2], taken[2], drained;
-    __shared__ uint32_t tmem_at;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __shared__ uint32_t tmem_at, bytes_of[GEMM_MAX_STAGES];
+    __shared__ int requested, failed;
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    uint32_t rank = 0;
+    if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const uint32_t pad = (1024 - (smem_u32(gemm_smem) & 1023)) & 1023;
     char *const ring = gemm_smem + pad;
-    const int stage_bytes = GEMM_A_BYTES + a.tile_n * (GEMM_BK * 2);
+    const int own_n = a.tile_n / CG, stage_bytes = GEMM_A_BYTES + (own_n + 63) / 64 * 64 * (GEMM_BK * 2);
+    const int tile0 = blockIdx.x / CG, tile_step = gridDim.x / CG;
     begin_and_let_next_begin();
     if (threadIdx.x == 0) {
+        requested = failed = 0;
         for (int s = 0; s < a.stages; ++s) bar_init(&full[s], 1), bar_init(&empty[s], 1);
-        for (int b = 0; b < 2; ++b) bar_init(&ready[b], 1), bar_init(&taken[b], GEMM_EPI_WARPS);
+        for (int b = 0; b < 2; ++b) bar_init(&ready[b], 1), bar_init(&taken[b], CG * GEMM_EPI_WARPS);
         bar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
     tmem_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_sync();
     tmem_fence_after();
     const uint32_t tmem = tmem_at;
     wait_for_earlier_kernels();
     const auto give_up = [&] {
         if (a.err) *reinterpret_cast<volatile int *>(a.err) = 1;
+        *reinterpret_cast<volatile int *>(&failed) = 1;
     };
 
     if (warp == 0) {
-        if (lane == 0) {
+        if (elect_one()) {
             TileWalk at;
             int s = 0, asked = 0;
             uint32_t phase = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
-                const GemmGroup &g = at.find(a, tile);
-                const int m0 = at.i * GEMM_BM, n0 = at.j * (a.dual ? a.tile_n / 2 : a.tile_n), steps = (g.k + GEMM_BK - 1) / GEMM_BK;
-                for (int kk = 0; ok && kk < steps * a.segments; ++kk) {
+            for (int tile = tile0; ok && tile < a.tiles; tile += tile_step) {
+                const GemmGroup &g = at.find<CG>(a, tile);
+                const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
+                const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
+                const int boxes = (own_n + 63) / 64;
+                const uint32_t bytes = GEMM_A_BYTES + (g.b_mn ? 64 * boxes : own_n) * (GEMM_BK * 2);
+                for (int kk = 0; kk < steps * a.segments; ++kk) {
                     ok = bar_wait(&empty[s], phase ^ 1, a.wait_limit);
                     if (!ok) break;
                     const int seg = kk >= steps ? 1 : 0, k0 = (kk - seg * steps) * GEMM_BK;
                     char *const sa = ring + s * stage_bytes, *const sb = sa + GEMM_A_BYTES;
                     const CUtensorMap *const ma = &a.maps[g.a_map + seg], *const mb = &a.maps[g.b_map + seg];
                     const int za = g.a_batch + at.batch, zb = g.b_batch + at.batch;
-                    bar_expect(&full[s], stage_bytes);
+                    const uint32_t bar = first_blocks<CG>(&full[s]);
+                    bytes_of[s] = bytes;
+                    if (rank == 0) bar_expect(&full[s], CG * bytes);
                     if (g.a_mn) {
-                        for (int x = 0; x < GEMM_BM; x += 64) tma_load(sa + x * (GEMM_BK * 2), ma, m0 + x, k0, za, &full[s]);
+                        for (int x = 0; x < GEMM_BM; x += 64) tma_load<CG>(sa + x * (GEMM_BK * 2), ma, m0 + x, k0, za, bar);
                     } else {
-                        tma_load(sa, ma, k0, m0, za, &full[s]);
+                        tma_load<CG>(sa, ma, k0, m0, za, bar);
                     }
                     if (g.b_mn) {
-                        for (int x = 0; x < a.tile_n; x += 64) tma_load(sb + x * (GEMM_BK * 2), mb, n0 + x, k0, zb, &full[s]);
+                        for (int x = 0; x < boxes; ++x) tma_load<CG>(sb + x * (64 * GEMM_BK * 2), mb, n0 + 64 * x, k0, zb, bar);
+                    } else if (!a.dual) {
+                        tma_load<CG>(sb, mb, k0, n0, zb, bar);
+                    } else if (CG == 2) {   // a half each
+                        tma_load<CG>(sb, mb + rank, k0, n0, zb, bar);
                     } else {
-                        tma_load(sb, mb, k0, n0, zb, &full[s]);
-                        if (a.dual) tma_load(sb + a.tile_n * GEMM_BK, mb + 1, k0, n0, zb, &full[s]);
+                        tma_load<CG>(sb, mb, k0, n0, zb, bar);
+                        tma_load<CG>(sb + a.tile_n * GEMM_BK, mb + 1, k0, n0, zb, bar);
                     }
                     ++asked;
                     if (++s == a.stages) s = 0, phase ^= 1;
                 }
             }
-            if (!ok) {   // the copies that are on their way land first
-                give_up();
-                for (int x = max(0, asked - a.stages); x < asked; ++x) bar_wait(&full[x % a.stages], (x / a.stages) & 1, GEMM_DRAIN_LIMIT);
-            }
+            requested = asked;
+            if (!ok) give_up();
+            // the products have read what this block brought (and told so) before it may leave
+            for (int x = max(0, asked - a.stages); ok && x < asked; ++x) ok = bar_wait(&empty[x % a.stages], (x / a.stages) & 1, a.wait_limit);
+            if (!ok) give_up();
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (rank == 0 && elect_one()) {
             TileWalk at;
             int s = 0, buf = 0;
             uint32_t phase = 0, turn = 0;
             bool ok = true;
-            for (int tile = blockIdx.x; ok && tile < a.tiles; tile += gridDim.x) {
-                const GemmGroup &g = at.find(a, tile);
+            for (int tile = tile0; ok && tile < a.tiles; tile += tile_step) {
+                const GemmGroup &g = at.find<CG>(a, tile);
                 const int steps = (g.k + GEMM_BK - 1) / GEMM_BK * a.segments;
                 ok = bar_wait(&taken[buf], turn ^ 1, a.wait_limit);
                 if (!ok) break;
@@ -326,52 +394,106 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                     const uint32_t sa = smem_u32(ring + s * stage_bytes);
                     const uint64_t da = operand_desc(sa, g.a_mn), db = operand_desc(sa + GEMM_A_BYTES, g.b_mn);
 #pragma unroll
-                    for (int x = 0; x < GEMM_BK / 16; ++x) mma_f16(d, da + x * ka, db + x * kb, idesc, kk > 0 || x > 0);
-                    mma_commit(&empty[s]);
+                    for (int x = 0; x < GEMM_BK / 16; ++x) mma_f16<CG>(d, da + x * ka, db + x * kb, idesc, kk > 0 || x > 0);
+                    mma_commit<CG>(&empty[s]);
                     if (++s == a.stages) s = 0, phase ^= 1;
                 }
                 if (!ok) break;
-                mma_commit(&ready[buf]);
+                mma_commit<CG>(&ready[buf]);
                 buf ^= 1;
                 if (buf == 0) turn ^= 1;
             }
             if (!ok) {   // the products that are on their way end first
                 give_up();
-                mma_commit(&drained);
+                mma_commit<CG>(&drained);
                 bar_wait(&drained, 0, GEMM_DRAIN_LIMIT);
             }
         }
         __syncwarp();
     } else if (warp >= 4) {
-        const int quadrant = warp & 3, half = (warp - 4) >> 2;
+        const int quadrant = warp & 3, c0 = (warp - 4) / 4 * 32;
         char *const st = ring + a.stages * stage_bytes + (warp - 4) * GEMM_STAGING;
-        TileWalk at;
-        int buf = 0;
-        uint32_t turn = 0;
         const int out_n = a.dual ? a.tile_n / 2 : a.tile_n;
-        for (int tile = blockIdx.x; tile < a.tiles; tile += gridDim.x) {
-            const GemmGroup &g = at.find(a, tile);
-            if (!bar_wait(&ready[buf], turn, a.wait_limit)) {
-                give_up();
-                break;
+        const int rows = (rank * 4 + quadrant) * 32;
+        TileWalk at;
+        typename E::Ahead ahead;
+        int buf = 0, tile = tile0, c = c0;
+        uint32_t turn = 0;
+        const GemmGroup *g = nullptr;
+        if (tile < a.tiles) {
+            g = &at.find<CG>(a, tile);
+            E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
+        }
+        while (tile < a.tiles) {
+            if (c == c0) {
+                if (!bar_wait(&ready[buf], turn, a.wait_limit)) {
+                    give_up();
+                    break;
+                }
+                tmem_fence_after();
             }
-            tmem_fence_after();
-            const uint32_t d = tmem + buf * 256 + (static_cast<uint32_t>(32 * quadrant) << 16);
-            const int row0 = at.i * GEMM_BM + 32 * quadrant;
-            for (int c = 32 * half; c < out_n; c += 64) E::piece(a, g, at.batch, row0, at.j * out_n + c, d + c, st, lane);
-            tmem_fence_before();
+            const GemmGroup &here = *g;
+            const int batch = at.batch, row0 = at.i * (CG * GEMM_BM) + rows, col0 = at.j * out_n + c;
+            const uint32_t d = tmem + buf * 256 + c + (static_cast<uint32_t>(32 * quadrant) << 16);
+            __syncwarp();   // (the piece before has been read)
+            E::settle(st, lane, ahead);
+            c += 64;
+            const bool last = c >= out_n;
+            if (last) {
+                c = c0, tile += tile_step;
+                if (tile < a.tiles) g = &at.find<CG>(a, tile);
+            }
+            if (tile < a.tiles) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
             __syncwarp();
-            if (lane == 0) bar_arrive(&taken[buf]);
-            buf ^= 1;
-            if (buf == 0) turn ^= 1;
+            E::finish(a, here, batch, row0, col0, d, st, lane);
+            if (last) {
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) {
+                    if constexpr (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(&taken[buf])) : "memory");
+                    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(first_blocks<CG>(&taken[buf])) : "memory");
+                }
+                buf ^= 1;
+                if (buf == 0) turn ^= 1;
+            }
         }
         __syncwarp();
     }
     tmem_fence_before();
     __syncthreads();
+    int others = 0, fell = failed;
+    if constexpr (CG == 2) {
+        cluster_sync();
+        uint32_t where, flag;
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(where) : "r"(smem_u32(&requested)), "r"(rank ^ 1));
+        asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(others) : "r"(where) : "memory");
+        asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(where) : "r"(smem_u32(&failed)), "r"(rank ^ 1));
+        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(flag) : "r"(where) : "memory");
+        fell |= static_cast<int>(flag);
+    }
+    if (fell && rank == 0 && threadIdx.x == 0) {
+        // Copies that are on their way land before anyone leaves.  Of a stage that one block of a pair has requested and the other has not, the other's
+        // part is made up: asked for less, or told as done.
+        const int mine = requested, most = CG == 2 ? max(mine, others) : mine, both = CG == 2 ? min(mine, others) : mine;
+        for (int x = max(0, most - a.stages); x < most; ++x) {
+            const int s = x % a.stages;
+            if (x >= both && mine < most) {
+                uint32_t where, bytes;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, 1;" : "=r"(where) : "r"(smem_u32(&bytes_of[s])));
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(bytes) : "r"(where) : "memory");
+                bar_expect(&full[s], bytes);
+            }
+            if (x >= both && mine == most)
+                asm volatile("mbarrier.complete_tx.relaxed.cluster.shared::cluster.b64 [%0], %1;" :: "r"(smem_u32(&full[s])), "r"(bytes_of[s]) : "memory");
+            bar_wait(&full[s], (x / a.stages) & 1, GEMM_DRAIN_LIMIT);
+        }
+    }
+    __syncwarp();
+    if constexpr (CG == 2) cluster_sync();   // (what one block reads of the other has been read)
     if (warp == 2) {
         tmem_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+        if constexpr (CG == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
+        else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" :: "r"(tmem) : "memory");
     }
 }
 
@@ -382,45 +504,98 @@ cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t 
 // Whether rows `ld` elements apart from `data` on can be fetched by the copy engine: 16-byte boundaries.
 inline bool boxes_fit(const void *data, int64_t ld) { return ((reinterpret_cast<uintptr_t>(data) | static_cast<uintptr_t>(ld * 2)) & 15u) == 0; }
 
-template <typename E>
-void begin_gemm(GemmArgs<E> &a, bool bf16, int tile_n, bool dual, bool symmetric, int segments) {
-    a.ngroups = a.tiles = 0;
-    a.tile_n = tile_n, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
-    const int stage = GEMM_A_BYTES + tile_n * GEMM_BK * 2;
-    a.stages = (GEMM_SMEM - 1024 - GEMM_EPI_WARPS * GEMM_STAGING) / stage;
-    if (a.stages > GEMM_MAX_STAGES) a.stages = GEMM_MAX_STAGES;
-    const uint32_t type = bf16 ? 1 : 0;
-    a.idesc = 1u << 4 | type << 7 | type << 10 | static_cast<uint32_t>(tile_n >> 3) << 17 | static_cast<uint32_t>(GEMM_BM >> 4) << 24;
-}
-inline int tiles_of(int m, int n, int tile_n, bool symmetric) {
-    const int mt = (m + GEMM_BM - 1) / GEMM_BM, nt = (n + tile_n - 1) / tile_n;
+// How a launch is cut: columns of a tile (dual: of both halves together), and whether blocks work in pairs.
+struct GemmCut {
+    int tile_n;
+    bool pairs;
+    int out_n(bool dual) const { return dual ? tile_n / 2 : tile_n; }
+    int box_n(bool dual) const { return dual || pairs ? tile_n / 2 : tile_n; }   // rows of a k-major box of B
+};
+inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric) {
+    const int bm = GEMM_BM * (cut.pairs ? 2 : 1), tile_n = cut.out_n(dual);
+    const int mt = (m + bm - 1) / bm, nt = (n + tile_n - 1) / tile_n;
     if (!symmetric) return mt * nt;
     int all = 0;
-    for (int i = 0; i < mt; ++i) all += std::min((i * GEMM_BM + GEMM_BM - 1) / tile_n + 1, nt);
+    for (int i = 0; i < mt; ++i) all += std::min((i * bm + bm - 1) / tile_n + 1, nt);
     return all;
+}
+// The cut that is done first: rounds of tiles, a tile as long as its products (in cycles for 64 k: what they take, or what shared memory takes to be written and read), or as
+// emptying it (some 800 cycles for the 64 columns that the warps take at a time).  tiles(cut): how many there are, all with k of about `k`.
+template <typename F>
+GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
+    GemmCut best{};
+    int64_t least = 0;
+    for (int pairs = 1; pairs >= 0; --pairs)
+        for (int n = 256; n >= (dual || pairs ? 128 : 64); n -= 64) {
+            const GemmCut cut{n, pairs != 0};
+            const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, rounds = (tiles(cut) + slots - 1) / slots;
+            const int64_t step = pairs ? std::max(2 * n, 256 + n) : 256 + 2 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 63) / 64 * 800;
+            const int64_t cost = rounds * (std::max(products, empty) + 200) + empty;
+            if (!best.tile_n || cost < least) best = cut, least = cost;
+        }
+    return best;
+}
+
+template <typename E>
+void begin_gemm(GemmArgs<E> &a, bool bf16, const GemmCut &cut, bool dual, bool symmetric, int segments) {
+    a.ngroups = a.tiles = 0;
+    a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
+    const uint32_t type = bf16 ? 1 : 0;
+    a.idesc = 1u << 4 | type << 7 | type << 10 | static_cast<uint32_t>(cut.tile_n >> 3) << 17 | static_cast<uint32_t>((cut.pairs ? 2 : 1) * GEMM_BM >> 4) << 24;
 }
 // The next group, of `count` matrices: its sizes and tiles; the rest is the caller's.
 template <typename E>
 GemmGroup &add_group(GemmArgs<E> &a, int m, int n, int k, int count) {
     GemmGroup &g = a.groups[a.ngroups++];
     g = GemmGroup{};
-    const int out_n = a.dual ? a.tile_n / 2 : a.tile_n;
+    const GemmCut cut{a.tile_n, a.pairs != 0};
+    const int out_n = cut.out_n(a.dual), bm = GEMM_BM * (a.pairs ? 2 : 1);
     g.tile0 = a.tiles;
     g.m = m, g.n = n, g.k = k;
-    g.mt = (m + GEMM_BM - 1) / GEMM_BM, g.nt = (n + out_n - 1) / out_n;
-    g.per = tiles_of(m, n, out_n, a.symmetric);
+    g.mt = (m + bm - 1) / bm, g.nt = (n + out_n - 1) / out_n;
+    g.per = tiles_of(m, n, cut, a.dual, a.symmetric);
     a.tiles += g.per * count;
     return g;
 }
 
+// Raises a kernel's limit of shared memory, once on each device.
+template <typename E, int CG>
+cudaError_t gemm_ready() {
+    static std::atomic<uint64_t> done{0};
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess || (device < 64 && (done.load() >> device & 1))) return e;
+    e = cudaFuncSetAttribute(gemm_kernel<E, CG>, cudaFuncAttributeMaxDynamicSharedMemorySize, GEMM_SMEM);
+    if (e == cudaSuccess && device < 64) done.fetch_or(1ull << device);
+    return e;
+}
+
+template <typename E, int CG>
+cudaError_t launch_gemm(GemmArgs<E> &a, cudaStream_t stream) {
+    const cudaError_t e = gemm_ready<E, CG>();
+    if (e != cudaSuccess) return e;
+    const int stage = GEMM_A_BYTES + (a.tile_n / CG + 63) / 64 * 64 * GEMM_BK * 2;
+    a.stages = std::min(GEMM_MAX_STAGES, (GEMM_SMEM - 1024 - GEMM_EPI_WARPS * GEMM_STAGING) / stage);
+    cudaLaunchConfig_t lc{};
+    lc.gridDim = dim3(static_cast<unsigned>(CG * std::min(a.tiles, NUM_SMS / CG)));
+    lc.blockDim = dim3(GEMM_THREADS);
+    lc.dynamicSmemBytes = 1024 + static_cast<size_t>(a.stages) * stage + GEMM_EPI_WARPS * GEMM_STAGING;
+    lc.stream = stream;
+    cudaLaunchAttribute at[2]{};
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    at[1].id = cudaLaunchAttributeClusterDimension;
+    at[1].val.clusterDim.x = CG, at[1].val.clusterDim.y = at[1].val.clusterDim.z = 1;
+    lc.attrs = at;
+    lc.numAttrs = CG == 2 ? 2 : 1;
+    void *args[1] = {&a};
+    return cudaLaunchKernelExC(&lc, reinterpret_cast<const void *>(gemm_kernel<E, CG>), args);
+}
 template <typename E>
 cudaError_t launch_gemm(GemmArgs<E> &a, int *err, int wait_limit, cudaStream_t stream, int *launches) {
     if (a.tiles == 0) return cudaSuccess;
     a.err = err, a.wait_limit = wait_limit;
-    const size_t smem = 1024 + static_cast<size_t>(a.stages) * (GEMM_A_BYTES + a.tile_n * GEMM_BK * 2) + GEMM_EPI_WARPS * GEMM_STAGING;
-    cudaError_t e = cudaFuncSetAttribute(gemm_kernel<E>, cudaFuncAttributeMaxDynamicSharedMemorySize, GEMM_SMEM);
-    if (e != cudaSuccess) return e;
-    e = launch_op(gemm_kernel<E>, dim3(static_cast<unsigned>(std::min(a.tiles, NUM_SMS))), dim3(GEMM_THREADS), smem, true, stream, a);
+    const cudaError_t e = a.pairs ? launch_gemm<E, 2>(a, stream) : launch_gemm<E, 1>(a, stream);
     if (e == cudaSuccess) ++*launches;
     return e;
 }

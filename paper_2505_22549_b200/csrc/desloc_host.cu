@@ -712,7 +712,7 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
     coefficients.clear();
     for (int i = 0; i < 3 * how.steps; ++i) {
         const float v = how.coefficients ? how.coefficients[i] : kNewtonSchulz[i % 3];
-        if (!std::isfinite(v) || std::fabs(v) > 64.f) return DESLOC_E_RANGE;
+        if (!std::isfinite(v) || std::fabs(v) > 16.f) return DESLOC_E_RANGE;
         coefficients.push_back(v);
     }
     std::vector<char> seen(static_cast<size_t>(c.num_tensors), 0);

@@ -13,7 +13,8 @@ namespace {
 //
 // Operands are fp16: with bf16's eight bits the result was off by 1 % of its norm (normal 576 x 1536 matrices) and by 10 % and more where few directions dominate,
 // since a step takes small singular values times a = 3.4 and the rounding errors next to them too.  X is carried as two fp16 numbers (hi + lo / 2^11, 22 bits): hi is
-// the operand, a X takes both, so that what is rounded away in one step is there in the next.  Off by 0.15 % for normal matrices, 0.03 % for few directions.
+// the operand, a X takes both (a is on the diagonal of the polynomial, a lo is added behind the product), so that what is rounded away in one step is there in the
+// next.  Off by 0.15 % for normal matrices, 0.03 % for few directions.
 // Everything is held times ORTH_UNIT: singular values stay below two, entries far below one.
 constexpr float ORTH_UNIT = 256.f, ORTH_LO = 2048.f;
 constexpr int ORTH_ROUND = 128, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
@@ -80,7 +81,7 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-// Squares of a block's rows, summed in fp64 (fp32's range ends at values of 1e19).  Bound: HBM, each element read once.
+// Squares of a block's rows, up to four in fp32 (values below 1e-22 count as 0, beyond 1e19 as infinite), then in fp64.  Bound: HBM, each element read once.
 template <typename UT, typename GT>
 __global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
@@ -89,8 +90,9 @@ __global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_co
     if (static_cast<int>(blockIdx.x) * sh.block_rows >= sh.rows) return;
     double sum = 0;
     visit_rows<UT, GT>(s, blockIdx.y, [&](int, int, const auto &v) {
-        double part = 0;
-        for (float x : v) part += static_cast<double>(x) * x;
+        float part = 0;
+#pragma unroll
+        for (float x : v) part += x * x;
         sum += part;
     });
     sum = block_sum(sum);
@@ -131,20 +133,25 @@ __global__ void __launch_bounds__(ORTH_THREADS) orth_scale_kernel(const __grid_c
 }
 
 // ---- the products' epilogues -------------------------------------------------------------------------
-// A symmetric result: alpha times the sums, plus beta times in[0]; of the pieces below the diagonal the other one's place, too.
-struct SymArgs {
-    float c, b;
-};
+// A symmetric result: alpha times the sums, plus b times in[0], plus `diagonal` there; pieces below the diagonal go to the other one's place, too.
 struct SymEpilogue {
-    float b;
-    __device__ static void piece(const GemmArgs<SymEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
-        if (p.rows <= 0 || p.cols <= 0 || col0 > row0) return;
+    float b, diagonal;
+    struct Ahead {
+        uint4 v[4];
+    };
+    using Args = GemmArgs<SymEpilogue>;
+    __device__ static void fetch(const Args &, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
+        if (g.in[0] && col0 <= row0)
+            fetch16(static_cast<const __half *>(g.in[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true), lane, x.v);
+    }
+    __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
+    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, true);
+        if (p.none() || col0 > row0) return;
         __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
-        const long long at = row0 * g.out_ld + col0;
         float v[32];
         uint32_t w[16];
-        if (g.in[0]) load_piece16(st, lane, static_cast<const __half *>(g.in[0]) + batch * g.out_batch + at, g.out_ld, p, w);
+        if (g.in[0]) row16(st, lane, w);
         tmem_load32(d, v);
         tmem_wait();
 #pragma unroll
@@ -155,42 +162,62 @@ struct SymEpilogue {
                 const float2 x = unpack_f16(w[e]);
                 v[2 * e] += a.epi.b * x.x, v[2 * e + 1] += a.epi.b * x.y;
             }
+            if (col0 == row0) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) v[e] += e == lane ? a.epi.diagonal : 0.f;
+            }
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
-        store_piece16(st, lane, out + at, g.out_ld, p, w);
-        if (col0 < row0 && lane < p.rows) {   // (columns of the one are rows of the other: p.cols is 32 here)
-            __half *const t = out + col0 * g.out_ld + row0 + lane;
+        put16(st, lane, w);
+        __syncwarp();
+        send16(st, lane, out + row0 * g.out_ld + col0, g.out_ld, p);
+        if (col0 < row0) {
+            // Columns of the one are rows of the other (p.cols is 32 here).  Neighbouring lanes, neighbouring rows of this piece, make words: the even one of the
+            // even column, the odd one of the odd column.
+            const bool odd = lane & 1;
+            uint32_t *const t = reinterpret_cast<uint32_t *>(out + (col0 + odd) * g.out_ld + row0 + (lane & ~1));
+            const bool both = (lane | 1) < p.rows, one = (lane & ~1) < p.rows;
 #pragma unroll
-            for (int e = 0; e < 32; ++e) t[e * g.out_ld] = __float2half_rn(v[e]);
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, w[e], 1);
+                const uint32_t pair = odd ? __byte_perm(other, w[e], 0x7632) : __byte_perm(w[e], other, 0x5410);
+                uint32_t *const to = t + e * g.out_ld;   // (two columns on: 2 ld halves)
+                if (both) *to = pair;
+                else if (one) *reinterpret_cast<unsigned short *>(to) = static_cast<unsigned short>(pair);
+            }
         }
     }
 };
 
-// hi + lo / 2^11, times a, plus alpha times the sums.
-__device__ __forceinline__ void carried(char *st, int lane, const GemmGroup &g, long long at, const Piece &p, float a, uint32_t d, float (&v)[32]) {
-    uint32_t hi[16], lo[16];
-    load_piece16(st, lane, static_cast<const __half *>(g.in[0]) + at, g.in_ld, p, hi);
-    load_piece16(st, lane, static_cast<const __half *>(g.in[1]) + at, g.in_ld, p, lo);
+// X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
+__device__ __forceinline__ void carried(const char *st, int lane, float alpha, float lo, uint32_t d, float (&v)[32]) {
+    uint32_t w[16];
+    row16(st, lane, w);
     tmem_load32(d, v);
     tmem_wait();
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-        const float2 h = unpack_f16(hi[e]), l = unpack_f16(lo[e]);
-        v[2 * e] = v[2 * e] * g.alpha + a * (h.x + l.x * (1.f / ORTH_LO));
-        v[2 * e + 1] = v[2 * e + 1] * g.alpha + a * (h.y + l.y * (1.f / ORTH_LO));
+        const float2 l = unpack_f16(w[e]);
+        v[2 * e] = v[2 * e] * alpha + lo * l.x, v[2 * e + 1] = v[2 * e + 1] * alpha + lo * l.y;
     }
 }
 
-// X of the next step, in two halves.
 struct NextEpilogue {
-    float a;
-    __device__ static void piece(const GemmArgs<NextEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
-        if (p.rows <= 0 || p.cols <= 0) return;
-        const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
+    float lo;
+    struct Ahead {
+        uint4 v[4];
+    };
+    using Args = GemmArgs<NextEpilogue>;
+    __device__ static void fetch(const Args &, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
+        fetch16(static_cast<const __half *>(g.in[0]) + batch * g.in_batch + row0 * g.in_ld + col0, g.in_ld, piece_at(g, row0, col0, true), lane, x.v);
+    }
+    __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
+    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, true);
+        if (p.none()) return;
         float v[32];
-        carried(st, lane, g, at, p, a.epi.a, d, v);
+        carried(st, lane, g.alpha, a.epi.lo, d, v);
         uint32_t hi[16], lo[16];
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -198,8 +225,12 @@ struct NextEpilogue {
             const float2 h = unpack_f16(hi[e]);
             lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
         }
-        store_piece16(st, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p, hi);
-        store_piece16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p, lo);
+        put16(st, lane, lo);   // (each lane where it has read)
+        put16(st + 2048, lane, hi);
+        __syncwarp();
+        const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
+        send16(st + 2048, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p);
+        send16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p);
     }
 };
 
@@ -207,40 +238,62 @@ struct NextEpilogue {
 enum { ORTH_TO_F32 = 0, ORTH_TO_BF16 = 1, ORTH_TO_X = 2 };
 template <int TO>
 struct LastEpilogue {
-    float a, scale[ORTH_SHAPES];      // of the shape: with 1 / ORTH_UNIT; of the step with the learning rate
+    float lo, scale[ORTH_SHAPES];     // of the shape: with 1 / ORTH_UNIT; of the step with the learning rate
     float decay;
     void *out[ORTH_ROUND];
     float *const *table;
     int index[ORTH_ROUND];
-    __device__ static void piece(const GemmArgs<LastEpilogue> &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        Piece p{min(32, g.m - row0), min(32, g.n - col0), true};
-        if (p.rows <= 0 || p.cols <= 0) return;
+    struct Ahead {
+        uint4 v[4], x[TO == ORTH_TO_X ? 8 : 1];
+    };
+    using Args = GemmArgs<LastEpilogue>;
+    __device__ __forceinline__ static void *to(const Args &a, const GemmGroup &g, int batch) {
+        if constexpr (TO == ORTH_TO_X) return a.epi.table[a.epi.index[g.first + batch]];
+        else return a.epi.out[g.first + batch];
+    }
+    __device__ __forceinline__ static Piece piece(const GemmGroup &g, const void *out, int row0, int col0) {
+        constexpr int SIZE = TO == ORTH_TO_BF16 ? 2 : 4;
+        return piece_at(g, row0, col0, ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * SIZE)) & 15) == 0);
+    }
+    __device__ static void fetch(const Args &a, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
+        fetch16(static_cast<const __half *>(g.in[0]) + batch * g.in_batch + row0 * g.in_ld + col0, g.in_ld, piece_at(g, row0, col0, true), lane, x.v);
+        if constexpr (TO == ORTH_TO_X) {
+            const float *out = static_cast<const float *>(to(a, g, batch));
+            fetch32(out + row0 * g.out_ld + col0, g.out_ld, piece(g, out, row0, col0), lane, x.x);
+        }
+    }
+    __device__ static void settle(char *st, int lane, const Ahead &x) {
+        settle16(st, lane, x.v);
+        if constexpr (TO == ORTH_TO_X) settle32(st + GEMM_IN, lane, x.x);
+    }
+    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        void *const out = to(a, g, batch);
+        const Piece p = piece(g, out, row0, col0);
+        if (p.none()) return;
         float v[32];
-        carried(st, lane, g, batch * g.in_batch + row0 * g.in_ld + col0, p, a.epi.a, d, v);
+        carried(st, lane, g.alpha, a.epi.lo, d, v);
         const float scale = a.epi.scale[&g - a.groups];
-        const int which = g.first + batch;
         const long long at = row0 * g.out_ld + col0;
-        p.wide = false;
         if constexpr (TO == ORTH_TO_BF16) {
-            __nv_bfloat16 *const out = static_cast<__nv_bfloat16 *>(a.epi.out[which]);
-            p.wide = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * 2)) & 15) == 0;
             uint32_t w[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e] * scale, v[2 * e + 1] * scale);
-            store_piece16(st, lane, out + at, g.out_ld, p, w);
+            put16(st, lane, w);
+            __syncwarp();
+            send16(st, lane, static_cast<__nv_bfloat16 *>(out) + at, g.out_ld, p);
         } else {
-            float *const out = TO == ORTH_TO_X ? a.epi.table[a.epi.index[which]] : static_cast<float *>(a.epi.out[which]);
-            p.wide = ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * 4)) & 15) == 0;
             if constexpr (TO == ORTH_TO_X) {
                 float x[32];
-                load_piece32(st, lane, out + at, g.out_ld, p, x);
+                row32(st + GEMM_IN, lane, x);
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] = a.epi.decay * x[e] - scale * v[e];
             } else {
 #pragma unroll
                 for (int e = 0; e < 32; ++e) v[e] *= scale;
             }
-            store_piece32(st, lane, out + at, g.out_ld, p, v);
+            put32(st + GEMM_IN, lane, v);
+            __syncwarp();
+            send32(st + GEMM_IN, lane, static_cast<float *>(out) + at, g.out_ld, p);
         }
     }
 };
@@ -289,7 +342,7 @@ Round next_round(const OrthArgs &a, int first) {
         ++r.shapes[r.nshapes - 1].count;
         ++r.count;
         r.bytes += bytes;
-        tiles += tiles_of(n, n, 256, true);
+        tiles += tiles_of(n, n, GemmCut{256, false}, false, true);
     }
     return r;
 }
@@ -320,17 +373,19 @@ void sort_list(const OrthArgs &a) {
     });
 }
 
-template <typename F>
-int pick_tile_n(const Round &r, const F &tiles) {
-    int best = 0;
-    int64_t least = 0;
-    for (int n = 256; n >= 64; n /= 2) {
-        int64_t all = 0;
-        for (int i = 0; i < r.nshapes; ++i) all += static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], n);
-        const int64_t cost = (all + NUM_SMS - 1) / NUM_SMS * (n + 64);
-        if (!best || cost < least) best = n, least = cost;
+// The cut of a product of all shapes: tiles(shape, cut) of one matrix, k(shape).
+template <typename K, typename F>
+GemmCut pick(const Round &r, const K &k, const F &tiles) {
+    int64_t all = 0, sum = 0;
+    for (int i = 0; i < r.nshapes; ++i) {
+        const int64_t n = static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], GemmCut{256, true});
+        all += n, sum += n * k(r.shapes[i]);
     }
-    return best;
+    return pick_cut(false, sum / all, [&](const GemmCut &cut) {
+        int64_t n = 0;
+        for (int i = 0; i < r.nshapes; ++i) n += static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], cut);
+        return n;
+    });
 }
 
 struct Run {
@@ -339,17 +394,17 @@ struct Run {
 };
 
 // A symmetric product of `from` (x: X of this step, else G) for all shapes.
-cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b, const Run &run) {
+cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b, float diagonal, const Run &run) {
     static thread_local GemmArgs<SymEpilogue> a;
-    const int tile = pick_tile_n(r, [](const Shape &s, int t) { return tiles_of(s.n, s.n, t, true); });
-    begin_gemm(a, false, tile, false, true, 1);
-    a.epi.b = b;
+    const GemmCut cut = pick(r, [&](const Shape &s) { return gram ? s.m : s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.n, s.n, c, false, true); });
+    begin_gemm(a, false, cut, false, true, 1);
+    a.epi.b = b, a.epi.diagonal = diagonal;
     for (int i = 0; i < r.nshapes; ++i) {
         const Shape &s = r.shapes[i];
         const bool mn = gram && s.tall;
         GemmGroup &g = add_group(a, s.n, s.n, gram ? s.m : s.n, s.count);
         for (int side_b = 0; side_b < 2; ++side_b) {
-            const int box = mn ? 64 : side_b ? tile : GEMM_BM;
+            const int box = mn ? 64 : side_b ? cut.box_n(false) : GEMM_BM;
             const cudaError_t e = gram ? encode_boxes(&a.maps[2 * i + side_b], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, box)
                                        : encode_boxes(&a.maps[2 * i + side_b], s.gram, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, box);
             if (e != cudaSuccess) return e;
@@ -367,8 +422,8 @@ cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b,
 // X := a X + (polynomial of G) X, to the other side or, at last, to `epi`'s places.
 template <typename E>
 cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const long long *out_ld, const Run &run) {
-    const int tile = pick_tile_n(r, [](const Shape &s, int t) { return tiles_of(s.rows, s.cols, t, false); });
-    begin_gemm(a, false, tile, false, false, 1);
+    const GemmCut cut = pick(r, [](const Shape &s) { return s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.rows, s.cols, c, false, false); });
+    begin_gemm(a, false, cut, false, false, 1);
     a.epi = epi;
     for (int i = 0; i < r.nshapes; ++i) {
         const Shape &s = r.shapes[i];
@@ -376,12 +431,12 @@ cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const
         const int of_x = 2 * i + (s.tall ? 0 : 1), of_poly = 2 * i + (s.tall ? 1 : 0);
         cudaError_t e = encode_boxes(&a.maps[of_x], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, s.tall ? GEMM_BM : 64);
         if (e == cudaSuccess)
-            e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? tile : GEMM_BM);
+            e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? cut.box_n(false) : GEMM_BM);
         if (e != cudaSuccess) return e;
         g.a_map = static_cast<short>(2 * i), g.b_map = static_cast<short>(2 * i + 1);
         g.b_mn = !s.tall;
         g.alpha = 1.f / ORTH_UNIT;
-        g.in[0] = s.hi[side], g.in[1] = s.lo;
+        g.in[0] = s.lo;
         g.in_ld = s.ld, g.in_batch = s.rows * s.ld;
         g.out[0] = s.hi[side ^ 1], g.out[1] = s.lo;
         g.out_ld = out_ld ? out_ld[i] : s.ld;
@@ -395,7 +450,7 @@ cudaError_t last(const OrthArgs &a, const Round &r, int side, const Run &run) {
     using E = LastEpilogue<TO>;
     static thread_local GemmArgs<E> args;
     static thread_local E epi;
-    epi.a = a.coefficients[3 * (a.steps - 1)];
+    epi.lo = a.coefficients[3 * (a.steps - 1)] / ORTH_LO;
     epi.decay = a.decay;
     epi.table = a.x_table;
     long long ld[ORTH_SHAPES];
@@ -458,10 +513,10 @@ cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit,
         int side = 0;
         for (int k = 0; k < a.steps && e == cudaSuccess; ++k, side ^= 1) {
             const float *c = a.coefficients + 3 * k;
-            e = symmetric(r, true, side, 1.f / ORTH_UNIT, 0.f, run);
-            if (e == cudaSuccess) e = symmetric(r, false, side, c[2] / ORTH_UNIT, c[1], run);
+            e = symmetric(r, true, side, 1.f / ORTH_UNIT, 0.f, 0.f, run);
+            if (e == cudaSuccess) e = symmetric(r, false, side, c[2] / ORTH_UNIT, c[1], c[0] * ORTH_UNIT, run);
             if (e != cudaSuccess) break;
-            if (k + 1 < a.steps) e = update(r, side, NextEpilogue{c[0]}, next, nullptr, run);
+            if (k + 1 < a.steps) e = update(r, side, NextEpilogue{c[0] / ORTH_LO}, next, nullptr, run);
             else if (a.list[at].out == nullptr) e = last<ORTH_TO_X>(a, r, side, run);
             else e = a.out_bf16 ? last<ORTH_TO_BF16>(a, r, side, run) : last<ORTH_TO_F32>(a, r, side, run);
         }
