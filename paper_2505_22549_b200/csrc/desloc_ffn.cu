@@ -8,11 +8,13 @@ namespace desloc {
 
 namespace {
 
-__device__ __forceinline__ float sigmoid(float x) { return 1.f / (1.f + __expf(-x)); }
+// (a few units of fp32's last place: the results are rounded to bf16)
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 // ---- forward -----------------------------------------------------------------------------------------
 // z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.
 struct UpEpilogue {
+    static constexpr int STAGING = 3 * 2048;
     struct Ahead {};
     using Args = GemmArgs<UpEpilogue>;
     __device__ static void fetch(const Args &, const GemmGroup &, int, int, int, int, Ahead &) {}
@@ -20,24 +22,27 @@ struct UpEpilogue {
     __device__ static void finish(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, g.wide & 1), q = piece_at(g, row0, col0, (g.wide & 2) != 0);
         if (p.none()) return;
-        float gv[32], uv[32];
-        tmem_load32(d, gv);
-        tmem_load32(d + a.tile_n / 2, uv);
-        tmem_wait();
-        uint32_t w[16];
-        if (g.out[1]) {
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            float gv[16], uv[16];
+            tmem_load16(d + 16 * half, gv);
+            tmem_load16(d + a.tile_n / 2 + 16 * half, uv);
+            tmem_wait();
+            uint32_t w[8];
+            if (g.out[1]) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
-            put16(st + 2048, lane, w);
+                for (int e = 0; e < 8; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
+                put16(st + 2048, lane, half, w);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(uv[2 * e], uv[2 * e + 1]);
-            put16(st + 4096, lane, w);
+                for (int e = 0; e < 8; ++e) w[e] = pack_bf16(uv[2 * e], uv[2 * e + 1]);
+                put16(st + 4096, lane, half, w);
+            }
+#pragma unroll
+            for (int e = 0; e < 16; ++e) gv[e] = gv[e] * sigmoid(gv[e]) * uv[e];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
+            put16(st, lane, half, w);
         }
-#pragma unroll
-        for (int e = 0; e < 32; ++e) gv[e] = gv[e] * sigmoid(gv[e]) * uv[e];
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
-        put16(st, lane, w);
         __syncwarp();
         send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p);
         if (g.out[1]) {
@@ -51,6 +56,7 @@ struct UpEpilogue {
 // A product as it is, in bf16 or fp32, or added to what is there.
 template <bool BF16, bool ADD>
 struct StoreEpilogue {
+    static constexpr int STAGING = BF16 ? 2048 : 4096;
     struct Was {
         uint4 v[BF16 ? 4 : 8];
     };
@@ -71,42 +77,45 @@ struct StoreEpilogue {
     __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, g.wide & 1);
         if (p.none()) return;
-        float v[32];
-        tmem_load32(d, v);
-        tmem_wait();
         const long long to = row0 * g.out_ld + col0;
-        if constexpr (BF16) {
-            uint32_t w[16];
-            if constexpr (ADD) {
-                row16(st, lane, w);
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            float v[16];
+            tmem_load16(d + 16 * half, v);
+            tmem_wait();
+            if constexpr (BF16) {
+                uint32_t w[8];
+                if constexpr (ADD) {
+                    row16(st, lane, half, w);
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const float2 was = unpack_bf16(w[e]);
-                    v[2 * e] += was.x, v[2 * e + 1] += was.y;
+                    for (int e = 0; e < 8; ++e) {
+                        const float2 was = unpack_bf16(w[e]);
+                        v[2 * e] += was.x, v[2 * e + 1] += was.y;
+                    }
                 }
-            }
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            put16(st, lane, w);
-            __syncwarp();
-            send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
-        } else {
-            if constexpr (ADD) {
-                float was[32];
-                row32(st, lane, was);
+                for (int e = 0; e < 8; ++e) w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                put16(st, lane, half, w);
+            } else {
+                if constexpr (ADD) {
+                    float was[16];
+                    row32(st, lane, half, was);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] += was[e];
+                    for (int e = 0; e < 16; ++e) v[e] += was[e];
+                }
+                put32(st, lane, half, v);
             }
-            put32(st, lane, v);
-            __syncwarp();
-            send32(st, lane, static_cast<float *>(g.out[0]) + to, g.out_ld, p);
         }
+        __syncwarp();
+        if constexpr (BF16) send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
+        else send32(st, lane, static_cast<float *>(g.out[0]) + to, g.out_ld, p);
     }
 };
 
 // ---- backward ----------------------------------------------------------------------------------------
 // From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.
 struct DzEpilogue {
+    static constexpr int STAGING = 3 * 2048;
     struct Ahead {
         uint4 g[4], u[4];
     };
@@ -124,23 +133,26 @@ struct DzEpilogue {
     __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, g.wide & 1);
         if (p.none()) return;
-        uint32_t gw[16], uw[16], zw[16];
-        row16(st, lane, gw);
-        row16(st + 2048, lane, uw);
-        float v[32];
-        tmem_load32(d, v);
-        tmem_wait();
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            uint32_t gw[8], uw[8], zw[8];
+            float v[16];
+            tmem_load16(d + 16 * half, v);
+            row16(st, lane, half, gw);
+            row16(st + 2048, lane, half, uw);
+            tmem_wait();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const float2 gg = unpack_bf16(gw[e]), uu = unpack_bf16(uw[e]);
-            const float sx = sigmoid(gg.x), sy = sigmoid(gg.y), ax = gg.x * sx, ay = gg.y * sy;
-            zw[e] = pack_bf16(ax * uu.x, ay * uu.y);
-            gw[e] = pack_bf16(v[2 * e] * uu.x * (sx + ax * (1.f - sx)), v[2 * e + 1] * uu.y * (sy + ay * (1.f - sy)));
-            uw[e] = pack_bf16(v[2 * e] * ax, v[2 * e + 1] * ay);
+            for (int e = 0; e < 8; ++e) {
+                const float2 gg = unpack_bf16(gw[e]), uu = unpack_bf16(uw[e]);
+                const float sx = sigmoid(gg.x), sy = sigmoid(gg.y), ax = gg.x * sx, ay = gg.y * sy;
+                zw[e] = pack_bf16(ax * uu.x, ay * uu.y);
+                gw[e] = pack_bf16(v[2 * e] * uu.x * (sx + ax * (1.f - sx)), v[2 * e + 1] * uu.y * (sy + ay * (1.f - sy)));
+                uw[e] = pack_bf16(v[2 * e] * ax, v[2 * e + 1] * ay);
+            }
+            put16(st, lane, half, gw);
+            put16(st + 2048, lane, half, uw);
+            put16(st + 4096, lane, half, zw);
         }
-        put16(st, lane, gw);   // (each lane where it has read)
-        put16(st + 2048, lane, uw);
-        put16(st + 4096, lane, zw);
         __syncwarp();
         const long long to = row0 * g.out_ld + col0;
         send16(st + 4096, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);

@@ -5,7 +5,7 @@
 // (rows of m or n, a k each): the copies bring 128-byte swizzled boxes of either kind, and the matrix instruction takes both, so nothing is
 // ever transposed in memory.  What lies outside a matrix is zeros, filled in by the copy engine.
 //
-// One block per SM, persistent: a warp requests boxes (TMA) into a ring of stages, a thread issues the products, eight warps empty one of two
+// One block per SM, persistent: a warp requests boxes (TMA) into a ring of stages, a thread issues the products, sixteen warps empty one of two
 // accumulators while the other is being filled, and fetch what they need from memory a piece ahead.
 //
 // Blocks work alone (128 rows of C a tile) or in pairs (256 rows; each brings its own 128 rows of A and half of B, and the tensor cores of both read both
@@ -23,9 +23,8 @@
 
 namespace desloc {
 
-constexpr int GEMM_BM = 128, GEMM_BK = 64, GEMM_MAX_STAGES = 8, GEMM_EPI_WARPS = 8, GEMM_THREADS = 128 + 32 * GEMM_EPI_WARPS;
+constexpr int GEMM_BM = 128, GEMM_BK = 64, GEMM_MAX_STAGES = 8, GEMM_EPI_WARPS = 16, GEMM_THREADS = 128 + 32 * GEMM_EPI_WARPS;
 constexpr int GEMM_A_BYTES = GEMM_BM * GEMM_BK * 2;
-constexpr int GEMM_IN = 4096, GEMM_STAGING = 2 * GEMM_IN;   // of every warp that empties accumulators: pieces that come, pieces that go
 constexpr int GEMM_SMEM = 227 * 1024 - 2048, GEMM_MAX_GROUPS = 48, GEMM_MAX_MAPS = 64, GEMM_DRAIN_LIMIT = 1 << 22;
 
 // A number of matrices of the same sizes, or a worker's.
@@ -120,132 +119,156 @@ __device__ __forceinline__ bool elect_one() {
 __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
-// 32 columns of this warp's 32 rows: a row per lane.
-__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+// 16 columns of this warp's 32 rows: a row per lane.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&v)[16]) {
     uint32_t *r = reinterpret_cast<uint32_t *>(v);
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,"
-                 "%25,%26,%27,%28,%29,%30,%31}, [%32];"
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]),
-                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
-                   "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]),
-                   "=r"(r[31])
+                   "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
                  : "r"(addr));
 }
 __device__ __forceinline__ void tmem_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- a warp's 32 x 32 pieces between rows in lanes and rows in memory --------------------------------
 // Staged so that global memory sees whole runs of a row: 16-bit values 64 bytes (four lanes), fp32 values 128 bytes (eight lanes).  16-byte pieces change
-// places by their row, so that neither side meets bank conflicts.
+// places by their row, so that neither side meets bank conflicts.  Rows in lanes are taken 16 columns at a time, half 0 and half 1: sixteen warps, which it takes to hide the
+// latencies of all this, leave 96 registers a thread.
 struct Piece {
     int rows, cols;   // how much of it lies inside
     bool wide;        // rows begin on 16-byte boundaries
     __device__ __forceinline__ bool none() const { return rows <= 0 || cols <= 0; }
+    __device__ __forceinline__ bool whole() const { return wide && rows == 32 && cols == 32; }
 };
 __device__ __forceinline__ Piece piece_at(const GemmGroup &g, int row0, int col0, bool wide) { return {min(32, g.m - row0), min(32, g.n - col0), wide}; }
 
-// f(number, row, column, place in the staging area) for the lane's 16 bytes each
-template <typename F>
-__device__ __forceinline__ void visit16(const Piece &p, int lane, const F &f) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = 8 * i + (lane >> 2), c = lane & 3;
-        if (row < p.rows && 8 * c < p.cols) f(i, row, 8 * c, row * 64 + ((c ^ ((row >> 1) & 3)) << 4));
-    }
-}
-template <typename F>
-__device__ __forceinline__ void visit32(const Piece &p, int lane, const F &f) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = 4 * i + (lane >> 3), c = lane & 7;
-        if (row < p.rows && 4 * c < p.cols) f(i, row, 4 * c, row * 128 + ((c ^ (row & 7)) << 4));
-    }
-}
+// The lane's 16 bytes of row 8 i + lane / 4 (16 bits) or 4 i + lane / 8 (fp32), where they are staged.
+__device__ __forceinline__ int spot16(int lane, int i) { return (8 * i + (lane >> 2)) * 64 + (((lane & 3) ^ ((lane >> 3) & 3)) << 4); }
+__device__ __forceinline__ int spot32(int lane, int i) { return (4 * i + (lane >> 3)) * 128 + (((lane & 7) ^ ((4 * i + (lane >> 3)) & 7)) << 4); }
+// Bytes [16 c, 16 c + 16) of the lane's own row.
 __device__ __forceinline__ int place16(int lane, int c) { return lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4); }
 __device__ __forceinline__ int place32(int lane, int c) { return lane * 128 + ((c ^ (lane & 7)) << 4); }
 
 // memory -> registers, as it lies there
 __device__ __forceinline__ void fetch16(const void *from, long long ld, const Piece &p, int lane, uint4 (&v)[4]) {
-    const unsigned short *src = static_cast<const unsigned short *>(from);
-    visit16(p, lane, [&](int i, int row, int col, int) {
-        if (p.wide && col + 8 <= p.cols) {
-            v[i] = *reinterpret_cast<const uint4 *>(src + row * ld + col);
+    const unsigned short *src = static_cast<const unsigned short *>(from) + (lane >> 2) * ld + 8 * (lane & 3);
+    if (p.whole()) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4 *>(src + 8 * i * ld);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = p.cols - 8 * (lane & 3);
+        if (8 * i + (lane >> 2) >= p.rows || left <= 0) continue;
+        if (p.wide && left >= 8) {
+            v[i] = *reinterpret_cast<const uint4 *>(src + 8 * i * ld);
         } else {
             uint32_t h[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) h[e] = col + e < p.cols ? src[row * ld + col + e] : 0;
+            for (int e = 0; e < 8; ++e) h[e] = e < left ? src[8 * i * ld + e] : 0;
             v[i] = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
         }
-    });
+    }
 }
-__device__ __forceinline__ void fetch32(const float *src, long long ld, const Piece &p, int lane, uint4 (&v)[8]) {
-    visit32(p, lane, [&](int i, int row, int col, int) {
-        if (p.wide && col + 4 <= p.cols) {
-            v[i] = *reinterpret_cast<const uint4 *>(src + row * ld + col);
+__device__ __forceinline__ void fetch32(const float *from, long long ld, const Piece &p, int lane, uint4 (&v)[8]) {
+    const float *src = from + (lane >> 3) * ld + 4 * (lane & 7);
+    if (p.whole()) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const uint4 *>(src + 4 * i * ld);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int left = p.cols - 4 * (lane & 7);
+        if (4 * i + (lane >> 3) >= p.rows || left <= 0) continue;
+        if (p.wide && left >= 4) {
+            v[i] = *reinterpret_cast<const uint4 *>(src + 4 * i * ld);
         } else {
             uint32_t h[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) h[e] = col + e < p.cols ? __float_as_uint(src[row * ld + col + e]) : 0;
+            for (int e = 0; e < 4; ++e) h[e] = e < left ? __float_as_uint(src[4 * i * ld + e]) : 0;
             v[i] = make_uint4(h[0], h[1], h[2], h[3]);
         }
-    });
+    }
 }
 // registers -> staging area, whence each lane reads its row (behind a __syncwarp())
 __device__ __forceinline__ void settle16(char *st, int lane, const uint4 (&v)[4]) {
-    visit16({32, 32, true}, lane, [&](int i, int, int, int at) { *reinterpret_cast<uint4 *>(st + at) = v[i]; });
+#pragma unroll
+    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(st + spot16(lane, i)) = v[i];
 }
 __device__ __forceinline__ void settle32(char *st, int lane, const uint4 (&v)[8]) {
-    visit32({32, 32, true}, lane, [&](int i, int, int, int at) { *reinterpret_cast<uint4 *>(st + at) = v[i]; });
-}
-__device__ __forceinline__ void row16(const char *st, int lane, uint32_t (&w)[16]) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(st + place16(lane, c));
+    for (int i = 0; i < 8; ++i) *reinterpret_cast<uint4 *>(st + spot32(lane, i)) = v[i];
+}
+__device__ __forceinline__ void row16(const char *st, int lane, int half, uint32_t (&w)[8]) {
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(st + place16(lane, 2 * half + c));
         w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
     }
 }
-__device__ __forceinline__ void row32(const char *st, int lane, float (&v)[32]) {
+__device__ __forceinline__ void row32(const char *st, int lane, int half, float (&v)[16]) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-        const float4 x = *reinterpret_cast<const float4 *>(st + place32(lane, c));
+    for (int c = 0; c < 4; ++c) {
+        const float4 x = *reinterpret_cast<const float4 *>(st + place32(lane, 4 * half + c));
         v[4 * c] = x.x, v[4 * c + 1] = x.y, v[4 * c + 2] = x.z, v[4 * c + 3] = x.w;
     }
 }
-// rows in lanes -> staging area
-__device__ __forceinline__ void put16(char *st, int lane, const uint32_t (&w)[16]) {
+// rows in lanes -> staging area (a lane may put where it has read)
+__device__ __forceinline__ void put16(char *st, int lane, int half, const uint32_t (&w)[8]) {
 #pragma unroll
-    for (int c = 0; c < 4; ++c) *reinterpret_cast<uint4 *>(st + place16(lane, c)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+    for (int c = 0; c < 2; ++c)
+        *reinterpret_cast<uint4 *>(st + place16(lane, 2 * half + c)) = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
 }
-__device__ __forceinline__ void put32(char *st, int lane, const float (&v)[32]) {
+__device__ __forceinline__ void put32(char *st, int lane, int half, const float (&v)[16]) {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) *reinterpret_cast<float4 *>(st + place32(lane, c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+    for (int c = 0; c < 4; ++c)
+        *reinterpret_cast<float4 *>(st + place32(lane, 4 * half + c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
 }
 // staging area -> memory (behind a __syncwarp())
 __device__ __forceinline__ void send16(const char *st, int lane, void *to, long long ld, const Piece &p) {
-    unsigned short *dst = static_cast<unsigned short *>(to);
-    visit16(p, lane, [&](int, int row, int col, int at) {
-        const uint4 v = *reinterpret_cast<const uint4 *>(st + at);
-        if (p.wide && col + 8 <= p.cols) {
-            *reinterpret_cast<uint4 *>(dst + row * ld + col) = v;
+    unsigned short *dst = static_cast<unsigned short *>(to) + (lane >> 2) * ld + 8 * (lane & 3);
+    if (p.whole()) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(dst + 8 * i * ld) = *reinterpret_cast<const uint4 *>(st + spot16(lane, i));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int left = p.cols - 8 * (lane & 3);
+        if (8 * i + (lane >> 2) >= p.rows || left <= 0) continue;
+        const uint4 v = *reinterpret_cast<const uint4 *>(st + spot16(lane, i));
+        if (p.wide && left >= 8) {
+            *reinterpret_cast<uint4 *>(dst + 8 * i * ld) = v;
         } else {
             const uint32_t h[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
             for (int e = 0; e < 8; ++e)
-                if (col + e < p.cols) dst[row * ld + col + e] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
+                if (e < left) dst[8 * i * ld + e] = static_cast<unsigned short>(h[e / 2] >> (16 * (e & 1)));
         }
-    });
+    }
 }
-__device__ __forceinline__ void send32(const char *st, int lane, float *dst, long long ld, const Piece &p) {
-    visit32(p, lane, [&](int, int row, int col, int at) {
-        const float4 x = *reinterpret_cast<const float4 *>(st + at);
-        if (p.wide && col + 4 <= p.cols) {
-            *reinterpret_cast<float4 *>(dst + row * ld + col) = x;
+__device__ __forceinline__ void send32(const char *st, int lane, float *to, long long ld, const Piece &p) {
+    float *dst = to + (lane >> 3) * ld + 4 * (lane & 7);
+    if (p.whole()) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(dst + 4 * i * ld) = *reinterpret_cast<const float4 *>(st + spot32(lane, i));
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int left = p.cols - 4 * (lane & 7);
+        if (4 * i + (lane >> 3) >= p.rows || left <= 0) continue;
+        const float4 x = *reinterpret_cast<const float4 *>(st + spot32(lane, i));
+        if (p.wide && left >= 4) {
+            *reinterpret_cast<float4 *>(dst + 4 * i * ld) = x;
         } else {
             const float h[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (col + e < p.cols) dst[row * ld + col + e] = h[e];
+                if (e < left) dst[4 * i * ld + e] = h[e];
         }
-    });
+    }
 }
 
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
@@ -283,7 +306,7 @@ struct TileWalk {
 };
 
 // E, the epilogue, takes 32 x 32 pieces: of what it reads, E::Ahead is fetched one piece ahead by E::fetch(args, group, batch, row, column, lane, ahead), put into the staging area
-// by E::settle(staging, lane, ahead), and E::finish(args, group, batch, row, column, accumulator, staging, lane) does the rest.
+// by E::settle(staging, lane, ahead), and E::finish(args, group, batch, row, column, accumulator, staging, lane) does the rest.  E::STAGING: bytes of that area, a warp's.
 template <typename E, int CG>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs<E> a) {
     extern __shared__ __align__(1024) char gemm_smem[];
@@ -411,8 +434,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         }
         __syncwarp();
     } else if (warp >= 4) {
+        constexpr int STEP = GEMM_EPI_WARPS / 4 * 32;   // columns that the warps take at a time
         const int quadrant = warp & 3, c0 = (warp - 4) / 4 * 32;
-        char *const st = ring + a.stages * stage_bytes + (warp - 4) * GEMM_STAGING;
+        char *const st = ring + a.stages * stage_bytes + (warp - 4) * E::STAGING;
         const int out_n = a.dual ? a.tile_n / 2 : a.tile_n;
         const int rows = (rank * 4 + quadrant) * 32;
         TileWalk at;
@@ -422,7 +446,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         const GemmGroup *g = nullptr;
         if (tile < a.tiles) {
             g = &at.find<CG>(a, tile);
-            E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
+            if (c0 < out_n) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
         }
         while (tile < a.tiles) {
             if (c == c0) {
@@ -437,15 +461,15 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             const uint32_t d = tmem + buf * 256 + c + (static_cast<uint32_t>(32 * quadrant) << 16);
             __syncwarp();   // (the piece before has been read)
             E::settle(st, lane, ahead);
-            c += 64;
+            c += STEP;
             const bool last = c >= out_n;
             if (last) {
                 c = c0, tile += tile_step;
                 if (tile < a.tiles) g = &at.find<CG>(a, tile);
             }
-            if (tile < a.tiles) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
+            if (tile < a.tiles && c0 < out_n) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
             __syncwarp();
-            E::finish(a, here, batch, row0, col0, d, st, lane);
+            if (c0 < out_n) E::finish(a, here, batch, row0, col0, d, st, lane);
             if (last) {
                 tmem_fence_before();
                 __syncwarp();
@@ -520,7 +544,7 @@ inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric)
     return all;
 }
 // The cut that is done first: rounds of tiles, a tile as long as its products (in cycles for 64 k: what they take, or what shared memory takes to be written and read), or as
-// emptying it (some 800 cycles for the 64 columns that the warps take at a time).  tiles(cut): how many there are, all with k of about `k`.
+// emptying it (some 900 cycles for the 128 columns that the warps take at a time).  tiles(cut): how many there are, all with k of about `k`.
 template <typename F>
 GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
     GemmCut best{};
@@ -529,7 +553,7 @@ GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
         for (int n = 256; n >= (dual || pairs ? 128 : 64); n -= 64) {
             const GemmCut cut{n, pairs != 0};
             const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, rounds = (tiles(cut) + slots - 1) / slots;
-            const int64_t step = pairs ? std::max(2 * n, 256 + n) : 256 + 2 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 63) / 64 * 800;
+            const int64_t step = pairs ? std::max(2 * n, 256 + n) : 256 + 2 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 900;
             const int64_t cost = rounds * (std::max(products, empty) + 200) + empty;
             if (!best.tile_n || cost < least) best = cut, least = cost;
         }
@@ -575,11 +599,11 @@ cudaError_t launch_gemm(GemmArgs<E> &a, cudaStream_t stream) {
     const cudaError_t e = gemm_ready<E, CG>();
     if (e != cudaSuccess) return e;
     const int stage = GEMM_A_BYTES + (a.tile_n / CG + 63) / 64 * 64 * GEMM_BK * 2;
-    a.stages = std::min(GEMM_MAX_STAGES, (GEMM_SMEM - 1024 - GEMM_EPI_WARPS * GEMM_STAGING) / stage);
+    a.stages = std::min(GEMM_MAX_STAGES, (GEMM_SMEM - 1024 - GEMM_EPI_WARPS * E::STAGING) / stage);
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3(static_cast<unsigned>(CG * std::min(a.tiles, NUM_SMS / CG)));
     lc.blockDim = dim3(GEMM_THREADS);
-    lc.dynamicSmemBytes = 1024 + static_cast<size_t>(a.stages) * stage + GEMM_EPI_WARPS * GEMM_STAGING;
+    lc.dynamicSmemBytes = 1024 + static_cast<size_t>(a.stages) * stage + GEMM_EPI_WARPS * E::STAGING;
     lc.stream = stream;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -135,6 +135,7 @@ __global__ void __launch_bounds__(ORTH_THREADS) orth_scale_kernel(const __grid_c
 // ---- the products' epilogues -------------------------------------------------------------------------
 // A symmetric result: alpha times the sums, plus b times in[0], plus `diagonal` there; pieces below the diagonal go to the other one's place, too.
 struct SymEpilogue {
+    static constexpr int STAGING = 2048;
     float b, diagonal;
     struct Ahead {
         uint4 v[4];
@@ -149,61 +150,63 @@ struct SymEpilogue {
         const Piece p = piece_at(g, row0, col0, true);
         if (p.none() || col0 > row0) return;
         __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
-        float v[32];
-        uint32_t w[16];
-        if (g.in[0]) row16(st, lane, w);
-        tmem_load32(d, v);
-        tmem_wait();
+        // Columns of a piece below the diagonal are rows of the other one (p.cols is 32 there).  Neighbouring lanes, neighbouring rows of this piece, make words: the even
+        // one of the even column, the odd one of the odd column.
+        const bool odd = lane & 1, both = (lane | 1) < p.rows, one = (lane & ~1) < p.rows;
+        uint32_t *t = reinterpret_cast<uint32_t *>(out + (col0 + odd) * g.out_ld + row0 + (lane & ~1));
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            float v[16];
+            uint32_t w[8];
+            tmem_load16(d + 16 * half, v);
+            if (g.in[0]) row16(st, lane, half, w);
+            tmem_wait();
 #pragma unroll
-        for (int e = 0; e < 32; ++e) v[e] *= g.alpha;
-        if (g.in[0]) {
+            for (int e = 0; e < 16; ++e) v[e] *= g.alpha;
+            if (g.in[0]) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const float2 x = unpack_f16(w[e]);
-                v[2 * e] += a.epi.b * x.x, v[2 * e + 1] += a.epi.b * x.y;
+                for (int e = 0; e < 8; ++e) {
+                    const float2 x = unpack_f16(w[e]);
+                    v[2 * e] += a.epi.b * x.x, v[2 * e + 1] += a.epi.b * x.y;
+                }
+                if (col0 == row0) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] += e + 16 * half == lane ? a.epi.diagonal : 0.f;
+                }
             }
-            if (col0 == row0) {
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] += e == lane ? a.epi.diagonal : 0.f;
+            for (int e = 0; e < 8; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+            put16(st, lane, half, w);
+            if (col0 < row0) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e, t += g.out_ld) {   // (two columns on: 2 ld halves)
+                    const uint32_t other = __shfl_xor_sync(0xffffffffu, w[e], 1);
+                    const uint32_t pair = odd ? __byte_perm(other, w[e], 0x7632) : __byte_perm(w[e], other, 0x5410);
+                    if (both) *t = pair;
+                    else if (one) *reinterpret_cast<unsigned short *>(t) = static_cast<unsigned short>(pair);
+                }
             }
         }
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = pack_f16(v[2 * e], v[2 * e + 1]);
-        put16(st, lane, w);
         __syncwarp();
         send16(st, lane, out + row0 * g.out_ld + col0, g.out_ld, p);
-        if (col0 < row0) {
-            // Columns of the one are rows of the other (p.cols is 32 here).  Neighbouring lanes, neighbouring rows of this piece, make words: the even one of the
-            // even column, the odd one of the odd column.
-            const bool odd = lane & 1;
-            uint32_t *const t = reinterpret_cast<uint32_t *>(out + (col0 + odd) * g.out_ld + row0 + (lane & ~1));
-            const bool both = (lane | 1) < p.rows, one = (lane & ~1) < p.rows;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const uint32_t other = __shfl_xor_sync(0xffffffffu, w[e], 1);
-                const uint32_t pair = odd ? __byte_perm(other, w[e], 0x7632) : __byte_perm(w[e], other, 0x5410);
-                uint32_t *const to = t + e * g.out_ld;   // (two columns on: 2 ld halves)
-                if (both) *to = pair;
-                else if (one) *reinterpret_cast<unsigned short *>(to) = static_cast<unsigned short>(pair);
-            }
-        }
     }
 };
 
 // X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
-__device__ __forceinline__ void carried(const char *st, int lane, float alpha, float lo, uint32_t d, float (&v)[32]) {
-    uint32_t w[16];
-    row16(st, lane, w);
-    tmem_load32(d, v);
+__device__ __forceinline__ void carried(const char *st, int lane, int half, float alpha, float lo, uint32_t d, float (&v)[16]) {
+    uint32_t w[8];
+    tmem_load16(d + 16 * half, v);
+    row16(st, lane, half, w);
     tmem_wait();
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
+    for (int e = 0; e < 8; ++e) {
         const float2 l = unpack_f16(w[e]);
         v[2 * e] = v[2 * e] * alpha + lo * l.x, v[2 * e + 1] = v[2 * e + 1] * alpha + lo * l.y;
     }
 }
 
 struct NextEpilogue {
+    static constexpr int STAGING = 2 * 2048;
     float lo;
     struct Ahead {
         uint4 v[4];
@@ -216,17 +219,20 @@ struct NextEpilogue {
     __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, true);
         if (p.none()) return;
-        float v[32];
-        carried(st, lane, g.alpha, a.epi.lo, d, v);
-        uint32_t hi[16], lo[16];
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            float v[16];
+            carried(st, lane, half, g.alpha, a.epi.lo, d, v);
+            uint32_t hi[8], lo[8];
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
-            const float2 h = unpack_f16(hi[e]);
-            lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
+            for (int e = 0; e < 8; ++e) {
+                hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
+                const float2 h = unpack_f16(hi[e]);
+                lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
+            }
+            put16(st, lane, half, lo);
+            put16(st + 2048, lane, half, hi);
         }
-        put16(st, lane, lo);   // (each lane where it has read)
-        put16(st + 2048, lane, hi);
         __syncwarp();
         const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
         send16(st + 2048, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p);
@@ -238,6 +244,7 @@ struct NextEpilogue {
 enum { ORTH_TO_F32 = 0, ORTH_TO_BF16 = 1, ORTH_TO_X = 2 };
 template <int TO>
 struct LastEpilogue {
+    static constexpr int STAGING = TO == ORTH_TO_BF16 ? 2048 : 2048 + 4096, WIDE = 2048;   // where fp32 pieces are
     float lo, scale[ORTH_SHAPES];     // of the shape: with 1 / ORTH_UNIT; of the step with the learning rate
     float decay;
     void *out[ORTH_ROUND];
@@ -264,37 +271,39 @@ struct LastEpilogue {
     }
     __device__ static void settle(char *st, int lane, const Ahead &x) {
         settle16(st, lane, x.v);
-        if constexpr (TO == ORTH_TO_X) settle32(st + GEMM_IN, lane, x.x);
+        if constexpr (TO == ORTH_TO_X) settle32(st + WIDE, lane, x.x);
     }
     __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         void *const out = to(a, g, batch);
         const Piece p = piece(g, out, row0, col0);
         if (p.none()) return;
-        float v[32];
-        carried(st, lane, g.alpha, a.epi.lo, d, v);
         const float scale = a.epi.scale[&g - a.groups];
         const long long at = row0 * g.out_ld + col0;
-        if constexpr (TO == ORTH_TO_BF16) {
-            uint32_t w[16];
+#pragma unroll 1
+        for (int half = 0; half < 2; ++half) {
+            float v[16];
+            carried(st, lane, half, g.alpha, a.epi.lo, d, v);
+            if constexpr (TO == ORTH_TO_BF16) {
+                uint32_t w[8];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) w[e] = pack_bf16(v[2 * e] * scale, v[2 * e + 1] * scale);
-            put16(st, lane, w);
-            __syncwarp();
-            send16(st, lane, static_cast<__nv_bfloat16 *>(out) + at, g.out_ld, p);
-        } else {
-            if constexpr (TO == ORTH_TO_X) {
-                float x[32];
-                row32(st + GEMM_IN, lane, x);
-#pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] = a.epi.decay * x[e] - scale * v[e];
+                for (int e = 0; e < 8; ++e) w[e] = pack_bf16(v[2 * e] * scale, v[2 * e + 1] * scale);
+                put16(st, lane, half, w);
             } else {
+                if constexpr (TO == ORTH_TO_X) {
+                    float x[16];
+                    row32(st + WIDE, lane, half, x);
 #pragma unroll
-                for (int e = 0; e < 32; ++e) v[e] *= scale;
+                    for (int e = 0; e < 16; ++e) v[e] = a.epi.decay * x[e] - scale * v[e];
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) v[e] *= scale;
+                }
+                put32(st + WIDE, lane, half, v);
             }
-            put32(st + GEMM_IN, lane, v);
-            __syncwarp();
-            send32(st + GEMM_IN, lane, static_cast<float *>(out) + at, g.out_ld, p);
         }
+        __syncwarp();
+        if constexpr (TO == ORTH_TO_BF16) send16(st, lane, static_cast<__nv_bfloat16 *>(out) + at, g.out_ld, p);
+        else send32(st + WIDE, lane, static_cast<float *>(out) + at, g.out_ld, p);
     }
 };
 
