@@ -19,9 +19,8 @@ struct UpEpilogue {
     using Args = GemmArgs<UpEpilogue>;
     __device__ static void fetch(const Args &, const GemmGroup &, int, int, int, int, Ahead &) {}
     __device__ static void settle(char *, int, const Ahead &) {}
-    __device__ static void finish(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p = piece_at(g, row0, col0, g.wide & 1), q = piece_at(g, row0, col0, (g.wide & 2) != 0);
-        if (p.none()) return;
+    __device__ static void drain(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        if (piece_at(g, row0, col0, true).none()) return;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float gv[16], uv[16];
@@ -43,7 +42,9 @@ struct UpEpilogue {
             for (int e = 0; e < 8; ++e) w[e] = pack_bf16(gv[2 * e], gv[2 * e + 1]);
             put16(st, lane, half, w);
         }
-        __syncwarp();
+    }
+    __device__ static void send(const Args &, const GemmGroup &g, int, int row0, int col0, const char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1), q = piece_at(g, row0, col0, (g.wide & 2) != 0);
         send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p);
         if (g.out[1]) {
             const long long kept = row0 * g.in_ld + col0;
@@ -74,10 +75,8 @@ struct StoreEpilogue {
         if constexpr (ADD && BF16) settle16(st, lane, x.v);
         else if constexpr (ADD) settle32(st, lane, x.v);
     }
-    __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p = piece_at(g, row0, col0, g.wide & 1);
-        if (p.none()) return;
-        const long long to = row0 * g.out_ld + col0;
+    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        if (piece_at(g, row0, col0, true).none()) return;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float v[16];
@@ -106,7 +105,10 @@ struct StoreEpilogue {
                 put32(st, lane, half, v);
             }
         }
-        __syncwarp();
+    }
+    __device__ static void send(const Args &, const GemmGroup &g, int, int row0, int col0, const char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1);
+        const long long to = row0 * g.out_ld + col0;
         if constexpr (BF16) send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
         else send32(st, lane, static_cast<float *>(g.out[0]) + to, g.out_ld, p);
     }
@@ -130,9 +132,8 @@ struct DzEpilogue {
         settle16(st, lane, x.g);
         settle16(st + 2048, lane, x.u);
     }
-    __device__ static void finish(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p = piece_at(g, row0, col0, g.wide & 1);
-        if (p.none()) return;
+    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
+        if (piece_at(g, row0, col0, true).none()) return;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             uint32_t gw[8], uw[8], zw[8];
@@ -153,7 +154,9 @@ struct DzEpilogue {
             put16(st + 2048, lane, half, uw);
             put16(st + 4096, lane, half, zw);
         }
-        __syncwarp();
+    }
+    __device__ static void send(const Args &, const GemmGroup &g, int, int row0, int col0, const char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, g.wide & 1);
         const long long to = row0 * g.out_ld + col0;
         send16(st + 4096, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + to, g.out_ld, p);
         send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[1]) + to, g.out_ld, p);

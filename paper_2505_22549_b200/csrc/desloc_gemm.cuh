@@ -306,7 +306,8 @@ struct TileWalk {
 };
 
 // E, the epilogue, takes 32 x 32 pieces: of what it reads, E::Ahead is fetched one piece ahead by E::fetch(args, group, batch, row, column, lane, ahead), put into the staging area
-// by E::settle(staging, lane, ahead), and E::finish(args, group, batch, row, column, accumulator, staging, lane) does the rest.  E::STAGING: bytes of that area, a warp's.
+// by E::settle(staging, lane, ahead); E::drain(args, group, batch, row, column, accumulator, staging, lane) takes it and the sums, and leaves what E::send(args, group, batch, row,
+// column, staging, lane) writes.  E::STAGING: bytes of that area, a warp's.
 template <typename E, int CG>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs<E> a) {
     extern __shared__ __align__(1024) char gemm_smem[];
@@ -469,17 +470,19 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             }
             if (tile < a.tiles && c0 < out_n) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
             __syncwarp();
-            if (c0 < out_n) E::finish(a, here, batch, row0, col0, d, st, lane);
+            if (c0 < out_n) E::drain(a, here, batch, row0, col0, d, st, lane);
+            tmem_fence_before();
+            __syncwarp();
             if (last) {
-                tmem_fence_before();
-                __syncwarp();
+                // (no more than that the accumulator has been read is told: a release to the other block would wait for this warp's stores)
                 if (lane == 0) {
                     if constexpr (CG == 1) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" :: "r"(smem_u32(&taken[buf])) : "memory");
-                    else asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" :: "r"(first_blocks<CG>(&taken[buf])) : "memory");
+                    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" :: "r"(first_blocks<CG>(&taken[buf])) : "memory");
                 }
                 buf ^= 1;
                 if (buf == 0) turn ^= 1;
             }
+            if (c0 < out_n) E::send(a, here, batch, row0, col0, st, lane);
         }
         __syncwarp();
     }
@@ -543,8 +546,9 @@ inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric)
     for (int i = 0; i < mt; ++i) all += std::min((i * bm + bm - 1) / tile_n + 1, nt);
     return all;
 }
-// The cut that is done first: rounds of tiles, a tile as long as its products (in cycles for 64 k: what they take, or what shared memory takes to be written and read), or as
-// emptying it (some 900 cycles for the 128 columns that the warps take at a time).  tiles(cut): how many there are, all with k of about `k`.
+// The cut that is done first: rounds of tiles, a tile as long as bringing and multiplying 64 k takes (measured, in cycles: 900 for 256 columns and 780 for 192 of a pair, 1000 for 256 of a
+// block alone, 600 for 128), or as emptying it (some 1500 for the 128 columns that the warps take at a time); and what a launch of a round takes before and behind.
+// tiles(cut): how many there are, all with k of about `k`.
 template <typename F>
 GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
     GemmCut best{};
@@ -553,8 +557,8 @@ GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
         for (int n = 256; n >= (dual || pairs ? 128 : 64); n -= 64) {
             const GemmCut cut{n, pairs != 0};
             const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, rounds = (tiles(cut) + slots - 1) / slots;
-            const int64_t step = pairs ? std::max(2 * n, 256 + n) : 256 + 2 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 900;
-            const int64_t cost = rounds * (std::max(products, empty) + 200) + empty;
+            const int64_t step = pairs ? 440 + 9 * n / 5 : 240 + 3 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 1500;
+            const int64_t cost = rounds * (std::max(products, empty) + 200) + std::min(products, empty);
             if (!best.tile_n || cost < least) best = cut, least = cost;
         }
     return best;

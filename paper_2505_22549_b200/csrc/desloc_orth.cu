@@ -17,7 +17,7 @@ namespace {
 // next.  Off by 0.15 % for normal matrices, 0.03 % for few directions.
 // Everything is held times ORTH_UNIT: singular values stay below two, entries far below one.
 constexpr float ORTH_UNIT = 256.f, ORTH_LO = 2048.f;
-constexpr int ORTH_ROUND = 128, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
+constexpr int ORTH_ROUND = 256, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
 constexpr int ORTH_THREADS = 256, ORTH_WARPS = ORTH_THREADS / 32;
 
 struct Sources {
@@ -146,7 +146,7 @@ struct SymEpilogue {
             fetch16(static_cast<const __half *>(g.in[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true), lane, x.v);
     }
     __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
-    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, true);
         if (p.none() || col0 > row0) return;
         __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
@@ -187,8 +187,10 @@ struct SymEpilogue {
                 }
             }
         }
-        __syncwarp();
-        send16(st, lane, out + row0 * g.out_ld + col0, g.out_ld, p);
+    }
+    __device__ static void send(const Args &, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
+        if (col0 <= row0)
+            send16(st, lane, static_cast<__half *>(g.out[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true));
     }
 };
 
@@ -216,9 +218,8 @@ struct NextEpilogue {
         fetch16(static_cast<const __half *>(g.in[0]) + batch * g.in_batch + row0 * g.in_ld + col0, g.in_ld, piece_at(g, row0, col0, true), lane, x.v);
     }
     __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
-    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        const Piece p = piece_at(g, row0, col0, true);
-        if (p.none()) return;
+    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        if (piece_at(g, row0, col0, true).none()) return;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float v[16];
@@ -233,7 +234,9 @@ struct NextEpilogue {
             put16(st, lane, half, lo);
             put16(st + 2048, lane, half, hi);
         }
-        __syncwarp();
+    }
+    __device__ static void send(const Args &, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
+        const Piece p = piece_at(g, row0, col0, true);
         const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
         send16(st + 2048, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p);
         send16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p);
@@ -273,12 +276,9 @@ struct LastEpilogue {
         settle16(st, lane, x.v);
         if constexpr (TO == ORTH_TO_X) settle32(st + WIDE, lane, x.x);
     }
-    __device__ static void finish(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        void *const out = to(a, g, batch);
-        const Piece p = piece(g, out, row0, col0);
-        if (p.none()) return;
+    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+        if (piece_at(g, row0, col0, true).none()) return;
         const float scale = a.epi.scale[&g - a.groups];
-        const long long at = row0 * g.out_ld + col0;
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float v[16];
@@ -301,7 +301,11 @@ struct LastEpilogue {
                 put32(st + WIDE, lane, half, v);
             }
         }
-        __syncwarp();
+    }
+    __device__ static void send(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
+        void *const out = to(a, g, batch);
+        const Piece p = piece(g, out, row0, col0);
+        const long long at = row0 * g.out_ld + col0;
         if constexpr (TO == ORTH_TO_BF16) send16(st, lane, static_cast<__nv_bfloat16 *>(out) + at, g.out_ld, p);
         else send32(st + WIDE, lane, static_cast<float *>(out) + at, g.out_ld, p);
     }
@@ -329,29 +333,31 @@ int64_t matrix_bytes(int rows, int cols) {
 }
 int block_rows(int cols) { return std::max(ORTH_WARPS, (16384 / std::max(cols, 1)) / ORTH_WARPS * ORTH_WARPS); }
 
-// The matrices from `first` on that are taken at once: as many as L2 holds, or as many as give every SM some tiles.
-constexpr int64_t ORTH_ROUND_BYTES = 80ll << 20;
-constexpr int ORTH_ROUND_TILES = 4 * NUM_SMS;
+// The matrices from `first` on that are taken at once.  The more, the better the SMs' rounds of tiles are filled and the fewer launches wait for the ones in front of them
+// (840 matrices of a 135 M-parameter model and its replicas: 12.1 ms of 128 at a time, 14.9 ms of so few that L2 holds them): up to ORTH_ROUND_BYTES of working memory,
+// the rounds alike.
+constexpr int64_t ORTH_ROUND_BYTES = 2ll << 30;
 Round next_round(const OrthArgs &a, int first) {
+    int64_t rest = 0;
+    for (int i = first; i < a.count; ++i) rest += matrix_bytes(a.list[i].rows, a.list[i].cols);
+    const int64_t rounds = std::max((rest + ORTH_ROUND_BYTES - 1) / ORTH_ROUND_BYTES, static_cast<int64_t>((a.count - first + ORTH_ROUND - 1) / ORTH_ROUND));
+    const int64_t fair = rest / rounds;
     Round r{};
     r.first = first;
-    int64_t tiles = 0;
     while (first + r.count < a.count && r.count < ORTH_ROUND) {
         const OrthMatrix &x = a.list[first + r.count];
         const int64_t bytes = matrix_bytes(x.rows, x.cols);
-        const int n = std::min(x.rows, x.cols);
-        if (r.count > 0 && r.bytes + bytes > ORTH_ROUND_BYTES && tiles >= ORTH_ROUND_TILES) break;
+        if (r.count > 0 && rounds > 1 && r.bytes + bytes / 2 > fair) break;
         if (r.nshapes == 0 || r.shapes[r.nshapes - 1].rows != x.rows || r.shapes[r.nshapes - 1].cols != x.cols) {
             if (r.nshapes == ORTH_SHAPES) break;
             Shape &s = r.shapes[r.nshapes++];
             s.rows = x.rows, s.cols = x.cols, s.count = 0, s.first = r.count;
-            s.n = n, s.m = std::max(x.rows, x.cols), s.tall = x.rows > x.cols;
-            s.ld = padded(x.cols), s.square_ld = padded(n);
+            s.n = std::min(x.rows, x.cols), s.m = std::max(x.rows, x.cols), s.tall = x.rows > x.cols;
+            s.ld = padded(x.cols), s.square_ld = padded(s.n);
         }
         ++r.shapes[r.nshapes - 1].count;
         ++r.count;
         r.bytes += bytes;
-        tiles += tiles_of(n, n, GemmCut{256, false}, false, true);
     }
     return r;
 }
