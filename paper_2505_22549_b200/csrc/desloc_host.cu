@@ -695,7 +695,7 @@ int check_ffn(const desloc_ctx *ctx, const desloc_ffn &f, desloc::FfnArgs &a) {
 int check_rows(const desloc_ctx *ctx, const desloc_ffn &f, const desloc_rows &r, bool written) {
     if (r.dtype != DESLOC_BF16 || !desloc::is_value_rows(r)) return DESLOC_E_INVALID;
     if (f.tokens > 0 && !r.data) return DESLOC_E_NULL;
-    return written && desloc::rows_overlap(r, ctx->cfg.M, f.tokens, f.width) ? DESLOC_E_INVALID : DESLOC_OK;
+    return written && f.tokens > 0 && desloc::rows_overlap(r, ctx->cfg.M, f.tokens, f.width) ? DESLOC_E_INVALID : DESLOC_OK;
 }
 
 constexpr float kNewtonSchulz[3] = {3.4445f, -4.7750f, 2.0315f};

@@ -18,6 +18,7 @@
 #include <cstring>
 #include <exception>
 #include <new>
+#include <type_traits>
 #include <vector>
 
 #include "../../include/desloc.h"
@@ -40,6 +41,13 @@ struct Entry {
     decltype(&desloc_clip_grads_bytes) clip_grads_bytes = nullptr;
     decltype(&desloc_token_logprobs) token_logprobs = nullptr;
     decltype(&desloc_token_logprobs_grad) token_logprobs_grad = nullptr;
+    decltype(&desloc_gated_ffn) gated_ffn = nullptr;
+    decltype(&desloc_gated_ffn_bytes) gated_ffn_bytes = nullptr;
+    decltype(&desloc_gated_ffn_grad) gated_ffn_grad = nullptr;
+    decltype(&desloc_gated_ffn_grad_bytes) gated_ffn_grad_bytes = nullptr;
+    decltype(&desloc_orthogonalize) orthogonalize = nullptr;
+    decltype(&desloc_orthogonal_step) orthogonal_step = nullptr;
+    decltype(&desloc_orthogonal_bytes) orthogonal_bytes = nullptr;
 } g_entry;
 
 struct Table {
@@ -675,26 +683,244 @@ PyObject *call_logprobs_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs
     });
 }
 
-// bind(addresses of desloc_step, _step_masked, _step_normclip, _step_diag, _rel_change, _get_diag_norms, _step_host, and of the operators around the
-// step: _embed, _embed_grad, _embed_grad_bytes, _clip_grads, _clip_grads_bytes, _token_logprobs, _token_logprobs_grad)
-PyObject *bind_entries(PyObject *, PyObject *args) {
-    unsigned long long a[14];
-    if (!PyArg_ParseTuple(args, "KKKKKKKKKKKKKK", &a[0], &a[1], &a[2], &a[3], &a[4], &a[5], &a[6], &a[7], &a[8], &a[9], &a[10], &a[11], &a[12], &a[13]))
+// ---- products of the workers' matrices ---------------------------------------------------------------
+// Addresses of the tensors `which` of nested lists (a list of `nt` tensors for each worker), at [m * nt + k]; false where something is not as it mostly is.  numel: of
+// all tensors.  type: of theirs, or -1 for that of the first one, fp32 or bf16, which is then in *type.
+bool pick(PyObject *nested, int64_t workers, const std::vector<int64_t> &numel, const std::vector<int32_t> &which, int *type, int64_t device,
+          std::vector<void *> &to, std::vector<const at::Tensor *> *tensors) {
+    const Py_ssize_t nt = static_cast<Py_ssize_t>(numel.size());
+    const bool list = PyList_Check(nested);
+    if ((!list && !PyTuple_Check(nested)) || PySequence_Fast_GET_SIZE(nested) != workers) return false;
+    to.assign(static_cast<size_t>(workers * nt), nullptr);
+    for (int64_t m = 0; m < workers; ++m) {
+        PyObject *row = PySequence_Fast_GET_ITEM(nested, m);
+        if ((!PyList_Check(row) && !PyTuple_Check(row)) || PySequence_Fast_GET_SIZE(row) != nt) return false;
+        for (int32_t k : which) {
+            const at::Tensor *t = tensor_on(PySequence_Fast_GET_ITEM(row, k), device);
+            if (!t) return false;
+            if (*type < 0) *type = value_type(t->scalar_type());
+            if (*type < 0 || value_type(t->scalar_type()) != *type || t->numel() != numel[k] || !t->is_contiguous()) return false;
+            to[static_cast<size_t>(m * nt + k)] = t->data_ptr();
+            if (tensors) tensors->push_back(t);
+        }
+    }
+    return true;
+}
+void wrote(const std::vector<const at::Tensor *> &tensors) {
+    const at::Tensor *last = nullptr;
+    for (const at::Tensor *t : tensors) {
+        if (!last || !same_counter(*last, *t)) wrote(*t);
+        last = t;
+    }
+}
+// Numbers of tensors, no two alike.
+bool numbers(PyObject *o, size_t nt, std::vector<int32_t> &out) {
+    PyObject *items = PySequence_Fast(o, "");
+    if (!items) {
+        PyErr_Clear();
+        return false;
+    }
+    std::vector<char> seen(nt, 0);
+    bool ok = true;
+    for (Py_ssize_t i = 0; ok && i < PySequence_Fast_GET_SIZE(items); ++i) {
+        PyObject *item = PySequence_Fast_GET_ITEM(items, i);
+        const long k = PyLong_Check(item) ? PyLong_AsLong(item) : -1;
+        ok = k >= 0 && static_cast<size_t>(k) < nt && !seen[static_cast<size_t>(k)];
+        if (ok) seen[static_cast<size_t>(k)] = 1, out.push_back(static_cast<int32_t>(k));
+    }
+    Py_DECREF(items);
+    PyErr_Clear();
+    return ok;
+}
+
+Table *as_table(PyObject *o) { return Py_TYPE(o) == &table_type ? reinterpret_cast<Table *>(o) : nullptr; }
+
+// Dense bf16 activations [workers, ..., width].
+bool activations(const at::Tensor *t, int64_t workers, desloc_rows *rows, int64_t *tokens) {
+    if (!t || t->scalar_type() != at::kBFloat16 || t->dim() < 2 || t->size(0) != workers || !t->is_contiguous() || t->size(-1) < 1) return false;
+    const int64_t width = t->size(-1);
+    *tokens = t->numel() / (workers * width);
+    *rows = {t->data_ptr(), DESLOC_BF16, {*tokens * width, width}};
+    return true;
+}
+
+struct FfnCall {
+    desloc_ffn f{};
+    std::vector<int32_t> three;
+    std::vector<void *> weights;
+    const at::Tensor *h = nullptr;
+    Table *table = nullptr;
+    c10::SmallVector<int64_t, 4> kept_shape;
+    // (table, tensors, h, weights)
+    bool read(PyObject *table_of, PyObject *tensors, PyObject *h_of, PyObject *weights_of, int64_t device) {
+        table = as_table(table_of);
+        if (!table || !numbers(tensors, table->numel->size(), three) || three.size() != 3) return false;
+        h = tensor_on(h_of, device);
+        if (!activations(h, table->workers, &f.h, &f.tokens)) return false;
+        f.width = h->size(-1);
+        const int64_t numel = (*table->numel)[three[0]];
+        if (numel % f.width || (*table->numel)[three[1]] != numel || (*table->numel)[three[2]] != numel) return false;
+        f.hidden = numel / f.width;
+        f.gate = three[0], f.up = three[1], f.down = three[2];
+        int type = DESLOC_BF16;
+        if (!pick(weights_of, table->workers, *table->numel, three, &type, device, weights, nullptr)) return false;
+        f.weights = weights.data();
+        kept_shape.assign(h->sizes().begin(), h->sizes().end());
+        kept_shape.back() = f.hidden;
+        return true;
+    }
+};
+
+// (context, table, tensors, h, weights, keep, device) -> y or (y, (g, u))
+PyObject *call_ffn(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr;
+    int64_t keep = 0, device = 0;
+    if (nargs != 7) {
+        PyErr_SetString(PyExc_TypeError, "gated_ffn(ctx, table, tensors, h, weights, keep, device)");
         return nullptr;
-    g_entry.step = reinterpret_cast<decltype(g_entry.step)>(a[0]);
-    g_entry.step_masked = reinterpret_cast<decltype(g_entry.step_masked)>(a[1]);
-    g_entry.step_normclip = reinterpret_cast<decltype(g_entry.step_normclip)>(a[2]);
-    g_entry.step_diag = reinterpret_cast<decltype(g_entry.step_diag)>(a[3]);
-    g_entry.rel_change = reinterpret_cast<decltype(g_entry.rel_change)>(a[4]);
-    g_entry.diag_norms = reinterpret_cast<decltype(g_entry.diag_norms)>(a[5]);
-    g_entry.step_host = reinterpret_cast<decltype(g_entry.step_host)>(a[6]);
-    g_entry.embed = reinterpret_cast<decltype(g_entry.embed)>(a[7]);
-    g_entry.embed_grad = reinterpret_cast<decltype(g_entry.embed_grad)>(a[8]);
-    g_entry.embed_grad_bytes = reinterpret_cast<decltype(g_entry.embed_grad_bytes)>(a[9]);
-    g_entry.clip_grads = reinterpret_cast<decltype(g_entry.clip_grads)>(a[10]);
-    g_entry.clip_grads_bytes = reinterpret_cast<decltype(g_entry.clip_grads_bytes)>(a[11]);
-    g_entry.token_logprobs = reinterpret_cast<decltype(g_entry.token_logprobs)>(a[12]);
-    g_entry.token_logprobs_grad = reinterpret_cast<decltype(g_entry.token_logprobs_grad)>(a[13]);
+    }
+    if (!as_pointer(args[0], &ctx) || !as_int64(args[5], &keep) || !as_int64(args[6], &device)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        FfnCall c;
+        if (!c.read(args[1], args[2], args[3], args[4], device)) Py_RETURN_NONE;
+        const int64_t bytes = g_entry.gated_ffn_bytes(static_cast<desloc_ctx *>(ctx), &c.f);
+        if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
+        const at::Tensor y = new_tensor(c.h->sizes(), at::kBFloat16, device), work = new_tensor({bytes}, at::kByte, device);
+        at::Tensor g, u;
+        if (keep) g = new_tensor(c.kept_shape, at::kBFloat16, device), u = new_tensor(c.kept_shape, at::kBFloat16, device);
+        const desloc_rows to{y.data_ptr(), DESLOC_BF16, {c.f.tokens * c.f.width, c.f.width}};
+        void *stream = stream_of(device), *at_work = work.data_ptr(), *at_g = keep ? g.data_ptr() : nullptr, *at_u = keep ? u.data_ptr() : nullptr;
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.gated_ffn(static_cast<desloc_ctx *>(ctx), &c.f, at_g, at_u, &to, at_work, bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        if (!keep) return THPVariable_Wrap(y);
+        PyObject *a = THPVariable_Wrap(g), *b = a ? THPVariable_Wrap(u) : nullptr, *both = b ? PyTuple_Pack(2, a, b) : nullptr;
+        PyObject *out = both ? THPVariable_Wrap(y) : nullptr, *all = out ? PyTuple_Pack(2, out, both) : nullptr;
+        Py_XDECREF(a);
+        Py_XDECREF(b);
+        Py_XDECREF(both);
+        Py_XDECREF(out);
+        return all;
+    });
+}
+
+// (context, table, tensors, h, g, u, dy, weights, grads, type, accumulate, device) -> dh
+PyObject *call_ffn_grad(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr;
+    int64_t type = 0, accumulate = 0, device = 0;
+    if (nargs != 12) {
+        PyErr_SetString(PyExc_TypeError, "gated_ffn_grad(ctx, table, tensors, h, g, u, dy, weights, grads, type, accumulate, device)");
+        return nullptr;
+    }
+    if (!as_pointer(args[0], &ctx) || !as_int64(args[9], &type) || !as_int64(args[10], &accumulate) || !as_int64(args[11], &device)) return nullptr;
+    return guarded([&]() -> PyObject * {
+        FfnCall c;
+        if (!c.read(args[1], args[2], args[3], args[7], device)) Py_RETURN_NONE;
+        const at::Tensor *g = tensor_on(args[4], device), *u = tensor_on(args[5], device), *d = tensor_on(args[6], device);
+        for (const at::Tensor *t : {g, u})
+            if (!t || t->scalar_type() != at::kBFloat16 || t->sizes() != at::IntArrayRef(c.kept_shape) || !t->is_contiguous()) Py_RETURN_NONE;
+        desloc_rows dy;
+        int64_t tokens = 0;
+        if (!activations(d, c.table->workers, &dy, &tokens) || d->sizes() != c.h->sizes()) Py_RETURN_NONE;
+        std::vector<void *> grads;
+        std::vector<const at::Tensor *> written;
+        int kind = static_cast<int>(type);
+        if (!pick(args[8], c.table->workers, *c.table->numel, c.three, &kind, device, grads, &written)) Py_RETURN_NONE;
+        const int64_t bytes = g_entry.gated_ffn_grad_bytes(static_cast<desloc_ctx *>(ctx), &c.f, &dy);
+        if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
+        const at::Tensor dh = new_tensor(c.h->sizes(), at::kBFloat16, device), work = new_tensor({bytes}, at::kByte, device);
+        const desloc_rows to{dh.data_ptr(), DESLOC_BF16, {c.f.tokens * c.f.width, c.f.width}};
+        void *stream = stream_of(device), *at_work = work.data_ptr(), *at_g = g->data_ptr(), *at_u = u->data_ptr();
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = g_entry.gated_ffn_grad(static_cast<desloc_ctx *>(ctx), &c.f, at_g, at_u, &dy, &to, static_cast<int32_t>(accumulate), grads.data(), at_work, bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        wrote(written);
+        return THPVariable_Wrap(dh);
+    });
+}
+
+// (context, table, tensors, columns of all tensors, updates or None, grads or None, out or None, lr, steps, eps, scale, type of grads, x, device) -> True.  out None: the
+// step of x.
+PyObject *call_orthogonal(PyObject *, PyObject *const *args, Py_ssize_t nargs) {
+    void *ctx = nullptr;
+    int64_t steps = 0, scale = 0, type = 0, device = 0;
+    float lr = 0.f, eps = 0.f;
+    if (nargs != 14) {
+        PyErr_SetString(PyExc_TypeError, "orthogonal(ctx, table, tensors, columns, updates, grads, out, lr, steps, eps, scale, type, x, device)");
+        return nullptr;
+    }
+    if (!as_pointer(args[0], &ctx) || !as_float(args[7], &lr) || !as_int64(args[8], &steps) || !as_float(args[9], &eps) || !as_int64(args[10], &scale) ||
+        !as_int64(args[11], &type) || !as_int64(args[13], &device))
+        return nullptr;
+    return guarded([&]() -> PyObject * {
+        Table *table = as_table(args[1]);
+        std::vector<int32_t> which;
+        if (!table || !numbers(args[2], table->numel->size(), which) || which.empty() || !PyTuple_Check(args[3]) ||
+            PyTuple_GET_SIZE(args[3]) != static_cast<Py_ssize_t>(table->numel->size()))
+            Py_RETURN_NONE;
+        std::vector<int64_t> columns;
+        for (int32_t k : which) {
+            columns.push_back(PyLong_AsLongLong(PyTuple_GET_ITEM(args[3], k)));
+            if (columns.back() < 1) {
+                PyErr_Clear();
+                Py_RETURN_NONE;
+            }
+        }
+        desloc_orthogonal how{};
+        std::vector<void *> updates, grads, out;
+        std::vector<const at::Tensor *> written;
+        if (args[4] != Py_None) {
+            int kind = -1;
+            if (!pick(args[4], table->workers, *table->numel, which, &kind, device, updates, nullptr)) Py_RETURN_NONE;
+            how.updates_dtype = kind, how.updates = updates.data();
+        }
+        if (args[5] != Py_None) {
+            int kind = static_cast<int>(type);
+            if (!pick(args[5], table->workers, *table->numel, which, &kind, device, grads, nullptr)) Py_RETURN_NONE;
+            how.grads = grads.data();
+        }
+        int out_type = args[6] == Py_None ? static_cast<int>(DESLOC_F32) : -1;
+        if (!pick(args[6] == Py_None ? args[12] : args[6], table->workers, *table->numel, which, &out_type, device, out, &written)) Py_RETURN_NONE;
+        how.tensors = which.data(), how.columns = columns.data(), how.count = static_cast<int32_t>(which.size());
+        how.steps = static_cast<int32_t>(steps), how.eps = eps, how.scale = static_cast<int32_t>(scale);
+        const int64_t bytes = g_entry.orthogonal_bytes(static_cast<desloc_ctx *>(ctx), &how);
+        if (bytes < 0) return PyLong_FromLong(static_cast<long>(bytes));
+        const at::Tensor work = new_tensor({bytes}, at::kByte, device);
+        void *stream = stream_of(device), *at_work = work.data_ptr();
+        const bool step = args[6] == Py_None;
+        int rc = 0;
+        Py_BEGIN_ALLOW_THREADS
+        rc = step ? g_entry.orthogonal_step(static_cast<desloc_ctx *>(ctx), &how, lr, at_work, bytes, stream)
+                  : g_entry.orthogonalize(static_cast<desloc_ctx *>(ctx), &how, out_type, out.data(), at_work, bytes, stream);
+        Py_END_ALLOW_THREADS
+        if (rc != DESLOC_OK) return PyLong_FromLong(rc);
+        wrote(written);
+        Py_RETURN_TRUE;
+    });
+}
+
+// bind(addresses of desloc_step, _step_masked, _step_normclip, _step_diag, _rel_change, _get_diag_norms, _step_host, and of the operators around the
+// step: _embed, _embed_grad, _embed_grad_bytes, _clip_grads, _clip_grads_bytes, _token_logprobs, _token_logprobs_grad, _gated_ffn, _gated_ffn_bytes,
+// _gated_ffn_grad, _gated_ffn_grad_bytes, _orthogonalize, _orthogonal_step, _orthogonal_bytes)
+PyObject *bind_entries(PyObject *, PyObject *args) {
+    constexpr Py_ssize_t N = 21;
+    void *a[N];
+    if (PyTuple_GET_SIZE(args) != N) {
+        PyErr_SetString(PyExc_TypeError, "bind() takes the addresses of the library's entry points");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < N; ++i)
+        if (!as_pointer(PyTuple_GET_ITEM(args, i), &a[i])) return nullptr;
+    Py_ssize_t at = 0;
+    const auto next = [&](auto &entry) { entry = reinterpret_cast<std::decay_t<decltype(entry)>>(a[at++]); };
+    next(g_entry.step), next(g_entry.step_masked), next(g_entry.step_normclip), next(g_entry.step_diag), next(g_entry.rel_change), next(g_entry.diag_norms);
+    next(g_entry.step_host), next(g_entry.embed), next(g_entry.embed_grad), next(g_entry.embed_grad_bytes), next(g_entry.clip_grads);
+    next(g_entry.clip_grads_bytes), next(g_entry.token_logprobs), next(g_entry.token_logprobs_grad), next(g_entry.gated_ffn), next(g_entry.gated_ffn_bytes);
+    next(g_entry.gated_ffn_grad), next(g_entry.gated_ffn_grad_bytes), next(g_entry.orthogonalize), next(g_entry.orthogonal_step), next(g_entry.orthogonal_bytes);
     Py_RETURN_NONE;
 }
 
@@ -715,6 +941,9 @@ PyMethodDef methods[] = {{"bind", bind_entries, METH_VARARGS, nullptr},
                          {"clip_grads", fast(call_clip_grads), METH_FASTCALL, nullptr},
                          {"token_logprobs", fast(call_logprobs), METH_FASTCALL, nullptr},
                          {"token_logprobs_grad", fast(call_logprobs_grad), METH_FASTCALL, nullptr},
+                         {"gated_ffn", fast(call_ffn), METH_FASTCALL, nullptr},
+                         {"gated_ffn_grad", fast(call_ffn_grad), METH_FASTCALL, nullptr},
+                         {"orthogonal", fast(call_orthogonal), METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -21,7 +21,8 @@ if _native.torch_version != str(torch.__version__):
 _entry = lambda f: ctypes.cast(f, ctypes.c_void_p).value
 _native.bind(*(_entry(getattr(B.raw_lib(), "desloc_" + n))
                for n in ("step", "step_masked", "step_normclip", "step_diag", "rel_change", "get_diag_norms", "step_host", "embed", "embed_grad",
-                         "embed_grad_bytes", "clip_grads", "clip_grads_bytes", "token_logprobs", "token_logprobs_grad")))
+                         "embed_grad_bytes", "clip_grads", "clip_grads_bytes", "token_logprobs", "token_logprobs_grad", "gated_ffn", "gated_ffn_bytes",
+                         "gated_ffn_grad", "gated_ffn_grad_bytes", "orthogonalize", "orthogonal_step", "orthogonal_bytes")))
 
 _GRAD_MISFIT = "gradient tensor of wrong dtype, size or layout"
 _SNAP_MISFIT = "snapshot tensor of wrong dtype, size or layout"
@@ -30,6 +31,7 @@ _HOST_MISFIT = "host gradient tensor of wrong dtype, size, layout or device"
 
 _TYPES = {torch.float32: B.DESLOC_F32, torch.bfloat16: B.DESLOC_BF16}
 _TORCH_TYPES = {code: t for t, code in _TYPES.items()}
+_SCALES = {"none": B.DESLOC_SCALE_NONE, "aspect": B.DESLOC_SCALE_ASPECT, "rms": B.DESLOC_SCALE_RMS}
 _TOKEN_TYPES = {torch.int32: B.DESLOC_I32, torch.int64: B.DESLOC_I64}
 
 
@@ -124,6 +126,7 @@ class DesLoc:
         self._table = _native.Table(self.numel, self.M)
         self._table2 = _native.Table(self.numel, self.M)
         self._fits = (self.M, tuple(self.numel), self.grad_dtype)
+        self._columns = None
 
     def bind_grads(self, grads: Sequence[Sequence[torch.Tensor]]):
         """Check a set of gradient tensors once and return a handle every step method accepts in
@@ -359,6 +362,12 @@ class DesLoc:
             raise ValueError(misfit)
         return kind
 
+    def _widths(self) -> tuple:
+        """Columns of every tensor of x; 0 of those with one dimension."""
+        if self._columns is None:
+            self._columns = tuple(int(t.shape[-1]) if t.dim() > 1 else 0 for t in self._keep[0][0])
+        return self._columns
+
     def _numbers(self, tensors):
         tensors = [int(k) for k in tensors]
         if any(not 0 <= k < len(self.numel) for k in tensors) or len(set(tensors)) != len(tensors):
@@ -404,6 +413,10 @@ class DesLoc:
         """The gated feed-forward block down(silu(gate h) * (up h)) of every worker with its own weights, on torch's current stream.  tensors: numbers of gate,
         up ([hidden, width]) and down ([width, hidden]); h: bf16 [M, ..., width]; weights: nested lists like x of bf16 copies, of which only those three are looked at.
         Returns y like h, or with keep (y, (gate h, up h)) for gated_ffn_grad()."""
+        if out is None:     # the usual layouts, natively
+            r = _native.gated_ffn(self.ctx, self._table, tensors, h, weights, keep, self._index)
+            if r is not None:
+                return r if type(r) is not int else self._raise(r, "desloc_gated_ffn")
         f, h, hidden = self._ffn(tensors, h, weights)
         to, out = self._result("out", out, tuple(h.shape))
         kept = tuple(torch.empty(tuple(h.shape[:-1]) + (hidden,), dtype=torch.bfloat16, device=self.device) for _ in range(2)) if keep else None
@@ -417,6 +430,10 @@ class DesLoc:
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The way back of gated_ffn(): returns dh (into `out` where it is given) and writes the three weights' gradients into the workers' gradients in `grads` (what
         step() reads, or bind_grads()' handle); accumulate: added to what they hold.  kept: what gated_ffn(keep=True) returned beside y."""
+        if out is None and len(kept) == 2:
+            r = _native.gated_ffn_grad(self.ctx, self._table, tensors, h, kept[0], kept[1], dy, weights, grads, self.grad_dtype, accumulate, self._index)
+            if r is not None:
+                return r if type(r) is not int else self._raise(r, "desloc_gated_ffn_grad")
         f, h, hidden = self._ffn(tensors, h, weights)
         tensors = (f.gate, f.up, f.down)
         shape = tuple(h.shape[:-1]) + (hidden,)
@@ -437,8 +454,7 @@ class DesLoc:
         tensors = self._numbers(tensors)
         if columns is None:
             columns = [self._rows_of(k, None) for k in tensors]
-        codes = {"none": B.DESLOC_SCALE_NONE, "aspect": B.DESLOC_SCALE_ASPECT, "rms": B.DESLOC_SCALE_RMS}
-        if scale not in codes:
+        if scale not in _SCALES:
             raise ValueError('scale is "none", "aspect" or "rms"')
         if coefficients is not None:
             coefficients = [float(v) for triple in coefficients for v in triple]
@@ -449,7 +465,7 @@ class DesLoc:
             updates = self._addresses(updates, tensors, kind, misfit)
         if grads is not None and tensors:
             grads = self._addresses(grads, tensors, self.grad_dtype, _GRAD_MISFIT)
-        return tensors, B.orthogonal(tensors, columns, steps, coefficients, eps, codes[scale], kind, updates if tensors else None, grads if tensors else None)
+        return tensors, B.orthogonal(tensors, columns, steps, coefficients, eps, _SCALES[scale], kind, updates if tensors else None, grads if tensors else None)
 
     def orthogonalize(self, tensors, updates, grads=None, out=None, columns=None, steps: int = 5, coefficients=None, eps: float = 1e-7,
                       scale: str = "none") -> None:
@@ -457,12 +473,17 @@ class DesLoc:
         Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad.  columns: of each matrix,
         where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones.  scale: "none", "aspect"
         (sqrt(max(1, rows / columns))) or "rms" (0.2 sqrt(max(rows, columns)))."""
+        if updates is None:
+            updates = self._keep[1]
+        if columns is None and coefficients is None and scale in _SCALES:     # the usual call, natively
+            r = _native.orthogonal(self.ctx, self._table, tensors, self._widths(), updates, grads, updates if out is None else out, 0.0, steps, eps, _SCALES[scale],
+                                   self.grad_dtype, None, self._index)
+            if r is not None:
+                return None if r is True else self._raise(r, "desloc_orthogonalize")
         tensors, how = self._orthogonal(tensors, updates, grads, columns, steps, coefficients, eps, scale)
         if not tensors:
             return
         written = updates if out is None else out
-        if written is None:
-            written = self._keep[1]
         misfit = "out tensor of wrong dtype, size or layout"
         kind = self._kind(written, tensors, misfit)
         work = torch.empty(B.desloc_orthogonal_bytes(self.ctx, how), dtype=torch.uint8, device=self.device)
@@ -474,6 +495,11 @@ class DesLoc:
                         scale: str = "aspect") -> None:
         """x of the matrices `tensors` := x (1 - lr weight_decay) - lr * orthogonalize(updates; the momentum u where None).  Behind step(t, 0.0, grads) of an SGDM
         context, which brings the momentum and the averages of this step, it is the step of the orthogonalised momentum; grads: its look-ahead."""
+        if columns is None and coefficients is None and scale in _SCALES:
+            r = _native.orthogonal(self.ctx, self._table, tensors, self._widths(), updates, grads, None, lr, steps, eps, _SCALES[scale], self.grad_dtype, self._keep[0],
+                                   self._index)
+            if r is not None:
+                return None if r is True else self._raise(r, "desloc_orthogonal_step")
         tensors, how = self._orthogonal(tensors, updates, grads, columns, steps, coefficients, eps, scale)
         if not tensors:
             return
