@@ -266,9 +266,9 @@ cudaError_t product_store(const Operand &x, const Operand &w, int M, int tokens,
     static thread_local GemmArgs<E> a;
     for (int m0 = 0; m0 < M; m0 += WORKERS) {
         const int some = std::min(WORKERS, M - m0);
-        const GemmCut cut = pick_cut(false, k, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(tokens, n, c, false, false); });
+        const GemmCut cut = pick_cut(false, tokens, k, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(tokens, n, c, false, false); });
         begin_gemm(a, true, cut, false, false, 1);
-        cudaError_t e = x.maps(a, 0, 0, M, m0, some, GEMM_BM);
+        cudaError_t e = x.maps(a, 0, 0, M, m0, some, box_rows(tokens));
         if (e == cudaSuccess) e = w.maps(a, 1, 1, M, m0, some, cut.box_n(false));
         if (e != cudaSuccess) return e;
         for (int i = 0; i < some; ++i) {
@@ -312,7 +312,7 @@ cudaError_t weight_grads(const FfnArgs &a, const Operands &o, const Operand &z, 
     static thread_local GemmArgs<E> g;
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
-        const GemmCut cut = pick_cut(false, a.tokens, [&](const GemmCut &c) {
+        const GemmCut cut = pick_cut(false, GEMM_BM, a.tokens, [&](const GemmCut &c) {
             return static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, c, false, false) + tiles_of(a.width, a.hidden, c, false, false));
         });
         begin_gemm(g, true, cut, false, false, 1);
@@ -358,10 +358,10 @@ cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, c
     static thread_local GemmArgs<UpEpilogue> g;
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
-        const GemmCut cut = pick_cut(true, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, true, false); });
+        const GemmCut cut = pick_cut(true, a.tokens, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, true, false); });
         const int box = cut.box_n(true);
         begin_gemm(g, true, cut, true, false, 1);
-        e = o.h.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
+        e = o.h.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
         // (gate and up of a worker next to one another: the second half of a tile's columns is the next map's)
         if (e == cudaSuccess) e = o.gate.maps(g, 1, 2, a.M, m0, some, box);
         if (e == cudaSuccess) e = o.up.maps(g, 2, 2, a.M, m0, some, box);
@@ -412,9 +412,9 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<DzEpilogue> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const GemmCut cut = pick_cut(false, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, false, false); });
+            const GemmCut cut = pick_cut(false, a.tokens, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, false, false); });
             begin_gemm(g, true, cut, false, false, 1);
-            e = o.dy.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
+            e = o.dy.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
             if (e == cudaSuccess) e = o.down.maps(g, 1, 1, a.M, m0, some, 64);
             if (e != cudaSuccess) return e;
             for (int i = 0; i < some; ++i) {
@@ -442,10 +442,10 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<E> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const GemmCut cut = pick_cut(false, 2 * a.hidden, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, c, false, false); });
+            const GemmCut cut = pick_cut(false, a.tokens, 2 * a.hidden, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, c, false, false); });
             begin_gemm(g, true, cut, false, false, 2);
-            e = dg.maps(g, 0, 0, a.M, m0, some, GEMM_BM);
-            if (e == cudaSuccess) e = du.maps(g, 1, 0, a.M, m0, some, GEMM_BM);
+            e = dg.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
+            if (e == cudaSuccess) e = du.maps(g, 1, 0, a.M, m0, some, box_rows(a.tokens));
             for (int i = 0; i < some && e == cudaSuccess; ++i)
                 for (int seg = 0; seg < 2 && e == cudaSuccess; ++seg) {
                     const Operand &w = seg ? o.up : o.gate;

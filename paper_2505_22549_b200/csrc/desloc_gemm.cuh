@@ -34,6 +34,7 @@ struct GemmGroup {
     int m, n, k;
     short a_map, b_map;      // the operands' boxes: of segment s and (dual) half h, the next ones
     short a_mn, b_mn;        // whether the operands lie m- and n-major
+    int a_rows;              // rows of A's boxes (k-major): what m leaves of 128; the products read what lies behind them, and nobody reads what comes of that
     int a_batch, b_batch;    // of its first matrix in those maps
     // what the epilogue reads and writes, and how far it is to the next matrix's (elements)
     void *out[3];
@@ -360,7 +361,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
                 const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
                 const int boxes = (own_n + 63) / 64;
-                const uint32_t bytes = GEMM_A_BYTES + (g.b_mn ? 64 * boxes : own_n) * (GEMM_BK * 2);
+                const uint32_t bytes = ((g.a_mn ? GEMM_BM : g.a_rows) + (g.b_mn ? 64 * boxes : own_n)) * (GEMM_BK * 2);
                 for (int kk = 0; kk < steps * a.segments; ++kk) {
                     ok = bar_wait(&empty[s], phase ^ 1, a.wait_limit);
                     if (!ok) break;
@@ -531,6 +532,9 @@ cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t 
 // Whether rows `ld` elements apart from `data` on can be fetched by the copy engine: 16-byte boundaries.
 inline bool boxes_fit(const void *data, int64_t ld) { return ((reinterpret_cast<uintptr_t>(data) | static_cast<uintptr_t>(ld * 2)) & 15u) == 0; }
 
+// Rows of a k-major box of an A with m rows.
+inline int box_rows(int64_t m) { return static_cast<int>(std::min<int64_t>(GEMM_BM, (m + 7) / 8 * 8)); }
+
 // How a launch is cut: columns of a tile (dual: of both halves together), and whether blocks work in pairs.
 struct GemmCut {
     int tile_n;
@@ -548,16 +552,17 @@ inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric)
 }
 // The cut that is done first: rounds of tiles, a tile as long as bringing and multiplying 64 k takes (measured, in cycles: 900 for 256 columns and 780 for 192 of a pair, 1000 for 256 of a
 // block alone, 600 for 128), or as emptying it (some 1500 for the 128 columns that the warps take at a time); and what a launch of a round takes before and behind.
-// tiles(cut): how many there are, all with k of about `k`.
+// Few rows (up to FEW_ROWS): what takes time is B from memory, some 6 cycles a column of 64 k when all SMs read.  tiles(cut): how many there are, all with k of about `k`.
+constexpr int64_t FEW_ROWS = 32;
 template <typename F>
-GemmCut pick_cut(bool dual, int64_t k, const F &tiles) {
+GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
     GemmCut best{};
     int64_t least = 0;
-    for (int pairs = 1; pairs >= 0; --pairs)
-        for (int n = 256; n >= (dual || pairs ? 128 : 64); n -= 64) {
+    for (int pairs = m > FEW_ROWS ? 1 : 0; pairs >= 0; --pairs)
+        for (int n = 256; n >= (pairs ? 128 : 64); n -= 64) {
             const GemmCut cut{n, pairs != 0};
             const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, rounds = (tiles(cut) + slots - 1) / slots;
-            const int64_t step = pairs ? 440 + 9 * n / 5 : 240 + 3 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 1500;
+            const int64_t step = m <= FEW_ROWS ? 60 + 6 * n : pairs ? 440 + 9 * n / 5 : 240 + 3 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 1500;
             const int64_t cost = rounds * (std::max(products, empty) + 200) + std::min(products, empty);
             if (!best.tile_n || cost < least) best = cut, least = cost;
         }
@@ -579,7 +584,7 @@ GemmGroup &add_group(GemmArgs<E> &a, int m, int n, int k, int count) {
     const GemmCut cut{a.tile_n, a.pairs != 0};
     const int out_n = cut.out_n(a.dual), bm = GEMM_BM * (a.pairs ? 2 : 1);
     g.tile0 = a.tiles;
-    g.m = m, g.n = n, g.k = k;
+    g.m = m, g.n = n, g.k = k, g.a_rows = box_rows(m);
     g.mt = (m + bm - 1) / bm, g.nt = (n + out_n - 1) / out_n;
     g.per = tiles_of(m, n, cut, a.dual, a.symmetric);
     a.tiles += g.per * count;

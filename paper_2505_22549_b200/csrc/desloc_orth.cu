@@ -3,6 +3,7 @@
 #include "desloc_gemm.cuh"
 
 #include <algorithm>
+#include <vector>
 
 namespace desloc {
 
@@ -382,10 +383,23 @@ int64_t place(Round &r, char *work, double **partial, int *most) {
     return used;
 }
 
-void sort_list(const OrthArgs &a) {
+// Small matrices first, then by shape; how many small ones.
+int sort_list(const OrthArgs &a) {
     std::sort(a.list, a.list + a.count, [](const OrthMatrix &x, const OrthMatrix &y) {
-        return x.rows != y.rows ? x.rows < y.rows : x.cols != y.cols ? x.cols < y.cols : x.index < y.index;
+        const bool sx = orth_is_small(x.rows, x.cols), sy = orth_is_small(y.rows, y.cols);
+        return sx != sy ? sx : x.rows != y.rows ? x.rows < y.rows : x.cols != y.cols ? x.cols < y.cols : x.index < y.index;
     });
+    int small = 0;
+    while (small < a.count && orth_is_small(a.list[small].rows, a.list[small].cols)) ++small;
+    return small;
+}
+
+// What the result is multiplied by.
+double scale_of(const OrthArgs &a, int rows, int cols) {
+    const double scale = a.scale == DESLOC_SCALE_ASPECT ? std::sqrt(std::max(1.0, static_cast<double>(rows) / cols))
+                         : a.scale == DESLOC_SCALE_RMS  ? 0.2 * std::sqrt(static_cast<double>(std::max(rows, cols)))
+                                                        : 1.0;
+    return scale * (a.list[0].out ? 1.0 : static_cast<double>(a.lr));
 }
 
 // The cut of a product of all shapes: tiles(shape, cut) of one matrix, k(shape).
@@ -396,7 +410,7 @@ GemmCut pick(const Round &r, const K &k, const F &tiles) {
         const int64_t n = static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], GemmCut{256, true});
         all += n, sum += n * k(r.shapes[i]);
     }
-    return pick_cut(false, sum / all, [&](const GemmCut &cut) {
+    return pick_cut(false, GEMM_BM, sum / all, [&](const GemmCut &cut) {
         int64_t n = 0;
         for (int i = 0; i < r.nshapes; ++i) n += static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], cut);
         return n;
@@ -419,7 +433,7 @@ cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b,
         const bool mn = gram && s.tall;
         GemmGroup &g = add_group(a, s.n, s.n, gram ? s.m : s.n, s.count);
         for (int side_b = 0; side_b < 2; ++side_b) {
-            const int box = mn ? 64 : side_b ? cut.box_n(false) : GEMM_BM;
+            const int box = mn ? 64 : side_b ? cut.box_n(false) : box_rows(s.n);
             const cudaError_t e = gram ? encode_boxes(&a.maps[2 * i + side_b], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, box)
                                        : encode_boxes(&a.maps[2 * i + side_b], s.gram, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, box);
             if (e != cudaSuccess) return e;
@@ -444,9 +458,9 @@ cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const
         const Shape &s = r.shapes[i];
         GemmGroup &g = add_group(a, s.rows, s.cols, s.n, s.count);
         const int of_x = 2 * i + (s.tall ? 0 : 1), of_poly = 2 * i + (s.tall ? 1 : 0);
-        cudaError_t e = encode_boxes(&a.maps[of_x], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, s.tall ? GEMM_BM : 64);
+        cudaError_t e = encode_boxes(&a.maps[of_x], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, s.tall ? box_rows(s.rows) : 64);
         if (e == cudaSuccess)
-            e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? cut.box_n(false) : GEMM_BM);
+            e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? cut.box_n(false) : box_rows(s.n));
         if (e != cudaSuccess) return e;
         g.a_map = static_cast<short>(2 * i), g.b_map = static_cast<short>(2 * i + 1);
         g.b_mn = !s.tall;
@@ -471,11 +485,7 @@ cudaError_t last(const OrthArgs &a, const Round &r, int side, const Run &run) {
     long long ld[ORTH_SHAPES];
     for (int i = 0; i < r.nshapes; ++i) {
         const Shape &s = r.shapes[i];
-        const double longer = std::max(s.rows, s.cols);
-        const double scale = a.scale == DESLOC_SCALE_ASPECT ? std::sqrt(std::max(1.0, static_cast<double>(s.rows) / s.cols))
-                             : a.scale == DESLOC_SCALE_RMS  ? 0.2 * std::sqrt(longer)
-                                                            : 1.0;
-        epi.scale[i] = static_cast<float>(scale * (TO == ORTH_TO_X ? a.lr : 1.0) / ORTH_UNIT);
+        epi.scale[i] = static_cast<float>(scale_of(a, s.rows, s.cols) / ORTH_UNIT);
         ld[i] = s.cols;
     }
     for (int i = 0; i < r.count; ++i) epi.out[i] = a.list[r.first + i].out, epi.index[i] = a.list[r.first + i].index;
@@ -494,9 +504,8 @@ cudaError_t prepare(const Sources &s, int count, const Run &run) {
 }  // namespace
 
 int64_t orth_work(const OrthArgs &a) {
-    sort_list(a);
-    int64_t most = 0;
-    for (int at = 0; at < a.count;) {
+    int64_t most = 256;
+    for (int at = sort_list(a); at < a.count;) {
         Round r = next_round(a, at);
         most = std::max(most, place(r, nullptr, nullptr, nullptr));
         at += r.count;
@@ -506,10 +515,16 @@ int64_t orth_work(const OrthArgs &a) {
 
 cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
     const Run run{stream, err, wait_limit, launches};
-    sort_list(a);
+    const int small = sort_list(a);
+    if (small > 0) {
+        std::vector<float> scales;
+        for (int i = 0; i < small; ++i) scales.push_back(static_cast<float>(scale_of(a, a.list[i].rows, a.list[i].cols)));
+        const cudaError_t e = launch_orth_small(a, 0, small, scales.data(), err, wait_limit, stream, launches);
+        if (e != cudaSuccess) return e;
+    }
     static thread_local Sources s;
     static thread_local GemmArgs<NextEpilogue> next;
-    for (int at = 0; at < a.count;) {
+    for (int at = small; at < a.count;) {
         Round r = next_round(a, at);
         place(r, work, &s.partial, &s.most);
         s.table = a.u_table, s.beta = a.beta, s.eps = a.eps;
