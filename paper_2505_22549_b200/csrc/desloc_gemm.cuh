@@ -54,6 +54,7 @@ struct GemmArgs {
     int pairs;               // blocks work in pairs
     int dual;                // the tile's columns are two halves, of two B operands
     int symmetric;           // only tiles that reach the lower triangle
+    int rotate;              // every tile begins with another k
     uint32_t idesc;          // without the operands' layouts
     int *err;
     int wait_limit;
@@ -360,12 +361,18 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 const GemmGroup &g = at.find<CG>(a, tile);
                 const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
                 const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
-                const int boxes = (own_n + 63) / 64;
+                const int boxes = (own_n + 63) / 64, turned = a.rotate ? static_cast<int>(tile * 29u % steps) : 0;
                 const uint32_t bytes = ((g.a_mn ? GEMM_BM : g.a_rows) + (g.b_mn ? 64 * boxes : own_n)) * (GEMM_BK * 2);
                 for (int kk = 0; kk < steps * a.segments; ++kk) {
                     ok = bar_wait(&empty[s], phase ^ 1, a.wait_limit);
                     if (!ok) break;
-                    const int seg = kk >= steps ? 1 : 0, k0 = (kk - seg * steps) * GEMM_BK;
+                    int seg = 0, step = kk;
+                    if (step >= steps) seg = 1, step -= steps;
+                    if (a.rotate) {
+                        step += turned;
+                        if (step >= steps) step -= steps;
+                    }
+                    const int k0 = step * GEMM_BK;
                     char *const sa = ring + s * stage_bytes, *const sb = sa + GEMM_A_BYTES;
                     const CUtensorMap *const ma = &a.maps[g.a_map + seg], *const mb = &a.maps[g.b_map + seg];
                     const int za = g.a_batch + at.batch, zb = g.b_batch + at.batch;
@@ -553,7 +560,7 @@ inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric)
 // The cut that is done first: rounds of tiles, a tile as long as bringing and multiplying 64 k takes (measured, in cycles: 900 for 256 columns and 780 for 192 of a pair, 1000 for 256 of a
 // block alone, 600 for 128), or as emptying it (some 1500 for the 128 columns that the warps take at a time); and what a launch of a round takes before and behind.
 // Few rows (up to FEW_ROWS): what takes time is B from memory, some 6 cycles a column of 64 k when all SMs read.  tiles(cut): how many there are, all with k of about `k`.
-constexpr int64_t FEW_ROWS = 32;
+constexpr int64_t FEW_ROWS = 64;
 template <typename F>
 GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
     GemmCut best{};
@@ -572,7 +579,7 @@ GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
 template <typename E>
 void begin_gemm(GemmArgs<E> &a, bool bf16, const GemmCut &cut, bool dual, bool symmetric, int segments) {
     a.ngroups = a.tiles = 0;
-    a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
+    a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.rotate = 0, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
     const uint32_t type = bf16 ? 1 : 0;
     a.idesc = 1u << 4 | type << 7 | type << 10 | static_cast<uint32_t>(cut.tile_n >> 3) << 17 | static_cast<uint32_t>((cut.pairs ? 2 : 1) * GEMM_BM >> 4) << 24;
 }
@@ -588,6 +595,9 @@ GemmGroup &add_group(GemmArgs<E> &a, int m, int n, int k, int count) {
     g.mt = (m + bm - 1) / bm, g.nt = (n + out_n - 1) / out_n;
     g.per = tiles_of(m, n, cut, a.dual, a.symmetric);
     a.tiles += g.per * count;
+    // Few rows: all that is read is B, once, and all blocks at once would read the same columns of rows that lie a power of two apart, of which a few of the memory's channels
+    // have to bring all (the 8192 columns of down, one row of h: 1.7 TB/s).
+    a.rotate = m <= FEW_ROWS;
     return g;
 }
 

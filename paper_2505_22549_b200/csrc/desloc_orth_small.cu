@@ -107,22 +107,35 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     const uint32_t tmem = tmem_at;
     wait_for_earlier_kernels();
 
-    // X and its norm; squares up to a thread's in fp32 would do for the range, four at a time keep the sum exact enough.
+    // The norm (squares eight at a time in fp32, then in fp64), and X.
     const void *const u = a.update[which] ? a.update[which] : a.u_table[a.index[which]];
     const void *const gr = a.grad[which];
     const int cols = a.cols[which], count = a.rows[which] * cols;
     const bool tall = a.rows[which] > cols;
     const float beta = a.beta, rest = 1.f - a.beta;
-    const auto element = [&](int i) {
-        float v = value_at(u, i, a.update_bf16);
-        if (gr) v = beta * v + rest * value_at(gr, i, a.grad_bf16);
-        return v;
+    // eight elements a thread, all of them on their way at once
+    constexpr int AHEAD = 8;
+    const auto fetch = [&](int i0, float (&v)[AHEAD]) {
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const int i = i0 + e * SMALL_THREADS;
+            v[e] = i < count ? value_at(u, i, a.update_bf16) : 0.f;
+        }
+        if (gr) {
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int i = i0 + e * SMALL_THREADS;
+                v[e] = beta * v[e] + rest * (i < count ? value_at(gr, i, a.grad_bf16) : 0.f);
+            }
+        }
     };
     double sum = 0;
-#pragma unroll 4
-    for (int i = tid; i < count; i += SMALL_THREADS) {
-        const float v = element(i);
-        sum += v * v;
+    for (int i0 = tid; i0 < count; i0 += AHEAD * SMALL_THREADS) {
+        float v[AHEAD], part = 0;
+        fetch(i0, v);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) part += v[e] * v[e];
+        sum += part;
     }
 #pragma unroll
     for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
@@ -132,14 +145,19 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
 #pragma unroll
     for (int w = 0; w < SMALL_THREADS / 32; ++w) sum += sums[w];
     const float factor = static_cast<float>(static_cast<double>(SMALL_UNIT) / (sqrt(sum) + static_cast<double>(a.eps)));
-#pragma unroll 4
-    for (int i = tid; i < count; i += SMALL_THREADS) {
-        const int r = i / cols, c = i - r * cols;
-        const float v = element(i) * factor;
-        char *const to = x + (tall ? place(p, c, r) : place(p, r, c));
-        const __half h = __float2half_rn(v);
-        *reinterpret_cast<__half *>(to) = h;
-        *reinterpret_cast<__half *>(to + p.x_bytes()) = __float2half_rn(v - __half2float(h));
+    for (int i0 = tid; i0 < count; i0 += AHEAD * SMALL_THREADS) {
+        float v[AHEAD];
+        fetch(i0, v);
+#pragma unroll
+        for (int e = 0; e < AHEAD; ++e) {
+            const int i = i0 + e * SMALL_THREADS, r = i / cols, c = i - r * cols;
+            if (i >= count) break;
+            v[e] *= factor;
+            char *const to = x + (tall ? place(p, c, r) : place(p, r, c));
+            const __half h = __float2half_rn(v[e]);
+            *reinterpret_cast<__half *>(to) = h;
+            *reinterpret_cast<__half *>(to + p.x_bytes()) = __float2half_rn(v[e] - __half2float(h));
+        }
     }
 
     const uint32_t at_x = smem_u32(x), at_g = smem_u32(g);
@@ -224,15 +242,19 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
                     }
                 } else if (row < p.n) {
                     const float scale = a.scale[which] / (SMALL_UNIT * SMALL_UNIT);
-                    float *const to = static_cast<float *>(a.out[which] ? a.out[which] : a.x_table[a.index[which]]);
+                    const bool step_of_x = !a.out[which];
+                    float *const to = static_cast<float *>(step_of_x ? a.x_table[a.index[which]] : a.out[which]);
+                    const int col0 = c0 + c, each = tall ? cols : 1, left = p.m - col0;
+                    const int i = tall ? col0 * cols + row : row * cols + col0;
+                    float was[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) was[e] = step_of_x && e < left ? to[i + e * each] : 0.f;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const int col = c0 + c + e;
-                        if (col >= p.m) break;
-                        const int i = tall ? col * cols + row : row * cols + col;
-                        if (!a.out[which]) to[i] = a.decay * to[i] - scale * v[e];
-                        else if (a.out_bf16) reinterpret_cast<__nv_bfloat16 *>(to)[i] = __float2bfloat16_rn(scale * v[e]);
-                        else to[i] = scale * v[e];
+                        v[e] = step_of_x ? a.decay * was[e] - scale * v[e] : scale * v[e];
+                        if (e >= left) continue;
+                        if (a.out_bf16) reinterpret_cast<__nv_bfloat16 *>(to)[i + e * each] = __float2bfloat16_rn(v[e]);
+                        else to[i + e * each] = v[e];
                     }
                 }
             }
