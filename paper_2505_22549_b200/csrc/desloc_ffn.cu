@@ -164,6 +164,116 @@ struct DzEpilogue {
     }
 };
 
+// ---- single tokens -----------------------------------------------------------------------------------
+// Up to FFN_FEW tokens of a worker: a warp for each row of the weights, which it reads from one end to the other.  Bound: HBM, the weights once.  (Tiles of the tensor cores
+// bring 128 bytes of many rows at a time, for which memory is slower.  Four workers, one token, width 2048, hidden 8192, 403 MB: 67 us, 6.0 TB/s, 0.92 of copy; by tiles
+// 100 us.)  Sums in fp32, lanes' sums in a fixed order.
+constexpr int FFN_FEW = 4, FEW_THREADS = 256, FEW_AHEAD = 4;
+
+// Sums of a row of w (and, where W = 2, of a second one) times T rows of x, of which the next one is x_ld further on.
+template <int W, int T>
+__device__ __forceinline__ void dots(const __nv_bfloat16 *const (&w)[W], const __nv_bfloat16 *x, long long x_ld, int k, float (&sum)[W][T]) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t) sum[i][t] = 0.f;
+    uintptr_t low = reinterpret_cast<uintptr_t>(x) | static_cast<uintptr_t>(T > 1 ? x_ld * 2 : 0) | static_cast<uintptr_t>(k * 2);
+    for (const __nv_bfloat16 *p : w) low |= reinterpret_cast<uintptr_t>(p);
+    if (low % 16 == 0) {
+        for (int c = 8 * lane; c < k; c += 256 * FEW_AHEAD) {
+            uint4 v[FEW_AHEAD][W];
+#pragma unroll
+            for (int a = 0; a < FEW_AHEAD; ++a)
+#pragma unroll
+                for (int i = 0; i < W; ++i) v[a][i] = c + 256 * a < k ? __ldcs(reinterpret_cast<const uint4 *>(w[i] + c + 256 * a)) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int a = 0; a < FEW_AHEAD; ++a) {
+                if (c + 256 * a >= k) break;
+                float f[W][8];
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    const uint32_t h[4] = {v[a][i].x, v[a][i].y, v[a][i].z, v[a][i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float2 two = unpack_bf16(h[e]);
+                        f[i][2 * e] = two.x, f[i][2 * e + 1] = two.y;
+                    }
+                }
+#pragma unroll
+                for (int t = 0; t < T; ++t) {
+                    float y[8];
+                    load_values(x + t * x_ld + c + 256 * a, y);
+#pragma unroll
+                    for (int i = 0; i < W; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum[i][t] = fmaf(f[i][e], y[e], sum[i][t]);
+                }
+            }
+        }
+    } else {
+#pragma unroll 4
+        for (int c = lane; c < k; c += 32)
+#pragma unroll
+            for (int t = 0; t < T; ++t) {
+                const float y = __bfloat162float(x[t * x_ld + c]);
+#pragma unroll
+                for (int i = 0; i < W; ++i) sum[i][t] = fmaf(__bfloat162float(w[i][c]), y, sum[i][t]);
+            }
+    }
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+#pragma unroll
+        for (int t = 0; t < T; ++t)
+#pragma unroll
+            for (int d = 16; d; d /= 2) sum[i][t] += __shfl_xor_sync(0xffffffffu, sum[i][t], d);
+}
+
+template <int T>
+__global__ void __launch_bounds__(FEW_THREADS, T <= 2 ? 4 : 3) ffn_few_up_kernel(const __grid_constant__ FfnArgs a, __nv_bfloat16 *z) {
+    begin_and_let_next_begin();
+    const int m = blockIdx.y, j = blockIdx.x * (FEW_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    wait_for_earlier_kernels();
+    if (j >= a.hidden) return;
+    const long long at = static_cast<long long>(j) * a.width;
+    const __nv_bfloat16 *const w[2] = {static_cast<const __nv_bfloat16 *>(a.gate[m]) + at, static_cast<const __nv_bfloat16 *>(a.up[m]) + at};
+    float sum[2][T];
+    dots<2, T>(w, static_cast<const __nv_bfloat16 *>(a.h) + m * a.hs0, a.hs1, a.width, sum);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+        if (lane == t) {
+            const long long to = (static_cast<long long>(m) * T + t) * a.hidden + j;
+            z[to] = __float2bfloat16_rn(sum[0][t] * sigmoid(sum[0][t]) * sum[1][t]);
+            if (a.kept_gate) {
+                static_cast<__nv_bfloat16 *>(a.kept_gate)[to] = __float2bfloat16_rn(sum[0][t]);
+                static_cast<__nv_bfloat16 *>(a.kept_up)[to] = __float2bfloat16_rn(sum[1][t]);
+            }
+        }
+}
+
+template <int T>
+__global__ void __launch_bounds__(FEW_THREADS, T <= 2 ? 4 : 3) ffn_few_down_kernel(const __grid_constant__ FfnArgs a, const __nv_bfloat16 *z) {
+    begin_and_let_next_begin();
+    const int m = blockIdx.y, j = blockIdx.x * (FEW_THREADS / 32) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    wait_for_earlier_kernels();
+    if (j >= a.width) return;
+    const __nv_bfloat16 *const w[1] = {static_cast<const __nv_bfloat16 *>(a.down[m]) + static_cast<long long>(j) * a.hidden};
+    float sum[1][T];
+    dots<1, T>(w, z + static_cast<long long>(m) * T * a.hidden, a.hidden, a.hidden, sum);
+#pragma unroll
+    for (int t = 0; t < T; ++t)
+        if (lane == t) static_cast<__nv_bfloat16 *>(a.y)[m * a.ys0 + t * a.ys1 + j] = __float2bfloat16_rn(sum[0][t]);
+}
+
+template <int T>
+cudaError_t launch_few(const FfnArgs &a, __nv_bfloat16 *z, cudaStream_t stream, int *launches) {
+    const auto blocks = [&](int n) { return dim3((n + FEW_THREADS / 32 - 1) / (FEW_THREADS / 32), a.M); };
+    cudaError_t e = launch_op(ffn_few_up_kernel<T>, blocks(a.hidden), dim3(FEW_THREADS), 0, true, stream, a, z);
+    if (e == cudaSuccess) ++*launches, e = launch_op(ffn_few_down_kernel<T>, blocks(a.width), dim3(FEW_THREADS), 0, true, stream, a, z);
+    if (e == cudaSuccess) ++*launches;
+    return e;
+}
+
 // ---- rows that the copy engine does not take ---------------------------------------------------------
 // Copies matrices into rows of a multiple of eight values.  Bound: HBM, two bytes each way; a warp per row, lanes along it.
 constexpr int PACK_MOST = 64;
@@ -342,7 +452,8 @@ cudaError_t weight_grads(const FfnArgs &a, const Operands &o, const Operand &z, 
 int64_t ffn_work(const FfnArgs &a, bool backward) {
     Bump bump{nullptr};
     const Operands o(a, backward);
-    for (const Operand *x : {&o.h, &o.dy, &o.gate, &o.up, &o.down}) bump.take(x->bytes);
+    if (backward || a.tokens > FFN_FEW)
+        for (const Operand *x : {&o.h, &o.dy, &o.gate, &o.up, &o.down}) bump.take(x->bytes);
     for (int i = 0; i < (backward ? 3 : 1); ++i) bump.take(static_cast<int64_t>(a.M) * a.tokens * padded(a.hidden) * 2);
     return bump.used;
 }
@@ -350,6 +461,10 @@ int64_t ffn_work(const FfnArgs &a, bool backward) {
 cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
     const Run r{stream, err, wait_limit, launches};
     Bump bump{work};
+    if (a.tokens <= FFN_FEW) {
+        __nv_bfloat16 *const few = static_cast<__nv_bfloat16 *>(bump.take(static_cast<int64_t>(a.M) * a.tokens * a.hidden * 2));
+        return (a.tokens == 1 ? launch_few<1> : a.tokens == 2 ? launch_few<2> : a.tokens == 3 ? launch_few<3> : launch_few<4>)(a, few, stream, launches);
+    }
     Operands o(a, false);
     const long long ld = padded(a.hidden), per = a.tokens * ld;
     __nv_bfloat16 *const z = static_cast<__nv_bfloat16 *>(bump.take(a.M * per * 2));
