@@ -53,7 +53,7 @@ struct GemmArgs {
     int tile_n, stages, segments;   // columns of a tile; stages of the ring; pairs of operands that one accumulator sums
     int pairs;               // blocks work in pairs
     int dual;                // the tile's columns are two halves, of two B operands
-    int symmetric;           // only tiles that reach the lower triangle
+    int symmetric;           // only tiles that reach the lower triangle, of a product of one operand with itself
     int rotate;              // every tile begins with another k
     uint32_t idesc;          // without the operands' layouts
     int *err;
@@ -285,6 +285,9 @@ __device__ __forceinline__ float2 unpack_bf16(uint32_t w) { return make_float2(_
 struct TileWalk {
     int group = 0;
     int batch, i, j;   // matrix of the group, tile along m and n
+    // Whether a tile's rows are its columns, too: then what is brought for A serves as B.
+    template <int CG, typename A>
+    __device__ __forceinline__ bool diagonal(const A &a) const { return a.symmetric && i == j && a.tile_n == CG * GEMM_BM; }
     template <int CG, typename A>
     __device__ __forceinline__ const GemmGroup &find(const A &a, int tile) {
         while (group + 1 < a.ngroups && a.groups[group + 1].tile0 <= tile) ++group;
@@ -362,7 +365,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
                 const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
                 const int boxes = (own_n + 63) / 64, turned = a.rotate ? static_cast<int>(tile * 29u % steps) : 0;
-                const uint32_t bytes = ((g.a_mn ? GEMM_BM : g.a_rows) + (g.b_mn ? 64 * boxes : own_n)) * (GEMM_BK * 2);
+                const bool once = at.diagonal<CG>(a);
+                const uint32_t bytes = ((g.a_mn ? GEMM_BM : g.a_rows) + (once ? 0 : g.b_mn ? 64 * boxes : own_n)) * (GEMM_BK * 2);
                 for (int kk = 0; kk < steps * a.segments; ++kk) {
                     ok = bar_wait(&empty[s], phase ^ 1, a.wait_limit);
                     if (!ok) break;
@@ -384,7 +388,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                     } else {
                         tma_load<CG>(sa, ma, k0, m0, za, bar);
                     }
-                    if (g.b_mn) {
+                    if (once) {
+                    } else if (g.b_mn) {
                         for (int x = 0; x < boxes; ++x) tma_load<CG>(sb + x * (64 * GEMM_BK * 2), mb, n0 + 64 * x, k0, zb, bar);
                     } else if (!a.dual) {
                         tma_load<CG>(sb, mb, k0, n0, zb, bar);
@@ -418,13 +423,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 if (!ok) break;
                 tmem_fence_after();
                 const uint32_t d = tmem + buf * 256, idesc = a.idesc | (g.a_mn ? 1u << 15 : 0) | (g.b_mn ? 1u << 16 : 0);
+                const bool once = at.diagonal<CG>(a);
                 const uint32_t ka = (g.a_mn ? 2048 : 32) >> 4, kb = (g.b_mn ? 2048 : 32) >> 4;
                 for (int kk = 0; kk < steps; ++kk) {
                     ok = bar_wait(&full[s], phase, a.wait_limit);
                     if (!ok) break;
                     tmem_fence_after();
                     const uint32_t sa = smem_u32(ring + s * stage_bytes);
-                    const uint64_t da = operand_desc(sa, g.a_mn), db = operand_desc(sa + GEMM_A_BYTES, g.b_mn);
+                    const uint64_t da = operand_desc(sa, g.a_mn), db = once ? da : operand_desc(sa + GEMM_A_BYTES, g.b_mn);
 #pragma unroll
                     for (int x = 0; x < GEMM_BK / 16; ++x) mma_f16<CG>(d, da + x * ka, db + x * kb, idesc, kk > 0 || x > 0);
                     mma_commit<CG>(&empty[s]);

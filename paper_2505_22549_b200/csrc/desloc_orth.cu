@@ -211,6 +211,7 @@ __device__ __forceinline__ void carried(const char *st, int lane, int half, floa
 struct NextEpilogue {
     static constexpr int STAGING = 2 * 2048;
     float lo;
+    int both;   // the smaller part is written, too
     struct Ahead {
         uint4 v[4];
     };
@@ -232,30 +233,31 @@ struct NextEpilogue {
                 const float2 h = unpack_f16(hi[e]);
                 lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
             }
-            put16(st, lane, half, lo);
+            if (a.epi.both) put16(st, lane, half, lo);
             put16(st + 2048, lane, half, hi);
         }
     }
-    __device__ static void send(const Args &, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
+    __device__ static void send(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, true);
         const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
         send16(st + 2048, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p);
-        send16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p);
+        if (a.epi.both) send16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p);
     }
 };
 
-// What the last step gives: to a tensor of the caller's, or into the step of x.
+// What the last step gives: to a tensor of the caller's, or into the step of x.  (The smaller part of X has no place in it: no step follows that would enlarge what is rounded
+// away here, 2^-12 of X times a.)
 enum { ORTH_TO_F32 = 0, ORTH_TO_BF16 = 1, ORTH_TO_X = 2 };
 template <int TO>
 struct LastEpilogue {
-    static constexpr int STAGING = TO == ORTH_TO_BF16 ? 2048 : 2048 + 4096, WIDE = 2048;   // where fp32 pieces are
-    float lo, scale[ORTH_SHAPES];     // of the shape: with 1 / ORTH_UNIT; of the step with the learning rate
+    static constexpr int STAGING = TO == ORTH_TO_BF16 ? 2048 : 4096;
+    float scale[ORTH_SHAPES];         // of the shape: with 1 / ORTH_UNIT^2; of the step with the learning rate
     float decay;
     void *out[ORTH_ROUND];
     float *const *table;
     int index[ORTH_ROUND];
     struct Ahead {
-        uint4 v[4], x[TO == ORTH_TO_X ? 8 : 1];
+        uint4 x[TO == ORTH_TO_X ? 8 : 1];
     };
     using Args = GemmArgs<LastEpilogue>;
     __device__ __forceinline__ static void *to(const Args &a, const GemmGroup &g, int batch) {
@@ -267,15 +269,13 @@ struct LastEpilogue {
         return piece_at(g, row0, col0, ((reinterpret_cast<uintptr_t>(out) | static_cast<uintptr_t>(g.out_ld * SIZE)) & 15) == 0);
     }
     __device__ static void fetch(const Args &a, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
-        fetch16(static_cast<const __half *>(g.in[0]) + batch * g.in_batch + row0 * g.in_ld + col0, g.in_ld, piece_at(g, row0, col0, true), lane, x.v);
         if constexpr (TO == ORTH_TO_X) {
             const float *out = static_cast<const float *>(to(a, g, batch));
             fetch32(out + row0 * g.out_ld + col0, g.out_ld, piece(g, out, row0, col0), lane, x.x);
         }
     }
     __device__ static void settle(char *st, int lane, const Ahead &x) {
-        settle16(st, lane, x.v);
-        if constexpr (TO == ORTH_TO_X) settle32(st + WIDE, lane, x.x);
+        if constexpr (TO == ORTH_TO_X) settle32(st, lane, x.x);
     }
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         if (piece_at(g, row0, col0, true).none()) return;
@@ -283,7 +283,8 @@ struct LastEpilogue {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float v[16];
-            carried(st, lane, half, g.alpha, a.epi.lo, d, v);
+            tmem_load16(d + 16 * half, v);
+            tmem_wait();
             if constexpr (TO == ORTH_TO_BF16) {
                 uint32_t w[8];
 #pragma unroll
@@ -292,14 +293,14 @@ struct LastEpilogue {
             } else {
                 if constexpr (TO == ORTH_TO_X) {
                     float x[16];
-                    row32(st + WIDE, lane, half, x);
+                    row32(st, lane, half, x);
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] = a.epi.decay * x[e] - scale * v[e];
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) v[e] *= scale;
                 }
-                put32(st + WIDE, lane, half, v);
+                put32(st, lane, half, v);
             }
         }
     }
@@ -308,7 +309,7 @@ struct LastEpilogue {
         const Piece p = piece(g, out, row0, col0);
         const long long at = row0 * g.out_ld + col0;
         if constexpr (TO == ORTH_TO_BF16) send16(st, lane, static_cast<__nv_bfloat16 *>(out) + at, g.out_ld, p);
-        else send32(st + WIDE, lane, static_cast<float *>(out) + at, g.out_ld, p);
+        else send32(st, lane, static_cast<float *>(out) + at, g.out_ld, p);
     }
 };
 
@@ -479,13 +480,12 @@ cudaError_t last(const OrthArgs &a, const Round &r, int side, const Run &run) {
     using E = LastEpilogue<TO>;
     static thread_local GemmArgs<E> args;
     static thread_local E epi;
-    epi.lo = a.coefficients[3 * (a.steps - 1)] / ORTH_LO;
     epi.decay = a.decay;
     epi.table = a.x_table;
     long long ld[ORTH_SHAPES];
     for (int i = 0; i < r.nshapes; ++i) {
         const Shape &s = r.shapes[i];
-        epi.scale[i] = static_cast<float>(scale_of(a, s.rows, s.cols) / ORTH_UNIT);
+        epi.scale[i] = static_cast<float>(scale_of(a, s.rows, s.cols) / (ORTH_UNIT * ORTH_UNIT));
         ld[i] = s.cols;
     }
     for (int i = 0; i < r.count; ++i) epi.out[i] = a.list[r.first + i].out, epi.index[i] = a.list[r.first + i].index;
@@ -546,7 +546,7 @@ cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit,
             e = symmetric(r, true, side, 1.f / ORTH_UNIT, 0.f, 0.f, run);
             if (e == cudaSuccess) e = symmetric(r, false, side, c[2] / ORTH_UNIT, c[1], c[0] * ORTH_UNIT, run);
             if (e != cudaSuccess) break;
-            if (k + 1 < a.steps) e = update(r, side, NextEpilogue{c[0] / ORTH_LO}, next, nullptr, run);
+            if (k + 1 < a.steps) e = update(r, side, NextEpilogue{c[0] / ORTH_LO, k + 2 < a.steps}, next, nullptr, run);
             else if (a.list[at].out == nullptr) e = last<ORTH_TO_X>(a, r, side, run);
             else e = a.out_bf16 ? last<ORTH_TO_BF16>(a, r, side, run) : last<ORTH_TO_F32>(a, r, side, run);
         }

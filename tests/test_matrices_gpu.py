@@ -290,9 +290,9 @@ def newton_schulz(u, steps=DEFAULT, eps=1e-7, rounded=False):
     unit, lo = 256.0, 2048.0
     half = lambda v: (v * unit).half().double() / unit if rounded else v
     one = torch.eye(x.shape[0], dtype=torch.float64, device=x.device)
-    for a, b, c in steps:
+    for k, (a, b, c) in enumerate(steps):
         hi = half(x)
-        rest = half((x - hi) * lo) / lo
+        rest = half((x - hi) * lo) / lo if not rounded or k + 1 < len(steps) else 0.0
         g = half(hi @ hi.mT)
         x = half(a * one + b * g + c * (g @ g)) @ hi + a * rest
     return x.mT if tall else x
