@@ -54,6 +54,7 @@ struct GemmArgs {
     int pairs;               // blocks work in pairs
     int dual;                // the tile's columns are two halves, of two B operands
     int symmetric;           // only tiles that reach the lower triangle, of a product of one operand with itself
+    int row_first, row_rest, row_more, row_rest_more;   // of those: tiles in the first row of tiles and in each further one, by division with rest
     int rotate;              // every tile begins with another k
     uint32_t idesc;          // without the operands' layouts
     int *err;
@@ -281,30 +282,51 @@ __device__ __forceinline__ float2 unpack_f16(uint32_t w) { return __half22float2
 __device__ __forceinline__ float2 unpack_bf16(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 
 // ---- the kernel --------------------------------------------------------------------------------------
-// Where a tile lies; goes on with the tile's number.
+// Where a tile lies; goes on with the tile's number.  Tiles of a matrix are counted along m first (of a symmetric product row by row, each as far as the diagonal), and a step is
+// the same every time: divisions where a group begins alone.
 struct TileWalk {
-    int group = 0;
-    int batch, i, j;   // matrix of the group, tile along m and n
+    int group = -1;
+    int batch, i, j;             // matrix of the group, tile along m and n
+    int at, by_batch, by_i, by_j;   // symmetric: number within the matrix; what a step adds
     // Whether a tile's rows are its columns, too: then what is brought for A serves as B.
     template <int CG, typename A>
     __device__ __forceinline__ bool diagonal(const A &a) const { return a.symmetric && i == j && a.tile_n == CG * GEMM_BM; }
     template <int CG, typename A>
     __device__ __forceinline__ const GemmGroup &find(const A &a, int tile) {
+        const int step = gridDim.x / CG, was = group;
+        group = max(group, 0);
         while (group + 1 < a.ngroups && a.groups[group + 1].tile0 <= tile) ++group;
         const GemmGroup &g = a.groups[group];
-        int t = tile - g.tile0;
-        batch = t / g.per;
-        t -= batch * g.per;
-        if (a.symmetric) {   // row i of tiles reaches as far as the diagonal
+        if (a.symmetric) {
+            if (group != was) {
+                at = tile - g.tile0;
+                batch = at / g.per, by_batch = step / g.per;
+                at -= batch * g.per, by_i = step - by_batch * g.per;
+            } else {
+                batch += by_batch, at += by_i;
+                if (at >= g.per) at -= g.per, ++batch;
+            }
+            // rows of the tiles: row i has 1 + (its last row / tile_n) of them
+            int t = at, here = a.row_first, rest = a.row_rest;
             for (i = 0;; ++i) {
-                const int here = min((i * CG * GEMM_BM + CG * GEMM_BM - 1) / a.tile_n + 1, g.nt);
-                if (t < here) break;
-                t -= here;
+                const int some = min(here, g.nt);
+                if (t < some) break;
+                t -= some;
+                here += a.row_more, rest += a.row_rest_more;
+                if (rest >= a.tile_n) rest -= a.tile_n, ++here;
             }
             j = t;
+        } else if (group != was) {
+            const int t = tile - g.tile0, column = t / g.mt;
+            i = t - column * g.mt;
+            batch = column / g.nt, j = column - batch * g.nt;
+            const int columns = step / g.mt;
+            by_i = step - columns * g.mt;
+            by_batch = columns / g.nt, by_j = columns - by_batch * g.nt;
         } else {
-            j = t / g.mt;
-            i = t - j * g.mt;
+            i += by_i, j += by_j, batch += by_batch;
+            if (i >= g.mt) i -= g.mt, ++j;
+            if (j >= g.nt) j -= g.nt, ++batch;
         }
         return g;
     }
@@ -586,6 +608,9 @@ template <typename E>
 void begin_gemm(GemmArgs<E> &a, bool bf16, const GemmCut &cut, bool dual, bool symmetric, int segments) {
     a.ngroups = a.tiles = 0;
     a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.rotate = 0, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
+    const int bm = GEMM_BM * (cut.pairs ? 2 : 1);
+    a.row_first = (bm - 1) / cut.tile_n + 1, a.row_rest = (bm - 1) % cut.tile_n;
+    a.row_more = bm / cut.tile_n, a.row_rest_more = bm % cut.tile_n;
     const uint32_t type = bf16 ? 1 : 0;
     a.idesc = 1u << 4 | type << 7 | type << 10 | static_cast<uint32_t>(cut.tile_n >> 3) << 17 | static_cast<uint32_t>((cut.pairs ? 2 : 1) * GEMM_BM >> 4) << 24;
 }

@@ -155,13 +155,15 @@ struct SymEpilogue {
         // one of the even column, the odd one of the odd column.
         const bool odd = lane & 1, both = (lane | 1) < p.rows, one = (lane & ~1) < p.rows;
         uint32_t *t = reinterpret_cast<uint32_t *>(out + (col0 + odd) * g.out_ld + row0 + (lane & ~1));
-#pragma unroll 1
+        float sums[2][16];
+        tmem_load16(d, sums[0]);
+        tmem_load16(d + 16, sums[1]);
+        tmem_wait();
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
-            float v[16];
+            float (&v)[16] = sums[half];
             uint32_t w[8];
-            tmem_load16(d + 16 * half, v);
             if (g.in[0]) row16(st, lane, half, w);
-            tmem_wait();
 #pragma unroll
             for (int e = 0; e < 16; ++e) v[e] *= g.alpha;
             if (g.in[0]) {
@@ -196,11 +198,9 @@ struct SymEpilogue {
 };
 
 // X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
-__device__ __forceinline__ void carried(const char *st, int lane, int half, float alpha, float lo, uint32_t d, float (&v)[16]) {
+__device__ __forceinline__ void carried(const char *st, int lane, int half, float alpha, float lo, float (&v)[16]) {
     uint32_t w[8];
-    tmem_load16(d + 16 * half, v);
     row16(st, lane, half, w);
-    tmem_wait();
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         const float2 l = unpack_f16(w[e]);
@@ -222,10 +222,14 @@ struct NextEpilogue {
     __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         if (piece_at(g, row0, col0, true).none()) return;
-#pragma unroll 1
+        float sums[2][16];
+        tmem_load16(d, sums[0]);
+        tmem_load16(d + 16, sums[1]);
+        tmem_wait();
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
-            float v[16];
-            carried(st, lane, half, g.alpha, a.epi.lo, d, v);
+            float (&v)[16] = sums[half];
+            carried(st, lane, half, g.alpha, a.epi.lo, v);
             uint32_t hi[8], lo[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
@@ -280,11 +284,13 @@ struct LastEpilogue {
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
         if (piece_at(g, row0, col0, true).none()) return;
         const float scale = a.epi.scale[&g - a.groups];
-#pragma unroll 1
+        float sums[2][16];
+        tmem_load16(d, sums[0]);
+        tmem_load16(d + 16, sums[1]);
+        tmem_wait();
+#pragma unroll
         for (int half = 0; half < 2; ++half) {
-            float v[16];
-            tmem_load16(d + 16 * half, v);
-            tmem_wait();
+            float (&v)[16] = sums[half];
             if constexpr (TO == ORTH_TO_BF16) {
                 uint32_t w[8];
 #pragma unroll
