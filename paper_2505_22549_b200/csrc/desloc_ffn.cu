@@ -15,12 +15,13 @@ __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f +
 // z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.
 struct UpEpilogue {
     static constexpr int STAGING = 3 * 2048;
+    static constexpr bool READS_BOXES = false, WRITES_BOXES = true;
     struct Ahead {};
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
     using Args = GemmArgs<UpEpilogue>;
     __device__ static void fetch(const Args &, const GemmGroup &, int, int, int, int, Ahead &) {}
     __device__ static void settle(char *, int, const Ahead &) {}
-    __device__ static void drain(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        if (piece_at(g, row0, col0, true).none()) return;
+    __device__ static void drain(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float gv[16], uv[16];
@@ -43,6 +44,9 @@ struct UpEpilogue {
             put16(st, lane, half, w);
         }
     }
+    __device__ static void send_boxes(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, const char *) {
+        for (int k = 0; k < (g.out[1] ? 3 : 1); ++k) tma_store(&a.maps[g.out_map + k], col0, row0, g.io_batch + batch, st + 2048 * k);
+    }
     __device__ static void send(const Args &, const GemmGroup &g, int, int row0, int col0, const char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, g.wide & 1), q = piece_at(g, row0, col0, (g.wide & 2) != 0);
         send16(st, lane, static_cast<__nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p);
@@ -58,6 +62,8 @@ struct UpEpilogue {
 template <bool BF16, bool ADD>
 struct StoreEpilogue {
     static constexpr int STAGING = BF16 ? 2048 : 4096;
+    static constexpr bool READS_BOXES = false, WRITES_BOXES = false;
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
     struct Was {
         uint4 v[BF16 ? 4 : 8];
     };
@@ -75,8 +81,7 @@ struct StoreEpilogue {
         if constexpr (ADD && BF16) settle16(st, lane, x.v);
         else if constexpr (ADD) settle32(st, lane, x.v);
     }
-    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        if (piece_at(g, row0, col0, true).none()) return;
+    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             float v[16];
@@ -118,6 +123,8 @@ struct StoreEpilogue {
 // From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.
 struct DzEpilogue {
     static constexpr int STAGING = 3 * 2048;
+    static constexpr bool READS_BOXES = false, WRITES_BOXES = true;
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
     struct Ahead {
         uint4 g[4], u[4];
     };
@@ -132,8 +139,7 @@ struct DzEpilogue {
         settle16(st, lane, x.g);
         settle16(st + 2048, lane, x.u);
     }
-    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, int lane) {
-        if (piece_at(g, row0, col0, true).none()) return;
+    __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
             uint32_t gw[8], uw[8], zw[8];
@@ -154,6 +160,9 @@ struct DzEpilogue {
             put16(st + 2048, lane, half, uw);
             put16(st + 4096, lane, half, zw);
         }
+    }
+    __device__ static void send_boxes(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, const char *) {
+        for (int k = 0; k < 3; ++k) tma_store(&a.maps[g.out_map + k], col0, row0, g.io_batch + batch, st + (k == 0 ? 4096 : 2048 * (k - 1)));
     }
     __device__ static void send(const Args &, const GemmGroup &g, int, int row0, int col0, const char *st, int lane) {
         const Piece p = piece_at(g, row0, col0, g.wide & 1);
@@ -361,6 +370,9 @@ cudaError_t pack(Operand &o, int M, long long s0, long long s1, Bump &bump, cuda
     return cudaSuccess;
 }
 
+// Results leave as boxes where emptying a tile takes longer than its products, in which the copy engine has more to do: products of up to BOXES_K (8192 x 576 x 1536 by four
+// workers 173 us instead of 194; 2048 x 2048 x 8192 304 us instead of 293).
+constexpr int BOXES_K = 1024;
 constexpr int WORKERS = 16;   // of a launch: three groups and two maps each at most
 
 struct Run {
@@ -493,9 +505,20 @@ cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, c
             }
             if (e != cudaSuccess) return e;
         }
+        // z, and g and u where they are kept and lie so, leave as boxes
+        const int boxes = 1 + 2 * WORKERS;
+        bool whole = a.width <= BOXES_K;
+        for (int k = 0; k < (a.kept_gate ? 3 : 1) && whole; ++k) {
+            const void *const to = k == 0 ? z : k == 1 ? a.kept_gate : a.kept_up;
+            const long long to_ld = k == 0 ? ld : a.hidden;
+            whole = boxes_fit(to, to_ld);
+            if (whole) e = encode_boxes(&g.maps[boxes + k], to, true, a.hidden, a.tokens, a.M, to_ld, a.tokens * to_ld, 32, 32);
+            if (e != cudaSuccess) return e;
+        }
         for (int i = 0; i < some; ++i) {
             const int m = m0 + i;
             GemmGroup &group = add_group(g, a.tokens, a.hidden, a.width, 1);
+            if (whole) group.out_map = static_cast<short>(boxes), group.io_batch = m;
             group.a_batch = m;
             group.b_map = static_cast<short>(batched ? 1 : 1 + 2 * i), group.b_batch = batched ? m : 0;
             group.out[0] = z + m * per, group.out_ld = ld;
@@ -531,6 +554,9 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
             begin_gemm(g, true, cut, false, false, 1);
             e = o.dy.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
             if (e == cudaSuccess) e = o.down.maps(g, 1, 1, a.M, m0, some, 64);
+            const int boxes = 1 + WORKERS;
+            for (int k = 0; k < 3 && e == cudaSuccess && a.width <= BOXES_K; ++k)
+                e = encode_boxes(&g.maps[boxes + k], inner[k], true, a.hidden, a.tokens, a.M, ld, per, 32, 32);
             if (e != cudaSuccess) return e;
             for (int i = 0; i < some; ++i) {
                 const int m = m0 + i;
@@ -543,6 +569,7 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
                 group.in[1] = static_cast<const __nv_bfloat16 *>(a.was_up) + from;
                 group.in_ld = a.hidden;
                 for (int k = 0; k < 3; ++k) group.out[k] = inner[k] + m * per;
+                if (a.width <= BOXES_K) group.out_map = static_cast<short>(boxes), group.io_batch = m;
                 group.out_ld = ld;
                 group.wide = 1 | (wide16(group.in[0], a.hidden) && wide16(group.in[1], a.hidden) ? 2 : 0);
             }

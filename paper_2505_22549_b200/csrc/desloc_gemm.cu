@@ -3,7 +3,8 @@
 
 namespace desloc {
 
-cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t inner, int64_t outer, int64_t batch, int64_t ld, int64_t batch_ld, int rows) {
+cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t inner, int64_t outer, int64_t batch, int64_t ld, int64_t batch_ld, int rows,
+                         int columns) {
     using Encode = decltype(&cuTensorMapEncodeTiled);
     static const Encode encode = [] {
         void *f = nullptr;
@@ -14,9 +15,9 @@ cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t 
     if (!encode) return cudaErrorNotSupported;
     const cuuint64_t dims[3] = {static_cast<cuuint64_t>(inner), static_cast<cuuint64_t>(outer), static_cast<cuuint64_t>(batch)};
     const cuuint64_t strides[2] = {static_cast<cuuint64_t>(2 * ld), static_cast<cuuint64_t>(2 * batch_ld)};
-    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(rows), 1}, every[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {static_cast<cuuint32_t>(columns), static_cast<cuuint32_t>(rows), 1}, every[3] = {1, 1, 1};
     const CUresult r = encode(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(data), dims, strides, box, every,
-                              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                              CU_TENSOR_MAP_INTERLEAVE_NONE, columns == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }

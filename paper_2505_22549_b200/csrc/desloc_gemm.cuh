@@ -43,6 +43,8 @@ struct GemmGroup {
     float alpha;
     int first;               // number of its first matrix in a table of the epilogue's
     int wide;                // bits: out (1) and in (2) rows can be moved 16 bytes at a time
+    short in_map, out_map;   // boxes of 32 x 32 of what the epilogue reads and writes (out_map + k of out[k]), where the copy engine moves them; else -1
+    int io_batch;            // of its first matrix in those maps
 };
 
 template <typename E>
@@ -73,6 +75,14 @@ __device__ __forceinline__ void tma_load(void *dst, const CUtensorMap *map, int 
         asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
                      :: "r"(smem_u32(dst)), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
+// A box out of shared memory, told to the issuing thread's bulk groups.
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, int z, const void *src) {
+    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+                 :: "l"(map), "r"(x), "r"(y), "r"(z), "r"(smem_u32(src)) : "memory");
+}
+__device__ __forceinline__ void stores_asked() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void stores_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void stores_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 // The address of the first block's copy of a barrier.
 template <int CG>
 __device__ __forceinline__ uint32_t first_blocks(const uint64_t *bar) {
@@ -332,13 +342,15 @@ struct TileWalk {
     }
 };
 
-// E, the epilogue, takes 32 x 32 pieces: of what it reads, E::Ahead is fetched one piece ahead by E::fetch(args, group, batch, row, column, lane, ahead), put into the staging area
-// by E::settle(staging, lane, ahead); E::drain(args, group, batch, row, column, accumulator, staging, lane) takes it and the sums, and leaves what E::send(args, group, batch, row,
-// column, staging, lane) writes.  E::STAGING: bytes of that area, a warp's.
+// E, the epilogue, takes 32 x 32 pieces, those that E::wants(group, row, column) says.  What it reads comes one piece ahead: E::READS_BOXES, as a box by the copy engine, pieces in turn
+// into the first and second 2 KB of the warp's staging area (of E::STAGING bytes); else as E::Ahead by E::fetch(args, group, batch, row, column, lane, ahead), which
+// E::settle(staging, lane, ahead) puts there.  E::drain(args, group, batch, row, column, accumulator, staging, input, lane) takes it and the sums, and leaves what is
+// written: by E::send(args, group, batch, row, column, staging, lane), or (E::WRITES_BOXES, where the group has maps for it) by E::send_boxes(args, group, batch, row, column, staging, input),
+// which one lane calls.  What moves so costs a warp no time: reading, staging and writing 16 bytes a lane were two thirds of what emptying a piece took.
 template <typename E, int CG>
 __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_constant__ GemmArgs<E> a) {
     extern __shared__ __align__(1024) char gemm_smem[];
-    __shared__ __align__(8) uint64_t full[GEMM_MAX_STAGES], empty[GEMM_MAX_STAGES], ready[2], taken[2], drained;
+    __shared__ __align__(8) uint64_t full[GEMM_MAX_STAGES], empty[GEMM_MAX_STAGES], ready[2], taken[2], drained, arrived[2 * GEMM_EPI_WARPS];
     __shared__ uint32_t tmem_at, bytes_of[GEMM_MAX_STAGES];
     __shared__ int requested, failed;
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
@@ -356,6 +368,11 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         bar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (E::READS_BOXES && warp == 3) {
+        bar_init(&arrived[lane], 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    static_assert(2 * GEMM_EPI_WARPS == 32, "a barrier for each lane to initialise");
     if (warp == 2) {
         if constexpr (CG == 1) {
             asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
@@ -474,39 +491,68 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         constexpr int STEP = GEMM_EPI_WARPS / 4 * 32;   // columns that the warps take at a time
         const int quadrant = warp & 3, c0 = (warp - 4) / 4 * 32;
         char *const st = ring + a.stages * stage_bytes + (warp - 4) * E::STAGING;
+        uint64_t *const came = &arrived[2 * (warp - 4)];
         const int out_n = a.dual ? a.tile_n / 2 : a.tile_n;
         const int rows = (rank * 4 + quadrant) * 32;
         TileWalk at;
         typename E::Ahead ahead;
-        int buf = 0, tile = tile0, c = c0;
+        int buf = 0, tile = tile0, c = c0, asked = 0, taken_boxes = 0;
         uint32_t turn = 0;
         const GemmGroup *g = nullptr;
+        // what the next piece reads
+        const auto ask = [&] {
+            const int row0 = at.i * (CG * GEMM_BM) + rows, col0 = at.j * out_n + c;
+            if (c0 >= out_n || !E::wants(*g, row0, col0)) return;
+            if constexpr (E::READS_BOXES) {
+                if (g->in_map < 0) return;
+                if (elect_one()) {
+                    uint64_t *const bar = &came[asked & 1];
+                    bar_expect(bar, 2048);
+                    tma_load<1>(st + (asked & 1) * 2048, &a.maps[g->in_map], col0, row0, g->io_batch + at.batch, smem_u32(bar));
+                }
+                __syncwarp();
+                ++asked;
+            } else {
+                E::fetch(a, *g, at.batch, row0, col0, lane, ahead);
+            }
+        };
         if (tile < a.tiles) {
             g = &at.find<CG>(a, tile);
-            if (c0 < out_n) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
+            ask();
         }
+        bool ok = true;
         while (tile < a.tiles) {
             if (c == c0) {
-                if (!bar_wait(&ready[buf], turn, a.wait_limit)) {
-                    give_up();
-                    break;
-                }
+                ok = bar_wait(&ready[buf], turn, a.wait_limit);
+                if (!ok) break;
                 tmem_fence_after();
             }
             const GemmGroup &here = *g;
             const int batch = at.batch, row0 = at.i * (CG * GEMM_BM) + rows, col0 = at.j * out_n + c;
             const uint32_t d = tmem + buf * 256 + c + (static_cast<uint32_t>(32 * quadrant) << 16);
-            __syncwarp();   // (the piece before has been read)
-            E::settle(st, lane, ahead);
+            const bool wanted = c0 < out_n && E::wants(here, row0, col0), reads = E::READS_BOXES && wanted && here.in_map >= 0;
+            const char *const input = st + (taken_boxes & 1) * 2048;
+            // the piece before has left the staging area
+            if constexpr (E::WRITES_BOXES) {
+                if (elect_one()) stores_read();
+            }
+            __syncwarp();
+            if constexpr (!E::READS_BOXES) E::settle(st, lane, ahead);
             c += STEP;
             const bool last = c >= out_n;
             if (last) {
                 c = c0, tile += tile_step;
                 if (tile < a.tiles) g = &at.find<CG>(a, tile);
             }
-            if (tile < a.tiles && c0 < out_n) E::fetch(a, *g, at.batch, at.i * (CG * GEMM_BM) + rows, at.j * out_n + c, lane, ahead);
+            if (tile < a.tiles) ask();
+            if (reads) {
+                ok = bar_wait(&came[taken_boxes & 1], (taken_boxes >> 1) & 1, a.wait_limit);
+                if (!ok) break;
+                ++taken_boxes;
+            }
             __syncwarp();
-            if (c0 < out_n) E::drain(a, here, batch, row0, col0, d, st, lane);
+            if (wanted) E::drain(a, here, batch, row0, col0, d, st, input, lane);
+            if constexpr (E::WRITES_BOXES) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             tmem_fence_before();
             __syncwarp();
             if (last) {
@@ -518,7 +564,27 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 buf ^= 1;
                 if (buf == 0) turn ^= 1;
             }
-            if (c0 < out_n) E::send(a, here, batch, row0, col0, st, lane);
+            if (wanted) {
+                if constexpr (E::WRITES_BOXES) {
+                    if (here.out_map >= 0) {
+                        if (elect_one()) {
+                            E::send_boxes(a, here, batch, row0, col0, st, input);
+                            stores_asked();
+                        }
+                        continue;
+                    }
+                }
+                E::send(a, here, batch, row0, col0, st, lane);
+            }
+        }
+        if (!ok) give_up();
+        // what is on its way lands first
+        if constexpr (E::READS_BOXES) {
+            for (; taken_boxes < asked; ++taken_boxes) bar_wait(&came[taken_boxes & 1], (taken_boxes >> 1) & 1, GEMM_DRAIN_LIMIT);
+        }
+        __syncwarp();
+        if constexpr (E::WRITES_BOXES) {
+            if (elect_one()) stores_done();
         }
         __syncwarp();
     }
@@ -562,7 +628,8 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
 
 // ---- host --------------------------------------------------------------------------------------------
 // Boxes of 64 x `rows` values (k-major: 64 k of so many rows; m/n-major: 64 columns of so many k) of `batch` matrices of `outer` rows of `inner` 16-bit values.
-cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t inner, int64_t outer, int64_t batch, int64_t ld, int64_t batch_ld, int rows);
+// columns = 32: of 32 columns, swizzled by 64 bytes, as the epilogues stage them.
+cudaError_t encode_boxes(CUtensorMap *map, const void *data, bool bf16, int64_t inner, int64_t outer, int64_t batch, int64_t ld, int64_t batch_ld, int rows, int columns = 64);
 
 // Whether rows `ld` elements apart from `data` on can be fetched by the copy engine: 16-byte boundaries.
 inline bool boxes_fit(const void *data, int64_t ld) { return ((reinterpret_cast<uintptr_t>(data) | static_cast<uintptr_t>(ld * 2)) & 15u) == 0; }
@@ -623,6 +690,7 @@ GemmGroup &add_group(GemmArgs<E> &a, int m, int n, int k, int count) {
     const int out_n = cut.out_n(a.dual), bm = GEMM_BM * (a.pairs ? 2 : 1);
     g.tile0 = a.tiles;
     g.m = m, g.n = n, g.k = k, g.a_rows = box_rows(m);
+    g.in_map = g.out_map = -1;
     g.mt = (m + bm - 1) / bm, g.nt = (n + out_n - 1) / out_n;
     g.per = tiles_of(m, n, cut, a.dual, a.symmetric);
     a.tiles += g.per * count;

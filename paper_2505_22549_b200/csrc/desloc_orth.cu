@@ -137,19 +137,20 @@ __global__ void __launch_bounds__(ORTH_THREADS) orth_scale_kernel(const __grid_c
 // A symmetric result: alpha times the sums, plus b times in[0], plus `diagonal` there; pieces below the diagonal go to the other one's place, too.
 struct SymEpilogue {
     static constexpr int STAGING = 2048;
+    static constexpr bool READS_BOXES = false, WRITES_BOXES = false;   // (as boxes, which the turned ones can be, too, 15 % slower: the copy engine has the operands to bring)
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 <= row0; }
     float b, diagonal;
     struct Ahead {
         uint4 v[4];
     };
     using Args = GemmArgs<SymEpilogue>;
     __device__ static void fetch(const Args &, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
-        if (g.in[0] && col0 <= row0)
+        if (g.in[0])
             fetch16(static_cast<const __half *>(g.in[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true), lane, x.v);
     }
     __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
-    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
+    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
         const Piece p = piece_at(g, row0, col0, true);
-        if (p.none() || col0 > row0) return;
         __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
         // Columns of a piece below the diagonal are rows of the other one (p.cols is 32 there).  Neighbouring lanes, neighbouring rows of this piece, make words: the even
         // one of the even column, the odd one of the odd column.
@@ -192,36 +193,20 @@ struct SymEpilogue {
         }
     }
     __device__ static void send(const Args &, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
-        if (col0 <= row0)
-            send16(st, lane, static_cast<__half *>(g.out[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true));
+        send16(st, lane, static_cast<__half *>(g.out[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true));
     }
 };
 
 // X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
-__device__ __forceinline__ void carried(const char *st, int lane, int half, float alpha, float lo, float (&v)[16]) {
-    uint32_t w[8];
-    row16(st, lane, half, w);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const float2 l = unpack_f16(w[e]);
-        v[2 * e] = v[2 * e] * alpha + lo * l.x, v[2 * e + 1] = v[2 * e + 1] * alpha + lo * l.y;
-    }
-}
-
 struct NextEpilogue {
-    static constexpr int STAGING = 2 * 2048;
+    static constexpr int STAGING = 3 * 2048;
+    static constexpr bool READS_BOXES = true, WRITES_BOXES = true;
     float lo;
     int both;   // the smaller part is written, too
-    struct Ahead {
-        uint4 v[4];
-    };
+    struct Ahead {};
     using Args = GemmArgs<NextEpilogue>;
-    __device__ static void fetch(const Args &, const GemmGroup &g, int batch, int row0, int col0, int lane, Ahead &x) {
-        fetch16(static_cast<const __half *>(g.in[0]) + batch * g.in_batch + row0 * g.in_ld + col0, g.in_ld, piece_at(g, row0, col0, true), lane, x.v);
-    }
-    __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
-    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        if (piece_at(g, row0, col0, true).none()) return;
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
+    __device__ static void drain(const Args &a, const GemmGroup &g, int, int, int, uint32_t d, char *st, const char *input, int lane) {
         float sums[2][16];
         tmem_load16(d, sums[0]);
         tmem_load16(d + 16, sums[1]);
@@ -229,24 +214,25 @@ struct NextEpilogue {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             float (&v)[16] = sums[half];
-            carried(st, lane, half, g.alpha, a.epi.lo, v);
             uint32_t hi[8], lo[8];
+            row16(input, lane, half, lo);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
+                const float2 l = unpack_f16(lo[e]);
+                v[2 * e] = v[2 * e] * g.alpha + a.epi.lo * l.x, v[2 * e + 1] = v[2 * e + 1] * g.alpha + a.epi.lo * l.y;
                 hi[e] = pack_f16(v[2 * e], v[2 * e + 1]);
                 const float2 h = unpack_f16(hi[e]);
                 lo[e] = pack_f16((v[2 * e] - h.x) * ORTH_LO, (v[2 * e + 1] - h.y) * ORTH_LO);
             }
-            if (a.epi.both) put16(st, lane, half, lo);
-            put16(st + 2048, lane, half, hi);
+            if (a.epi.both) put16(const_cast<char *>(input), lane, half, lo);
+            put16(st + 4096, lane, half, hi);
         }
     }
-    __device__ static void send(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, int lane) {
-        const Piece p = piece_at(g, row0, col0, true);
-        const long long at = batch * g.in_batch + row0 * g.in_ld + col0;
-        send16(st + 2048, lane, static_cast<__half *>(g.out[0]) + at, g.in_ld, p);
-        if (a.epi.both) send16(st, lane, static_cast<__half *>(g.out[1]) + at, g.in_ld, p);
+    __device__ static void send_boxes(const Args &a, const GemmGroup &g, int batch, int row0, int col0, const char *st, const char *input) {
+        tma_store(&a.maps[g.out_map], col0, row0, g.io_batch + batch, st + 4096);
+        if (a.epi.both) tma_store(&a.maps[g.in_map], col0, row0, g.io_batch + batch, input);
     }
+    __device__ static void send(const Args &, const GemmGroup &, int, int, int, const char *, int) {}
 };
 
 // What the last step gives: to a tensor of the caller's, or into the step of x.  (The smaller part of X has no place in it: no step follows that would enlarge what is rounded
@@ -255,6 +241,8 @@ enum { ORTH_TO_F32 = 0, ORTH_TO_BF16 = 1, ORTH_TO_X = 2 };
 template <int TO>
 struct LastEpilogue {
     static constexpr int STAGING = TO == ORTH_TO_BF16 ? 2048 : 4096;
+    static constexpr bool READS_BOXES = false, WRITES_BOXES = false;
+    __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
     float scale[ORTH_SHAPES];         // of the shape: with 1 / ORTH_UNIT^2; of the step with the learning rate
     float decay;
     void *out[ORTH_ROUND];
@@ -281,8 +269,7 @@ struct LastEpilogue {
     __device__ static void settle(char *st, int lane, const Ahead &x) {
         if constexpr (TO == ORTH_TO_X) settle32(st, lane, x.x);
     }
-    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, int lane) {
-        if (piece_at(g, row0, col0, true).none()) return;
+    __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
         const float scale = a.epi.scale[&g - a.groups];
         float sums[2][16];
         tmem_load16(d, sums[0]);
@@ -468,13 +455,16 @@ cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const
         cudaError_t e = encode_boxes(&a.maps[of_x], s.hi[side], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, s.tall ? box_rows(s.rows) : 64);
         if (e == cudaSuccess)
             e = encode_boxes(&a.maps[of_poly], s.poly, false, s.n, s.n, s.count, s.square_ld, s.n * s.square_ld, s.tall ? cut.box_n(false) : box_rows(s.n));
+        if (!out_ld) {
+            const int boxes = 2 * ORTH_SHAPES + 2 * i;
+            if (e == cudaSuccess) e = encode_boxes(&a.maps[boxes], s.hi[side ^ 1], false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, 32, 32);
+            if (e == cudaSuccess) e = encode_boxes(&a.maps[boxes + 1], s.lo, false, s.cols, s.rows, s.count, s.ld, s.rows * s.ld, 32, 32);
+            g.out_map = static_cast<short>(boxes), g.in_map = static_cast<short>(boxes + 1);
+        }
         if (e != cudaSuccess) return e;
         g.a_map = static_cast<short>(2 * i), g.b_map = static_cast<short>(2 * i + 1);
         g.b_mn = !s.tall;
         g.alpha = 1.f / ORTH_UNIT;
-        g.in[0] = s.lo;
-        g.in_ld = s.ld, g.in_batch = s.rows * s.ld;
-        g.out[0] = s.hi[side ^ 1], g.out[1] = s.lo;
         g.out_ld = out_ld ? out_ld[i] : s.ld;
         g.first = s.first;
     }
