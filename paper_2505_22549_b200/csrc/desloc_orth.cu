@@ -271,13 +271,11 @@ struct LastEpilogue {
     }
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
         const float scale = a.epi.scale[&g - a.groups];
-        float sums[2][16];
-        tmem_load16(d, sums[0]);
-        tmem_load16(d + 16, sums[1]);
-        tmem_wait();
-#pragma unroll
+#pragma unroll 1
         for (int half = 0; half < 2; ++half) {
-            float (&v)[16] = sums[half];
+            float v[16];
+            tmem_load16(d + 16 * half, v);
+            tmem_wait();
             if constexpr (TO == ORTH_TO_BF16) {
                 uint32_t w[8];
 #pragma unroll
