@@ -20,7 +20,7 @@ struct UpEpilogue {
     __device__ static bool wants(const GemmGroup &g, int row0, int col0) { return row0 < g.m && col0 < g.n; }
     using Args = GemmArgs<UpEpilogue>;
     __device__ static void fetch(const Args &, const GemmGroup &, int, int, int, int, Ahead &) {}
-    __device__ static void settle(char *, int, const Ahead &) {}
+    __device__ static void settle(const Args &, const GemmGroup &, int, int, int, char *, int, const Ahead &) {}
     __device__ static void drain(const Args &a, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
         for (int half = 0; half < 2; ++half) {
@@ -77,9 +77,12 @@ struct StoreEpilogue {
             else fetch32(static_cast<const float *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, p, lane, x.v);
         }
     }
-    __device__ static void settle(char *st, int lane, const Ahead &x) {
-        if constexpr (ADD && BF16) settle16(st, lane, x.v);
-        else if constexpr (ADD) settle32(st, lane, x.v);
+    __device__ static void settle(const Args &, const GemmGroup &g, int, int row0, int col0, char *st, int lane, const Ahead &x) {
+        if constexpr (ADD) {
+            if constexpr (BF16)
+                settle16(st, lane, static_cast<const __nv_bfloat16 *>(g.out[0]) + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, g.wide & 1), x.v);
+            else settle32(st, lane, x.v);
+        }
     }
     __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
@@ -135,9 +138,11 @@ struct DzEpilogue {
         fetch16(static_cast<const __nv_bfloat16 *>(g.in[0]) + from, g.in_ld, p, lane, x.g);
         fetch16(static_cast<const __nv_bfloat16 *>(g.in[1]) + from, g.in_ld, p, lane, x.u);
     }
-    __device__ static void settle(char *st, int lane, const Ahead &x) {
-        settle16(st, lane, x.g);
-        settle16(st + 2048, lane, x.u);
+    __device__ static void settle(const Args &, const GemmGroup &g, int, int row0, int col0, char *st, int lane, const Ahead &x) {
+        const Piece p = piece_at(g, row0, col0, (g.wide & 2) != 0);
+        const long long from = row0 * g.in_ld + col0;
+        settle16(st, lane, static_cast<const __nv_bfloat16 *>(g.in[0]) + from, g.in_ld, p, x.g);
+        settle16(st + 2048, lane, static_cast<const __nv_bfloat16 *>(g.in[1]) + from, g.in_ld, p, x.u);
     }
     __device__ static void drain(const Args &, const GemmGroup &g, int, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
 #pragma unroll 1
@@ -284,7 +289,8 @@ cudaError_t launch_few(const FfnArgs &a, __nv_bfloat16 *z, cudaStream_t stream, 
 }
 
 // ---- rows that the copy engine does not take ---------------------------------------------------------
-// Copies matrices into rows of a multiple of eight values.  Bound: HBM, two bytes each way; a warp per row, lanes along it.
+// Copies matrices into rows on 16-byte boundaries.  Bound: HBM, two bytes each way.  A warp takes a row, a lane 16 bytes of the copy: they lie in two aligned pieces of 16 bytes, the second of
+// which is the next lane's first one.
 constexpr int PACK_MOST = 64;
 struct PackArgs {
     const unsigned short *from[PACK_MOST];
@@ -298,8 +304,40 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
     const unsigned short *from = a.from[blockIdx.y];
     unsigned short *to = a.to + blockIdx.y * a.to_batch;
     const int lane = threadIdx.x & 31;
-    for (long long r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < a.rows; r += gridDim.x * 8ll)
-        for (int c = lane; c < a.cols; c += 32) to[r * a.to_ld + c] = from[r * a.from_ld + c];
+    for (long long r = blockIdx.x * 8ll + (threadIdx.x >> 5); r < a.rows; r += gridDim.x * 8ll) {
+        const unsigned short *const row = from + r * a.from_ld;
+        const int off = static_cast<int>(reinterpret_cast<uintptr_t>(row) & 15);   // bytes, even
+        const uint4 *const pieces = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(row) - off);
+        const int chunks = a.cols / 8, last = (off + 2 * a.cols) / 16;   // whole ones of the copy; aligned pieces [first, last) lie in the row
+        const int first = off ? 1 : 0;
+#pragma unroll 4
+        for (int c0 = 0; c0 < chunks; c0 += 31) {   // (31 at a time: a lane more for the last one's second piece)
+            const int c = c0 + lane;
+            uint4 v = make_uint4(0, 0, 0, 0);
+            if (c >= first && c < last) v = pieces[c];
+            uint32_t w[8] = {v.x, v.y, v.z, v.w, __shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1), __shfl_down_sync(0xffffffffu, v.z, 1),
+                             __shfl_down_sync(0xffffffffu, v.w, 1)};
+            if (lane == 31 || c >= chunks) continue;
+            if (off == 0 || (c >= first && c + 1 < last)) {
+                if (off & 8) {
+#pragma unroll
+                    for (int e = 0; e < 6; ++e) w[e] = w[e + 2];
+                }
+                if (off & 4) {
+#pragma unroll
+                    for (int e = 0; e < 5; ++e) w[e] = w[e + 1];
+                }
+                if (off & 2) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(w[e], w[e + 1], 16);
+                }
+                *reinterpret_cast<uint4 *>(to + r * a.to_ld + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
+            } else {
+                for (int e = 0; e < 8; ++e) to[r * a.to_ld + 8 * c + e] = row[8 * c + e];
+            }
+        }
+        for (int e = 8 * chunks + lane; e < a.cols; e += 32) to[r * a.to_ld + e] = row[e];
+    }
 }
 
 int64_t padded(int64_t n) { return (n + 7) & ~int64_t{7}; }

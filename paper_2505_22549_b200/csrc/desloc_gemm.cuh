@@ -161,7 +161,7 @@ __device__ __forceinline__ int spot32(int lane, int i) { return (4 * i + (lane >
 __device__ __forceinline__ int place16(int lane, int c) { return lane * 64 + ((c ^ ((lane >> 1) & 3)) << 4); }
 __device__ __forceinline__ int place32(int lane, int c) { return lane * 128 + ((c ^ (lane & 7)) << 4); }
 
-// memory -> registers, as it lies there
+// memory -> registers, as it lies there (16 bits: rows on 16-byte boundaries alone)
 __device__ __forceinline__ void fetch16(const void *from, long long ld, const Piece &p, int lane, uint4 (&v)[4]) {
     const unsigned short *src = static_cast<const unsigned short *>(from) + (lane >> 2) * ld + 8 * (lane & 3);
     if (p.whole()) {
@@ -169,11 +169,12 @@ __device__ __forceinline__ void fetch16(const void *from, long long ld, const Pi
         for (int i = 0; i < 4; ++i) v[i] = *reinterpret_cast<const uint4 *>(src + 8 * i * ld);
         return;
     }
+    const int left = p.cols - 8 * (lane & 3);
+    if (!p.wide || left <= 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int left = p.cols - 8 * (lane & 3);
-        if (8 * i + (lane >> 2) >= p.rows || left <= 0) continue;
-        if (p.wide && left >= 8) {
+        if (8 * i + (lane >> 2) >= p.rows) continue;
+        if (left >= 8) {
             v[i] = *reinterpret_cast<const uint4 *>(src + 8 * i * ld);
         } else {
             uint32_t h[8];
@@ -190,10 +191,11 @@ __device__ __forceinline__ void fetch32(const float *from, long long ld, const P
         for (int i = 0; i < 8; ++i) v[i] = *reinterpret_cast<const uint4 *>(src + 4 * i * ld);
         return;
     }
+    const int left = p.cols - 4 * (lane & 7);
+    if (left <= 0) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int left = p.cols - 4 * (lane & 7);
-        if (4 * i + (lane >> 3) >= p.rows || left <= 0) continue;
+        if (4 * i + (lane >> 3) >= p.rows) continue;
         if (p.wide && left >= 4) {
             v[i] = *reinterpret_cast<const uint4 *>(src + 4 * i * ld);
         } else {
@@ -204,10 +206,16 @@ __device__ __forceinline__ void fetch32(const float *from, long long ld, const P
         }
     }
 }
-// registers -> staging area, whence each lane reads its row (behind a __syncwarp())
-__device__ __forceinline__ void settle16(char *st, int lane, const uint4 (&v)[4]) {
+// registers -> staging area, whence each lane reads its row (behind a __syncwarp()); 16-bit rows on other boundaries come only now, an instruction each.
+__device__ __forceinline__ void settle16(char *st, int lane, const void *from, long long ld, const Piece &p, const uint4 (&v)[4]) {
+    if (p.wide) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(st + spot16(lane, i)) = v[i];
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(st + spot16(lane, i)) = v[i];
+    } else if (lane < p.cols) {
+        const unsigned short *const src = static_cast<const unsigned short *>(from) + lane;
+#pragma unroll 8
+        for (int r = 0; r < p.rows; ++r) *reinterpret_cast<unsigned short *>(st + place16(r, lane >> 3) + (lane & 7) * 2) = src[r * ld];
+    }
 }
 __device__ __forceinline__ void settle32(char *st, int lane, const uint4 (&v)[8]) {
 #pragma unroll
@@ -238,7 +246,7 @@ __device__ __forceinline__ void put32(char *st, int lane, int half, const float 
     for (int c = 0; c < 4; ++c)
         *reinterpret_cast<float4 *>(st + place32(lane, 4 * half + c)) = make_float4(v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
 }
-// staging area -> memory (behind a __syncwarp())
+// staging area -> memory (behind a __syncwarp()); rows on other than 16-byte boundaries one by one, a column per lane
 __device__ __forceinline__ void send16(const char *st, int lane, void *to, long long ld, const Piece &p) {
     unsigned short *dst = static_cast<unsigned short *>(to) + (lane >> 2) * ld + 8 * (lane & 3);
     if (p.whole()) {
@@ -246,12 +254,21 @@ __device__ __forceinline__ void send16(const char *st, int lane, void *to, long 
         for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(dst + 8 * i * ld) = *reinterpret_cast<const uint4 *>(st + spot16(lane, i));
         return;
     }
+    if (!p.wide) {
+        dst = static_cast<unsigned short *>(to) + lane;
+        if (lane < p.cols) {
+#pragma unroll 8
+            for (int r = 0; r < p.rows; ++r) dst[r * ld] = *reinterpret_cast<const unsigned short *>(st + place16(r, lane >> 3) + (lane & 7) * 2);
+        }
+        return;
+    }
+    const int left = p.cols - 8 * (lane & 3);
+    if (left <= 0) return;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int left = p.cols - 8 * (lane & 3);
-        if (8 * i + (lane >> 2) >= p.rows || left <= 0) continue;
+        if (8 * i + (lane >> 2) >= p.rows) continue;
         const uint4 v = *reinterpret_cast<const uint4 *>(st + spot16(lane, i));
-        if (p.wide && left >= 8) {
+        if (left >= 8) {
             *reinterpret_cast<uint4 *>(dst + 8 * i * ld) = v;
         } else {
             const uint32_t h[4] = {v.x, v.y, v.z, v.w};
@@ -268,12 +285,20 @@ __device__ __forceinline__ void send32(const char *st, int lane, float *to, long
         for (int i = 0; i < 8; ++i) *reinterpret_cast<float4 *>(dst + 4 * i * ld) = *reinterpret_cast<const float4 *>(st + spot32(lane, i));
         return;
     }
+    if (!p.wide) {
+        if (lane < p.cols) {
+#pragma unroll 8
+            for (int r = 0; r < p.rows; ++r) to[lane + r * ld] = *reinterpret_cast<const float *>(st + place32(r, lane >> 2) + (lane & 3) * 4);
+        }
+        return;
+    }
+    const int left = p.cols - 4 * (lane & 7);
+    if (left <= 0) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int left = p.cols - 4 * (lane & 7);
-        if (4 * i + (lane >> 3) >= p.rows || left <= 0) continue;
+        if (4 * i + (lane >> 3) >= p.rows) continue;
         const float4 x = *reinterpret_cast<const float4 *>(st + spot32(lane, i));
-        if (p.wide && left >= 4) {
+        if (left >= 4) {
             *reinterpret_cast<float4 *>(dst + 4 * i * ld) = x;
         } else {
             const float h[4] = {x.x, x.y, x.z, x.w};
@@ -344,7 +369,7 @@ struct TileWalk {
 
 // E, the epilogue, takes 32 x 32 pieces, those that E::wants(group, row, column) says.  What it reads comes one piece ahead: E::READS_BOXES, as a box by the copy engine, pieces in turn
 // into the first and second 2 KB of the warp's staging area (of E::STAGING bytes); else as E::Ahead by E::fetch(args, group, batch, row, column, lane, ahead), which
-// E::settle(staging, lane, ahead) puts there.  E::drain(args, group, batch, row, column, accumulator, staging, input, lane) takes it and the sums, and leaves what is
+// E::settle(args, group, batch, row, column, staging, lane, ahead) puts there.  E::drain(args, group, batch, row, column, accumulator, staging, input, lane) takes it and the sums, and leaves what is
 // written: by E::send(args, group, batch, row, column, staging, lane), or (E::WRITES_BOXES, where the group has maps for it) by E::send_boxes(args, group, batch, row, column, staging, input),
 // which one lane calls.  What moves so costs a warp no time: reading, staging and writing 16 bytes a lane were two thirds of what emptying a piece took.
 template <typename E, int CG>
@@ -537,7 +562,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 if (elect_one()) stores_read();
             }
             __syncwarp();
-            if constexpr (!E::READS_BOXES) E::settle(st, lane, ahead);
+            if constexpr (!E::READS_BOXES) if (wanted) E::settle(a, here, batch, row0, col0, st, lane, ahead);
             c += STEP;
             const bool last = c >= out_n;
             if (last) {

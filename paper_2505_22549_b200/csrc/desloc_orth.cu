@@ -82,22 +82,55 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-// Squares of a block's rows, up to four in fp32 (values below 1e-22 count as 0, beyond 1e19 as infinite), then in fp64.  Bound: HBM, each element read once.
+// Squares of a block's share of a matrix, whose elements follow one another: up to four in fp32 (values below 1e-22 count as 0, beyond 1e19 as infinite), then in fp64.
+// Bound: HBM, each element read once, eight vectors of four on their way per thread.
 template <typename UT, typename GT>
 __global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
     wait_for_earlier_kernels();
-    const auto &sh = s.shapes[s.shape[blockIdx.y]];
-    if (static_cast<int>(blockIdx.x) * sh.block_rows >= sh.rows) return;
+    const int which = blockIdx.y;
+    const auto &sh = s.shapes[s.shape[which]];
+    const long long first = static_cast<long long>(blockIdx.x) * sh.block_rows * sh.cols;
+    const int count = static_cast<int>(min(static_cast<long long>(sh.block_rows) * sh.cols, static_cast<long long>(sh.rows) * sh.cols - first));
+    if (count <= 0) return;
+    const UT *const u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]) + first;
+    const GT *const g = s.grad[which] ? static_cast<const GT *>(s.grad[which]) + first : nullptr;
+    const float beta = s.beta, rest = 1.f - s.beta;
     double sum = 0;
-    visit_rows<UT, GT>(s, blockIdx.y, [&](int, int, const auto &v) {
-        float part = 0;
+    const auto go = [&](auto width) {
+        constexpr int N = decltype(width)::value, AHEAD = 8;
+        for (int at = threadIdx.x * N; at < count; at += ORTH_THREADS * N * AHEAD) {
+            float v[AHEAD][N];
 #pragma unroll
-        for (float x : v) part += x * x;
-        sum += part;
-    });
+            for (int e = 0; e < AHEAD; ++e) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[e][k] = 0.f;
+                if (at + e * ORTH_THREADS * N < count) load_values(u + at + e * ORTH_THREADS * N, v[e]);
+            }
+            if (g) {
+#pragma unroll
+                for (int e = 0; e < AHEAD; ++e) {
+                    if (at + e * ORTH_THREADS * N >= count) continue;
+                    float w[N];
+                    load_values(g + at + e * ORTH_THREADS * N, w);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[e][k] = beta * v[e][k] + rest * w[k];
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                float part = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k) part += v[e][k] * v[e][k];
+                sum += part;
+            }
+        }
+    };
+    const uintptr_t low = (reinterpret_cast<uintptr_t>(u) & (4 * sizeof(UT) - 1)) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(GT) - 1));
+    if (count % 4 == 0 && low == 0) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
     sum = block_sum(sum);
-    if (threadIdx.x == 0) s.partial[static_cast<long long>(blockIdx.y) * s.most + blockIdx.x] = sum;
+    if (threadIdx.x == 0) s.partial[static_cast<long long>(which) * s.most + blockIdx.x] = sum;
 }
 
 // X in two halves.  Bound: L2 or HBM, each element read again and four bytes written.
@@ -148,7 +181,9 @@ struct SymEpilogue {
         if (g.in[0])
             fetch16(static_cast<const __half *>(g.in[0]) + batch * g.out_batch + row0 * g.out_ld + col0, g.out_ld, piece_at(g, row0, col0, true), lane, x.v);
     }
-    __device__ static void settle(char *st, int lane, const Ahead &x) { settle16(st, lane, x.v); }
+    __device__ static void settle(const Args &, const GemmGroup &g, int, int row0, int col0, char *st, int lane, const Ahead &x) {
+        settle16(st, lane, nullptr, 0, piece_at(g, row0, col0, true), x.v);
+    }
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
         const Piece p = piece_at(g, row0, col0, true);
         __half *const out = static_cast<__half *>(g.out[0]) + batch * g.out_batch;
@@ -266,7 +301,7 @@ struct LastEpilogue {
             fetch32(out + row0 * g.out_ld + col0, g.out_ld, piece(g, out, row0, col0), lane, x.x);
         }
     }
-    __device__ static void settle(char *st, int lane, const Ahead &x) {
+    __device__ static void settle(const Args &, const GemmGroup &, int, int, int, char *st, int lane, const Ahead &x) {
         if constexpr (TO == ORTH_TO_X) settle32(st, lane, x.x);
     }
     __device__ static void drain(const Args &a, const GemmGroup &g, int batch, int row0, int col0, uint32_t d, char *st, const char *, int lane) {
