@@ -33,6 +33,7 @@ struct OrthMatrix {
     int rows, cols, index;
     const void *update, *grad;   // update: null where the tables say
     void *out;                   // null: a step of x
+    float scale;                 // of the result, with the learning rate; filled in by launch_orth()
 };
 struct OrthArgs {
     OrthMatrix *list;            // sorted in place
@@ -44,9 +45,9 @@ struct OrthArgs {
     int scale;                   // desloc_scale_t
     float lr, decay;             // of the step: x := decay * x - lr * scale * result
 };
-// Whether a matrix is taken by a block of its own, and the launch of such ones: list[first, first + count), each times scales[i].
+// Whether a matrix is taken by a block of its own, and the launch of such ones: list[first, first + count).
 bool orth_is_small(int rows, int cols);
-cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, const float *scales, int *err, int wait_limit, cudaStream_t stream, int *launches);
+cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, int *err, int wait_limit, cudaStream_t stream, int *launches);
 int64_t orth_work(const OrthArgs &a);
 cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches);
 

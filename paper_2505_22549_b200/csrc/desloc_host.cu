@@ -730,7 +730,7 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
         if (cols < 1 || cols > (1 << 20) || ctx->numel[k] % cols || ctx->numel[k] / cols > (1 << 20)) return DESLOC_E_RANGE;
         for (int m = 0; m < c.M; ++m) {
             const int64_t at = static_cast<int64_t>(m) * c.num_tensors + k;
-            desloc::OrthMatrix x{static_cast<int>(ctx->numel[k] / cols), static_cast<int>(cols), static_cast<int>(at), nullptr, nullptr, nullptr};
+            desloc::OrthMatrix x{static_cast<int>(ctx->numel[k] / cols), static_cast<int>(cols), static_cast<int>(at), nullptr, nullptr, nullptr, 1.f};
             if (addresses && how.updates) {
                 if (!(x.update = how.updates[at])) return DESLOC_E_NULL;
                 if (reinterpret_cast<uintptr_t>(x.update) % usz) return DESLOC_E_INVALID;

@@ -3,7 +3,6 @@
 #include "desloc_gemm.cuh"
 
 #include <algorithm>
-#include <vector>
 
 namespace desloc {
 
@@ -514,7 +513,7 @@ cudaError_t last(const OrthArgs &a, const Round &r, int side, const Run &run) {
     long long ld[ORTH_SHAPES];
     for (int i = 0; i < r.nshapes; ++i) {
         const Shape &s = r.shapes[i];
-        epi.scale[i] = static_cast<float>(scale_of(a, s.rows, s.cols) / (ORTH_UNIT * ORTH_UNIT));
+        epi.scale[i] = a.list[r.first + s.first].scale / (ORTH_UNIT * ORTH_UNIT);
         ld[i] = s.cols;
     }
     for (int i = 0; i < r.count; ++i) epi.out[i] = a.list[r.first + i].out, epi.index[i] = a.list[r.first + i].index;
@@ -545,10 +544,9 @@ int64_t orth_work(const OrthArgs &a) {
 cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit, cudaStream_t stream, int *launches) {
     const Run run{stream, err, wait_limit, launches};
     const int small = sort_list(a);
+    for (int i = 0; i < a.count; ++i) a.list[i].scale = static_cast<float>(scale_of(a, a.list[i].rows, a.list[i].cols));
     if (small > 0) {
-        std::vector<float> scales;
-        for (int i = 0; i < small; ++i) scales.push_back(static_cast<float>(scale_of(a, a.list[i].rows, a.list[i].cols)));
-        const cudaError_t e = launch_orth_small(a, 0, small, scales.data(), err, wait_limit, stream, launches);
+        const cudaError_t e = launch_orth_small(a, 0, small, err, wait_limit, stream, launches);
         if (e != cudaSuccess) return e;
     }
     static thread_local Sources s;

@@ -275,7 +275,7 @@ bool orth_is_small(int rows, int cols) {
     return n <= 128 && m <= 4096 && SmallPlan(rows, cols).bytes() + 1024 <= SMALL_BYTES;
 }
 
-cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, const float *scales, int *err, int wait_limit, cudaStream_t stream, int *launches) {
+cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, int *err, int wait_limit, cudaStream_t stream, int *launches) {
     static thread_local SmallArgs s;
     static std::atomic<uint64_t> ready{0};
     int device = 0;
@@ -289,7 +289,7 @@ cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, const flo
         int bytes = 0;
         for (int i = 0; i < some; ++i) {
             const OrthMatrix &m = a.list[at + i];
-            s.update[i] = m.update, s.grad[i] = m.grad, s.out[i] = m.out, s.index[i] = m.index, s.rows[i] = m.rows, s.cols[i] = m.cols, s.scale[i] = scales[at + i - first];
+            s.update[i] = m.update, s.grad[i] = m.grad, s.out[i] = m.out, s.index[i] = m.index, s.rows[i] = m.rows, s.cols[i] = m.cols, s.scale[i] = m.scale;
             bytes = std::max(bytes, SmallPlan(m.rows, m.cols).bytes());
         }
         std::memcpy(s.coefficients, a.coefficients, sizeof(float) * 3 * a.steps);
