@@ -413,6 +413,7 @@ class DesLoc:
         """The gated feed-forward block down(silu(gate h) * (up h)) of every worker with its own weights, on torch's current stream.  tensors: numbers of gate,
         up ([hidden, width]) and down ([width, hidden]); h: bf16 [M, ..., width]; weights: nested lists like x of bf16 copies, of which only those three are looked at.
         Returns y like h, or with keep (y, (gate h, up h)) for gated_ffn_grad()."""
+        tensors = tuple(tensors)
         if out is None:     # the usual layouts, natively
             r = _native.gated_ffn(self.ctx, self._table, tensors, h, weights, keep, self._index)
             if r is not None:
@@ -430,6 +431,7 @@ class DesLoc:
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """The way back of gated_ffn(): returns dh (into `out` where it is given) and writes the three weights' gradients into the workers' gradients in `grads` (what
         step() reads, or bind_grads()' handle); accumulate: added to what they hold.  kept: what gated_ffn(keep=True) returned beside y."""
+        tensors = tuple(tensors)
         if out is None and len(kept) == 2:
             r = _native.gated_ffn_grad(self.ctx, self._table, tensors, h, kept[0], kept[1], dy, weights, grads, self.grad_dtype, accumulate, self._index)
             if r is not None:
@@ -437,6 +439,8 @@ class DesLoc:
         f, h, hidden = self._ffn(tensors, h, weights)
         tensors = (f.gate, f.up, f.down)
         shape = tuple(h.shape[:-1]) + (hidden,)
+        if len(kept) != 2:
+            raise ValueError("kept is the pair that gated_ffn(keep=True) returned for this h")
         for t in kept:
             if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
                 raise ValueError("kept is the pair that gated_ffn(keep=True) returned for this h")
@@ -473,6 +477,7 @@ class DesLoc:
         Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad.  columns: of each matrix,
         where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones.  scale: "none", "aspect"
         (sqrt(max(1, rows / columns))) or "rms" (0.2 sqrt(max(rows, columns)))."""
+        tensors = tuple(tensors)
         if updates is None:
             updates = self._keep[1]
         if columns is None and coefficients is None and scale in _SCALES:     # the usual call, natively
@@ -495,6 +500,7 @@ class DesLoc:
                         scale: str = "aspect") -> None:
         """x of the matrices `tensors` := x (1 - lr weight_decay) - lr * orthogonalize(updates; the momentum u where None).  Behind step(t, 0.0, grads) of an SGDM
         context, which brings the momentum and the averages of this step, it is the step of the orthogonalised momentum; grads: its look-ahead."""
+        tensors = tuple(tensors)
         if columns is None and coefficients is None and scale in _SCALES:
             r = _native.orthogonal(self.ctx, self._table, tensors, self._widths(), updates, grads, None, lr, steps, eps, _SCALES[scale], self.grad_dtype, self._keep[0],
                                    self._index)

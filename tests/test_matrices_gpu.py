@@ -97,7 +97,8 @@ class Block:
 
 
 SIZES = [(1, 1, 1, 1), (2, 1, 8, 16), (1, 3, 5, 7), (4, 37, 72, 200), (2, 129, 71, 203), (3, 300, 576, 1536), (2, 128, 64, 64), (1, 257, 130, 66),
-         (17, 5, 24, 40), (3, 2, 201, 77), (2, 3, 2048, 1000), (5, 4, 576, 1536), (2, 60, 136, 264), (2, 1000, 200, 520), (1, 2048, 512, 1024), (4, 1, 512, 2048)]
+         (17, 5, 24, 40), (3, 2, 201, 77), (2, 3, 2048, 1000), (5, 4, 576, 1536), (2, 60, 136, 264), (2, 1000, 200, 520), (1, 2048, 512, 1024), (4, 1, 512, 2048), (200, 1, 8, 16),
+         (40, 6, 16, 24), (2, 257, 1030, 300)]
 
 
 @pytest.mark.parametrize("M,T,D,F", SIZES)
