@@ -393,6 +393,18 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         bar_init(&drained, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 0 && elect_one() && tile0 < a.tiles) {   // the descriptions of the first boxes come while earlier kernels end
+        TileWalk at;
+        const GemmGroup &g = at.find<CG>(a, tile0);
+        const auto soon = [&](int map) {
+            if (map >= 0) asm volatile("prefetch.tensormap [%0];" :: "l"(&a.maps[map]) : "memory");
+        };
+        soon(g.a_map), soon(g.b_map);
+        if (a.dual || a.segments > 1) soon(g.b_map + 1);
+        if (E::READS_BOXES) soon(g.in_map);
+        if (E::WRITES_BOXES) soon(g.out_map);
+    }
+    __syncwarp();
     if (E::READS_BOXES && warp == 3) {
         bar_init(&arrived[lane], 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");

@@ -17,7 +17,7 @@ namespace {
 // next.  Off by 0.15 % for normal matrices, 0.03 % for few directions.
 // Everything is held times ORTH_UNIT: singular values stay below two, entries far below one.
 constexpr float ORTH_UNIT = 256.f, ORTH_LO = 2048.f;
-constexpr int ORTH_ROUND = 256, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
+constexpr int ORTH_ROUND = 512, ORTH_SHAPES = 16;   // matrices and shapes of one round of launches
 constexpr int ORTH_THREADS = 256, ORTH_WARPS = ORTH_THREADS / 32;
 
 struct Sources {
