@@ -3,6 +3,7 @@
 #include "desloc_gemm.cuh"
 
 #include <cstring>
+#include <type_traits>
 
 namespace desloc {
 
@@ -42,10 +43,6 @@ struct SmallPlan {
 
 __device__ __forceinline__ int place(const SmallPlan &p, int row, int col) {
     return (col >> 6) * p.half() + row * 128 + ((((col >> 3) & 7) ^ (row & 7)) << 4) + (col & 7) * 2;
-}
-
-__device__ __forceinline__ float value_at(const void *p, long long i, bool bf16) {
-    return bf16 ? __bfloat162float(static_cast<const __nv_bfloat16 *>(p)[i]) : static_cast<const float *>(p)[i];
 }
 
 // Sixteen values of a row as hi and lo; col is a multiple of 16.
@@ -107,58 +104,93 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     const uint32_t tmem = tmem_at;
     wait_for_earlier_kernels();
 
-    // The norm (squares eight at a time in fp32, then in fp64), and X.
+    // The norm (squares up to four at a time in fp32, then in fp64), and X.
     const void *const u = a.update[which] ? a.update[which] : a.u_table[a.index[which]];
     const void *const gr = a.grad[which];
     const int cols = a.cols[which], count = a.rows[which] * cols;
     const bool tall = a.rows[which] > cols;
     const float beta = a.beta, rest = 1.f - a.beta;
-    // eight elements a thread, all of them on their way at once
+    // Eight times N neighbouring elements a thread, all of them on their way at once; N = 4 where rows allow it.
     constexpr int AHEAD = 8;
-    const auto fetch = [&](int i0, float (&v)[AHEAD]) {
-#pragma unroll
-        for (int e = 0; e < AHEAD; ++e) {
-            const int i = i0 + e * SMALL_THREADS;
-            v[e] = i < count ? value_at(u, i, a.update_bf16) : 0.f;
-        }
-        if (gr) {
+    const auto go = [&](auto width) {
+        constexpr int N = decltype(width)::value;
+        float v[AHEAD][N];
+        const auto fetch = [&](int i0) {
 #pragma unroll
             for (int e = 0; e < AHEAD; ++e) {
-                const int i = i0 + e * SMALL_THREADS;
-                v[e] = beta * v[e] + rest * (i < count ? value_at(gr, i, a.grad_bf16) : 0.f);
+                const int i = i0 + e * SMALL_THREADS * N;
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[e][k] = 0.f;
+                if (i < count) {
+                    if (a.update_bf16) load_values(static_cast<const __nv_bfloat16 *>(u) + i, v[e]);
+                    else load_values(static_cast<const float *>(u) + i, v[e]);
+                }
+            }
+            if (!gr) return;
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int i = i0 + e * SMALL_THREADS * N;
+                float w[N] = {};
+                if (i < count) {
+                    if (a.grad_bf16) load_values(static_cast<const __nv_bfloat16 *>(gr) + i, w);
+                    else load_values(static_cast<const float *>(gr) + i, w);
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) v[e][k] = beta * v[e][k] + rest * w[k];
+            }
+        };
+        constexpr int EACH = AHEAD * SMALL_THREADS * N;
+        double sum = 0;
+        for (int i0 = tid * N; i0 < count; i0 += EACH) {
+            fetch(i0);
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                float part = 0;
+#pragma unroll
+                for (int k = 0; k < N; ++k) part += v[e][k] * v[e][k];
+                sum += part;
+            }
+        }
+#pragma unroll
+        for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lane == 0) sums[warp] = sum;
+        __syncthreads();
+        sum = 0;
+#pragma unroll
+        for (int w = 0; w < SMALL_THREADS / 32; ++w) sum += sums[w];
+        const float factor = static_cast<float>(static_cast<double>(SMALL_UNIT) / (sqrt(sum) + static_cast<double>(a.eps)));
+        const int x_lo = p.x_bytes();
+        for (int i0 = tid * N; i0 < count; i0 += EACH) {
+            if (count > EACH) fetch(i0);   // (else they are still here)
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                const int i = i0 + e * SMALL_THREADS * N, r = i / cols, c = i - r * cols;
+                if (i >= count) break;
+                __half h[N], l[N];
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    const float y = v[e][k] * factor;
+                    h[k] = __float2half_rn(y);
+                    l[k] = __float2half_rn(y - __half2float(h[k]));
+                }
+                if (N == 4 && !tall) {
+                    char *const to = x + place(p, r, c);
+                    *reinterpret_cast<uint2 *>(to) = *reinterpret_cast<const uint2 *>(h);
+                    *reinterpret_cast<uint2 *>(to + x_lo) = *reinterpret_cast<const uint2 *>(l);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < N; ++k) {
+                        char *const to = x + (tall ? place(p, c + k, r) : place(p, r, c + k));
+                        *reinterpret_cast<__half *>(to) = h[k];
+                        *reinterpret_cast<__half *>(to + x_lo) = l[k];
+                    }
+                }
             }
         }
     };
-    double sum = 0;
-    for (int i0 = tid; i0 < count; i0 += AHEAD * SMALL_THREADS) {
-        float v[AHEAD], part = 0;
-        fetch(i0, v);
-#pragma unroll
-        for (int e = 0; e < AHEAD; ++e) part += v[e] * v[e];
-        sum += part;
-    }
-#pragma unroll
-    for (int d = 16; d; d /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    if (lane == 0) sums[warp] = sum;
-    __syncthreads();
-    sum = 0;
-#pragma unroll
-    for (int w = 0; w < SMALL_THREADS / 32; ++w) sum += sums[w];
-    const float factor = static_cast<float>(static_cast<double>(SMALL_UNIT) / (sqrt(sum) + static_cast<double>(a.eps)));
-    for (int i0 = tid; i0 < count; i0 += AHEAD * SMALL_THREADS) {
-        float v[AHEAD];
-        fetch(i0, v);
-#pragma unroll
-        for (int e = 0; e < AHEAD; ++e) {
-            const int i = i0 + e * SMALL_THREADS, r = i / cols, c = i - r * cols;
-            if (i >= count) break;
-            v[e] *= factor;
-            char *const to = x + (tall ? place(p, c, r) : place(p, r, c));
-            const __half h = __float2half_rn(v[e]);
-            *reinterpret_cast<__half *>(to) = h;
-            *reinterpret_cast<__half *>(to + p.x_bytes()) = __float2half_rn(v[e] - __half2float(h));
-        }
-    }
+    const uintptr_t low = (reinterpret_cast<uintptr_t>(u) & (a.update_bf16 ? 7u : 15u)) | (reinterpret_cast<uintptr_t>(gr) & (a.grad_bf16 ? 7u : 15u));
+    if (cols % 4 == 0 && low == 0) go(std::integral_constant<int, 4>());
+    else go(std::integral_constant<int, 1>());
 
     const uint32_t at_x = smem_u32(x), at_g = smem_u32(g);
     const uint32_t idesc = 1u << 4 | static_cast<uint32_t>(GEMM_BM >> 4) << 24;
