@@ -503,7 +503,7 @@ DESLOC_API int64_t desloc_gated_ffn_grad_bytes(const desloc_ctx *ctx, const desl
  *   X := a X + (b G + c G^2) X,  G = X X^T,
  * by which singular values of 1e-3 and more come near 1 (with the default triples, within 0.7 .. 1.2) and the singular vectors stay.  Products take fp16 operands with sums
  * in fp32, X itself is carried in 22 bits from step to step; the result is off by some 2e-3 of its norm.  A matrix of zeros stays one; one that holds
- * values that are not finite has results that are not, and no other matrix does.  Squares are fp32: values below 1e-22 count as 0 in the norm, beyond 1e19 as infinite.
+ * values that are not finite has results that are not, and no other matrix does.  Squares are fp32: values below 1e-22 count as 0 in the norm, beyond 1e18 as infinite.
  */
 typedef enum {
     DESLOC_SCALE_NONE = 0,

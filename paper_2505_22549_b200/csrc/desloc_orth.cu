@@ -36,36 +36,79 @@ struct Sources {
     float beta, eps;
 };
 
-// The elements that a block of a matrix takes, as fp32: f(row, column, values) for N columns at a time, N = 4 where all rows begin on boundaries of 4 elements.
-template <typename UT, typename GT, typename F>
-__device__ __forceinline__ void visit_rows(const Sources &s, int which, const F &f) {
-    const auto &sh = s.shapes[s.shape[which]];
-    const int row0 = blockIdx.x * sh.block_rows, row1 = min(row0 + sh.block_rows, sh.rows);
-    const UT *u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]);
-    const GT *g = static_cast<const GT *>(s.grad[which]);
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, cols = sh.cols;
-    const float beta = s.beta, rest = 1.f - s.beta;
-    const auto go = [&](auto width) {
-        constexpr int N = decltype(width)::value;
-        for (int r = row0 + warp; r < row1; r += ORTH_WARPS) {
-            const long long at = static_cast<long long>(r) * cols;
-#pragma unroll 4
-            for (int c = lane * N; c < cols; c += 32 * N) {
-                float v[N];
-                load_values(u + at + c, v);
-                if (g) {
-                    float w[N];
-                    load_values(g + at + c, w);
+// N values as they lie in memory: they wait in as few registers as they can, since how many are on their way is what the bandwidth comes from.
+template <typename T, int N>
+struct Raw {
+    uint4 q[N * sizeof(T) / 16];
+    __device__ __forceinline__ void load(const T *p) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e) v[e] = beta * v[e] + rest * w[e];
+        for (int i = 0; i < static_cast<int>(N * sizeof(T) / 16); ++i) q[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void values(float (&f)[N]) const {
+#pragma unroll
+        for (int i = 0; i < static_cast<int>(N * sizeof(T) / 16); ++i) {
+            const uint32_t w[4] = {q[i].x, q[i].y, q[i].z, q[i].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if constexpr (sizeof(T) == 4) {
+                    f[4 * i + e] = __uint_as_float(w[e]);
+                } else {
+                    const float2 two = unpack_bf16(w[e]);
+                    f[8 * i + 2 * e] = two.x, f[8 * i + 2 * e + 1] = two.y;
                 }
-                f(r, c, v);
+            }
+        }
+    }
+};
+template <typename T>
+struct Raw<T, 1> {
+    T v;
+    __device__ __forceinline__ void load(const T *p) { v = *p; }
+    __device__ __forceinline__ void values(float (&f)[1]) const { f[0] = static_cast<float>(v); }
+};
+
+// The elements that a block of a matrix takes (they follow one another), as fp32: f(first one's number within the block, values) for N of them at a time, AHEAD times as
+// many on their way per thread; N = 8 where rows and addresses allow it.
+template <typename UT, typename GT, typename F>
+__device__ __forceinline__ void visit(const Sources &s, int which, long long first, int count, const F &f) {
+    const UT *const u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]) + first;
+    const GT *const g = s.grad[which] ? static_cast<const GT *>(s.grad[which]) + first : nullptr;
+    const float beta = s.beta, rest = 1.f - s.beta;
+    const auto go = [&](auto width, auto ahead) {
+        constexpr int N = decltype(width)::value, STEP = ORTH_THREADS * N;
+        constexpr bool WITH = decltype(ahead)::value;   // with gradients
+        constexpr int AHEAD = N == 1 ? 8 : sizeof(UT) == 2 && !WITH ? 4 : 2;
+        for (int at = threadIdx.x * N; at < count; at += STEP * AHEAD) {
+            Raw<UT, N> x[AHEAD];
+            Raw<GT, N> y[WITH ? AHEAD : 1];
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e)
+                if (at + e * STEP < count) x[e].load(u + at + e * STEP);
+            if constexpr (WITH) {
+#pragma unroll
+                for (int e = 0; e < AHEAD; ++e)
+                    if (at + e * STEP < count) y[e].load(g + at + e * STEP);
+            }
+#pragma unroll
+            for (int e = 0; e < AHEAD; ++e) {
+                if (at + e * STEP >= count) break;
+                float v[N];
+                x[e].values(v);
+                if constexpr (WITH) {
+                    float w[N];
+                    y[e].values(w);
+#pragma unroll
+                    for (int k = 0; k < N; ++k) v[k] = beta * v[k] + rest * w[k];
+                }
+                f(at + e * STEP, v);
             }
         }
     };
-    const uintptr_t low = (reinterpret_cast<uintptr_t>(u) & (4 * sizeof(UT) - 1)) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(GT) - 1));
-    if (cols % 4 == 0 && low == 0) go(std::integral_constant<int, 4>());
-    else go(std::integral_constant<int, 1>());
+    const bool wide = s.shapes[s.shape[which]].cols % 8 == 0 && ((reinterpret_cast<uintptr_t>(u) | reinterpret_cast<uintptr_t>(g)) & 15) == 0;
+    using Wide = std::integral_constant<int, 8>;
+    using One = std::integral_constant<int, 1>;
+    if (g) wide ? go(Wide(), std::true_type()) : go(One(), std::true_type());
+    else wide ? go(Wide(), std::false_type()) : go(One(), std::false_type());
 }
 
 __device__ __forceinline__ double block_sum(double v) {
@@ -81,10 +124,9 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-// Squares of a block's share of a matrix, whose elements follow one another: up to four in fp32 (values below 1e-22 count as 0, beyond 1e19 as infinite), then in fp64.
-// Bound: HBM, each element read once, eight vectors of four on their way per thread.
+// Squares, eight at a time in fp32 (values below 1e-22 count as 0, beyond 1e18 as infinite), then in fp64.  Bound: HBM, each element read once.
 template <typename UT, typename GT>
-__global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_constant__ Sources s) {
+__global__ void __launch_bounds__(ORTH_THREADS, 4) orth_norm_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
     wait_for_earlier_kernels();
     const int which = blockIdx.y;
@@ -92,75 +134,52 @@ __global__ void __launch_bounds__(ORTH_THREADS) orth_norm_kernel(const __grid_co
     const long long first = static_cast<long long>(blockIdx.x) * sh.block_rows * sh.cols;
     const int count = static_cast<int>(min(static_cast<long long>(sh.block_rows) * sh.cols, static_cast<long long>(sh.rows) * sh.cols - first));
     if (count <= 0) return;
-    const UT *const u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]) + first;
-    const GT *const g = s.grad[which] ? static_cast<const GT *>(s.grad[which]) + first : nullptr;
-    const float beta = s.beta, rest = 1.f - s.beta;
     double sum = 0;
-    const auto go = [&](auto width) {
-        constexpr int N = decltype(width)::value, AHEAD = 8;
-        for (int at = threadIdx.x * N; at < count; at += ORTH_THREADS * N * AHEAD) {
-            float v[AHEAD][N];
+    visit<UT, GT>(s, which, first, count, [&](int, const auto &v) {
+        float part = 0;
 #pragma unroll
-            for (int e = 0; e < AHEAD; ++e) {
-#pragma unroll
-                for (int k = 0; k < N; ++k) v[e][k] = 0.f;
-                if (at + e * ORTH_THREADS * N < count) load_values(u + at + e * ORTH_THREADS * N, v[e]);
-            }
-            if (g) {
-#pragma unroll
-                for (int e = 0; e < AHEAD; ++e) {
-                    if (at + e * ORTH_THREADS * N >= count) continue;
-                    float w[N];
-                    load_values(g + at + e * ORTH_THREADS * N, w);
-#pragma unroll
-                    for (int k = 0; k < N; ++k) v[e][k] = beta * v[e][k] + rest * w[k];
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < AHEAD; ++e) {
-                float part = 0;
-#pragma unroll
-                for (int k = 0; k < N; ++k) part += v[e][k] * v[e][k];
-                sum += part;
-            }
-        }
-    };
-    const uintptr_t low = (reinterpret_cast<uintptr_t>(u) & (4 * sizeof(UT) - 1)) | (reinterpret_cast<uintptr_t>(g) & (4 * sizeof(GT) - 1));
-    if (count % 4 == 0 && low == 0) go(std::integral_constant<int, 4>());
-    else go(std::integral_constant<int, 1>());
+        for (float x : v) part += x * x;
+        sum += part;
+    });
     sum = block_sum(sum);
     if (threadIdx.x == 0) s.partial[static_cast<long long>(which) * s.most + blockIdx.x] = sum;
 }
 
 // X in two halves.  Bound: L2 or HBM, each element read again and four bytes written.
 template <typename UT, typename GT>
-__global__ void __launch_bounds__(ORTH_THREADS) orth_scale_kernel(const __grid_constant__ Sources s) {
+__global__ void __launch_bounds__(ORTH_THREADS, 4) orth_scale_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
     wait_for_earlier_kernels();
     const int which = blockIdx.y;
     const auto &sh = s.shapes[s.shape[which]];
-    if (static_cast<int>(blockIdx.x) * sh.block_rows >= sh.rows) return;
-    const int parts = (sh.rows + sh.block_rows - 1) / sh.block_rows;
+    const int row0 = static_cast<int>(blockIdx.x) * sh.block_rows;
+    if (row0 >= sh.rows) return;
+    const int parts = (sh.rows + sh.block_rows - 1) / sh.block_rows, cols = sh.cols, ld = sh.ld;
     double sum = 0;
     for (int i = threadIdx.x; i < parts; i += ORTH_THREADS) sum += s.partial[static_cast<long long>(which) * s.most + i];
     const float factor = static_cast<float>(static_cast<double>(ORTH_UNIT) / (sqrt(block_sum(sum)) + static_cast<double>(s.eps)));
-    const long long first = static_cast<long long>(s.number[which]) * sh.rows * sh.ld;
-    __half *const hi = sh.hi + first, *const lo = sh.lo + first;
-    visit_rows<UT, GT>(s, which, [&](int r, int c, const auto &v) {
+    const long long to = (static_cast<long long>(s.number[which]) * sh.rows + row0) * ld;
+    __half *const hi = sh.hi + to, *const lo = sh.lo + to;
+    visit<UT, GT>(s, which, static_cast<long long>(row0) * cols, min(sh.block_rows, sh.rows - row0) * cols, [&](int i, const auto &v) {
         constexpr int N = sizeof(v) / sizeof(float);
-        const long long at = static_cast<long long>(r) * sh.ld + c;
-        __half h[N], l[N];
+        const int r = i / cols;
+        const long long at = static_cast<long long>(r) * (ld - cols) + i;
+        if constexpr (N == 8) {
+            uint32_t h[4], l[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float x = v[e] * factor;
-            h[e] = __float2half_rn(x);
-            l[e] = __float2half_rn((x - __half2float(h[e])) * ORTH_LO);
-        }
-        if constexpr (N == 4) {
-            *reinterpret_cast<uint2 *>(hi + at) = *reinterpret_cast<const uint2 *>(h);
-            *reinterpret_cast<uint2 *>(lo + at) = *reinterpret_cast<const uint2 *>(l);
+            for (int e = 0; e < 4; ++e) {
+                const float a = v[2 * e] * factor, b = v[2 * e + 1] * factor;
+                h[e] = pack_f16(a, b);
+                const float2 x = unpack_f16(h[e]);
+                l[e] = pack_f16((a - x.x) * ORTH_LO, (b - x.y) * ORTH_LO);
+            }
+            *reinterpret_cast<uint4 *>(hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+            *reinterpret_cast<uint4 *>(lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
         } else {
-            hi[at] = h[0], lo[at] = l[0];
+            const float x = v[0] * factor;
+            const __half h = __float2half_rn(x);
+            hi[at] = h;
+            lo[at] = __float2half_rn((x - __half2float(h)) * ORTH_LO);
         }
     });
 }
