@@ -289,8 +289,8 @@ cudaError_t launch_few(const FfnArgs &a, __nv_bfloat16 *z, cudaStream_t stream, 
 }
 
 // ---- rows that the copy engine does not take ---------------------------------------------------------
-// Copies matrices into rows on 16-byte boundaries.  Bound: HBM, two bytes each way.  A warp takes a row, a lane 16 bytes of the copy: they lie in two aligned pieces of 16 bytes, the second of
-// which is the next lane's first one.
+// Copies matrices into rows on 16-byte boundaries.  Bound: HBM, two bytes each way.  A warp takes a row, a lane 16 bytes of the copy, which lie in two aligned
+// pieces of 16 bytes.
 constexpr int PACK_MOST = 64;
 struct PackArgs {
     const unsigned short *from[PACK_MOST];
@@ -310,15 +310,26 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
         const uint4 *const pieces = reinterpret_cast<const uint4 *>(reinterpret_cast<uintptr_t>(row) - off);
         const int chunks = a.cols / 8, last = (off + 2 * a.cols) / 16;   // whole ones of the copy; aligned pieces [first, last) lie in the row
         const int first = off ? 1 : 0;
-#pragma unroll 4
-        for (int c0 = 0; c0 < chunks; c0 += 31) {   // (31 at a time: a lane more for the last one's second piece)
-            const int c = c0 + lane;
-            uint4 v = make_uint4(0, 0, 0, 0);
-            if (c >= first && c < last) v = pieces[c];
-            uint32_t w[8] = {v.x, v.y, v.z, v.w, __shfl_down_sync(0xffffffffu, v.x, 1), __shfl_down_sync(0xffffffffu, v.y, 1), __shfl_down_sync(0xffffffffu, v.z, 1),
-                             __shfl_down_sync(0xffffffffu, v.w, 1)};
-            if (lane == 31 || c >= chunks) continue;
-            if (off == 0 || (c >= first && c + 1 < last)) {
+        constexpr int AHEAD = 4;
+        for (int c0 = lane; c0 < chunks; c0 += 32 * AHEAD) {
+            uint4 v[AHEAD], n[AHEAD];
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int c = c0 + 32 * k;
+                const bool whole = c >= first && c + first < last;   // all of its pieces lie in the row
+                v[k] = whole ? pieces[c] : make_uint4(0, 0, 0, 0);
+                n[k] = whole && off ? pieces[c + 1] : make_uint4(0, 0, 0, 0);
+            }
+#pragma unroll
+            for (int k = 0; k < AHEAD; ++k) {
+                const int c = c0 + 32 * k;
+                if (c >= chunks) break;
+                unsigned short *const out = to + r * a.to_ld + 8 * c;
+                if (c < first || c + first >= last) {
+                    for (int e = 0; e < 8; ++e) out[e] = row[8 * c + e];
+                    continue;
+                }
+                uint32_t w[8] = {v[k].x, v[k].y, v[k].z, v[k].w, n[k].x, n[k].y, n[k].z, n[k].w};
                 if (off & 8) {
 #pragma unroll
                     for (int e = 0; e < 6; ++e) w[e] = w[e + 2];
@@ -331,9 +342,7 @@ __global__ void __launch_bounds__(256) pack_kernel(const __grid_constant__ PackA
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = __funnelshift_r(w[e], w[e + 1], 16);
                 }
-                *reinterpret_cast<uint4 *>(to + r * a.to_ld + 8 * c) = make_uint4(w[0], w[1], w[2], w[3]);
-            } else {
-                for (int e = 0; e < 8; ++e) to[r * a.to_ld + 8 * c + e] = row[8 * c + e];
+                *reinterpret_cast<uint4 *>(out) = make_uint4(w[0], w[1], w[2], w[3]);
             }
         }
         for (int e = 8 * chunks + lane; e < a.cols; e += 32) to[r * a.to_ld + e] = row[e];

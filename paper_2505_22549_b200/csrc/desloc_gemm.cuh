@@ -206,15 +206,20 @@ __device__ __forceinline__ void fetch32(const float *from, long long ld, const P
         }
     }
 }
-// registers -> staging area, whence each lane reads its row (behind a __syncwarp()); 16-bit rows on other boundaries come only now, an instruction each.
+// registers -> staging area, whence each lane reads its row (behind a __syncwarp()); 16-bit rows on other boundaries come only now, 16 of them at a time.
 __device__ __forceinline__ void settle16(char *st, int lane, const void *from, long long ld, const Piece &p, const uint4 (&v)[4]) {
     if (p.wide) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(st + spot16(lane, i)) = v[i];
     } else if (lane < p.cols) {
-        const unsigned short *const src = static_cast<const unsigned short *>(from) + lane;
-#pragma unroll 8
-        for (int r = 0; r < p.rows; ++r) *reinterpret_cast<unsigned short *>(st + place16(r, lane >> 3) + (lane & 7) * 2) = src[r * ld];
+        const unsigned short *src = static_cast<const unsigned short *>(from) + lane;
+        for (int r0 = 0; r0 < p.rows; r0 += 16, src += 16 * ld) {
+            unsigned short x[16];
+#pragma unroll
+            for (int r = 0; r < 16; ++r) x[r] = r0 + r < p.rows ? src[r * ld] : 0;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) *reinterpret_cast<unsigned short *>(st + place16(r0 + r, lane >> 3) + (lane & 7) * 2) = x[r];
+        }
     }
 }
 __device__ __forceinline__ void settle32(char *st, int lane, const uint4 (&v)[8]) {
