@@ -12,7 +12,7 @@ namespace {
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 // ---- forward -----------------------------------------------------------------------------------------
-// z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.
+// z = silu(g) u of the two halves of the accumulator; g and u, too, where they are kept.  Bound: tensor cores.  4 x 2048 tokens, 2048 x 8192: 440 us for 550 GFLOP.
 struct UpEpilogue {
     static constexpr int STAGING = 3 * 2048;
     static constexpr bool READS_BOXES = false, WRITES_BOXES = true;
@@ -58,7 +58,8 @@ struct UpEpilogue {
     }
 };
 
-// A product as it is, in bf16 or fp32, or added to what is there.
+// A product as it is, in bf16 or fp32, or added to what is there.  Bound: tensor cores.  The same sizes: down 216 us for 275 GFLOP, dh 447 for 550, the weights' gradients added to bf16 ones
+// 766 for 825.
 template <bool BF16, bool ADD>
 struct StoreEpilogue {
     static constexpr int STAGING = BF16 ? 2048 : 4096;
@@ -123,7 +124,8 @@ struct StoreEpilogue {
 };
 
 // ---- backward ----------------------------------------------------------------------------------------
-// From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.
+// From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.  Bound: at short k what comes and goes by element, 10 bytes each; 4 x 8192
+// tokens, 576 x 1536: 170 us, 3 TB/s of those; 4 x 2048, 2048 x 8192: 300 us for 275 GFLOP.
 struct DzEpilogue {
     static constexpr int STAGING = 3 * 2048;
     static constexpr bool READS_BOXES = false, WRITES_BOXES = true;
@@ -289,7 +291,7 @@ cudaError_t launch_few(const FfnArgs &a, __nv_bfloat16 *z, cudaStream_t stream, 
 }
 
 // ---- rows that the copy engine does not take ---------------------------------------------------------
-// Copies matrices into rows on 16-byte boundaries.  Bound: HBM, two bytes each way.  A warp takes a row, a lane 16 bytes of the copy, which lie in two aligned
+// Copies matrices into rows on 16-byte boundaries.  Bound: HBM, two bytes each way; 4 x 3 matrices of 1501 x 4003 in 68 us, 4.2 TB/s.  A warp takes a row, a lane 16 bytes of the copy, which lie in two aligned
 // pieces of 16 bytes.
 constexpr int PACK_MOST = 64;
 struct PackArgs {

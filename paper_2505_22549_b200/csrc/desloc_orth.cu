@@ -124,7 +124,8 @@ __device__ __forceinline__ double block_sum(double v) {
     return v;
 }
 
-// Squares, eight at a time in fp32 (values below 1e-22 count as 0, beyond 1e18 as infinite), then in fp64.  Bound: HBM, each element read once.
+// Squares, eight at a time in fp32 (values below 1e-22 count as 0, beyond 1e18 as infinite), then in fp64.  Bound: HBM, each element read once; 57 M of fp32 with bf16 gradients
+// 55 us, 6.2 TB/s.
 template <typename UT, typename GT>
 __global__ void __launch_bounds__(ORTH_THREADS, 4) orth_norm_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(ORTH_THREADS, 4) orth_norm_kernel(const __grid
     if (threadIdx.x == 0) s.partial[static_cast<long long>(which) * s.most + blockIdx.x] = sum;
 }
 
-// X in two halves.  Bound: L2 or HBM, each element read again and four bytes written.
+// X in two halves.  Bound: HBM, each element read again and four bytes written; the same 57 M 87 us, 6.5 TB/s.
 template <typename UT, typename GT>
 __global__ void __launch_bounds__(ORTH_THREADS, 4) orth_scale_kernel(const __grid_constant__ Sources s) {
     begin_and_let_next_begin();
@@ -185,6 +186,8 @@ __global__ void __launch_bounds__(ORTH_THREADS, 4) orth_scale_kernel(const __gri
 }
 
 // ---- the products' epilogues -------------------------------------------------------------------------
+// Bound: bringing operands and emptying accumulators, nearly alike: 840 matrices of 192 .. 1536 x 576, k as G's is the longer side and of G^2 the shorter one, 4.2 ms of ten such products each
+// (1.75 TFLOP, half of them counted).
 // A symmetric result: alpha times the sums, plus b times in[0], plus `diagonal` there; pieces below the diagonal go to the other one's place, too.
 struct SymEpilogue {
     static constexpr int STAGING = 2048;
@@ -251,6 +254,7 @@ struct SymEpilogue {
 };
 
 // X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
+// Bound: as above; the same 840 matrices 3.3 ms of four such products each (2.4 TFLOP), 3.4 without boxes.
 struct NextEpilogue {
     static constexpr int STAGING = 3 * 2048;
     static constexpr bool READS_BOXES = true, WRITES_BOXES = true;
