@@ -437,7 +437,7 @@ cudaError_t product_store(const Operand &x, const Operand &w, int M, int tokens,
     static thread_local GemmArgs<E> a;
     for (int m0 = 0; m0 < M; m0 += WORKERS) {
         const int some = std::min(WORKERS, M - m0);
-        const GemmCut cut = pick_cut(false, tokens, k, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(tokens, n, c, false, false); });
+        const GemmCut cut = pick_cut(false, tokens, k, [&](const GemmCut &c) { return TileCount{static_cast<int64_t>(some) * tiles_of(tokens, n, c, false, false), 0}; });
         begin_gemm(a, true, cut, false, false, 1);
         cudaError_t e = x.maps(a, 0, 0, M, m0, some, box_rows(tokens));
         if (e == cudaSuccess) e = w.maps(a, 1, 1, M, m0, some, cut.box_n(false));
@@ -484,7 +484,7 @@ cudaError_t weight_grads(const FfnArgs &a, const Operands &o, const Operand &z, 
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
         const GemmCut cut = pick_cut(false, GEMM_BM, a.tokens, [&](const GemmCut &c) {
-            return static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, c, false, false) + tiles_of(a.width, a.hidden, c, false, false));
+            return TileCount{static_cast<int64_t>(some) * (2 * tiles_of(a.hidden, a.width, c, false, false) + tiles_of(a.width, a.hidden, c, false, false)), 0};
         });
         begin_gemm(g, true, cut, false, false, 1);
         int map = 0;
@@ -534,7 +534,7 @@ cudaError_t launch_ffn(const FfnArgs &a, char *work, int *err, int wait_limit, c
     static thread_local GemmArgs<UpEpilogue> g;
     for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
         const int some = std::min(WORKERS, a.M - m0);
-        const GemmCut cut = pick_cut(true, a.tokens, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, true, false); });
+        const GemmCut cut = pick_cut(true, a.tokens, a.width, [&](const GemmCut &c) { return TileCount{static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, true, false), 0}; });
         const int box = cut.box_n(true);
         begin_gemm(g, true, cut, true, false, 1);
         e = o.h.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
@@ -599,7 +599,7 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<DzEpilogue> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const GemmCut cut = pick_cut(false, a.tokens, a.width, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, false, false); });
+            const GemmCut cut = pick_cut(false, a.tokens, a.width, [&](const GemmCut &c) { return TileCount{static_cast<int64_t>(some) * tiles_of(a.tokens, a.hidden, c, false, false), 0}; });
             begin_gemm(g, true, cut, false, false, 1);
             e = o.dy.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
             if (e == cudaSuccess) e = o.down.maps(g, 1, 1, a.M, m0, some, 64);
@@ -633,7 +633,7 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         static thread_local GemmArgs<E> g;
         for (int m0 = 0; m0 < a.M; m0 += WORKERS) {
             const int some = std::min(WORKERS, a.M - m0);
-            const GemmCut cut = pick_cut(false, a.tokens, 2 * a.hidden, [&](const GemmCut &c) { return static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, c, false, false); });
+            const GemmCut cut = pick_cut(false, a.tokens, 2 * a.hidden, [&](const GemmCut &c) { return TileCount{static_cast<int64_t>(some) * tiles_of(a.tokens, a.width, c, false, false), 0}; });
             begin_gemm(g, true, cut, false, false, 2);
             e = dg.maps(g, 0, 0, a.M, m0, some, box_rows(a.tokens));
             if (e == cudaSuccess) e = du.maps(g, 1, 0, a.M, m0, some, box_rows(a.tokens));

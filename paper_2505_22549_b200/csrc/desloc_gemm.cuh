@@ -695,9 +695,14 @@ inline int tiles_of(int m, int n, const GemmCut &cut, bool dual, bool symmetric)
     for (int i = 0; i < mt; ++i) all += std::min((i * bm + bm - 1) / tile_n + 1, nt);
     return all;
 }
-// The cut that is done first: rounds of tiles, a tile as long as bringing and multiplying 64 k takes (measured, in cycles: 900 for 256 columns and 780 for 192 of a pair, 1000 for 256 of a
-// block alone, 600 for 128), or as emptying it (some 1500 for the 128 columns that the warps take at a time); and what a launch of a round takes before and behind.
-// Few rows (up to FEW_ROWS): what takes time is B from memory, some 6 cycles a column of 64 k when all SMs read.  tiles(cut): how many there are, all with k of about `k`.
+// How many tiles a launch has, and how many of those lie on the diagonal of a symmetric product and bring one operand.
+struct TileCount {
+    int64_t all, once;
+};
+// The cut that is done first: rounds of tiles (half of what the last round leaves empty counted: tiles differ in k), a tile as long as bringing and multiplying 64 k takes, or as
+// emptying it (some 1500 cycles for the 128 columns that the warps take at a time); and what a launch takes before and behind.  In cycles for 64 k, from products of 8192 k: 775 for
+// 256, 672 for 192 and 657 for 128 columns of a pair, 844, 740 and 615 of a block alone; tiles that bring one operand a quarter less.  Few rows (up to FEW_ROWS): what
+// takes time is B from memory, some 6 cycles a column when all SMs read.  tiles(cut): a TileCount, all with k of about `k`.
 constexpr int64_t FEW_ROWS = 64;
 template <typename F>
 GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
@@ -706,9 +711,11 @@ GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
     for (int pairs = m > FEW_ROWS ? 1 : 0; pairs >= 0; --pairs)
         for (int n = 256; n >= (pairs ? 128 : 64); n -= 64) {
             const GemmCut cut{n, pairs != 0};
-            const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, rounds = (tiles(cut) + slots - 1) / slots;
-            const int64_t step = m <= FEW_ROWS ? 60 + 6 * n : pairs ? 440 + 9 * n / 5 : 240 + 3 * n, products = (k + GEMM_BK - 1) / GEMM_BK * step, empty = (cut.out_n(dual) + 127) / 128 * 1500;
-            const int64_t cost = rounds * (std::max(products, empty) + 200) + std::min(products, empty);
+            const TileCount count = tiles(cut);
+            const int64_t slots = pairs ? NUM_SMS / 2 : NUM_SMS, step = m <= FEW_ROWS ? 60 + 6 * n : pairs ? 440 + 13 * n / 10 : 384 + 9 * n / 5;
+            const int64_t products = (k + GEMM_BK - 1) / GEMM_BK * (step * (4 * count.all - count.once) / (4 * count.all)), empty = (cut.out_n(dual) + 127) / 128 * 1500;
+            const int64_t each = std::max(products, empty) + 200;
+            const int64_t cost = (count.all + slots - 1) / slots * each + std::max(count.all, slots) * each / slots + 2 * std::min(products, empty);
             if (!best.tile_n || cost < least) best = cut, least = cost;
         }
     return best;

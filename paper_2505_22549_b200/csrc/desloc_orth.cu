@@ -453,15 +453,20 @@ double scale_of(const OrthArgs &a, int rows, int cols) {
 
 // The cut of a product of all shapes: tiles(shape, cut) of one matrix, k(shape).
 template <typename K, typename F>
-GemmCut pick(const Round &r, const K &k, const F &tiles) {
+GemmCut pick(const Round &r, bool symmetric, const K &k, const F &tiles) {
     int64_t all = 0, sum = 0;
     for (int i = 0; i < r.nshapes; ++i) {
         const int64_t n = static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], GemmCut{256, true});
         all += n, sum += n * k(r.shapes[i]);
     }
     return pick_cut(false, GEMM_BM, sum / all, [&](const GemmCut &cut) {
-        int64_t n = 0;
-        for (int i = 0; i < r.nshapes; ++i) n += static_cast<int64_t>(r.shapes[i].count) * tiles(r.shapes[i], cut);
+        TileCount n{0, 0};
+        const int rows = GEMM_BM * (cut.pairs ? 2 : 1);
+        for (int i = 0; i < r.nshapes; ++i) {
+            const Shape &s = r.shapes[i];
+            n.all += static_cast<int64_t>(s.count) * tiles(s, cut);
+            if (symmetric && cut.tile_n == rows) n.once += static_cast<int64_t>(s.count) * ((s.n + rows - 1) / rows);
+        }
         return n;
     });
 }
@@ -474,7 +479,7 @@ struct Run {
 // A symmetric product of `from` (x: X of this step, else G) for all shapes.
 cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b, float diagonal, const Run &run) {
     static thread_local GemmArgs<SymEpilogue> a;
-    const GemmCut cut = pick(r, [&](const Shape &s) { return gram ? s.m : s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.n, s.n, c, false, true); });
+    const GemmCut cut = pick(r, true, [&](const Shape &s) { return gram ? s.m : s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.n, s.n, c, false, true); });
     begin_gemm(a, false, cut, false, true, 1);
     a.epi.b = b, a.epi.diagonal = diagonal;
     for (int i = 0; i < r.nshapes; ++i) {
@@ -500,7 +505,7 @@ cudaError_t symmetric(const Round &r, bool gram, int side, float alpha, float b,
 // X := a X + (polynomial of G) X, to the other side or, at last, to `epi`'s places.
 template <typename E>
 cudaError_t update(const Round &r, int side, const E &epi, GemmArgs<E> &a, const long long *out_ld, const Run &run) {
-    const GemmCut cut = pick(r, [](const Shape &s) { return s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.rows, s.cols, c, false, false); });
+    const GemmCut cut = pick(r, false, [](const Shape &s) { return s.n; }, [](const Shape &s, const GemmCut &c) { return tiles_of(s.rows, s.cols, c, false, false); });
     begin_gemm(a, false, cut, false, false, 1);
     a.epi = epi;
     for (int i = 0; i < r.nshapes; ++i) {
