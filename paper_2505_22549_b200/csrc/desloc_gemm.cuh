@@ -430,7 +430,6 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     if constexpr (CG == 2) cluster_sync();
     tmem_fence_after();
     const uint32_t tmem = tmem_at;
-    wait_for_earlier_kernels();
     const auto give_up = [&] {
         if (a.err) *reinterpret_cast<volatile int *>(a.err) = 1;
         *reinterpret_cast<volatile int *>(&failed) = 1;
@@ -441,9 +440,10 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             TileWalk at;
             int s = 0, asked = 0;
             uint32_t phase = 0;
-            bool ok = true;
+            bool ok = true, first = true;   // (memory is touched by this thread and the warps below; where the first tile lies is looked up before earlier kernels end)
             for (int tile = tile0; ok && tile < a.tiles; tile += tile_step) {
                 const GemmGroup &g = at.find<CG>(a, tile);
+                if (first) wait_for_earlier_kernels(), first = false;
                 const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
                 const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
                 const int boxes = (own_n + 63) / 64, turned = a.rotate ? static_cast<int>(tile * 29u % steps) : 0;
@@ -561,6 +561,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         };
         if (tile < a.tiles) {
             g = &at.find<CG>(a, tile);
+            wait_for_earlier_kernels();
             ask();
         }
         bool ok = true;
