@@ -123,6 +123,8 @@ __device__ __forceinline__ void bar_init(uint64_t *bar, int count) {
 __device__ __forceinline__ void bar_expect(uint64_t *bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" :: "r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
+// A whole warp's wait, with one answer: lanes poll on their own, and at the limit some may have seen what others have not.
+__device__ __forceinline__ bool warp_wait(uint64_t *bar, uint32_t parity, int limit) { return __any_sync(0xffffffffu, bar_wait(bar, parity, limit)); }
 // One lane of a warp.  (By this instruction the compiler knows that what follows runs in one lane alone and holds addresses and descriptors in uniform registers; behind
 // `lane == 0` it did not, and every product took 150 cycles to issue.)
 __device__ __forceinline__ bool elect_one() {
@@ -567,7 +569,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
         bool ok = true;
         while (tile < a.tiles) {
             if (c == c0) {
-                ok = bar_wait(&ready[buf], turn, a.wait_limit);
+                ok = warp_wait(&ready[buf], turn, a.wait_limit);
                 if (!ok) break;
                 tmem_fence_after();
             }
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             }
             if (tile < a.tiles) ask();
             if (reads) {
-                ok = bar_wait(&came[taken_boxes & 1], (taken_boxes >> 1) & 1, a.wait_limit);
+                ok = warp_wait(&came[taken_boxes & 1], (taken_boxes >> 1) & 1, a.wait_limit);
                 if (!ok) break;
                 ++taken_boxes;
             }

@@ -325,7 +325,8 @@ def matrices(M, shapes, seed=0, dtype=F32, kind="normal"):
 
 
 SHAPES = [[(1, 1)], [(1, 5), (5, 1)], [(8, 8), (7, 9), (9, 7)], [(72, 72), (24, 72), (200, 72), (72, 200)], [(64, 64), (128, 128), (129, 127)], [(71, 33), (300, 301)],
-          [(576, 576), (192, 576), (1536, 576), (576, 1536)], [(1000, 1000), (260, 1030)], [(3, 4000), (4000, 3)]]
+          [(576, 576), (192, 576), (1536, 576), (576, 1536)], [(1000, 1000), (260, 1030)], [(3, 4000), (4000, 3)],
+          [(128, 250), (128, 330), (340, 128), (129, 129), (120, 500), (16, 1600), (1750, 16), (17, 900), (64, 790)]]   # on both sides of what a block takes alone
 
 
 @pytest.mark.parametrize("shapes", SHAPES)
