@@ -24,7 +24,7 @@
 
 namespace desloc {
 
-constexpr int GEMM_BM = 128, GEMM_BK = 64, GEMM_MAX_STAGES = 8, GEMM_EPI_WARPS = 16, GEMM_THREADS = 128 + 32 * GEMM_EPI_WARPS;
+constexpr int GEMM_BM = 128, GEMM_BK = 64, GEMM_MAX_STAGES = 16, GEMM_EPI_WARPS = 16, GEMM_THREADS = 128 + 32 * GEMM_EPI_WARPS;
 constexpr int GEMM_A_BYTES = GEMM_BM * GEMM_BK * 2;
 constexpr int GEMM_SMEM = 227 * 1024 - 2048, GEMM_MAX_GROUPS = 48, GEMM_MAX_MAPS = 64, GEMM_DRAIN_LIMIT = 1 << 22;
 
@@ -54,6 +54,7 @@ struct GemmArgs {
     GemmGroup groups[GEMM_MAX_GROUPS];
     int ngroups, tiles;
     int tile_n, stages, segments;   // columns of a tile; stages of the ring; pairs of operands that one accumulator sums
+    int a_bytes;             // room for A in a stage: of its boxes (the products read 128 rows; what lies behind is never looked at)
     int pairs;               // blocks work in pairs
     int dual;                // the tile's columns are two halves, of two B operands
     int symmetric;           // only tiles that reach the lower triangle, of a product of one operand with itself
@@ -391,7 +392,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     if constexpr (CG == 2) asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(rank));
     const uint32_t pad = (1024 - (smem_u32(gemm_smem) & 1023)) & 1023;
     char *const ring = gemm_smem + pad;
-    const int own_n = a.tile_n / CG, stage_bytes = GEMM_A_BYTES + (own_n + 63) / 64 * 64 * (GEMM_BK * 2);
+    const int own_n = a.tile_n / CG, stage_bytes = a.a_bytes + (own_n + 63) / 64 * 64 * (GEMM_BK * 2);
     const int tile0 = blockIdx.x / CG, tile_step = gridDim.x / CG;
     begin_and_let_next_begin();
     if (threadIdx.x == 0) {
@@ -461,7 +462,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                         if (step >= steps) step -= steps;
                     }
                     const int k0 = step * GEMM_BK;
-                    char *const sa = ring + s * stage_bytes, *const sb = sa + GEMM_A_BYTES;
+                    char *const sa = ring + s * stage_bytes, *const sb = sa + a.a_bytes;
                     const CUtensorMap *const ma = &a.maps[g.a_map + seg], *const mb = &a.maps[g.b_map + seg];
                     const int za = g.a_batch + at.batch, zb = g.b_batch + at.batch;
                     const uint32_t bar = first_blocks<CG>(&full[s]);
@@ -514,7 +515,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                     if (!ok) break;
                     tmem_fence_after();
                     const uint32_t sa = smem_u32(ring + s * stage_bytes);
-                    const uint64_t da = operand_desc(sa, g.a_mn), db = once ? da : operand_desc(sa + GEMM_A_BYTES, g.b_mn);
+                    const uint64_t da = operand_desc(sa, g.a_mn), db = once ? da : operand_desc(sa + a.a_bytes, g.b_mn);
 #pragma unroll
                     for (int x = 0; x < GEMM_BK / 16; ++x) mma_f16<CG>(d, da + x * ka, db + x * kb, idesc, kk > 0 || x > 0);
                     mma_commit<CG>(&empty[s]);
@@ -726,7 +727,7 @@ GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
 
 template <typename E>
 void begin_gemm(GemmArgs<E> &a, bool bf16, const GemmCut &cut, bool dual, bool symmetric, int segments) {
-    a.ngroups = a.tiles = 0;
+    a.ngroups = a.tiles = a.a_bytes = 0;
     a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.rotate = 0, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
     const int bm = GEMM_BM * (cut.pairs ? 2 : 1);
     a.row_first = (bm - 1) / cut.tile_n + 1, a.row_rest = (bm - 1) % cut.tile_n;
@@ -769,12 +770,14 @@ template <typename E, int CG>
 cudaError_t launch_gemm(GemmArgs<E> &a, cudaStream_t stream) {
     const cudaError_t e = gemm_ready<E, CG>();
     if (e != cudaSuccess) return e;
-    const int stage = GEMM_A_BYTES + (a.tile_n / CG + 63) / 64 * 64 * GEMM_BK * 2;
-    a.stages = std::min(GEMM_MAX_STAGES, (GEMM_SMEM - 1024 - GEMM_EPI_WARPS * E::STAGING) / stage);
+    for (int i = 0; i < a.ngroups; ++i) a.a_bytes = std::max(a.a_bytes, (a.groups[i].a_mn ? GEMM_BM : a.groups[i].a_rows) * GEMM_BK * 2);
+    const int stage = a.a_bytes + (a.tile_n / CG + 63) / 64 * 64 * GEMM_BK * 2;
+    // (behind the last stage there is room for the rows of A that it lacks)
+    a.stages = std::min(GEMM_MAX_STAGES, (GEMM_SMEM - 1024 - std::max(GEMM_EPI_WARPS * E::STAGING, GEMM_A_BYTES)) / stage);
     cudaLaunchConfig_t lc{};
     lc.gridDim = dim3(static_cast<unsigned>(CG * std::min(a.tiles, NUM_SMS / CG)));
     lc.blockDim = dim3(GEMM_THREADS);
-    lc.dynamicSmemBytes = 1024 + static_cast<size_t>(a.stages) * stage + GEMM_EPI_WARPS * E::STAGING;
+    lc.dynamicSmemBytes = 1024 + static_cast<size_t>(a.stages) * stage + std::max(GEMM_EPI_WARPS * E::STAGING, GEMM_A_BYTES);
     lc.stream = stream;
     cudaLaunchAttribute at[2]{};
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
