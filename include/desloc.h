@@ -478,7 +478,7 @@ typedef struct {
 /*
  * y as above.
  *   kept_gate, kept_up : device, bf16, dense [M][tokens][hidden]: g and u for the way back; both or neither (NULL).
- *   y                  : row (m, i), bf16.
+ *   y                  : row (m, i), bf16; may be h.
  *   work, work_bytes   : device memory, 256-byte aligned, of desloc_gated_ffn_bytes() bytes at least; that answer goes by the sizes and by how h and the weights
  *                        lie (rows that begin on 16-byte boundaries are read in place, others are copied first).
  */
@@ -491,7 +491,7 @@ DESLOC_API int64_t desloc_gated_ffn_bytes(const desloc_ctx *ctx, const desloc_ff
  *   du = dz g s,  dg = dz u s (1 + g (1 - s)),  dh = dg gate + du up;
  * gradients of the weights dg^T h, du^T h and dy^T z in the place of the workers' gradients of the three tensors, in cfg.grad_dtype -- or, where `accumulate`
  * is not 0, added to what those hold.  z, dg and du enter their products in bf16.
- *   kept_gate, kept_up : what desloc_gated_ffn() kept.      dy, dh : rows (m, i), bf16.
+ *   kept_gate, kept_up : what desloc_gated_ffn() kept.      dy, dh : rows (m, i), bf16; dh may be dy, or h.
  *   grads              : host array of M*num_tensors DEVICE pointers, as for desloc_step(); only those of the three are read.  DESLOC_E_INVALID where two overlap.
  */
 DESLOC_API int desloc_gated_ffn_grad(desloc_ctx *ctx, const desloc_ffn *ffn, const void *kept_gate, const void *kept_up, const desloc_rows *dy,
@@ -511,13 +511,15 @@ typedef enum {
     DESLOC_SCALE_RMS = 2     /* times 0.2 sqrt(max(rows, columns)): entries as large as those of an Adam step */
 } desloc_scale_t;
 #define DESLOC_MAX_NEWTON_SCHULZ 32
+#define DESLOC_MAX_COEFFICIENTS 60.0f
 
 typedef struct {
     const int32_t *tensors;     /* host, [count] numbers of tensors, no two alike */
     const int64_t *columns;     /* host, [count]: each divides numel into rows; rows and columns up to 2^20 */
     int32_t count;              /* of them, for every worker; 0: nothing is done */
     int32_t steps;              /* 1 .. DESLOC_MAX_NEWTON_SCHULZ */
-    const float *coefficients;  /* host, [steps][3], finite, at most 16 in magnitude; NULL: (3.4445, -4.7750, 2.0315) at every step */
+    const float *coefficients;  /* host, [steps][3], |a| + |b| + |c| up to DESLOC_MAX_COEFFICIENTS; NULL: (3.4445, -4.7750, 2.0315) at every step.  Singular values
+                                   are to stay below 2 from step to step: far beyond, results are infinite or NaN */
     float eps;                  /* >= 0; 0 makes NaN of a matrix of zeros */
     int32_t scale;              /* desloc_scale_t */
     int32_t updates_dtype;

@@ -28,6 +28,7 @@ DESLOC_I32, DESLOC_I64 = 0, 1
 DESLOC_MAX_TOP = 32
 DESLOC_SCALE_NONE, DESLOC_SCALE_ASPECT, DESLOC_SCALE_RMS = 0, 1, 2
 DESLOC_MAX_NEWTON_SCHULZ = 32
+DESLOC_MAX_COEFFICIENTS = 60.0
 
 OPT_BY_NAME = {"adam": DESLOC_ADAM, "adopt": DESLOC_ADOPT, "sgdm": DESLOC_SGDM}
 DTYPE_BY_NAME = {"f32": DESLOC_F32, "bf16": DESLOC_BF16}

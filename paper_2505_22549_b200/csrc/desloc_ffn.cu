@@ -627,6 +627,10 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
         }
     }
     const Operand z = inner_operand(inner[0], a, a.hidden), dg = inner_operand(inner[1], a, a.hidden), du = inner_operand(inner[2], a, a.hidden);
+    // (before dh, which may come in the place of h or dy)
+    if (a.grad_bf16) e = (a.accumulate ? weight_grads<true, true> : weight_grads<true, false>)(a, o, z, dg, du, r);
+    else e = (a.accumulate ? weight_grads<false, true> : weight_grads<false, false>)(a, o, z, dg, du, r);
+    if (e != cudaSuccess) return e;
     {
         // dh = dg gate + du up, one accumulator
         using E = StoreEpilogue<true, false>;
@@ -656,8 +660,7 @@ cudaError_t launch_ffn_grad(const FfnArgs &a, char *work, int *err, int wait_lim
             if (e != cudaSuccess) return e;
         }
     }
-    if (a.grad_bf16) return a.accumulate ? weight_grads<true, true>(a, o, z, dg, du, r) : weight_grads<true, false>(a, o, z, dg, du, r);
-    return a.accumulate ? weight_grads<false, true>(a, o, z, dg, du, r) : weight_grads<false, false>(a, o, z, dg, du, r);
+    return cudaSuccess;
 }
 
 }  // namespace desloc

@@ -710,10 +710,10 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
     const auto known = [](int32_t t) { return t == DESLOC_F32 || t == DESLOC_BF16; };
     if (how.scale < DESLOC_SCALE_NONE || how.scale > DESLOC_SCALE_RMS || (how.updates && !known(how.updates_dtype))) return DESLOC_E_INVALID;
     coefficients.clear();
-    for (int i = 0; i < 3 * how.steps; ++i) {
-        const float v = how.coefficients ? how.coefficients[i] : kNewtonSchulz[i % 3];
-        if (!std::isfinite(v) || std::fabs(v) > 16.f) return DESLOC_E_RANGE;
-        coefficients.push_back(v);
+    for (int i = 0; i < how.steps; ++i) {
+        const float *const v = how.coefficients ? how.coefficients + 3 * i : kNewtonSchulz;
+        if (!(std::fabs(v[0]) + std::fabs(v[1]) + std::fabs(v[2]) <= DESLOC_MAX_COEFFICIENTS)) return DESLOC_E_RANGE;   // (nor NaN)
+        coefficients.insert(coefficients.end(), v, v + 3);
     }
     std::vector<char> seen(static_cast<size_t>(c.num_tensors), 0);
     list.clear();

@@ -14,7 +14,7 @@ namespace {
 // product is three, hi hi + hi lo + lo hi: 20 bits, at no cost that shows here.  What takes time is latency: three products, each behind the other, a step, with all threads
 // turning sums into operands in between.  Two 72 x 72 matrices 28 us (92 in the seventeen launches of the kernels for large ones), 3.6 of it a step; 56 of up to 200 x 72 as a step of x 47 us
 // (127).
-constexpr float SMALL_UNIT = 1024.f;   // (of everything held: coefficients up to 16 keep P in fp16's range)
+constexpr float SMALL_UNIT = 1024.f;   // (of everything held: coefficients of 60 together keep P in fp16's range)
 constexpr int SMALL_THREADS = 512, SMALL_GROUPS = SMALL_THREADS / 128, SMALL_MOST = 256, SMALL_COLUMNS = 256, SMALL_BYTES = 225 * 1024;
 
 struct SmallArgs {

@@ -412,7 +412,7 @@ class DesLoc:
     def gated_ffn(self, tensors, h: torch.Tensor, weights, keep: bool = False, out: Optional[torch.Tensor] = None):
         """The gated feed-forward block down(silu(gate h) * (up h)) of every worker with its own weights, on torch's current stream.  tensors: numbers of gate,
         up ([hidden, width]) and down ([width, hidden]); h: bf16 [M, ..., width]; weights: nested lists like x of bf16 copies, of which only those three are looked at.
-        Returns y like h, or with keep (y, (gate h, up h)) for gated_ffn_grad()."""
+        Returns y like h (into `out`, which may be h, where it is given), or with keep (y, (gate h, up h)) for gated_ffn_grad()."""
         tensors = tuple(tensors)
         if out is None:     # the usual layouts, natively
             r = _native.gated_ffn(self.ctx, self._table, tensors, h, weights, keep, self._index)
@@ -429,7 +429,7 @@ class DesLoc:
 
     def gated_ffn_grad(self, tensors, h: torch.Tensor, kept, dy: torch.Tensor, weights, grads, accumulate: bool = False,
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """The way back of gated_ffn(): returns dh (into `out` where it is given) and writes the three weights' gradients into the workers' gradients in `grads` (what
+        """The way back of gated_ffn(): returns dh (into `out` where it is given, which may be dy or h) and writes the three weights' gradients into the workers' gradients in `grads` (what
         step() reads, or bind_grads()' handle); accumulate: added to what they hold.  kept: what gated_ffn(keep=True) returned beside y."""
         tensors = tuple(tensors)
         if out is None and len(kept) == 2:
@@ -475,7 +475,7 @@ class DesLoc:
                       scale: str = "none") -> None:
         """Every worker's matrices `tensors` (numbers) of `updates` (nested lists like x, fp32 or bf16; None: the momentum u) brought to singular values near 1 by `steps`
         Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad.  columns: of each matrix,
-        where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones.  scale: "none", "aspect"
+        where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones; magnitudes sum to 60 at most.  scale: "none", "aspect"
         (sqrt(max(1, rows / columns))) or "rms" (0.2 sqrt(max(rows, columns)))."""
         tensors = tuple(tensors)
         if updates is None:

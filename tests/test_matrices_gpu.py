@@ -188,6 +188,42 @@ def test_gated_ffn_layouts():
         assert torch.equal(dh, same) and all(torch.equal(p, q) for r, s in zip(first, second) for p, q in zip(r, s))
 
 
+@pytest.mark.parametrize("T,D,F", [(3, 40, 72), (50, 40, 72), (50, 41, 72), (400, 512, 640)])
+def test_gated_ffn_in_the_place_of_what_it_reads(T, D, F):
+    b = Block(2, T, D, F)
+    y, kept = b.opt.gated_ffn(b.TENSORS, b.h, b.weights, keep=True)
+    h = b.h.clone()
+    assert b.opt.gated_ffn(b.TENSORS, h, b.weights, out=h) is h and torch.equal(h, y)
+    grads = lambda: [[torch.zeros(s, dtype=BF, device="cuda") for s in ((F, D), (D, F), (5,), (F, D))] for _ in range(2)]
+    want = grads()
+    dh = b.opt.gated_ffn_grad(b.TENSORS, b.h, kept, b.dy, b.weights, want)
+    for place in range(2):
+        h, dy, got = b.h.clone(), b.dy.clone(), grads()
+        out = (h, dy)[place]
+        b.opt.gated_ffn_grad(b.TENSORS, h, kept, dy, b.weights, got, out=out)
+        assert torch.equal(out, dh) and all(torch.equal(p, q) for r, s in zip(want, got) for p, q in zip(r, s))
+
+
+def test_gated_ffn_beyond_32_bits():
+    """More than 2^31 elements per worker of what lies between the products; gradients of the first and last tokens alone, all others add zeros."""
+    M, T, D, F, few = 2, 525000, 64, 4104, 8
+    b = Block(M, T, D, F)
+    ends = lambda t: torch.cat([t[:, :few], t[:, -few:]], 1)
+    y, kept = b.opt.gated_ffn(b.TENSORS, b.h, b.weights, keep=True)
+    want, tol = b.forward(ends(b.h))
+    for got, w, t in zip((*kept, y), want, tol):
+        check(ends(got), w, t)
+    b.dy[:, few:-few] = 0
+    grads = [[torch.zeros(s, dtype=BF, device="cuda") for s in ((F, D), (D, F), (5,), (F, D))] for _ in range(M)]
+    dh = b.opt.gated_ffn_grad(b.TENSORS, b.h, kept, b.dy, b.weights, grads)
+    (want, tol), *weights = b.backward(ends(b.h), *map(ends, kept), ends(b.dy))
+    check(ends(dh), want, tol + HB * (want.abs() + tol) + 1e-30)
+    assert bool((dh[:, few:-few] == 0).all())
+    for k, (want, tol) in zip(b.TENSORS, weights):
+        for m in range(M):
+            check(grads[m][k], want[m], tol[m] + (HB + 2 * U) * (want[m].abs() + tol[m]) + 1e-30)
+
+
 def test_gated_ffn_extremes():
     """Far gates, zeros, infinities and NaN: each row for itself."""
     b = Block(1, 6, 16, 24)
@@ -372,6 +408,57 @@ def test_look_ahead_scales_and_coefficients(grad_dtype):
         assert all(bool((row[1] == 0).all()) for row in out)
 
 
+@pytest.mark.parametrize("shape", [(72, 72), (200, 72), (130, 260), (576, 1536)])
+def test_triples_that_change_from_step_to_step(shape):
+    """Of large coefficients at first, which take singular values up to two on the way."""
+    steps = [(8.3, -23.6, 17.3), (4.1, -2.95, 0.55), (3.95, -2.9, 0.55), (3.3, -2.5, 0.51), (2.3, -1.7, 0.42)]
+    opt = context(1, [shape])
+    u = matrices(1, [shape], 13)
+    out = [[torch.empty(shape, device="cuda")]]
+    opt.orthogonalize([0], u, out=out, coefficients=steps)
+    close(out[0][0], *allowed(u[0][0], steps))
+
+
+@pytest.mark.parametrize("shapes", [[(130, 260)] * 5, [(260, 130)] * 5, [(300, 200), (200, 300), (300, 200), (129, 129), (576, 192)], [(40, 24)] * 5])
+def test_a_matrix_that_is_not_finite_leaves_the_others_alone(shapes):
+    opt = context(1, shapes)
+    u = matrices(1, shapes, 14)
+    out = [[torch.empty(s, device="cuda") for s in shapes]]
+    opt.orthogonalize(range(5), u, out=out)
+    was = [t.clone() for t in out[0]]
+    u[0][1][3, 5] = math.nan
+    u[0][3][-1, -1] = -math.inf
+    opt.orthogonalize(range(5), u, out=out)
+    assert all(torch.equal(out[0][k], was[k]) for k in (0, 2, 4))
+    assert not any(bool(torch.isfinite(out[0][k]).all()) for k in (1, 3))
+    u[0][1].zero_()
+    opt.orthogonalize(range(5), u, out=out)
+    assert all(torch.equal(out[0][k], was[k]) for k in (0, 2, 4)) and bool((out[0][1] == 0).all())
+
+
+@pytest.mark.parametrize("tall", [True, False])
+def test_orthogonalize_beyond_32_bits(tall):
+    """2.2e9 elements: rows at both ends against the definition, of which the square matrices are small."""
+    long, short = (1 << 20) - 3, 2056
+    shape = (long, short) if tall else (short, long)
+    opt = context(1, [shape])
+    g = gen_of(15)
+    u = [[torch.randn(shape, generator=g, device="cuda", dtype=BF)]]
+    out = [[torch.empty(shape, device="cuda", dtype=BF)]]
+    opt.orthogonalize([0], u, out=out, steps=2)
+    x = u[0][0] if tall else u[0][0].mT
+    gram = sum(p.double().mT @ p.double() for p in x.split(1 << 16))
+    norm = gram.diagonal().sum().sqrt() + 1e-7
+    gram, product, (a, b, c) = gram / norm ** 2, torch.eye(short, dtype=torch.float64, device="cuda"), DEFAULT[0]
+    for _ in range(2):
+        p = a * torch.eye(short, dtype=torch.float64, device="cuda") + b * gram + c * gram @ gram
+        product, gram = product @ p, p @ gram @ p
+    got = out[0][0] if tall else out[0][0].mT
+    for rows in (slice(0, 100), slice(-100, None)):
+        # fp16 operands are off by 2^-11, of X, of the polynomial twice a step (its square, itself), and bf16's half step: 2^-7 of the norm is above all of them together
+        close(got[rows], x[rows].double() / norm @ product, 2.0 ** -7 * float(torch.linalg.matrix_norm(x[rows].double() / norm @ product)))
+
+
 def test_in_place_and_flat_tensors():
     M, shape = 2, (48, 100)
     flat = [[t.view(-1) for t in row] for row in matrices(M, [shape], 3)]
@@ -460,7 +547,7 @@ def test_orthogonal_refusals():
                         (ValueError, lambda: opt.orthogonalize([0], u, out=[[t.mT for t in row[:2]] + row[2:] for row in out])),
                         (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, columns=[7])), (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, steps=0)),
                         (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, steps=33)), (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, eps=-1.0)),
-                        (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, coefficients=[(17.0, 0.0, 0.0)])),
+                        (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, coefficients=[(30.0, -30.0, 0.1)])),
                         (d.DeslocError, lambda: opt.orthogonalize([0], u, out=out, coefficients=[(math.nan, 0.0, 0.0)])),
                         (d.DeslocError, lambda: opt.orthogonal_step([0], math.inf)),
                         (d.DeslocError, lambda: opt.orthogonalize([0, 1], u, out=[[row[0], row[0], row[2]] for row in out])),
