@@ -125,7 +125,7 @@ struct StoreEpilogue {
 
 // ---- backward ----------------------------------------------------------------------------------------
 // From dz = dy down: z = silu(g) u again, du = dz silu(g), dg = dz u (s + silu(g) (1 - s)) with s the sigmoid of g.  Bound: at short k what comes and goes by element, 10 bytes each; 4 x 8192
-// tokens, 576 x 1536: 170 us, 3 TB/s of those; 4 x 2048, 2048 x 8192: 300 us for 275 GFLOP.
+// tokens, 576 x 1536: 150 us, 3.4 TB/s of those; 4 x 2048, 2048 x 8192: 300 .. 340 us for 275 GFLOP.
 struct DzEpilogue {
     static constexpr int STAGING = 3 * 2048;
     static constexpr bool READS_BOXES = false, WRITES_BOXES = true;

@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(ORTH_THREADS, 4) orth_scale_kernel(const __gri
 }
 
 // ---- the products' epilogues -------------------------------------------------------------------------
-// Bound: bringing operands and emptying accumulators, nearly alike: 840 matrices of 192 .. 1536 x 576, k as G's is the longer side and of G^2 the shorter one, 4.2 ms of ten such products each
+// Bound: bringing operands and emptying accumulators, nearly alike: 840 matrices of 192 .. 1536 x 576, k as G's is the longer side and of G^2 the shorter one, 4.1 ms of ten such products each
 // (1.75 TFLOP, half of them counted).
 // A symmetric result: alpha times the sums, plus b times in[0], plus `diagonal` there; pieces below the diagonal go to the other one's place, too.
 struct SymEpilogue {
@@ -254,7 +254,7 @@ struct SymEpilogue {
 };
 
 // X of the next step: alpha times the sums (with a X's larger part in them) and `lo` times its smaller part; in two halves.
-// Bound: as above; the same 840 matrices 3.3 ms of four such products each (2.4 TFLOP), 3.4 without boxes.
+// Bound: as above; the same 840 matrices 3.15 ms of four such products each (2.4 TFLOP), 3.3 without boxes.
 struct NextEpilogue {
     static constexpr int STAGING = 3 * 2048;
     static constexpr bool READS_BOXES = true, WRITES_BOXES = true;
