@@ -394,7 +394,6 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     char *const ring = gemm_smem + pad;
     const int own_n = a.tile_n / CG, stage_bytes = a.a_bytes + (own_n + 63) / 64 * 64 * (GEMM_BK * 2);
     const int tile0 = blockIdx.x / CG, tile_step = gridDim.x / CG;
-    begin_and_let_next_begin();
     if (threadIdx.x == 0) {
         requested = failed = 0;
         for (int s = 0; s < a.stages; ++s) bar_init(&full[s], 1), bar_init(&empty[s], 1);
@@ -432,6 +431,9 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();
     tmem_fence_after();
+    // (Only now: the next kernel's blocks may take TMEM and wait for this one's end.  Where one of those could come first on an SM that a block of this kernel has begun on, either would
+    // wait for the other.)
+    begin_and_let_next_begin();
     const uint32_t tmem = tmem_at;
     const auto give_up = [&] {
         if (a.err) *reinterpret_cast<volatile int *>(a.err) = 1;

@@ -84,7 +84,6 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     __shared__ __align__(8) uint64_t done;
     __shared__ uint32_t tmem_at;
     __shared__ double sums[SMALL_THREADS / 32];
-    begin_and_let_next_begin();
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x, which = blockIdx.x;
     const uint32_t pad = (1024 - (smem_u32(small_smem) & 1023)) & 1023;
     const SmallPlan p(a.rows[which], a.cols[which]);
@@ -102,6 +101,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
+    begin_and_let_next_begin();   // (not before this block has its TMEM: the next kernel's may take all of an SM's and wait for this one's end)
     const uint32_t tmem = tmem_at;
     wait_for_earlier_kernels();
 

@@ -1,0 +1,38 @@
+"""Products of the workers' matrices next to one another and to other work: calls in a row, lists that fill launches and rounds, every element of the results."""
+import pytest
+import torch
+
+import paper_2505_22549_b200 as d
+from paper_2505_22549_b200 import binding as B
+import test_matrices_gpu as base
+
+pytestmark = pytest.mark.gpu
+
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def test_small_matrices_and_the_block_in_turn():
+    """Blocks that take some of an SM's TMEM and little shared memory next to those of a kernel that takes all of it, each kernel beginning while the one in front still runs."""
+    shapes = [(8, 8), (16, 24), (72, 72)]
+    opt = base.context(3, shapes)
+    u = base.matrices(3, shapes, 1)
+    out = [[torch.empty(s, device="cuda") for s in shapes] for _ in range(3)]
+    blocks = [base.Block(2, 300, 64, 512), base.Block(1, 8, 40, 72), base.Block(2, 1024, 512, 1024)]
+    opt.orthogonalize(range(3), u, out=out)
+    wants = [t.clone() for row in out for t in row], [b.opt.gated_ffn(b.TENSORS, b.h, b.weights).clone() for b in blocks]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.current_stream(), torch.cuda.Stream()]
+    for t in (t for row in out for t in row):
+        t.zero_()
+    torch.cuda.synchronize()
+    ys = []
+    for _ in range(30):
+        for k, b in enumerate(blocks):
+            opt.orthogonalize(range(3), u, out=out)
+            with torch.cuda.stream(streams[1]):
+                other = b.opt.gated_ffn(b.TENSORS, b.h, b.weights)
+            ys.append((k, b.opt.gated_ffn(b.TENSORS, b.h, b.weights)))
+            ys.append((k, other))
+    torch.cuda.synchronize()
+    assert all(torch.equal(y, wants[1][k]) for k, y in ys)
+    assert all(torch.equal(t, w) for t, w in zip((t for row in out for t in row), wants[0]))
