@@ -426,14 +426,14 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" :: "r"(smem_u32(&tmem_at)) : "memory");
             asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
         }
+        // (Only now: the next kernel's blocks may take TMEM and wait for this one's end.  Where one of those could come first on an SM that a block of this kernel has begun on, either would
+        // wait for the other.)
+        begin_and_let_next_begin();
     }
     tmem_fence_before();
     __syncthreads();
     if constexpr (CG == 2) cluster_sync();
     tmem_fence_after();
-    // (Only now: the next kernel's blocks may take TMEM and wait for this one's end.  Where one of those could come first on an SM that a block of this kernel has begun on, either would
-    // wait for the other.)
-    begin_and_let_next_begin();
     const uint32_t tmem = tmem_at;
     const auto give_up = [&] {
         if (a.err) *reinterpret_cast<volatile int *>(a.err) = 1;

@@ -96,12 +96,12 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 256;" :: "r"(smem_u32(&tmem_at)) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        begin_and_let_next_begin();   // (not before this block has its TMEM: the next kernel's may take all of an SM's and wait for this one's end)
     }
     for (int i = tid * 16; i < 2 * p.x_bytes() + 2 * p.g_bytes(); i += SMALL_THREADS * 16) *reinterpret_cast<uint4 *>(x + i) = make_uint4(0, 0, 0, 0);
     tmem_fence_before();
     __syncthreads();
     tmem_fence_after();
-    begin_and_let_next_begin();   // (not before this block has its TMEM: the next kernel's may take all of an SM's and wait for this one's end)
     const uint32_t tmem = tmem_at;
     wait_for_earlier_kernels();
 
