@@ -503,6 +503,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
             int s = 0, buf = 0;
             uint32_t phase = 0, turn = 0;
             bool ok = true;
+            wait_for_earlier_kernels();   // (nothing is asked for before: what earlier kernels take is no part of the wait below, whose polls are counted)
             for (int tile = tile0; ok && tile < a.tiles; tile += tile_step) {
                 const GemmGroup &g = at.find<CG>(a, tile);
                 const int steps = (g.k + GEMM_BK - 1) / GEMM_BK * a.segments;

@@ -36,3 +36,23 @@ def test_small_matrices_and_the_block_in_turn():
     torch.cuda.synchronize()
     assert all(torch.equal(y, wants[1][k]) for k, y in ys)
     assert all(torch.equal(t, w) for t, w in zip((t for row in out for t in row), wants[0]))
+
+
+@pytest.mark.parametrize("tokens,width,hidden", [(8, 40, 72), (300, 512, 640)])
+def test_polls_are_not_spent_on_earlier_kernels(tokens, width, hidden):
+    """A kernel that began while one in front of it has 32 steps of a small matrix to go, 700 us or 400 polls: its own waits are a few microseconds, and only those count."""
+    shape = (128, 500)
+    long, b = base.context(1, [shape]), base.Block(2, tokens, width, hidden)
+    u, out = base.matrices(1, [shape]), [[torch.empty(shape, device="cuda")]]
+    steps = [(1.5, -0.5, 0.0)] * 32
+    want = b.opt.gated_ffn(b.TENSORS, b.h, b.weights).clone()
+    long.orthogonalize([0], u, out=out, coefficients=steps)
+    torch.cuda.synchronize()
+    B.desloc_testing_set_wait_limit(b.opt.ctx, 128)
+    for _ in range(3):
+        long.orthogonalize([0], u, out=out, coefficients=steps)
+        y = b.opt.gated_ffn(b.TENSORS, b.h, b.weights)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want)
+    b.opt.gated_ffn(b.TENSORS, b.h, b.weights)     # (refused where a wait had run out)
+    torch.cuda.synchronize()
