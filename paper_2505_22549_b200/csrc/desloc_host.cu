@@ -89,6 +89,7 @@ struct WorkerRes {
     std::vector<int64_t> heads;          // [num_tensors] elements of the short first chunk
     std::vector<HostGroup> groups;
     void **d_tables = nullptr;  // [3][nptr] x, u, v
+    std::vector<void *> tables; // the same on the host
     Slot slots[kSlots];
     void **h_slots = nullptr;   // the slots' tables, pinned, and
     void **d_slots = nullptr;   // on the device
@@ -193,15 +194,15 @@ cudaError_t make_worker_res(WorkerRes &r, const desloc_config &cfg, int M, const
     r.d_diag_parts = reinterpret_cast<int *>(r.d_tstart + num_tensors + 1);
 
     const int64_t nptr = static_cast<int64_t>(M) * num_tensors;
-    std::vector<void *> tables(static_cast<size_t>(3 * nptr), nullptr);
+    r.tables.assign(static_cast<size_t>(3 * nptr), nullptr);
     for (int64_t i = 0; i < nptr; ++i) {
-        tables[i] = x[i];
-        tables[nptr + i] = u[i];
-        tables[2 * nptr + i] = has_v ? static_cast<void *>(v[i]) : nullptr;
+        r.tables[i] = x[i];
+        r.tables[nptr + i] = u[i];
+        r.tables[2 * nptr + i] = has_v ? static_cast<void *>(v[i]) : nullptr;
     }
-    cudaError_t e = cudaMalloc(&r.d_tables, tables.size() * sizeof(void *));
+    cudaError_t e = cudaMalloc(&r.d_tables, r.tables.size() * sizeof(void *));
     if (e == cudaSuccess)
-        e = cudaMemcpy(r.d_tables, tables.data(), tables.size() * sizeof(void *), cudaMemcpyHostToDevice);
+        e = cudaMemcpy(r.d_tables, r.tables.data(), r.tables.size() * sizeof(void *), cudaMemcpyHostToDevice);
     const size_t npart = static_cast<size_t>(2) * M * static_cast<size_t>(desloc::reduce_row(nrchunks));
     if (e == cudaSuccess) e = cudaMalloc(&r.d_partial, npart * sizeof(float));
     if (e == cudaSuccess) e = cudaMalloc(&r.d_norms, static_cast<size_t>(2) * M * sizeof(float));
@@ -750,6 +751,22 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
     return DESLOC_OK;
 }
 
+// Whether results (in x.out) share bytes with one another or with a matrix that is read, but for the one at their own place.  Host vectors: throws std::bad_alloc.
+bool shares_what_it_reads(const desloc_ctx *ctx, const desloc_orthogonal &how, const desloc::OrthArgs &a, const std::vector<desloc::OrthMatrix> &list, uintptr_t out_size) {
+    if (list.empty()) return false;
+    std::vector<int64_t> numel;
+    std::vector<const void *> from, ahead;
+    std::vector<void *> to;
+    for (const desloc::OrthMatrix &x : list) {
+        numel.push_back(static_cast<int64_t>(x.rows) * x.cols);
+        from.push_back(how.updates ? x.update : ctx->res.tables[ctx->nptr + x.index]);
+        ahead.push_back(x.grad), to.push_back(x.out);
+    }
+    const int n = static_cast<int>(list.size());
+    return share_memory(numel.data(), n, 1, from.data(), a.update_bf16 ? 2 : 4, to.data(), out_size) ||
+           (how.grads && share_memory(numel.data(), n, 1, ahead.data(), a.grad_bf16 ? 2 : 4, to.data(), out_size));
+}
+
 int run_orthogonal(desloc_ctx *ctx, const desloc::OrthArgs &a, void *work, int64_t work_bytes, void *stream) {
     if (a.count == 0) return DESLOC_OK;
     if (!work) return DESLOC_E_NULL;
@@ -1242,20 +1259,11 @@ int desloc_orthogonalize(desloc_ctx *ctx, const desloc_orthogonal *how, int32_t 
         if (rc != DESLOC_OK) return rc;
         a.out_bf16 = out_dtype == DESLOC_BF16;
         const uintptr_t osz = a.out_bf16 ? 2 : 4;
-        std::vector<int64_t> numel;
-        std::vector<const void *> from, ahead;
-        std::vector<void *> to;
         for (desloc::OrthMatrix &x : list) {
             if (!(x.out = out[x.index])) return DESLOC_E_NULL;
             if (reinterpret_cast<uintptr_t>(x.out) % osz) return DESLOC_E_INVALID;
-            numel.push_back(static_cast<int64_t>(x.rows) * x.cols);
-            from.push_back(x.update), ahead.push_back(x.grad), to.push_back(x.out);
         }
-        const int n = static_cast<int>(list.size());
-        if (n > 0 && (share_memory(numel.data(), n, 1, how->updates ? from.data() : const_cast<const void *const *>(to.data()), how->updates ? (a.update_bf16 ? 2 : 4) : osz,
-                                   to.data(), osz) ||
-                      (how->grads && share_memory(numel.data(), n, 1, ahead.data(), a.grad_bf16 ? 2 : 4, to.data(), osz))))
-            return DESLOC_E_INVALID;
+        if (shares_what_it_reads(ctx, *how, a, list, osz)) return DESLOC_E_INVALID;
         return run_orthogonal(ctx, a, work, work_bytes, stream);
     } catch (const std::bad_alloc &) {
         return DESLOC_E_NOMEM;

@@ -56,3 +56,26 @@ def test_polls_are_not_spent_on_earlier_kernels(tokens, width, hidden):
         assert torch.equal(y, want)
     b.opt.gated_ffn(b.TENSORS, b.h, b.weights)     # (refused where a wait had run out)
     torch.cuda.synchronize()
+
+
+# ---- what shares memory ------------------------------------------------------------------------------
+def addresses(lists):
+    return B.ptr_array([t.data_ptr() for row in lists for t in row])
+
+
+def test_results_over_the_contexts_momentum_are_refused_at_the_entry():
+    """updates NULL, the context's u: a result at the place of another matrix's u, or of another type at its own.  (No working memory: no call gets as far as a launch.)"""
+    shapes = [(16, 24), (16, 24), (130, 200)]
+    u = base.matrices(2, shapes, 1)
+    opt = base.context(2, shapes, u=u)
+    how = B.orthogonal([0, 1, 2], [24, 24, 200])
+    go = lambda out, dtype=d.DESLOC_F32: B.raw_lib().desloc_orthogonalize(opt.ctx, how, dtype, addresses(out), None, 0, None)
+    fresh = base.matrices(2, shapes, 2)
+    assert go(fresh) == d.DESLOC_E_NULL and go(u) == d.DESLOC_E_NULL      # apart; each in place
+    swapped = [[u[0][1], u[0][0], u[0][2]], u[1]]
+    workers = [[u[1][0], *u[0][1:]], [u[0][0], *u[1][1:]]]
+    behind = [[fresh[0][0], u[0][2].view(-1)[4:4 + 384], fresh[0][2]], fresh[1]]
+    for out in (swapped, workers, behind):
+        assert go(out) == d.DESLOC_E_INVALID
+    assert go(u, d.DESLOC_BF16) == d.DESLOC_E_INVALID
+    assert B.raw_lib().desloc_orthogonalize(opt.ctx, B.orthogonal([0], [24]), d.DESLOC_F32, addresses(behind), None, 0, None) == d.DESLOC_E_NULL   # (what is not read may be written)
