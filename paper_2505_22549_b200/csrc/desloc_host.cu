@@ -751,7 +751,7 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
     return DESLOC_OK;
 }
 
-// Whether results (in x.out) share bytes with one another or with a matrix that is read, but for the one at their own place.  Host vectors: throws std::bad_alloc.
+// Whether what is written (x.out, or the context's x) shares bytes with itself or with another matrix that is read.  Host vectors: throws std::bad_alloc.
 bool shares_what_it_reads(const desloc_ctx *ctx, const desloc_orthogonal &how, const desloc::OrthArgs &a, const std::vector<desloc::OrthMatrix> &list, uintptr_t out_size) {
     if (list.empty()) return false;
     std::vector<int64_t> numel;
@@ -760,7 +760,7 @@ bool shares_what_it_reads(const desloc_ctx *ctx, const desloc_orthogonal &how, c
     for (const desloc::OrthMatrix &x : list) {
         numel.push_back(static_cast<int64_t>(x.rows) * x.cols);
         from.push_back(how.updates ? x.update : ctx->res.tables[ctx->nptr + x.index]);
-        ahead.push_back(x.grad), to.push_back(x.out);
+        ahead.push_back(x.grad), to.push_back(x.out ? x.out : ctx->res.tables[x.index]);
     }
     const int n = static_cast<int>(list.size());
     return share_memory(numel.data(), n, 1, from.data(), a.update_bf16 ? 2 : 4, to.data(), out_size) ||
@@ -1280,6 +1280,7 @@ int desloc_orthogonal_step(desloc_ctx *ctx, const desloc_orthogonal *how, float 
         desloc::OrthArgs a{};
         const int rc = check_orthogonal(ctx, *how, true, list, coefficients, a);
         if (rc != DESLOC_OK) return rc;
+        if ((how->updates || how->grads) && shares_what_it_reads(ctx, *how, a, list, 4)) return DESLOC_E_INVALID;
         a.lr = lr, a.decay = static_cast<float>(1.0 - static_cast<double>(lr) * ctx->cfg.weight_decay);
         return run_orthogonal(ctx, a, work, work_bytes, stream);
     } catch (const std::bad_alloc &) {

@@ -79,3 +79,36 @@ def test_results_over_the_contexts_momentum_are_refused_at_the_entry():
         assert go(out) == d.DESLOC_E_INVALID
     assert go(u, d.DESLOC_BF16) == d.DESLOC_E_INVALID
     assert B.raw_lib().desloc_orthogonalize(opt.ctx, B.orthogonal([0], [24]), d.DESLOC_F32, addresses(behind), None, 0, None) == d.DESLOC_E_NULL   # (what is not read may be written)
+
+
+def test_a_step_along_what_lies_in_another_matrix_is_refused():
+    """At the entry without working memory, so that no call gets as far as a launch; then from Python, what is fine."""
+    shapes = [(16, 24), (16, 24), (130, 200)]
+    x, fresh = base.matrices(2, shapes, 1), base.matrices(2, shapes, 2)
+    opt = base.context(2, shapes, x=x, grad_dtype="f32")
+    bf = B.DESLOC_BF16
+
+    def go(updates=None, grads=None, dtype=d.DESLOC_F32):
+        how = B.orthogonal([0, 1, 2], [24, 24, 200], updates_dtype=dtype, updates=addresses(updates) if updates else None, grads=addresses(grads) if grads else None)
+        return B.raw_lib().desloc_orthogonal_step(opt.ctx, how, 0.1, None, 0, None)
+
+    swapped = [[x[0][1], x[0][0], x[0][2]], x[1]]
+    workers = [[x[1][0], *x[0][1:]], [x[0][0], *x[1][1:]]]
+    behind = [[fresh[0][0], x[0][2].view(-1)[4:4 + 384], fresh[0][2]], fresh[1]]
+    for lists in (swapped, workers, behind):
+        assert go(updates=lists) == d.DESLOC_E_INVALID and go(grads=lists) == d.DESLOC_E_INVALID and go(updates=fresh, grads=lists) == d.DESLOC_E_INVALID
+    assert go(updates=x, dtype=bf) == d.DESLOC_E_INVALID
+    for lists in (x, fresh):
+        assert go(updates=lists) == d.DESLOC_E_NULL and go(grads=lists) == d.DESLOC_E_NULL
+    assert go() == d.DESLOC_E_NULL
+
+
+def test_a_step_along_the_weights_themselves():
+    shapes = [(16, 24), (130, 200)]
+    x = base.matrices(1, shapes, 1)
+    opt = base.context(1, shapes, x=x)
+    before = [t.double() for t in x[0]]
+    opt.orthogonal_step([0, 1], 1e-4, updates=x, scale="none")
+    for t, was in zip(x[0], before):
+        want, off = base.allowed(was)
+        base.close(t, was - float(torch.tensor(1e-4)) * want, 1e-4 * off + 4 * base.U * float(was.norm() + 1e-4 * want.norm()))
