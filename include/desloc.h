@@ -524,7 +524,9 @@ typedef struct {
     int32_t scale;              /* desloc_scale_t */
     int32_t updates_dtype;
     const void *const *updates; /* host array of M*num_tensors DEVICE pointers, only those of `tensors` are read; NULL: the context's u (fp32) */
-    const void *const *grads;   /* NULL, or the same of gradients in cfg.grad_dtype: U is then the look-ahead beta1 update + (1 - beta1) grad */
+    const void *const *grads;   /* NULL, or the same of gradients in cfg.grad_dtype: U is then the look-ahead beta1 update + (1 - beta1) grad, each coordinate of grad
+                                   clipped at cfg.clip_rho as desloc_step() clips it (but NaN stays).  Behind desloc_step_normclip() or desloc_step_diag() with max_norm
+                                   the factors are the caller's to apply: desloc_clip_grads() in front of desloc_step() instead, whose gradients both calls then take */
 } desloc_orthogonal;
 
 /*

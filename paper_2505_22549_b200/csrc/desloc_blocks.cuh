@@ -39,12 +39,18 @@ struct OrthArgs {
     OrthMatrix *list;            // sorted in place
     int count, steps;
     const float *coefficients;   // [steps][3]
-    float eps, beta;             // beta: of the look-ahead beta * update + (1 - beta) * grad
+    float eps, beta, rho;        // of the look-ahead beta * update + (1 - beta) * grad, grad clipped to +-rho (infinity: not at all)
     bool update_bf16, grad_bf16, out_bf16;
     float *const *u_table, *const *x_table;   // on the device
     int scale;                   // desloc_scale_t
     float lr, decay;             // of the step: x := decay * x - lr * scale * result
 };
+// A gradient as the step has it in the momentum: sgn(g) min(|g|, rho).  (NaN stays NaN, so that the result shows it.)
+__device__ __forceinline__ float clipped(float g, float rho) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;\n min.NaN.f32 %0, %0, %3;" : "=&f"(r) : "f"(g), "f"(-rho), "f"(rho));
+    return r;
+}
 // Whether a matrix is taken by a block of its own, and the launch of such ones: list[first, first + count).
 bool orth_is_small(int rows, int cols);
 cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, int *err, int wait_limit, cudaStream_t stream, int *launches);

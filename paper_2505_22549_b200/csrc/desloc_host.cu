@@ -746,6 +746,7 @@ int check_orthogonal(const desloc_ctx *ctx, const desloc_orthogonal &how, bool a
     a.list = list.data(), a.count = static_cast<int>(list.size()), a.steps = how.steps;
     a.coefficients = coefficients.data();
     a.eps = how.eps, a.beta = c.beta1, a.scale = how.scale;
+    a.rho = c.clip_rho > 0.f ? c.clip_rho : std::numeric_limits<float>::infinity();
     a.u_table = reinterpret_cast<float *const *>(ctx->res.d_tables + ctx->nptr);
     a.x_table = reinterpret_cast<float *const *>(ctx->res.d_tables);
     return DESLOC_OK;

@@ -33,7 +33,7 @@ struct Sources {
     float *const *table;
     double *partial;                  // [matrices][most]
     int most;
-    float beta, eps;
+    float beta, eps, rho;
 };
 
 // N values as they lie in memory: they wait in as few registers as they can, since how many are on their way is what the bandwidth comes from.
@@ -73,7 +73,7 @@ template <typename UT, typename GT, typename F>
 __device__ __forceinline__ void visit(const Sources &s, int which, long long first, int count, const F &f) {
     const UT *const u = static_cast<const UT *>(s.update[which] ? s.update[which] : s.table[s.index[which]]) + first;
     const GT *const g = s.grad[which] ? static_cast<const GT *>(s.grad[which]) + first : nullptr;
-    const float beta = s.beta, rest = 1.f - s.beta;
+    const float beta = s.beta, rest = 1.f - s.beta, rho = s.rho;
     const auto go = [&](auto width, auto ahead) {
         constexpr int N = decltype(width)::value, STEP = ORTH_THREADS * N;
         constexpr bool WITH = decltype(ahead)::value;   // with gradients
@@ -98,7 +98,7 @@ __device__ __forceinline__ void visit(const Sources &s, int which, long long fir
                     float w[N];
                     y[e].values(w);
 #pragma unroll
-                    for (int k = 0; k < N; ++k) v[k] = beta * v[k] + rest * w[k];
+                    for (int k = 0; k < N; ++k) v[k] = beta * v[k] + rest * clipped(w[k], rho);
                 }
                 f(at + e * STEP, v);
             }
@@ -582,7 +582,7 @@ cudaError_t launch_orth(const OrthArgs &a, char *work, int *err, int wait_limit,
     for (int at = small; at < a.count;) {
         Round r = next_round(a, at);
         place(r, work, &s.partial, &s.most);
-        s.table = a.u_table, s.beta = a.beta, s.eps = a.eps;
+        s.table = a.u_table, s.beta = a.beta, s.eps = a.eps, s.rho = a.rho;
         for (int i = 0; i < r.nshapes; ++i) {
             const Shape &sh = r.shapes[i];
             s.shapes[i] = {sh.rows, sh.cols, static_cast<int>(sh.ld), block_rows(sh.cols), sh.hi[0], sh.lo};

@@ -24,7 +24,7 @@ struct SmallArgs {
     float scale[SMALL_MOST];
     float coefficients[DESLOC_MAX_NEWTON_SCHULZ][3];
     int steps;
-    float beta, eps, decay;
+    float beta, eps, rho, decay;
     int update_bf16, grad_bf16, out_bf16;
     float *const *u_table, *const *x_table;
     int *err;
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
     const void *const gr = a.grad[which];
     const int cols = a.cols[which], count = a.rows[which] * cols;
     const bool tall = a.rows[which] > cols;
-    const float beta = a.beta, rest = 1.f - a.beta;
+    const float beta = a.beta, rest = 1.f - a.beta, rho = a.rho;
     // Eight times N neighbouring elements a thread, all of them on their way at once; N = 4 where rows allow it.
     constexpr int AHEAD = 8;
     const auto go = [&](auto width) {
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(SMALL_THREADS) orth_small_kernel(const __grid_
                     else load_values(static_cast<const float *>(gr) + i, w);
                 }
 #pragma unroll
-                for (int k = 0; k < N; ++k) v[e][k] = beta * v[e][k] + rest * w[k];
+                for (int k = 0; k < N; ++k) v[e][k] = beta * v[e][k] + rest * clipped(w[k], rho);
             }
         };
         constexpr int EACH = AHEAD * SMALL_THREADS * N;
@@ -326,7 +326,7 @@ cudaError_t launch_orth_small(const OrthArgs &a, int first, int count, int *err,
             bytes = std::max(bytes, SmallPlan(m.rows, m.cols).bytes());
         }
         std::memcpy(s.coefficients, a.coefficients, sizeof(float) * 3 * a.steps);
-        s.steps = a.steps, s.beta = a.beta, s.eps = a.eps, s.decay = a.decay;
+        s.steps = a.steps, s.beta = a.beta, s.eps = a.eps, s.rho = a.rho, s.decay = a.decay;
         s.update_bf16 = a.update_bf16, s.grad_bf16 = a.grad_bf16, s.out_bf16 = a.out_bf16;
         s.u_table = a.u_table, s.x_table = a.x_table, s.err = err, s.wait_limit = wait_limit;
         cudaLaunchConfig_t lc{};

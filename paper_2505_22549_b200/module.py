@@ -474,7 +474,8 @@ class DesLoc:
     def orthogonalize(self, tensors, updates, grads=None, out=None, columns=None, steps: int = 5, coefficients=None, eps: float = 1e-7,
                       scale: str = "none") -> None:
         """Every worker's matrices `tensors` (numbers) of `updates` (nested lists like x, fp32 or bf16; None: the momentum u) brought to singular values near 1 by `steps`
-        Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad.  columns: of each matrix,
+        Newton-Schulz products, into `out` (the same, either type) or in place.  grads: of the look-ahead beta1 update + (1 - beta1) grad, grad
+        clipped at clip_rho as step() clips it (norm-based clipping is clip_grads()', in front of step() and this).  columns: of each matrix,
         where x has other shapes than [rows, columns].  coefficients: triples (a, b, c), one a step, in place of the default ones; magnitudes sum to 60 at most.  scale: "none", "aspect"
         (sqrt(max(1, rows / columns))) or "rms" (0.2 sqrt(max(rows, columns)))."""
         tensors = tuple(tensors)

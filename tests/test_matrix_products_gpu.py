@@ -112,3 +112,53 @@ def test_a_step_along_the_weights_themselves():
     for t, was in zip(x[0], before):
         want, off = base.allowed(was)
         base.close(t, was - float(torch.tensor(1e-4)) * want, 1e-4 * off + 4 * base.U * float(was.norm() + 1e-4 * want.norm()))
+
+
+# ---- the look-ahead ----------------------------------------------------------------------------------
+@pytest.mark.parametrize("grad_dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("src", ["bf16", "f32"])
+def test_look_ahead_of_clipped_gradients(grad_dtype, src):
+    """Of gradients of which a third lie beyond the clip radius, for matrices that a block takes alone and others."""
+    shapes, rho = [(24, 60), (23, 61), (300, 200), (200, 301), (576, 192), (131, 130)], 1e-4
+    opt = base.context(2, shapes, grad_dtype, beta1=0.9, clip_rho=rho)
+    u, g = base.matrices(2, shapes, 1, base.TYPE[src]), base.matrices(2, shapes, 2, base.TYPE[grad_dtype])
+    out = [[torch.empty(s, device="cuda") for s in shapes] for _ in range(2)]
+    opt.orthogonalize(range(len(shapes)), u, grads=g, out=out)
+    beta, bound = float(torch.tensor(0.9)), float(torch.tensor(rho))
+    for m in range(2):
+        for k in range(len(shapes)):
+            ahead = beta * u[m][k].double() + (1 - beta) * g[m][k].double().clamp(-bound, bound)
+            want, off = base.allowed(ahead)
+            # (the look-ahead is formed in fp32: three roundings of it, which no product enlarges by more than 3.5^5)
+            base.close(out[m][k], want, off + 3 * base.U * 3.5 ** 5 * float(want.norm()))
+    g[1][2][5, 7] = float("nan")
+    g[1][0][3, 2] = float("nan")
+    g[0][0][3, 2] = float("inf")       # (clipped as any other)
+    opt.orthogonalize(range(len(shapes)), u, grads=g, out=out)
+    assert not bool(torch.isfinite(out[1][2]).all()) and not bool(torch.isfinite(out[1][0]).all()) and bool(torch.isfinite(out[0][0]).all())
+
+
+def test_a_step_with_clipping_in_both_halves():
+    """step() at rate 0 and orthogonal_step() of the same gradients, in a context that clips coordinates: momentum and look-ahead of the same clipped gradients."""
+    M, shapes, rho, lr = 3, [(40, 96), (300, 130), (7,)], 0.5, 0.01
+    g = base.gen_of(3)
+    x = [[torch.randn(s, generator=g, device="cuda") * 0.1 for s in shapes] for _ in range(M)]
+    opt = base.context(M, shapes, x=x, grad_dtype="f32", beta1=0.9, clip_rho=rho)
+    momentum = [[torch.zeros(s, dtype=torch.float64, device="cuda") for s in shapes] for _ in range(M)]
+    beta = float(torch.tensor(0.9))
+    for t in (1, 5):                     # (K = 2, 3, 4: nothing is averaged)
+        grads = [[torch.randn(s, generator=g, device="cuda") for s in shapes] for _ in range(M)]
+        before = [[w.double() for w in row] for row in x]
+        assert opt.step(t, 0.0, grads) == 0
+        opt.orthogonal_step([0, 1], lr, grads=grads, scale="none")
+        for m in range(M):
+            for k in range(3):
+                clipped = grads[m][k].double().clamp(-rho, rho)
+                momentum[m][k] = beta * momentum[m][k] + (1 - beta) * clipped
+                base.check(opt._keep[1][m][k], momentum[m][k], 8 * base.U * rho)
+                if k == 2:
+                    assert torch.equal(x[m][k].double(), before[m][k])
+                    continue
+                want, off = base.allowed(beta * momentum[m][k] + (1 - beta) * clipped)
+                rate = float(torch.tensor(lr))
+                base.close(x[m][k], before[m][k] - rate * want, rate * (off + 8 * base.U * 3.5 ** 5 * float(want.norm())) + 4 * base.U * float(before[m][k].norm()))
