@@ -539,6 +539,8 @@ DESLOC_API int desloc_orthogonalize(desloc_ctx *ctx, const desloc_orthogonal *ho
 /*
  * The step of every worker's x along them: x := x (1 - lr weight_decay) - lr * result, weight_decay from the configuration.  With u from desloc_step() of
  * an SGDM context at rate 0 (momentum and the averages of u and x, each on its period) in front, this is Algorithm 1 with orthogonalised momentum as OPT.
+ * That order is the one of averages in front of the update: with DESLOC_FLAG_POST_AVERAGE desloc_step() would have averaged x and u before x is moved, and updates = NULL is
+ * DESLOC_E_INVALID (unless there is one worker, or nothing is ever averaged); updates of the caller's own are taken.
  * lr must be finite.  updates[i], or grads[i], may be x[i] where the types are equal; DESLOC_E_INVALID where a matrix of them shares bytes with another one's x.
  */
 DESLOC_API int desloc_orthogonal_step(desloc_ctx *ctx, const desloc_orthogonal *how, float lr, void *work, int64_t work_bytes, void *stream);

@@ -1275,6 +1275,9 @@ int desloc_orthogonal_step(desloc_ctx *ctx, const desloc_orthogonal *how, float 
     desloc::NvtxRange range("desloc_orthogonal_step");
     if (!ctx || !how) return DESLOC_E_NULL;
     if (!std::isfinite(lr)) return DESLOC_E_RANGE;
+    // The momentum's step in a context that averages behind the update: desloc_step() has averaged x before this call moves it, and u before this call reads it.
+    const desloc_config &c = ctx->cfg;
+    if (!how->updates && (c.flags & DESLOC_FLAG_POST_AVERAGE) && c.M > 1 && (c.Kx > 0 || c.Ku > 0)) return DESLOC_E_INVALID;
     try {
         std::vector<desloc::OrthMatrix> list;
         std::vector<float> coefficients;

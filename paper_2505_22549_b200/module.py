@@ -500,7 +500,8 @@ class DesLoc:
     def orthogonal_step(self, tensors, lr: float, updates=None, grads=None, columns=None, steps: int = 5, coefficients=None, eps: float = 1e-7,
                         scale: str = "aspect") -> None:
         """x of the matrices `tensors` := x (1 - lr weight_decay) - lr * orthogonalize(updates; the momentum u where None).  Behind step(t, 0.0, grads) of an SGDM
-        context, which brings the momentum and the averages of this step, it is the step of the orthogonalised momentum; grads: its look-ahead."""
+        context, which brings the momentum and the averages of this step, it is the step of the orthogonalised momentum; grads: its look-ahead.  (Averages in front of the
+        update: where they come behind it, updates of None are refused.)"""
         tensors = tuple(tensors)
         if columns is None and coefficients is None and scale in _SCALES:
             r = _native.orthogonal(self.ctx, self._table, tensors, self._widths(), updates, grads, None, lr, steps, eps, _SCALES[scale], self.grad_dtype, self._keep[0],

@@ -162,3 +162,24 @@ def test_a_step_with_clipping_in_both_halves():
                 want, off = base.allowed(beta * momentum[m][k] + (1 - beta) * clipped)
                 rate = float(torch.tensor(lr))
                 base.close(x[m][k], before[m][k] - rate * want, rate * (off + 8 * base.U * 3.5 ** 5 * float(want.norm())) + 4 * base.U * float(before[m][k].norm()))
+
+
+def test_a_step_of_the_momentum_where_averages_come_behind_is_refused():
+    shapes = [(16, 24), (5,)]
+    def made(M, K):
+        zeros = lambda: [[torch.ones(s, device="cuda") for s in shapes] for _ in range(M)]
+        return d.DesLoc(zeros(), zeros(), None, opt="sgdm", grad_dtype="f32", K=K, flags=d.DESLOC_FLAG_POST_AVERAGE)
+    for K in ((2, 0, 0), (0, 3, 0), (2, 3, 4)):
+        opt = made(2, K)
+        for call in (lambda: opt.orthogonal_step([0], 0.1), lambda: opt.orthogonal_step([0], 0.1, grads=base.matrices(2, [(16, 24), (5, 1)], 1)),
+                     lambda: opt.orthogonal_step([0], 0.1, columns=[48])):
+            with pytest.raises(d.DeslocError) as e:
+                call()
+            assert e.value.status == d.DESLOC_E_INVALID
+        assert all(bool((t == 1).all()) for row in opt._keep[0] for t in row)
+        opt.orthogonal_step([0], 0.1, updates=base.matrices(2, [(16, 24), (5, 1)], 1))
+        assert not any(bool((row[0] == 1).all()) for row in opt._keep[0])
+    for M, K in ((1, (2, 3, 4)), (2, (0, 0, 4))):
+        opt = made(M, K)
+        opt.orthogonal_step([0], 0.1)
+        assert not any(bool((row[0] == 1).all()) for row in opt._keep[0])
