@@ -46,6 +46,7 @@ struct GemmGroup {
     int wide;                // bits: out (1) and in (2) rows can be moved 16 bytes at a time
     short in_map, out_map;   // boxes of 32 x 32 of what the epilogue reads and writes (out_map + k of out[k]), where the copy engine moves them; else -1
     int io_batch;            // of its first matrix in those maps
+    int rotate;              // every tile begins with another k
 };
 
 template <typename E>
@@ -59,7 +60,6 @@ struct GemmArgs {
     int dual;                // the tile's columns are two halves, of two B operands
     int symmetric;           // only tiles that reach the lower triangle, of a product of one operand with itself
     int row_first, row_rest, row_more, row_rest_more;   // of those: tiles in the first row of tiles and in each further one, by division with rest
-    int rotate;              // every tile begins with another k
     uint32_t idesc;          // without the operands' layouts
     int *err;
     int wait_limit;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                 if (first) wait_for_earlier_kernels(), first = false;
                 const int m0 = (at.i * CG + rank) * GEMM_BM, steps = (g.k + GEMM_BK - 1) / GEMM_BK;
                 const int n0 = a.dual ? at.j * (a.tile_n / 2) : at.j * a.tile_n + rank * own_n;
-                const int boxes = (own_n + 63) / 64, turned = a.rotate ? static_cast<int>(tile * 29u % steps) : 0;
+                const int boxes = (own_n + 63) / 64, turned = g.rotate ? static_cast<int>(tile * 29u % steps) : 0;
                 const bool once = at.diagonal<CG>(a);
                 const uint32_t bytes = ((g.a_mn ? GEMM_BM : g.a_rows) + (once ? 0 : g.b_mn ? 64 * boxes : own_n)) * (GEMM_BK * 2);
                 for (int kk = 0; kk < steps * a.segments; ++kk) {
@@ -459,7 +459,7 @@ __global__ void __launch_bounds__(GEMM_THREADS, 1) gemm_kernel(const __grid_cons
                     if (!ok) break;
                     int seg = 0, step = kk;
                     if (step >= steps) seg = 1, step -= steps;
-                    if (a.rotate) {
+                    if (turned > 0) {
                         step += turned;
                         if (step >= steps) step -= steps;
                     }
@@ -731,7 +731,7 @@ GemmCut pick_cut(bool dual, int64_t m, int64_t k, const F &tiles) {
 template <typename E>
 void begin_gemm(GemmArgs<E> &a, bool bf16, const GemmCut &cut, bool dual, bool symmetric, int segments) {
     a.ngroups = a.tiles = a.a_bytes = 0;
-    a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.rotate = 0, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
+    a.tile_n = cut.tile_n, a.pairs = cut.pairs, a.dual = dual, a.symmetric = symmetric, a.segments = segments;
     const int bm = GEMM_BM * (cut.pairs ? 2 : 1);
     a.row_first = (bm - 1) / cut.tile_n + 1, a.row_rest = (bm - 1) % cut.tile_n;
     a.row_more = bm / cut.tile_n, a.row_rest_more = bm % cut.tile_n;
@@ -753,7 +753,7 @@ GemmGroup &add_group(GemmArgs<E> &a, int m, int n, int k, int count) {
     a.tiles += g.per * count;
     // Few rows: all that is read is B, once, and all blocks at once would read the same columns of rows that lie a power of two apart, of which a few of the memory's channels
     // have to bring all (the 8192 columns of down, one row of h: 1.7 TB/s).
-    a.rotate = m <= FEW_ROWS;
+    g.rotate = m <= FEW_ROWS;
     return g;
 }
 

@@ -183,3 +183,16 @@ def test_a_step_of_the_momentum_where_averages_come_behind_is_refused():
         opt = made(M, K)
         opt.orthogonal_step([0], 0.1)
         assert not any(bool((row[0] == 1).all()) for row in opt._keep[0])
+
+
+@pytest.mark.parametrize("shape", [(300, 400), (400, 300), (576, 1536)])
+def test_a_matrix_beside_one_of_few_rows_keeps_its_bits(shape):
+    """Products of few rows begin with another k in every tile; what stands beside them in a launch does not."""
+    shapes = [shape, (5000, 60)]
+    opt = base.context(1, shapes)
+    u = base.matrices(1, shapes, 1)
+    out = [[torch.empty(s, device="cuda") for s in shapes]]
+    opt.orthogonalize([0], u, out=out)
+    alone = out[0][0].clone()
+    opt.orthogonalize([0, 1], u, out=out)
+    assert torch.equal(out[0][0], alone)
