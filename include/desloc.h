@@ -501,9 +501,11 @@ DESLOC_API int64_t desloc_gated_ffn_grad_bytes(const desloc_ctx *ctx, const desl
 /*
  * Orthogonalised updates: of matrices U [rows, columns], X_0 = U / (|U|_F + eps) and, for each of `steps` triples (a, b, c),
  *   X := a X + (b G + c G^2) X,  G = X X^T,
- * by which singular values of 1e-3 and more come near 1 (with the default triples, within 0.7 .. 1.2) and the singular vectors stay.  Products take fp16 operands with sums
- * in fp32, X itself is carried in 22 bits from step to step; the result is off by some 2e-3 of its norm.  A matrix of zeros stays one; one that holds
- * values that are not finite has results that are not, and no other matrix does.  Squares are fp32: values below 1e-22 count as 0 in the norm, beyond 1e18 as infinite.
+ * by which singular values come near 1 and the singular vectors stay: by the default triples those of 1.6e-3 and more of |U|_F within 0.68 .. 1.21 in five steps, smaller
+ * ones grow by 3.4445 a step at most (1e-3 to 0.47).  Products take fp16 operands with sums in fp32 (G and the polynomial are fp16, too; in matrices with a side of up to 128
+ * that a block takes alone, two fp16 numbers each), X itself is carried in 22 bits from step to step, in 11 into the last product; the result is off by some 2e-3 of
+ * its norm.  A matrix of zeros stays one; one that holds values that are not finite has results that are not, and no other matrix does.  The norm's squares are fp32: values
+ * below 1e-19 lose digits in it, those below 2e-23 count as 0; from 6e18 on it may be infinite, and the result is 0 then.
  */
 typedef enum {
     DESLOC_SCALE_NONE = 0,

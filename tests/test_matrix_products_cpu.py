@@ -3,7 +3,10 @@ import glob
 import os
 import re
 
-CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_22549_b200", "csrc")
+import numpy as np
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2505_22549_b200", "csrc")
 
 
 def kernels():
@@ -28,3 +31,23 @@ def test_no_kernel_lets_the_next_begin_before_its_blocks_have_their_tmem():
         assert body.count("begin_and_let_next_begin()") == 1
         begin = body.index("begin_and_let_next_begin()")
         assert body.rindex("tcgen05.alloc") < begin < body.index("wait_for_earlier_kernels()"), f"{name}: the next kernel may begin before this block has its TMEM"
+
+
+def test_where_the_header_says_that_singular_values_end():
+    """The default triples, five steps, in exact arithmetic up to 64 bits: the smallest singular value of the statement, its range, and what smaller ones grow by."""
+    text = " ".join(open(os.path.join(ROOT, "include", "desloc.h")).read().replace("\n *", " ").split())
+    first, low, high = map(float, re.search(r"those of (\S+) and more of \|U\|_F within (\S+) \.\. (\S+) in five steps", text).groups())
+    a, small, to = map(float, re.search(r"smaller ones grow by (\S+) a step at most \((\S+) to ([\d.]+)\)", text).groups())
+    host = open(os.path.join(CSRC, "desloc_host.cu")).read()
+    triple = [float(v) for v in re.search(r"kNewtonSchulz\[3\] = \{([^}]*)\}", host).group(1).replace("f", "").split(",")]
+
+    def after(s, steps=5):
+        for _ in range(steps):
+            s = s * (triple[0] + s ** 2 * (triple[1] + s ** 2 * triple[2]))
+        return s
+
+    ends = after(np.exp(np.linspace(np.log(first), 0.0, 1_000_001)))
+    assert low <= ends.min() < low + 0.01 and high - 0.01 < ends.max() <= high
+    assert after(0.95 * first) < after(first) and after(np.array(small)) == np.clip(after(np.array(small)), to - 0.005, to + 0.005)
+    below = np.exp(np.linspace(np.log(1e-7), np.log(first), 1001))
+    assert a == triple[0] and np.all(after(below) <= a ** 5 * below)

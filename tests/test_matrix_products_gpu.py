@@ -196,3 +196,19 @@ def test_a_matrix_beside_one_of_few_rows_keeps_its_bits(shape):
     alone = out[0][0].clone()
     opt.orthogonalize([0, 1], u, out=out)
     assert torch.equal(out[0][0], alone)
+
+
+@pytest.mark.parametrize("shape", [(40, 24), (200, 130)])
+def test_ends_of_the_norms_range(shape):
+    """Values whose squares are no normal numbers any more, down to those that count as 0, and beyond fp32's."""
+    opt = base.context(1, [shape])
+    u, out = base.matrices(1, [shape], 5), [[torch.empty(shape, device="cuda")]]
+    start = u[0][0] * 1e4
+    for far, eps in ((1e-19, 0.0), (1e-24, 1e-7), (1e20, 1e-7)):
+        u[0][0].copy_(start.clamp(-4, 4) * far)
+        opt.orthogonalize([0], u, out=out, eps=eps)
+        if far == 1e-19:
+            # (squares between 1e-45 and 2e-37, off by 2^-150 or 2^-24 of them: the norm by far less than the operands)
+            base.close(out[0][0], *base.allowed(u[0][0], eps=eps))
+        else:
+            assert bool((out[0][0] == 0).all())
