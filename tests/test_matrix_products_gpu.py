@@ -212,3 +212,168 @@ def test_ends_of_the_norms_range(shape):
             base.close(out[0][0], *base.allowed(u[0][0], eps=eps))
         else:
             assert bool((out[0][0] == 0).all())
+
+
+# ---- every element of orthogonalised updates ---------------------------------------------------------
+def definition(u, steps=base.DEFAULT, eps=1e-7, rounded=False):
+    """Of matrices [count, rows, columns] in 64 bits; `rounded`: with what the grouped kernels round to fp16 rounded there."""
+    x = u.double()
+    x = x / (x.square().sum((1, 2), keepdim=True).sqrt() + eps)
+    tall = x.shape[1] > x.shape[2]
+    x = x.mT if tall else x
+    half = (lambda v, unit=256.0: (v * unit).half().double() / unit) if rounded else lambda v: v
+    one = torch.eye(x.shape[1], dtype=torch.float64, device=x.device)
+    for k, (a, b, c) in enumerate(steps):
+        hi = half(x)
+        rest = half((x - hi) * 2048.0) / 2048.0 if rounded and k + 1 < len(steps) else torch.zeros_like(x)
+        gram = half(hi @ hi.mT)
+        x = half(a * one + b * gram + c * (gram @ gram)) @ hi + a * rest
+    return x.mT if tall else x
+
+
+def elements(got, u, dst, factor=1.0, steps=base.DEFAULT, eps=1e-7):
+    """[count, rows, columns] of results, each element for itself.  An element's error is the sum of thousands of independent roundings, near normal, and the emulation's errors are
+    another draw of the same: of a million such values none is beyond eight times their root mean square, and the kernels' is at most twice the emulation's (sums in fp32,
+    cut off, beside fp16's roundings).  The result's own rounding on top."""
+    want = definition(u, steps, eps)
+    error = definition(u, steps, eps, True) - want
+    rms = error.square().mean((1, 2), keepdim=True).sqrt()
+    want = want * factor
+    tol = 16 * rms * factor + base.HALF[dst] * want.abs() + 8 * base.U * want.abs()
+    assert bool(torch.isfinite(got).all())
+    over = (got.double() - want).abs() - tol
+    assert float(over.max()) <= 0, f"off by {float(over.max()):.3e} more than allowed, {float(tol.max()):.3e}"
+    # (a row or an element of zeros, or of another place, would be far outside)
+    assert float((want.abs() > 3 * tol).double().mean()) > 0.8
+
+
+def placed(t, shift):
+    """The same values `shift` elements off a boundary of 16 bytes."""
+    buf = torch.empty(t.numel() + 8, dtype=t.dtype, device="cuda")[shift:shift + t.numel()].view(t.shape)
+    return buf.copy_(t)
+
+
+LARGE = [(300, 200), (576, 192), (200, 301), (131, 130), (257, 129), (160, 600)]
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("grad", [None, "bf16", "f32"])
+@pytest.mark.parametrize("src,dst", [("f32", "bf16"), ("bf16", "f32"), ("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("scale", ["aspect", "rms"])
+def test_every_element_of_larger_matrices(src, dst, grad, scale, shift):
+    """Both sides above what a block takes alone: with and without the look-ahead, of all types, on and off boundaries, scaled, into another tensor and in place."""
+    M = 2
+    opt = base.context(M, LARGE, grad or "bf16", beta1=0.9)
+    S, D = base.TYPE[src], base.TYPE[dst]
+    at = lambda lists: [[placed(t, shift) for t in row] for row in lists]
+    u = at(base.matrices(M, LARGE, 1, S))
+    g = at(base.matrices(M, LARGE, 2, base.TYPE[grad])) if grad else None
+    out = at([[torch.empty(s, dtype=D, device="cuda") for s in LARGE] for _ in range(M)])
+    opt.orthogonalize(range(len(LARGE)), u, grads=g, out=out, scale=scale)
+    beta = torch.tensor(0.9)
+    for k, (r, c) in enumerate(LARGE):
+        ahead = torch.stack([row[k] for row in u])
+        if grad:     # (formed in fp32, as the kernels do: two roundings next to fp16's are none)
+            ahead = float(beta) * ahead.double() + (1 - float(beta)) * torch.stack([row[k] for row in g]).double()
+        factor = max(1.0, r / c) ** 0.5 if scale == "aspect" else 0.2 * max(r, c) ** 0.5
+        elements(torch.stack([row[k] for row in out]), ahead, D, factor)
+    if src == dst:
+        opt.orthogonalize(range(len(LARGE)), u, grads=g, scale=scale)
+        assert all(torch.equal(p, q) for r, s in zip(u, out) for p, q in zip(r, s))
+    if grad == dst:      # in the place of the gradients
+        u = at(base.matrices(M, LARGE, 1, S))
+        opt.orthogonalize(range(len(LARGE)), u, grads=g, out=g, scale=scale)
+        assert all(torch.equal(p, q) for r, s in zip(g, out) for p, q in zip(r, s))
+
+
+@pytest.mark.parametrize("shift", [0, 3])
+@pytest.mark.parametrize("grad", [None, "bf16"])
+def test_every_element_of_a_step(grad, shift):
+    M, shapes, lr, decay = 2, LARGE + [(40, 96), (96, 40), (23, 61)], 0.05, 0.1
+    x = [[placed(torch.randn(s, generator=base.gen_of(9 + m), device="cuda") * 0.02, shift) for s in shapes] for m in range(M)]
+    u = base.matrices(M, shapes, 6)
+    g = base.matrices(M, shapes, 7, BF) if grad else None
+    before = [[t.double() for t in row] for row in x]
+    opt = base.context(M, shapes, x=x, u=u, weight_decay=decay, beta1=0.9)
+    opt.orthogonal_step(range(len(shapes)), lr, grads=g, scale="aspect")
+    lr, decay, beta = float(torch.tensor(lr)), float(torch.tensor(decay)), float(torch.tensor(0.9))
+    for k, (r, c) in enumerate(shapes):
+        ahead = torch.stack([row[k] for row in u]).double()
+        if grad:
+            ahead = beta * ahead + (1 - beta) * torch.stack([row[k] for row in g]).double()
+        was, now = torch.stack([row[k] for row in before]), torch.stack([row[k] for row in x]).double()
+        f = lr * max(1.0, r / c) ** 0.5
+        want = definition(ahead)
+        rms = (definition(ahead, rounded=True) - want).square().mean((1, 2), keepdim=True).sqrt()
+        total = was * (1 - lr * decay) - f * want
+        over = (now - total).abs() - (16 * rms * f + 4 * base.U * (was.abs() + f * want.abs()))
+        assert float(over.max()) <= 0, f"{(r, c)}: off by {float(over.max()):.3e} more than allowed"
+
+
+def test_more_matrices_than_a_round_and_more_shapes_than_a_launch():
+    """660 matrices, none for a block alone: 21 shapes (a launch takes 16), 600 matrices of one (a round takes 512).  Each of them against the definition; the same bits in another order."""
+    M = 3
+    shapes = [(129 + 5 * k, 131 + (k * 37) % 120) for k in range(20)] + [(130, 133)] * 200
+    opt = base.context(M, shapes)
+    u = base.matrices(M, shapes, 7)
+    out, again = ([[torch.zeros(s, device="cuda") for s in shapes] for _ in range(M)] for _ in range(2))
+    opt.orthogonalize(range(len(shapes)), u, out=out)
+    opt.orthogonalize(list(range(len(shapes)))[::-1], u, out=again)
+    assert all(torch.equal(p, q) for r, s in zip(out, again) for p, q in zip(r, s))
+    for k in range(20):
+        elements(torch.stack([row[k] for row in out]), torch.stack([row[k] for row in u]), F32)
+    for m in range(M):
+        elements(torch.stack(out[m][20:]), torch.stack(u[m][20:]), F32)
+
+
+def test_more_than_a_rounds_bytes():
+    """2.6 GB of working memory, of which a round takes 2: the second round's matrices use the first one's memory again, and one of the shapes is cut in two."""
+    shapes = [(4096, 2048)] * 13 + [(2048, 4090)] * 29
+    opt = base.context(1, shapes)
+    u = base.matrices(1, shapes, 8)
+    out = [[torch.zeros(s, dtype=BF, device="cuda") for s in shapes]]
+    steps = base.DEFAULT[:2]
+    opt.orthogonalize(range(len(shapes)), u, out=out, coefficients=steps)
+    for k in range(len(shapes)):
+        elements(out[0][k][None], u[0][k][None], BF, steps=steps)
+
+
+# ---- matrices that a block takes alone ---------------------------------------------------------------
+def by_pairs(u, steps=base.DEFAULT, eps=1e-7, terms=(1, 1), lo_of="XGP", cut=0.0):
+    """In 64 bits with every operand as two fp16 numbers and three products of them, as those matrices are multiplied.  terms, lo_of: with one of the products, or the smaller numbers
+    of X, G or the polynomial, left out.  cut: with sums cut off: an instruction adds sixteen products to an fp32 accumulator, off by four units of 2^-24 of the
+    magnitudes at most, all in the same direction at worst."""
+    x = u.double()
+    x = x / (x.norm() + eps)
+    tall = x.shape[0] > x.shape[1]
+    x = x.mT if tall else x
+    one = torch.eye(x.shape[0], dtype=torch.float64, device=x.device)
+
+    def two(v, name):
+        hi = (v * 1024.0).half().double()
+        return hi / 1024.0, (v * 1024.0 - hi).half().double() / 1024.0 * (name in lo_of)
+
+    def product(a, b):
+        total = a[0] @ b[0] + terms[0] * (a[0] @ b[1]) + terms[1] * (a[1] @ b[0])
+        return total - torch.sign(total) * cut * 12 * -(-a[0].shape[1] // 16) * base.U * (a[0].abs() @ b[0].abs())
+
+    for a, b, c in steps:
+        X = two(x, "X")
+        G = two(product(X, [t.mT for t in X]), "G")
+        x = product(two(a * one + b * (G[0] + G[1]) + c * product(G, [t.mT for t in G]), "P"), X)
+    return x.mT if tall else x
+
+
+@pytest.mark.parametrize("shape", [(1, 5), (8, 8), (24, 72), (64, 64), (72, 72), (200, 72), (128, 128), (128, 250)])
+def test_small_matrices_are_as_exact_as_pairs_of_numbers(shape):
+    """fp32 results; 2^-20 of the norm stands for the roundings to fp32 between the products.  Without any one of the products or of the smaller numbers a result would be outside."""
+    opt = base.context(1, [shape])
+    u, out = base.matrices(1, [shape], 3), [[torch.empty(shape, device="cuda")]]
+    opt.orthogonalize([0], u, out=out)
+    u, want = u[0][0], base.newton_schulz(u[0][0])
+    pairs = by_pairs(u)
+    bound = 2 * float((pairs - want).norm()) + float((by_pairs(u, cut=1.0) - pairs).norm()) + 2.0 ** -20 * float(want.norm())
+    base.close(out[0][0], want, bound)
+    if shape != (1, 5):
+        for less in (dict(terms=(0, 1)), dict(terms=(1, 0)), dict(lo_of="GP"), dict(lo_of="XP"), dict(lo_of="XG")):
+            assert float((by_pairs(u, **less) - want).norm()) > bound
