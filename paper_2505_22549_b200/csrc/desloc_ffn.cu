@@ -8,7 +8,7 @@ namespace desloc {
 
 namespace {
 
-// (a few units of fp32's last place: the results are rounded to bf16)
+// (Off by 2 + 1.2 |x| units of fp32's last place for the exponential, two for the quotient: 2^-20 near 0, 2^-16 at |x| = 80; the results are rounded to bf16, 2^-8.)
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
 
 // ---- forward -----------------------------------------------------------------------------------------
@@ -183,7 +183,10 @@ struct DzEpilogue {
 // ---- single tokens -----------------------------------------------------------------------------------
 // Up to FFN_FEW tokens of a worker: a warp for each row of the weights, which it reads from one end to the other.  Bound: HBM, the weights once.  (Tiles of the tensor cores
 // bring 128 bytes of many rows at a time, for which memory is slower.  Four workers, one token, width 2048, hidden 8192, 403 MB: 67 us, 6.0 TB/s, 0.92 of copy; by tiles
-// 100 us.)  Sums in fp32, lanes' sums in a fixed order.
+// 92 us.)  Sums in fp32, lanes' sums in a fixed order.
+// Tiles take the same for 1 to 64 tokens, rows longer with each (every warp reads the tokens' values again).  Rows at 1 / 2 / 3 / 4 / 5 / 8 tokens against tiles: four workers, 2048 x
+// 8192, 68 / 78 / 83 / 99 / 125 / 188 us against 92; eight, 960 x 2560, 25 / 30 / 34 / 40 / 50 / 75 against 38; four, 576 x 1536, 9 / 10 / 11 / 13 / 15 / 22 against 23.  So at four
+// tokens rows lose 5 to 8 % in large blocks and win 44 % in small ones; at five they lose a third in large ones.
 constexpr int FFN_FEW = 4, FEW_THREADS = 256, FEW_AHEAD = 4;
 
 // Sums of a row of w (and, where W = 2, of a second one) times T rows of x, of which the next one is x_ld further on.
@@ -420,7 +423,9 @@ cudaError_t pack(Operand &o, int M, long long s0, long long s1, Bump &bump, cuda
 }
 
 // Results leave as boxes where emptying a tile takes longer than its products, in which the copy engine has more to do: products of up to BOXES_K (8192 x 576 x 1536 by four
-// workers 173 us instead of 194; 2048 x 2048 x 8192 304 us instead of 293).
+// workers 173 us instead of 194; 2048 x 2048 x 8192 304 us instead of 293).  The whole way back with / without them, four workers, two runs each, us: 8192 tokens of width 576 419, 419 /
+// 440, 445; 4096 of 768 299, 299 / 310, 312; of 960 464, 474 / 479, 480; of 1024 720, 740 / 748, 862; of 1280 886, 787 / 796, 867; 2048 of 1536 519, 524 / 526, 526; of 2048 1407,
+// 1409 / 1361, 1423: beyond 1024 no difference that lasts.  The way forward takes 0 to 2 % longer with boxes at all of these.
 constexpr int BOXES_K = 1024;
 constexpr int WORKERS = 16;   // of a launch: three groups and two maps each at most
 

@@ -97,8 +97,8 @@ struct __align__(16) Chunk {
 };
 
 // Programmatic dependent launch.  Every kernel here is launched so that it may begin while the kernel in
-// front of it in the stream is still running: each block tells the next kernel at once that it may come
-// (its blocks move in as the last ones of this kernel leave), does what depends on no earlier kernel --
+// front of it in the stream is still running: each block tells the next kernel at once (one that takes TMEM: as soon
+// as it has it) that it may come (its blocks move in as the last ones of this kernel leave), does what depends on no earlier kernel --
 // barriers, look-ups in tables that only copies write -- and then waits until everything in front
 // of it is complete and visible.  No state, gradient, scale factor or partial sum is touched
 // before that.  The wait is the launch's own dependency, resolved by the hardware, not a poll.
