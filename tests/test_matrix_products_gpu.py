@@ -377,3 +377,132 @@ def test_small_matrices_are_as_exact_as_pairs_of_numbers(shape):
     if shape != (1, 5):
         for less in (dict(terms=(0, 1)), dict(terms=(1, 0)), dict(lo_of="GP"), dict(lo_of="XP"), dict(lo_of="XG")):
             assert float((by_pairs(u, **less) - want).norm()) > bound
+
+
+# ---- the block in calls of other kinds ---------------------------------------------------------------
+def all_of_it(b, M):
+    """y, kept, dh and the weights' gradients of a block against the definition."""
+    (g, u, y), tols = b.forward(b.h)
+    got, kept = b.opt.gated_ffn(b.TENSORS, b.h, b.weights, keep=True)
+    for have, want, tol in zip((*kept, got), (g, u, y), tols):
+        base.check(have, want, tol)
+    grads = [[torch.zeros(s, dtype=BF, device="cuda") for s in ((b.F, b.D), (b.D, b.F), (5,), (b.F, b.D))] for _ in range(M)]
+    dh = b.opt.gated_ffn_grad(b.TENSORS, b.h, kept, b.dy, b.weights, grads)
+    (want, tol), *weights = b.backward(b.h, *kept, b.dy)
+    base.check(dh, want, tol + base.HB * (want.abs() + tol) + 1e-30)
+    for k, (want, tol) in zip(b.TENSORS, weights):
+        for m in range(M):
+            base.check(grads[m][k], want[m], tol[m] + (base.HB + 2 * base.U) * (want[m].abs() + tol[m]) + 1e-30)
+
+
+@pytest.mark.parametrize("M,T,D,F,shift", [(70, 6, 15, 23, 1), (70, 2, 16, 24, 1), (130, 9, 8, 16, 3), (256, 5, 8, 8, 0), (18, 40, 72, 200, 4)])
+def test_more_workers_than_a_launch_with_weights_off_boundaries(M, T, D, F, shift):
+    all_of_it(base.Block(M, T, D, F, shift=shift), M)
+
+
+@pytest.mark.parametrize("off", [(0, 1, 0), (1, 0, 0), (0, 0, 1), (1, 1, 0), (1, 0, 1)])
+@pytest.mark.parametrize("M,T", [(2, 50), (18, 7)])
+def test_some_weights_on_and_some_off_boundaries(M, T, off):
+    b = base.Block(M, T, 40, 72)
+    for k, shift in zip(b.TENSORS, off):
+        for row in b.weights[1:]:        # (the first worker's lie well)
+            row[k] = placed(row[k], shift)
+    all_of_it(b, M)
+
+
+def test_after_the_workers_have_changed():
+    b = base.Block(2, 30, 40, 72)
+    want = b.opt.gated_ffn(b.TENSORS, b.h, b.weights)
+    shapes = ((72, 40), (40, 72), (5,), (72, 40))
+    x, u = ([[torch.zeros(s, device="cuda") for s in shapes] for _ in range(3)] for _ in range(2))
+    keep = b.opt._keep
+    b.opt.set_workers([keep[0][0], keep[0][1], x[2]], [keep[1][0], keep[1][1], u[2]], None, 2)
+    h = torch.cat([b.h, b.h[:1]])
+    y = b.opt.gated_ffn(b.TENSORS, h, b.weights + [b.weights[0]])
+    assert torch.equal(y[:2], want) and torch.equal(y[2], want[0])
+    with pytest.raises(ValueError):
+        b.opt.gated_ffn(b.TENSORS, b.h, b.weights)
+    new = base.matrices(3, [(72, 40), (40, 72), (5, 1), (72, 40)], 4)
+    for row, values in zip(b.opt._keep[1], new):
+        for t, v in zip(row, values):
+            t.copy_(v.view(t.shape))
+    before = [[t.double() for t in row] for row in b.opt._keep[0]]
+    b.opt.orthogonal_step([0, 1], 0.01, scale="none")
+    for m in range(3):
+        for k in (0, 1):
+            want, off = base.allowed(new[m][k])
+            rate = float(torch.tensor(0.01))
+            base.close(b.opt._keep[0][m][k], before[m][k] - rate * want, rate * off + 4 * base.U * float(want.norm()))
+    # the momentum's addresses are the new ones
+    how = B.orthogonal([0, 1], [40, 72])
+    rows = b.opt._keep[1]
+    go = lambda out: B.raw_lib().desloc_orthogonalize(b.opt.ctx, how, d.DESLOC_F32, addresses(out), None, 0, None)
+    assert go(rows) == d.DESLOC_E_NULL and go([rows[0], rows[2], rows[1]]) == d.DESLOC_E_INVALID
+
+
+def test_one_weight_in_several_places():
+    """gate and up the same tensor; one set of weights for all workers."""
+    b = base.Block(3, 33, 40, 72)
+    row = list(b.weights[0])
+    row[b.TENSORS[1]] = row[b.TENSORS[0]]
+    b.weights = [row] * 3
+    b.gate, b.up, b.down = (torch.stack([r[k] for r in b.weights]).double() for k in b.TENSORS)
+    all_of_it(b, 3)
+
+
+def test_contexts_of_two_threads():
+    """Each with its own context and stream, calls at the same time: what launches are made of is a thread's own."""
+    import threading
+    blocks = [base.Block(2, 200 + 60 * k, 64 + 8 * k, 256, seed=k) for k in range(2)]
+    shapes = [[(300, 200), (64, 40)], [(200, 301), (24, 72)]]
+    opts, us = [base.context(2, s) for s in shapes], [base.matrices(2, s, 5 + k) for k, s in enumerate(shapes)]
+    outs = [[[torch.empty(s, device="cuda") for s in row] for _ in range(2)] for row in shapes]
+    wants = []
+    for k in range(2):
+        opts[k].orthogonalize([0, 1], us[k], out=outs[k])
+        wants.append([blocks[k].opt.gated_ffn(blocks[k].TENSORS, blocks[k].h, blocks[k].weights)] + [t.clone() for row in outs[k] for t in row])
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(60):
+                    y = blocks[k].opt.gated_ffn(blocks[k].TENSORS, blocks[k].h, blocks[k].weights)
+                    opts[k].orthogonalize([0, 1], us[k], out=outs[k])
+                    got = [y] + [t for row in outs[k] for t in row]
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(p, q) for p, q in zip(got, wants[k])):
+                        failed.append(k)
+                    torch.cuda.current_stream().synchronize()
+        except Exception as e:     # noqa: BLE001 (told to the test below)
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed
+
+
+def test_as_many_tokens_as_there_may_be():
+    """2^24 of one worker: sums of the weights' gradients over 262144 boxes, gradients of the first and last tokens alone."""
+    T, D, F, few = 1 << 24, 8, 16, 8
+    b = base.Block(1, T, D, F)
+    ends = lambda t: torch.cat([t[:, :few], t[:, -few:]], 1)
+    y, kept = b.opt.gated_ffn(b.TENSORS, b.h, b.weights, keep=True)
+    want, tol = b.forward(ends(b.h))
+    for got, w, t in zip((*kept, y), want, tol):
+        base.check(ends(got), w, t)
+    b.dy[:, few:-few] = 0
+    grads = [[torch.zeros(s, dtype=BF, device="cuda") for s in ((F, D), (D, F), (5,), (F, D))]]
+    dh = b.opt.gated_ffn_grad(b.TENSORS, b.h, kept, b.dy, b.weights, grads)
+    (want, tol), *weights = b.backward(ends(b.h), *map(ends, kept), ends(b.dy))
+    base.check(ends(dh), want, tol + base.HB * (want.abs() + tol) + 1e-30)
+    for k, (want, tol) in zip(b.TENSORS, weights):
+        base.check(grads[0][k], want[0], tol[0] + (base.HB + 2 * base.U) * (want[0].abs() + tol[0]) + 1e-30)
+    b.opt.gated_ffn(b.TENSORS, b.h[:, :4], b.weights)      # (refused where a wait had run out)
+    with pytest.raises(d.DeslocError) as e:
+        b.opt.gated_ffn(b.TENSORS, b.h.new_empty(1, T + 1, D), b.weights)
+    assert e.value.status == d.DESLOC_E_RANGE
